@@ -39,7 +39,9 @@ typedef enum {
     QUARTZ_ERR_UNSUPPORTED = 3,   /* valid per the paper but not built (e.g. group_q != 64) */
     QUARTZ_ERR_CUDA = 4,          /* a CUDA runtime / driver call failed */
     QUARTZ_ERR_TIMEOUT = 5,       /* a kernel's bounded wait expired (reported by quartz_device_status) */
-    QUARTZ_ERR_WORKSPACE = 6      /* workspace missing or smaller than quartz_linear_workspace_size */
+    QUARTZ_ERR_WORKSPACE = 6,     /* workspace missing or smaller than its size function says */
+    QUARTZ_ERR_INDEX = 7          /* a page, slot, length or kept index read on the device was out of
+                                   * range (reported by quartz_device_status) */
 } quartz_status_t;
 
 /* Eq. 1 conventions.  The paper's printed Eq. 1 (s = (max-min)/255, clamp to
@@ -348,10 +350,144 @@ int32_t quartz_attention_decode(const quartz_encoded_t *q, const quartz_encoded_
                                 const quartz_encoded_t *v_cache, int64_t L_max, int64_t L, float scale, void *o,
                                 int32_t o_type, void *workspace, size_t workspace_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Paged key / value cache.  The paper has no counterpart to these entry
+ * points: they serve sequences of different lengths, with grouped query heads
+ * and rotary positions, over a cache whose tokens sit in pages of a common
+ * pool, in 16 bits or QuaRTZ-encoded (Eq. 1 + Eq. 2 along the head dimension).
+ *
+ * Token t of sequence b is slot t % page_size of page
+ * block_table[b, t / page_size].  Pages may be shared between sequences for
+ * attention; pages that are written belong to one sequence.  Page numbers,
+ * lengths, slots and kept indices live on the device and are checked there:
+ * one out of range is not followed (the token is skipped, or read from page 0,
+ * or the length is cut) and quartz_device_status then returns
+ * QUARTZ_ERR_INDEX; results of that sequence are undefined.
+ * ------------------------------------------------------------------------- */
+
+typedef enum { QUARTZ_PAGES_F16 = 0, QUARTZ_PAGES_BF16 = 1, QUARTZ_PAGES_ENCODED = 2 } quartz_pages_type_t;
+
+/* One side (keys or values) of a paged cache.
+ *   16-bit pages:  element (page, slot, head, d) at data[page * stride_page +
+ *                  slot * stride_slot + head * stride_head + d]; data 16-byte
+ *                  aligned, strides in elements, multiples of 8 in [0, 2^31)
+ *   encoded pages: `enc`, num_pages * heads * page_size rows of dim columns,
+ *                  token (page, head, slot) in row (page * heads + head) *
+ *                  page_size + slot; group_q 64, SYMMETRIC, 8-bit codes, one
+ *                  FLAG byte per subgroup, any G_s (the same for both sides) */
+typedef struct {
+    void *data;
+    int64_t stride_page, stride_slot, stride_head;
+    quartz_encoded_t enc;
+} quartz_pages_t;
+
+typedef struct {
+    int32_t type;       /* quartz_pages_type_t */
+    int32_t page_size;  /* a power of two, 1 .. 4096 */
+    int32_t heads;      /* key / value heads, 1 .. 1024 */
+    int32_t dim;        /* head dimension: 64, 128, 192 or 256 */
+    int64_t num_pages;  /* 1 .. 2^31 - 1 */
+    quartz_pages_t k, v;
+} quartz_paged_cache_t;
+
+/* Rotary positions: pair i of a head's first `rotary` elements is turned by
+ * positions[t] * freqs[i] radians,
+ *   y1 = scale (x1 cos - x2 sin),  y2 = scale (x1 sin + x2 cos),
+ * (x1, x2) = elements (i, i + rotary/2), or (2i, 2i + 1) with `interleaved`.
+ * The angle is reduced exactly (positions times freqs / 2 pi as a 64-bit
+ * fraction of a turn), so far positions lose nothing.  `backward` applies the
+ * transpose, which is the gradient with respect to x. */
+typedef struct {
+    const int64_t *positions;  /* device, one per token */
+    const double *freqs;       /* device, [rotary / 2], radians per position, finite */
+    int32_t rotary;            /* even, 2 .. min(dim, 512) */
+    int32_t interleaved;       /* 0 or 1 */
+    int32_t backward;          /* 0 or 1 */
+    float scale;               /* on cosine and sine (1; the attention factor of some long-context scalings) */
+} quartz_rope_t;
+
+/* Rotate x [tokens, heads, dim] of `type` (quartz_out_t) into y of the same
+ * type, in binary32, rounded once; elements from `rotary` on are copied.
+ * Strides in elements: x[t * x_stride_token + h * x_stride_head + d], y alike.
+ * y == x with equal strides works in place; other overlaps are undefined.
+ * dim 2 .. 1024; any alignment of the type itself. */
+int32_t quartz_rope(const void *x, int64_t x_stride_token, int64_t x_stride_head, void *y, int64_t y_stride_token,
+                    int64_t y_stride_head, int32_t type, int64_t tokens, int32_t heads, int32_t dim,
+                    const quartz_rope_t *rope, void *stream);
+
+/* Write the keys and values of `tokens` new tokens into their slots
+ * (slots[t] = page * page_size + slot; negative: the token is skipped).  k and
+ * v are [tokens, heads, dim] in the pages' type (fp16 for encoded pages),
+ * k[t * k_stride_token + h * k_stride_head + d], 16-byte aligned, strides
+ * multiples of 8.  With `rope` (NULL: none) k is rotated first, the same
+ * values as quartz_rope gives; encoded pages get the arithmetic of
+ * quartz_quantize.  The slots of one call are distinct. */
+int32_t quartz_paged_append(const quartz_paged_cache_t *cache, const void *k, int64_t k_stride_token,
+                            int64_t k_stride_head, const void *v, int64_t v_stride_token, int64_t v_stride_head,
+                            int64_t tokens, const int64_t *slots, const quartz_rope_t *rope, void *stream);
+
+/* Attention of one new token per sequence:
+ *   s_t = scale * q . k_t,  p = softmax(s) over the tokens max(0, len -
+ *   window) <= t < len (window 0: all),  o = sum_t p_t v_t
+ * for each of q_heads query heads; query head h reads key / value head
+ * h / (q_heads / heads).  An empty sequence gives zeros.  Products, softmax
+ * and sums in binary32; the weights p enter the value product as a sum of two
+ * 16-bit parts.
+ *   q            [seqs, q_heads, dim], strides in elements (multiples of 8),
+ *                16-byte aligned, the pages' type (fp16 for encoded pages)
+ *   block_table  int32 [seqs, >= ceil(max_len / page_size)], row stride
+ *                table_stride; places past a sequence's length are not read
+ *   seq_lens     int32 [seqs], 0 <= len <= max_len
+ *   o            [seqs, q_heads, dim] contiguous, o_type (quartz_out_t),
+ *                16-byte aligned
+ *   weights      NULL, or fp32 sums of attention weights,
+ *                weights[b * weights_stride_seq + h * weights_stride_head + t]
+ *                per key / value head: each gets the sum of p_t over its query
+ *                heads added for the tokens attended (no two places alike)
+ *   workspace    >= quartz_paged_attention_workspace_size bytes, 16-byte
+ *                aligned, scratch
+ * seqs <= 65535. */
+size_t quartz_paged_attention_workspace_size(const quartz_paged_cache_t *cache, int64_t seqs, int32_t q_heads,
+                                             int64_t max_len, int64_t window, int32_t with_weights);
+int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_stride_head, int64_t seqs,
+                               int32_t q_heads, const quartz_paged_cache_t *cache, const int32_t *block_table,
+                               int64_t table_stride, const int32_t *seq_lens, int64_t max_len, int64_t window,
+                               float scale, void *o, int32_t o_type, float *weights, int64_t weights_stride_seq,
+                               int64_t weights_stride_head, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Choose the tokens that stay in each key / value head's cache: all of them
+ * while len <= budget; else the first `sinks`, the last `recent`, and of those
+ * between the budget - sinks - recent with the largest weights (equal weights:
+ * the lowest index; -0 equals 0; NaN counts below everything).
+ *   weights   fp32 [seqs, heads, >= max_len] with strides, as above
+ *   kept      int32 [seqs, heads, budget]: the kept indices, ascending, then -1
+ *   new_lens  int32 [seqs]: min(len, budget)
+ * sinks, recent >= 0, 1 <= budget, sinks + recent <= budget, max_len < 2^31,
+ * seqs * heads < 2^31, seqs <= 65535. */
+int32_t quartz_evict_select(const float *weights, int64_t weights_stride_seq, int64_t weights_stride_head,
+                            const int32_t *seq_lens, int64_t seqs, int32_t heads, int64_t max_len, int64_t budget,
+                            int64_t recent, int64_t sinks, int32_t *kept, int32_t *new_lens, void *stream);
+
+/* Close up a cache after quartz_evict_select: row j of each sequence and head
+ * becomes its row kept[b, h, j] (j < min(len, budget)), keys and values.
+ *   new_table  NULL: in place, in the pages of block_table; the table's pages
+ *              then belong to one sequence each.  Else the rows go to the
+ *              pages of new_table (row stride new_table_stride, >=
+ *              ceil(budget / page_size) wide), none of which is a page of
+ *              block_table, and the old pages stay as they were.
+ *   max_len    seq_lens are at most this (block_table covers it)
+ *   weights    NULL, or the sums of quartz_paged_attention: closed up in place
+ *              alike, and 0 from the new length to the old */
+int32_t quartz_cache_compact(const quartz_paged_cache_t *cache, int64_t seqs, const int32_t *block_table,
+                             int64_t table_stride, const int32_t *new_table, int64_t new_table_stride,
+                             const int32_t *seq_lens, int64_t max_len, const int32_t *kept, int64_t budget,
+                             float *weights, int64_t weights_stride_seq, int64_t weights_stride_head, void *stream);
+
 /* Synchronise `stream`, then read and clear the library's device error word.
  * Returns QUARTZ_OK, QUARTZ_ERR_TIMEOUT if a kernel gave up on a bounded
- * wait since the last call (its outputs are then invalid), or
- * QUARTZ_ERR_CUDA if the stream reports an error. */
+ * wait since the last call (its outputs are then invalid), QUARTZ_ERR_INDEX
+ * if one met an index out of range (paged cache), or QUARTZ_ERR_CUDA if the
+ * stream reports an error. */
 int32_t quartz_device_status(void *stream);
 
 /* Failure-detection self-test: launches one CTA that waits on an mbarrier

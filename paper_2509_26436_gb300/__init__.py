@@ -25,6 +25,8 @@ from ._native import (ALGO_SHIFT, ALGO_SIMT, ALGO_TCGEN05, ASYMMETRIC, OUT_BF16,
 __all__ = ["Params", "Encoded", "quantize", "encode_weights", "dequantize", "linear",
            "linear_workspace_size", "empty_encoded", "device_status", "selftest_timeout",
            "kv_append", "attention_decode", "attention_workspace_size", "prepare_weights",
+           "rope_frequencies", "rope", "PagedCache", "empty_paged_cache", "paged_append",
+           "attention_paged", "evict_select", "cache_compact",
            "SYMMETRIC", "ASYMMETRIC", "QuartzError"]
 
 
@@ -363,3 +365,9 @@ def attention_decode(q: Encoded, k_cache: Encoded, v_cache: Encoded, L_max: int,
                                              workspace.numel() * workspace.element_size(), _stream(stream)),
             "quartz_attention_decode")
     return o
+
+
+# --- paged key / value cache (no counterpart in the paper) -------------------
+
+from .paged import (PagedCache, attention_paged, attention_paged_workspace_size, cache_compact, empty_paged_cache, evict_select,  # noqa: E402
+                    paged_append, rope, rope_frequencies)  # noqa: E402

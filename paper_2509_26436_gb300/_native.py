@@ -18,6 +18,7 @@ QUARTZ_ERR_UNSUPPORTED = 3
 QUARTZ_ERR_CUDA = 4
 QUARTZ_ERR_TIMEOUT = 5
 QUARTZ_ERR_WORKSPACE = 6
+QUARTZ_ERR_INDEX = 7
 
 SYMMETRIC = 0
 ASYMMETRIC = 1
@@ -25,6 +26,10 @@ ASYMMETRIC = 1
 OUT_F16 = 0
 OUT_BF16 = 1
 OUT_F32 = 2
+
+PAGES_F16 = 0
+PAGES_BF16 = 1
+PAGES_ENCODED = 2
 
 ALGO_TCGEN05 = 0
 ALGO_SIMT = 1
@@ -50,6 +55,21 @@ class QuartzEncoded(C.Structure):
 class QuartzLinearOpts(C.Structure):
     _fields_ = [("partials", _P), ("partials_group", C.c_int32), ("algo", C.c_int32),
                 ("gemm_event_begin", _P), ("gemm_event_end", _P), ("w_prepared", _P)]
+
+
+class QuartzPages(C.Structure):
+    _fields_ = [("data", _P), ("stride_page", C.c_int64), ("stride_slot", C.c_int64), ("stride_head", C.c_int64),
+                ("enc", QuartzEncoded)]
+
+
+class QuartzPagedCache(C.Structure):
+    _fields_ = [("type", C.c_int32), ("page_size", C.c_int32), ("heads", C.c_int32), ("dim", C.c_int32),
+                ("num_pages", C.c_int64), ("k", QuartzPages), ("v", QuartzPages)]
+
+
+class QuartzRope(C.Structure):
+    _fields_ = [("positions", _P), ("freqs", _P), ("rotary", C.c_int32), ("interleaved", C.c_int32),
+                ("backward", C.c_int32), ("scale", C.c_float)]
 
 
 SIGNATURES = {
@@ -79,6 +99,15 @@ SIGNATURES = {
     "quartz_attention_decode": (_I32, [C.POINTER(QuartzEncoded), C.POINTER(QuartzEncoded),
                                        C.POINTER(QuartzEncoded), _I64, _I64, C.c_float, _P, _I32, _P, _SZ,
                                        _P]),
+    "quartz_rope": (_I32, [_P, _I64, _I64, _P, _I64, _I64, _I32, _I64, _I32, _I32, C.POINTER(QuartzRope), _P]),
+    "quartz_paged_append": (_I32, [C.POINTER(QuartzPagedCache), _P, _I64, _I64, _P, _I64, _I64, _I64, _P,
+                                   C.POINTER(QuartzRope), _P]),
+    "quartz_paged_attention_workspace_size": (_SZ, [C.POINTER(QuartzPagedCache), _I64, _I32, _I64, _I64, _I32]),
+    "quartz_paged_attention": (_I32, [_P, _I64, _I64, _I64, _I32, C.POINTER(QuartzPagedCache), _P, _I64, _P, _I64,
+                                      _I64, C.c_float, _P, _I32, _P, _I64, _I64, _P, _SZ, _P]),
+    "quartz_evict_select": (_I32, [_P, _I64, _I64, _P, _I64, _I32, _I64, _I64, _I64, _I64, _P, _P, _P]),
+    "quartz_cache_compact": (_I32, [C.POINTER(QuartzPagedCache), _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P,
+                                    _I64, _I64, _P]),
     "quartz_device_status": (_I32, [_P]),
     "quartz_selftest_timeout": (_I32, [_I64, _P]),
     "quartz_probe_fp32_pipe": (_I32, [_I32, _I64, _P, _P]),

@@ -96,6 +96,7 @@ const char *quartz_status_string(int32_t status)
         case QUARTZ_ERR_CUDA: return "QUARTZ_ERR_CUDA";
         case QUARTZ_ERR_TIMEOUT: return "QUARTZ_ERR_TIMEOUT";
         case QUARTZ_ERR_WORKSPACE: return "QUARTZ_ERR_WORKSPACE";
+        case QUARTZ_ERR_INDEX: return "QUARTZ_ERR_INDEX";
         default: return "QUARTZ_ERR_UNKNOWN";
     }
 }
@@ -386,7 +387,7 @@ int32_t quartz_device_status(void *stream)
     const int zero = 0;
     if (cudaMemcpy(&v, p, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return QUARTZ_ERR_CUDA;
     if (cudaMemcpy(p, &zero, sizeof(int), cudaMemcpyHostToDevice) != cudaSuccess) return QUARTZ_ERR_CUDA;
-    return v == QUARTZ_DEV_TIMEOUT ? QUARTZ_ERR_TIMEOUT : QUARTZ_OK;
+    return v == QUARTZ_DEV_TIMEOUT ? QUARTZ_ERR_TIMEOUT : v == QUARTZ_DEV_INDEX ? QUARTZ_ERR_INDEX : QUARTZ_OK;
 }
 
 int32_t quartz_selftest_timeout(int64_t limit_ns, void *stream)

@@ -1,0 +1,280 @@
+// Attention of one new token over a paged cache: what the kernels for 16-bit
+// and for encoded pages share.
+//
+// A CTA takes one sequence, one key / value head, up to 8 of the query heads
+// that share it and one split (a run of consecutive tokens); its 4 warps take
+// tiles of 8 NT tokens in turn.  The products run on the warp-level tensor
+// instruction m16n8k16 with fp32 accumulators:
+//   S = Q K^T:  A rows 0-7 and again 8-15 = the query heads; B column n =
+//               token.  The order of the head dimension inside the
+//               contraction is free, so each lane loads 16 (or 8) consecutive
+//               bytes of its token's row straight into B fragments: keys need
+//               no shared memory, no transpose and no barrier.
+//   O += P V:   A rows 0-7 = the upper 16 bits of the softmax weights, rows
+//               8-15 = what is left of them, rounded again: the accumulator's
+//               lower half, added at the end, makes the weights good to twice
+//               the 16-bit type's precision, in rows that eight heads leave
+//               free anyway.  B column n = a piece of 8 (of each 64) head
+//               dimensions; its rows are tokens, so the four lanes of a column
+//               hold consecutive tokens and pair them with byte permutes.
+// The scores' accumulator layout is the weights' operand layout (lane = head
+// lane/4, tokens 2 NT (lane%4) ...), so the softmax stays in registers.
+// Legacy tensor instructions are enough here: the step is bound by HBM, the
+// tensor pipe has to keep up with one product pair per loaded row only.
+#pragma once
+
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "quartz_internal.h"
+
+namespace quartz {
+
+constexpr int kPagedWarps = 4;
+constexpr int kPagedThreads = kPagedWarps * 32;
+constexpr int kPagedHeads = 8;  // query heads per CTA
+constexpr float kPagedLog2e = 1.4426950408889634f;
+
+struct PagedSide {
+    const uint8_t *data;  // 16-bit pages
+    uint32_t stride_page, stride_slot;  // elements
+    int64_t stride_head;
+    const uint8_t *codes;  // encoded pages
+    const uint8_t *flags;
+    const __half *scales;
+};
+
+struct PagedArgs {
+    const uint16_t *q;
+    int64_t q_sb, q_sh;
+    const int32_t *table;
+    int64_t table_stride;
+    const int32_t *lens;
+    PagedSide k, v;
+    uint32_t num_pages;
+    int page_shift, kv_heads, group, head_blocks;  // query heads per key head; CTAs they take
+    int max_len, window, n_split, chunk;
+    float scale_log2;
+    float *part_o, *part_ml;  // [seqs * q_heads][n_split][dim], [..][2]; NULL: one split, o is written
+    float *lse;               // with scores: [seqs * q_heads], log2 domain
+    float *scores;            // NULL, or [seqs * q_heads][score_stride], log2 domain
+    int64_t score_stride;
+    void *o;
+    int o_type;
+    int *dev_err;
+};
+
+// The tokens a sequence's new token sees: [first, first + count).
+struct PagedRange {
+    int first, count;
+};
+
+__device__ __forceinline__ PagedRange paged_range(const int32_t *lens, int b, int max_len, int window, int *dev_err)
+{
+    int len = lens[b];
+    if (len < 0 || len > max_len) {
+        if (threadIdx.x == 0) atomicExch(dev_err, QUARTZ_DEV_INDEX);
+        len = len < 0 ? 0 : max_len;
+    }
+    PagedRange r;
+    r.first = window > 0 && len > window ? len - window : 0;
+    r.count = len - r.first;
+    return r;
+}
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel)
+{
+    uint32_t d;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
+    return d;
+}
+
+// d += A B, 16 x 8 x 16 (or 16 x 8 x 8 with one B register).
+template <bool BF>
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                      uint32_t b1)
+{
+    if (BF)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+template <bool BF>
+__device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0)
+{
+    if (BF)
+        asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(b0));
+    else
+        asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a0), "r"(a1), "r"(b0));
+}
+
+// Two weights as a 16-bit pair and the pair of what the rounding left.
+template <bool BF>
+__device__ __forceinline__ void split_pair(float p0, float p1, uint32_t &hi, uint32_t &lo)
+{
+    if (BF) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
+        hi = *reinterpret_cast<const uint32_t *>(&h);
+        const __nv_bfloat162 l = __floats2bfloat162_rn(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xFFFF0000u));
+        lo = *reinterpret_cast<const uint32_t *>(&l);
+    } else {
+        const __half2 h = __floats2half2_rn(p0, p1);
+        const float2 f = __half22float2(h);
+        const __half2 l = __floats2half2_rn(p0 - f.x, p1 - f.y);
+        hi = *reinterpret_cast<const uint32_t *>(&h);
+        lo = *reinterpret_cast<const uint32_t *>(&l);
+    }
+}
+
+// Running softmax of a warp over its tiles: m is its head's maximum (log2
+// domain), l this lane's part of the sum of weights.
+template <int D>
+struct PagedState {
+    float o[D / 8][4];
+    float m, l;
+
+    __device__ __forceinline__ void init()
+    {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+        m = -INFINITY;
+        l = 0.f;
+    }
+
+    // Scores sc (log2 domain, -inf where masked) to weights 2^(sc - m + up);
+    // `up` keeps small weights of a 16-bit type with few exponent bits normal.
+    template <int NT>
+    __device__ __forceinline__ void weigh(float (&sc)[NT][2], float up)
+    {
+        float mx = fmaxf(sc[0][0], sc[0][1]);
+        if (NT == 2) mx = fmaxf(mx, fmaxf(sc[NT - 1][0], sc[NT - 1][1]));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        if (__any_sync(0xffffffffu, mx > m)) {
+            const float m_new = fmaxf(m, mx), f = ex2(m - m_new);
+            m = m_new;
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[i][j] *= f;
+        }
+        const float off = up - m;
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            sc[i][0] = ex2(sc[i][0] + off);
+            sc[i][1] = ex2(sc[i][1] + off);
+            l += sc[i][0] + sc[i][1];
+        }
+    }
+};
+
+template <typename T> __device__ __forceinline__ void paged_store4(void *o, int64_t at, float4 v);
+template <> __device__ __forceinline__ void paged_store4<float>(void *o, int64_t at, float4 v)
+{
+    *reinterpret_cast<float4 *>(static_cast<float *>(o) + at) = v;
+}
+template <> __device__ __forceinline__ void paged_store4<__half>(void *o, int64_t at, float4 v)
+{
+    const __half2 a = __floats2half2_rn(v.x, v.y), b = __floats2half2_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(static_cast<__half *>(o) + at) =
+        make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+template <> __device__ __forceinline__ void paged_store4<__nv_bfloat16>(void *o, int64_t at, float4 v)
+{
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(static_cast<__nv_bfloat16 *>(o) + at) =
+        make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+__device__ __forceinline__ void paged_store4(void *o, int type, int64_t at, float4 v)
+{
+    if (type == QUARTZ_OUT_F16) paged_store4<__half>(o, at, v);
+    else if (type == QUARTZ_OUT_BF16) paged_store4<__nv_bfloat16>(o, at, v);
+    else paged_store4<float>(o, at, v);
+}
+
+// Join the warps of a CTA in a fixed order and write the split's result: the
+// output itself where there is one split, else o (relative to the split's
+// maximum) with maximum and sum.
+template <int D>
+struct PagedJoin {
+    static constexpr int kRow = D + 4;
+    float o[kPagedWarps][kPagedHeads][kRow];
+    float m[kPagedWarps][kPagedHeads], l[kPagedWarps][kPagedHeads];
+};
+
+template <int D>
+__device__ __forceinline__ void paged_finish(PagedJoin<D> &s, PagedState<D> &st, const PagedArgs &a, int b, int kv_head,
+                                             int head0, int split, float up)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
+    float l = st.l;
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    if (q == 0) s.m[warp][n] = st.m, s.l[warp][n] = l;
+#pragma unroll
+    for (int hv = 0; hv < D / 64; ++hv)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int j = 0; j < 8; j += 4) {
+                const float(*o)[4] = &st.o[hv * 8 + j];
+                *reinterpret_cast<float4 *>(&s.o[warp][n][hv * 64 + (2 * q + x) * 8 + j]) =
+                    make_float4(o[0][x] + o[0][x + 2], o[1][x] + o[1][x + 2], o[2][x] + o[2][x + 2], o[3][x] + o[3][x + 2]);
+            }
+    __syncthreads();
+    const int64_t row0 = (static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0;
+    for (int e = threadIdx.x; e < kPagedHeads * (D / 4); e += kPagedThreads) {
+        const int h = e / (D / 4), d = (e - h * (D / 4)) * 4;
+        if (head0 + h >= a.group) break;
+        float m = s.m[0][h];
+#pragma unroll
+        for (int w = 1; w < kPagedWarps; ++w) m = fmaxf(m, s.m[w][h]);
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kPagedWarps; ++w) {
+            const float f = m == -INFINITY ? 0.f : ex2(s.m[w][h] - m - up);
+            const float4 u = *reinterpret_cast<const float4 *>(&s.o[w][h][d]);
+            sum += f * s.l[w][h];
+            v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
+        }
+        const int64_t row = row0 + h;
+        if (a.part_o) {
+            const int64_t at = row * a.n_split + split;
+            *reinterpret_cast<float4 *>(a.part_o + at * D + d) = v;
+            if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, sum);
+        } else {
+            const float r = sum > 0.f ? 1.f / sum : 0.f;
+            paged_store4(a.o, a.o_type, row * D + d, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+            if (a.lse && d == 0) a.lse[row] = m + log2f(sum);
+        }
+    }
+}
+
+// CTAs resident per SM of the kernel that serves this cache.
+int paged_kernel_occupancy_16bit(int type, int dim);
+int paged_kernel_occupancy_encoded(int dim, int group_s);
+cudaError_t launch_paged_16bit(int type, int dim, const PagedArgs &a, dim3 grid, cudaStream_t s);
+cudaError_t launch_paged_encoded(int dim, int group_s, const PagedArgs &a, dim3 grid, cudaStream_t s);
+
+}  // namespace quartz

@@ -12,6 +12,7 @@ namespace quartz {
 // Values of the library's device error word (0 = no error).
 constexpr int QUARTZ_DEV_OK = 0;
 constexpr int QUARTZ_DEV_TIMEOUT = 1;
+constexpr int QUARTZ_DEV_INDEX = 2;  // a page, slot, length or kept index out of range
 
 // Upper bound on any single mbarrier wait inside a kernel.  No legitimate
 // wait on a healthy GPU comes near it; it only turns a would-be hang into an
@@ -151,6 +152,57 @@ cudaError_t launch_gemm_simt(const LinearWorkspace &ws, int64_t M, int64_t N, in
                              const void *bias, void *y, int y_type, int32_t *partials,
                              int partials_group, cudaStream_t s);
 cudaError_t launch_selftest_timeout(int64_t limit_ns, int *dev_err, cudaStream_t s);
+// Paged cache (rope.cu, paged.cu, paged_attention.cu, evict.cu).  Arguments
+// are pre-validated (paged_api.cu).
+struct RopeArgs {
+    const void *x;
+    void *y;
+    int64_t x_st, x_sh, y_st, y_sh;  // strides in elements
+    int type, heads, dim;
+    quartz_rope_t rope;
+};
+cudaError_t launch_rope(const RopeArgs &a, int64_t tokens, cudaStream_t s);
+struct AppendArgs {
+    const void *k, *v;
+    int64_t k_st, k_sh, v_st, v_sh;
+    const int64_t *slots;
+    quartz_rope_t rope;  // positions NULL: none
+    int *dev_err;
+};
+cudaError_t launch_paged_append(const quartz_paged_cache_t *c, const AppendArgs &a, int64_t tokens, cudaStream_t s);
+struct PagedAttnCall {
+    const void *q;
+    int64_t q_sb, q_sh, seqs;
+    int q_heads;
+    const int32_t *table;
+    int64_t table_stride;
+    const int32_t *lens;
+    int64_t max_len, window;
+    float scale;
+    void *o;
+    int o_type;
+    float *weights;
+    int64_t w_sb, w_sh;
+    void *workspace;
+    int *dev_err;
+};
+size_t paged_attention_workspace_bytes(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, int64_t max_len,
+                                       int64_t window, bool with_weights);
+cudaError_t launch_paged_attention(const quartz_paged_cache_t *c, const PagedAttnCall &a, cudaStream_t s);
+cudaError_t launch_evict_select(const float *w, int64_t w_sb, int64_t w_sh, const int32_t *lens, int64_t seqs, int heads,
+                                int64_t max_len, int64_t budget, int64_t recent, int64_t sinks, int32_t *kept,
+                                int32_t *new_lens, int *dev_err, cudaStream_t s);
+struct CompactCall {
+    int64_t seqs;
+    const int32_t *table, *new_table;
+    int64_t table_stride, new_table_stride;
+    const int32_t *lens, *kept;
+    int64_t max_len, budget;
+    float *weights;
+    int64_t w_sb, w_sh;
+    int *dev_err;
+};
+cudaError_t launch_cache_compact(const quartz_paged_cache_t *c, const CompactCall &a, cudaStream_t s);
 // Pipe-rate probes (probe.cu).
 cudaError_t launch_probe_fp32(int blocks, int64_t iters, float *sink, cudaStream_t s);
 cudaError_t launch_probe_mma_f8(int blocks, int64_t iters, int *dev_err, cudaStream_t s);
