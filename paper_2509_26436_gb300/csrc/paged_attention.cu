@@ -17,17 +17,18 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_kernel(PagedAr
     griddep_wait();
     constexpr int TILE = 8 * NT, KC = D / 32, VC = D / 64;
     constexpr bool kQRegs = D <= 128;  // wider heads read the query from shared memory again for each tile
-    constexpr float kUp = BF ? 0.f : 14.f;
+    constexpr float kUp = BF ? 0.f : 13.f, kSlack = BF ? 8.f : 2.f;  // 2^(up + slack) fits fp16
     __shared__ __align__(16) uint16_t s_q[kPagedHeads][D + 8];
-    __shared__ __align__(16) PagedJoin<D> s_join;
+    __shared__ PagedJoin s_join;
+    __shared__ __align__(16) uint8_t s_o[kPagedWarps][kPagedJoinBytes<D>];
 
     const int head_block = blockIdx.x % a.head_blocks, split = blockIdx.x / a.head_blocks;
     const int kv_head = blockIdx.y, b = blockIdx.z, head0 = head_block * kPagedHeads;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
     const int begin = split * a.chunk;
-    if (a.part_o && begin >= range.count) return;
-    const int end = range.first + min(begin + a.chunk, range.count);  // first token behind the split
+    if (a.part_o && begin >= range.count()) return;
+    const int end = range.base + min(begin + a.chunk, range.count());  // first token behind the split
 
     for (int e = threadIdx.x; e < kPagedHeads * (D / 8); e += kPagedThreads) {
         const int h = e / (D / 8), d = (e - h * (D / 8)) * 8;
@@ -71,7 +72,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_kernel(PagedAr
 
     PagedState<D> st;
     st.init();
-    int base = range.first + begin + warp * TILE;
+    int base = range.base + begin + warp * TILE;
     uint32_t pages = 0, next_pages = 0;
     if (base < end) {
         pages = page_of(base);
@@ -110,19 +111,21 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_kernel(PagedAr
         float sc[NT][2];
 #pragma unroll
         for (int i = 0; i < NT; ++i) sc[i][0] = s[i][0] * a.scale_log2, sc[i][1] = s[i][1] * a.scale_log2;
-        if (base + TILE > end) {
+        if (base + TILE > end || base < range.first) {
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                if (base + 2 * NT * q + 2 * i >= end) sc[i][0] = -INFINITY;
-                if (base + 2 * NT * q + 2 * i + 1 >= end) sc[i][1] = -INFINITY;
-            }
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int t = base + 2 * NT * q + 2 * i + x;
+                    if (t >= end || t < range.first) sc[i][x] = -INFINITY;
+                }
         }
         if (score_row) {
-            float *to = score_row + (base - range.first) + 2 * NT * q;
+            float *to = score_row + (base - range.base) + 2 * NT * q;
 #pragma unroll
             for (int i = 0; i < NT; ++i) *reinterpret_cast<float2 *>(to + 2 * i) = make_float2(sc[i][0], sc[i][1]);
         }
-        st.template weigh<NT>(sc, kUp);
+        st.template weigh<NT>(sc, kUp, kSlack);
         uint32_t hi[NT], lo[NT];
 #pragma unroll
         for (int i = 0; i < NT; ++i) split_pair<BF>(sc[i][0], sc[i][1], hi[i], lo[i]);
@@ -145,7 +148,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_kernel(PagedAr
         base = next;
     }
     if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
-    paged_finish<D>(s_join, st, a, b, kv_head, head0, split, kUp);
+    paged_finish<D>(s_join, s_o[0], sizeof(s_o[0]), st, a, b, kv_head, head0, split, kUp);
 }
 
 template <int D, bool BF>
@@ -159,7 +162,7 @@ struct Kernel16 {
             int k = 0;
             if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, paged_attn_kernel<D, NT, BF, MINB>, kPagedThreads, 0) !=
                 cudaSuccess)
-                k = 1;
+                return 1;
             occ = k > 0 ? k : 1;
             cache.store(occ, std::memory_order_relaxed);
         }
@@ -189,7 +192,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a)
     const int64_t row = blockIdx.x;
     const int b = static_cast<int>(row / (a.kv_heads * a.group));
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
-    const int splits = (range.count + a.chunk - 1) / a.chunk;
+    const int splits = (range.count() + a.chunk - 1) / a.chunk;
     const float *ml = a.part_ml + 2 * row * a.n_split;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     float m = -INFINITY;
@@ -251,7 +254,7 @@ __global__ void __launch_bounds__(256) paged_weights_kernel(PagedArgs a, float *
     const int h = blockIdx.y, b = blockIdx.z;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
     const int t = (blockIdx.x * 256 + threadIdx.x) * 4;
-    if (t >= range.count) return;
+    if (t >= range.count()) return;
     const int64_t row0 = (static_cast<int64_t>(b) * a.kv_heads + h) * a.group;
     float p[4] = {0.f, 0.f, 0.f, 0.f};
     for (int g = 0; g < a.group; ++g) {
@@ -259,10 +262,10 @@ __global__ void __launch_bounds__(256) paged_weights_kernel(PagedArgs a, float *
         const float lse = a.lse[row0 + g];
         p[0] += ex2(s.x - lse), p[1] += ex2(s.y - lse), p[2] += ex2(s.z - lse), p[3] += ex2(s.w - lse);
     }
-    float *w = weights + b * w_sb + h * w_sh + range.first + t;
+    float *w = weights + b * w_sb + h * w_sh + range.base + t;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (t + i < range.count) w[i] += p[i];
+        if (t + i < range.count() && range.base + t + i >= range.first) w[i] += p[i];
 }
 
 int log2_of(int v)
@@ -284,7 +287,8 @@ struct PagedPlan {
 PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, int64_t max_len, int64_t window)
 {
     PagedPlan p;
-    p.tokens = window > 0 && window < max_len ? window : max_len;
+    // a window's first tile may hold 15 tokens before it
+    p.tokens = window > 0 && window + 15 < max_len ? window + 15 : max_len;
     const int group = q_heads / c->heads;
     const int64_t ctas = seqs * c->heads * ((group + kPagedHeads - 1) / kPagedHeads);
     const int occ = c->type == QUARTZ_PAGES_ENCODED ? paged_kernel_occupancy_encoded(c->dim, c->k.enc.p.group_s)

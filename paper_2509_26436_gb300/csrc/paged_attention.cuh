@@ -65,9 +65,12 @@ struct PagedArgs {
     int *dev_err;
 };
 
-// The tokens a sequence's new token sees: [first, first + count).
+// The tokens a sequence's new token sees: [first, end).  Splits and tiles are
+// counted from `base`, the multiple of 16 at or below `first`, so that a tile
+// of 16 tokens lies in one page of 16 or more and at an aligned place.
 struct PagedRange {
-    int first, count;
+    int base, first, end;
+    __device__ __forceinline__ int count() const { return end - base; }
 };
 
 __device__ __forceinline__ PagedRange paged_range(const int32_t *lens, int b, int max_len, int window, int *dev_err)
@@ -79,7 +82,8 @@ __device__ __forceinline__ PagedRange paged_range(const int32_t *lens, int b, in
     }
     PagedRange r;
     r.first = window > 0 && len > window ? len - window : 0;
-    r.count = len - r.first;
+    r.base = r.first & ~15;
+    r.end = len;
     return r;
 }
 
@@ -143,6 +147,15 @@ __device__ __forceinline__ void split_pair(float p0, float p1, uint32_t &hi, uin
     }
 }
 
+// Asynchronous 16-byte copies global -> shared, one group per tile.
+__device__ __forceinline__ void paged_copy16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void paged_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void paged_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Running softmax of a warp over its tiles: m is its head's maximum (log2
 // domain), l this lane's part of the sum of weights.
 template <int D>
@@ -162,14 +175,17 @@ struct PagedState {
 
     // Scores sc (log2 domain, -inf where masked) to weights 2^(sc - m + up);
     // `up` keeps small weights of a 16-bit type with few exponent bits normal.
+    // The maximum follows only when it is passed by more than `slack`: a weight
+    // of 2^slack does no harm, and eight heads pass their maxima by little in
+    // every other tile, while a rescale touches every accumulator.
     template <int NT>
-    __device__ __forceinline__ void weigh(float (&sc)[NT][2], float up)
+    __device__ __forceinline__ void weigh(float (&sc)[NT][2], float up, float slack)
     {
         float mx = fmaxf(sc[0][0], sc[0][1]);
         if (NT == 2) mx = fmaxf(mx, fmaxf(sc[NT - 1][0], sc[NT - 1][1]));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        if (__any_sync(0xffffffffu, mx > m)) {
+        if (__any_sync(0xffffffffu, mx > m + slack)) {
             const float m_new = fmaxf(m, mx), f = ex2(m - m_new);
             m = m_new;
             l *= f;
@@ -215,17 +231,22 @@ __device__ __forceinline__ void paged_store4(void *o, int type, int64_t at, floa
 // Join the warps of a CTA in a fixed order and write the split's result: the
 // output itself where there is one split, else o (relative to the split's
 // maximum) with maximum and sum.
-template <int D>
 struct PagedJoin {
-    static constexpr int kRow = D + 4;
-    float o[kPagedWarps][kPagedHeads][kRow];
     float m[kPagedWarps][kPagedHeads], l[kPagedWarps][kPagedHeads];
 };
 
+// `smem` + warp * warp_bytes: the warp's own shared memory, at least
+// kPagedJoinBytes<D>, free by now.
 template <int D>
-__device__ __forceinline__ void paged_finish(PagedJoin<D> &s, PagedState<D> &st, const PagedArgs &a, int b, int kv_head,
-                                             int head0, int split, float up)
+constexpr int kPagedJoinBytes = kPagedHeads * (D + 4) * 4;
+
+template <int D>
+__device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int warp_bytes, PagedState<D> &st,
+                                             const PagedArgs &a, int b, int kv_head, int head0, int split, float up)
 {
+    auto so = [&](int w, int h, int d) {
+        return reinterpret_cast<float4 *>(smem + w * warp_bytes + (h * (D + 4) + d) * 4);
+    };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
     float l = st.l;
     l += __shfl_xor_sync(0xffffffffu, l, 1);
@@ -238,7 +259,7 @@ __device__ __forceinline__ void paged_finish(PagedJoin<D> &s, PagedState<D> &st,
 #pragma unroll
             for (int j = 0; j < 8; j += 4) {
                 const float(*o)[4] = &st.o[hv * 8 + j];
-                *reinterpret_cast<float4 *>(&s.o[warp][n][hv * 64 + (2 * q + x) * 8 + j]) =
+                *so(warp, n, hv * 64 + (2 * q + x) * 8 + j) =
                     make_float4(o[0][x] + o[0][x + 2], o[1][x] + o[1][x + 2], o[2][x] + o[2][x + 2], o[3][x] + o[3][x + 2]);
             }
     __syncthreads();
@@ -254,7 +275,7 @@ __device__ __forceinline__ void paged_finish(PagedJoin<D> &s, PagedState<D> &st,
 #pragma unroll
         for (int w = 0; w < kPagedWarps; ++w) {
             const float f = m == -INFINITY ? 0.f : ex2(s.m[w][h] - m - up);
-            const float4 u = *reinterpret_cast<const float4 *>(&s.o[w][h][d]);
+            const float4 u = *so(w, h, d);
             sum += f * s.l[w][h];
             v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
         }

@@ -75,42 +75,193 @@ __device__ __forceinline__ void value_codes(uint32_t w0, uint32_t w1, uint32_t f
     }
 }
 
-// The G scales of a row (2 G bytes, aligned to their largest power of two).
-template <int G>
-__device__ __forceinline__ void load_scales(const __half *p, float (&s)[G])
+// A warp's tile of 16 tokens in shared memory, keys and values: codes, FLAGs
+// and scales.  Rows and 16-byte chunks of the codes are permuted so that the
+// reads below hit different banks: 8-byte reads of one chunk pair of tokens 0,
+// 1, 4, 5 (keys), 4-byte reads of tokens 0, 4, 8, 12 (values).
+template <int D, int GS>
+struct LzsTile {
+    static constexpr int kTokens = 16, kChunks = D / 32;  // 16-byte chunks of codes per row
+    static constexpr int kCodes = kTokens * D / 2, kFlags = kTokens * D / GS, kScales = kTokens * D / 32;
+    static constexpr int kSide = kCodes + kFlags + kScales, kBytes = 2 * kSide;
+    static constexpr int kStages = D <= 128 ? 4 : 3;
+    // The small planes of both sides as 16-byte chunks: FLAGs, scales, FLAGs, scales.
+    static constexpr int kSmall = 2 * (kFlags + kScales) / 16, kSmallPerLane = (kSmall + 31) / 32;
+    static constexpr int kCodesPerLane = kCodes / 16 / 32 > 0 ? kCodes / 16 / 32 : 1;
+
+    __host__ __device__ static constexpr int key_at(int t, int c)
+    {
+        const int odd = (t >> 2) & 1;
+        const int r = D == 64 || D == 192 ? t ^ (odd << 1) : t;
+        const int x = D == 128 ? odd * 2 : D == 256 ? ((t & 1) + 2 * odd) * 2 : 0;
+        return (r * kChunks + (c ^ x)) * 16;
+    }
+    __host__ __device__ static constexpr int value_at(int t, int c)
+    {
+        const int q = t >> 2, r = (t & 3) * 4 + q;
+        const int x = D == 128 ? (q >> 1) * 2 : D == 256 ? q * 2 : 0;
+        return (r * kChunks + (c ^ x)) * 16;
+    }
+};
+
+__device__ __forceinline__ uint32_t lds32(uint32_t a)
 {
-    if (G == 1) {
-        s[0] = __half2float(__ldg(p));
-    } else if (G == 2 || G == 4) {
+    uint32_t v;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t a)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint4 lds128(uint32_t a)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds16(uint32_t a)
+{
+    uint16_t v;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a)
+{
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
+    return v;
+}
+
+// The scales of tokens 4 q .. 4 q + 3, G each: consecutive in the tile.
+template <int G>
+__device__ __forceinline__ void lds_scales(uint32_t a, float (&s)[4][G])
+{
+    uint32_t w[2 * G];
 #pragma unroll
-        for (int i = 0; i < G; i += 2) {
-            const float2 f = __half22float2(__ldg(reinterpret_cast<const __half2 *>(p + i)));
-            s[i] = f.x, s[i + (G > 1)] = f.y;
-        }
-    } else {
+    for (int i = 0; i < 2 * G; i += 2) {
+        const uint2 v = lds64(a + 4 * i);
+        w[i] = v.x, w[i + 1] = v.y;
+    }
 #pragma unroll
-        for (int i = 0; i < G; ++i) s[i] = __half2float(__ldg(p + i));
+    for (int i = 0; i < 4 * G; ++i) {
+        const __half2 h = *reinterpret_cast<const __half2 *>(&w[i / 2]);
+        s[i / G][i % G] = i % 2 ? __high2float(h) : __low2float(h);
     }
 }
 
-template <int D, int GS, int NT, int MINB>
+template <int D, int GS, int MINB>
 __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(PagedArgs a)
 {
     griddep_wait();
-    constexpr int TILE = 8 * NT, G = D / 64, FPR = D / GS;  // FLAGs per row
+    using Tile = LzsTile<D, GS>;
+    constexpr int G = D / 64, FPR = D / GS;  // groups and FLAGs per row
+    constexpr int kStages = Tile::kStages, kWarpBytes = kStages * Tile::kBytes;
     constexpr bool kQRegs = D <= 128;
+    static_assert(kWarpBytes >= kPagedJoinBytes<D>, "the join uses the ring");
+    extern __shared__ __align__(16) uint8_t s_ring[];
     __shared__ __align__(16) uint16_t s_q[kPagedHeads][D + 8];
-    __shared__ __align__(16) PagedJoin<D> s_join;
+    __shared__ PagedJoin s_join;
 
     const int head_block = blockIdx.x % a.head_blocks, split = blockIdx.x / a.head_blocks;
     const int kv_head = blockIdx.y, b = blockIdx.z, head0 = head_block * kPagedHeads;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
     const int begin = split * a.chunk;
-    if (a.part_o && begin >= range.count) return;
-    const int end = range.first + min(begin + a.chunk, range.count);
+    if (a.part_o && begin >= range.count()) return;
+    const int end = range.base + min(begin + a.chunk, range.count());
+    const int base0 = range.base + begin + warp * 16;
+    const int tiles = base0 < end ? (end - base0 + kPagedWarps * 16 - 1) / (kPagedWarps * 16) : 0;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + warp * kWarpBytes;
 
-    // the query, in the order the keys' codes unpack to: pairs (k, k + 4) of
+    // --- copies of a tile -------------------------------------------------
+    const int32_t *table = a.table + b * a.table_stride;
+    const uint32_t page_mask = (1u << a.page_shift) - 1;
+    bool bad = false;
+    // lane's part of the codes: chunk i = lane + 32 k of the tile
+    int key_dst[Tile::kCodesPerLane], value_dst[Tile::kCodesPerLane];
+#pragma unroll
+    for (int k = 0; k < Tile::kCodesPerLane; ++k) {
+        const int i = lane + 32 * k, t = i / Tile::kChunks, c = i % Tile::kChunks;
+        key_dst[k] = Tile::key_at(t, c);
+        value_dst[k] = Tile::kSide + Tile::value_at(t, c);
+    }
+    // and of the small planes
+    const uint8_t *small_src[Tile::kSmallPerLane];
+    int small_row[Tile::kSmallPerLane], small_dst[Tile::kSmallPerLane];
+#pragma unroll
+    for (int k = 0; k < Tile::kSmallPerLane; ++k) {
+        int i = lane + 32 * k;
+        const bool in = i < Tile::kSmall;
+        const int side = i >= Tile::kSmall / 2;
+        i -= side * (Tile::kSmall / 2);
+        const bool flag = i < Tile::kFlags / 16;
+        const PagedSide &ps = side ? a.v : a.k;
+        small_src[k] = (flag ? ps.flags : reinterpret_cast<const uint8_t *>(ps.scales) - Tile::kFlags) + i * 16;
+        small_row[k] = in ? (flag ? FPR : 2 * G) : -1;
+        small_dst[k] = side * Tile::kSide + Tile::kCodes + i * 16;
+    }
+    auto page_of = [&](int t) {
+        const uint32_t page = static_cast<uint32_t>(__ldg(table + (min(t, end - 1) >> a.page_shift)));
+        bad |= page >= a.num_pages;
+        return page < a.num_pages ? page : 0u;
+    };
+    auto row_of = [&](uint32_t page, int t) {
+        return ((page * a.kv_heads + kv_head) << a.page_shift) + (static_cast<uint32_t>(t) & page_mask);
+    };
+    const bool small_pages = a.page_shift < 4;
+    // Pages of 16 or more: 16 consecutive rows.  Smaller ones: row by row; the
+    // small planes' rows are then below the 16 bytes of a copy and go through
+    // registers.  A token past the end repeats the last one.
+    auto fetch = [&](int base, uint32_t page, int stage) {
+        const uint32_t to = ring + stage * Tile::kBytes;
+        if (!small_pages) {
+            const uint64_t row = row_of(page, base);
+            const uint8_t *kc = a.k.codes + row * (D / 2) + lane * 16, *vc = a.v.codes + row * (D / 2) + lane * 16;
+#pragma unroll
+            for (int k = 0; k < Tile::kCodesPerLane; ++k)
+                if (Tile::kCodes / 16 >= 32 || lane < Tile::kCodes / 16) {
+                    paged_copy16(to + key_dst[k], kc + k * 512);
+                    paged_copy16(to + value_dst[k], vc + k * 512);
+                }
+#pragma unroll
+            for (int k = 0; k < Tile::kSmallPerLane; ++k)
+                if (small_row[k] >= 0) paged_copy16(to + small_dst[k], small_src[k] + row * small_row[k]);
+        } else {
+            const int mine = min(base + (lane & 15), end - 1);
+            const uint32_t my_row = row_of(page_of(mine), mine);
+#pragma unroll
+            for (int k = 0; k < Tile::kCodesPerLane; ++k) {
+                const int i = lane + 32 * k, t = i / Tile::kChunks, c = i % Tile::kChunks;
+                const uint64_t row = __shfl_sync(0xffffffffu, my_row, t & 15);
+                if (Tile::kCodes / 16 >= 32 || lane < Tile::kCodes / 16) {
+                    paged_copy16(to + key_dst[k], a.k.codes + row * (D / 2) + c * 16);
+                    paged_copy16(to + value_dst[k], a.v.codes + row * (D / 2) + c * 16);
+                }
+            }
+            const PagedSide &ps = lane < 16 ? a.k : a.v;  // a lane per row and side
+            uint8_t *dst = s_ring + (to - static_cast<uint32_t>(__cvta_generic_to_shared(s_ring))) +
+                           (lane < 16 ? 0 : Tile::kSide) + Tile::kCodes;
+            const uint8_t *fl = ps.flags + static_cast<uint64_t>(my_row) * FPR;
+#pragma unroll
+            for (int i = 0; i < FPR; ++i) dst[(lane & 15) * FPR + i] = __ldg(fl + i);
+            const __half *sc = ps.scales + static_cast<uint64_t>(my_row) * G;
+#pragma unroll
+            for (int i = 0; i < G; ++i)
+                reinterpret_cast<__half *>(dst + Tile::kFlags)[(lane & 15) * G + i] = __ldg(sc + i);
+        }
+    };
+    uint32_t next_page = 0;  // of the next tile to fetch
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) {
+        if (s < tiles) fetch(base0 + s * kPagedWarps * 16, page_of(base0 + s * kPagedWarps * 16), s);
+        paged_commit();
+    }
+    if (kStages - 1 < tiles) next_page = page_of(base0 + (kStages - 1) * kPagedWarps * 16);
+
+    // --- the query, in the order the keys' codes unpack to: pairs (k, k + 4) of
     // each 8 elements
     for (int e = threadIdx.x; e < kPagedHeads * (D / 8); e += kPagedThreads) {
         const int h = e / (D / 8), d = (e - h * (D / 8)) * 8;
@@ -128,145 +279,128 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 #pragma unroll
         for (int g = 0; g < G; ++g) qf[g][0] = query(g, 0), qf[g][1] = query(g, 1);
 
-    const int32_t *table = a.table + b * a.table_stride;
-    const int mask = (1 << a.page_shift) - 1;
-    bool bad = false;
-    auto page_of = [&](int base) {
-        const int t = min(base + (lane & (TILE - 1)), end - 1);
-        const uint32_t page = static_cast<uint32_t>(table[t >> a.page_shift]);
-        bad |= page >= a.num_pages;
-        return page < a.num_pages ? page : 0u;
-    };
-    // cache row (below 2^31) of token base + i
-    auto row_of = [&](uint32_t pages, int base, int i) {
-        const uint32_t page = __shfl_sync(0xffffffffu, pages, i);
-        const uint32_t slot = static_cast<uint32_t>(min(base + i, end - 1)) & mask;
-        return ((page * a.kv_heads + kv_head) << a.page_shift) + slot;
-    };
-
-    uint2 kc[NT][G];
-    uint32_t kfl[NT][G];  // FLAG of the lane's 16 codes (G_s = 8: two bytes)
-    auto load_k = [&](uint32_t pages, int base) {
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const uint32_t row = row_of(pages, base, (n >> 1) * 2 * NT + 2 * i + (n & 1));
-            const uint8_t *c = a.k.codes + static_cast<uint64_t>(row) * (D / 2) + q * 8;
-            const uint8_t *f = a.k.flags + static_cast<uint64_t>(row) * FPR + (q * 16) / GS;
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                kc[i][g] = __ldg(reinterpret_cast<const uint2 *>(c + g * 32));
-                kfl[i][g] = GS == 8 ? __ldg(reinterpret_cast<const uint16_t *>(f + g * 8)) : __ldg(f + g * (64 / GS));
-            }
-        }
-    };
-    uint32_t vc[2 * NT][G], vfl[2 * NT][G];
-    float ks[2 * NT][G], vs[2 * NT][G];
-    auto load_v = [&](uint32_t pages, int base) {
-#pragma unroll
-        for (int j = 0; j < 2 * NT; ++j) {
-            const uint32_t row = row_of(pages, base, 2 * NT * q + j);
-            const uint8_t *c = a.v.codes + static_cast<uint64_t>(row) * (D / 2) + n * 4;
-            const uint8_t *f = a.v.flags + static_cast<uint64_t>(row) * FPR + (n * 8) / GS;
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                vc[j][g] = __ldg(reinterpret_cast<const uint32_t *>(c + g * 32));
-                vfl[j][g] = __ldg(f + g * (64 / GS));
-            }
-            load_scales<G>(a.k.scales + static_cast<uint64_t>(row) * G, ks[j]);
-            load_scales<G>(a.v.scales + static_cast<uint64_t>(row) * G, vs[j]);
-        }
-    };
-
+    // --- places of the lane's pieces in a tile: keys of token (n / 2) 4 + 2 i +
+    // n % 2, values of tokens 4 q + j
+    const int key_token = (n >> 1) * 4 + (n & 1);
     PagedState<D> st;
     st.init();
-    int base = range.first + begin + warp * TILE;
-    uint32_t pages = 0;
-    if (base < end) {
-        pages = page_of(base);
-        load_k(pages, base);
-        load_v(pages, base);
-        if (base + kPagedWarps * TILE < end) pages = page_of(base + kPagedWarps * TILE);
-    }
     float *score_row = a.scores && head0 + n < a.group
                            ? a.scores + ((static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0 + n) * a.score_stride
                            : nullptr;
-    while (base < end) {
+    int stage = 0;
+    for (int it = 0; it < tiles; ++it) {
+        const int base = base0 + it * kPagedWarps * 16;
+        paged_wait<kStages - 2>();
+        __syncwarp();
+        {
+            const int ahead = it + kStages - 1;
+            if (ahead < tiles) {
+                fetch(base0 + ahead * kPagedWarps * 16, next_page, stage == 0 ? kStages - 1 : stage - 1);
+                if (ahead + 1 < tiles) next_page = page_of(base0 + (ahead + 1) * kPagedWarps * 16);
+            }
+            paged_commit();
+        }
+        const uint32_t tile = ring + stage * Tile::kBytes;
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+
         // scores: a sum per group, times the group's scale
-        float sc[NT][2];
+        float ks[4][G];
+        lds_scales<G>(tile + Tile::kCodes + Tile::kFlags + q * 8 * G, ks);
+        float sc[2][2];
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
+        for (int i = 0; i < 2; ++i) {
             sc[i][0] = sc[i][1] = 0.f;
+            const int t = key_token + 2 * i;
+            const uint32_t flags = tile + Tile::kCodes + t * FPR + (q * 16) / GS;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
+                const uint2 c = lds64(tile + Tile::key_at(t, g * 2 + (q >> 1)) + (q & 1) * 8);
+                const uint32_t f = GS == 8 ? lds16(flags + g * 8) : lds8(flags + g * (64 / GS));
+                const uint32_t f0 = (GS == 8 ? f & 0xFFu : f) * 0x04000400u;
+                const uint32_t f1 = GS == 8 ? (f >> 8) * 0x04000400u : f0;
                 float s[4] = {0.f, 0.f, 0.f, 0.f};
-                const uint32_t f0 = (GS == 8 ? kfl[i][g] & 0xFFu : kfl[i][g]) * 0x04000400u;
-                const uint32_t f1 = GS == 8 ? (kfl[i][g] >> 8) * 0x04000400u : f0;
                 uint32_t k[4];
                 uint4 w = kQRegs ? qf[kQRegs ? g : 0][0] : query(g, 0);
-                key_codes(kc[i][g].x, f0, k);
+                key_codes(c.x, f0, k);
                 mma16<false>(s, w.x, w.x, w.y, w.y, k[0], k[1]);
                 mma16<false>(s, w.z, w.z, w.w, w.w, k[2], k[3]);
                 w = kQRegs ? qf[kQRegs ? g : 0][1] : query(g, 1);
-                key_codes(kc[i][g].y, f1, k);
+                key_codes(c.y, f1, k);
                 mma16<false>(s, w.x, w.x, w.y, w.y, k[0], k[1]);
                 mma16<false>(s, w.z, w.z, w.w, w.w, k[2], k[3]);
                 sc[i][0] += s[0] * ks[2 * i][g];
                 sc[i][1] += s[1] * ks[2 * i + 1][g];
             }
         }
-        const int next = base + kPagedWarps * TILE;
-        if (next < end) load_k(pages, next);
 #pragma unroll
-        for (int i = 0; i < NT; ++i) sc[i][0] *= a.scale_log2, sc[i][1] *= a.scale_log2;
-        if (base + TILE > end) {
+        for (int i = 0; i < 2; ++i) sc[i][0] *= a.scale_log2, sc[i][1] *= a.scale_log2;
+
+        float vs[4][G];
+        lds_scales<G>(tile + Tile::kSide + Tile::kCodes + Tile::kFlags + q * 8 * G, vs);
+        const uint32_t vflags = tile + Tile::kSide + Tile::kCodes + 4 * q * FPR + (n * 8) / GS;
+        uint32_t vf[2][G];  // FLAGs of token pairs
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                if (base + 2 * NT * q + 2 * i >= end) sc[i][0] = -INFINITY;
-                if (base + 2 * NT * q + 2 * i + 1 >= end) sc[i][1] = -INFINITY;
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+                vf[i][g] = lds8(vflags + 2 * i * FPR + g * (64 / GS)) + (lds8(vflags + (2 * i + 1) * FPR + g * (64 / GS)) << 16);
+        if (base + 16 > end || base < range.first) {
+            // tokens that are not seen: no weight, and nothing of what their
+            // slots happen to hold (a scale may be NaN)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = base + 4 * q + j;
+                if (t >= end || t < range.first) {
+                    sc[j / 2][j % 2] = -INFINITY;
+#pragma unroll
+                    for (int g = 0; g < G; ++g) {
+                        vs[j][g] = 0.f;
+                        vf[j / 2][g] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+                    }
+                }
             }
         }
         if (score_row) {
-            float *to = score_row + (base - range.first) + 2 * NT * q;
-#pragma unroll
-            for (int i = 0; i < NT; ++i) *reinterpret_cast<float2 *>(to + 2 * i) = make_float2(sc[i][0], sc[i][1]);
+            float *to = score_row + (base - range.base) + 4 * q;
+            *reinterpret_cast<float4 *>(to) = make_float4(sc[0][0], sc[0][1], sc[1][0], sc[1][1]);
         }
-        st.template weigh<NT>(sc, 0.f);
+        st.template weigh<2>(sc, 0.f, 8.f);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            uint32_t hi[NT], lo[NT], v0[8], v1[8];
+            uint32_t hi[2], lo[2], v0[8], v1[8], c[4];
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
-                split_pair<true>(sc[i][0] * vs[2 * i][g], sc[i][1] * vs[2 * i + 1][g], hi[i], lo[i]);
-            value_codes(vc[0][g], vc[1][g], vfl[0][g] | (vfl[1][g] << 16), v0);
-            if (NT == 2) value_codes(vc[2 * NT - 2][g], vc[2 * NT - 1][g], vfl[2 * NT - 2][g] | (vfl[2 * NT - 1][g] << 16), v1);
+            for (int j = 0; j < 4; ++j) c[j] = lds32(tile + Tile::kSide + Tile::value_at(4 * q + j, g * 2 + (n >> 2)) + (n & 3) * 4);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (NT == 2) mma16<true>(st.o[g * 8 + j], hi[0], lo[0], hi[NT - 1], lo[NT - 1], v0[j], v1[j]);
-                else mma8<true>(st.o[g * 8 + j], hi[0], lo[0], v0[j]);
-            }
+            for (int i = 0; i < 2; ++i) split_pair<true>(sc[i][0] * vs[2 * i][g], sc[i][1] * vs[2 * i + 1][g], hi[i], lo[i]);
+            value_codes(c[0], c[1], vf[0][g], v0);
+            value_codes(c[2], c[3], vf[1][g], v1);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mma16<true>(st.o[g * 8 + j], hi[0], lo[0], hi[1], lo[1], v0[j], v1[j]);
         }
-        if (next < end) {
-            load_v(pages, next);
-            if (next + kPagedWarps * TILE < end) pages = page_of(next + kPagedWarps * TILE);
-        }
-        base = next;
     }
+    paged_wait<0>();
+    __syncwarp();
     if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
-    paged_finish<D>(s_join, st, a, b, kv_head, head0, split, 0.f);
+    paged_finish<D>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, 0.f);
 }
 
 template <int D, int GS>
 struct KernelLzs {
-    static constexpr int NT = D <= 192 ? 2 : 1, MINB = D <= 64 ? 4 : D <= 128 ? 3 : 2;
+    static constexpr int MINB = D <= 64 ? 4 : D <= 128 ? 3 : 2;
+    static constexpr int kSmem = kPagedWarps * LzsTile<D, GS>::kStages * LzsTile<D, GS>::kBytes;
+    static cudaError_t ready()
+    {
+        return cudaFuncSetAttribute(paged_attn_lzs_kernel<D, GS, MINB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    }
     static int occupancy()
     {
         static std::atomic<int> cache{0};
         int occ = cache.load(std::memory_order_relaxed);
         if (occ == 0) {
             int k = 0;
-            if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, paged_attn_lzs_kernel<D, GS, NT, MINB>, kPagedThreads, 0) !=
-                cudaSuccess)
-                k = 1;
+            if (ready() != cudaSuccess || cudaOccupancyMaxActiveBlocksPerMultiprocessor(
+                                              &k, paged_attn_lzs_kernel<D, GS, MINB>, kPagedThreads, kSmem) != cudaSuccess)
+                return 1;
             occ = k > 0 ? k : 1;
             cache.store(occ, std::memory_order_relaxed);
         }
@@ -274,7 +408,9 @@ struct KernelLzs {
     }
     static cudaError_t launch(const PagedArgs &a, dim3 grid, cudaStream_t s)
     {
-        return launch_pdl(paged_attn_lzs_kernel<D, GS, NT, MINB>, grid, dim3(kPagedThreads), 0, s, a);
+        const cudaError_t e = ready();  // of the current device
+        if (e != cudaSuccess) return e;
+        return launch_pdl(paged_attn_lzs_kernel<D, GS, MINB>, grid, dim3(kPagedThreads), kSmem, s, a);
     }
 };
 
