@@ -148,6 +148,9 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_kernel(PagedAr
         base = next;
     }
     if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
+    st.l += __shfl_xor_sync(0xffffffffu, st.l, 1);
+    st.l += __shfl_xor_sync(0xffffffffu, st.l, 2);
+    if (q == 0) s_join.m[warp][n] = st.m, s_join.l[warp][n] = st.l;
     paged_finish<D>(s_join, s_o[0], sizeof(s_o[0]), st, a, b, kv_head, head0, split, kUp);
 }
 

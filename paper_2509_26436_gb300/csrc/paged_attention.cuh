@@ -156,8 +156,9 @@ __device__ __forceinline__ void paged_commit() { asm volatile("cp.async.commit_g
 template <int N>
 __device__ __forceinline__ void paged_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Running softmax of a warp over its tiles: m is its head's maximum (log2
-// domain), l this lane's part of the sum of weights.
+// A warp's accumulators and its running softmax where a lane holds scores of
+// head lane / 4: m is the head's maximum (log2 domain), l this lane's part of
+// the sum of weights.
 template <int D>
 struct PagedState {
     float o[D / 8][4];
@@ -235,8 +236,9 @@ struct PagedJoin {
     float m[kPagedWarps][kPagedHeads], l[kPagedWarps][kPagedHeads];
 };
 
-// `smem` + warp * warp_bytes: the warp's own shared memory, at least
-// kPagedJoinBytes<D>, free by now.
+// The warps have left their heads' maxima and sums in `s`; `smem` + warp *
+// warp_bytes is the warp's own shared memory, at least kPagedJoinBytes<D>,
+// free by now.
 template <int D>
 constexpr int kPagedJoinBytes = kPagedHeads * (D + 4) * 4;
 
@@ -248,10 +250,6 @@ __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int wa
         return reinterpret_cast<float4 *>(smem + w * warp_bytes + (h * (D + 4) + d) * 4);
     };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
-    float l = st.l;
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
-    if (q == 0) s.m[warp][n] = st.m, s.l[warp][n] = l;
 #pragma unroll
     for (int hv = 0; hv < D / 64; ++hv)
 #pragma unroll

@@ -16,6 +16,11 @@
 //   values (bf16, so that a weight times a scale, whatever its size, keeps its
 //     8 bits; with the remainder 16): words of two tokens are paired by halves
 //     first, since an operand register holds two tokens of one column.
+// The keys are the first operand here (S' = K Q', 16 tokens x 8 heads per
+// instruction: every row used, and its four registers are two decoded words
+// as they come), so the scores arrive transposed: lane = tokens of row n and n
+// + 8, heads 2 q and 2 q + 1.  The 16-bit weights change sides with one
+// register transpose (movmatrix) per 8 x 8 block.
 #include <atomic>
 
 #include "paged_attention.cuh"
@@ -135,20 +140,39 @@ __device__ __forceinline__ uint32_t lds8(uint32_t a)
     return v;
 }
 
-// The scales of tokens 4 q .. 4 q + 3, G each: consecutive in the tile.
-template <int G>
-__device__ __forceinline__ void lds_scales(uint32_t a, float (&s)[4][G])
+// An opaque copy: what follows from it is not recomputed from the lane.
+__device__ __forceinline__ uint32_t fixed(uint32_t v)
 {
-    uint32_t w[2 * G];
+    asm volatile("" : "+r"(v));
+    return v;
+}
+
+// The transpose of an 8 x 8 block of 16-bit values, lane = row lane / 4,
+// columns 2 (lane % 4) and the next.
+__device__ __forceinline__ uint32_t transposed(uint32_t v)
+{
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
+
+// The G scales of a row of the tile.
+template <int G>
+__device__ __forceinline__ void lds_scales(uint32_t a, float (&s)[G])
+{
+    if (G == 1) {
+        s[0] = __half2float(__ushort_as_half(static_cast<unsigned short>(lds16(a))));
+    } else if (G == 4) {
+        const uint2 v = lds64(a);
+        const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v.x)), y = __half22float2(*reinterpret_cast<const __half2 *>(&v.y));
+        s[0] = x.x, s[1 % G] = x.y, s[2 % G] = y.x, s[3 % G] = y.y;
+    } else if (G == 2) {
+        const uint32_t v = lds32(a);
+        const float2 x = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+        s[0] = x.x, s[1 % G] = x.y;
+    } else {
 #pragma unroll
-    for (int i = 0; i < 2 * G; i += 2) {
-        const uint2 v = lds64(a + 4 * i);
-        w[i] = v.x, w[i + 1] = v.y;
-    }
-#pragma unroll
-    for (int i = 0; i < 4 * G; ++i) {
-        const __half2 h = *reinterpret_cast<const __half2 *>(&w[i / 2]);
-        s[i / G][i % G] = i % 2 ? __high2float(h) : __low2float(h);
+        for (int i = 0; i < G; ++i) s[i] = __half2float(__ushort_as_half(static_cast<unsigned short>(lds16(a + 2 * i))));
     }
 }
 
@@ -279,14 +303,31 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 #pragma unroll
         for (int g = 0; g < G; ++g) qf[g][0] = query(g, 0), qf[g][1] = query(g, 1);
 
-    // --- places of the lane's pieces in a tile: keys of token (n / 2) 4 + 2 i +
-    // n % 2, values of tokens 4 q + j
-    const int key_token = (n >> 1) * 4 + (n & 1);
+    // --- places of the lane's pieces in a tile: keys of tokens (n / 2) 4 + n % 2
+    // + 2 i, values of tokens 4 q + j.  Bases that differ between lanes are
+    // held in registers (`fixed` keeps the compiler from recomputing them for
+    // every tile), the rest are immediate offsets.
+    const int key_token = (n >> 1) * 4 + (n & 1), odd = (n >> 1) & 1;
+    constexpr int kRow = Tile::kChunks * 16;
+    constexpr int KB = D == 256 ? 4 : 2, VB = D == 256 ? 4 : D == 128 ? 2 : 1;
+    uint32_t kb[KB], vb[VB];
+#pragma unroll
+    for (int i = 0; i < KB; ++i)  // 64, 192: per token i; else per group
+        kb[i] = fixed(Tile::key_at(key_token + (D == 64 || D == 192 ? 2 * i : 0), (D == 128 || D == 256 ? 2 * i : 0) + (q >> 1)) + (q & 1) * 8);
+#pragma unroll
+    for (int i = 0; i < VB; ++i) vb[i] = fixed(Tile::kSide + Tile::value_at(4 * q, 2 * i + (n >> 2)) + (n & 3) * 4);
+    auto key_off = [&](int i, int g) { return D == 64 || D == 192 ? kb[i] + g * 32 : kb[g] + i * 2 * kRow; };
+    auto value_off = [&](int j, int g) { return (VB > 1 ? vb[VB > 1 ? g : 0] : vb[0] + g * 32) + j * 4 * kRow; };
+    const uint32_t kfb = fixed(Tile::kCodes + key_token * FPR + (q * 16) / GS);
+    const uint32_t ksb = fixed(Tile::kCodes + Tile::kFlags + key_token * 2 * G);
+    const uint32_t vfb = fixed(Tile::kSide + Tile::kCodes + 4 * q * FPR + (n * 8) / GS);
+
     PagedState<D> st;
     st.init();
-    float *score_row = a.scores && head0 + n < a.group
-                           ? a.scores + ((static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0 + n) * a.score_stride
-                           : nullptr;
+    // of heads 2 q and 2 q + 1: a maximum that all their lanes share, and this
+    // lane's part of the sum of weights
+    float m[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f};
+    const int64_t score_row = ((static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0 + 2 * q) * a.score_stride;
     int stage = 0;
     for (int it = 0; it < tiles; ++it) {
         const int base = base0 + it * kPagedWarps * 16;
@@ -303,80 +344,123 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
         const uint32_t tile = ring + stage * Tile::kBytes;
         stage = stage == kStages - 1 ? 0 : stage + 1;
 
-        // scores: a sum per group, times the group's scale
-        float ks[4][G];
-        lds_scales<G>(tile + Tile::kCodes + Tile::kFlags + q * 8 * G, ks);
-        float sc[2][2];
+        // scores of tokens i and heads x: a sum per group, times the group's scale
+        float sc[2][2] = {{0.f, 0.f}, {0.f, 0.f}}, ks[2][G], vs[2][G];
+        lds_scales<G>(tile + ksb, ks[0]);
+        lds_scales<G>(tile + ksb + 4 * G, ks[1]);
+        lds_scales<G>(tile + ksb + Tile::kSide, vs[0]);
+        lds_scales<G>(tile + ksb + Tile::kSide + 4 * G, vs[1]);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            sc[i][0] = sc[i][1] = 0.f;
-            const int t = key_token + 2 * i;
-            const uint32_t flags = tile + Tile::kCodes + t * FPR + (q * 16) / GS;
+        for (int g = 0; g < G; ++g) {
+            uint32_t k[2][2][4];  // token, word
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const uint2 c = lds64(tile + Tile::key_at(t, g * 2 + (q >> 1)) + (q & 1) * 8);
-                const uint32_t f = GS == 8 ? lds16(flags + g * 8) : lds8(flags + g * (64 / GS));
+            for (int i = 0; i < 2; ++i) {
+                const uint2 c = lds64(tile + key_off(i, g));
+                const uint32_t f = GS == 8 ? lds16(tile + kfb + 2 * i * FPR + g * 8) : lds8(tile + kfb + 2 * i * FPR + g * (64 / GS));
                 const uint32_t f0 = (GS == 8 ? f & 0xFFu : f) * 0x04000400u;
-                const uint32_t f1 = GS == 8 ? (f >> 8) * 0x04000400u : f0;
-                float s[4] = {0.f, 0.f, 0.f, 0.f};
-                uint32_t k[4];
-                uint4 w = kQRegs ? qf[kQRegs ? g : 0][0] : query(g, 0);
-                key_codes(c.x, f0, k);
-                mma16<false>(s, w.x, w.x, w.y, w.y, k[0], k[1]);
-                mma16<false>(s, w.z, w.z, w.w, w.w, k[2], k[3]);
-                w = kQRegs ? qf[kQRegs ? g : 0][1] : query(g, 1);
-                key_codes(c.y, f1, k);
-                mma16<false>(s, w.x, w.x, w.y, w.y, k[0], k[1]);
-                mma16<false>(s, w.z, w.z, w.w, w.w, k[2], k[3]);
-                sc[i][0] += s[0] * ks[2 * i][g];
-                sc[i][1] += s[1] * ks[2 * i + 1][g];
+                key_codes(c.x, f0, k[i][0]);
+                key_codes(c.y, GS == 8 ? (f >> 8) * 0x04000400u : f0, k[i][1]);
             }
+            float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                const uint4 qw = kQRegs ? qf[kQRegs ? g : 0][w] : query(g, w);
+                mma16<false>(s, k[0][w][0], k[1][w][0], k[0][w][1], k[1][w][1], qw.x, qw.y);
+                mma16<false>(s, k[0][w][2], k[1][w][2], k[0][w][3], k[1][w][3], qw.z, qw.w);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) sc[i][0] += s[2 * i] * ks[i][g], sc[i][1] += s[2 * i + 1] * ks[i][g];
         }
+
 #pragma unroll
         for (int i = 0; i < 2; ++i) sc[i][0] *= a.scale_log2, sc[i][1] *= a.scale_log2;
-
-        float vs[4][G];
-        lds_scales<G>(tile + Tile::kSide + Tile::kCodes + Tile::kFlags + q * 8 * G, vs);
-        const uint32_t vflags = tile + Tile::kSide + Tile::kCodes + 4 * q * FPR + (n * 8) / GS;
-        uint32_t vf[2][G];  // FLAGs of token pairs
+        uint32_t vf[2][G];  // FLAGs of token pairs 4 q, 4 q + 1 and 4 q + 2, 4 q + 3
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int g = 0; g < G; ++g)
-                vf[i][g] = lds8(vflags + 2 * i * FPR + g * (64 / GS)) + (lds8(vflags + (2 * i + 1) * FPR + g * (64 / GS)) << 16);
+                vf[i][g] = lds8(tile + vfb + 2 * i * FPR + g * (64 / GS)) + (lds8(tile + vfb + (2 * i + 1) * FPR + g * (64 / GS)) << 16);
         if (base + 16 > end || base < range.first) {
             // tokens that are not seen: no weight, and nothing of what their
             // slots happen to hold (a scale may be NaN)
+            auto unseen = [&](int t) { return base + t >= end || base + t < range.first; };
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int t = base + 4 * q + j;
-                if (t >= end || t < range.first) {
-                    sc[j / 2][j % 2] = -INFINITY;
+            for (int i = 0; i < 2; ++i)
+                if (unseen(key_token + 2 * i)) {
+                    sc[i][0] = sc[i][1] = -INFINITY;
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        vs[j][g] = 0.f;
-                        vf[j / 2][g] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-                    }
+                    for (int g = 0; g < G; ++g) vs[i][g] = 0.f;
                 }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (unseen(4 * q + j)) {
+#pragma unroll
+                    for (int g = 0; g < G; ++g) vf[j / 2][g] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
+                }
+        }
+        if (a.scores) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (head0 + 2 * q + x < a.group)
+                        a.scores[score_row + x * a.score_stride + (base - range.base) + key_token + 2 * i] = sc[i][x];
+        }
+        // weights 2^(score - m); m follows when a score passes it by 8
+        float p[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) p[i][x] = sc[i][x] - m[x];
+        if (__any_sync(0xffffffffu, fmaxf(fmaxf(p[0][0], p[0][1]), fmaxf(p[1][0], p[1][1])) > 8.f)) {
+            float f[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float top = fmaxf(m[x], fmaxf(sc[0][x], sc[1][x]));
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                f[x] = ex2(m[x] - top);
+                m[x] = top;
+                l[x] *= f[x];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) p[i][x] = sc[i][x] - top;
             }
+            const float f0 = __shfl_sync(0xffffffffu, f[0], n >> 1), f1 = __shfl_sync(0xffffffffu, f[1], n >> 1);
+            const float fn = n & 1 ? f1 : f0;  // of head n, the accumulators' row
+#pragma unroll
+            for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) st.o[i][j] *= fn;
         }
-        if (score_row) {
-            float *to = score_row + (base - range.base) + 4 * q;
-            *reinterpret_cast<float4 *>(to) = make_float4(sc[0][0], sc[0][1], sc[1][0], sc[1][1]);
-        }
-        st.template weigh<2>(sc, 0.f, 8.f);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                p[i][x] = ex2(p[i][x]);
+                l[x] += p[i][x];
+            }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             uint32_t hi[2], lo[2], v0[8], v1[8], c[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) c[j] = lds32(tile + Tile::kSide + Tile::value_at(4 * q + j, g * 2 + (n >> 2)) + (n & 3) * 4);
+            for (int j = 0; j < 4; ++j) c[j] = lds32(tile + value_off(j, g));
 #pragma unroll
-            for (int i = 0; i < 2; ++i) split_pair<true>(sc[i][0] * vs[2 * i][g], sc[i][1] * vs[2 * i + 1][g], hi[i], lo[i]);
+            for (int i = 0; i < 2; ++i) {
+                split_pair<true>(p[i][0] * vs[i][g], p[i][1] * vs[i][g], hi[i], lo[i]);
+                hi[i] = transposed(hi[i]);
+                lo[i] = transposed(lo[i]);
+            }
             value_codes(c[0], c[1], vf[0][g], v0);
             value_codes(c[2], c[3], vf[1][g], v1);
 #pragma unroll
             for (int j = 0; j < 8; ++j) mma16<true>(st.o[g * 8 + j], hi[0], lo[0], hi[1], lo[1], v0[j], v1[j]);
         }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+#pragma unroll
+        for (int d = 4; d < 32; d *= 2) l[x] += __shfl_xor_sync(0xffffffffu, l[x], d);
+        if (n == 0) s_join.m[warp][2 * q + x] = m[x], s_join.l[warp][2 * q + x] = l[x];
     }
     paged_wait<0>();
     __syncwarp();
@@ -386,7 +470,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 
 template <int D, int GS>
 struct KernelLzs {
-    static constexpr int MINB = D <= 64 ? 4 : D <= 128 ? 3 : 2;
+    static constexpr int MINB = D <= 64 ? 5 : D <= 128 ? 3 : 2;
     static constexpr int kSmem = kPagedWarps * LzsTile<D, GS>::kStages * LzsTile<D, GS>::kBytes;
     static cudaError_t ready()
     {
