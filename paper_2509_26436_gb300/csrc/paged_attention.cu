@@ -9,18 +9,43 @@
 namespace quartz {
 namespace {
 
-// Query rows of the CTA's heads, 16 bits, rows of D + 8: the 16-byte reads of
-// the eight heads' lanes then fall into different banks.
-template <int D, int NT, bool BF, int MINB>
-__global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_kernel(PagedArgs a)
+// A warp's ring of tiles: 16 rows of keys, then of values, D elements each, as
+// 16-byte chunks.  Chunk c of row t sits at c ^ (t % 8) (in its group of 8), so
+// that the matrix loads, which read one chunk of 8 rows, hit all banks.
+template <int D>
+struct Tile16 {
+    static constexpr int kChunks = D / 8, kRow = D * 2, kSide = 16 * kRow, kBytes = 2 * kSide;
+    static constexpr int kPerLane = 16 * kChunks / 32;  // chunks a lane copies, each side
+    // Stages and CTAs per SM so that some 128 KB per SM are on their way.
+    static constexpr int kStages = D == 192 ? 4 : 3, kCtas = D == 64 ? 4 : D == 128 ? 2 : 1;
+    __device__ static constexpr int at(int t, int c) { return t * kRow + (((c & ~7) | ((c ^ t) & 7)) << 4); }
+};
+
+__device__ __forceinline__ void ldmatrix4(uint32_t a, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(a));
+}
+__device__ __forceinline__ void ldmatrix4_trans(uint32_t a, uint32_t (&r)[4])
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(a));
+}
+
+template <int D, bool BF>
+__global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_kernel(PagedArgs a)
 {
     griddep_wait();
-    constexpr int TILE = 8 * NT, KC = D / 32, VC = D / 64;
+    using Tile = Tile16<D>;
+    constexpr int kStages = Tile::kStages, kWarpBytes = kStages * Tile::kBytes;
     constexpr bool kQRegs = D <= 128;  // wider heads read the query from shared memory again for each tile
     constexpr float kUp = BF ? 0.f : 13.f, kSlack = BF ? 8.f : 2.f;  // 2^(up + slack) fits fp16
+    static_assert(kWarpBytes >= kPagedJoinBytes<D>, "the join uses the ring");
+    extern __shared__ __align__(16) uint8_t s_ring[];
     __shared__ __align__(16) uint16_t s_q[kPagedHeads][D + 8];
     __shared__ PagedJoin s_join;
-    __shared__ __align__(16) uint8_t s_o[kPagedWarps][kPagedJoinBytes<D>];
 
     const int head_block = blockIdx.x % a.head_blocks, split = blockIdx.x / a.head_blocks;
     const int kv_head = blockIdx.y, b = blockIdx.z, head0 = head_block * kPagedHeads;
@@ -29,142 +54,150 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_kernel(PagedAr
     const int begin = split * a.chunk;
     if (a.part_o && begin >= range.count()) return;
     const int end = range.base + min(begin + a.chunk, range.count());  // first token behind the split
+    const int base0 = range.base + begin + warp * 16;
+    const int tiles = base0 < end ? (end - base0 + kPagedWarps * 16 - 1) / (kPagedWarps * 16) : 0;
+    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + warp * kWarpBytes;
 
-    for (int e = threadIdx.x; e < kPagedHeads * (D / 8); e += kPagedThreads) {
-        const int h = e / (D / 8), d = (e - h * (D / 8)) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (head0 + h < a.group)
-            v = *reinterpret_cast<const uint4 *>(a.q + b * a.q_sb + (static_cast<int64_t>(kv_head) * a.group + head0 + h) * a.q_sh + d);
-        *reinterpret_cast<uint4 *>(&s_q[h][d]) = v;
-    }
-    __syncthreads();
-    uint4 qf[kQRegs ? KC : 1];
-    if (kQRegs)
-#pragma unroll
-        for (int c = 0; c < KC; ++c) qf[c] = *reinterpret_cast<const uint4 *>(&s_q[n][(c * 4 + q) * 8]);
-
+    // --- copies of a tile: a lane takes chunks lane + 32 k.  Tokens that are not
+    // seen repeat the nearest that is: nothing of theirs, which may be infinite
+    // or NaN, meets a weight of 0.
     const int32_t *table = a.table + b * a.table_stride;
-    const int mask = (1 << a.page_shift) - 1;
-    const uint16_t *kbase = reinterpret_cast<const uint16_t *>(a.k.data) + kv_head * a.k.stride_head + q * 8;
-    const uint16_t *vbase = reinterpret_cast<const uint16_t *>(a.v.data) + kv_head * a.v.stride_head + n * 8;
+    const uint32_t page_mask = (1u << a.page_shift) - 1;
+    const uint16_t *kbase = reinterpret_cast<const uint16_t *>(a.k.data) + kv_head * a.k.stride_head;
+    const uint16_t *vbase = reinterpret_cast<const uint16_t *>(a.v.data) + kv_head * a.v.stride_head;
     bool bad = false;
-    // page of token base + (lane mod TILE); past the end: the last token's
-    auto page_of = [&](int base) {
-        const int t = min(base + (lane & (TILE - 1)), end - 1);
-        const uint32_t page = static_cast<uint32_t>(table[t >> a.page_shift]);
+    auto seen = [&](int t) { return max(min(t, end - 1), range.first); };
+    // page of token base + lane % 16
+    auto pages_of = [&](int base) {
+        const uint32_t page = static_cast<uint32_t>(__ldg(table + (seen(base + (lane & 15)) >> a.page_shift)));
         bad |= page >= a.num_pages;
         return page < a.num_pages ? page : 0u;
     };
-    auto row_of = [&](const uint16_t *p, const PagedSide &s, uint32_t pages, int base, int i) {
-        const uint32_t page = __shfl_sync(0xffffffffu, pages, i);
-        const uint32_t slot = static_cast<uint32_t>(min(base + i, end - 1)) & mask;
-        return p + (static_cast<uint64_t>(page) * s.stride_page + static_cast<uint64_t>(slot) * s.stride_slot);
-    };
-    uint4 kf[NT][KC];
-    auto load_k = [&](uint32_t pages, int base) {
+    auto fetch = [&](int base, uint32_t pages, int stage) {
+        const uint32_t to = ring + stage * Tile::kBytes;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            const uint16_t *p = row_of(kbase, a.k, pages, base, (n >> 1) * 2 * NT + 2 * i + (n & 1));
-#pragma unroll
-            for (int c = 0; c < KC; ++c) kf[i][c] = __ldg(reinterpret_cast<const uint4 *>(p + c * 32));
+        for (int k = 0; k < Tile::kPerLane; ++k) {
+            const int i = lane + 32 * k, t = i / Tile::kChunks, c = i % Tile::kChunks;
+            const uint64_t page = __shfl_sync(0xffffffffu, pages, t);
+            const uint64_t slot = static_cast<uint32_t>(seen(base + t)) & page_mask;
+            paged_copy16(to + Tile::at(t, c), kbase + (page * a.k.stride_page + slot * a.k.stride_slot) + c * 8);
+            paged_copy16(to + Tile::kSide + Tile::at(t, c), vbase + (page * a.v.stride_page + slot * a.v.stride_slot) + c * 8);
         }
     };
+    uint32_t next_pages = 0;  // of the next tile to fetch
+#pragma unroll
+    for (int s = 0; s < kStages - 1; ++s) {
+        if (s < tiles) fetch(base0 + s * kPagedWarps * 16, pages_of(base0 + s * kPagedWarps * 16), s);
+        paged_commit();
+    }
+    if (kStages - 1 < tiles) next_pages = pages_of(base0 + (kStages - 1) * kPagedWarps * 16);
 
+    // --- the query: per 16 elements, lane q of a head holds 2 q, 2 q + 1 and 2 q
+    // + 8, 2 q + 9, which are stored side by side
+    for (int e = threadIdx.x; e < kPagedHeads * (D / 16); e += kPagedThreads) {
+        const int h = e / (D / 16), d = (e - h * (D / 16)) * 16;
+        uint4 v = make_uint4(0, 0, 0, 0), w = v;
+        if (head0 + h < a.group) {
+            const uint4 *p = reinterpret_cast<const uint4 *>(a.q + b * a.q_sb + (static_cast<int64_t>(kv_head) * a.group + head0 + h) * a.q_sh + d);
+            v = p[0], w = p[1];
+        }
+        *reinterpret_cast<uint4 *>(&s_q[h][d]) = make_uint4(v.x, w.x, v.y, w.y);
+        *reinterpret_cast<uint4 *>(&s_q[h][d + 8]) = make_uint4(v.z, w.z, v.w, w.w);
+    }
+    __syncthreads();
+    auto query = [&](int c) { return *reinterpret_cast<const uint2 *>(&s_q[n][c * 16 + q * 4]); };
+    uint2 qf[kQRegs ? D / 16 : 1];
+    if (kQRegs)
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) qf[c] = query(c);
+
+    // matrix loads: lane l gives the address of row l % 8 of block l / 8; keys:
+    // blocks (tokens 0-7, 8-15) x (first, second 8 of 16 dimensions), values:
+    // the same blocks, transposed
+    const int ld_row = lane & 15, ld_col = lane >> 4;
     PagedState<D> st;
     st.init();
-    int base = range.base + begin + warp * TILE;
-    uint32_t pages = 0, next_pages = 0;
-    if (base < end) {
-        pages = page_of(base);
-        load_k(pages, base);
-        if (base + kPagedWarps * TILE < end) next_pages = page_of(base + kPagedWarps * TILE);
-    }
-    float *score_row = a.scores && head0 + n < a.group
-                           ? a.scores + ((static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0 + n) * a.score_stride
-                           : nullptr;
-    while (base < end) {
-        uint4 vf[2 * NT][VC];
-#pragma unroll
-        for (int j = 0; j < 2 * NT; ++j) {
-            const uint16_t *p = row_of(vbase, a.v, pages, base, 2 * NT * q + j);
-#pragma unroll
-            for (int c = 0; c < VC; ++c) vf[j][c] = __ldg(reinterpret_cast<const uint4 *>(p + c * 64));
-        }
-        float s[NT][4];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-#pragma unroll
-        for (int c = 0; c < KC; ++c) {
-            const uint4 w = kQRegs ? qf[kQRegs ? c : 0] : *reinterpret_cast<const uint4 *>(&s_q[n][(c * 4 + q) * 8]);
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                mma16<BF>(s[i], w.x, w.x, w.y, w.y, kf[i][c].x, kf[i][c].y);
-                mma16<BF>(s[i], w.z, w.z, w.w, w.w, kf[i][c].z, kf[i][c].w);
+    const int64_t score_row = ((static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0 + 2 * q) * a.score_stride;
+    int stage = 0;
+    for (int it = 0; it < tiles; ++it) {
+        const int base = base0 + it * kPagedWarps * 16;
+        paged_wait<kStages - 2>();
+        __syncwarp();
+        {
+            const int ahead = it + kStages - 1;
+            if (ahead < tiles) {
+                fetch(base0 + ahead * kPagedWarps * 16, next_pages, stage == 0 ? kStages - 1 : stage - 1);
+                if (ahead + 1 < tiles) next_pages = pages_of(base0 + (ahead + 1) * kPagedWarps * 16);
             }
+            paged_commit();
         }
-        const int next = base + kPagedWarps * TILE;
-        if (next < end) {
-            load_k(next_pages, next);
-            pages = next_pages;
-            if (next + kPagedWarps * TILE < end) next_pages = page_of(next + kPagedWarps * TILE);
+        const uint32_t tile = ring + stage * Tile::kBytes;
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+
+        float s[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};  // two chains
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+            uint32_t k[4];
+            ldmatrix4(tile + Tile::at(ld_row, 2 * c + ld_col), k);
+            const uint2 w = kQRegs ? qf[kQRegs ? c : 0] : query(c);
+            mma16<BF>(s[c & 1], k[0], k[1], k[2], k[3], w.x, w.y);
         }
-        float sc[NT][2];
+        float sc[2][2];  // tokens n and n + 8, heads 2 q and 2 q + 1
 #pragma unroll
-        for (int i = 0; i < NT; ++i) sc[i][0] = s[i][0] * a.scale_log2, sc[i][1] = s[i][1] * a.scale_log2;
-        if (base + TILE > end || base < range.first) {
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
+            for (int x = 0; x < 2; ++x) sc[i][x] = (s[0][2 * i + x] + s[1][2 * i + x]) * a.scale_log2;
+        if (base + 16 > end || base < range.first) {
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int t = base + 2 * NT * q + 2 * i + x;
-                    if (t >= end || t < range.first) sc[i][x] = -INFINITY;
-                }
+            for (int i = 0; i < 2; ++i)
+                if (base + n + 8 * i >= end || base + n + 8 * i < range.first) sc[i][0] = sc[i][1] = -INFINITY;
         }
-        if (score_row) {
-            float *to = score_row + (base - range.base) + 2 * NT * q;
+        if (a.scores) {
 #pragma unroll
-            for (int i = 0; i < NT; ++i) *reinterpret_cast<float2 *>(to + 2 * i) = make_float2(sc[i][0], sc[i][1]);
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+                    if (head0 + 2 * q + x < a.group)
+                        a.scores[score_row + x * a.score_stride + (base - range.base) + n + 8 * i] = sc[i][x];
         }
-        st.template weigh<NT>(sc, kUp, kSlack);
-        uint32_t hi[NT], lo[NT];
+        float p[2][2];
+        st.weigh(sc, p, kUp, kSlack);
+        uint32_t hi[2], lo[2];
 #pragma unroll
-        for (int i = 0; i < NT; ++i) split_pair<BF>(sc[i][0], sc[i][1], hi[i], lo[i]);
+        for (int i = 0; i < 2; ++i) {
+            split_pair<BF>(p[i][0], p[i][1], hi[i], lo[i]);
+            hi[i] = transposed(hi[i]);
+            lo[i] = transposed(lo[i]);
+        }
 #pragma unroll
-        for (int c = 0; c < VC; ++c)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                auto word = [&](int j) { return reinterpret_cast<const uint32_t *>(&vf[j][c])[e]; };
-                float(&o0)[4] = st.o[c * 8 + 2 * e], (&o1)[4] = st.o[c * 8 + 2 * e + 1];
-                if (NT == 2) {
-                    mma16<BF>(o0, hi[0], lo[0], hi[NT - 1], lo[NT - 1], permute(word(0), word(1), 0x5410),
-                              permute(word(2 * NT - 2), word(2 * NT - 1), 0x5410));
-                    mma16<BF>(o1, hi[0], lo[0], hi[NT - 1], lo[NT - 1], permute(word(0), word(1), 0x7632),
-                              permute(word(2 * NT - 2), word(2 * NT - 1), 0x7632));
-                } else {
-                    mma8<BF>(o0, hi[0], lo[0], permute(word(0), word(1), 0x5410));
-                    mma8<BF>(o1, hi[0], lo[0], permute(word(0), word(1), 0x7632));
-                }
-            }
-        base = next;
+        for (int c = 0; c < D / 16; ++c) {
+            uint32_t v[4];
+            ldmatrix4_trans(tile + Tile::kSide + Tile::at(ld_row, 2 * c + ld_col), v);
+            mma16<BF>(st.o[2 * c], hi[0], lo[0], hi[1], lo[1], v[0], v[1]);
+            mma16<BF>(st.o[2 * c + 1], hi[0], lo[0], hi[1], lo[1], v[2], v[3]);
+        }
     }
+    paged_wait<0>();
+    __syncwarp();
     if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
-    st.l += __shfl_xor_sync(0xffffffffu, st.l, 1);
-    st.l += __shfl_xor_sync(0xffffffffu, st.l, 2);
-    if (q == 0) s_join.m[warp][n] = st.m, s_join.l[warp][n] = st.l;
-    paged_finish<D>(s_join, s_o[0], sizeof(s_o[0]), st, a, b, kv_head, head0, split, kUp);
+    paged_finish<D, false>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, kUp);
 }
 
 template <int D, bool BF>
 struct Kernel16 {
-    static constexpr int NT = D <= 128 ? 2 : 1, MINB = D <= 128 ? 3 : 2;
+    static constexpr int kSmem = kPagedWarps * Tile16<D>::kStages * Tile16<D>::kBytes;
+    static cudaError_t ready()
+    {
+        return cudaFuncSetAttribute(paged_attn_kernel<D, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    }
     static int occupancy()
     {
         static std::atomic<int> cache{0};
         int occ = cache.load(std::memory_order_relaxed);
         if (occ == 0) {
             int k = 0;
-            if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, paged_attn_kernel<D, NT, BF, MINB>, kPagedThreads, 0) !=
-                cudaSuccess)
+            if (ready() != cudaSuccess || cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, paged_attn_kernel<D, BF>, kPagedThreads,
+                                                                                        kSmem) != cudaSuccess)
                 return 1;
             occ = k > 0 ? k : 1;
             cache.store(occ, std::memory_order_relaxed);
@@ -173,7 +206,9 @@ struct Kernel16 {
     }
     static cudaError_t launch(const PagedArgs &a, dim3 grid, cudaStream_t s)
     {
-        return launch_pdl(paged_attn_kernel<D, NT, BF, MINB>, grid, dim3(kPagedThreads), 0, s, a);
+        const cudaError_t e = ready();  // of the current device
+        if (e != cudaSuccess) return e;
+        return launch_pdl(paged_attn_kernel<D, BF>, grid, dim3(kPagedThreads), kSmem, s, a);
     }
 };
 
@@ -210,7 +245,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a)
     __syncthreads();
     float sum = 0.f;
     for (int i = tid; i < splits; i += 256) {
-        const float f = m == -INFINITY ? 0.f : ex2(ml[2 * i] - m);
+        const float f = ex2(ml[2 * i] - m);
         s_f[i] = f;
         sum += f * ml[2 * i + 1];
     }

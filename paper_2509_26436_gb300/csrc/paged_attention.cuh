@@ -3,24 +3,21 @@
 //
 // A CTA takes one sequence, one key / value head, up to 8 of the query heads
 // that share it and one split (a run of consecutive tokens); its 4 warps take
-// tiles of 8 NT tokens in turn.  The products run on the warp-level tensor
-// instruction m16n8k16 with fp32 accumulators:
-//   S = Q K^T:  A rows 0-7 and again 8-15 = the query heads; B column n =
-//               token.  The order of the head dimension inside the
-//               contraction is free, so each lane loads 16 (or 8) consecutive
-//               bytes of its token's row straight into B fragments: keys need
-//               no shared memory, no transpose and no barrier.
-//   O += P V:   A rows 0-7 = the upper 16 bits of the softmax weights, rows
-//               8-15 = what is left of them, rounded again: the accumulator's
+// tiles of 16 tokens in turn, each through a ring in shared memory of its own
+// that asynchronous copies fill some tiles ahead, so no warp waits for
+// another.  The products run on the warp-level tensor instruction m16n8k16
+// with fp32 accumulators:
+//   S' = K Q':  rows: 16 tokens, columns: 8 heads;
+//   O += P V:   rows 0-7: the upper 16 bits of the heads' softmax weights, rows
+//               8-15: what is left of them, rounded again; the accumulator's
 //               lower half, added at the end, makes the weights good to twice
 //               the 16-bit type's precision, in rows that eight heads leave
-//               free anyway.  B column n = a piece of 8 (of each 64) head
-//               dimensions; its rows are tokens, so the four lanes of a column
-//               hold consecutive tokens and pair them with byte permutes.
-// The scores' accumulator layout is the weights' operand layout (lane = head
-// lane/4, tokens 2 NT (lane%4) ...), so the softmax stays in registers.
-// Legacy tensor instructions are enough here: the step is bound by HBM, the
-// tensor pipe has to keep up with one product pair per loaded row only.
+//               free anyway.
+// The scores arrive transposed to what the second product takes: one register
+// transpose (movmatrix) per 8 x 8 block of 16-bit weights, nothing through
+// shared memory.  Legacy tensor instructions are enough here: the step is
+// bound by HBM (or, encoded, by the decoding), and the tensor pipe has to keep
+// up with one pair of products per loaded row only.
 #pragma once
 
 #include <cstdint>
@@ -101,7 +98,7 @@ __device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel
     return d;
 }
 
-// d += A B, 16 x 8 x 16 (or 16 x 8 x 8 with one B register).
+// d += A B, 16 x 8 x 16.
 template <bool BF>
 __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                       uint32_t b1)
@@ -114,19 +111,6 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-template <bool BF>
-__device__ __forceinline__ void mma8(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t b0)
-{
-    if (BF)
-        asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a0), "r"(a1), "r"(b0));
-    else
-        asm("mma.sync.aligned.m16n8k8.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%0,%1,%2,%3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a0), "r"(a1), "r"(b0));
 }
 
 // Two weights as a 16-bit pair and the pair of what the rounding left.
@@ -156,13 +140,14 @@ __device__ __forceinline__ void paged_commit() { asm volatile("cp.async.commit_g
 template <int N>
 __device__ __forceinline__ void paged_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// A warp's accumulators and its running softmax where a lane holds scores of
-// head lane / 4: m is the head's maximum (log2 domain), l this lane's part of
-// the sum of weights.
+// A warp's accumulators (rows: heads; 8 columns of the head dimension per
+// entry) and its running softmax.  A lane holds the scores of two tokens and
+// heads 2 q and 2 q + 1 (q = lane % 4): m are their maxima so far (log2 domain),
+// which all lanes of a head share, l this lane's part of the sums of weights.
 template <int D>
 struct PagedState {
     float o[D / 8][4];
-    float m, l;
+    float m[2], l[2];
 
     __device__ __forceinline__ void init()
     {
@@ -170,40 +155,60 @@ struct PagedState {
         for (int i = 0; i < D / 8; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
-        m = -INFINITY;
-        l = 0.f;
+        m[0] = m[1] = -1e30f;
+        l[0] = l[1] = 0.f;
     }
 
-    // Scores sc (log2 domain, -inf where masked) to weights 2^(sc - m + up);
-    // `up` keeps small weights of a 16-bit type with few exponent bits normal.
-    // The maximum follows only when it is passed by more than `slack`: a weight
-    // of 2^slack does no harm, and eight heads pass their maxima by little in
-    // every other tile, while a rescale touches every accumulator.
-    template <int NT>
-    __device__ __forceinline__ void weigh(float (&sc)[NT][2], float up, float slack)
+    // Scores sc[token][head] (log2 domain, -inf where masked) to weights
+    // p = 2^(sc - m + up).  The maximum follows only when a score passes it by
+    // more than `slack`: a weight of 2^slack does no harm, and then no lane
+    // has to hear of the others' scores, and no accumulator to be rescaled, in
+    // most tiles.  `up` keeps small weights of fp16 normal.
+    __device__ __forceinline__ void weigh(const float (&sc)[2][2], float (&p)[2][2], float up, float slack)
     {
-        float mx = fmaxf(sc[0][0], sc[0][1]);
-        if (NT == 2) mx = fmaxf(mx, fmaxf(sc[NT - 1][0], sc[NT - 1][1]));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        if (__any_sync(0xffffffffu, mx > m + slack)) {
-            const float m_new = fmaxf(m, mx), f = ex2(m - m_new);
-            m = m_new;
-            l *= f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) p[i][x] = sc[i][x] - m[x];
+        if (__any_sync(0xffffffffu, fmaxf(fmaxf(p[0][0], p[0][1]), fmaxf(p[1][0], p[1][1])) > slack)) {
+            const int n = (threadIdx.x & 31) >> 2;
+            float f[2];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                float top = fmaxf(m[x], fmaxf(sc[0][x], sc[1][x]));
+#pragma unroll
+                for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                f[x] = ex2(m[x] - top);
+                m[x] = top;
+                l[x] *= f[x];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) p[i][x] = sc[i][x] - top;
+            }
+            const float f0 = __shfl_sync(0xffffffffu, f[0], n >> 1), f1 = __shfl_sync(0xffffffffu, f[1], n >> 1);
+            const float fn = n & 1 ? f1 : f0;  // of head n, the accumulators' row
 #pragma unroll
             for (int i = 0; i < D / 8; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o[i][j] *= f;
+                for (int j = 0; j < 4; ++j) o[i][j] *= fn;
         }
-        const float off = up - m;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            sc[i][0] = ex2(sc[i][0] + off);
-            sc[i][1] = ex2(sc[i][1] + off);
-            l += sc[i][0] + sc[i][1];
-        }
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                p[i][x] = ex2(up == 0.f ? p[i][x] : p[i][x] + up);
+                l[x] += p[i][x];
+            }
     }
 };
+
+// The transpose of an 8 x 8 block of 16-bit values, lane = row lane / 4,
+// columns 2 (lane % 4) and the next.
+__device__ __forceinline__ uint32_t transposed(uint32_t v)
+{
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
+    return d;
+}
 
 template <typename T> __device__ __forceinline__ void paged_store4(void *o, int64_t at, float4 v);
 template <> __device__ __forceinline__ void paged_store4<float>(void *o, int64_t at, float4 v)
@@ -236,13 +241,15 @@ struct PagedJoin {
     float m[kPagedWarps][kPagedHeads], l[kPagedWarps][kPagedHeads];
 };
 
-// The warps have left their heads' maxima and sums in `s`; `smem` + warp *
-// warp_bytes is the warp's own shared memory, at least kPagedJoinBytes<D>,
-// free by now.
+// `smem` + warp * warp_bytes is the warp's own shared memory, at least
+// kPagedJoinBytes<D>, free by now.
 template <int D>
 constexpr int kPagedJoinBytes = kPagedHeads * (D + 4) * 4;
 
-template <int D>
+//
+// The accumulators' column 2 q + x of entry i is dimension 8 i + 2 q + x, or
+// (STRIDED) (i / 8) 64 + (2 q + x) 8 + i % 8.
+template <int D, bool STRIDED>
 __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int warp_bytes, PagedState<D> &st,
                                              const PagedArgs &a, int b, int kv_head, int head0, int split, float up)
 {
@@ -251,15 +258,28 @@ __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int wa
     };
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
 #pragma unroll
-    for (int hv = 0; hv < D / 64; ++hv)
+    for (int x = 0; x < 2; ++x) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int d = 4; d < 32; d *= 2) st.l[x] += __shfl_xor_sync(0xffffffffu, st.l[x], d);
+        if (n == 0) s.m[warp][2 * q + x] = st.m[x], s.l[warp][2 * q + x] = st.l[x];
+    }
+    if constexpr (STRIDED) {
 #pragma unroll
-            for (int j = 0; j < 8; j += 4) {
-                const float(*o)[4] = &st.o[hv * 8 + j];
-                *so(warp, n, hv * 64 + (2 * q + x) * 8 + j) =
-                    make_float4(o[0][x] + o[0][x + 2], o[1][x] + o[1][x + 2], o[2][x] + o[2][x + 2], o[3][x] + o[3][x + 2]);
-            }
+        for (int hv = 0; hv < D / 64; ++hv)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int j = 0; j < 8; j += 4) {
+                    const float(*o)[4] = &st.o[hv * 8 + j];
+                    *so(warp, n, hv * 64 + (2 * q + x) * 8 + j) =
+                        make_float4(o[0][x] + o[0][x + 2], o[1][x] + o[1][x + 2], o[2][x] + o[2][x + 2], o[3][x] + o[3][x + 2]);
+                }
+    } else {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i)
+            *reinterpret_cast<float2 *>(so(warp, n, 8 * i + 2 * q)) =
+                make_float2(st.o[i][0] + st.o[i][2], st.o[i][1] + st.o[i][3]);
+    }
     __syncthreads();
     const int64_t row0 = (static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0;
     for (int e = threadIdx.x; e < kPagedHeads * (D / 4); e += kPagedThreads) {
@@ -272,7 +292,7 @@ __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int wa
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < kPagedWarps; ++w) {
-            const float f = m == -INFINITY ? 0.f : ex2(s.m[w][h] - m - up);
+            const float f = ex2(s.m[w][h] - m - up);
             const float4 u = *so(w, h, d);
             sum += f * s.l[w][h];
             v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;

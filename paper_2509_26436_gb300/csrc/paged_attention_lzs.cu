@@ -16,11 +16,9 @@
 //   values (bf16, so that a weight times a scale, whatever its size, keeps its
 //     8 bits; with the remainder 16): words of two tokens are paired by halves
 //     first, since an operand register holds two tokens of one column.
-// The keys are the first operand here (S' = K Q', 16 tokens x 8 heads per
-// instruction: every row used, and its four registers are two decoded words
-// as they come), so the scores arrive transposed: lane = tokens of row n and n
-// + 8, heads 2 q and 2 q + 1.  The 16-bit weights change sides with one
-// register transpose (movmatrix) per 8 x 8 block.
+// The contraction over the head dimension may take it in any order, so a
+// lane's 8 consecutive bytes of codes go into the operand's registers as they
+// unpack, and the query is permuted to match, once.
 #include <atomic>
 
 #include "paged_attention.cuh"
@@ -147,15 +145,6 @@ __device__ __forceinline__ uint32_t fixed(uint32_t v)
     return v;
 }
 
-// The transpose of an 8 x 8 block of 16-bit values, lane = row lane / 4,
-// columns 2 (lane % 4) and the next.
-__device__ __forceinline__ uint32_t transposed(uint32_t v)
-{
-    uint32_t d;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(v));
-    return d;
-}
-
 // The G scales of a row of the tile.
 template <int G>
 __device__ __forceinline__ void lds_scales(uint32_t a, float (&s)[G])
@@ -227,8 +216,9 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
         small_row[k] = in ? (flag ? FPR : 2 * G) : -1;
         small_dst[k] = side * Tile::kSide + Tile::kCodes + i * 16;
     }
+    auto seen = [&](int t) { return max(min(t, end - 1), range.first); };
     auto page_of = [&](int t) {
-        const uint32_t page = static_cast<uint32_t>(__ldg(table + (min(t, end - 1) >> a.page_shift)));
+        const uint32_t page = static_cast<uint32_t>(__ldg(table + (seen(t) >> a.page_shift)));
         bad |= page >= a.num_pages;
         return page < a.num_pages ? page : 0u;
     };
@@ -238,7 +228,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     const bool small_pages = a.page_shift < 4;
     // Pages of 16 or more: 16 consecutive rows.  Smaller ones: row by row; the
     // small planes' rows are then below the 16 bytes of a copy and go through
-    // registers.  A token past the end repeats the last one.
+    // registers.  There a token that is not seen repeats the nearest that is.
     auto fetch = [&](int base, uint32_t page, int stage) {
         const uint32_t to = ring + stage * Tile::kBytes;
         if (!small_pages) {
@@ -254,7 +244,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
             for (int k = 0; k < Tile::kSmallPerLane; ++k)
                 if (small_row[k] >= 0) paged_copy16(to + small_dst[k], small_src[k] + row * small_row[k]);
         } else {
-            const int mine = min(base + (lane & 15), end - 1);
+            const int mine = seen(base + (lane & 15));
             const uint32_t my_row = row_of(page_of(mine), mine);
 #pragma unroll
             for (int k = 0; k < Tile::kCodesPerLane; ++k) {
@@ -324,9 +314,6 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 
     PagedState<D> st;
     st.init();
-    // of heads 2 q and 2 q + 1: a maximum that all their lanes share, and this
-    // lane's part of the sum of weights
-    float m[2] = {-1e30f, -1e30f}, l[2] = {0.f, 0.f};
     const int64_t score_row = ((static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0 + 2 * q) * a.score_stride;
     int stage = 0;
     for (int it = 0; it < tiles; ++it) {
@@ -406,39 +393,8 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
                     if (head0 + 2 * q + x < a.group)
                         a.scores[score_row + x * a.score_stride + (base - range.base) + key_token + 2 * i] = sc[i][x];
         }
-        // weights 2^(score - m); m follows when a score passes it by 8
         float p[2][2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) p[i][x] = sc[i][x] - m[x];
-        if (__any_sync(0xffffffffu, fmaxf(fmaxf(p[0][0], p[0][1]), fmaxf(p[1][0], p[1][1])) > 8.f)) {
-            float f[2];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                float top = fmaxf(m[x], fmaxf(sc[0][x], sc[1][x]));
-#pragma unroll
-                for (int d = 4; d < 32; d *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                f[x] = ex2(m[x] - top);
-                m[x] = top;
-                l[x] *= f[x];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) p[i][x] = sc[i][x] - top;
-            }
-            const float f0 = __shfl_sync(0xffffffffu, f[0], n >> 1), f1 = __shfl_sync(0xffffffffu, f[1], n >> 1);
-            const float fn = n & 1 ? f1 : f0;  // of head n, the accumulators' row
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) st.o[i][j] *= fn;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                p[i][x] = ex2(p[i][x]);
-                l[x] += p[i][x];
-            }
+        st.weigh(sc, p, 0.f, 8.f);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             uint32_t hi[2], lo[2], v0[8], v1[8], c[4];
@@ -456,16 +412,10 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
             for (int j = 0; j < 8; ++j) mma16<true>(st.o[g * 8 + j], hi[0], lo[0], hi[1], lo[1], v0[j], v1[j]);
         }
     }
-#pragma unroll
-    for (int x = 0; x < 2; ++x) {
-#pragma unroll
-        for (int d = 4; d < 32; d *= 2) l[x] += __shfl_xor_sync(0xffffffffu, l[x], d);
-        if (n == 0) s_join.m[warp][2 * q + x] = m[x], s_join.l[warp][2 * q + x] = l[x];
-    }
     paged_wait<0>();
     __syncwarp();
     if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
-    paged_finish<D>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, 0.f);
+    paged_finish<D, true>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, 0.f);
 }
 
 template <int D, int GS>
