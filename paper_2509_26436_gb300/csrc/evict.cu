@@ -3,12 +3,16 @@
 // the tokens between the `want` with the largest weights, equal weights by the
 // lowest index, as ascending indices.
 //
-// A radix select: each weight becomes a 32-bit key that orders like it, and
-// four passes count the keys that share the digits found so far by their next
-// eight bits, from the top, until the `want`-th largest key is known.  Two
-// more passes count and write what stays, in order.  The work is a few reads
-// of 4 bytes per token, so latency of the passes counts: the keys are read
-// from global memory once and held in shared memory where they fit.
+// Each weight becomes a 32-bit key that orders like it.  The range of the keys
+// is cut into 2048 equal buckets, their populations counted, and the bucket
+// that holds the `want`-th largest key becomes the next range, until a bucket
+// is one key: three passes at most, the later ones over the few keys that are
+// left.  (Cut by the range, not by fixed digits: sums of attention weights
+// share their leading bits, and as keys, which grow with the logarithm, they
+// spread evenly; lanes that meet in a bucket wait for each other.)  Two more
+// passes count and write what stays, in order.  The work is a few reads of 4
+// bytes per token, so the latency of the passes counts: the keys are read from
+// global memory once and held in shared memory where they fit.
 #include "quartz_internal.h"
 
 namespace quartz {
@@ -16,7 +20,7 @@ namespace {
 
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
-constexpr int kDigits = 256;
+constexpr int kBuckets = 2048;
 
 struct SelectArgs {
     const float *w;
@@ -41,9 +45,9 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
 {
     griddep_wait();
     extern __shared__ uint32_t s_keys[];
-    __shared__ uint32_t s_hist[kDigits];
+    __shared__ uint32_t s_hist[kBuckets];
     __shared__ uint32_t s_above[kWarps], s_equal[kWarps];
-    __shared__ uint32_t s_digit, s_left;
+    __shared__ uint32_t s_bucket, s_left;
     const int64_t bh = blockIdx.x;
     const int64_t b = bh / a.heads;
     const int h = static_cast<int>(bh - b * a.heads);
@@ -64,57 +68,71 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
     const float *w = a.w + b * a.w_sb + h * a.w_sh;
     const int lo = a.sinks, hi = len - a.recent;  // the tokens between
     uint32_t want = static_cast<uint32_t>(a.budget - a.sinks - a.recent);  // < hi - lo
-    if (HELD) {
-        for (int t = lo + tid; t < hi; t += kThreads) s_keys[t - lo] = order_key(w[t]);
-        __syncthreads();
+    const bool none = want == 0;  // only sinks and recent tokens stay
+    uint32_t top = 0, bottom = 0xffffffffu;
+    for (int t0 = lo + tid; t0 < hi; t0 += 4 * kThreads) {
+        float f[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = t0 + i * kThreads < hi ? w[t0 + i * kThreads] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t0 + i * kThreads < hi) {
+                const uint32_t key = order_key(f[i]);
+                if (HELD) s_keys[t0 + i * kThreads - lo] = key;
+                top = max(top, key);
+                bottom = min(bottom, key);
+            }
     }
+    top = __reduce_max_sync(0xffffffffu, top);
+    bottom = __reduce_min_sync(0xffffffffu, bottom);
+    if (lane == 0) s_above[warp] = top, s_equal[warp] = bottom;
+    __syncthreads();
+    top = __reduce_max_sync(0xffffffffu, s_above[lane]);
+    bottom = __reduce_min_sync(0xffffffffu, s_equal[lane]);
     auto key_at = [&](int t) { return HELD ? s_keys[t - lo] : order_key(w[t]); };
 
-    // the want-th largest key: `prefix` holds its digits found so far
-    uint32_t prefix = 0, mask = 0;
-    for (int shift = 24; shift >= 0 && want > 0; shift -= 8) {
-        for (int i = tid; i < kDigits; i += kThreads) s_hist[i] = 0;
+    // the want-th largest key is in [bottom, bottom + span]
+    uint32_t span = top - bottom;
+    while (span > 0 && !none) {
+        const int shift = max(0, 21 - __clz(span));  // span >> shift < 2048
+        for (int i = tid; i < kBuckets; i += kThreads) s_hist[i] = 0;
         __syncthreads();
-        for (int t0 = lo + warp * 32; t0 < hi; t0 += kThreads) {
-            const int t = t0 + lane;
-            const uint32_t key = t < hi ? key_at(t) : 0u;
-            const bool mine = t < hi && (key & mask) == prefix;
-            const uint32_t digit = mine ? (key >> shift) & 255u : kDigits;
-            // sums of attention weights share few leading digits: one addition
-            // for all lanes with the same
-            const uint32_t same = __match_any_sync(0xffffffffu, digit);
-            if (mine && lane == __ffs(same) - 1) atomicAdd(&s_hist[digit], __popc(same));
+#pragma unroll 4
+        for (int t = lo + tid; t < hi; t += kThreads) {
+            const uint32_t off = key_at(t) - bottom;
+            if (off <= span) atomicAdd(&s_hist[off >> shift], 1u);
         }
         __syncthreads();
-        if (warp == 0) {  // eight digits per lane, from the top
-            uint32_t c[8], sum = 0;
+        // two buckets per thread, from the top: how many keys lie above them
+        const uint32_t c0 = s_hist[kBuckets - 1 - 2 * tid], c1 = s_hist[kBuckets - 2 - 2 * tid];
+        uint32_t upto = c0 + c1;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                c[i] = s_hist[kDigits - 1 - (lane * 8 + i)];
-                sum += c[i];
-            }
-            uint32_t before = sum;
+        for (int d = 1; d < 32; d *= 2) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, upto, d);
+            if (lane >= d) upto += v;
+        }
+        if (lane == 31) s_above[warp] = upto;
+        __syncthreads();
+        uint32_t warps = s_above[lane];  // kWarps = 32
 #pragma unroll
-            for (int d = 1; d < 32; d *= 2) {
-                const uint32_t v = __shfl_up_sync(0xffffffffu, before, d);
-                if (lane >= d) before += v;
-            }
-            before -= sum;
-            if (before < want && want <= before + sum) {  // one lane
-                int i = 0;
-                while (want > before + c[i]) before += c[i++];
-                s_digit = kDigits - 1 - (lane * 8 + i);
-                s_left = want - before;
-            }
+        for (int d = 1; d < 32; d *= 2) {
+            const uint32_t v = __shfl_up_sync(0xffffffffu, warps, d);
+            if (lane >= d) warps += v;
+        }
+        upto += warp ? __shfl_sync(0xffffffffu, warps, (warp + 31) & 31) : 0u;
+        const uint32_t before = upto - c0 - c1;
+        if (before < want && want <= upto) {  // one thread
+            const bool second = want > before + c0;
+            s_bucket = kBuckets - 1 - 2 * tid - second;
+            s_left = want - before - (second ? c0 : 0u);
         }
         __syncthreads();
-        prefix |= s_digit << shift;
-        mask |= 255u << shift;
-        want = s_left;  // of those with this prefix
+        want = s_left;  // of those in the bucket
+        bottom += s_bucket << shift;
+        span = min((1u << shift) - 1, top - bottom);
+        __syncthreads();
     }
-    // now: keys above `prefix` stay, and the first `want` that equal it (none
-    // where only sinks and recent tokens stay: mask is still 0)
-    const bool none = mask == 0;
+    const uint32_t prefix = bottom;  // keys above stay, and the first `want` that equal it
 
     // each warp takes a run of consecutive tokens
     const int per = ((len + kWarps - 1) / kWarps + 31) & ~31;

@@ -55,92 +55,120 @@ __device__ __forceinline__ void pack16(const float (&f)[16], uint4 &lo, uint4 &h
     hi = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
+// A lane's unit of a row: 16 elements, and for keys that are rotated in halves
+// their 16 partners (read again as vectors where the unit lies in one half).
+struct RawUnit {
+    uint4 lo, hi, plo, phi;
+};
+
 // The 16 elements d0 .. d0 + 15 of a key row, rotated, in the type of the row
-// (one rounding, as the rotation by itself gives).  Pairs of halves take their
-// partner elements from the row again: as vectors where a unit lies in one
-// half, else one by one.
+// (one rounding, as the rotation by itself gives).
 template <typename T>
-__device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_rope_t &rope, const float2 *cs, uint4 &lo,
-                                            uint4 &hi)
+__device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_rope_t &rope, const float2 *cs, RawUnit &r)
 {
-    if (d0 >= rope.rotary) return;
     const int pairs = rope.rotary / 2;
     float x[16], y[16];
-    unpack16<T>(lo, hi, x);
+    unpack16<T>(r.lo, r.hi, x);
     if (rope.interleaved) {
 #pragma unroll
         for (int e = 0; e < 16; e += 2) {
             y[e] = x[e], y[e + 1] = x[e + 1];
             if (d0 + e < rope.rotary) {
-                const float2 r = rope_turn(x[e], x[e + 1], cs[(d0 + e) / 2]);
-                y[e] = r.x, y[e + 1] = r.y;
+                const float2 v = rope_turn(x[e], x[e + 1], cs[(d0 + e) / 2]);
+                y[e] = v.x, y[e + 1] = v.y;
             }
         }
-    } else {
+    } else if (pairs % 16 == 0) {
         float p[16];
-        if (pairs % 16 == 0) {
-            const uint4 *q = reinterpret_cast<const uint4 *>(row + (d0 < pairs ? d0 + pairs : d0 - pairs));
-            unpack16<T>(q[0], q[1], p);
+        unpack16<T>(r.plo, r.phi, p);
+        if (d0 < pairs) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) y[e] = rope_turn(x[e], p[e], cs[d0 + e]).x;
         } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int d = d0 + e;
-                p[e] = d < rope.rotary ? to_f32<T>(row[d < pairs ? d + pairs : d - pairs]) : 0.f;
-            }
+            for (int e = 0; e < 16; ++e) y[e] = rope_turn(p[e], x[e], cs[d0 - pairs + e]).y;
         }
+    } else {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             const int d = d0 + e;
             y[e] = x[e];
-            if (d < pairs) y[e] = rope_turn(x[e], p[e], cs[d]).x;
-            else if (d < rope.rotary) y[e] = rope_turn(p[e], x[e], cs[d - pairs]).y;
+            if (d < pairs) y[e] = rope_turn(x[e], to_f32<T>(row[d + pairs]), cs[d]).x;
+            else if (d < rope.rotary) y[e] = rope_turn(to_f32<T>(row[d - pairs]), x[e], cs[d - pairs]).y;
         }
     }
-    pack16<T>(y, lo, hi);
+    pack16<T>(y, r.lo, r.hi);
 }
 
-// One CTA per token; a lane takes 16 elements of a key or value row.  GS = 0:
-// 16-bit pages of type T; else encoded pages (T = __half, four lanes per
-// 64-element group, which never cross a row: dim is a multiple of 64).
+// A CTA goes through tokens; a lane has the same 16 elements of a key or value
+// row in all of them (blockIdx.y: further rows), and loads the next token's
+// while it works on this one's.  GS = 0: 16-bit pages of type T; else encoded
+// pages (T = __half, four lanes per 64-element group, which never cross a row:
+// dim is a multiple of 64).
 template <typename T, int GS>
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendCall c)
+__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendCall c, int tokens)
 {
     griddep_wait();
-    __shared__ float2 s_cs[kMaxPairs];
-    const int64_t t = blockIdx.x;
-    const int64_t slot = c.a.slots[t];
-    if (slot < 0) return;
-    if (slot >= c.slots_total) {
-        if (threadIdx.x == 0) atomicExch(c.a.dev_err, QUARTZ_DEV_INDEX);
-        return;
-    }
-    const int64_t page = slot >> c.page_shift, in_page = slot - (page << c.page_shift);
+    __shared__ float2 s_cs[2][kMaxPairs];
+    __shared__ uint64_t s_unit[kMaxPairs];
     const bool rope = c.a.rope.positions != nullptr;
-    if (rope) {
-        const int64_t pos = c.a.rope.positions[t];
-        for (int i = threadIdx.x; i < c.a.rope.rotary / 2; i += blockDim.x)
-            s_cs[i] = rope_cos_sin(pos, c.a.rope.freqs[i], c.a.rope.scale);
-        __syncthreads();
-    }
-    const int side_units = c.heads * c.units, total = 2 * side_units, lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < ((total + 31) & ~31); i += blockDim.x) {
-        const bool in = i < total;
-        const int side = i >= side_units && in;
-        const int r = in ? i - side * side_units : 0;
-        const int h = r / c.units, u = r - h * c.units;
-        const T *row = side ? static_cast<const T *>(c.a.v) + t * c.a.v_st + h * c.a.v_sh
-                            : static_cast<const T *>(c.a.k) + t * c.a.k_st + h * c.a.k_sh;
-        uint4 lo = reinterpret_cast<const uint4 *>(row)[2 * u], hi = reinterpret_cast<const uint4 *>(row)[2 * u + 1];
-        if (rope && !side) rotate_unit<T>(row, 16 * u, c.a.rope, s_cs, lo, hi);
-        const AppendDst &d = c.dst[side];
+    const int pairs = rope ? c.a.rope.rotary / 2 : 0;
+    for (int i = threadIdx.x; i < pairs; i += blockDim.x) s_unit[i] = rope_unit(c.a.rope.freqs[i]);
+
+    const int side_units = c.heads * c.units, lane = threadIdx.x & 31;
+    const int item = blockIdx.y * blockDim.x + threadIdx.x;
+    const bool in = item < 2 * side_units;
+    const int side = in && item >= side_units;
+    const int r = in ? item - side * side_units : 0;
+    const int h = r / c.units, u = r - h * c.units;
+    const T *src = side ? static_cast<const T *>(c.a.v) + h * c.a.v_sh : static_cast<const T *>(c.a.k) + h * c.a.k_sh;
+    const int64_t st = side ? c.a.v_st : c.a.k_st;
+    const bool turn = rope && !side && 16 * u < 2 * pairs;
+    const bool partners = turn && !c.a.rope.interleaved && pairs % 16 == 0;
+    const int partner = 16 * u < pairs ? pairs : -pairs;
+    const AppendDst &d = c.dst[side];
+
+    RawUnit next;
+    auto load = [&](int64_t t) {
+        const T *row = src + t * st + 16 * u;
+        next.lo = reinterpret_cast<const uint4 *>(row)[0];
+        next.hi = reinterpret_cast<const uint4 *>(row)[1];
+        if (partners) {
+            next.plo = reinterpret_cast<const uint4 *>(row + partner)[0];
+            next.phi = reinterpret_cast<const uint4 *>(row + partner)[1];
+        }
+    };
+    int64_t t = blockIdx.x;
+    int64_t slot = c.a.slots[t], pos = rope ? c.a.rope.positions[t] : 0;
+    load(t);
+    __syncthreads();  // s_unit
+    for (int buffer = 0; t < tokens; buffer ^= 1) {
+        for (int i = threadIdx.x; i < pairs; i += blockDim.x) s_cs[buffer][i] = rope_cos_sin(pos, s_unit[i], c.a.rope.scale);
+        RawUnit now = next;
+        const int64_t to = slot;
+        const T *row = src + t * st;
+        t += gridDim.x;
+        if (t < tokens) {
+            slot = c.a.slots[t];
+            if (rope) pos = c.a.rope.positions[t];
+            load(t);
+        }
+        if (rope) __syncthreads();  // the angles; the other buffer's readers are past the barrier before
+        if (to < 0) continue;
+        if (to >= c.slots_total) {
+            if (threadIdx.x == 0) atomicExch(c.a.dev_err, QUARTZ_DEV_INDEX);
+            continue;
+        }
+        if (turn) rotate_unit<T>(row, 16 * u, c.a.rope, s_cs[buffer], now);
+        const int64_t page = to >> c.page_shift, in_page = to - (page << c.page_shift);
         if constexpr (GS == 0) {
             if (in) {
-                T *to = reinterpret_cast<T *>(d.data) + page * d.stride_page + in_page * d.stride_slot + h * d.stride_head;
-                reinterpret_cast<uint4 *>(to)[2 * u] = lo;
-                reinterpret_cast<uint4 *>(to)[2 * u + 1] = hi;
+                T *p = reinterpret_cast<T *>(d.data) + page * d.stride_page + in_page * d.stride_slot + h * d.stride_head;
+                reinterpret_cast<uint4 *>(p)[2 * u] = now.lo;
+                reinterpret_cast<uint4 *>(p)[2 * u + 1] = now.hi;
             }
         } else {
-            const UnitCodes e = encode_unit_sym<GS>(lo, hi);
+            const UnitCodes e = encode_unit_sym<GS>(now.lo, now.hi);
             const int64_t dst_row = ((page * c.heads + h) << c.page_shift) + in_page;
             if (in) store_unit_sym<GS>(e, dst_row * c.units + u, lane, d.codes, d.flags, d.scales, false);
         }
@@ -158,7 +186,8 @@ int log2_of(int v)
 // Closing up
 // ---------------------------------------------------------------------------
 constexpr int kMoveThreads = 256;
-constexpr int kMoveRows = 4;  // pieces in flight per thread
+constexpr int kMovePieces = 8;                       // pieces in flight per thread
+constexpr int kMoveTile = 512;                       // most rows of a tile
 
 // One array of the cache: a row of `row_bytes` per (page, slot, head), moved in
 // pieces of `piece` bytes (1, 2, 4, 8 or 16).
@@ -202,14 +231,19 @@ __device__ __forceinline__ void store_piece(uint8_t *p, const uint4 v, int bytes
 }
 
 // blockIdx.x = (sequence x head) * parts + part, blockIdx.y = plane (the one
-// behind the last is the weights').  Into new pages, a part is a range of
-// rows; in place it is a slice of every row, and the CTA goes through the rows
-// in order: row j is written after all rows up to j's tile are read (a barrier
-// per tile), and rows after them come from places >= j's tile (the kept
-// indices ascend, so kept[j] >= j), which no earlier tile writes.
+// behind the last is the weights').  A tile of rows at a time: first a thread
+// per row follows its kept index and the tables to the two addresses, then all
+// threads move pieces, eight loads in flight each; so the dependent reads are
+// paid once per tile and row, not per piece.  Into new pages, a part is a
+// range of rows; in place it is a slice of every row, and the CTA goes through
+// the rows in order: row j is written after all rows up to its tile's last are
+// read (a barrier per tile), and rows after them come from places behind the
+// tile (the kept indices ascend, so kept[j] >= j), which no earlier tile
+// writes.
 __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
 {
     griddep_wait();
+    __shared__ uint8_t *s_from[kMoveTile], *s_to[kMoveTile];
     const int64_t bh = blockIdx.x / m.parts;
     const int part = static_cast<int>(blockIdx.x - bh * m.parts);
     const int64_t b = bh / m.heads;
@@ -228,10 +262,10 @@ __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
     if (blockIdx.y == m.planes) {  // the sums of attention weights, in place
         if (part != 0) return;
         float *w = m.c.weights + b * m.c.w_sb + h * m.c.w_sh;
-        for (int64_t j0 = 0; j0 < rows; j0 += kMoveThreads * kMoveRows) {
-            float v[kMoveRows];
+        for (int64_t j0 = 0; j0 < rows; j0 += kMoveThreads * kMovePieces) {
+            float v[kMovePieces];
 #pragma unroll
-            for (int r = 0; r < kMoveRows; ++r) {
+            for (int r = 0; r < kMovePieces; ++r) {
                 const int64_t j = j0 + r * kMoveThreads + threadIdx.x;
                 v[r] = 0.f;
                 if (j < rows) {
@@ -241,7 +275,7 @@ __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
             }
             __syncthreads();
 #pragma unroll
-            for (int r = 0; r < kMoveRows; ++r) {
+            for (int r = 0; r < kMovePieces; ++r) {
                 const int64_t j = j0 + r * kMoveThreads + threadIdx.x;
                 if (j < rows) w[j] = v[r];
             }
@@ -263,42 +297,45 @@ __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
         last = first + per < rows ? first + per : rows;
     }
     uint8_t *base = p.base + h * p.stride_head + static_cast<int64_t>(slice) * p.pieces * p.piece;
-    // a tile of rows; each thread has the same places in all of them
-    const int tile_rows = kMoveThreads * kMoveRows / p.pieces;
-    int row[kMoveRows], at[kMoveRows];
+    const int tile_rows = min(kMoveTile, kMoveThreads * kMovePieces / p.pieces);
+    // a thread's places in a tile, the same in all of them
+    int row[kMovePieces], at[kMovePieces];
 #pragma unroll
-    for (int r = 0; r < kMoveRows; ++r) {
+    for (int r = 0; r < kMovePieces; ++r) {
         const int i = r * kMoveThreads + threadIdx.x;
         row[r] = i / p.pieces;
         at[r] = (i - row[r] * p.pieces) * p.piece;
     }
     bool bad = false;
     for (int64_t j0 = first; j0 < last; j0 += tile_rows) {
-        uint4 v[kMoveRows];
-        uint8_t *to[kMoveRows];
-#pragma unroll
-        for (int r = 0; r < kMoveRows; ++r) {
-            const int64_t j = j0 + row[r];
-            to[r] = nullptr;
-            if (row[r] >= tile_rows || j >= last) continue;
-            const int64_t src = kept[j];
+        const int n = last - j0 < tile_rows ? static_cast<int>(last - j0) : tile_rows;
+        for (int i = threadIdx.x; i < n; i += kMoveThreads) {
+            const int64_t j = j0 + i, src = kept[j];
+            uint8_t *from = nullptr, *to = nullptr;
             if (src < 0 || src >= len) {
                 bad = true;
-                continue;
+            } else if (!(m.in_place && src == j)) {
+                const int64_t sp = from_table[src >> m.page_shift], dp = to_table[j >> m.page_shift];
+                if (sp < 0 || sp >= m.num_pages || dp < 0 || dp >= m.num_pages) {
+                    bad = true;
+                } else {
+                    from = base + sp * p.stride_page + (src & page_mask) * p.stride_slot;
+                    to = base + dp * p.stride_page + (j & page_mask) * p.stride_slot;
+                }
             }
-            if (m.in_place && src == j) continue;
-            const int64_t sp = from_table[src >> m.page_shift], dp = to_table[j >> m.page_shift];
-            if (sp < 0 || sp >= m.num_pages || dp < 0 || dp >= m.num_pages) {
-                bad = true;
-                continue;
-            }
-            v[r] = load_piece(base + sp * p.stride_page + (src & page_mask) * p.stride_slot + at[r], p.piece);
-            to[r] = base + dp * p.stride_page + (j & page_mask) * p.stride_slot + at[r];
+            s_from[i] = from;
+            s_to[i] = to;
         }
+        __syncthreads();
+        uint4 v[kMovePieces];
+#pragma unroll
+        for (int r = 0; r < kMovePieces; ++r)
+            if (row[r] < n && s_from[row[r]]) v[r] = load_piece(s_from[row[r]] + at[r], p.piece);
         if (m.in_place) __syncthreads();
 #pragma unroll
-        for (int r = 0; r < kMoveRows; ++r)
-            if (to[r]) store_piece(to[r], v[r], p.piece);
+        for (int r = 0; r < kMovePieces; ++r)
+            if (row[r] < n && s_to[row[r]]) store_piece(s_to[row[r]] + at[r], v[r], p.piece);
+        __syncthreads();  // the next tile's addresses
     }
     if (bad) atomicExch(m.c.dev_err, QUARTZ_DEV_INDEX);
 }
@@ -332,14 +369,19 @@ cudaError_t launch_paged_append(const quartz_paged_cache_t *c, const AppendArgs 
     call.heads = c->heads;
     call.units = c->dim / 16;
     const int total = 2 * call.heads * call.units;
-    const dim3 grid(static_cast<unsigned>(tokens)), block(total < kAppendThreads ? (total + 31) & ~31 : kAppendThreads);
-    if (c->type == QUARTZ_PAGES_F16) return launch_pdl(paged_append_kernel<__half, 0>, grid, block, 0, s, call);
-    if (c->type == QUARTZ_PAGES_BF16) return launch_pdl(paged_append_kernel<__nv_bfloat16, 0>, grid, block, 0, s, call);
+    const int threads = total < kAppendThreads ? (total + 31) & ~31 : kAppendThreads;
+    const int y = (total + threads - 1) / threads;
+    int64_t x = (152 * (2048 / threads) + y - 1) / y;  // what fits the SMs; each CTA has several tokens where there are more
+    if (x > tokens) x = tokens;
+    const dim3 grid(static_cast<unsigned>(x), static_cast<unsigned>(y)), block(threads);
+    const int n = static_cast<int>(tokens);
+    if (c->type == QUARTZ_PAGES_F16) return launch_pdl(paged_append_kernel<__half, 0>, grid, block, 0, s, call, n);
+    if (c->type == QUARTZ_PAGES_BF16) return launch_pdl(paged_append_kernel<__nv_bfloat16, 0>, grid, block, 0, s, call, n);
     switch (c->k.enc.p.group_s) {
-        case 8: return launch_pdl(paged_append_kernel<__half, 8>, grid, block, 0, s, call);
-        case 16: return launch_pdl(paged_append_kernel<__half, 16>, grid, block, 0, s, call);
-        case 32: return launch_pdl(paged_append_kernel<__half, 32>, grid, block, 0, s, call);
-        default: return launch_pdl(paged_append_kernel<__half, 64>, grid, block, 0, s, call);
+        case 8: return launch_pdl(paged_append_kernel<__half, 8>, grid, block, 0, s, call, n);
+        case 16: return launch_pdl(paged_append_kernel<__half, 16>, grid, block, 0, s, call, n);
+        case 32: return launch_pdl(paged_append_kernel<__half, 32>, grid, block, 0, s, call, n);
+        default: return launch_pdl(paged_append_kernel<__half, 64>, grid, block, 0, s, call, n);
     }
 }
 

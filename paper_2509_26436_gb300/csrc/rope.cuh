@@ -9,33 +9,41 @@
 
 namespace quartz {
 
-// (scale cos, scale sin) of position * freq radians.  freq / 2 pi becomes a
-// fraction of a turn in units of 2^-64, and position times that, modulo 2^64,
-// is the angle's fraction of a turn without rounding: the only errors are the
-// frequency's (2^-53 relative, from its 64-bit type and the division by 2 pi:
-// 2^-33 turns at position 2^20 and one radian per position) and the last
-// conversion's.  Whole quarter turns are taken off as integers, so that the
-// binary32 argument of sine and cosine has 24 good bits of at most an eighth
-// of a turn.  A product in binary32 would be off by 2^-24 of the angle itself:
-// 0.008 radians at position 131072.
-__device__ __forceinline__ float2 rope_cos_sin(int64_t position, double freq, float scale)
+// A frequency in radians per position as a fraction of a turn per position, in
+// units of 2^-64 (whole turns dropped): freq = M 2^(E - 1075) with the 53-bit
+// M, so M times 2^66 / (2 pi) in integers, shifted by 1077 - E.  Good to 2^-63
+// of itself and one unit; and no 64-bit floating point, of which an SM does
+// two operations a clock.
+__device__ __forceinline__ uint64_t rope_unit(double freq)
 {
-    double turn = freq * 0.15915494309189533577;  // 1 / (2 pi)
-    turn -= floor(turn);
-    const uint64_t unit = static_cast<uint64_t>(turn * 18446744073709551616.0);
+    const uint64_t bits = static_cast<uint64_t>(__double_as_longlong(freq));
+    const int e = static_cast<int>((bits >> 52) & 0x7FF), r = 1077 - (e ? e : 1);
+    const uint64_t m = (bits & 0xFFFFFFFFFFFFFull) | (e ? 1ull << 52 : 0ull);
+    constexpr uint64_t kTurn = 0xA2F9836E4E441529ull;  // 2^66 / (2 pi)
+    const uint64_t lo = m * kTurn, hi = __umul64hi(m, kTurn);
+    uint64_t u = 0;
+    if (r >= 128) u = 0;
+    else if (r >= 64) u = hi >> (r - 64);
+    else if (r > 0) u = (lo >> r) | (hi << (64 - r));
+    else if (r > -64) u = lo << -r;
+    return bits >> 63 ? 0 - u : u;
+}
+
+// (scale cos, scale sin) of position times unit.  The product modulo 2^64 is
+// the angle's fraction of a turn without rounding.  Whole quarter turns are
+// taken off as integers, so that the binary32 argument of sine and cosine has
+// 24 good bits of at most an eighth of a turn.  A product in binary32 would be
+// off by 2^-24 of the angle itself: 0.008 radians at position 131072.
+__device__ __forceinline__ float2 rope_cos_sin(int64_t position, uint64_t unit, float scale)
+{
     const uint64_t angle = static_cast<uint64_t>(position) * unit;
     const uint64_t quarter = (angle + (1ull << 61)) >> 62;
     const int64_t rest = static_cast<int64_t>(angle - (quarter << 62));  // in [-2^61, 2^61)
     float s, c;
     sincospif(static_cast<float>(rest) * 1.0842021724855044e-19f, &s, &c);  // 2^-63: half turns
-    float cos_a, sin_a;
-    switch (quarter & 3) {
-        case 0: cos_a = c, sin_a = s; break;
-        case 1: cos_a = -s, sin_a = c; break;
-        case 2: cos_a = -c, sin_a = -s; break;
-        default: cos_a = s, sin_a = -c; break;
-    }
-    return make_float2(__fmul_rn(scale, cos_a), __fmul_rn(scale, sin_a));
+    const bool swap = quarter & 1, neg_c = (quarter + 1) & 2, neg_s = quarter & 2;
+    const float cos_a = swap ? s : c, sin_a = swap ? c : s;
+    return make_float2(__fmul_rn(neg_c ? -scale : scale, cos_a), __fmul_rn(neg_s ? -scale : scale, sin_a));
 }
 
 // One pair turned; cs = (cos, sin), sine negated for the transpose.  The

@@ -24,31 +24,44 @@ from . import _native as N
 _byref = C.byref
 
 
-def _dtypes():
-    """(float16, bfloat16, float32, float64, int32, int64)"""
+# torch and its types, bound on the first use (the package is imported without
+# torch); lib is the loaded library.
+torch = f16 = bf16 = f32 = f64 = i32 = i64 = lib = _device = None
+_KIND = {}  # torch type -> quartz_out_t
+
+
+def _bind():
+    global torch, f16, bf16, f32, f64, i32, i64, lib, _device
     t = _Q._torch()
-    return t.float16, t.bfloat16, t.float32, t.float64, t.int32, t.int64
+    f16, bf16, f32, f64, i32, i64 = t.float16, t.bfloat16, t.float32, t.float64, t.int32, t.int64
+    _KIND.update({f16: N.OUT_F16, bf16: N.OUT_BF16, f32: N.OUT_F32})
+    _device = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
+    lib = N.load()
+    torch = t
 
 
-def _check(name, x, dim, dtypes, last_contiguous=True):
-    """x is a `dim`-D CUDA tensor of one of `dtypes` on the current device."""
-    if not (x.is_cuda and x.dim() == dim and x.dtype in dtypes and (not last_contiguous or x.stride(-1) == 1 or x.shape[-1] == 1)):
-        kinds = " or ".join(str(d).replace("torch.", "") for d in dtypes)
-        raise ValueError(f"{name} must be a {dim}-D {kinds} CUDA tensor" +
-                         (" with a contiguous last dimension" if last_contiguous else ""))
-    if x.get_device() != _current_device():
-        raise ValueError(f"{name} is on another device than the current one")
+def _refuse(name, x, dim, kind, last=True):
+    """Say what is wrong with x (called where a call's quick check failed)."""
+    if not (x.is_cuda and x.dim() == dim and x.dtype is kind and (not last or x.stride(-1) == 1 or x.shape[-1] <= 1)):
+        raise ValueError(f"{name} must be a {dim}-D {str(kind).replace('torch.', '')} CUDA tensor" +
+                         (" with a contiguous last dimension" if last else ""))
+    raise ValueError(f"{name} is on another device than the current one")
 
 
-_device_getter = None
+def _vector(name, x, kind, device):
+    """x is a contiguous 1-D tensor of `kind` on the current device; its address."""
+    if not (x.dtype is kind and x.dim() == 1 and x.get_device() == device and (x.is_contiguous())):
+        _refuse(name, x, 1, kind)
+    return x.data_ptr()
 
 
-def _current_device() -> int:
-    global _device_getter
-    if _device_getter is None:
-        torch = _Q._torch()
-        _device_getter = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    return _device_getter()
+def _rows(name, x, dim, kind, device):
+    """x is a `dim`-D tensor of `kind` with a contiguous last dimension on the
+    current device; its strides."""
+    st = x.stride()
+    if not (x.dtype is kind and len(st) == dim and x.get_device() == device and (st[-1] == 1 or x.shape[-1] <= 1)):
+        _refuse(name, x, dim, kind)
+    return st
 
 
 # --- rotary positions ---------------------------------------------------------
@@ -65,10 +78,13 @@ def rope_frequencies(rotary: int, base: float = 10000.0, scaling: str = "none", 
         between; cosine and sine times 0.1 ln(factor) + 1;
     "llama3": the same between low_freq_factor and high_freq_factor turns,
         with the ramp over the turns, and no factor."""
-    torch = _Q._torch()
+    if torch is None:
+        import torch as t
+    else:
+        t = torch
     if rotary < 2 or rotary % 2 or not base > 0 or not factor > 0 or not original_length > 0:
         raise ValueError("rotary must be even and positive; base, factor and original_length positive")
-    i = torch.arange(rotary // 2, dtype=torch.float64)
+    i = t.arange(rotary // 2, dtype=t.float64)
     f = float(base) ** (-2.0 * i / rotary)
     scale = 1.0
     if scaling == "linear":
@@ -93,13 +109,11 @@ def rope_frequencies(rotary: int, base: float = 10000.0, scaling: str = "none", 
     return f.to(device), scale
 
 
-def _rope_struct(positions, freqs, tokens, scale, interleaved, backward) -> N.QuartzRope:
-    _, _, _, f64, _, i64 = _dtypes()
-    _check("positions", positions, 1, (i64,))
-    _check("freqs", freqs, 1, (f64,))
+def _rope_struct(positions, freqs, tokens, scale, interleaved, backward, device) -> N.QuartzRope:
+    at, f = _vector("positions", positions, i64, device), _vector("freqs", freqs, f64, device)
     if positions.shape[0] != tokens:
         raise ValueError("positions must have one entry per token")
-    return N.QuartzRope(positions.data_ptr(), freqs.data_ptr(), 2 * freqs.shape[0], int(interleaved), int(backward), scale)
+    return N.QuartzRope(at, f, 2 * freqs.shape[0], interleaved, backward, scale)
 
 
 def rope(x, positions, freqs, interleaved: bool = False, scale: float = 1.0, backward: bool = False, out=None,
@@ -110,19 +124,26 @@ def rope(x, positions, freqs, interleaved: bool = False, scale: float = 1.0, bac
     (2 i, 2 i + 1) with `interleaved`; the rest is copied.  `backward` applies
     the transpose: the gradient of x from that of the result.  `out` may be x
     itself (in place), or must not overlap it."""
-    f16, bf16, f32, _, _, _ = _dtypes()
-    _check("x", x, 3, (f16, bf16, f32))
+    if torch is None:
+        _bind()
+    dtype = x.dtype
+    kind = _KIND.get(dtype)
+    if kind is None or not x.is_cuda:
+        raise ValueError("x must be a 3-D float16, bfloat16 or float32 CUDA tensor")
+    device = _device()
+    xs = _rows("x", x, 3, dtype, device)
     T, H, D = x.shape
+    r = _rope_struct(positions, freqs, T, scale, interleaved, backward, device)
     if out is None:
-        out = _Q._torch().empty((T, H, D), dtype=x.dtype, device=x.device)
+        out = torch.empty((T, H, D), dtype=dtype, device=x.device)
+        s0, s1 = H * D, D
     else:
-        _check("out", out, 3, (x.dtype,))
+        s0, s1, _ = _rows("out", out, 3, dtype, device)
         if out.shape != x.shape:
             raise ValueError("out must have the shape of x")
-    r = _rope_struct(positions, freqs, T, scale, interleaved, backward)
-    xs, os_ = x.stride(), out.stride()
-    N.check(N.load().quartz_rope(x.data_ptr(), xs[0], xs[1], out.data_ptr(), os_[0], os_[1], _Q._out_type(x.dtype), T, H,
-                                 D, _byref(r), _Q._stream(stream)), "quartz_rope")
+    rc = lib.quartz_rope(x.data_ptr(), xs[0], xs[1], out.data_ptr(), s0, s1, kind, T, H, D, _byref(r), _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_rope")
     return out
 
 
@@ -142,7 +163,8 @@ class PagedCache:
     it is made once and kept as long as the tensors are."""
 
     def __init__(self, k, v, page_size: int, heads: int | None = None):
-        f16, bf16, _, _, _, _ = _dtypes()
+        if torch is None:
+            _bind()
         self.k, self.v, self.page_size = k, v, page_size
         if page_size < 1 or page_size & (page_size - 1):
             raise ValueError("page_size must be a power of two")
@@ -171,6 +193,8 @@ class PagedCache:
             sides = [N.QuartzPages(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2), N.QuartzEncoded()) for t in (k, v)]
             kind = N.PAGES_F16 if k.dtype is f16 else N.PAGES_BF16
         self.c = N.QuartzPagedCache(kind, page_size, self.heads, self.dim, self.num_pages, *sides)
+        self._ref = _byref(self.c)
+        self._index = self.device.index
         self._workspace_sizes = {}
 
     def _workspace_size(self, seqs, q_heads, max_len, window, with_weights) -> int:
@@ -179,20 +203,23 @@ class PagedCache:
         if n is None:
             if len(self._workspace_sizes) >= 1024:
                 self._workspace_sizes.clear()
-            n = N.load().quartz_paged_attention_workspace_size(_byref(self.c), seqs, q_heads, max_len, window, with_weights)
+            n = N.load().quartz_paged_attention_workspace_size(self._ref, seqs, q_heads, max_len, window, with_weights)
             self._workspace_sizes[key] = n
         return n
 
-    def _check_device(self):
-        if self.device.index != _current_device():
+    def _check_device(self) -> int:
+        device = _device()
+        if self._index != device:
             raise ValueError("the cache is on another device than the current one")
+        return device
 
 
 def empty_paged_cache(num_pages: int, page_size: int, heads: int, dim: int, dtype=None, params=None,
                       device="cuda") -> PagedCache:
     """A cache with uninitialised pages: 16-bit ones of `dtype` (float16 by
     default), or encoded ones of `params`."""
-    torch = _Q._torch()
+    if torch is None:
+        _bind()
     if params is not None:
         k, v = (_Q.empty_encoded(num_pages * heads * page_size, dim, params, device) for _ in range(2))
         return PagedCache(k, v, page_size, heads)
@@ -207,21 +234,21 @@ def paged_append(cache: PagedCache, k, v, slots, positions=None, freqs=None, int
     pages, which store Eq. 1 + Eq. 2 of them) to slots[t] = page * page_size +
     slot (int64; negative ones are skipped, no two are alike).  With
     `positions` and `freqs` the keys are rotated on the way, as rope() does."""
-    _, _, _, _, _, i64 = _dtypes()
-    _check("k", k, 3, (cache.dtype,))
-    _check("v", v, 3, (cache.dtype,))
-    _check("slots", slots, 1, (i64,))
-    cache._check_device()
+    device, kind = cache._check_device(), cache.dtype
+    ks, vs = _rows("k", k, 3, kind, device), _rows("v", v, 3, kind, device)
+    at = _vector("slots", slots, i64, device)
     T = slots.shape[0]
     if k.shape != (T, cache.heads, cache.dim) or v.shape != k.shape:
         raise ValueError("k and v must be [tokens, heads, dim] of the cache, with one slot per token")
-    if (positions is None) != (freqs is None):
+    r = None
+    if positions is not None and freqs is not None:
+        r = _byref(_rope_struct(positions, freqs, T, rope_scale, interleaved, False, device))
+    elif positions is not None or freqs is not None:
         raise ValueError("positions and freqs go together")
-    r = None if freqs is None else _rope_struct(positions, freqs, T, rope_scale, interleaved, False)
-    ks, vs = k.stride(), v.stride()
-    N.check(N.load().quartz_paged_append(_byref(cache.c), k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], T,
-                                         slots.data_ptr(), None if r is None else _byref(r), _Q._stream(stream)),
-            "quartz_paged_append")
+    rc = lib.quartz_paged_append(cache._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], T, at, r,
+                                 _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_paged_append")
 
 
 def attention_paged(q, cache: PagedCache, block_table, seq_lens, scale: float, window: int = 0,
@@ -234,38 +261,48 @@ def attention_paged(q, cache: PagedCache, block_table, seq_lens, scale: float, w
     max_len]: the attention weights, summed over each head's queries, are added
     in place.  A workspace of the caller's is only good for one call at a time,
     and for one captured graph."""
-    f16, bf16, f32, _, i32, _ = _dtypes()
-    _check("q", q, 3, (cache.dtype,))
-    _check("block_table", block_table, 2, (i32,))
-    _check("seq_lens", seq_lens, 1, (i32,))
-    cache._check_device()
+    device = cache._check_device()
+    qs = _rows("q", q, 3, cache.dtype, device)
+    ts = _rows("block_table", block_table, 2, i32, device)
+    lens = _vector("seq_lens", seq_lens, i32, device)
     B, Hq, D = q.shape
-    if D != cache.dim or Hq % cache.heads or block_table.shape[0] != B or seq_lens.shape[0] != B:
+    n, width = block_table.shape
+    if D != cache.dim or Hq % cache.heads or n != B or seq_lens.shape[0] != B:
         raise ValueError("q must be [seqs, a multiple of the cache's heads, dim]; block_table and seq_lens one row per sequence")
-    held = block_table.shape[1] * cache.page_size
+    held = width * cache.page_size
     if max_len is None:
         max_len = held
     elif not 0 <= max_len <= held:
         raise ValueError("max_len must be within what block_table holds")
-    o = out if out is not None else _Q._torch().empty((B, Hq, D), dtype=out_dtype or q.dtype, device=q.device)
-    if out is not None:
-        _check("out", out, 3, (f16, bf16, f32))
-        if out.shape != q.shape or not out.is_contiguous():
+    if out is None:
+        out_dtype = out_dtype or q.dtype
+        o = torch.empty((B, Hq, D), dtype=out_dtype, device=cache.device)
+    else:
+        o, out_dtype = out, out.dtype
+        _rows("out", o, 3, out_dtype, device)
+        if o.shape != q.shape or not o.is_contiguous():
             raise ValueError("out must be contiguous, of the shape of q")
-    w_ptr, w_sb, w_sh = None, 0, 0
+    kind = _KIND.get(out_dtype)
+    if kind is None:
+        raise ValueError("the result is float16, bfloat16 or float32")
+    w_ptr, w_sb, w_sh, with_weights = None, 0, 0, 0
     if weights is not None:
-        _check("weights", weights, 3, (f32,))
+        w_sb, w_sh, _ = _rows("weights", weights, 3, f32, device)
         if weights.shape[0] != B or weights.shape[1] != cache.heads or weights.shape[2] < max_len:
             raise ValueError("weights must be [seqs, heads, at least max_len]")
-        w_ptr, (w_sb, w_sh, _) = weights.data_ptr(), weights.stride()
-    need = cache._workspace_size(B, Hq, max_len, window, 1 if weights is not None else 0)
+        w_ptr, with_weights = weights.data_ptr(), 1
     if workspace is None:
-        workspace = _Q._torch().empty(max(need, 16), dtype=_Q._torch().uint8, device=q.device)
-    qs = q.stride()
-    N.check(N.load().quartz_paged_attention(
-        q.data_ptr(), qs[0], qs[1], B, Hq, _byref(cache.c), block_table.data_ptr(), block_table.stride(0),
-        seq_lens.data_ptr(), max_len, window, scale, o.data_ptr(), _Q._out_type(o.dtype), w_ptr, w_sb, w_sh,
-        workspace.data_ptr(), workspace.numel() * workspace.element_size(), _Q._stream(stream)), "quartz_paged_attention")
+        size = max(cache._workspace_size(B, Hq, max_len, window, with_weights), 16)
+        workspace = torch.empty(size, dtype=torch.uint8, device=cache.device)
+    else:
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
+        size = workspace.numel() * workspace.element_size()
+    rc = lib.quartz_paged_attention(q.data_ptr(), qs[0], qs[1], B, Hq, cache._ref, block_table.data_ptr(), ts[0], lens,
+                                    max_len, window, scale, o.data_ptr(), kind, w_ptr, w_sb, w_sh, workspace.data_ptr(),
+                                    size, _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_paged_attention")
     return o
 
 
@@ -280,9 +317,13 @@ def evict_select(weights, seq_lens, budget: int, recent: int = 0, sinks: int = 0
     that stay in each head's cache, ascending and then -1: all of them up to
     `budget`, else the first `sinks`, the last `recent` and the largest
     weights between (ties: the lowest index; NaN is the smallest)."""
-    _, _, f32, _, i32, _ = _dtypes()
-    _check("weights", weights, 3, (f32,))
-    _check("seq_lens", seq_lens, 1, (i32,))
+    if torch is None:
+        _bind()
+    if not weights.is_cuda:
+        _refuse("weights", weights, 3, f32)
+    device = _device()
+    sb, sh, _ = _rows("weights", weights, 3, f32, device)
+    lens = _vector("seq_lens", seq_lens, i32, device)
     B, H, n = weights.shape
     if seq_lens.shape[0] != B:
         raise ValueError("seq_lens must have one entry per sequence")
@@ -290,19 +331,20 @@ def evict_select(weights, seq_lens, budget: int, recent: int = 0, sinks: int = 0
         max_len = n
     elif not 0 <= max_len <= n:
         raise ValueError("max_len must be within weights' last dimension")
-    torch = _Q._torch()
     if kept is None:
-        kept = torch.empty((B, H, budget), dtype=torch.int32, device=weights.device)
+        kept = torch.empty((B, H, max(budget, 0)), dtype=i32, device=weights.device)
+    else:
+        _rows("kept", kept, 3, i32, device)
+        if kept.shape != (B, H, budget) or not kept.is_contiguous():
+            raise ValueError("kept must be contiguous [seqs, heads, budget]")
     if new_lens is None:
-        new_lens = torch.empty((B,), dtype=torch.int32, device=weights.device)
-    _check("kept", kept, 3, (i32,))
-    _check("new_lens", new_lens, 1, (i32,))
-    if kept.shape != (B, H, budget) or not kept.is_contiguous() or new_lens.shape[0] != B:
-        raise ValueError("kept must be contiguous [seqs, heads, budget], new_lens [seqs]")
-    sb, sh, _ = weights.stride()
-    N.check(N.load().quartz_evict_select(weights.data_ptr(), sb, sh, seq_lens.data_ptr(), B, H, max_len, budget, recent,
-                                         sinks, kept.data_ptr(), new_lens.data_ptr(), _Q._stream(stream)),
-            "quartz_evict_select")
+        new_lens = torch.empty((B,), dtype=i32, device=weights.device)
+    elif new_lens.shape[0] != B:
+        raise ValueError("new_lens must have one entry per sequence")
+    rc = lib.quartz_evict_select(weights.data_ptr(), sb, sh, lens, B, H, max_len, budget, recent, sinks, kept.data_ptr(),
+                                 _vector("new_lens", new_lens, i32, device), _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_evict_select")
     return kept, new_lens
 
 
@@ -314,31 +356,32 @@ def cache_compact(cache: PagedCache, block_table, seq_lens, kept, new_lens=None,
     pages of new_table, which are none of block_table's.  `weights` (the sums
     of attention_paged) close up in place alike, with 0 from the new length to
     the old."""
-    _, _, f32, _, i32, _ = _dtypes()
-    _check("block_table", block_table, 2, (i32,))
-    _check("seq_lens", seq_lens, 1, (i32,))
-    _check("kept", kept, 3, (i32,))
-    cache._check_device()
+    device = cache._check_device()
+    ts = _rows("block_table", block_table, 2, i32, device)
+    lens = _vector("seq_lens", seq_lens, i32, device)
+    _rows("kept", kept, 3, i32, device)
     B, H, budget = kept.shape
-    if H != cache.heads or block_table.shape[0] != B or seq_lens.shape[0] != B or not kept.is_contiguous():
+    n, width = block_table.shape
+    if H != cache.heads or n != B or seq_lens.shape[0] != B or not kept.is_contiguous():
         raise ValueError("kept must be contiguous [seqs, heads, budget]; block_table and seq_lens one row per sequence")
-    held = block_table.shape[1] * cache.page_size
+    held = width * cache.page_size
     if max_len is None:
         max_len = held
     elif not 0 <= max_len <= held:
         raise ValueError("max_len must be within what block_table holds")
     n_ptr, n_stride = None, 0
     if new_table is not None:
-        _check("new_table", new_table, 2, (i32,))
+        n_stride = _rows("new_table", new_table, 2, i32, device)[0]
         if new_table.shape[0] != B or new_table.shape[1] * cache.page_size < min(budget, max_len):
             raise ValueError("new_table must hold min(budget, max_len) tokens of each sequence")
-        n_ptr, n_stride = new_table.data_ptr(), new_table.stride(0)
+        n_ptr = new_table.data_ptr()
     w_ptr, w_sb, w_sh = None, 0, 0
     if weights is not None:
-        _check("weights", weights, 3, (f32,))
+        w_sb, w_sh, _ = _rows("weights", weights, 3, f32, device)
         if weights.shape[0] != B or weights.shape[1] != H or weights.shape[2] < max_len:
             raise ValueError("weights must be [seqs, heads, at least max_len]")
-        w_ptr, (w_sb, w_sh, _) = weights.data_ptr(), weights.stride()
-    N.check(N.load().quartz_cache_compact(_byref(cache.c), B, block_table.data_ptr(), block_table.stride(0), n_ptr,
-                                          n_stride, seq_lens.data_ptr(), max_len, kept.data_ptr(), budget, w_ptr, w_sb,
-                                          w_sh, _Q._stream(stream)), "quartz_cache_compact")
+        w_ptr = weights.data_ptr()
+    rc = lib.quartz_cache_compact(cache._ref, B, block_table.data_ptr(), ts[0], n_ptr, n_stride, lens, max_len,
+                                  kept.data_ptr(), budget, w_ptr, w_sb, w_sh, _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_cache_compact")
