@@ -70,12 +70,12 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
     uint32_t want = static_cast<uint32_t>(a.budget - a.sinks - a.recent);  // < hi - lo
     const bool none = want == 0;  // only sinks and recent tokens stay
     uint32_t top = 0, bottom = 0xffffffffu;
-    for (int t0 = lo + tid; t0 < hi; t0 += 4 * kThreads) {
-        float f[4];
+    for (int t0 = lo + tid; t0 < hi; t0 += 16 * kThreads) {
+        float f[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = t0 + i * kThreads < hi ? w[t0 + i * kThreads] : 0.f;
+        for (int i = 0; i < 16; ++i) f[i] = t0 + i * kThreads < hi ? w[t0 + i * kThreads] : 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < 16; ++i)
             if (t0 + i * kThreads < hi) {
                 const uint32_t key = order_key(f[i]);
                 if (HELD) s_keys[t0 + i * kThreads - lo] = key;
@@ -148,12 +148,16 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
     }
     if (lane == 0) s_above[warp] = above, s_equal[warp] = equal;
     __syncthreads();
-    uint32_t stay = 0, seen = 0;  // kept and equal ones before this warp's run
-    for (int i = 0; i < warp; ++i) {
-        const uint32_t e = s_equal[i];
-        stay += s_above[i] + (seen < want ? min(e, want - seen) : 0u);
-        seen += e;
+    // kept and equal ones before this warp's run: lane i adds up the warps to i
+    uint32_t n_above = s_above[lane], n_equal = s_equal[lane];
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const uint32_t x = __shfl_up_sync(0xffffffffu, n_above, d), y = __shfl_up_sync(0xffffffffu, n_equal, d);
+        if (lane >= d) n_above += x, n_equal += y;
     }
+    uint32_t stay = __shfl_sync(0xffffffffu, n_above, (warp + 31) & 31), seen = __shfl_sync(0xffffffffu, n_equal, (warp + 31) & 31);
+    if (warp == 0) stay = seen = 0;
+    stay += min(seen, want);  // the first `want` equal ones stay
     const uint32_t before = (1u << lane) - 1;
     for (int t0 = from; t0 < to; t0 += 32) {
         const int t = t0 + lane;

@@ -12,7 +12,8 @@ namespace {
 // Append
 // ---------------------------------------------------------------------------
 constexpr int kAppendThreads = 256;
-constexpr int kMaxPairs = 128;  // dim <= 256
+constexpr int kAppendTokens = 8;                       // most tokens per CTA
+constexpr int kAngles = kAppendTokens * 128;           // dim <= 256: 128 pairs
 
 struct AppendDst {
     uint8_t *data;  // 16-bit pages
@@ -26,8 +27,23 @@ struct AppendCall {
     AppendArgs a;
     AppendDst dst[2];
     int64_t slots_total;
-    int page_shift, heads, units;  // units of 16 elements per row
+    int page_shift, heads, units;    // units of 16 elements per row
+    int tokens_here, groups, each;   // per CTA; head groups; heads per thread
 };
+
+// The angles of a CTA's token in shared memory, (cos, -sin) for the first
+// element of a pair and behind them (sin, cos) for the second: both are m a + n
+// b with (a, b) = (first, second).  Neighbouring units, which neighbouring
+// lanes hold, side by side.
+struct AngleTable {
+    const float2 *cs;
+    static constexpr int kStride = kAngles / 16;
+    __device__ __forceinline__ float2 operator()(int i) const { return cs[(i & 15) * kStride + (i >> 4)]; }
+};
+
+// rope_turn's two results from the table: the same operations.
+__device__ __forceinline__ float rope_first(float2 v, float x1, float x2) { return __fmaf_rn(v.x, x1, __fmul_rn(v.y, x2)); }
+__device__ __forceinline__ float rope_second(float2 v, float x1, float x2) { return __fmaf_rn(-v.y, x1, __fmul_rn(v.x, x2)); }
 
 template <typename T>
 __device__ __forceinline__ void unpack16(const uint4 lo, const uint4 hi, float (&f)[16])
@@ -55,123 +71,135 @@ __device__ __forceinline__ void pack16(const float (&f)[16], uint4 &lo, uint4 &h
     hi = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// A lane's unit of a row: 16 elements, and for keys that are rotated in halves
-// their 16 partners (read again as vectors where the unit lies in one half).
-struct RawUnit {
-    uint4 lo, hi, plo, phi;
-};
-
 // The 16 elements d0 .. d0 + 15 of a key row, rotated, in the type of the row
-// (one rounding, as the rotation by itself gives).
+// (one rounding, as the rotation by itself gives).  Pairs of halves take their
+// partners from the row again: as vectors where a unit lies in one half, else
+// one by one.
 template <typename T>
-__device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_rope_t &rope, const float2 *cs, RawUnit &r)
+__device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_rope_t &rope, const AngleTable &cs, uint4 &lo,
+                                            uint4 &hi, const uint4 plo, const uint4 phi)
 {
     const int pairs = rope.rotary / 2;
-    float x[16], y[16];
-    unpack16<T>(r.lo, r.hi, x);
+    float y[16];
     if (rope.interleaved) {
+        unpack16<T>(lo, hi, y);
 #pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            y[e] = x[e], y[e + 1] = x[e + 1];
+        for (int e = 0; e < 16; e += 2)
             if (d0 + e < rope.rotary) {
-                const float2 v = rope_turn(x[e], x[e + 1], cs[(d0 + e) / 2]);
-                y[e] = v.x, y[e + 1] = v.y;
+                const float2 v = cs((d0 + e) / 2);
+                const float x1 = y[e], x2 = y[e + 1];
+                y[e] = rope_first(v, x1, x2);
+                y[e + 1] = rope_second(v, x1, x2);
             }
-        }
     } else if (pairs % 16 == 0) {
-        float p[16];
-        unpack16<T>(r.plo, r.phi, p);
-        if (d0 < pairs) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = rope_turn(x[e], p[e], cs[d0 + e]).x;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) y[e] = rope_turn(p[e], x[e], cs[d0 - pairs + e]).y;
-        }
-    } else {
+        // one form for both halves: lanes of both share a warp
+        const bool second = d0 >= pairs;
+        float a[16], b[16];
+        unpack16<T>(second ? plo : lo, second ? phi : hi, a);
+        unpack16<T>(second ? lo : plo, second ? hi : phi, b);
+        const AngleTable mn{cs.cs + (second ? kAngles : 0)};
+        const int i0 = second ? d0 - pairs : d0;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
+            const float2 v = mn.cs[e * AngleTable::kStride + (i0 >> 4)];
+            y[e] = rope_first(v, a[e], b[e]);
+        }
+    } else {
+#pragma unroll 1
+        for (int e = 0; e < 16; ++e) {
             const int d = d0 + e;
-            y[e] = x[e];
-            if (d < pairs) y[e] = rope_turn(x[e], to_f32<T>(row[d + pairs]), cs[d]).x;
-            else if (d < rope.rotary) y[e] = rope_turn(to_f32<T>(row[d - pairs]), x[e], cs[d - pairs]).y;
+            float v = to_f32<T>(row[d]);
+            if (d < pairs) v = rope_first(cs(d), v, to_f32<T>(row[d + pairs]));
+            else if (d < rope.rotary) v = rope_second(cs(d - pairs), to_f32<T>(row[d - pairs]), v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i == e) y[i] = v;
         }
     }
-    pack16<T>(y, r.lo, r.hi);
+    pack16<T>(y, lo, hi);
 }
 
-// A CTA goes through tokens; a lane has the same 16 elements of a key or value
-// row in all of them (blockIdx.y: further rows), and loads the next token's
-// while it works on this one's.  GS = 0: 16-bit pages of type T; else encoded
-// pages (T = __half, four lanes per 64-element group, which never cross a row:
-// dim is a multiple of 64).
+// A thread takes 16 elements (a unit) of one token's keys and values in several
+// heads; the head groups of a CTA share its tokens' angles.  Few tokens: keys
+// and values by different CTAs (blockIdx.y).  GS = 0: 16-bit pages of type T; else encoded pages (T = __half, four
+// neighbouring lanes per 64-element group: dim is a multiple of 64).
 template <typename T, int GS>
-__global__ void __launch_bounds__(kAppendThreads) paged_append_kernel(AppendCall c, int tokens)
+__global__ void __launch_bounds__(kAppendThreads, 4) paged_append_kernel(AppendCall c, int tokens)
 {
     griddep_wait();
-    __shared__ float2 s_cs[2][kMaxPairs];
-    __shared__ uint64_t s_unit[kMaxPairs];
-    const bool rope = c.a.rope.positions != nullptr;
+    __shared__ float2 s_cs[2 * kAngles];
+    const bool keys = gridDim.y == 1 || blockIdx.y == 0, values = gridDim.y == 1 || blockIdx.y == 1;
+    const bool rope = c.a.rope.positions != nullptr && keys;
     const int pairs = rope ? c.a.rope.rotary / 2 : 0;
-    for (int i = threadIdx.x; i < pairs; i += blockDim.x) s_unit[i] = rope_unit(c.a.rope.freqs[i]);
-
-    const int side_units = c.heads * c.units, lane = threadIdx.x & 31;
-    const int item = blockIdx.y * blockDim.x + threadIdx.x;
-    const bool in = item < 2 * side_units;
-    const int side = in && item >= side_units;
-    const int r = in ? item - side * side_units : 0;
-    const int h = r / c.units, u = r - h * c.units;
-    const T *src = side ? static_cast<const T *>(c.a.v) + h * c.a.v_sh : static_cast<const T *>(c.a.k) + h * c.a.k_sh;
-    const int64_t st = side ? c.a.v_st : c.a.k_st;
-    const bool turn = rope && !side && 16 * u < 2 * pairs;
+    const int first = blockIdx.x * c.tokens_here;
+    if (rope) {
+        const int per = (pairs + 15) / 16;  // of the table's 16 lines, per token
+        for (int i = threadIdx.x; i < c.tokens_here * pairs; i += blockDim.x) {
+            const int n = i / pairs, j = i - n * pairs;
+            if (first + n < tokens) {
+                const float2 v = rope_cos_sin(c.a.rope.positions[first + n], rope_unit(c.a.rope.freqs[j]), c.a.rope.scale);
+                float2 *to = s_cs + (j & 15) * AngleTable::kStride + n * per + (j >> 4);
+                to[0] = make_float2(v.x, -v.y);
+                to[kAngles] = make_float2(v.y, v.x);
+            }
+        }
+        __syncthreads();
+    }
+    const int places = c.tokens_here * c.units;
+    const int group = threadIdx.x / places, place = threadIdx.x - group * places;
+    const int n = place / c.units, u = place - n * c.units, lane = threadIdx.x & 31;
+    const int t = first + n;
+    int64_t slot = t < tokens && group < c.groups ? c.a.slots[t] : -1;
+    if (slot >= c.slots_total) {
+        atomicExch(c.a.dev_err, QUARTZ_DEV_INDEX);
+        slot = -1;
+    }
+    const AngleTable cs{s_cs + n * ((pairs + 15) / 16)};
+    const int64_t page = slot >> c.page_shift, in_page = slot - (page << c.page_shift);
+    const bool turn = 16 * u < 2 * pairs;
     const bool partners = turn && !c.a.rope.interleaved && pairs % 16 == 0;
     const int partner = 16 * u < pairs ? pairs : -pairs;
-    const AppendDst &d = c.dst[side];
-
-    RawUnit next;
-    auto load = [&](int64_t t) {
-        const T *row = src + t * st + 16 * u;
-        next.lo = reinterpret_cast<const uint4 *>(row)[0];
-        next.hi = reinterpret_cast<const uint4 *>(row)[1];
-        if (partners) {
-            next.plo = reinterpret_cast<const uint4 *>(row + partner)[0];
-            next.phi = reinterpret_cast<const uint4 *>(row + partner)[1];
-        }
-    };
-    int64_t t = blockIdx.x;
-    int64_t slot = c.a.slots[t], pos = rope ? c.a.rope.positions[t] : 0;
-    load(t);
-    __syncthreads();  // s_unit
-    for (int buffer = 0; t < tokens; buffer ^= 1) {
-        for (int i = threadIdx.x; i < pairs; i += blockDim.x) s_cs[buffer][i] = rope_cos_sin(pos, s_unit[i], c.a.rope.scale);
-        RawUnit now = next;
-        const int64_t to = slot;
-        const T *row = src + t * st;
-        t += gridDim.x;
-        if (t < tokens) {
-            slot = c.a.slots[t];
-            if (rope) pos = c.a.rope.positions[t];
-            load(t);
-        }
-        if (rope) __syncthreads();  // the angles; the other buffer's readers are past the barrier before
-        if (to < 0) continue;
-        if (to >= c.slots_total) {
-            if (threadIdx.x == 0) atomicExch(c.a.dev_err, QUARTZ_DEV_INDEX);
-            continue;
-        }
-        if (turn) rotate_unit<T>(row, 16 * u, c.a.rope, s_cs[buffer], now);
-        const int64_t page = to >> c.page_shift, in_page = to - (page << c.page_shift);
+    const T *k_row = static_cast<const T *>(c.a.k) + t * c.a.k_st, *v_row = static_cast<const T *>(c.a.v) + t * c.a.v_st;
+    // encoded pages: unit of head 0; heads are page_size rows apart
+    const int64_t unit0 = (((page * c.heads) << c.page_shift) + in_page) * c.units + u;
+    auto store = [&](int side, int h, bool in, const uint4 lo, const uint4 hi) {
+        const AppendDst &d = c.dst[side];
         if constexpr (GS == 0) {
             if (in) {
-                T *p = reinterpret_cast<T *>(d.data) + page * d.stride_page + in_page * d.stride_slot + h * d.stride_head;
-                reinterpret_cast<uint4 *>(p)[2 * u] = now.lo;
-                reinterpret_cast<uint4 *>(p)[2 * u + 1] = now.hi;
+                uint4 *to = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(d.data) + page * d.stride_page +
+                                                      in_page * d.stride_slot + h * d.stride_head + 16 * u);
+                to[0] = lo;
+                to[1] = hi;
             }
         } else {
-            const UnitCodes e = encode_unit_sym<GS>(now.lo, now.hi);
-            const int64_t dst_row = ((page * c.heads + h) << c.page_shift) + in_page;
-            if (in) store_unit_sym<GS>(e, dst_row * c.units + u, lane, d.codes, d.flags, d.scales, false);
+            const UnitCodes e = encode_unit_sym<GS>(lo, hi);
+            if (in) store_unit_sym<GS>(e, unit0 + (static_cast<int64_t>(h * c.units) << c.page_shift), lane, d.codes, d.flags, d.scales, false);
         }
+    };
+    for (int k = 0; k < c.each; ++k) {  // the same trips for all lanes: encoding takes them together
+        const int h = group + k * c.groups;
+        const bool in = slot >= 0 && h < c.heads;
+        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+        const T *row = k_row + h * c.a.k_sh;
+        if (keys && in) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(row + 16 * u);
+            lo = from[0], hi = from[1];
+            if (turn) {
+                uint4 plo = lo, phi = hi;
+                if (partners) {
+                    from = reinterpret_cast<const uint4 *>(row + 16 * u + partner);
+                    plo = from[0], phi = from[1];
+                }
+                rotate_unit<T>(row, 16 * u, c.a.rope, cs, lo, hi, plo, phi);
+            }
+        }
+        if (keys) store(0, h, in, lo, hi);
+        if (!values) continue;
+        if (in) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(v_row + h * c.a.v_sh + 16 * u);
+            lo = from[0], hi = from[1];
+        }
+        store(1, h, in, lo, hi);
     }
 }
 
@@ -185,6 +213,7 @@ int log2_of(int v)
 // ---------------------------------------------------------------------------
 // Closing up
 // ---------------------------------------------------------------------------
+
 constexpr int kMoveThreads = 256;
 constexpr int kMovePieces = 8;                       // pieces in flight per thread
 constexpr int kMoveTile = 512;                       // most rows of a tile
@@ -243,7 +272,7 @@ __device__ __forceinline__ void store_piece(uint8_t *p, const uint4 v, int bytes
 __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
 {
     griddep_wait();
-    __shared__ uint8_t *s_from[kMoveTile], *s_to[kMoveTile];
+    __shared__ uint8_t *s_from[2][kMoveTile], *s_to[2][kMoveTile];
     const int64_t bh = blockIdx.x / m.parts;
     const int part = static_cast<int>(blockIdx.x - bh * m.parts);
     const int64_t b = bh / m.heads;
@@ -307,9 +336,8 @@ __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
         at[r] = (i - row[r] * p.pieces) * p.piece;
     }
     bool bad = false;
-    for (int64_t j0 = first; j0 < last; j0 += tile_rows) {
-        const int n = last - j0 < tile_rows ? static_cast<int>(last - j0) : tile_rows;
-        for (int i = threadIdx.x; i < n; i += kMoveThreads) {
+    auto addresses = [&](int64_t j0, int buffer) {
+        for (int i = threadIdx.x; i < tile_rows && j0 + i < last; i += kMoveThreads) {
             const int64_t j = j0 + i, src = kept[j];
             uint8_t *from = nullptr, *to = nullptr;
             if (src < 0 || src >= len) {
@@ -323,19 +351,25 @@ __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
                     to = base + dp * p.stride_page + (j & page_mask) * p.stride_slot;
                 }
             }
-            s_from[i] = from;
-            s_to[i] = to;
+            s_from[buffer][i] = from;
+            s_to[buffer][i] = to;
         }
-        __syncthreads();
+    };
+    addresses(first, 0);
+    __syncthreads();
+    int buffer = 0;
+    for (int64_t j0 = first; j0 < last; j0 += tile_rows, buffer ^= 1) {
+        const int n = last - j0 < tile_rows ? static_cast<int>(last - j0) : tile_rows;
         uint4 v[kMovePieces];
 #pragma unroll
         for (int r = 0; r < kMovePieces; ++r)
-            if (row[r] < n && s_from[row[r]]) v[r] = load_piece(s_from[row[r]] + at[r], p.piece);
+            if (row[r] < n && s_from[buffer][row[r]]) v[r] = load_piece(s_from[buffer][row[r]] + at[r], p.piece);
+        addresses(j0 + tile_rows, buffer ^ 1);  // the next tile's, while the loads are under way
         if (m.in_place) __syncthreads();
 #pragma unroll
         for (int r = 0; r < kMovePieces; ++r)
-            if (row[r] < n && s_to[row[r]]) store_piece(s_to[row[r]] + at[r], v[r], p.piece);
-        __syncthreads();  // the next tile's addresses
+            if (row[r] < n && s_to[buffer][row[r]]) store_piece(s_to[buffer][row[r]] + at[r], v[r], p.piece);
+        __syncthreads();
     }
     if (bad) atomicExch(m.c.dev_err, QUARTZ_DEV_INDEX);
 }
@@ -368,20 +402,27 @@ cudaError_t launch_paged_append(const quartz_paged_cache_t *c, const AppendArgs 
     call.slots_total = c->num_pages << call.page_shift;
     call.heads = c->heads;
     call.units = c->dim / 16;
-    const int total = 2 * call.heads * call.units;
-    const int threads = total < kAppendThreads ? (total + 31) & ~31 : kAppendThreads;
-    const int y = (total + threads - 1) / threads;
-    int64_t x = (152 * (2048 / threads) + y - 1) / y;  // what fits the SMs; each CTA has several tokens where there are more
-    if (x > tokens) x = tokens;
-    const dim3 grid(static_cast<unsigned>(x), static_cast<unsigned>(y)), block(threads);
-    const int n = static_cast<int>(tokens);
-    if (c->type == QUARTZ_PAGES_F16) return launch_pdl(paged_append_kernel<__half, 0>, grid, block, 0, s, call, n);
-    if (c->type == QUARTZ_PAGES_BF16) return launch_pdl(paged_append_kernel<__nv_bfloat16, 0>, grid, block, 0, s, call, n);
+    // Heads per thread: two where there are tokens for 1024 threads per SM, else
+    // as few as fit a CTA.  Places of several tokens keep a CTA's warps full
+    // (a power of two of tokens times 4, 8, 12 or 16 units).
+    const bool many = tokens * call.heads * call.units >= int64_t(152) * 1024 * 2;
+    int groups = many ? (call.heads + 1) / 2 : call.heads;
+    if (groups > kAppendThreads / call.units) groups = kAppendThreads / call.units;
+    int n = 1;
+    while (many && 2 * n <= kAppendTokens && 2 * n * call.units * groups <= kAppendThreads) n *= 2;
+    call.tokens_here = n;
+    call.groups = groups;
+    call.each = (call.heads + groups - 1) / groups;
+    const int threads = n * call.units * groups;  // a multiple of 4
+    const dim3 grid(static_cast<unsigned>((tokens + n - 1) / n), many ? 1 : 2), block((threads + 31) & ~31);
+    const int total = static_cast<int>(tokens);
+    if (c->type == QUARTZ_PAGES_F16) return launch_pdl(paged_append_kernel<__half, 0>, grid, block, 0, s, call, total);
+    if (c->type == QUARTZ_PAGES_BF16) return launch_pdl(paged_append_kernel<__nv_bfloat16, 0>, grid, block, 0, s, call, total);
     switch (c->k.enc.p.group_s) {
-        case 8: return launch_pdl(paged_append_kernel<__half, 8>, grid, block, 0, s, call, n);
-        case 16: return launch_pdl(paged_append_kernel<__half, 16>, grid, block, 0, s, call, n);
-        case 32: return launch_pdl(paged_append_kernel<__half, 32>, grid, block, 0, s, call, n);
-        default: return launch_pdl(paged_append_kernel<__half, 64>, grid, block, 0, s, call, n);
+        case 8: return launch_pdl(paged_append_kernel<__half, 8>, grid, block, 0, s, call, total);
+        case 16: return launch_pdl(paged_append_kernel<__half, 16>, grid, block, 0, s, call, total);
+        case 32: return launch_pdl(paged_append_kernel<__half, 32>, grid, block, 0, s, call, total);
+        default: return launch_pdl(paged_append_kernel<__half, 64>, grid, block, 0, s, call, total);
     }
 }
 
@@ -424,7 +465,8 @@ cudaError_t launch_cache_compact(const quartz_paged_cache_t *c, const CompactCal
         for (int i = 0; i < m.planes; ++i) m.parts = m.plane[i].slices > m.parts ? m.plane[i].slices : m.parts;
     } else {
         const int64_t rows = a.budget < a.max_len ? a.budget : a.max_len;
-        int64_t want = (152 * 8 + bh * 2 - 1) / (bh * 2), most = (rows + 127) / 128;
+        const int64_t tile = kMoveThreads * kMovePieces * 16 / (2 * c->dim), most = (rows + tile - 1) / tile;
+        int64_t want = (152 * 8 + bh * 2 - 1) / (bh * 2);
         if (want > most) want = most;
         m.parts = want < 1 ? 1 : static_cast<int>(want);
     }

@@ -47,7 +47,7 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
     __shared__ __align__(16) uint16_t s_q[kPagedHeads][D + 8];
     __shared__ PagedJoin s_join;
 
-    const int head_block = blockIdx.x % a.head_blocks, split = blockIdx.x / a.head_blocks;
+    const int head_block = blockIdx.x / a.n_split, split = blockIdx.x - head_block * a.n_split;
     const int kv_head = blockIdx.y, b = blockIdx.z, head0 = head_block * kPagedHeads;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
@@ -208,6 +208,7 @@ struct Kernel16 {
     {
         const cudaError_t e = ready();  // of the current device
         if (e != cudaSuccess) return e;
+        if (a.cluster) return launch_pdl_cluster(paged_attn_kernel<D, BF>, a.n_split, grid, dim3(kPagedThreads), kSmem, s, a);
         return launch_pdl(paged_attn_kernel<D, BF>, grid, dim3(kPagedThreads), kSmem, s, a);
     }
 };
@@ -216,94 +217,127 @@ struct Kernel16 {
 // Join of the splits, and the sums of weights
 // ---------------------------------------------------------------------------
 constexpr int kMaxSplits = 1024;
+constexpr int kMaxCluster = 8;  // splits joined within a cluster (the portable size)
+constexpr int kJoinThreads = 256;
+constexpr int kJoinHeads = 64;  // query heads whose sums are held at a time
 
-// One CTA per (sequence, query head), a thread per 4 elements and group of
-// splits; the splits that hold tokens follow from the length.
+// CTA (x, key / value head, sequence).  Join of the splits: head x of the key
+// head's query heads (and x + gridDim.x, ...), a thread per 4 elements and
+// group of splits.  Sums of weights: 1024 tokens from 1024 x on, four per
+// thread, weights[b, h, t] += sum over the query heads of 2^(score - m) / l, in
+// head order; every CTA finds the heads' m and l from the splits itself, which
+// is less than another launch.
 template <int D>
-__global__ void __launch_bounds__(256) paged_join_kernel(PagedArgs a)
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, float *weights, int64_t w_sb, int64_t w_sh)
 {
     griddep_wait();
-    constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+    constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
     __shared__ float s_f[kMaxSplits];
     __shared__ float4 s_o[kGroups][kLanes];
     __shared__ float s_red[8], s_inv;
-    const int64_t row = blockIdx.x;
-    const int b = static_cast<int>(row / (a.kv_heads * a.group));
+    __shared__ float s_lse[kJoinHeads];
+    const int b = blockIdx.z;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
-    const int splits = (range.count() + a.chunk - 1) / a.chunk;
-    const float *ml = a.part_ml + 2 * row * a.n_split;
+    const int splits = (range.count() + a.chunk - 1) / a.chunk;  // that hold tokens
+    const int64_t row0 = (static_cast<int64_t>(b) * a.kv_heads + blockIdx.y) * a.group;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    float m = -INFINITY;
-    for (int i = tid; i < splits; i += 256) m = fmaxf(m, ml[2 * i]);
-#pragma unroll
-    for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-    if (lane == 0) s_red[warp] = m;
-    __syncthreads();
-    m = s_red[0];
-#pragma unroll
-    for (int w = 1; w < 8; ++w) m = fmaxf(m, s_red[w]);
-    __syncthreads();
-    float sum = 0.f;
-    for (int i = tid; i < splits; i += 256) {
-        const float f = ex2(ml[2 * i] - m);
-        s_f[i] = f;
-        sum += f * ml[2 * i + 1];
-    }
-#pragma unroll
-    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) s_red[warp] = sum;
-    __syncthreads();
-    if (tid == 0) {
-        float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) t += s_red[w];
-        s_inv = t > 0.f ? 1.f / t : 0.f;
-        if (a.lse) a.lse[row] = m + log2f(t);
-    }
-    const int g = tid / kLanes, c = tid - g * kLanes;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (g < kGroups) {
-        const float4 *o = reinterpret_cast<const float4 *>(a.part_o + row * a.n_split * D) + c;
-#pragma unroll 4
-        for (int i = g; i < splits; i += kGroups) {
-            const float4 u = o[static_cast<int64_t>(i) * kLanes];
-            const float f = s_f[i];
-            v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
-        }
-        s_o[g][c] = v;
-    }
-    __syncthreads();
-    if (g == 0) {
-#pragma unroll
-        for (int k = 1; k < kGroups; ++k) {
-            const float4 u = s_o[k][c];
-            v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
-        }
-        const float r = s_inv;
-        paged_store4(a.o, a.o_type, row * D + c * 4, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
-    }
-}
 
-// weights[b, h, t] += sum over the head's query heads of 2^(score - lse), in
-// head order: four tokens per thread.
-__global__ void __launch_bounds__(256) paged_weights_kernel(PagedArgs a, float *weights, int64_t w_sb, int64_t w_sh)
-{
-    griddep_wait();
-    const int h = blockIdx.y, b = blockIdx.z;
-    const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
-    const int t = (blockIdx.x * 256 + threadIdx.x) * 4;
-    if (t >= range.count()) return;
-    const int64_t row0 = (static_cast<int64_t>(b) * a.kv_heads + h) * a.group;
-    float p[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int g = 0; g < a.group; ++g) {
-        const float4 s = *reinterpret_cast<const float4 *>(a.scores + (row0 + g) * a.score_stride + t);
-        const float lse = a.lse[row0 + g];
-        p[0] += ex2(s.x - lse), p[1] += ex2(s.y - lse), p[2] += ex2(s.z - lse), p[3] += ex2(s.w - lse);
-    }
-    float *w = weights + b * w_sb + h * w_sh + range.base + t;
+    for (int head = blockIdx.x; a.part_o && head < a.group; head += gridDim.x) {
+        const int64_t row = row0 + head;
+        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row * a.n_split;
+        float m = -1e30f;
+        for (int i = tid; i < splits; i += kJoinThreads) m = fmaxf(m, ml[i].x);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (t + i < range.count() && range.base + t + i >= range.first) w[i] += p[i];
+        for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+        if (lane == 0) s_red[warp] = m;
+        __syncthreads();
+        m = s_red[0];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) m = fmaxf(m, s_red[w]);
+        __syncthreads();
+        float sum = 0.f;
+        for (int i = tid; i < splits; i += kJoinThreads) {
+            const float2 v = ml[i];
+            const float f = ex2(v.x - m);
+            s_f[i] = f;
+            sum += f * v.y;
+        }
+#pragma unroll
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) s_red[warp] = sum;
+        __syncthreads();
+        if (tid == 0) {
+            float t = 0.f;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) t += s_red[w];
+            s_inv = t > 0.f ? 1.f / t : 0.f;
+        }
+        const int g = tid / kLanes, c = tid - g * kLanes;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (g < kGroups) {
+            const float4 *o = reinterpret_cast<const float4 *>(a.part_o + row * a.n_split * D) + c;
+#pragma unroll 4
+            for (int i = g; i < splits; i += kGroups) {
+                const float4 u = o[static_cast<int64_t>(i) * kLanes];
+                const float f = s_f[i];
+                v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
+            }
+            s_o[g][c] = v;
+        }
+        __syncthreads();
+        if (g == 0) {
+#pragma unroll
+            for (int k = 1; k < kGroups; ++k) {
+                const float4 u = s_o[k][c];
+                v.x += u.x, v.y += u.y, v.z += u.z, v.w += u.w;
+            }
+            const float r = s_inv;
+            paged_store4(a.o, a.o_type, row * D + c * 4, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+        }
+        __syncthreads();  // shared memory serves the next head
+    }
+    if (!weights) return;
+
+    float *w = weights + b * w_sb + blockIdx.y * w_sh + range.base;
+    bool held = false;
+    for (int t0 = blockIdx.x * 4 * kJoinThreads; t0 < range.count(); t0 += gridDim.x * 4 * kJoinThreads) {
+        const int t = t0 + 4 * tid;
+        float p[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int g0 = 0; g0 < a.group; g0 += kJoinHeads) {
+            const int heads = min(kJoinHeads, a.group - g0);
+            if (!held) {  // m + log2 l of each head, a warp each
+                __syncthreads();
+                for (int g = warp; g < heads; g += kJoinThreads / 32) {
+                    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (row0 + g0 + g) * a.n_split;
+                    float m = -1e30f, sum = 0.f;
+                    for (int i = lane; i < splits; i += 32) m = fmaxf(m, ml[i].x);
+#pragma unroll
+                    for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                    for (int i = lane; i < splits; i += 32) {
+                        const float2 v = ml[i];
+                        sum += ex2(v.x - m) * v.y;
+                    }
+#pragma unroll
+                    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                    if (lane == 0) s_lse[g] = m + log2f(sum);
+                }
+                __syncthreads();
+                held = a.group <= kJoinHeads;
+            }
+            if (t < range.count()) {
+                const float *score = a.scores + (row0 + g0) * a.score_stride + t;
+#pragma unroll 4
+                for (int g = 0; g < heads; ++g) {
+                    const float4 s = *reinterpret_cast<const float4 *>(score + g * a.score_stride);
+                    const float lse = s_lse[g];
+                    p[0] += ex2(s.x - lse), p[1] += ex2(s.y - lse), p[2] += ex2(s.z - lse), p[3] += ex2(s.w - lse);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t + i < range.count() && range.base + t + i >= range.first) w[t + i] += p[i];
+    }
 }
 
 int log2_of(int v)
@@ -313,16 +347,22 @@ int log2_of(int v)
     return n;
 }
 
-// Splits per sequence and tokens per split.  A split is a multiple of one tile
-// of each of the CTA's warps.  Long sequences are cut to pieces that keep the
-// SMs evenly loaded when lengths differ; short ones only as far as SMs are
+// Splits per sequence and tokens per split (a multiple of one tile of each of
+// the CTA's warps).  Where lengths differ, many CTAs are empty or short: four
+// times as many as the SMs hold keep them loaded, of 256 tokens at least (a CTA
+// costs some 5 us besides its tiles).  Long sequences are cut to 1024 tokens,
+// up to 16 times what the SMs hold: 8 sequences of up to 65536 tokens, encoded,
+// 100.9 us (2048 102.3, 512 110.0, 4096 122.9); 32 of up to 8192, bf16, 98.6
+// (2048 100.6, 512 104.8, 256 113.8).  A few short ones only as far as SMs are
 // free.
 struct PagedPlan {
     int n_split, chunk;
+    bool cluster;
     int64_t tokens, score_stride;
 };
 
-PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, int64_t max_len, int64_t window)
+PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, int64_t max_len, int64_t window,
+                     bool with_weights)
 {
     PagedPlan p;
     // a window's first tile may hold 15 tokens before it
@@ -337,7 +377,8 @@ PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, i
         sms = 152;
     const int64_t slots = static_cast<int64_t>(sms) * occ;
     int64_t n = (4 * slots + ctas - 1) / ctas;
-    const int64_t most = (p.tokens + 255) / 256;
+    const int64_t most = (p.tokens + 255) / 256, by_length = (p.tokens + 1023) / 1024, full = 16 * slots / ctas;
+    if (n < by_length && n < full) n = by_length < full ? by_length : full;
     if (n > most) n = most;
     if (n * ctas < slots) {
         const int64_t fill = (slots + ctas - 1) / ctas, tiles = (p.tokens + 63) / 64;
@@ -349,6 +390,9 @@ PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, i
     p.chunk = static_cast<int>(chunk);
     p.n_split = static_cast<int>((p.tokens + chunk - 1) / chunk);
     if (p.n_split < 1) p.n_split = 1;
+    // All CTAs resident at once and at most 8 splits: a head's splits are a
+    // cluster and join themselves, which saves the join's launch.
+    p.cluster = p.n_split > 1 && p.n_split <= kMaxCluster && p.n_split * ctas <= slots && !with_weights;
     p.score_stride = (p.tokens + 63) / 64 * 64;
     return p;
 }
@@ -382,17 +426,19 @@ cudaError_t launch_paged_16bit(int type, int dim, const PagedArgs &a, dim3 grid,
 size_t paged_attention_workspace_bytes(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, int64_t max_len,
                                        int64_t window, bool with_weights)
 {
-    const PagedPlan p = paged_plan(c, seqs, q_heads, max_len, window);
+    const PagedPlan p = paged_plan(c, seqs, q_heads, max_len, window, with_weights);
     const size_t rows = static_cast<size_t>(seqs) * q_heads;
     size_t n = 256;
-    if (p.n_split > 1) n += up256(rows * p.n_split * c->dim * 4) + up256(rows * p.n_split * 8);
-    if (with_weights) n += up256(rows * 4) + up256(rows * static_cast<size_t>(p.score_stride) * 4);
+    const bool join = p.n_split > 1 && !p.cluster;
+    if (join) n += up256(rows * p.n_split * c->dim * 4);
+    if (join || with_weights) n += up256(rows * p.n_split * 8);
+    if (with_weights) n += up256(rows * static_cast<size_t>(p.score_stride) * 4);
     return n;
 }
 
 cudaError_t launch_paged_attention(const quartz_paged_cache_t *c, const PagedAttnCall &call, cudaStream_t s)
 {
-    const PagedPlan p = paged_plan(c, call.seqs, call.q_heads, call.max_len, call.window);
+    const PagedPlan p = paged_plan(c, call.seqs, call.q_heads, call.max_len, call.window, call.weights != nullptr);
     PagedArgs a{};
     a.q = static_cast<const uint16_t *>(call.q);
     a.q_sb = call.q_sb, a.q_sh = call.q_sh;
@@ -422,15 +468,17 @@ cudaError_t launch_paged_attention(const quartz_paged_cache_t *c, const PagedAtt
     a.dev_err = call.dev_err;
     uint8_t *ws = static_cast<uint8_t *>(call.workspace);
     const size_t rows = static_cast<size_t>(call.seqs) * call.q_heads;
-    if (p.n_split > 1) {
+    const bool join = p.n_split > 1 && !p.cluster;
+    a.cluster = p.cluster;
+    if (join) {
         a.part_o = reinterpret_cast<float *>(ws);
         ws += up256(rows * p.n_split * c->dim * 4);
+    }
+    if (join || call.weights) {
         a.part_ml = reinterpret_cast<float *>(ws);
         ws += up256(rows * p.n_split * 8);
     }
     if (call.weights) {
-        a.lse = reinterpret_cast<float *>(ws);
-        ws += up256(rows * 4);
         a.scores = reinterpret_cast<float *>(ws);
         a.score_stride = p.score_stride;
     }
@@ -438,19 +486,16 @@ cudaError_t launch_paged_attention(const quartz_paged_cache_t *c, const PagedAtt
                     static_cast<unsigned>(call.seqs));
     cudaError_t e = c->type == QUARTZ_PAGES_ENCODED ? launch_paged_encoded(c->dim, c->k.enc.p.group_s, a, grid, s)
                                                     : launch_paged_16bit(c->type, c->dim, a, grid, s);
-    if (e == cudaSuccess && p.n_split > 1) {
-        const dim3 join(static_cast<unsigned>(rows));
+    if (e == cudaSuccess && (join || call.weights)) {
+        int64_t x = join ? a.group : 1;
+        if (call.weights && (p.tokens + 4 * kJoinThreads - 1) / (4 * kJoinThreads) > x) x = (p.tokens + 4 * kJoinThreads - 1) / (4 * kJoinThreads);
+        const dim3 g(static_cast<unsigned>(x), static_cast<unsigned>(c->heads), static_cast<unsigned>(call.seqs));
         switch (c->dim) {
-            case 64: e = launch_pdl(paged_join_kernel<64>, join, dim3(256), 0, s, a); break;
-            case 128: e = launch_pdl(paged_join_kernel<128>, join, dim3(256), 0, s, a); break;
-            case 192: e = launch_pdl(paged_join_kernel<192>, join, dim3(256), 0, s, a); break;
-            default: e = launch_pdl(paged_join_kernel<256>, join, dim3(256), 0, s, a); break;
+            case 64: e = launch_pdl(paged_join_kernel<64>, g, dim3(kJoinThreads), 0, s, a, call.weights, call.w_sb, call.w_sh); break;
+            case 128: e = launch_pdl(paged_join_kernel<128>, g, dim3(kJoinThreads), 0, s, a, call.weights, call.w_sb, call.w_sh); break;
+            case 192: e = launch_pdl(paged_join_kernel<192>, g, dim3(kJoinThreads), 0, s, a, call.weights, call.w_sb, call.w_sh); break;
+            default: e = launch_pdl(paged_join_kernel<256>, g, dim3(kJoinThreads), 0, s, a, call.weights, call.w_sb, call.w_sh); break;
         }
-    }
-    if (e == cudaSuccess && call.weights) {
-        const dim3 g(static_cast<unsigned>((p.tokens + 1023) / 1024), static_cast<unsigned>(c->heads),
-                     static_cast<unsigned>(call.seqs));
-        e = launch_pdl(paged_weights_kernel, g, dim3(256), 0, s, a, call.weights, call.w_sb, call.w_sh);
     }
     return e;
 }

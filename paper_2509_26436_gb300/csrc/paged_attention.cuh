@@ -53,9 +53,10 @@ struct PagedArgs {
     int page_shift, kv_heads, group, head_blocks;  // query heads per key head; CTAs they take
     int max_len, window, n_split, chunk;
     float scale_log2;
-    float *part_o, *part_ml;  // [seqs * q_heads][n_split][dim], [..][2]; NULL: one split, o is written
-    float *lse;               // with scores: [seqs * q_heads], log2 domain
-    float *scores;            // NULL, or [seqs * q_heads][score_stride], log2 domain
+    float *part_o;   // NULL, or [seqs * q_heads][n_split][dim]: splits for the join kernel; NULL: o is written
+    float *part_ml;  // NULL, or [seqs * q_heads][n_split][2]: maximum and sum (with part_o or scores)
+    int cluster;     // the splits of a head are one cluster, which joins them itself
+    float *scores;   // NULL, or [seqs * q_heads][score_stride], log2 domain
     int64_t score_stride;
     void *o;
     int o_type;
@@ -234,11 +235,38 @@ __device__ __forceinline__ void paged_store4(void *o, int type, int64_t at, floa
     else paged_store4<float>(o, at, v);
 }
 
+// Cluster barrier (all threads of all CTAs) and reads of another CTA's shared
+// memory.
+__device__ __forceinline__ void paged_cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t paged_remote(uint32_t addr, int rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float paged_remote_f32(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 paged_remote_f4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
+}
+
 // Join the warps of a CTA in a fixed order and write the split's result: the
-// output itself where there is one split, else o (relative to the split's
-// maximum) with maximum and sum.
+// output itself where there is one split; o (relative to the split's maximum)
+// with maximum and sum for the join kernel; or, where the splits of a head are
+// a cluster, the output of all of them, each CTA its share of the elements.
 struct PagedJoin {
     float m[kPagedWarps][kPagedHeads], l[kPagedWarps][kPagedHeads];
+    float all_m[kPagedHeads], all_l[kPagedHeads];  // of the CTA
 };
 
 // `smem` + warp * warp_bytes is the warp's own shared memory, at least
@@ -297,17 +325,42 @@ __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int wa
             sum += f * s.l[w][h];
             v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
         }
-        const int64_t row = row0 + h;
-        if (a.part_o) {
-            const int64_t at = row * a.n_split + split;
+        const int64_t row = row0 + h, at = row * a.n_split + split;
+        if (a.part_ml && d == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, sum);
+        if (a.cluster) {
+            *so(0, h, d) = v;  // read by this thread only, above
+            if (d == 0) s.all_m[h] = m, s.all_l[h] = sum;
+        } else if (a.part_o) {
             *reinterpret_cast<float4 *>(a.part_o + at * D + d) = v;
-            if (d == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, sum);
         } else {
             const float r = sum > 0.f ? 1.f / sum : 0.f;
             paged_store4(a.o, a.o_type, row * D + d, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
-            if (a.lse && d == 0) a.lse[row] = m + log2f(sum);
         }
     }
+    if (!a.cluster) return;
+    __syncwarp();
+    paged_cluster_sync();
+    const uint32_t s_m = static_cast<uint32_t>(__cvta_generic_to_shared(s.all_m));
+    const uint32_t s_l = static_cast<uint32_t>(__cvta_generic_to_shared(s.all_l));
+    for (int e = split * kPagedThreads + threadIdx.x; e < kPagedHeads * (D / 4); e += a.n_split * kPagedThreads) {
+        const int h = e / (D / 4), d = (e - h * (D / 4)) * 4;
+        if (head0 + h >= a.group) break;
+        float m = -1e30f, sum = 0.f;
+        for (int c = 0; c < a.n_split; ++c) m = fmaxf(m, paged_remote_f32(paged_remote(s_m + 4 * h, c)));
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(so(0, h, d)));
+#pragma unroll 4
+        for (int c = 0; c < a.n_split; ++c) {
+            const float f = ex2(paged_remote_f32(paged_remote(s_m + 4 * h, c)) - m);
+            const float4 u = paged_remote_f4(paged_remote(mine, c));
+            sum += f * paged_remote_f32(paged_remote(s_l + 4 * h, c));
+            v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
+        }
+        const float r = sum > 0.f ? 1.f / sum : 0.f;
+        paged_store4(a.o, a.o_type, (row0 + h) * D + d, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
+    }
+    __syncwarp();
+    paged_cluster_sync();  // no CTA leaves while another reads its shared memory
 }
 
 // CTAs resident per SM of the kernel that serves this cache.

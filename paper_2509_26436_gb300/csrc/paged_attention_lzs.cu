@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     __shared__ __align__(16) uint16_t s_q[kPagedHeads][D + 8];
     __shared__ PagedJoin s_join;
 
-    const int head_block = blockIdx.x % a.head_blocks, split = blockIdx.x / a.head_blocks;
+    const int head_block = blockIdx.x / a.n_split, split = blockIdx.x - head_block * a.n_split;
     const int kv_head = blockIdx.y, b = blockIdx.z, head0 = head_block * kPagedHeads;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
@@ -444,6 +444,8 @@ struct KernelLzs {
     {
         const cudaError_t e = ready();  // of the current device
         if (e != cudaSuccess) return e;
+        if (a.cluster)
+            return launch_pdl_cluster(paged_attn_lzs_kernel<D, GS, MINB>, a.n_split, grid, dim3(kPagedThreads), kSmem, s, a);
         return launch_pdl(paged_attn_lzs_kernel<D, GS, MINB>, grid, dim3(kPagedThreads), kSmem, s, a);
     }
 };

@@ -1,18 +1,20 @@
 // Rotary positions for sm_103a: y = rotation of x [tokens, heads, dim] by
 // position times frequency, pairs (i, i + rotary/2) or (2i, 2i + 1).
 //
-// HBM-bound: x is read and y written once, 3 operations per element.  A CTA
-// goes through tokens; a thread has the same pieces of a head (V pairs each,
-// two V-element vectors) in all of them.  The next token's vectors are loaded
-// while this one's angles, one per thread, are computed into shared memory and
-// its pairs turned.
+// HBM-bound: x is read and y written once, 3 operations per element.  A thread
+// turns V pairs of one token (two V-element vectors) in several heads; the
+// threads of a CTA that have the same pairs in other heads share the angles,
+// computed once per CTA, which costs about as much as turning them in ten
+// heads.  Many threads with one head in flight each (64 registers, 1024 per SM)
+// measured better than fewer with more: 8192 x 32 x 128 bf16, of a strided
+// tensor: with angles per thread 28.5 us with one head in flight, 31.2 with two,
+// 38.3 with four; with shared angles 26.7 (a plain copy of as many bytes: 22.9).
 #include "quartz_internal.h"
 #include "rope.cuh"
 
 namespace quartz {
 namespace {
 
-constexpr int kMaxPairs = 256;
 constexpr int kThreads = 128;
 
 template <typename T, int V>
@@ -21,113 +23,89 @@ struct alignas(sizeof(T) * V) Vec {
 };
 
 // Piece p < pairs / V of a head turns V pairs, the others copy V elements each
-// from `rotary` on.  ITEMS pieces per thread; blockIdx.y: further pieces.
-template <typename T, int V, int ITEMS>
-__global__ void __launch_bounds__(kThreads) rope_kernel(RopeArgs a, int tokens)
+// from `rotary` on.  `here` (token, piece) places per CTA, as consecutive
+// threads; the threads behind them: the same places in further heads.
+template <typename T, int V>
+__global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs a, int64_t places, int here, int heads_each)
 {
     griddep_wait();
-    __shared__ float2 s_cs[2][kMaxPairs];
-    __shared__ uint64_t s_unit[kMaxPairs];
+    __shared__ float2 s_cs[V * kThreads];  // [pair of the piece][place]
     const int pairs = a.rope.rotary / 2;
     const int turns = pairs / V, pieces = turns + (a.dim - a.rope.rotary) / V;
-    const T *x = static_cast<const T *>(a.x);
-    T *y = static_cast<T *>(a.y);
-    int64_t in1[ITEMS], out1[ITEMS];
-    int gap[ITEMS], cs_at[ITEMS];  // from the first vector to the second (0: none, copy); angles
-    bool mine[ITEMS];
-#pragma unroll
-    for (int k = 0; k < ITEMS; ++k) {
-        const int i = (blockIdx.y * ITEMS + k) * kThreads + threadIdx.x;
-        const int h = i / pieces, p = i - h * pieces;
-        mine[k] = h < a.heads;
-        const bool turn = p < turns;
-        const int o1 = turn ? (a.rope.interleaved ? 2 * p * V : p * V) : a.rope.rotary + (p - turns) * V;
-        gap[k] = turn ? (a.rope.interleaved ? V : pairs) : 0;
-        cs_at[k] = turn ? p * V : 0;
-        in1[k] = h * a.x_sh + o1;
-        out1[k] = h * a.y_sh + o1;
-    }
-    for (int i = threadIdx.x; i < pairs; i += kThreads) s_unit[i] = rope_unit(a.rope.freqs[i]);
-    const float sign = a.rope.backward ? -1.f : 1.f;
+    const int64_t first_place = static_cast<int64_t>(blockIdx.x) * here;
+    const int group = threadIdx.x / here, place = threadIdx.x - group * here;
+    const int64_t id = first_place + place;
+    const bool in = id < places;
+    const int64_t t = in ? id / pieces : 0;
+    const int p = in ? static_cast<int>(id - t * pieces) : 0;
+    const bool turn = p < turns;
+    const int first = turn ? (a.rope.interleaved ? 2 * p * V : p * V) : a.rope.rotary + (p - turns) * V;
+    const int gap = a.rope.interleaved ? V : pairs;  // from the first vector to the second
+    const int h0 = group * heads_each, h1 = in ? min(a.heads, h0 + heads_each) : 0;
+    const T *x = static_cast<const T *>(a.x) + t * a.x_st + first;
+    T *y = static_cast<T *>(a.y) + t * a.y_st + first;
 
-    Vec<T, V> u[ITEMS], w[ITEMS];
-    auto load = [&](int64_t t) {
-#pragma unroll
-        for (int k = 0; k < ITEMS; ++k)
-            if (mine[k]) {
-                const T *p = x + t * a.x_st + in1[k];
-                u[k] = *reinterpret_cast<const Vec<T, V> *>(p);
-                if (gap[k]) w[k] = *reinterpret_cast<const Vec<T, V> *>(p + gap[k]);
-            }
-    };
-    int64_t t = blockIdx.x;
-    int64_t pos = a.rope.positions[t];
-    load(t);
-    __syncthreads();  // s_unit
-    for (int buffer = 0; t < tokens; buffer ^= 1) {
-        for (int i = threadIdx.x; i < pairs; i += kThreads) {
-            const float2 cs = rope_cos_sin(pos, s_unit[i], a.rope.scale);
-            s_cs[buffer][i] = make_float2(cs.x, sign * cs.y);
+    Vec<T, V> u, w;
+    if (h0 < h1) {  // the first head's loads, under way meanwhile
+        u = *reinterpret_cast<const Vec<T, V> *>(x + h0 * a.x_sh);
+        if (turn) w = *reinterpret_cast<const Vec<T, V> *>(x + h0 * a.x_sh + gap);
+    }
+    for (int i = threadIdx.x; i < here * V; i += kThreads) {
+        const int j = i / here;
+        const int64_t at = first_place + (i - j * here);
+        const int64_t token = at / pieces;
+        const int piece = static_cast<int>(at - token * pieces);
+        if (at < places && piece < turns) {
+            const float2 cs = rope_cos_sin(a.rope.positions[token], rope_unit(a.rope.freqs[piece * V + j]), a.rope.scale);
+            s_cs[i] = make_float2(cs.x, a.rope.backward ? -cs.y : cs.y);
         }
-        const int64_t now = t;
-        t += gridDim.x;
-        Vec<T, V> cu[ITEMS], cw[ITEMS];
+    }
+    __syncthreads();
+    float2 cs[V];
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) cu[k] = u[k], cw[k] = w[k];
-        if (t < tokens) {
-            pos = a.rope.positions[t];
-            load(t);
+    for (int j = 0; j < V; ++j) cs[j] = s_cs[j * here + place];
+    for (int h = h0; h < h1; ++h) {
+        if (h > h0) {
+            u = *reinterpret_cast<const Vec<T, V> *>(x + h * a.x_sh);
+            if (turn) w = *reinterpret_cast<const Vec<T, V> *>(x + h * a.x_sh + gap);
         }
-        __syncthreads();  // the angles; the other buffer's readers are past the barrier before
+        T *to = y + h * a.y_sh;
+        if (turn) {
+            Vec<T, V> r1, r2;
 #pragma unroll
-        for (int k = 0; k < ITEMS; ++k) {
-            if (!mine[k]) continue;
-            T *to = y + now * a.y_st + out1[k];
-            if (gap[k]) {
-                Vec<T, V> r1, r2;
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float2 cs = s_cs[buffer][cs_at[k] + j];
-                    if (a.rope.interleaved) {
-                        // elements 2j and 2j + 1 of the 2V read
-                        const T x1 = 2 * j < V ? cu[k].e[(2 * j) % V] : cw[k].e[(2 * j) % V];
-                        const T x2 = 2 * j + 1 < V ? cu[k].e[(2 * j + 1) % V] : cw[k].e[(2 * j + 1) % V];
-                        const float2 r = rope_turn(to_f32<T>(x1), to_f32<T>(x2), cs);
-                        (2 * j < V ? r1 : r2).e[(2 * j) % V] = from_f32<T>(r.x);
-                        (2 * j + 1 < V ? r1 : r2).e[(2 * j + 1) % V] = from_f32<T>(r.y);
-                    } else {
-                        const float2 r = rope_turn(to_f32<T>(cu[k].e[j]), to_f32<T>(cw[k].e[j]), cs);
-                        r1.e[j] = from_f32<T>(r.x);
-                        r2.e[j] = from_f32<T>(r.y);
-                    }
+            for (int j = 0; j < V; ++j) {
+                if (a.rope.interleaved) {
+                    // elements 2j and 2j + 1 of the 2V read
+                    const T x1 = 2 * j < V ? u.e[(2 * j) % V] : w.e[(2 * j) % V];
+                    const T x2 = 2 * j + 1 < V ? u.e[(2 * j + 1) % V] : w.e[(2 * j + 1) % V];
+                    const float2 r = rope_turn(to_f32<T>(x1), to_f32<T>(x2), cs[j]);
+                    (2 * j < V ? r1 : r2).e[(2 * j) % V] = from_f32<T>(r.x);
+                    (2 * j + 1 < V ? r1 : r2).e[(2 * j + 1) % V] = from_f32<T>(r.y);
+                } else {
+                    const float2 r = rope_turn(to_f32<T>(u.e[j]), to_f32<T>(w.e[j]), cs[j]);
+                    r1.e[j] = from_f32<T>(r.x);
+                    r2.e[j] = from_f32<T>(r.y);
                 }
-                *reinterpret_cast<Vec<T, V> *>(to) = r1;
-                *reinterpret_cast<Vec<T, V> *>(to + gap[k]) = r2;
-            } else {
-                *reinterpret_cast<Vec<T, V> *>(to) = cu[k];
             }
+            *reinterpret_cast<Vec<T, V> *>(to) = r1;
+            *reinterpret_cast<Vec<T, V> *>(to + gap) = r2;
+        } else {
+            *reinterpret_cast<Vec<T, V> *>(to) = u;
         }
     }
-}
-
-template <typename T, int V, int ITEMS>
-cudaError_t launch_items(const RopeArgs &a, int64_t tokens, int64_t items, cudaStream_t s)
-{
-    const int64_t y = (items + ITEMS * kThreads - 1) / (ITEMS * kThreads);
-    int64_t x = (152 * 16 + y - 1) / y;  // some 16 CTAs per SM, each with several tokens where there are more
-    if (x > tokens) x = tokens;
-    return launch_pdl(rope_kernel<T, V, ITEMS>, dim3(static_cast<unsigned>(x), static_cast<unsigned>(y)), dim3(kThreads), 0, s, a,
-                      static_cast<int>(tokens));
 }
 
 template <typename T, int V>
 cudaError_t launch_v(const RopeArgs &a, int64_t tokens, cudaStream_t s)
 {
-    const int64_t items = static_cast<int64_t>(a.heads) * (a.rope.rotary / 2 / V + (a.dim - a.rope.rotary) / V);
-    // Two pieces per thread share a CTA's angles where there is work for all
-    // SMs; else one.
-    if (tokens * items >= 152 * 2048) return launch_items<T, V, 2>(a, tokens, items, s);
-    return launch_items<T, V, 1>(a, tokens, items, s);
+    const int64_t places = tokens * (a.rope.rotary / 2 / V + (a.dim - a.rope.rotary) / V);
+    // More groups of heads per CTA while there are fewer than 2048 threads per SM
+    // (8192 x 32 x 128: 26.7 us; up to 1024 27.3, up to 8192 35.3)
+    int groups = 1;
+    while (groups < 32 && groups < a.heads && places * groups < 152 * 2048) groups *= 2;
+    const int here = kThreads / groups, each = (a.heads + groups - 1) / groups;
+    return launch_pdl(rope_kernel<T, V>, dim3(static_cast<unsigned>((places + here - 1) / here)), dim3(kThreads), 0, s, a, places,
+                      here, each);
 }
 
 // The widest vectors of V elements (16 bytes, or 8) that sizes, strides and
