@@ -48,19 +48,44 @@ __device__ __forceinline__ uint32_t and_xor(uint32_t x, uint32_t mask, uint32_t 
     return d;
 }
 
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+
+// What a key's codes with FLAG F take: pairs of 2^F, 2^F / 16, -1032 2^F and
+// -72 2^F (all exact; by fp16 products rather than integer sums, since the
+// logic pipe is the busiest).
+struct KeyFlag {
+    uint32_t m0, m1, a0, a1;
+    __device__ __forceinline__ explicit KeyFlag(uint32_t f)
+    {
+        m0 = f * 0x04000400u + 0x3C003C00u;
+        m1 = mul_f16x2(m0, 0x2C002C00u);
+        a0 = mul_f16x2(m0, 0xE408E408u);
+        a1 = mul_f16x2(m0, 0xD480D480u);
+    }
+};
+
 // The eight codes of a word (code k in bits 4k ..) times 2^F as fp16 pairs
 // (k, k + 4): f = 1024 + (c + 8), or 1024 + 16 (c + 8) for the odd nibbles of
-// each byte; f 2^F - 1032 2^F, f 2^F / 16 - 72 2^F.  `flag4` = F in the
-// exponent fields of a pair (F * 0x04000400).
-__device__ __forceinline__ void key_codes(uint32_t w, uint32_t flag4, uint32_t (&k)[4])
+// each byte; f 2^F - 1032 2^F, f 2^F / 16 - 72 2^F.
+__device__ __forceinline__ void key_codes(uint32_t w, const KeyFlag &f, uint32_t (&k)[4])
 {
-    const uint32_t m0 = 0x3C003C00u + flag4, m1 = 0x2C002C00u + flag4;  // 2^F, 2^F / 16
-    const uint32_t a0 = 0xE408E408u + flag4, a1 = 0xD480D480u + flag4;  // -1032 2^F, -72 2^F
     const uint32_t w8 = w >> 8;
-    k[0] = fma_f16x2(and_xor(w, 0x000F000Fu, 0x64086408u), m0, a0);
-    k[1] = fma_f16x2(and_xor(w, 0x00F000F0u, 0x64806480u), m1, a1);
-    k[2] = fma_f16x2(and_xor(w8, 0x000F000Fu, 0x64086408u), m0, a0);
-    k[3] = fma_f16x2(and_xor(w8, 0x00F000F0u, 0x64806480u), m1, a1);
+    k[0] = fma_f16x2(and_xor(w, 0x000F000Fu, 0x64086408u), f.m0, f.a0);
+    k[1] = fma_f16x2(and_xor(w, 0x00F000F0u, 0x64806480u), f.m1, f.a1);
+    k[2] = fma_f16x2(and_xor(w8, 0x000F000Fu, 0x64086408u), f.m0, f.a0);
+    k[3] = fma_f16x2(and_xor(w8, 0x00F000F0u, 0x64806480u), f.m1, f.a1);
 }
 
 // The eight codes of a word of token 0 and of token 1, times 2^F0 and 2^F1, as
@@ -68,8 +93,7 @@ __device__ __forceinline__ void key_codes(uint32_t w, uint32_t flag4, uint32_t (
 // = F0 + (F1 << 16).
 __device__ __forceinline__ void value_codes(uint32_t w0, uint32_t w1, uint32_t flags, uint32_t (&v)[8])
 {
-    const uint32_t f = flags << 7;
-    const uint32_t m = 0x3F803F80u + f, a = 0xC308C308u + f;  // 2^F, -136 2^F
+    const uint32_t m = flags * 128u + 0x3F803F80u, a = mul_bf16x2(m, 0xC308C308u);  // 2^F, -136 2^F
     const uint32_t lo = permute(w0, w1, 0x5410), hi = permute(w0, w1, 0x7632);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -87,7 +111,7 @@ struct LzsTile {
     static constexpr int kTokens = 16, kChunks = D / 32;  // 16-byte chunks of codes per row
     static constexpr int kCodes = kTokens * D / 2, kFlags = kTokens * D / GS, kScales = kTokens * D / 32;
     static constexpr int kSide = kCodes + kFlags + kScales, kBytes = 2 * kSide;
-    static constexpr int kStages = D <= 128 ? 4 : 3;
+    static constexpr int kStages = 5;
     // The small planes of both sides as 16-byte chunks: FLAGs, scales, FLAGs, scales.
     static constexpr int kSmall = 2 * (kFlags + kScales) / 16, kSmallPerLane = (kSmall + 31) / 32;
     static constexpr int kCodesPerLane = kCodes / 16 / 32 > 0 ? kCodes / 16 / 32 : 1;
@@ -107,34 +131,36 @@ struct LzsTile {
     }
 };
 
+// Loads of a tile that has arrived: free to move, from the point on where its
+// address was made (`fixed`, after the wait).
 __device__ __forceinline__ uint32_t lds32(uint32_t a)
 {
     uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
+    asm("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(a));
     return v;
 }
 __device__ __forceinline__ uint2 lds64(uint32_t a)
 {
     uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
+    asm("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
     return v;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t a)
 {
     uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
+    asm("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a));
     return v;
 }
 __device__ __forceinline__ uint32_t lds16(uint32_t a)
 {
     uint16_t v;
-    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
+    asm("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(a));
     return v;
 }
 __device__ __forceinline__ uint32_t lds8(uint32_t a)
 {
     uint32_t v;
-    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
+    asm("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a));
     return v;
 }
 
@@ -165,14 +191,16 @@ __device__ __forceinline__ void lds_scales(uint32_t a, float (&s)[G])
     }
 }
 
-template <int D, int GS, int MINB>
+// GENERAL: pages below 16 tokens, or with scores for the sums of weights; the
+// other instance is for pages of 16 and more without.
+template <int D, int GS, bool GENERAL, int MINB>
 __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(PagedArgs a)
 {
     griddep_wait();
     using Tile = LzsTile<D, GS>;
     constexpr int G = D / 64, FPR = D / GS;  // groups and FLAGs per row
     constexpr int kStages = Tile::kStages, kWarpBytes = kStages * Tile::kBytes;
-    constexpr bool kQRegs = D <= 128;
+    constexpr bool kQRegs = D <= 128;  // wider heads read the query from shared memory again for each tile
     static_assert(kWarpBytes >= kPagedJoinBytes<D>, "the join uses the ring");
     extern __shared__ __align__(16) uint8_t s_ring[];
     __shared__ __align__(16) uint16_t s_q[kPagedHeads][D + 8];
@@ -185,8 +213,10 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     const int begin = split * a.chunk;
     if (a.part_o && begin >= range.count()) return;
     const int end = range.base + min(begin + a.chunk, range.count());
-    const int base0 = range.base + begin + warp * 16;
-    const int tiles = base0 < end ? (end - base0 + kPagedWarps * 16 - 1) / (kPagedWarps * 16) : 0;
+    // a warp's tiles are consecutive, so that most follow the one before in its page
+    const int all_tiles = max(0, end - range.base - begin + 15) >> 4, warp_tiles = (all_tiles + kPagedWarps - 1) / kPagedWarps;
+    const int tiles = max(0, min(warp_tiles, all_tiles - warp * warp_tiles));
+    const int base0 = range.base + begin + warp * warp_tiles * 16;
     const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + warp * kWarpBytes;
 
     // --- copies of a tile -------------------------------------------------
@@ -216,48 +246,57 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
         small_row[k] = in ? (flag ? FPR : 2 * G) : -1;
         small_dst[k] = side * Tile::kSide + Tile::kCodes + i * 16;
     }
-    auto seen = [&](int t) { return max(min(t, end - 1), range.first); };
-    auto page_of = [&](int t) {
-        const uint32_t page = static_cast<uint32_t>(__ldg(table + (seen(t) >> a.page_shift)));
-        bad |= page >= a.num_pages;
-        return page < a.num_pages ? page : 0u;
+    auto checked = [&](int32_t page) {
+        bad |= static_cast<uint32_t>(page) >= a.num_pages;
+        return static_cast<uint32_t>(page) < a.num_pages ? static_cast<uint32_t>(page) : 0u;
     };
     auto row_of = [&](uint32_t page, int t) {
         return ((page * a.kv_heads + kv_head) << a.page_shift) + (static_cast<uint32_t>(t) & page_mask);
     };
-    const bool small_pages = a.page_shift < 4;
+    const bool small_pages = GENERAL && a.page_shift < 4;
+    // The next tile to fetch: its first token and cache row; the table's entry
+    // for the page behind, read a page ahead.
+    int at = base0;
+    uint32_t at_row = 0;
+    int32_t page_behind = 0;
+    const int last_page = (end - 1) >> a.page_shift;
+    auto enter = [&](int32_t page) {
+        at_row = row_of(checked(page), at);
+        const int behind = (at >> a.page_shift) + 1;
+        if (behind <= last_page) page_behind = __ldg(table + behind);
+    };
+    if (tiles > 0 && !small_pages) enter(__ldg(table + (at >> a.page_shift)));
     // Pages of 16 or more: 16 consecutive rows.  Smaller ones: row by row; the
     // small planes' rows are then below the 16 bytes of a copy and go through
     // registers.  There a token that is not seen repeats the nearest that is.
-    auto fetch = [&](int base, uint32_t page, int stage) {
+    auto fetch = [&](int stage) {
         const uint32_t to = ring + stage * Tile::kBytes;
         if (!small_pages) {
-            const uint64_t row = row_of(page, base);
+            const uint64_t row = at_row;
             const uint8_t *kc = a.k.codes + row * (D / 2) + lane * 16, *vc = a.v.codes + row * (D / 2) + lane * 16;
 #pragma unroll
-            for (int k = 0; k < Tile::kCodesPerLane; ++k)
-                if (Tile::kCodes / 16 >= 32 || lane < Tile::kCodes / 16) {
-                    paged_copy16(to + key_dst[k], kc + k * 512);
-                    paged_copy16(to + value_dst[k], vc + k * 512);
-                }
+            for (int k = 0; k < Tile::kCodesPerLane; ++k) {
+                paged_copy16(to + key_dst[k], kc + k * 512);
+                paged_copy16(to + value_dst[k], vc + k * 512);
+            }
 #pragma unroll
             for (int k = 0; k < Tile::kSmallPerLane; ++k)
                 if (small_row[k] >= 0) paged_copy16(to + small_dst[k], small_src[k] + row * small_row[k]);
+            at += 16;
+            at_row += 16;
+            if ((at & page_mask) == 0 && at < end) enter(page_behind);
         } else {
-            const int mine = seen(base + (lane & 15));
-            const uint32_t my_row = row_of(page_of(mine), mine);
+            const int mine = max(min(at + (lane & 15), end - 1), range.first);
+            const uint32_t my_row = row_of(checked(__ldg(table + (mine >> a.page_shift))), mine);
 #pragma unroll
             for (int k = 0; k < Tile::kCodesPerLane; ++k) {
                 const int i = lane + 32 * k, t = i / Tile::kChunks, c = i % Tile::kChunks;
-                const uint64_t row = __shfl_sync(0xffffffffu, my_row, t & 15);
-                if (Tile::kCodes / 16 >= 32 || lane < Tile::kCodes / 16) {
-                    paged_copy16(to + key_dst[k], a.k.codes + row * (D / 2) + c * 16);
-                    paged_copy16(to + value_dst[k], a.v.codes + row * (D / 2) + c * 16);
-                }
+                const uint64_t row = __shfl_sync(0xffffffffu, my_row, t);
+                paged_copy16(to + key_dst[k], a.k.codes + row * (D / 2) + c * 16);
+                paged_copy16(to + value_dst[k], a.v.codes + row * (D / 2) + c * 16);
             }
             const PagedSide &ps = lane < 16 ? a.k : a.v;  // a lane per row and side
-            uint8_t *dst = s_ring + (to - static_cast<uint32_t>(__cvta_generic_to_shared(s_ring))) +
-                           (lane < 16 ? 0 : Tile::kSide) + Tile::kCodes;
+            uint8_t *dst = s_ring + warp * kWarpBytes + stage * Tile::kBytes + (lane < 16 ? 0 : Tile::kSide) + Tile::kCodes;
             const uint8_t *fl = ps.flags + static_cast<uint64_t>(my_row) * FPR;
 #pragma unroll
             for (int i = 0; i < FPR; ++i) dst[(lane & 15) * FPR + i] = __ldg(fl + i);
@@ -265,15 +304,14 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 #pragma unroll
             for (int i = 0; i < G; ++i)
                 reinterpret_cast<__half *>(dst + Tile::kFlags)[(lane & 15) * G + i] = __ldg(sc + i);
+            at += 16;
         }
     };
-    uint32_t next_page = 0;  // of the next tile to fetch
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) {
-        if (s < tiles) fetch(base0 + s * kPagedWarps * 16, page_of(base0 + s * kPagedWarps * 16), s);
+        if (s < tiles) fetch(s);
         paged_commit();
     }
-    if (kStages - 1 < tiles) next_page = page_of(base0 + (kStages - 1) * kPagedWarps * 16);
 
     // --- the query, in the order the keys' codes unpack to: pairs (k, k + 4) of
     // each 8 elements
@@ -297,7 +335,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     // + 2 i, values of tokens 4 q + j.  Bases that differ between lanes are
     // held in registers (`fixed` keeps the compiler from recomputing them for
     // every tile), the rest are immediate offsets.
-    const int key_token = (n >> 1) * 4 + (n & 1), odd = (n >> 1) & 1;
+    const int key_token = (n >> 1) * 4 + (n & 1);
     constexpr int kRow = Tile::kChunks * 16;
     constexpr int KB = D == 256 ? 4 : 2, VB = D == 256 ? 4 : D == 128 ? 2 : 1;
     uint32_t kb[KB], vb[VB];
@@ -312,31 +350,13 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     const uint32_t ksb = fixed(Tile::kCodes + Tile::kFlags + key_token * 2 * G);
     const uint32_t vfb = fixed(Tile::kSide + Tile::kCodes + 4 * q * FPR + (n * 8) / GS);
 
-    PagedState<D> st;
-    st.init();
-    const int64_t score_row = ((static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0 + 2 * q) * a.score_stride;
-    int stage = 0;
-    for (int it = 0; it < tiles; ++it) {
-        const int base = base0 + it * kPagedWarps * 16;
-        paged_wait<kStages - 2>();
-        __syncwarp();
-        {
-            const int ahead = it + kStages - 1;
-            if (ahead < tiles) {
-                fetch(base0 + ahead * kPagedWarps * 16, next_page, stage == 0 ? kStages - 1 : stage - 1);
-                if (ahead + 1 < tiles) next_page = page_of(base0 + (ahead + 1) * kPagedWarps * 16);
-            }
-            paged_commit();
-        }
-        const uint32_t tile = ring + stage * Tile::kBytes;
-        stage = stage == kStages - 1 ? 0 : stage + 1;
-
-        // scores of tokens i and heads x: a sum per group, times the group's scale
-        float sc[2][2] = {{0.f, 0.f}, {0.f, 0.f}}, ks[2][G], vs[2][G];
+    // Scores of a tile's tokens i and heads x: a sum per group, times the
+    // group's scale.
+    auto score = [&](uint32_t tile, int base, float (&sc)[2][2]) {
+        float ks[2][G];
         lds_scales<G>(tile + ksb, ks[0]);
         lds_scales<G>(tile + ksb + 4 * G, ks[1]);
-        lds_scales<G>(tile + ksb + Tile::kSide, vs[0]);
-        lds_scales<G>(tile + ksb + Tile::kSide + 4 * G, vs[1]);
+        sc[0][0] = sc[0][1] = sc[1][0] = sc[1][1] = 0.f;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             uint32_t k[2][2][4];  // token, word
@@ -344,9 +364,10 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
             for (int i = 0; i < 2; ++i) {
                 const uint2 c = lds64(tile + key_off(i, g));
                 const uint32_t f = GS == 8 ? lds16(tile + kfb + 2 * i * FPR + g * 8) : lds8(tile + kfb + 2 * i * FPR + g * (64 / GS));
-                const uint32_t f0 = (GS == 8 ? f & 0xFFu : f) * 0x04000400u;
+                const KeyFlag f0(GS == 8 ? f & 0xFFu : f);
                 key_codes(c.x, f0, k[i][0]);
-                key_codes(c.y, GS == 8 ? (f >> 8) * 0x04000400u : f0, k[i][1]);
+                if (GS == 8) key_codes(c.y, KeyFlag(f >> 8), k[i][1]);
+                else key_codes(c.y, f0, k[i][1]);
             }
             float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -358,9 +379,26 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 #pragma unroll
             for (int i = 0; i < 2; ++i) sc[i][0] += s[2 * i] * ks[i][g], sc[i][1] += s[2 * i + 1] * ks[i][g];
         }
-
 #pragma unroll
-        for (int i = 0; i < 2; ++i) sc[i][0] *= a.scale_log2, sc[i][1] *= a.scale_log2;
+        for (int i = 0; i < 2; ++i) {
+            const int t = base + key_token + 2 * i;
+            const bool hidden = t >= end || t < range.first;
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                sc[i][x] = hidden ? -INFINITY : sc[i][x] * a.scale_log2;
+                if (GENERAL && a.scores && head0 + 2 * q + x < a.group)
+                    a.scores[(((static_cast<int64_t>(b) * a.kv_heads + kv_head) * a.group + head0 + 2 * q) + x) * a.score_stride +
+                             (t - range.base)] = sc[i][x];
+            }
+        }
+    };
+    PagedState<D> st;
+    st.init();
+    // The weighted values of a tile.
+    auto add_values = [&](uint32_t tile, int base, const float (&p)[2][2]) {
+        float vs[2][G];
+        lds_scales<G>(tile + ksb + Tile::kSide, vs[0]);
+        lds_scales<G>(tile + ksb + Tile::kSide + 4 * G, vs[1]);
         uint32_t vf[2][G];  // FLAGs of token pairs 4 q, 4 q + 1 and 4 q + 2, 4 q + 3
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -368,33 +406,18 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
             for (int g = 0; g < G; ++g)
                 vf[i][g] = lds8(tile + vfb + 2 * i * FPR + g * (64 / GS)) + (lds8(tile + vfb + (2 * i + 1) * FPR + g * (64 / GS)) << 16);
         if (base + 16 > end || base < range.first) {
-            // tokens that are not seen: no weight, and nothing of what their
-            // slots happen to hold (a scale may be NaN)
-            auto unseen = [&](int t) { return base + t >= end || base + t < range.first; };
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (unseen(key_token + 2 * i)) {
-                    sc[i][0] = sc[i][1] = -INFINITY;
-#pragma unroll
-                    for (int g = 0; g < G; ++g) vs[i][g] = 0.f;
-                }
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (unseen(4 * q + j)) {
-#pragma unroll
-                    for (int g = 0; g < G; ++g) vf[j / 2][g] &= j % 2 ? 0x0000FFFFu : 0xFFFF0000u;
-                }
-        }
-        if (a.scores) {
+            // tokens that are not seen have no weight, and nothing of what
+            // their slots happen to hold may meet it (a scale may be NaN)
+            auto hidden = [&](int t) { return base + t >= end || base + t < range.first; };
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
-                    if (head0 + 2 * q + x < a.group)
-                        a.scores[score_row + x * a.score_stride + (base - range.base) + key_token + 2 * i] = sc[i][x];
+                for (int g = 0; g < G; ++g) {
+                    if (hidden(key_token + 2 * i)) vs[i][g] = 0.f;
+                    if (hidden(4 * q + 2 * i)) vf[i][g] &= 0xFFFF0000u;
+                    if (hidden(4 * q + 2 * i + 1)) vf[i][g] &= 0x0000FFFFu;
+                }
         }
-        float p[2][2];
-        st.weigh(sc, p, 0.f, 8.f);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             uint32_t hi[2], lo[2], v0[8], v1[8], c[4];
@@ -411,6 +434,35 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 #pragma unroll
             for (int j = 0; j < 8; ++j) mma16<true>(st.o[g * 8 + j], hi[0], lo[0], hi[1], lo[1], v0[j], v1[j]);
         }
+    };
+
+    // A tile's values and the next one's scores side by side: one run of
+    // instructions without a branch, in which the one's tensor instructions
+    // overlap the other's unpacking.
+    float sc[2][2], p[2][2];
+    if (tiles > 0) {
+        paged_wait<kStages - 2>();
+        __syncwarp();
+        score(fixed(ring), base0, sc);
+        st.weigh(sc, p, 0.f, 8.f);
+    }
+    int stage = 0;
+    for (int it = 0; it < tiles; ++it) {
+        const int base = base0 + it * 16;
+        paged_wait<kStages - 3>();
+        __syncwarp();
+        if (it + kStages - 1 < tiles) fetch(stage == 0 ? kStages - 1 : stage - 1);
+        paged_commit();
+        const uint32_t tile = fixed(ring + stage * Tile::kBytes);
+        stage = stage == kStages - 1 ? 0 : stage + 1;
+        if (it + 1 < tiles) {
+            const uint32_t next = fixed(ring + stage * Tile::kBytes);
+            add_values(tile, base, p);
+            score(next, base + 16, sc);
+            st.weigh(sc, p, 0.f, 8.f);
+        } else {
+            add_values(tile, base, p);
+        }
     }
     paged_wait<0>();
     __syncwarp();
@@ -420,11 +472,14 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 
 template <int D, int GS>
 struct KernelLzs {
-    static constexpr int MINB = D <= 64 ? 5 : D <= 128 ? 3 : 2;
+    static constexpr int MINB = D <= 64 ? 4 : D <= 128 ? 3 : 2;
     static constexpr int kSmem = kPagedWarps * LzsTile<D, GS>::kStages * LzsTile<D, GS>::kBytes;
     static cudaError_t ready()
     {
-        return cudaFuncSetAttribute(paged_attn_lzs_kernel<D, GS, MINB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        const cudaError_t e = cudaFuncSetAttribute(paged_attn_lzs_kernel<D, GS, false, MINB>,
+                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e != cudaSuccess) return e;
+        return cudaFuncSetAttribute(paged_attn_lzs_kernel<D, GS, true, MINB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     }
     static int occupancy()
     {
@@ -433,7 +488,7 @@ struct KernelLzs {
         if (occ == 0) {
             int k = 0;
             if (ready() != cudaSuccess || cudaOccupancyMaxActiveBlocksPerMultiprocessor(
-                                              &k, paged_attn_lzs_kernel<D, GS, MINB>, kPagedThreads, kSmem) != cudaSuccess)
+                                              &k, paged_attn_lzs_kernel<D, GS, false, MINB>, kPagedThreads, kSmem) != cudaSuccess)
                 return 1;
             occ = k > 0 ? k : 1;
             cache.store(occ, std::memory_order_relaxed);
@@ -444,9 +499,15 @@ struct KernelLzs {
     {
         const cudaError_t e = ready();  // of the current device
         if (e != cudaSuccess) return e;
+        if (a.scores || a.page_shift < 4) return launch_as<true>(a, grid, s);
+        return launch_as<false>(a, grid, s);
+    }
+    template <bool GENERAL>
+    static cudaError_t launch_as(const PagedArgs &a, dim3 grid, cudaStream_t s)
+    {
         if (a.cluster)
-            return launch_pdl_cluster(paged_attn_lzs_kernel<D, GS, MINB>, a.n_split, grid, dim3(kPagedThreads), kSmem, s, a);
-        return launch_pdl(paged_attn_lzs_kernel<D, GS, MINB>, grid, dim3(kPagedThreads), kSmem, s, a);
+            return launch_pdl_cluster(paged_attn_lzs_kernel<D, GS, GENERAL, MINB>, a.n_split, grid, dim3(kPagedThreads), kSmem, s, a);
+        return launch_pdl(paged_attn_lzs_kernel<D, GS, GENERAL, MINB>, grid, dim3(kPagedThreads), kSmem, s, a);
     }
 };
 
