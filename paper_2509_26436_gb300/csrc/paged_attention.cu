@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
         uint32_t hi[2], lo[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            split_pair<BF>(p[i][0], p[i][1], hi[i], lo[i]);
+            split_pair<BF>(p[i][0], p[i][1], hi[i], lo[i], true);
             hi[i] = transposed(hi[i]);
             lo[i] = transposed(lo[i]);
         }
@@ -175,6 +175,16 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
             ldmatrix4_trans(tile + Tile::kSide + Tile::at(ld_row, 2 * c + ld_col), v);
             mma16<BF>(st.o[2 * c], hi[0], lo[0], hi[1], lo[1], v[0], v[1]);
             mma16<BF>(st.o[2 * c + 1], hi[0], lo[0], hi[1], lo[1], v[2], v[3]);
+        }
+        if (BF && a.o_type == QUARTZ_OUT_F32) {
+            const uint32_t r0 = transposed(bf16_pair(p[0][0], p[0][1])), r1 = transposed(bf16_pair(p[1][0], p[1][1]));
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c) {
+                uint32_t v[4];
+                ldmatrix4_trans(tile + Tile::kSide + Tile::at(ld_row, 2 * c + ld_col), v);
+                mma16<BF>(st.o[2 * c], r0, 0u, r1, 0u, v[0], v[1]);
+                mma16<BF>(st.o[2 * c + 1], r0, 0u, r1, 0u, v[2], v[3]);
+            }
         }
     }
     paged_wait<0>();

@@ -12,7 +12,8 @@
 //               8-15: what is left of them, rounded again; the accumulator's
 //               lower half, added at the end, makes the weights good to twice
 //               the 16-bit type's precision, in rows that eight heads leave
-//               free anyway.
+//               free anyway: 2^-22 with fp16, 2^-17 with bf16, for which
+//               binary32 results take the rest of the weights in a third part.
 // The scores arrive transposed to what the second product takes: one register
 // transpose (movmatrix) per 8 x 8 block of 16-bit weights, nothing through
 // shared memory.  Legacy tensor instructions are enough here: the step is
@@ -114,15 +115,18 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
             : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Two weights as a 16-bit pair and the pair of what the rounding left.
+// Two weights as a 16-bit pair and the pair of what the rounding left; what
+// that leaves stays in p0 and p1 where it is asked for.
 template <bool BF>
-__device__ __forceinline__ void split_pair(float p0, float p1, uint32_t &hi, uint32_t &lo)
+__device__ __forceinline__ void split_pair(float &p0, float &p1, uint32_t &hi, uint32_t &lo, bool rest = false)
 {
     if (BF) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
         hi = *reinterpret_cast<const uint32_t *>(&h);
-        const __nv_bfloat162 l = __floats2bfloat162_rn(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xFFFF0000u));
+        const float r0 = p0 - __uint_as_float(hi << 16), r1 = p1 - __uint_as_float(hi & 0xFFFF0000u);
+        const __nv_bfloat162 l = __floats2bfloat162_rn(r0, r1);
         lo = *reinterpret_cast<const uint32_t *>(&l);
+        if (rest) p0 = r0 - __uint_as_float(lo << 16), p1 = r1 - __uint_as_float(lo & 0xFFFF0000u);
     } else {
         const __half2 h = __floats2half2_rn(p0, p1);
         const float2 f = __half22float2(h);
@@ -130,6 +134,13 @@ __device__ __forceinline__ void split_pair(float p0, float p1, uint32_t &hi, uin
         hi = *reinterpret_cast<const uint32_t *>(&h);
         lo = *reinterpret_cast<const uint32_t *>(&l);
     }
+}
+
+// What split_pair left, in bf16.
+__device__ __forceinline__ uint32_t bf16_pair(float p0, float p1)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
+    return *reinterpret_cast<const uint32_t *>(&h);
 }
 
 // Asynchronous 16-byte copies global -> shared, one group per tile.

@@ -191,8 +191,9 @@ __device__ __forceinline__ void lds_scales(uint32_t a, float (&s)[G])
     }
 }
 
-// GENERAL: pages below 16 tokens, or with scores for the sums of weights; the
-// other instance is for pages of 16 and more without.
+// GENERAL: pages below 16 tokens, scores for the sums of weights, or binary32
+// results; the other instance is for pages of 16 and more, 16-bit results and
+// no scores.
 template <int D, int GS, bool GENERAL, int MINB>
 __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(PagedArgs a)
 {
@@ -420,12 +421,14 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            uint32_t hi[2], lo[2], v0[8], v1[8], c[4];
+            uint32_t hi[2], lo[2], rest[2], v0[8], v1[8], c[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) c[j] = lds32(tile + value_off(j, g));
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                split_pair<true>(p[i][0] * vs[i][g], p[i][1] * vs[i][g], hi[i], lo[i]);
+                float p0 = p[i][0] * vs[i][g], p1 = p[i][1] * vs[i][g];
+                split_pair<true>(p0, p1, hi[i], lo[i], GENERAL);
+                if (GENERAL) rest[i] = transposed(bf16_pair(p0, p1));
                 hi[i] = transposed(hi[i]);
                 lo[i] = transposed(lo[i]);
             }
@@ -433,6 +436,10 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
             value_codes(c[2], c[3], vf[1][g], v1);
 #pragma unroll
             for (int j = 0; j < 8; ++j) mma16<true>(st.o[g * 8 + j], hi[0], lo[0], hi[1], lo[1], v0[j], v1[j]);
+            if (GENERAL && a.o_type == QUARTZ_OUT_F32) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) mma16<true>(st.o[g * 8 + j], rest[0], 0u, rest[1], 0u, v0[j], v1[j]);
+            }
         }
     };
 
@@ -499,7 +506,7 @@ struct KernelLzs {
     {
         const cudaError_t e = ready();  // of the current device
         if (e != cudaSuccess) return e;
-        if (a.scores || a.page_shift < 4) return launch_as<true>(a, grid, s);
+        if (a.scores || a.page_shift < 4 || a.o_type == QUARTZ_OUT_F32) return launch_as<true>(a, grid, s);
         return launch_as<false>(a, grid, s);
     }
     template <bool GENERAL>
