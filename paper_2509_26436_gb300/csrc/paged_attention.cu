@@ -227,7 +227,6 @@ struct Kernel16 {
 // Join of the splits, and the sums of weights
 // ---------------------------------------------------------------------------
 constexpr int kMaxSplits = 1024;
-constexpr int kMaxCluster = 8;  // splits joined within a cluster (the portable size)
 constexpr int kJoinThreads = 256;
 constexpr int kJoinHeads = 64;  // query heads whose sums are held at a time
 
@@ -363,8 +362,8 @@ int log2_of(int v)
 // costs some 5 us besides its tiles).  Long sequences are cut to 1024 tokens,
 // up to 16 times what the SMs hold: 8 sequences of up to 65536 tokens, encoded,
 // 100.9 us (2048 102.3, 512 110.0, 4096 122.9); 32 of up to 8192, bf16, 98.6
-// (2048 100.6, 512 104.8, 256 113.8).  A few short ones only as far as SMs are
-// free.
+// (2048 100.6, 512 104.8, 256 113.8).  A few short ones are cut only as far as
+// SMs are free, or, to few enough splits for a cluster, two thirds of them.
 struct PagedPlan {
     int n_split, chunk;
     bool cluster;
@@ -391,8 +390,9 @@ PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, i
     if (n < by_length && n < full) n = by_length < full ? by_length : full;
     if (n > most) n = most;
     if (n * ctas < slots) {
-        const int64_t fill = (slots + ctas - 1) / ctas, tiles = (p.tokens + 63) / 64;
+        const int64_t fill = (slots + ctas - 1) / ctas, tiles = (p.tokens + 63) / 64, loose = 2 * slots / (3 * ctas);
         n = fill < tiles ? fill : tiles;
+        if (n <= kPagedCluster && loose >= 2 && n > loose) n = loose;
     }
     if (n > kMaxSplits) n = kMaxSplits;
     if (n < 1) n = 1;
@@ -400,9 +400,12 @@ PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, i
     p.chunk = static_cast<int>(chunk);
     p.n_split = static_cast<int>((p.tokens + chunk - 1) / chunk);
     if (p.n_split < 1) p.n_split = 1;
-    // All CTAs resident at once and at most 8 splits: a head's splits are a
-    // cluster and join themselves, which saves the join's launch.
-    p.cluster = p.n_split > 1 && p.n_split <= kMaxCluster && p.n_split * ctas <= slots && !with_weights;
+    // At most 8 splits and two thirds of the SMs' places taken: a head's splits
+    // are a cluster and join themselves, which saves the join's launch (40
+    // heads, 777 tokens, encoded: 5.9 us against 6.7; 200 tokens, fp16: 4.6
+    // against 5.7).  With the SMs nearly full, clusters wait for places next to
+    // each other (777 tokens, fp16, 7 splits: 8.8 against 7.0).
+    p.cluster = p.n_split > 1 && p.n_split <= kPagedCluster && 3 * p.n_split * ctas <= 2 * slots && !with_weights;
     p.score_stride = (p.tokens + 63) / 64 * 64;
     return p;
 }

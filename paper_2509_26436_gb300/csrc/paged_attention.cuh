@@ -32,6 +32,7 @@ namespace quartz {
 constexpr int kPagedWarps = 4;
 constexpr int kPagedThreads = kPagedWarps * 32;
 constexpr int kPagedHeads = 8;  // query heads per CTA
+constexpr int kPagedCluster = 8;  // most splits joined within a cluster (the portable size)
 constexpr float kPagedLog2e = 1.4426950408889634f;
 
 struct PagedSide {
@@ -356,16 +357,25 @@ __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int wa
     for (int e = split * kPagedThreads + threadIdx.x; e < kPagedHeads * (D / 4); e += a.n_split * kPagedThreads) {
         const int h = e / (D / 4), d = (e - h * (D / 4)) * 4;
         if (head0 + h >= a.group) break;
-        float m = -1e30f, sum = 0.f;
-        for (int c = 0; c < a.n_split; ++c) m = fmaxf(m, paged_remote_f32(paged_remote(s_m + 4 * h, c)));
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(so(0, h, d)));
-#pragma unroll 4
-        for (int c = 0; c < a.n_split; ++c) {
-            const float f = ex2(paged_remote_f32(paged_remote(s_m + 4 * h, c)) - m);
-            const float4 u = paged_remote_f4(paged_remote(mine, c));
-            sum += f * paged_remote_f32(paged_remote(s_l + 4 * h, c));
-            v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
+        float ms[kPagedCluster], ls[kPagedCluster];  // all loads before their first use
+        float4 us[kPagedCluster];
+#pragma unroll
+        for (int c = 0; c < kPagedCluster; ++c) {
+            const int from = min(c, a.n_split - 1);
+            ms[c] = paged_remote_f32(paged_remote(s_m + 4 * h, from));
+            ls[c] = paged_remote_f32(paged_remote(s_l + 4 * h, from));
+            us[c] = paged_remote_f4(paged_remote(mine, from));
+        }
+        float m = ms[0], sum = 0.f;
+#pragma unroll
+        for (int c = 1; c < kPagedCluster; ++c) m = fmaxf(m, ms[c]);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < kPagedCluster; ++c) {
+            const float f = c < a.n_split ? ex2(ms[c] - m) : 0.f;
+            sum += f * ls[c];
+            v.x += f * us[c].x, v.y += f * us[c].y, v.z += f * us[c].z, v.w += f * us[c].w;
         }
         const float r = sum > 0.f ? 1.f / sum : 0.f;
         paged_store4(a.o, a.o_type, (row0 + h) * D + d, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
