@@ -410,7 +410,7 @@ typedef struct {
  * type, in binary32, rounded once; elements from `rotary` on are copied.
  * Strides in elements: x[t * x_stride_token + h * x_stride_head + d], y alike.
  * y == x with equal strides works in place; other overlaps are undefined.
- * dim 2 .. 1024; any alignment of the type itself. */
+ * dim 2 .. 1024, tokens <= 2^30; any alignment of the type itself. */
 int32_t quartz_rope(const void *x, int64_t x_stride_token, int64_t x_stride_head, void *y, int64_t y_stride_token,
                     int64_t y_stride_head, int32_t type, int64_t tokens, int32_t heads, int32_t dim,
                     const quartz_rope_t *rope, void *stream);
@@ -421,7 +421,7 @@ int32_t quartz_rope(const void *x, int64_t x_stride_token, int64_t x_stride_head
  * k[t * k_stride_token + h * k_stride_head + d], 16-byte aligned, strides
  * multiples of 8.  With `rope` (NULL: none) k is rotated first, the same
  * values as quartz_rope gives; encoded pages get the arithmetic of
- * quartz_quantize.  The slots of one call are distinct. */
+ * quartz_quantize.  The slots of one call are distinct; tokens <= 2^30. */
 int32_t quartz_paged_append(const quartz_paged_cache_t *cache, const void *k, int64_t k_stride_token,
                             int64_t k_stride_head, const void *v, int64_t v_stride_token, int64_t v_stride_head,
                             int64_t tokens, const int64_t *slots, const quartz_rope_t *rope, void *stream);
@@ -446,7 +446,7 @@ int32_t quartz_paged_append(const quartz_paged_cache_t *cache, const void *k, in
  *                heads added for the tokens attended (no two places alike)
  *   workspace    >= quartz_paged_attention_workspace_size bytes, 16-byte
  *                aligned, scratch
- * seqs <= 65535. */
+ * seqs <= 65535, max_len <= 2^30. */
 size_t quartz_paged_attention_workspace_size(const quartz_paged_cache_t *cache, int64_t seqs, int32_t q_heads,
                                              int64_t max_len, int64_t window, int32_t with_weights);
 int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_stride_head, int64_t seqs,
@@ -462,8 +462,8 @@ int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_st
  *   weights   fp32 [seqs, heads, >= max_len] with strides, as above
  *   kept      int32 [seqs, heads, budget]: the kept indices, ascending, then -1
  *   new_lens  int32 [seqs]: min(len, budget)
- * sinks, recent >= 0, 1 <= budget, sinks + recent <= budget, max_len < 2^31,
- * seqs * heads < 2^31, seqs <= 65535. */
+ * sinks, recent >= 0, 1 <= budget, sinks + recent <= budget, budget and max_len
+ * <= 2^30, heads <= 1024, seqs <= 65535. */
 int32_t quartz_evict_select(const float *weights, int64_t weights_stride_seq, int64_t weights_stride_head,
                             const int32_t *seq_lens, int64_t seqs, int32_t heads, int64_t max_len, int64_t budget,
                             int64_t recent, int64_t sinks, int32_t *kept, int32_t *new_lens, void *stream);

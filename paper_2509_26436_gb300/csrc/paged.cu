@@ -62,11 +62,7 @@ __device__ __forceinline__ void pack16(const float (&f)[16], uint4 &lo, uint4 &h
 {
     uint32_t w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        T *p = reinterpret_cast<T *>(&w[i]);
-        p[0] = from_f32<T>(f[2 * i]);
-        p[1] = from_f32<T>(f[2 * i + 1]);
-    }
+    for (int i = 0; i < 8; ++i) w[i] = pack_pair<T>(f[2 * i], f[2 * i + 1]);
     lo = make_uint4(w[0], w[1], w[2], w[3]);
     hi = make_uint4(w[4], w[5], w[6], w[7]);
 }

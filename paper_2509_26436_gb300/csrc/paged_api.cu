@@ -86,7 +86,7 @@ int32_t quartz_rope(const void *x, int64_t x_stride_token, int64_t x_stride_head
                     int64_t y_stride_head, int32_t type, int64_t tokens, int32_t heads, int32_t dim,
                     const quartz_rope_t *rope, void *stream)
 {
-    if (!rope || !type_ok(type) || tokens < 0 || tokens >= (int64_t(1) << 31) || heads < 0 || heads > 65535 || dim < 2 ||
+    if (!rope || !type_ok(type) || tokens < 0 || tokens > kMaxLen || heads < 0 || heads > 65535 || dim < 2 ||
         dim > 1024)
         return QUARTZ_ERR_INVALID_ARG;
     if (!stride_ok(x_stride_token, 1) || !stride_ok(x_stride_head, 1) || !stride_ok(y_stride_token, 1) ||
@@ -108,7 +108,7 @@ int32_t quartz_paged_append(const quartz_paged_cache_t *cache, const void *k, in
 {
     int32_t rc = check_cache(cache);
     if (rc) return rc;
-    if (tokens < 0 || tokens >= (int64_t(1) << 31)) return QUARTZ_ERR_INVALID_ARG;
+    if (tokens < 0 || tokens > kMaxLen) return QUARTZ_ERR_INVALID_ARG;
     const int64_t s[4] = {k_stride_token, k_stride_head, v_stride_token, v_stride_head};
     for (int64_t i : s) {
         if (!stride_ok(i, 1)) return QUARTZ_ERR_INVALID_ARG;

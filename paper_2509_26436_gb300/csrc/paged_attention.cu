@@ -359,7 +359,9 @@ int log2_of(int v)
 // Splits per sequence and tokens per split (a multiple of one tile of each of
 // the CTA's warps).  Where lengths differ, many CTAs are empty or short: four
 // times as many as the SMs hold keep them loaded, of 256 tokens at least (a CTA
-// costs some 5 us besides its tiles).  Long sequences are cut to 1024 tokens,
+// costs some 5 us besides its tiles); where sequences and heads alone are twice
+// what they hold, none is cut for that (128 x 8 heads of up to 1000 tokens, bf16:
+// 47.6 us whole, 60.4 in two).  Long sequences are cut to 1024 tokens,
 // up to 16 times what the SMs hold: 8 sequences of up to 65536 tokens, encoded,
 // 100.9 us (2048 102.3, 512 110.0, 4096 122.9); 32 of up to 8192, bf16, 98.6
 // (2048 100.6, 512 104.8, 256 113.8).  A few short ones are cut only as far as
@@ -374,10 +376,12 @@ PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, i
                      bool with_weights)
 {
     PagedPlan p;
-    // a window's first tile may hold 15 tokens before it
-    p.tokens = window > 0 && window + 15 < max_len ? window + 15 : max_len;
+    // a window's first tile may hold 15 tokens before it; a table without room
+    // for any token is planned as for one
+    p.tokens = window > 0 && window < max_len - 15 ? window + 15 : max_len;
+    if (p.tokens < 1) p.tokens = 1;
     const int group = q_heads / c->heads;
-    const int64_t ctas = seqs * c->heads * ((group + kPagedHeads - 1) / kPagedHeads);
+    const int64_t ctas = (seqs > 0 ? seqs : 1) * c->heads * ((group + kPagedHeads - 1) / kPagedHeads);
     const int occ = c->type == QUARTZ_PAGES_ENCODED ? paged_kernel_occupancy_encoded(c->dim, c->k.enc.p.group_s)
                                                     : paged_kernel_occupancy_16bit(c->type, c->dim);
     int dev = 0, sms = 0;
@@ -385,7 +389,7 @@ PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, i
         sms <= 0)
         sms = 152;
     const int64_t slots = static_cast<int64_t>(sms) * occ;
-    int64_t n = (4 * slots + ctas - 1) / ctas;
+    int64_t n = ctas < 2 * slots ? (4 * slots + ctas - 1) / ctas : 1;
     const int64_t most = (p.tokens + 255) / 256, by_length = (p.tokens + 1023) / 1024, full = 16 * slots / ctas;
     if (n < by_length && n < full) n = by_length < full ? by_length : full;
     if (n > most) n = most;

@@ -22,6 +22,21 @@ struct alignas(sizeof(T) * V) Vec {
     T e[V];
 };
 
+template <typename T, int V>
+__device__ __forceinline__ void store_rounded(T *to, const float (&f)[V])
+{
+    Vec<T, V> v;
+    if constexpr (sizeof(T) == 2 && V > 1) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) w[j] = pack_pair<T>(f[2 * j], f[2 * j + 1]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v.e[j] = from_f32<T>(f[j]);
+    }
+    *reinterpret_cast<Vec<T, V> *>(to) = v;
+}
+
 // Piece p < pairs / V of a head turns V pairs, the others copy V elements each
 // from `rotary` on.  `here` (token, piece) places per CTA, as consecutive
 // threads; the threads behind them: the same places in further heads.
@@ -71,7 +86,7 @@ __global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs a, int64_t p
         }
         T *to = y + h * a.y_sh;
         if (turn) {
-            Vec<T, V> r1, r2;
+            float f[2][V];  // the two vectors' elements
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 if (a.rope.interleaved) {
@@ -79,16 +94,16 @@ __global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs a, int64_t p
                     const T x1 = 2 * j < V ? u.e[(2 * j) % V] : w.e[(2 * j) % V];
                     const T x2 = 2 * j + 1 < V ? u.e[(2 * j + 1) % V] : w.e[(2 * j + 1) % V];
                     const float2 r = rope_turn(to_f32<T>(x1), to_f32<T>(x2), cs[j]);
-                    (2 * j < V ? r1 : r2).e[(2 * j) % V] = from_f32<T>(r.x);
-                    (2 * j + 1 < V ? r1 : r2).e[(2 * j + 1) % V] = from_f32<T>(r.y);
+                    f[2 * j / V][(2 * j) % V] = r.x;
+                    f[(2 * j + 1) / V][(2 * j + 1) % V] = r.y;
                 } else {
                     const float2 r = rope_turn(to_f32<T>(u.e[j]), to_f32<T>(w.e[j]), cs[j]);
-                    r1.e[j] = from_f32<T>(r.x);
-                    r2.e[j] = from_f32<T>(r.y);
+                    f[0][j] = r.x;
+                    f[1][j] = r.y;
                 }
             }
-            *reinterpret_cast<Vec<T, V> *>(to) = r1;
-            *reinterpret_cast<Vec<T, V> *>(to + gap) = r2;
+            store_rounded<T, V>(to, f[0]);
+            store_rounded<T, V>(to + gap, f[1]);
         } else {
             *reinterpret_cast<Vec<T, V> *>(to) = u;
         }

@@ -64,6 +64,15 @@ def _rows(name, x, dim, kind, device):
     return st
 
 
+def _empty(shape, dtype, device, stream):
+    """Uninitialised memory of the stream that the call runs on: memory of
+    another one could still be in use there, or be given away too early."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 # --- rotary positions ---------------------------------------------------------
 
 def rope_frequencies(rotary: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0,
@@ -135,7 +144,7 @@ def rope(x, positions, freqs, interleaved: bool = False, scale: float = 1.0, bac
     T, H, D = x.shape
     r = _rope_struct(positions, freqs, T, scale, interleaved, backward, device)
     if out is None:
-        out = torch.empty((T, H, D), dtype=dtype, device=x.device)
+        out = _empty((T, H, D), dtype, x.device, stream)
         s0, s1 = H * D, D
     else:
         s0, s1, _ = _rows("out", out, 3, dtype, device)
@@ -276,7 +285,7 @@ def attention_paged(q, cache: PagedCache, block_table, seq_lens, scale: float, w
         raise ValueError("max_len must be within what block_table holds")
     if out is None:
         out_dtype = out_dtype or q.dtype
-        o = torch.empty((B, Hq, D), dtype=out_dtype, device=cache.device)
+        o = _empty((B, Hq, D), out_dtype, cache.device, stream)
     else:
         o, out_dtype = out, out.dtype
         _rows("out", o, 3, out_dtype, device)
@@ -293,7 +302,7 @@ def attention_paged(q, cache: PagedCache, block_table, seq_lens, scale: float, w
         w_ptr, with_weights = weights.data_ptr(), 1
     if workspace is None:
         size = max(cache._workspace_size(B, Hq, max_len, window, with_weights), 16)
-        workspace = torch.empty(size, dtype=torch.uint8, device=cache.device)
+        workspace = _empty(size, torch.uint8, cache.device, stream)
     else:
         if workspace.get_device() != device or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
@@ -332,13 +341,13 @@ def evict_select(weights, seq_lens, budget: int, recent: int = 0, sinks: int = 0
     elif not 0 <= max_len <= n:
         raise ValueError("max_len must be within weights' last dimension")
     if kept is None:
-        kept = torch.empty((B, H, max(budget, 0)), dtype=i32, device=weights.device)
+        kept = _empty((B, H, max(budget, 0)), i32, weights.device, stream)
     else:
         _rows("kept", kept, 3, i32, device)
         if kept.shape != (B, H, budget) or not kept.is_contiguous():
             raise ValueError("kept must be contiguous [seqs, heads, budget]")
     if new_lens is None:
-        new_lens = torch.empty((B,), dtype=i32, device=weights.device)
+        new_lens = _empty((B,), i32, weights.device, stream)
     elif new_lens.shape[0] != B:
         raise ValueError("new_lens must have one entry per sequence")
     rc = lib.quartz_evict_select(weights.data_ptr(), sb, sh, lens, B, H, max_len, budget, recent, sinks, kept.data_ptr(),

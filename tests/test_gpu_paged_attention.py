@@ -120,6 +120,21 @@ def test_window(Q, store, window):
 
 
 @pytest.mark.parametrize("store", ["f16", "lzs"])
+@pytest.mark.parametrize("page", [1, 4, 8, 16, 32])
+def test_pages_before_the_window_may_be_gone(Q, store, page):
+    """A page none of whose tokens is in the window is not looked up: its place in the table may be free."""
+    lens, window = [333, 50, 201], 45
+    c, table, ln = make_cache(Q, lens, 2, 64, page, store, seed=page)
+    q = _q(3, 4, 64, torch.float16, 18).cuda()
+    want = Q.attention_paged(q, c, table.cuda(), ln.cuda(), 0.1, window=window)
+    gone = table.clone()
+    for b, n in enumerate(lens):
+        gone[b, :max(0, n - window) // page] = -7
+    assert torch.equal(Q.attention_paged(q, c, gone.cuda(), ln.cuda(), 0.1, window=window), want)
+    assert Q.device_status() == 0
+
+
+@pytest.mark.parametrize("store", ["f16", "lzs"])
 def test_many_splits(Q, store):
     """One sequence cut into as many splits as there are SMs for; a short one beside it leaves most of them empty."""
     c, table, ln = make_cache(Q, [9001, 70], 1, 128, 16, store, seed=9)
@@ -172,6 +187,42 @@ def test_query_strides_and_shared_pages(Q):
     a = Q.attention_paged(fused.cuda()[:, 2:6], c, table.cuda(), ln.cuda(), 0.1)
     b = Q.attention_paged(fused[:, 2:6].contiguous().cuda(), c, table.cuda(), ln.cuda(), 0.1)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("store", ["f16", "lzs"])
+def test_a_table_without_places(Q, store):
+    """Sequences that have no page at all: zeros, and the sums as they were."""
+    c, _, _ = make_cache(Q, [20], 2, 64, 16, store, seed=18)
+    q = _q(3, 4, 64, torch.float16, 14).cuda()
+    table, lens = torch.empty(3, 0, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    w = torch.rand(3, 2, 5, device="cuda")
+    before = w.clone()
+    o = Q.attention_paged(q, c, table, lens, 0.1, weights=w)
+    assert Q.device_status() == 0 and not o.any() and torch.equal(w, before)
+    none = Q.attention_paged(q[:0], c, table[:0], lens[:0], 0.1)
+    assert none.shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("groups", [9, 16, 33])
+def test_many_query_heads_per_key_head(Q, groups):
+    """More heads than a CTA takes, and than the sums of weights hold at a time (65 below)."""
+    c, table, ln = make_cache(Q, [70, 300], 1, 64, 16, "bf16", seed=groups)
+    check(Q, c, table, ln, _q(2, groups, 64, torch.bfloat16, 15), 0.125, store="bf16", weights=True)
+
+
+def test_more_query_heads_than_the_sums_hold(Q):
+    c, table, ln = make_cache(Q, [40], 1, 64, 16, "f16", seed=19)
+    check(Q, c, table, ln, _q(1, 65, 64, torch.float16, 16), 0.125, store="f16", weights=True)
+
+
+@pytest.mark.parametrize("store", ["f16", "lzs"])
+@pytest.mark.parametrize("B,H,n", [(1, 40, 777), (1, 1, 500), (2, 8, 3000), (200, 4, 90), (3, 16, 1100)])
+def test_every_plan(Q, store, B, H, n):
+    """One split, clusters, many splits with a join, and more heads than the SMs hold: against each other by the
+    definition, ragged lengths included."""
+    lens = [max(0, n - 37 * i % (n + 1)) for i in range(B)]
+    c, table, ln = make_cache(Q, lens, H, 128, 16, store, seed=B + H)
+    check(Q, c, table, ln, _q(B, H, 128, torch.float16, 17), 128 ** -0.5, store=store, out="f16")
 
 
 def test_far_pages(Q):

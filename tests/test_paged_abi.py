@@ -115,6 +115,22 @@ def test_attention_refusals(lib):
     assert call(B=0, q=None) == 0
 
 
+def test_workspace_of_nothing(lib):
+    """No sequences, or a table without a place: planned, not divided by."""
+    c = _cache()
+    for B, n, window in ((0, 64, 0), (1, 0, 0), (0, 0, 0), (1, 64, (1 << 63) - 1), (65535, 1 << 30, 1)):
+        for weights in (0, 1):
+            assert lib.quartz_paged_attention_workspace_size(C.byref(c), B, 2, n, window, weights) > 0
+    assert lib.quartz_paged_attention(None, 256, 128, 0, 2, C.byref(c), None, 0, None, 0, 0, 1.0, None, 0, None, 0, 0, None,
+                                      0, None) == 0
+
+
+def test_token_limits(lib):
+    c, r = _cache(), _rope()
+    assert lib.quartz_paged_append(C.byref(c), P, 256, 128, P, 256, 128, (1 << 30) + 1, P, None, None) == BAD
+    assert lib.quartz_rope(P, 256, 128, P, 256, 128, 0, (1 << 30) + 1, 2, 128, C.byref(r), None) == BAD
+
+
 def test_evict_refusals(lib):
     def call(w=P, st=(64, 32), lens=P, B=1, H=2, n=32, budget=8, recent=2, sinks=1, kept=P, new=P):
         return lib.quartz_evict_select(w, *st, lens, B, H, n, budget, recent, sinks, kept, new, None)
