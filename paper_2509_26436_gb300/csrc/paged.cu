@@ -119,6 +119,9 @@ __device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_r
 // heads; the head groups of a CTA share its tokens' angles.  Few tokens: keys
 // and values by different CTAs (blockIdx.y).  GS = 0: 16-bit pages of type T; else encoded pages (T = __half, four
 // neighbouring lanes per 64-element group: dim is a multiple of 64).
+// Bound by the encoder's instructions, some 400 per 32 x 16 elements with the
+// rotation: 16384 tokens of 8 heads of 128, rotated and encoded, 38.6 us (12.9
+// of bytes); 43.4 with three CTAs per SM, 55.9 with a token per CTA.
 template <typename T, int GS>
 __global__ void __launch_bounds__(kAppendThreads, 4) paged_append_kernel(AppendCall c, int tokens)
 {
@@ -259,7 +262,9 @@ __device__ __forceinline__ void store_piece(uint8_t *p, const uint4 v, int bytes
 // behind the last is the weights').  A tile of rows at a time: first a thread
 // per row follows its kept index and the tables to the two addresses, then all
 // threads move pieces, eight loads in flight each; so the dependent reads are
-// paid once per tile and row, not per piece.  Into new pages, a part is a
+// paid once per tile and row, not per piece, and for the next tile while this
+// one's loads are under way (16 x 8 heads, 4096 rows of 2 x 256 bytes: 75 us, 93%
+// of the copy rate; followed per piece 97).  Into new pages, a part is a
 // range of rows; in place it is a slice of every row, and the CTA goes through
 // the rows in order: row j is written after all rows up to its tile's last are
 // read (a barrier per tile), and rows after them come from places behind the
