@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
     __shared__ float s_f[kMaxSplits];
     __shared__ float4 s_o[kGroups][kLanes];
     __shared__ float s_red[8], s_inv;
-    __shared__ float s_lse[kJoinHeads];
+    __shared__ float2 s_ml[kJoinHeads];  // m and log2 l: apart, since together they would lose l where m is large
     const int b = blockIdx.z;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
     const int splits = (range.count() + a.chunk - 1) / a.chunk;  // that hold tokens
@@ -254,7 +254,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
     for (int head = blockIdx.x; a.part_o && head < a.group; head += gridDim.x) {
         const int64_t row = row0 + head;
         const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row * a.n_split;
-        float m = -1e30f;
+        float m = kPagedLow;
         for (int i = tid; i < splits; i += kJoinThreads) m = fmaxf(m, ml[i].x);
 #pragma unroll
         for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
@@ -314,11 +314,11 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
         float p[4] = {0.f, 0.f, 0.f, 0.f};
         for (int g0 = 0; g0 < a.group; g0 += kJoinHeads) {
             const int heads = min(kJoinHeads, a.group - g0);
-            if (!held) {  // m + log2 l of each head, a warp each
+            if (!held) {  // m and log2 l of each head, a warp each
                 __syncthreads();
                 for (int g = warp; g < heads; g += kJoinThreads / 32) {
                     const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (row0 + g0 + g) * a.n_split;
-                    float m = -1e30f, sum = 0.f;
+                    float m = kPagedLow, sum = 0.f;
                     for (int i = lane; i < splits; i += 32) m = fmaxf(m, ml[i].x);
 #pragma unroll
                     for (int d = 16; d; d /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
                     }
 #pragma unroll
                     for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                    if (lane == 0) s_lse[g] = m + log2f(sum);
+                    if (lane == 0) s_ml[g] = make_float2(m, log2f(sum));
                 }
                 __syncthreads();
                 held = a.group <= kJoinHeads;
@@ -338,8 +338,8 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
 #pragma unroll 4
                 for (int g = 0; g < heads; ++g) {
                     const float4 s = *reinterpret_cast<const float4 *>(score + g * a.score_stride);
-                    const float lse = s_lse[g];
-                    p[0] += ex2(s.x - lse), p[1] += ex2(s.y - lse), p[2] += ex2(s.z - lse), p[3] += ex2(s.w - lse);
+                    const float m = s_ml[g].x, l = s_ml[g].y;
+                    p[0] += ex2(s.x - m - l), p[1] += ex2(s.y - m - l), p[2] += ex2(s.z - m - l), p[3] += ex2(s.w - m - l);
                 }
             }
         }

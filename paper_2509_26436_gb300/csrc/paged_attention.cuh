@@ -37,6 +37,7 @@ constexpr int kPagedThreads = kPagedWarps * 32;
 constexpr int kPagedHeads = 8;  // query heads per CTA
 constexpr int kPagedCluster = 8;  // most splits joined within a cluster (the portable size)
 constexpr float kPagedLog2e = 1.4426950408889634f;
+constexpr float kPagedLow = -3e38f;  // a maximum before any score: finite, below the scores of a head that are
 
 struct PagedSide {
     const uint8_t *data;  // 16-bit pages
@@ -171,7 +172,7 @@ struct PagedState {
         for (int i = 0; i < D / 8; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
-        m[0] = m[1] = -1e30f;
+        m[0] = m[1] = kPagedLow;
         l[0] = l[1] = 0.f;
     }
 

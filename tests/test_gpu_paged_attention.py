@@ -149,6 +149,35 @@ def test_large_scores_and_small_values(Q, store):
         check(Q, c, table, ln, _q(2, 4, 128, c.dtype, 7, size), scale, store=store)
 
 
+@pytest.mark.parametrize("store,size,scale", [("f16", 60000.0, 1e22), ("bf16", 2.0 ** 58, 1.0), ("lzs", 60000.0, 1e22)])
+@pytest.mark.parametrize("lens,H", [([5, 900, 0, 1], 2), ([777], 40), ([3000] * 2, 8)])
+def test_scores_far_below_zero(Q, store, size, scale, lens, H):
+    """Equal scores of -1e33 and below (finite in binary32: -2^122 with bf16; with factors of 2^62 they would be -2^130),
+    which no maximum to start from may hide: every token weighs the same.  The
+    weights are 2^0 over their number, exact until the division and its sum: the bound is that of the values alone."""
+    c, table, ln = make_cache(Q, lens, H, 64, 16, store, seed=20)
+    total = int(ln.sum())
+    slots = torch.cat([table[b].long()[torch.arange(n) // 16] * 16 + torch.arange(n) % 16 for b, n in enumerate(lens)])
+    g = torch.Generator().manual_seed(21)
+    v = torch.randn(total, H, 64, generator=g).to(c.dtype)
+    Q.paged_append(c, torch.full((total, H, 64), size, dtype=c.dtype, device="cuda"), v.cuda(), slots.cuda())
+    q = torch.full((len(lens), H, 64), -size, dtype=c.dtype)
+    w = torch.zeros(len(lens), H, table.shape[1] * 16, device="cuda")
+    a = Q.attention_paged(q.cuda(), c, table.cuda(), ln.cuda(), scale, out_dtype=torch.float32)
+    b = Q.attention_paged(q.cuda(), c, table.cuda(), ln.cuda(), scale, out_dtype=torch.float32, weights=w)
+    held = R.held(c)[1]
+    for i, n in enumerate(lens):
+        t = torch.arange(n)
+        at = held[table[i].long()[t // 16], t % 16]
+        want, mag = (at.mean(0), at.abs().mean(0)) if n else (torch.zeros(H, 64), torch.zeros(H, 64))
+        # the weights' parts 2^-17, and n / 16 + 64 steps of 2^-23 in each of two sums
+        for o in (a, b):
+            assert bool(((o[i].cpu().double() - want).abs() <= mag * (2.0 ** -17 + 2 * (n / 16 + 64) * 2.0 ** -23)).all())
+        got = w[i, :, :n].cpu().double()
+        assert bool(((got * n - 1).abs() <= (n / 16 + 72) * 2.0 ** -23).all()) and not w[i, :, n:].any()
+    assert Q.device_status() == 0
+
+
 def test_a_sink_does_not_drown_small_weights(Q):
     """One token 17 nats ahead of 8000 others that together weigh 3e-4: their values are not lost below fp16's
     smallest weights."""
