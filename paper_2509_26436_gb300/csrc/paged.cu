@@ -27,119 +27,150 @@ struct AppendCall {
     AppendArgs a;
     AppendDst dst[2];
     int64_t slots_total;
-    int page_shift, heads, units;    // units of 16 elements per row
+    int page_shift, heads, units;    // units per row, of half a row with BOTH
     int tokens_here, groups, each;   // per CTA; head groups; heads per thread
 };
 
-// The angles of a CTA's token in shared memory, (cos, -sin) for the first
-// element of a pair and behind them (sin, cos) for the second: both are m a + n
-// b with (a, b) = (first, second).  Neighbouring units, which neighbouring
-// lanes hold, side by side.
+// Elements a thread takes at a time (a unit): as much of a 64-element group as
+// the encoder's lanes hold, or 16 bytes.
+constexpr int unit_size(bool encoded) { return encoded ? 16 : 8; }
+
+// The angles of a CTA's tokens in shared memory, (cos, -sin) for the first
+// element of a pair and, unless a thread turns both elements of its pairs,
+// behind them (sin, cos) for the second: both are m a + n b with (a, b) =
+// (first, second).  Neighbouring units, which neighbouring lanes hold, side by
+// side.
+template <int E>
 struct AngleTable {
     const float2 *cs;
-    static constexpr int kStride = kAngles / 16;
-    __device__ __forceinline__ float2 operator()(int i) const { return cs[(i & 15) * kStride + (i >> 4)]; }
+    static constexpr int kStride = kAngles / E;
+    __device__ __forceinline__ float2 operator()(int i) const { return cs[(i % E) * kStride + i / E]; }
 };
 
 // rope_turn's two results from the table: the same operations.
 __device__ __forceinline__ float rope_first(float2 v, float x1, float x2) { return __fmaf_rn(v.x, x1, __fmul_rn(v.y, x2)); }
 __device__ __forceinline__ float rope_second(float2 v, float x1, float x2) { return __fmaf_rn(-v.y, x1, __fmul_rn(v.x, x2)); }
 
-template <typename T>
-__device__ __forceinline__ void unpack16(const uint4 lo, const uint4 hi, float (&f)[16])
-{
-    const uint32_t w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+template <int E>
+struct Unit {
+    uint32_t w[E / 2];
+    __device__ __forceinline__ void clear()
+    {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const T *p = reinterpret_cast<const T *>(&w[i]);
-        f[2 * i] = to_f32<T>(p[0]);
-        f[2 * i + 1] = to_f32<T>(p[1]);
+        for (int i = 0; i < E / 2; ++i) w[i] = 0;
+    }
+    __device__ __forceinline__ void load(const void *from)
+    {
+#pragma unroll
+        for (int i = 0; i < E / 8; ++i) {
+            const uint4 v = static_cast<const uint4 *>(from)[i];
+            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+        }
+    }
+    __device__ __forceinline__ uint4 quad(int i) const { return make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]); }
+    template <typename T>
+    __device__ __forceinline__ float get(int e) const { return to_f32<T>(reinterpret_cast<const T *>(&w[e / 2])[e % 2]); }
+};
+
+// A unit and its partner, turned: E angles for 2 E elements.
+template <typename T, int E>
+__device__ __forceinline__ void rotate_both(int d0, const AngleTable<E> &cs, Unit<E> &a, Unit<E> &b)
+{
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+        float y1[2], y2[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const float x1 = a.template get<T>(2 * i + x), x2 = b.template get<T>(2 * i + x);
+            const float2 v = cs.cs[(2 * i + x) * AngleTable<E>::kStride + d0 / E];
+            y1[x] = rope_first(v, x1, x2);
+            y2[x] = rope_second(v, x1, x2);
+        }
+        a.w[i] = pack_pair<T>(y1[0], y1[1]);
+        b.w[i] = pack_pair<T>(y2[0], y2[1]);
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void pack16(const float (&f)[16], uint4 &lo, uint4 &hi)
-{
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = pack_pair<T>(f[2 * i], f[2 * i + 1]);
-    lo = make_uint4(w[0], w[1], w[2], w[3]);
-    hi = make_uint4(w[4], w[5], w[6], w[7]);
-}
-
-// The 16 elements d0 .. d0 + 15 of a key row, rotated, in the type of the row
-// (one rounding, as the rotation by itself gives).  Pairs of halves take their
-// partners from the row again: as vectors where a unit lies in one half, else
-// one by one.
-template <typename T>
-__device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_rope_t &rope, const AngleTable &cs, uint4 &lo,
-                                            uint4 &hi, const uint4 plo, const uint4 phi)
+// The E elements from d0 on of a key row, rotated, in the type of the row (one
+// rounding, as the rotation by itself gives).  Pairs of halves take their
+// partners from the row again: as vectors (p) where a unit lies in one half,
+// else one by one.
+template <typename T, int E>
+__device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_rope_t &rope, const AngleTable<E> &cs,
+                                            Unit<E> &u, const Unit<E> &p)
 {
     const int pairs = rope.rotary / 2;
-    float y[16];
+    float y[E];
     if (rope.interleaved) {
-        unpack16<T>(lo, hi, y);
 #pragma unroll
-        for (int e = 0; e < 16; e += 2)
+        for (int e = 0; e < E; e += 2) {
+            const float x1 = u.template get<T>(e), x2 = u.template get<T>(e + 1);
+            y[e] = x1, y[e + 1] = x2;
             if (d0 + e < rope.rotary) {
                 const float2 v = cs((d0 + e) / 2);
-                const float x1 = y[e], x2 = y[e + 1];
                 y[e] = rope_first(v, x1, x2);
                 y[e + 1] = rope_second(v, x1, x2);
             }
-    } else if (pairs % 16 == 0) {
+        }
+    } else if (pairs % E == 0) {
         // one form for both halves: lanes of both share a warp
         const bool second = d0 >= pairs;
-        float a[16], b[16];
-        unpack16<T>(second ? plo : lo, second ? phi : hi, a);
-        unpack16<T>(second ? lo : plo, second ? hi : phi, b);
-        const AngleTable mn{cs.cs + (second ? kAngles : 0)};
+        const AngleTable<E> mn{cs.cs + (second ? kAngles : 0)};
         const int i0 = second ? d0 - pairs : d0;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float2 v = mn.cs[e * AngleTable::kStride + (i0 >> 4)];
-            y[e] = rope_first(v, a[e], b[e]);
+        for (int e = 0; e < E; ++e) {
+            const float mine = u.template get<T>(e), other = p.template get<T>(e);
+            const float2 v = mn.cs[e * AngleTable<E>::kStride + i0 / E];
+            y[e] = rope_first(v, second ? other : mine, second ? mine : other);
         }
     } else {
 #pragma unroll 1
-        for (int e = 0; e < 16; ++e) {
+        for (int e = 0; e < E; ++e) {
             const int d = d0 + e;
             float v = to_f32<T>(row[d]);
             if (d < pairs) v = rope_first(cs(d), v, to_f32<T>(row[d + pairs]));
             else if (d < rope.rotary) v = rope_second(cs(d - pairs), to_f32<T>(row[d - pairs]), v);
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
+            for (int i = 0; i < E; ++i)
                 if (i == e) y[i] = v;
         }
     }
-    pack16<T>(y, lo, hi);
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) u.w[i] = pack_pair<T>(y[2 * i], y[2 * i + 1]);
 }
 
-// A thread takes 16 elements (a unit) of one token's keys and values in several
-// heads; the head groups of a CTA share its tokens' angles.  Few tokens: keys
-// and values by different CTAs (blockIdx.y).  GS = 0: 16-bit pages of type T; else encoded pages (T = __half, four
-// neighbouring lanes per 64-element group: dim is a multiple of 64).
-// Bound by the encoder's instructions, some 400 per 32 x 16 elements with the
-// rotation: 16384 tokens of 8 heads of 128, rotated and encoded, 38.6 us (12.9
-// of bytes); 43.4 with three CTAs per SM, 55.9 with a token per CTA.
-template <typename T, int GS>
-__global__ void __launch_bounds__(kAppendThreads, 4) paged_append_kernel(AppendCall c, int tokens)
+// A thread takes a unit of one token's keys and values in several heads, or
+// (BOTH) a unit and the one half a row behind, its partners where whole heads
+// are turned in halves; the head groups of a CTA share its tokens' angles.  Few
+// tokens: keys and values by different CTAs (blockIdx.y).
+// GS = 0: 16-bit pages of type T; else encoded pages (T = __half, four
+// neighbouring lanes per 64-element group: dim is a multiple of 64, of 128 with
+// BOTH).
+// BOTH reads a pair's angle and elements once for both results instead of once
+// for each, and keeps twice the bytes under way.  16384 tokens of 8 heads of
+// 128, rotated: bf16 pages 23.1 us, 86% of the copy rate (36.9 without BOTH and
+// with units of 16, whose 32 bytes per lane split every line between two
+// loads; 24.2 with 5 CTAs per SM, 26.5 with 4; not rotated 20.0, 25.6 without
+// BOTH); encoded 26.4 us (38.8 without BOTH; 10% more with 3 CTAs per SM, 7%
+// with 5), bound by the encoder's instructions (12.9 us of bytes).
+template <typename T, int GS, bool BOTH>
+__global__ void __launch_bounds__(kAppendThreads, GS == 0 ? 6 : 4) paged_append_kernel(AppendCall c, int tokens)
 {
     griddep_wait();
-    __shared__ float2 s_cs[2 * kAngles];
+    constexpr int E = unit_size(GS != 0), N = BOTH ? 2 : 1;
+    __shared__ float2 s_cs[(BOTH ? 1 : 2) * kAngles];
     const bool keys = gridDim.y == 1 || blockIdx.y == 0, values = gridDim.y == 1 || blockIdx.y == 1;
     const bool rope = c.a.rope.positions != nullptr && keys;
-    const int pairs = rope ? c.a.rope.rotary / 2 : 0;
+    const int pairs = rope ? c.a.rope.rotary / 2 : 0, per = (pairs + E - 1) / E;  // of the table's E lines, per token
     const int first = blockIdx.x * c.tokens_here;
     if (rope) {
-        const int per = (pairs + 15) / 16;  // of the table's 16 lines, per token
         for (int i = threadIdx.x; i < c.tokens_here * pairs; i += blockDim.x) {
             const int n = i / pairs, j = i - n * pairs;
             if (first + n < tokens) {
                 const float2 v = rope_cos_sin(c.a.rope.positions[first + n], rope_unit(c.a.rope.freqs[j]), c.a.rope.scale);
-                float2 *to = s_cs + (j & 15) * AngleTable::kStride + n * per + (j >> 4);
+                float2 *to = s_cs + (j % E) * AngleTable<E>::kStride + n * per + j / E;
                 to[0] = make_float2(v.x, -v.y);
-                to[kAngles] = make_float2(v.y, v.x);
+                if (!BOTH) to[kAngles] = make_float2(v.y, v.x);
             }
         }
         __syncthreads();
@@ -153,53 +184,59 @@ __global__ void __launch_bounds__(kAppendThreads, 4) paged_append_kernel(AppendC
         atomicExch(c.a.dev_err, QUARTZ_DEV_INDEX);
         slot = -1;
     }
-    const AngleTable cs{s_cs + n * ((pairs + 15) / 16)};
+    const AngleTable<E> cs{s_cs + n * per};
     const int64_t page = slot >> c.page_shift, in_page = slot - (page << c.page_shift);
-    const bool turn = 16 * u < 2 * pairs;
-    const bool partners = turn && !c.a.rope.interleaved && pairs % 16 == 0;
-    const int partner = 16 * u < pairs ? pairs : -pairs;
-    const T *k_row = static_cast<const T *>(c.a.k) + t * c.a.k_st, *v_row = static_cast<const T *>(c.a.v) + t * c.a.v_st;
+    const bool turn = E * u < 2 * pairs;
+    const bool partners = turn && !c.a.rope.interleaved && pairs % E == 0;
+    const int partner = BOTH ? E * c.units : E * u < pairs ? pairs : -pairs;
+    const T *k_row = static_cast<const T *>(c.a.k) + t * c.a.k_st + E * u, *v_row = static_cast<const T *>(c.a.v) + t * c.a.v_st + E * u;
     // encoded pages: unit of head 0; heads are page_size rows apart
-    const int64_t unit0 = (((page * c.heads) << c.page_shift) + in_page) * c.units + u;
-    auto store = [&](int side, int h, bool in, const uint4 lo, const uint4 hi) {
+    const int64_t unit0 = (((page * c.heads) << c.page_shift) + in_page) * (N * c.units) + u;
+    auto store = [&](int side, int h, bool in, const Unit<E> &x, int i) {
         const AppendDst &d = c.dst[side];
         if constexpr (GS == 0) {
-            if (in) {
-                uint4 *to = reinterpret_cast<uint4 *>(reinterpret_cast<T *>(d.data) + page * d.stride_page +
-                                                      in_page * d.stride_slot + h * d.stride_head + 16 * u);
-                to[0] = lo;
-                to[1] = hi;
-            }
+            if (in)
+                *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(d.data) + page * d.stride_page + in_page * d.stride_slot +
+                                           h * d.stride_head + E * (u + i * c.units)) = x.quad(0);
         } else {
-            const UnitCodes e = encode_unit_sym<GS>(lo, hi);
-            if (in) store_unit_sym<GS>(e, unit0 + (static_cast<int64_t>(h * c.units) << c.page_shift), lane, d.codes, d.flags, d.scales, false);
+            const UnitCodes e = encode_unit_sym<GS>(x.quad(0), x.quad(1));
+            if (in)
+                store_unit_sym<GS>(e, unit0 + i * c.units + (static_cast<int64_t>(h * N * c.units) << c.page_shift), lane, d.codes,
+                                   d.flags, d.scales, false);
         }
     };
     for (int k = 0; k < c.each; ++k) {  // the same trips for all lanes: encoding takes them together
         const int h = group + k * c.groups;
         const bool in = slot >= 0 && h < c.heads;
-        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
         const T *row = k_row + h * c.a.k_sh;
+        Unit<E> x[2], y[N];
+        x[0].clear(), x[1].clear(), y[0].clear(), y[N - 1].clear();
         if (keys && in) {
-            const uint4 *from = reinterpret_cast<const uint4 *>(row + 16 * u);
-            lo = from[0], hi = from[1];
-            if (turn) {
-                uint4 plo = lo, phi = hi;
-                if (partners) {
-                    from = reinterpret_cast<const uint4 *>(row + 16 * u + partner);
-                    plo = from[0], phi = from[1];
-                }
-                rotate_unit<T>(row, 16 * u, c.a.rope, cs, lo, hi, plo, phi);
-            }
+            x[0].load(row);
+            if (BOTH || partners) x[1].load(row + partner);
         }
-        if (keys) store(0, h, in, lo, hi);
-        if (!values) continue;
-        if (in) {
-            const uint4 *from = reinterpret_cast<const uint4 *>(v_row + h * c.a.v_sh + 16 * u);
-            lo = from[0], hi = from[1];
+        if (values && in) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) y[i].load(v_row + h * c.a.v_sh + i * partner);
         }
-        store(1, h, in, lo, hi);
+        if (keys) {
+            if (in && BOTH && rope) rotate_both<T, E>(E * u, cs, x[0], x[1]);
+            if (in && !BOTH && turn) rotate_unit<T, E>(row - E * u, E * u, c.a.rope, cs, x[0], x[1]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) store(0, h, in, x[i], i);
+        }
+        if (values) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) store(1, h, in, y[i], i);
+        }
     }
+}
+
+template <typename T, int GS>
+cudaError_t launch_append(bool both, dim3 grid, dim3 block, cudaStream_t s, const AppendCall &c, int tokens)
+{
+    return both ? launch_pdl(paged_append_kernel<T, GS, true>, grid, block, 0, s, c, tokens)
+                : launch_pdl(paged_append_kernel<T, GS, false>, grid, block, 0, s, c, tokens);
 }
 
 int log2_of(int v)
@@ -402,11 +439,14 @@ cudaError_t launch_paged_append(const quartz_paged_cache_t *c, const AppendArgs 
     call.page_shift = log2_of(c->page_size);
     call.slots_total = c->num_pages << call.page_shift;
     call.heads = c->heads;
-    call.units = c->dim / 16;
+    const bool encoded = c->type == QUARTZ_PAGES_ENCODED;
+    call.units = c->dim / unit_size(encoded);
     // Heads per thread: two where there are tokens for 1024 threads per SM, else
-    // as few as fit a CTA.  Places of several tokens keep a CTA's warps full
-    // (a power of two of tokens times 4, 8, 12 or 16 units).
-    const bool many = tokens * call.heads * call.units >= int64_t(152) * 1024 * 2;
+    // as few as fit a CTA.  Places of several tokens keep a CTA's warps full.
+    const bool many = tokens * call.heads * c->dim >= int64_t(152) * 1024 * 2 * 16;
+    // (a power of two of tokens times 4 to 32 units)
+    const bool both = many && (!a.rope.positions || (!a.rope.interleaved && a.rope.rotary == c->dim)) && (!encoded || c->dim % 128 == 0);
+    if (both) call.units /= 2;
     int groups = many ? (call.heads + 1) / 2 : call.heads;
     if (groups > kAppendThreads / call.units) groups = kAppendThreads / call.units;
     int n = 1;
@@ -417,13 +457,13 @@ cudaError_t launch_paged_append(const quartz_paged_cache_t *c, const AppendArgs 
     const int threads = n * call.units * groups;  // a multiple of 4
     const dim3 grid(static_cast<unsigned>((tokens + n - 1) / n), many ? 1 : 2), block((threads + 31) & ~31);
     const int total = static_cast<int>(tokens);
-    if (c->type == QUARTZ_PAGES_F16) return launch_pdl(paged_append_kernel<__half, 0>, grid, block, 0, s, call, total);
-    if (c->type == QUARTZ_PAGES_BF16) return launch_pdl(paged_append_kernel<__nv_bfloat16, 0>, grid, block, 0, s, call, total);
+    if (c->type == QUARTZ_PAGES_F16) return launch_append<__half, 0>(both, grid, block, s, call, total);
+    if (c->type == QUARTZ_PAGES_BF16) return launch_append<__nv_bfloat16, 0>(both, grid, block, s, call, total);
     switch (c->k.enc.p.group_s) {
-        case 8: return launch_pdl(paged_append_kernel<__half, 8>, grid, block, 0, s, call, total);
-        case 16: return launch_pdl(paged_append_kernel<__half, 16>, grid, block, 0, s, call, total);
-        case 32: return launch_pdl(paged_append_kernel<__half, 32>, grid, block, 0, s, call, total);
-        default: return launch_pdl(paged_append_kernel<__half, 64>, grid, block, 0, s, call, total);
+        case 8: return launch_append<__half, 8>(both, grid, block, s, call, total);
+        case 16: return launch_append<__half, 16>(both, grid, block, s, call, total);
+        case 32: return launch_append<__half, 32>(both, grid, block, s, call, total);
+        default: return launch_append<__half, 64>(both, grid, block, s, call, total);
     }
 }
 

@@ -104,6 +104,41 @@ def test_encoded_pages(Q, gs, T, H, D, page, rope):
         assert torch.equal(got, exp)
 
 
+@pytest.mark.parametrize("store", ["f16", "bf16", 8, 16, 32, 64])
+@pytest.mark.parametrize("H,D", [(17, 64), (16, 128), (3, 128), (5, 192), (7, 256)])
+@pytest.mark.parametrize("rotary,interleaved", [(0, False), (-1, False), (-1, True), (48, False)])
+def test_many_tokens(Q, store, H, D, rotary, interleaved):
+    """Enough tokens for every SM, where a thread takes units that are each other's partners and several tokens share a
+    CTA; an odd number of tokens, some without a slot, keys inside a fused projection: the bits of rope() and quantize()."""
+    T, page = 152 * 1024 * 32 // (H * D) + 13, 16
+    total = (T + 40) // page + 1
+    dtype = DTYPES.get(store, torch.float16)
+    encoded = not isinstance(store, str)
+    c, ts = _filled(Q, total, page, H, D, dtype, Q.Params(group_s=store) if encoded else None, heads_first=D == 192)
+    k, v = _new(T, H, D, dtype, 21, True), _new(T, H, D, dtype, 22)
+    slots = _slots(T, total * page, 23, skip=(0, 7, T - 1))
+    want, kk, args = [t.clone() for t in ts], k, {}
+    if rotary:
+        freqs, pos = Q.rope_frequencies(D if rotary < 0 else rotary)[0], (torch.arange(T) * 3 + 9).cuda()
+        kk = Q.rope(k, pos, freqs, interleaved=interleaved, scale=0.9)
+        args = dict(positions=pos, freqs=freqs, interleaved=interleaved, rope_scale=0.9)
+    there = slots >= 0
+    at = slots[there]
+    for i, x in enumerate((kk, v)):
+        x = x[there.cuda()]
+        if encoded:
+            e = Q.quantize(x.reshape(-1, D), group_s=store)
+            rows = ((at // page * H)[:, None] + torch.arange(H)).mul(page).add((at % page)[:, None]).view(-1).cuda()
+            for dst, src in zip(want[3 * i:3 * i + 3], (e.codes, e.flags, e.scales)):
+                dst[rows] = src
+        else:
+            want[i][(at // page).cuda(), (at % page).cuda()] = x
+    Q.paged_append(c, k, v, slots.cuda(), **args)
+    assert Q.device_status() == 0
+    for got, exp in zip(ts, want):
+        assert torch.equal(got, exp)
+
+
 def test_slot_out_of_range_is_reported_and_not_followed(Q):
     c, ts = _filled(Q, 2, 8, 2, 64, torch.float16)
     before = [t.clone() for t in ts]
