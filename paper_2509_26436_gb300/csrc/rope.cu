@@ -2,13 +2,13 @@
 // position times frequency, pairs (i, i + rotary/2) or (2i, 2i + 1).
 //
 // HBM-bound: x is read and y written once, 3 operations per element.  A thread
-// turns V pairs of one token (two V-element vectors) in several heads; the
-// threads of a CTA that have the same pairs in other heads share the angles,
-// computed once per CTA, which costs about as much as turning them in ten
-// heads.  Many threads with one head in flight each (64 registers, 1024 per SM)
-// measured better than fewer with more: 8192 x 32 x 128 bf16, of a strided
-// tensor: with angles per thread 28.5 us with one head in flight, 31.2 with two,
-// 38.3 with four; with shared angles 26.7 (a plain copy of as many bytes: 22.9).
+// turns V pairs of one token (two V-element vectors) in several heads, the next
+// head's loads under way; the threads of a CTA that have the same pairs in other
+// heads share the angles, computed once per CTA, which costs about as much as
+// turning them in ten heads.  8192 x 32 x 128 bf16, of a strided tensor: 23.7 us,
+// 84% of the copy rate, with 1280 threads per SM (48 registers, the angles read
+// from shared memory for each head); 1024 26.1, 1536 24.6; one head in flight
+// 24.8; angles in registers as well 26.6; angles per thread 28.5.
 #include "quartz_internal.h"
 #include "rope.cuh"
 
@@ -41,7 +41,7 @@ __device__ __forceinline__ void store_rounded(T *to, const float (&f)[V])
 // from `rotary` on.  `here` (token, piece) places per CTA, as consecutive
 // threads; the threads behind them: the same places in further heads.
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs a, int64_t places, int here, int heads_each)
+__global__ void __launch_bounds__(kThreads, 10) rope_kernel(RopeArgs a, int64_t places, int here, int heads_each)
 {
     griddep_wait();
     __shared__ float2 s_cs[V * kThreads];  // [pair of the piece][place]
@@ -76,13 +76,11 @@ __global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs a, int64_t p
         }
     }
     __syncthreads();
-    float2 cs[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) cs[j] = s_cs[j * here + place];
     for (int h = h0; h < h1; ++h) {
-        if (h > h0) {
-            u = *reinterpret_cast<const Vec<T, V> *>(x + h * a.x_sh);
-            if (turn) w = *reinterpret_cast<const Vec<T, V> *>(x + h * a.x_sh + gap);
+        Vec<T, V> u2, w2;
+        if (h + 1 < h1) {  // the next head's
+            u2 = *reinterpret_cast<const Vec<T, V> *>(x + (h + 1) * a.x_sh);
+            if (turn) w2 = *reinterpret_cast<const Vec<T, V> *>(x + (h + 1) * a.x_sh + gap);
         }
         T *to = y + h * a.y_sh;
         if (turn) {
@@ -93,11 +91,11 @@ __global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs a, int64_t p
                     // elements 2j and 2j + 1 of the 2V read
                     const T x1 = 2 * j < V ? u.e[(2 * j) % V] : w.e[(2 * j) % V];
                     const T x2 = 2 * j + 1 < V ? u.e[(2 * j + 1) % V] : w.e[(2 * j + 1) % V];
-                    const float2 r = rope_turn(to_f32<T>(x1), to_f32<T>(x2), cs[j]);
+                    const float2 r = rope_turn(to_f32<T>(x1), to_f32<T>(x2), s_cs[j * here + place]);
                     f[2 * j / V][(2 * j) % V] = r.x;
                     f[(2 * j + 1) / V][(2 * j + 1) % V] = r.y;
                 } else {
-                    const float2 r = rope_turn(to_f32<T>(u.e[j]), to_f32<T>(w.e[j]), cs[j]);
+                    const float2 r = rope_turn(to_f32<T>(u.e[j]), to_f32<T>(w.e[j]), s_cs[j * here + place]);
                     f[0][j] = r.x;
                     f[1][j] = r.y;
                 }
@@ -107,6 +105,7 @@ __global__ void __launch_bounds__(kThreads, 8) rope_kernel(RopeArgs a, int64_t p
         } else {
             *reinterpret_cast<Vec<T, V> *>(to) = u;
         }
+        u = u2, w = w2;
     }
 }
 
@@ -115,7 +114,7 @@ cudaError_t launch_v(const RopeArgs &a, int64_t tokens, cudaStream_t s)
 {
     const int64_t places = tokens * (a.rope.rotary / 2 / V + (a.dim - a.rope.rotary) / V);
     // More groups of heads per CTA while there are fewer than 2048 threads per SM
-    // (8192 x 32 x 128: 26.7 us; up to 1024 27.3, up to 8192 35.3)
+    // (8192 x 32 x 128: 23.7 us; up to 1024 25.6, up to 4096 24.5)
     int groups = 1;
     while (groups < 32 && groups < a.heads && places * groups < 152 * 2048) groups *= 2;
     const int here = kThreads / groups, each = (a.heads + groups - 1) / groups;
