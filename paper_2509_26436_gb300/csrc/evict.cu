@@ -188,8 +188,7 @@ cudaError_t launch_evict_select(const float *w, int64_t w_sb, int64_t w_sh, cons
     const dim3 grid(static_cast<unsigned>(seqs * heads));
     if (max_len <= kHeldKeys) {
         const int bytes = static_cast<int>(max_len) * 4;
-        const cudaError_t e = cudaFuncSetAttribute(evict_select_kernel<true>,
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, kHeldKeys * 4);
+        const cudaError_t e = allow_shared<evict_select_kernel<true>>(kHeldKeys * 4);
         if (e != cudaSuccess) return e;
         return launch_pdl(evict_select_kernel<true>, grid, dim3(kThreads), bytes, s, a);
     }

@@ -196,10 +196,7 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
 template <int D, bool BF>
 struct Kernel16 {
     static constexpr int kSmem = kPagedWarps * Tile16<D>::kStages * Tile16<D>::kBytes;
-    static cudaError_t ready()
-    {
-        return cudaFuncSetAttribute(paged_attn_kernel<D, BF>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    }
+    static cudaError_t ready() { return allow_shared<paged_attn_kernel<D, BF>>(kSmem); }
     static int occupancy()
     {
         static std::atomic<int> cache{0};

@@ -490,10 +490,8 @@ struct KernelLzs {
     static constexpr int kSmem = kPagedWarps * LzsTile<D, GS>::kStages * LzsTile<D, GS>::kBytes;
     static cudaError_t ready()
     {
-        const cudaError_t e = cudaFuncSetAttribute(paged_attn_lzs_kernel<D, GS, false, MINB>,
-                                                   cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        if (e != cudaSuccess) return e;
-        return cudaFuncSetAttribute(paged_attn_lzs_kernel<D, GS, true, MINB>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        const cudaError_t e = allow_shared<paged_attn_lzs_kernel<D, GS, false, MINB>>(kSmem);
+        return e != cudaSuccess ? e : allow_shared<paged_attn_lzs_kernel<D, GS, true, MINB>>(kSmem);
     }
     static int occupancy()
     {

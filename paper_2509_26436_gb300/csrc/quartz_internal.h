@@ -1,6 +1,7 @@
 // Declarations shared by the translation units of libquartz (not installed).
 #pragma once
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 #include <cuda_runtime.h>
@@ -21,6 +22,25 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 
 // Device error word of the current device (see api.cu).
 int *device_error_word();
+
+#ifdef __CUDACC__
+// Let launches of Kernel on the current device have up to `bytes` of dynamic
+// shared memory (always the same number): once per device, since the call costs
+// a tenth of a launch.
+template <auto Kernel>
+cudaError_t allow_shared(int bytes)
+{
+    static std::atomic<uint64_t> allowed{0};
+    int dev = 0;
+    const cudaError_t got = cudaGetDevice(&dev);
+    if (got != cudaSuccess) return got;
+    const uint64_t bit = dev < 64 ? uint64_t(1) << dev : 0;
+    if (allowed.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
+#endif
 
 // Programmatic dependent launch.  The library's kernels are launched with
 // launch_pdl, which lets the launch of a kernel overlap the end of the

@@ -28,6 +28,7 @@ _byref = C.byref
 # torch); lib is the loaded library.
 torch = f16 = bf16 = f32 = f64 = i32 = i64 = lib = _device = None
 _KIND = {}  # torch type -> quartz_out_t
+_NO_WORKSPACE = 256  # attention's workspace where one kernel does all: nothing is written to it
 
 
 def _bind():
@@ -205,6 +206,7 @@ class PagedCache:
         self._ref = _byref(self.c)
         self._index = self.device.index
         self._workspace_sizes = {}
+        self._no_workspace = torch.empty(_NO_WORKSPACE, dtype=torch.uint8, device=self.device)
 
     def _workspace_size(self, seqs, q_heads, max_len, window, with_weights) -> int:
         key = (seqs, q_heads, max_len, window, with_weights)
@@ -301,8 +303,8 @@ def attention_paged(q, cache: PagedCache, block_table, seq_lens, scale: float, w
             raise ValueError("weights must be [seqs, heads, at least max_len]")
         w_ptr, with_weights = weights.data_ptr(), 1
     if workspace is None:
-        size = max(cache._workspace_size(B, Hq, max_len, window, with_weights), 16)
-        workspace = _empty(size, torch.uint8, cache.device, stream)
+        size = cache._workspace_size(B, Hq, max_len, window, with_weights)
+        workspace = cache._no_workspace if size <= _NO_WORKSPACE else _empty(size, torch.uint8, cache.device, stream)
     else:
         if workspace.get_device() != device or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
