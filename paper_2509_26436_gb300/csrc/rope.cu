@@ -37,11 +37,20 @@ __device__ __forceinline__ void store_rounded(T *to, const float (&f)[V])
     *reinterpret_cast<Vec<T, V> *>(to) = v;
 }
 
+// n / pieces by a product with 2^64 / pieces, rounded up (0: pieces is 1): exact
+// for n pieces < 2^64, and places are below 2^39.  (A 64-bit division is some
+// hundred instructions.)
+__device__ __forceinline__ int64_t token_of(int64_t n, uint64_t inverse)
+{
+    return inverse ? static_cast<int64_t>(__umul64hi(static_cast<uint64_t>(n), inverse)) : n;
+}
+
 // Piece p < pairs / V of a head turns V pairs, the others copy V elements each
 // from `rotary` on.  `here` (token, piece) places per CTA, as consecutive
 // threads; the threads behind them: the same places in further heads.
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads, 10) rope_kernel(RopeArgs a, int64_t places, int here, int heads_each)
+__global__ void __launch_bounds__(kThreads, 10) rope_kernel(RopeArgs a, int64_t places, uint64_t inverse, int here,
+                                                            int heads_each)
 {
     griddep_wait();
     __shared__ float2 s_cs[V * kThreads];  // [pair of the piece][place]
@@ -51,7 +60,7 @@ __global__ void __launch_bounds__(kThreads, 10) rope_kernel(RopeArgs a, int64_t 
     const int group = threadIdx.x / here, place = threadIdx.x - group * here;
     const int64_t id = first_place + place;
     const bool in = id < places;
-    const int64_t t = in ? id / pieces : 0;
+    const int64_t t = in ? token_of(id, inverse) : 0;
     const int p = in ? static_cast<int>(id - t * pieces) : 0;
     const bool turn = p < turns;
     const int first = turn ? (a.rope.interleaved ? 2 * p * V : p * V) : a.rope.rotary + (p - turns) * V;
@@ -68,7 +77,7 @@ __global__ void __launch_bounds__(kThreads, 10) rope_kernel(RopeArgs a, int64_t 
     for (int i = threadIdx.x; i < here * V; i += kThreads) {
         const int j = i / here;
         const int64_t at = first_place + (i - j * here);
-        const int64_t token = at / pieces;
+        const int64_t token = token_of(at, inverse);
         const int piece = static_cast<int>(at - token * pieces);
         if (at < places && piece < turns) {
             const float2 cs = rope_cos_sin(a.rope.positions[token], rope_unit(a.rope.freqs[piece * V + j]), a.rope.scale);
@@ -112,14 +121,16 @@ __global__ void __launch_bounds__(kThreads, 10) rope_kernel(RopeArgs a, int64_t 
 template <typename T, int V>
 cudaError_t launch_v(const RopeArgs &a, int64_t tokens, cudaStream_t s)
 {
-    const int64_t places = tokens * (a.rope.rotary / 2 / V + (a.dim - a.rope.rotary) / V);
+    const int pieces = a.rope.rotary / 2 / V + (a.dim - a.rope.rotary) / V;
+    const int64_t places = tokens * pieces;
+    const uint64_t inverse = pieces > 1 ? ~uint64_t(0) / pieces + 1 : 0;
     // More groups of heads per CTA while there are fewer than 2048 threads per SM
     // (8192 x 32 x 128: 23.7 us; up to 1024 25.6, up to 4096 24.5)
     int groups = 1;
     while (groups < 32 && groups < a.heads && places * groups < 152 * 2048) groups *= 2;
     const int here = kThreads / groups, each = (a.heads + groups - 1) / groups;
     return launch_pdl(rope_kernel<T, V>, dim3(static_cast<unsigned>((places + here - 1) / here)), dim3(kThreads), 0, s, a, places,
-                      here, each);
+                      inverse, here, each);
 }
 
 // The widest vectors of V elements (16 bytes, or 8) that sizes, strides and
