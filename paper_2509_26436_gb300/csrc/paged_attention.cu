@@ -34,7 +34,7 @@ __device__ __forceinline__ void ldmatrix4_trans(uint32_t a, uint32_t (&r)[4])
                  : "r"(a));
 }
 
-template <int D, bool BF>
+template <int D, bool BF, bool SHARE>
 __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_kernel(PagedArgs a)
 {
     griddep_wait();
@@ -48,12 +48,13 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
     __shared__ PagedJoin s_join;
 
     const int head_block = blockIdx.x / a.n_split, split = blockIdx.x - head_block * a.n_split;
-    const int kv_head = blockIdx.y, b = blockIdx.z, head0 = head_block * kPagedHeads;
+    const int kv_head = blockIdx.y, head0 = head_block * kPagedHeads;
+    int b, begin, chunk;
+    if (!paged_place<SHARE>(a, split, b, begin, chunk)) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
-    const int begin = split * a.chunk;
     if (a.part_o && begin >= range.count()) return;
-    const int end = range.base + min(begin + a.chunk, range.count());  // first token behind the split
+    const int end = range.base + min(begin + chunk, range.count());  // first token behind the split
     const int base0 = range.base + begin + warp * 16;
     const int tiles = base0 < end ? (end - base0 + kPagedWarps * 16 - 1) / (kPagedWarps * 16) : 0;
     const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + warp * kWarpBytes;
@@ -190,21 +191,20 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
     paged_wait<0>();
     __syncwarp();
     if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
-    paged_finish<D, false>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, kUp);
+    paged_finish<D, false, SHARE>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, kUp);
 }
 
 template <int D, bool BF>
 struct Kernel16 {
     static constexpr int kSmem = kPagedWarps * Tile16<D>::kStages * Tile16<D>::kBytes;
-    static cudaError_t ready() { return allow_shared<paged_attn_kernel<D, BF>>(kSmem); }
     static int occupancy()
     {
         static std::atomic<int> cache{0};
         int occ = cache.load(std::memory_order_relaxed);
         if (occ == 0) {
             int k = 0;
-            if (ready() != cudaSuccess || cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, paged_attn_kernel<D, BF>, kPagedThreads,
-                                                                                        kSmem) != cudaSuccess)
+            if (allow_shared<paged_attn_kernel<D, BF, false>>(kSmem) != cudaSuccess ||
+                cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, paged_attn_kernel<D, BF, false>, kPagedThreads, kSmem) != cudaSuccess)
                 return 1;
             occ = k > 0 ? k : 1;
             cache.store(occ, std::memory_order_relaxed);
@@ -213,10 +213,15 @@ struct Kernel16 {
     }
     static cudaError_t launch(const PagedArgs &a, dim3 grid, cudaStream_t s)
     {
-        const cudaError_t e = ready();  // of the current device
+        return a.share ? launch_as<true>(a, grid, s) : launch_as<false>(a, grid, s);
+    }
+    template <bool SHARE>
+    static cudaError_t launch_as(const PagedArgs &a, dim3 grid, cudaStream_t s)
+    {
+        const cudaError_t e = allow_shared<paged_attn_kernel<D, BF, SHARE>>(kSmem);
         if (e != cudaSuccess) return e;
-        if (a.cluster) return launch_pdl_cluster(paged_attn_kernel<D, BF>, a.n_split, grid, dim3(kPagedThreads), kSmem, s, a);
-        return launch_pdl(paged_attn_kernel<D, BF>, grid, dim3(kPagedThreads), kSmem, s, a);
+        if (a.cluster) return launch_pdl_cluster(paged_attn_kernel<D, BF, SHARE>, a.n_split, grid, dim3(kPagedThreads), kSmem, s, a);
+        return launch_pdl(paged_attn_kernel<D, BF, SHARE>, grid, dim3(kPagedThreads), kSmem, s, a);
     }
 };
 
@@ -244,13 +249,20 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
     __shared__ float2 s_ml[kJoinHeads];  // m and log2 l: apart, since together they would lose l where m is large
     const int b = blockIdx.z;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
-    const int splits = (range.count() + a.chunk - 1) / a.chunk;  // that hold tokens
     const int64_t row0 = (static_cast<int64_t>(b) * a.kv_heads + blockIdx.y) * a.group;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    int splits = (range.count() + a.chunk - 1) / a.chunk;  // that hold tokens
+    int64_t part0 = row0 * a.n_split;                      // of the key head's first query head
+    if (a.share) {
+        const PagedShare s = paged_share(a);
+        splits = __shfl_sync(0xffffffffu, s.count, b);
+        part0 = static_cast<int64_t>(blockIdx.y) * a.group * a.n_split + __shfl_sync(0xffffffffu, s.first, b);
+    }
 
     for (int head = blockIdx.x; a.part_o && head < a.group; head += gridDim.x) {
         const int64_t row = row0 + head;
-        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + row * a.n_split;
+        const int64_t part = part0 + static_cast<int64_t>(head) * a.n_split;
+        const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + part;
         float m = kPagedLow;
         for (int i = tid; i < splits; i += kJoinThreads) m = fmaxf(m, ml[i].x);
 #pragma unroll
@@ -281,7 +293,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
         const int g = tid / kLanes, c = tid - g * kLanes;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (g < kGroups) {
-            const float4 *o = reinterpret_cast<const float4 *>(a.part_o + row * a.n_split * D) + c;
+            const float4 *o = reinterpret_cast<const float4 *>(a.part_o + part * D) + c;
 #pragma unroll 4
             for (int i = g; i < splits; i += kGroups) {
                 const float4 u = o[static_cast<int64_t>(i) * kLanes];
@@ -314,7 +326,7 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
             if (!held) {  // m and log2 l of each head, a warp each
                 __syncthreads();
                 for (int g = warp; g < heads; g += kJoinThreads / 32) {
-                    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (row0 + g0 + g) * a.n_split;
+                    const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + part0 + static_cast<int64_t>(g0 + g) * a.n_split;
                     float m = kPagedLow, sum = 0.f;
                     for (int i = lane; i < splits; i += 32) m = fmaxf(m, ml[i].x);
 #pragma unroll
@@ -365,6 +377,7 @@ int log2_of(int v)
 // SMs are free, or, to few enough splits for a cluster, two thirds of them.
 struct PagedPlan {
     int n_split, chunk;
+    int share;
     bool cluster;
     int64_t tokens, score_stride;
 };
@@ -407,6 +420,17 @@ PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, i
     // against 5.7).  With the SMs nearly full, clusters wait for places next to
     // each other (777 tokens, fp16, 7 splits: 8.8 against 7.0).
     p.cluster = p.n_split > 1 && p.n_split <= kPagedCluster && 3 * p.n_split * ctas <= 2 * slots && !with_weights;
+    // Few sequences (what rounding to whole places loses is an eighth at most):
+    // one wave, shared out by the lengths.  Against the splits above, 8 heads,
+    // encoded: one of 131072 tokens 48.1 us (60.3), 2 and 4 of 32768 each 27.5 and
+    // 50.0 (34.0, 54.6), of up to 32768 19.3 and 32.0 (23.9, 36.5); 8 of up to
+    // 65536, a wave of 7 places each, 98.1 (96.4).  bf16: one of 131072 89.2 (93.4).
+    const int64_t wave = slots / (ctas / (seqs > 0 ? seqs : 1)), units = (p.tokens + kShareUnit - 1) / kShareUnit;
+    p.share = 0;
+    if (!p.cluster && p.n_split > 1 && seqs <= kShareSeqs && wave >= 8 * seqs) {
+        p.share = static_cast<int>(wave < kMaxSplits ? wave : kMaxSplits);
+        p.n_split = static_cast<int>(p.share < seqs * units ? p.share : seqs * units);
+    }
     p.score_stride = (p.tokens + 63) / 64 * 64;
     return p;
 }
@@ -444,8 +468,9 @@ size_t paged_attention_workspace_bytes(const quartz_paged_cache_t *c, int64_t se
     const size_t rows = static_cast<size_t>(seqs) * q_heads;
     size_t n = 256;
     const bool join = p.n_split > 1 && !p.cluster;
-    if (join) n += up256(rows * p.n_split * c->dim * 4);
-    if (join || with_weights) n += up256(rows * p.n_split * 8);
+    const size_t parts = (p.share ? q_heads : rows) * p.n_split;
+    if (join) n += up256(parts * c->dim * 4);
+    if (join || with_weights) n += up256(parts * 8);
     if (with_weights) n += up256(rows * static_cast<size_t>(p.score_stride) * 4);
     return n;
 }
@@ -477,27 +502,29 @@ cudaError_t launch_paged_attention(const quartz_paged_cache_t *c, const PagedAtt
     a.max_len = static_cast<int>(call.max_len);
     a.window = static_cast<int>(call.window < call.max_len ? call.window : 0);
     a.n_split = p.n_split, a.chunk = p.chunk;
+    a.share = p.share, a.seqs = static_cast<int>(call.seqs);
     a.scale_log2 = call.scale * kPagedLog2e;
     a.o = call.o, a.o_type = call.o_type;
     a.dev_err = call.dev_err;
     uint8_t *ws = static_cast<uint8_t *>(call.workspace);
     const size_t rows = static_cast<size_t>(call.seqs) * call.q_heads;
+    const size_t parts = (p.share ? call.q_heads : rows) * p.n_split;
     const bool join = p.n_split > 1 && !p.cluster;
     a.cluster = p.cluster;
     if (join) {
         a.part_o = reinterpret_cast<float *>(ws);
-        ws += up256(rows * p.n_split * c->dim * 4);
+        ws += up256(parts * c->dim * 4);
     }
     if (join || call.weights) {
         a.part_ml = reinterpret_cast<float *>(ws);
-        ws += up256(rows * p.n_split * 8);
+        ws += up256(parts * 8);
     }
     if (call.weights) {
         a.scores = reinterpret_cast<float *>(ws);
         a.score_stride = p.score_stride;
     }
     const dim3 grid(static_cast<unsigned>(p.n_split * a.head_blocks), static_cast<unsigned>(c->heads),
-                    static_cast<unsigned>(call.seqs));
+                    static_cast<unsigned>(p.share ? 1 : call.seqs));
     cudaError_t e = c->type == QUARTZ_PAGES_ENCODED ? launch_paged_encoded(c->dim, c->k.enc.p.group_s, a, grid, s)
                                                     : launch_paged_16bit(c->type, c->dim, a, grid, s);
     if (e == cudaSuccess && (join || call.weights)) {

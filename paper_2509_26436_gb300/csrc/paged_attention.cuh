@@ -2,10 +2,11 @@
 // and for encoded pages share.
 //
 // A CTA takes one sequence, one key / value head, up to 8 of the query heads
-// that share it and one split (a run of consecutive tokens); its 4 warps take
-// tiles of 16 tokens in turn, each through a ring in shared memory of its own
-// that asynchronous copies fill some tiles ahead, so no warp waits for
-// another.  The products run on the warp-level tensor instruction m16n8k16
+// that share it and one split (a run of consecutive tokens; for few sequences
+// given out by their lengths, PagedShare); its 4 warps take tiles of 16 tokens
+// in turn, each through a ring in shared memory of its own that asynchronous
+// copies fill some tiles ahead, so no warp waits for another.  The products run
+// on the warp-level tensor instruction m16n8k16
 // with fp32 accumulators:
 //   S' = K Q':  rows: 16 tokens, columns: 8 heads;
 //   O += P V:   rows 0-7: the upper 16 bits of the heads' softmax weights, rows
@@ -58,9 +59,10 @@ struct PagedArgs {
     uint32_t num_pages;
     int page_shift, kv_heads, group, head_blocks;  // query heads per key head; CTAs they take
     int max_len, window, n_split, chunk;
+    int share, seqs;  // share > 0: as many CTAs, at most, share the tokens of all sequences (PagedShare)
     float scale_log2;
-    float *part_o;   // NULL, or [seqs * q_heads][n_split][dim]: splits for the join kernel; NULL: o is written
-    float *part_ml;  // NULL, or [seqs * q_heads][n_split][2]: maximum and sum (with part_o or scores)
+    float *part_o;   // NULL, or [seqs * q_heads, share: q_heads][n_split][dim]: splits for the join; NULL: o is written
+    float *part_ml;  // NULL, or as many [2]: maximum and sum (with part_o or scores)
     int cluster;     // the splits of a head are one cluster, which joins them itself
     float *scores;   // NULL, or [seqs * q_heads][score_stride], log2 domain
     int64_t score_stride;
@@ -89,6 +91,59 @@ __device__ __forceinline__ PagedRange paged_range(const int32_t *lens, int b, in
     r.base = r.first & ~15;
     r.end = len;
     return r;
+}
+
+// Few sequences: `share` places per key head and block of query heads, one wave
+// of CTAs, go to the sequences by their lengths.  In units of 64 tokens (a tile
+// of each warp), a place takes `each` = ceil(all / (share - seqs)), a sequence
+// ceil(its units / each) places in a row, which is at most `share` together.
+// (All lanes of a warp; of lane's sequence.)
+constexpr int kShareSeqs = 32;
+constexpr int kShareUnit = 64;
+
+struct PagedShare {
+    int first, count;  // places
+    int chunk;         // tokens of a place
+};
+
+__device__ __forceinline__ PagedShare paged_share(const PagedArgs &a)
+{
+    const int lane = threadIdx.x & 31;
+    int units = 0;
+    if (lane < a.seqs) units = (paged_range(a.lens, lane, a.max_len, a.window, a.dev_err).count() + kShareUnit - 1) / kShareUnit;
+    const int all = __reduce_add_sync(0xffffffffu, units), left = a.share - a.seqs;
+    const int each = max(1, (all + left - 1) / left);
+    PagedShare s;
+    s.count = (units + each - 1) / each;
+    s.chunk = each * kShareUnit;
+    s.first = s.count;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        const int v = __shfl_up_sync(0xffffffffu, s.first, d);
+        if (lane >= d) s.first += v;
+    }
+    s.first -= s.count;
+    return s;
+}
+
+// What a CTA takes: tokens [begin, begin + chunk) of a sequence, counted from the
+// range's base.  False: nothing.  (SHARE is an instance of its own: as a branch
+// it cost the other calls 1%, 0.1 us at the start of each of their CTAs.)
+template <bool SHARE>
+__device__ __forceinline__ bool paged_place(const PagedArgs &a, int place, int &b, int &begin, int &chunk)
+{
+    b = blockIdx.z;
+    chunk = a.chunk;
+    begin = place * chunk;
+    if (SHARE) {
+        const PagedShare s = paged_share(a);
+        const unsigned behind = __ballot_sync(0xffffffffu, place < s.first + s.count);
+        if (!behind) return false;
+        b = __ffs(behind) - 1;
+        chunk = s.chunk;
+        begin = (place - __shfl_sync(0xffffffffu, s.first, b)) * chunk;
+    }
+    return true;
 }
 
 __device__ __forceinline__ float ex2(float x)
@@ -293,7 +348,7 @@ constexpr int kPagedJoinBytes = kPagedHeads * (D + 4) * 4;
 //
 // The accumulators' column 2 q + x of entry i is dimension 8 i + 2 q + x, or
 // (STRIDED) (i / 8) 64 + (2 q + x) 8 + i % 8.
-template <int D, bool STRIDED>
+template <int D, bool STRIDED, bool SHARE>
 __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int warp_bytes, PagedState<D> &st,
                                              const PagedArgs &a, int b, int kv_head, int head0, int split, float up)
 {
@@ -341,7 +396,8 @@ __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int wa
             sum += f * s.l[w][h];
             v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
         }
-        const int64_t row = row0 + h, at = row * a.n_split + split;
+        const int64_t row = row0 + h;
+        const int64_t at = (SHARE ? row - static_cast<int64_t>(b) * a.kv_heads * a.group : row) * a.n_split + split;
         if (a.part_ml && d == 0) *reinterpret_cast<float2 *>(a.part_ml + 2 * at) = make_float2(m, sum);
         if (a.cluster) {
             *so(0, h, d) = v;  // read by this thread only, above

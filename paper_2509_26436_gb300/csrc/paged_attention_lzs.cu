@@ -201,7 +201,7 @@ __device__ __forceinline__ void lds_scales(uint32_t a, float (&s)[G])
 // GENERAL: pages below 16 tokens, scores for the sums of weights, or binary32
 // results; the other instance is for pages of 16 and more, 16-bit results and
 // no scores.
-template <int D, int GS, bool GENERAL, int MINB>
+template <int D, int GS, bool GENERAL, bool SHARE, int MINB>
 __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(PagedArgs a)
 {
     griddep_wait();
@@ -215,12 +215,13 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     __shared__ PagedJoin s_join;
 
     const int head_block = blockIdx.x / a.n_split, split = blockIdx.x - head_block * a.n_split;
-    const int kv_head = blockIdx.y, b = blockIdx.z, head0 = head_block * kPagedHeads;
+    const int kv_head = blockIdx.y, head0 = head_block * kPagedHeads;
+    int b, begin, chunk;
+    if (!paged_place<SHARE>(a, split, b, begin, chunk)) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, q = lane & 3;
     const PagedRange range = paged_range(a.lens, b, a.max_len, a.window, a.dev_err);
-    const int begin = split * a.chunk;
     if (a.part_o && begin >= range.count()) return;
-    const int end = range.base + min(begin + a.chunk, range.count());
+    const int end = range.base + min(begin + chunk, range.count());
     // a warp's tiles are consecutive, so that most follow the one before in its page
     const int all_tiles = max(0, end - range.base - begin + 15) >> 4, warp_tiles = (all_tiles + kPagedWarps - 1) / kPagedWarps;
     const int tiles = max(0, min(warp_tiles, all_tiles - warp * warp_tiles));
@@ -481,26 +482,22 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     paged_wait<0>();
     __syncwarp();
     if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
-    paged_finish<D, true>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, 0.f);
+    paged_finish<D, true, SHARE>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, 0.f);
 }
 
 template <int D, int GS>
 struct KernelLzs {
     static constexpr int MINB = D <= 64 ? 4 : D <= 128 ? 3 : 2;
     static constexpr int kSmem = kPagedWarps * LzsTile<D, GS>::kStages * LzsTile<D, GS>::kBytes;
-    static cudaError_t ready()
-    {
-        const cudaError_t e = allow_shared<paged_attn_lzs_kernel<D, GS, false, MINB>>(kSmem);
-        return e != cudaSuccess ? e : allow_shared<paged_attn_lzs_kernel<D, GS, true, MINB>>(kSmem);
-    }
     static int occupancy()
     {
         static std::atomic<int> cache{0};
         int occ = cache.load(std::memory_order_relaxed);
         if (occ == 0) {
             int k = 0;
-            if (ready() != cudaSuccess || cudaOccupancyMaxActiveBlocksPerMultiprocessor(
-                                              &k, paged_attn_lzs_kernel<D, GS, false, MINB>, kPagedThreads, kSmem) != cudaSuccess)
+            if (allow_shared<paged_attn_lzs_kernel<D, GS, false, false, MINB>>(kSmem) != cudaSuccess ||
+                cudaOccupancyMaxActiveBlocksPerMultiprocessor(&k, paged_attn_lzs_kernel<D, GS, false, false, MINB>, kPagedThreads,
+                                                              kSmem) != cudaSuccess)
                 return 1;
             occ = k > 0 ? k : 1;
             cache.store(occ, std::memory_order_relaxed);
@@ -509,17 +506,18 @@ struct KernelLzs {
     }
     static cudaError_t launch(const PagedArgs &a, dim3 grid, cudaStream_t s)
     {
-        const cudaError_t e = ready();  // of the current device
-        if (e != cudaSuccess) return e;
-        if (a.scores || a.page_shift < 4 || a.o_type == QUARTZ_OUT_F32) return launch_as<true>(a, grid, s);
-        return launch_as<false>(a, grid, s);
+        if (a.scores || a.page_shift < 4 || a.o_type == QUARTZ_OUT_F32)
+            return a.share ? launch_as<true, true>(a, grid, s) : launch_as<true, false>(a, grid, s);
+        return a.share ? launch_as<false, true>(a, grid, s) : launch_as<false, false>(a, grid, s);
     }
-    template <bool GENERAL>
+    template <bool GENERAL, bool SHARE>
     static cudaError_t launch_as(const PagedArgs &a, dim3 grid, cudaStream_t s)
     {
+        const cudaError_t e = allow_shared<paged_attn_lzs_kernel<D, GS, GENERAL, SHARE, MINB>>(kSmem);
+        if (e != cudaSuccess) return e;
         if (a.cluster)
-            return launch_pdl_cluster(paged_attn_lzs_kernel<D, GS, GENERAL, MINB>, a.n_split, grid, dim3(kPagedThreads), kSmem, s, a);
-        return launch_pdl(paged_attn_lzs_kernel<D, GS, GENERAL, MINB>, grid, dim3(kPagedThreads), kSmem, s, a);
+            return launch_pdl_cluster(paged_attn_lzs_kernel<D, GS, GENERAL, SHARE, MINB>, a.n_split, grid, dim3(kPagedThreads), kSmem, s, a);
+        return launch_pdl(paged_attn_lzs_kernel<D, GS, GENERAL, SHARE, MINB>, grid, dim3(kPagedThreads), kSmem, s, a);
     }
 };
 

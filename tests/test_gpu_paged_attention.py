@@ -254,6 +254,21 @@ def test_every_plan(Q, store, B, H, n):
     check(Q, c, table, ln, _q(B, H, 128, torch.float16, 17), 128 ** -0.5, store=store, out="f16")
 
 
+@pytest.mark.parametrize("store", ["f16", "bf16", "lzs"])
+@pytest.mark.parametrize("lens,H,group,D,window", [([2500, 0, 1, 700], 1, 5, 128, 0), ([0, 0, 3000], 2, 9, 64, 0),
+                                                   ([64 * i % 1500 for i in range(32)], 1, 2, 128, 0), ([0] * 5, 1, 1, 64, 0),
+                                                   ([5000, 3000, 90], 1, 4, 192, 1100), ([2049], 2, 3, 256, 0)])
+def test_few_sequences_share_a_wave(Q, store, lens, H, group, D, window):
+    """CTAs given out by the lengths: empty sequences among them, a window, more heads than a CTA takes; the table's
+    bound and a far larger one (the lengths count, not the bound)."""
+    c, table, ln = make_cache(Q, lens, H, D, 16, store, seed=len(lens) + D)
+    q = _q(len(lens), H * group, D, c.dtype, 18)
+    check(Q, c, table, ln, q, D ** -0.5, window=window, store=store, out="f16")
+    check(Q, c, table, ln, q, D ** -0.5, window=window, store=store, weights=True)
+    wide = torch.cat([table, torch.full((len(lens), 500), -3, dtype=torch.int32)], 1)
+    check(Q, c, wide, ln, q, D ** -0.5, window=window, store=store, out="f16")
+
+
 def test_far_pages(Q):
     """Element offsets past 2^31 (and byte offsets past 2^32): a pool of 4.3 GB a side whose last pages are used."""
     pages, page, H, D = 2 ** 15 + 4, 64, 8, 128
