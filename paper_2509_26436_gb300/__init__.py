@@ -26,7 +26,7 @@ __all__ = ["Params", "Encoded", "quantize", "encode_weights", "dequantize", "lin
            "linear_workspace_size", "empty_encoded", "device_status", "selftest_timeout",
            "kv_append", "attention_decode", "attention_workspace_size", "prepare_weights",
            "rope_frequencies", "rope", "PagedCache", "empty_paged_cache", "paged_append",
-           "attention_paged", "evict_select", "cache_compact",
+           "attention_paged", "attention_paged_workspace_size", "evict_select", "cache_compact",
            "SYMMETRIC", "ASYMMETRIC", "QuartzError"]
 
 
@@ -369,5 +369,5 @@ def attention_decode(q: Encoded, k_cache: Encoded, v_cache: Encoded, L_max: int,
 
 # --- paged key / value cache (no counterpart in the paper) -------------------
 
-from .paged import (PagedCache, attention_paged, attention_paged_workspace_size, cache_compact, empty_paged_cache, evict_select,  # noqa: E402
-                    paged_append, rope, rope_frequencies)  # noqa: E402
+from .paged import (PagedCache, attention_paged, attention_paged_workspace_size, cache_compact,  # noqa: E402
+                    empty_paged_cache, evict_select, paged_append, rope, rope_frequencies)

@@ -442,9 +442,9 @@ cudaError_t launch_paged_append(const quartz_paged_cache_t *c, const AppendArgs 
     const bool encoded = c->type == QUARTZ_PAGES_ENCODED;
     call.units = c->dim / unit_size(encoded);
     // Heads per thread: two where there are tokens for 1024 threads per SM, else
-    // as few as fit a CTA.  Places of several tokens keep a CTA's warps full.
+    // as few as fit a CTA.  Places of several tokens keep a CTA's warps full
+    // (a power of two of tokens times 4 to 32 units).
     const bool many = tokens * call.heads * c->dim >= int64_t(152) * 1024 * 2 * 16;
-    // (a power of two of tokens times 4 to 32 units)
     const bool both = many && (!a.rope.positions || (!a.rope.interleaved && a.rope.rotary == c->dim)) && (!encoded || c->dim % 128 == 0);
     if (both) call.units /= 2;
     int groups = many ? (call.heads + 1) / 2 : call.heads;
