@@ -59,13 +59,15 @@ struct Unit {
 #pragma unroll
         for (int i = 0; i < E / 2; ++i) w[i] = 0;
     }
+    __device__ __forceinline__ void load8(int i, const void *from)
+    {
+        const uint4 v = *static_cast<const uint4 *>(from);
+        w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+    }
     __device__ __forceinline__ void load(const void *from)
     {
 #pragma unroll
-        for (int i = 0; i < E / 8; ++i) {
-            const uint4 v = static_cast<const uint4 *>(from)[i];
-            w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
-        }
+        for (int i = 0; i < E / 8; ++i) load8(i, static_cast<const uint4 *>(from) + i);
     }
     __device__ __forceinline__ uint4 quad(int i) const { return make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]); }
     template <typename T>
@@ -93,7 +95,7 @@ __device__ __forceinline__ void rotate_both(int d0, const AngleTable<E> &cs, Uni
 
 // The E elements from d0 on of a key row, rotated, in the type of the row (one
 // rounding, as the rotation by itself gives).  Pairs of halves take their
-// partners from the row again: as vectors (p) where a unit lies in one half,
+// partners from the row again: as vectors of 8 (p) where those lie in one half,
 // else one by one.
 template <typename T, int E>
 __device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_rope_t &rope, const AngleTable<E> &cs,
@@ -112,16 +114,19 @@ __device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_r
                 y[e + 1] = rope_second(v, x1, x2);
             }
         }
-    } else if (pairs % E == 0) {
+    } else if (pairs % 8 == 0) {
         // one form for both halves: lanes of both share a warp
-        const bool second = d0 >= pairs;
-        const AngleTable<E> mn{cs.cs + (second ? kAngles : 0)};
-        const int i0 = second ? d0 - pairs : d0;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float mine = u.template get<T>(e), other = p.template get<T>(e);
-            const float2 v = mn.cs[e * AngleTable<E>::kStride + i0 / E];
-            y[e] = rope_first(v, second ? other : mine, second ? mine : other);
+        for (int g = 0; g < E; g += 8) {
+            const bool second = d0 + g >= pairs, turn = d0 + g < rope.rotary;
+            const int i0 = second ? d0 + g - pairs : d0 + g;
+            const float2 *mn = cs.cs + (second ? kAngles : 0) + (turn ? (i0 % E) * AngleTable<E>::kStride + i0 / E : 0);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float mine = u.template get<T>(g + e), other = p.template get<T>(g + e);
+                const float r = rope_first(mn[e * AngleTable<E>::kStride], second ? other : mine, second ? mine : other);
+                y[g + e] = turn ? r : mine;
+            }
         }
     } else {
 #pragma unroll 1
@@ -187,8 +192,7 @@ __global__ void __launch_bounds__(kAppendThreads, GS == 0 ? 6 : 4) paged_append_
     const AngleTable<E> cs{s_cs + n * per};
     const int64_t page = slot >> c.page_shift, in_page = slot - (page << c.page_shift);
     const bool turn = E * u < 2 * pairs;
-    const bool partners = turn && !c.a.rope.interleaved && pairs % E == 0;
-    const int partner = BOTH ? E * c.units : E * u < pairs ? pairs : -pairs;
+    const bool partners = turn && !c.a.rope.interleaved && pairs % 8 == 0;
     const T *k_row = static_cast<const T *>(c.a.k) + t * c.a.k_st + E * u, *v_row = static_cast<const T *>(c.a.v) + t * c.a.v_st + E * u;
     // encoded pages: unit of head 0; heads are page_size rows apart
     const int64_t unit0 = (((page * c.heads) << c.page_shift) + in_page) * (N * c.units) + u;
@@ -213,11 +217,18 @@ __global__ void __launch_bounds__(kAppendThreads, GS == 0 ? 6 : 4) paged_append_
         x[0].clear(), x[1].clear(), y[0].clear(), y[N - 1].clear();
         if (keys && in) {
             x[0].load(row);
-            if (BOTH || partners) x[1].load(row + partner);
+            if (BOTH) x[1].load(row + E * c.units);
+            if (!BOTH && partners) {
+#pragma unroll
+                for (int i = 0; i < E / 8; ++i) {
+                    const int d = E * u + 8 * i;
+                    if (d < 2 * pairs) x[1].load8(i, row + 8 * i + (d < pairs ? pairs : -pairs));
+                }
+            }
         }
         if (values && in) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) y[i].load(v_row + h * c.a.v_sh + i * partner);
+            for (int i = 0; i < N; ++i) y[i].load(v_row + h * c.a.v_sh + i * E * c.units);
         }
         if (keys) {
             if (in && BOTH && rope) rotate_both<T, E>(E * u, cs, x[0], x[1]);
@@ -441,21 +452,26 @@ cudaError_t launch_paged_append(const quartz_paged_cache_t *c, const AppendArgs 
     call.heads = c->heads;
     const bool encoded = c->type == QUARTZ_PAGES_ENCODED;
     call.units = c->dim / unit_size(encoded);
-    // Heads per thread: two where there are tokens for 1024 threads per SM, else
-    // as few as fit a CTA.  Places of several tokens keep a CTA's warps full
-    // (a power of two of tokens times 4 to 32 units).
-    const bool many = tokens * call.heads * c->dim >= int64_t(152) * 1024 * 2 * 16;
-    const bool both = many && (!a.rope.positions || (!a.rope.interleaved && a.rope.rotary == c->dim)) && (!encoded || c->dim % 128 == 0);
+    // By the elements per SM.  Few: keys and values by different CTAs, a token
+    // each.  2048: both by one, and BOTH, and several tokens where they leave four
+    // CTAs per SM (a power of two of them times 4 to 32 units keeps a CTA's warps
+    // full).  32768: a thread takes two heads.  In a graph, heads of 128, encoded /
+    // bf16: 16384 tokens of one head 11.6 / 9.1 us (39.7 / 28.3 as few), 4096 of 8
+    // 7.7 / 6.2 (13.4 / 12.3; with two CTAs per SM 8.5 / 6.2), 4096 of one 6.8 / 4.8
+    // (11.8 / 8.6, and the same from 4096 elements on), 256 of 8 3.1 / 2.9.
+    const int64_t per_sm = tokens * call.heads * c->dim / 152;
+    const bool some = per_sm >= 2048, many = per_sm >= 32768;
+    const bool both = some && (!a.rope.positions || (!a.rope.interleaved && a.rope.rotary == c->dim)) && (!encoded || c->dim % 128 == 0);
     if (both) call.units /= 2;
     int groups = many ? (call.heads + 1) / 2 : call.heads;
     if (groups > kAppendThreads / call.units) groups = kAppendThreads / call.units;
     int n = 1;
-    while (many && 2 * n <= kAppendTokens && 2 * n * call.units * groups <= kAppendThreads) n *= 2;
+    while (some && 2 * n <= kAppendTokens && 2 * n * call.units * groups <= kAppendThreads && tokens >= 2 * n * 608) n *= 2;
     call.tokens_here = n;
     call.groups = groups;
     call.each = (call.heads + groups - 1) / groups;
     const int threads = n * call.units * groups;  // a multiple of 4
-    const dim3 grid(static_cast<unsigned>((tokens + n - 1) / n), many ? 1 : 2), block((threads + 31) & ~31);
+    const dim3 grid(static_cast<unsigned>((tokens + n - 1) / n), some ? 1 : 2), block((threads + 31) & ~31);
     const int total = static_cast<int>(tokens);
     if (c->type == QUARTZ_PAGES_F16) return launch_append<__half, 0>(both, grid, block, s, call, total);
     if (c->type == QUARTZ_PAGES_BF16) return launch_append<__nv_bfloat16, 0>(both, grid, block, s, call, total);

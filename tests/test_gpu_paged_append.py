@@ -107,10 +107,10 @@ def test_encoded_pages(Q, gs, T, H, D, page, rope):
 @pytest.mark.parametrize("store", ["f16", "bf16", 8, 16, 32, 64])
 @pytest.mark.parametrize("H,D", [(17, 64), (16, 128), (3, 128), (5, 192), (7, 256)])
 @pytest.mark.parametrize("rotary,interleaved", [(0, False), (-1, False), (-1, True), (48, False)])
-def test_many_tokens(Q, store, H, D, rotary, interleaved):
+def test_many_tokens(Q, store, H, D, rotary, interleaved, T=None):
     """Enough tokens for every SM, where a thread takes units that are each other's partners and several tokens share a
     CTA; an odd number of tokens, some without a slot, keys inside a fused projection: the bits of rope() and quantize()."""
-    T, page = 152 * 1024 * 32 // (H * D) + 13, 16
+    T, page = T or 152 * 1024 * 32 // (H * D) + 13, 16
     total = (T + 40) // page + 1
     dtype = DTYPES.get(store, torch.float16)
     encoded = not isinstance(store, str)
@@ -137,6 +137,14 @@ def test_many_tokens(Q, store, H, D, rotary, interleaved):
     assert Q.device_status() == 0
     for got, exp in zip(ts, want):
         assert torch.equal(got, exp)
+
+
+@pytest.mark.parametrize("store", ["bf16", 16])
+@pytest.mark.parametrize("T,H,D", [(303, 8, 128), (305, 8, 128), (1217, 2, 128), (2433, 1, 256), (4871, 1, 64), (1300, 3, 192)])
+@pytest.mark.parametrize("rotary,interleaved", [(0, False), (-1, False), (-1, True), (16, False), (20, False)])
+def test_some_tokens(Q, store, T, H, D, rotary, interleaved):
+    """Both sides of the sizes from which on a CTA takes keys and values, and several tokens."""
+    test_many_tokens(Q, store, H, D, rotary, interleaved, T)
 
 
 def test_slot_out_of_range_is_reported_and_not_followed(Q):
