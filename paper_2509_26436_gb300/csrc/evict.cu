@@ -20,8 +20,6 @@
 namespace quartz {
 namespace {
 
-constexpr int kThreads = 1024;
-constexpr int kWarps = kThreads / 32;
 constexpr int kBuckets = 2048;
 
 struct SelectArgs {
@@ -42,10 +40,11 @@ __device__ __forceinline__ uint32_t order_key(float f)
     return (u & 0x80000000u) ? ~u : u | 0x80000000u;
 }
 
-template <bool HELD>
-__global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
+template <bool HELD, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 1024 ? 1 : 6) evict_select_kernel(SelectArgs a)
 {
     griddep_wait();
+    constexpr int kWarps = kThreads / 32;
     extern __shared__ uint32_t s_keys[];
     __shared__ uint32_t s_hist[kBuckets];
     __shared__ uint32_t s_above[kWarps], s_equal[kWarps];
@@ -89,8 +88,8 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
     bottom = __reduce_min_sync(0xffffffffu, bottom);
     if (lane == 0) s_above[warp] = top, s_equal[warp] = bottom;
     __syncthreads();
-    top = __reduce_max_sync(0xffffffffu, s_above[lane]);
-    bottom = __reduce_min_sync(0xffffffffu, s_equal[lane]);
+    top = __reduce_max_sync(0xffffffffu, s_above[lane % kWarps]);
+    bottom = __reduce_min_sync(0xffffffffu, s_equal[lane % kWarps]);
     auto key_at = [&](int t) { return HELD ? s_keys[t - lo] : order_key(w[t]); };
 
     // the want-th largest key is in [bottom, bottom + span]
@@ -105,9 +104,13 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
             if (off <= span) atomicAdd(&s_hist[off >> shift], 1u);
         }
         __syncthreads();
-        // two buckets per thread, from the top: how many keys lie above them
-        const uint32_t c0 = s_hist[kBuckets - 1 - 2 * tid], c1 = s_hist[kBuckets - 2 - 2 * tid];
-        uint32_t upto = c0 + c1;
+        // kEach buckets per thread, from the top: how many keys lie above them
+        constexpr int kEach = kBuckets / kThreads;
+        const int high = kBuckets - 1 - kEach * tid;
+        uint32_t c[kEach], mine = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) c[i] = s_hist[high - i], mine += c[i];
+        uint32_t upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
             const uint32_t v = __shfl_up_sync(0xffffffffu, upto, d);
@@ -115,18 +118,21 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
         }
         if (lane == 31) s_above[warp] = upto;
         __syncthreads();
-        uint32_t warps = s_above[lane];  // kWarps = 32
+        uint32_t warps = lane < kWarps ? s_above[lane] : 0u;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
             const uint32_t v = __shfl_up_sync(0xffffffffu, warps, d);
             if (lane >= d) warps += v;
         }
         upto += warp ? __shfl_sync(0xffffffffu, warps, (warp + 31) & 31) : 0u;
-        const uint32_t before = upto - c0 - c1;
+        uint32_t before = upto - mine;
         if (before < want && want <= upto) {  // one thread
-            const bool second = want > before + c0;
-            s_bucket = kBuckets - 1 - 2 * tid - second;
-            s_left = want - before - (second ? c0 : 0u);
+            int i = 0;
+#pragma unroll
+            for (int k = 0; k < kEach - 1; ++k)
+                if (i == k && want > before + c[k]) before += c[k], ++i;
+            s_bucket = high - i;
+            s_left = want - before;
         }
         __syncthreads();
         want = s_left;  // of those in the bucket
@@ -151,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
     if (lane == 0) s_above[warp] = above, s_equal[warp] = equal;
     __syncthreads();
     // kept and equal ones before this warp's run: lane i adds up the warps to i
-    uint32_t n_above = s_above[lane], n_equal = s_equal[lane];
+    uint32_t n_above = lane < kWarps ? s_above[lane] : 0u, n_equal = lane < kWarps ? s_equal[lane] : 0u;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
         const uint32_t x = __shfl_up_sync(0xffffffffu, n_above, d), y = __shfl_up_sync(0xffffffffu, n_equal, d);
@@ -176,6 +182,7 @@ __global__ void __launch_bounds__(kThreads, 1) evict_select_kernel(SelectArgs a)
 }
 
 constexpr int64_t kHeldKeys = 48 * 1024;  // 192 KB of the 227 a CTA may have
+constexpr int64_t kSmallKeys = 8 * 1024;
 
 }  // namespace
 
@@ -186,13 +193,21 @@ cudaError_t launch_evict_select(const float *w, int64_t w_sb, int64_t w_sh, cons
     SelectArgs a{w, w_sb, w_sh, lens, heads, static_cast<int32_t>(max_len), static_cast<int32_t>(budget),
                  static_cast<int32_t>(recent), static_cast<int32_t>(sinks), kept, new_lens, dev_err};
     const dim3 grid(static_cast<unsigned>(seqs * heads));
-    if (max_len <= kHeldKeys) {
-        const int bytes = static_cast<int>(max_len) * 4;
-        const cudaError_t e = allow_shared<evict_select_kernel<true>>(kHeldKeys * 4);
+    const int bytes = max_len <= kHeldKeys ? static_cast<int>(max_len) * 4 : 0;
+    // More CTAs than SMs, of keys that leave room for several: CTAs of 256 threads,
+    // up to six of which share an SM (64 x 32 heads of 4096 tokens: 40.8 us, 94.8
+    // with 1024 threads; 32 x 8 of 8192: 16.3, 18.3; of 16384: 28.4, 26.2).
+    if (grid.x > 152 && max_len <= kSmallKeys) {
+        const cudaError_t e = allow_shared<evict_select_kernel<true, 256>>(kSmallKeys * 4);
         if (e != cudaSuccess) return e;
-        return launch_pdl(evict_select_kernel<true>, grid, dim3(kThreads), bytes, s, a);
+        return launch_pdl(evict_select_kernel<true, 256>, grid, dim3(256), bytes, s, a);
     }
-    return launch_pdl(evict_select_kernel<false>, grid, dim3(kThreads), 0, s, a);
+    if (max_len <= kHeldKeys) {
+        const cudaError_t e = allow_shared<evict_select_kernel<true, 1024>>(kHeldKeys * 4);
+        if (e != cudaSuccess) return e;
+        return launch_pdl(evict_select_kernel<true, 1024>, grid, dim3(1024), bytes, s, a);
+    }
+    return launch_pdl(evict_select_kernel<false, 1024>, grid, dim3(1024), 0, s, a);
 }
 
 }  // namespace quartz

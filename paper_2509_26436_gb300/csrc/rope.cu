@@ -74,14 +74,15 @@ __global__ void __launch_bounds__(kThreads, 10) rope_kernel(RopeArgs a, int64_t 
         u = *reinterpret_cast<const Vec<T, V> *>(x + h0 * a.x_sh);
         if (turn) w = *reinterpret_cast<const Vec<T, V> *>(x + h0 * a.x_sh + gap);
     }
-    for (int i = threadIdx.x; i < here * V; i += kThreads) {
-        const int j = i / here;
-        const int64_t at = first_place + (i - j * here);
-        const int64_t token = token_of(at, inverse);
-        const int piece = static_cast<int>(at - token * pieces);
-        if (at < places && piece < turns) {
-            const float2 cs = rope_cos_sin(a.rope.positions[token], rope_unit(a.rope.freqs[piece * V + j]), a.rope.scale);
-            s_cs[i] = make_float2(cs.x, a.rope.backward ? -cs.y : cs.y);
+    // the CTA's tokens' pairs, those whose piece is among its places
+    const int64_t token0 = token_of(first_place, inverse), behind = min(first_place + here, places);
+    const int its = static_cast<int>(token_of(behind - 1, inverse) - token0) + 1;
+    for (int i = threadIdx.x; i < its * pairs; i += kThreads) {
+        const int k = i / pairs, j = i - k * pairs;
+        const int64_t at = (token0 + k) * pieces + j / V - first_place;
+        if (at >= 0 && at < behind - first_place) {
+            const float2 cs = rope_cos_sin(a.rope.positions[token0 + k], rope_unit(a.rope.freqs[j]), a.rope.scale);
+            s_cs[(j % V) * here + at] = make_float2(cs.x, a.rope.backward ? -cs.y : cs.y);
         }
     }
     __syncthreads();
