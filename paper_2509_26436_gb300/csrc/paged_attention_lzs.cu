@@ -23,7 +23,7 @@
 // takes 466 instructions of a warp, 172 of them logic and 152 of the half-rate
 // multiply-add pipe, which take two cycles of the scheduler each: 818 cycles, of
 // which unpacking is two fifths.  8 sequences of up to 65536 tokens, 64 / 8
-// heads, G_s = 16: 96.7 us, 50% of the copy rate (245 us with tiles in
+// heads, G_s = 16: 96.0 us, 51% of the copy rate (245 us with tiles in
 // registers, 125 with the query as the first operand of the keys' product, whose
 // duplicated rows had to be copied for every tile).
 #include <atomic>
