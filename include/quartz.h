@@ -462,7 +462,8 @@ int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_st
  * the lowest index; -0 equals 0; NaN counts below everything).
  *   weights   fp32 [seqs, heads, >= max_len] with strides, as above
  *   kept      int32 [seqs, heads, budget]: the kept indices, ascending, then -1
- *   new_lens  int32 [seqs]: min(len, budget)
+ *   new_lens  int32 [seqs]: min(len, budget); not the memory of seq_lens,
+ *             which quartz_cache_compact needs too
  * sinks, recent >= 0, 1 <= budget, sinks + recent <= budget, budget and max_len
  * <= 2^30, heads <= 1024, seqs <= 65535. */
 int32_t quartz_evict_select(const float *weights, int64_t weights_stride_seq, int64_t weights_stride_head,

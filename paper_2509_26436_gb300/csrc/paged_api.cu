@@ -172,6 +172,8 @@ int32_t quartz_evict_select(const float *weights, int64_t weights_stride_seq, in
     if ((reinterpret_cast<uintptr_t>(weights) | reinterpret_cast<uintptr_t>(seq_lens) | reinterpret_cast<uintptr_t>(kept) |
          reinterpret_cast<uintptr_t>(new_lens)) & 3)
         return QUARTZ_ERR_ALIGNMENT;
+    // every head's CTA reads its sequence's length, which the first head's replaces
+    if (new_lens < seq_lens + seqs && seq_lens < new_lens + seqs) return QUARTZ_ERR_INVALID_ARG;
     int *err = device_error_word();
     if (!err) return QUARTZ_ERR_CUDA;
     return map_cuda(launch_evict_select(weights, weights_stride_seq, weights_stride_head, seq_lens, seqs, heads, max_len,

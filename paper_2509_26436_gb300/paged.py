@@ -327,7 +327,8 @@ def evict_select(weights, seq_lens, budget: int, recent: int = 0, sinks: int = 0
     """(kept int32 [seqs, heads, budget], new_lens int32 [seqs]): the tokens
     that stay in each head's cache, ascending and then -1: all of them up to
     `budget`, else the first `sinks`, the last `recent` and the largest
-    weights between (ties: the lowest index; NaN is the smallest)."""
+    weights between (ties: the lowest index; NaN is the smallest).  `new_lens`
+    must not be seq_lens, which cache_compact needs too."""
     if torch is None:
         _bind()
     if not weights.is_cuda:
