@@ -38,7 +38,7 @@ constexpr int kPagedThreads = kPagedWarps * 32;
 constexpr int kPagedHeads = 8;  // query heads per CTA
 constexpr int kPagedCluster = 8;  // most splits joined within a cluster (the portable size)
 constexpr float kPagedLog2e = 1.4426950408889634f;
-constexpr float kPagedLow = -3e38f;  // a maximum before any score: finite, below the scores of a head that are
+constexpr float kPagedLow = -3.402823466e38f;  // a maximum before any score: finite, and no finite score is below it
 
 struct PagedSide {
     const uint8_t *data;  // 16-bit pages
