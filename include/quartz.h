@@ -487,9 +487,9 @@ int32_t quartz_cache_compact(const quartz_paged_cache_t *cache, int64_t seqs, co
 
 /* Synchronise `stream`, then read and clear the library's device error word.
  * Returns QUARTZ_OK, QUARTZ_ERR_TIMEOUT if a kernel gave up on a bounded
- * wait since the last call (its outputs are then invalid), QUARTZ_ERR_INDEX
- * if one met an index out of range (paged cache), or QUARTZ_ERR_CUDA if the
- * stream reports an error. */
+ * wait since the last call (its outputs are then invalid), else
+ * QUARTZ_ERR_INDEX if one met an index out of range (paged cache), or
+ * QUARTZ_ERR_CUDA if the stream reports an error. */
 int32_t quartz_device_status(void *stream);
 
 /* Failure-detection self-test: launches one CTA that waits on an mbarrier

@@ -387,7 +387,7 @@ int32_t quartz_device_status(void *stream)
     const int zero = 0;
     if (cudaMemcpy(&v, p, sizeof(int), cudaMemcpyDeviceToHost) != cudaSuccess) return QUARTZ_ERR_CUDA;
     if (cudaMemcpy(p, &zero, sizeof(int), cudaMemcpyHostToDevice) != cudaSuccess) return QUARTZ_ERR_CUDA;
-    return v == QUARTZ_DEV_TIMEOUT ? QUARTZ_ERR_TIMEOUT : v == QUARTZ_DEV_INDEX ? QUARTZ_ERR_INDEX : QUARTZ_OK;
+    return device_word_status(v);
 }
 
 int32_t quartz_selftest_timeout(int64_t limit_ns, void *stream)

@@ -58,7 +58,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 1024 ? 1 : 6) evict_sele
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int len = a.lens[b];
     if (len < 0 || len > a.max_len) {
-        if (tid == 0) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
+        if (tid == 0) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
         len = len < 0 ? 0 : a.max_len;
     }
     int32_t *kept = a.kept + bh * a.budget;

@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kAppendThreads, GS == 0 ? 6 : 4) paged_append_
     const int t = first + n;
     int64_t slot = t < tokens && group < c.groups ? c.a.slots[t] : -1;
     if (slot >= c.slots_total) {
-        atomicExch(c.a.dev_err, QUARTZ_DEV_INDEX);
+        atomicOr(c.a.dev_err, QUARTZ_DEV_INDEX);
         slot = -1;
     }
     const AngleTable<E> cs{s_cs + n * per};
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
     const int h = static_cast<int>(bh - b * m.heads);
     int64_t len = m.c.lens[b];
     if (len < 0 || len > m.c.max_len) {
-        if (threadIdx.x == 0) atomicExch(m.c.dev_err, QUARTZ_DEV_INDEX);
+        if (threadIdx.x == 0) atomicOr(m.c.dev_err, QUARTZ_DEV_INDEX);
         len = len < 0 ? 0 : m.c.max_len;
     }
     const int64_t rows = len < m.c.budget ? len : m.c.budget;
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(kMoveThreads) cache_compact_kernel(MoveCall m)
             if (row[r] < n && s_to[buffer][row[r]]) store_piece(s_to[buffer][row[r]] + at[r], v[r], p.piece);
         __syncthreads();
     }
-    if (bad) atomicExch(m.c.dev_err, QUARTZ_DEV_INDEX);
+    if (bad) atomicOr(m.c.dev_err, QUARTZ_DEV_INDEX);
 }
 
 int piece_of(int64_t row_bytes)

@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
     }
     paged_wait<0>();
     __syncwarp();
-    if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
+    if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
     paged_finish<D, false, SHARE>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, kUp);
 }
 

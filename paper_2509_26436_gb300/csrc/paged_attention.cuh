@@ -83,7 +83,7 @@ __device__ __forceinline__ PagedRange paged_range(const int32_t *lens, int b, in
 {
     int len = lens[b];
     if (len < 0 || len > max_len) {
-        if (threadIdx.x == 0) atomicExch(dev_err, QUARTZ_DEV_INDEX);
+        if (threadIdx.x == 0) atomicOr(dev_err, QUARTZ_DEV_INDEX);
         len = len < 0 ? 0 : max_len;
     }
     PagedRange r;

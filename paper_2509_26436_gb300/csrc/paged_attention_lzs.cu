@@ -481,7 +481,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     }
     paged_wait<0>();
     __syncwarp();
-    if (bad) atomicExch(a.dev_err, QUARTZ_DEV_INDEX);
+    if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
     paged_finish<D, true, SHARE>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, 0.f);
 }
 

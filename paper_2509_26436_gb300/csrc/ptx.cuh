@@ -114,7 +114,7 @@ __device__ __forceinline__ bool mbar_wait_bounded(uint32_t bar, uint32_t parity,
         if (*abort_flag) return false;
         if (global_timer_ns() - t0 > limit_ns) {
             *abort_flag = 1;
-            atomicExch(dev_err, QUARTZ_DEV_TIMEOUT);
+            atomicOr(dev_err, QUARTZ_DEV_TIMEOUT);
             return false;
         }
     }
@@ -132,7 +132,7 @@ __device__ __forceinline__ bool mbar_wait_warp_slow(uint32_t bar, uint32_t parit
         if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
         if (__any_sync(0xffffffffu, global_timer_ns() - t0 > limit_ns)) {
             *abort_flag = 1;
-            atomicExch(dev_err, QUARTZ_DEV_TIMEOUT);
+            atomicOr(dev_err, QUARTZ_DEV_TIMEOUT);
             return false;
         }
     }

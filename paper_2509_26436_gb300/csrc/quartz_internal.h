@@ -10,10 +10,18 @@
 
 namespace quartz {
 
-// Values of the library's device error word (0 = no error).
+// Bits of the library's device error word (0 = no error); kernels add theirs
+// with atomicOr, so that one kind of error does not hide the other.
 constexpr int QUARTZ_DEV_OK = 0;
 constexpr int QUARTZ_DEV_TIMEOUT = 1;
 constexpr int QUARTZ_DEV_INDEX = 2;  // a page, slot, length or kept index out of range
+
+// The word's status.  An expired wait comes first: what it leaves invalid is a
+// whole result, of any kernel.
+constexpr int32_t device_word_status(int word)
+{
+    return word & QUARTZ_DEV_TIMEOUT ? QUARTZ_ERR_TIMEOUT : word & QUARTZ_DEV_INDEX ? QUARTZ_ERR_INDEX : QUARTZ_OK;
+}
 
 // Upper bound on any single mbarrier wait inside a kernel.  No legitimate
 // wait on a healthy GPU comes near it; it only turns a would-be hang into an
