@@ -2,7 +2,9 @@
 of one new token per sequence, and eviction by accumulated attention weight.
 
 As the rest of the package this only marshals torch CUDA tensors into the C
-ABI; every call is asynchronous on the current stream (or `stream`).
+ABI; every call is asynchronous on the current stream (or `stream`).  Autograd
+sees none of it: rope(), which training needs too, refuses a tensor whose
+gradient would be lost; the others are steps of serving.
 
     freqs, scale = rope_frequencies(128, base=500000.0, device="cuda")
     cache = empty_paged_cache(num_pages, 64, heads=8, dim=128, params=Params(group_s=16))
@@ -133,9 +135,15 @@ def rope(x, positions, freqs, interleaved: bool = False, scale: float = 1.0, bac
     head turned by positions[t] * freqs: pairs (i, i + len(freqs)), or
     (2 i, 2 i + 1) with `interleaved`; the rest is copied.  `backward` applies
     the transpose: the gradient of x from that of the result.  `out` may be x
-    itself (in place), or must not overlap it."""
+    itself (in place), or must not overlap it.  Nothing is recorded for
+    autograd: where gradients are enabled, an x or `out` that requires one is
+    refused (call it from an autograd function's forward and, with `backward`,
+    from its backward)."""
     if torch is None:
         _bind()
+    if (x.requires_grad or (out is not None and out.requires_grad)) and torch.is_grad_enabled():
+        raise ValueError("rope records no gradient: use torch.no_grad(), or an autograd function whose backward calls "
+                         "rope(..., backward=True)")
     dtype = x.dtype
     kind = _KIND.get(dtype)
     if kind is None or not x.is_cuda:
