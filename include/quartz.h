@@ -394,9 +394,10 @@ typedef struct {
  * positions[t] * freqs[i] radians,
  *   y1 = scale (x1 cos - x2 sin),  y2 = scale (x1 sin + x2 cos),
  * (x1, x2) = elements (i, i + rotary/2), or (2i, 2i + 1) with `interleaved`.
- * The angle is reduced exactly (positions times freqs / 2 pi as a 64-bit
- * fraction of a turn), so far positions lose nothing.  `backward` applies the
- * transpose, which is the gradient with respect to x. */
+ * The angle is kept as a 64-bit fraction of a turn, off by at most |positions|
+ * (2^-63 |freqs| / 2 pi + 2^-64) turns: up to position 2^35 less than binary32
+ * resolves.  `backward` applies the transpose, which is the gradient with
+ * respect to x. */
 typedef struct {
     const int64_t *positions;  /* device, one per token */
     const double *freqs;       /* device, [rotary / 2], radians per position, finite */

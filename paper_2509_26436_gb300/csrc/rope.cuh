@@ -29,8 +29,10 @@ __device__ __forceinline__ uint64_t rope_unit(double freq)
     return bits >> 63 ? 0 - u : u;
 }
 
-// (scale cos, scale sin) of position times unit.  The product modulo 2^64 is
-// the angle's fraction of a turn without rounding.  Whole quarter turns are
+// (scale cos, scale sin) of position times unit.  The product modulo 2^64 loses
+// nothing: the angle is off by the unit's own error, |position| times at most
+// 2^-63 of the frequency and 2^-64 turns (2^-28, what binary32 holds of an
+// eighth of a turn, from position 2^35 on).  Whole quarter turns are
 // taken off as integers, so that the binary32 argument of sine and cosine has
 // 24 good bits of at most an eighth of a turn.  A product in binary32 would be
 // off by 2^-24 of the angle itself: 0.008 radians at position 131072.
