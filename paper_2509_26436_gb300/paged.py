@@ -191,10 +191,11 @@ class PagedCache:
                     k.rows % (heads * page_size):
                 raise ValueError("encoded pages need `heads`, and k and v of pages * heads * page_size equal rows")
             for e in (k, v):
-                sizes = [(e.codes, e.rows * (e.K // 2)), (e.scales, e.rows * (e.K // 64)),
-                         (e.flags, e.rows * (e.K // e.params.group_s))]
-                if any(not (t.is_cuda and t.is_contiguous() and t.numel() >= n) for t, n in sizes):
-                    raise ValueError("encoded pages must be contiguous CUDA tensors of their full size")
+                sizes = [(e.codes, 1, e.rows * (e.K // 2)), (e.scales, 2, e.rows * (e.K // 64)),
+                         (e.flags, 1, e.rows * (e.K // e.params.group_s))]
+                if any(not (t.is_cuda and t.device == k.codes.device and t.is_contiguous() and t.element_size() == width and
+                            t.numel() >= n) for t, width, n in sizes):
+                    raise ValueError("encoded pages must be contiguous CUDA tensors of one device, of their type and full size")
             self.heads, self.dim, self.num_pages = heads, k.K, k.rows // (heads * page_size)
             self.dtype, self.device = f16, k.codes.device
             sides = [N.QuartzPages(None, 0, 0, 0, e.c()) for e in (k, v)]
@@ -204,6 +205,8 @@ class PagedCache:
                 if not (t.is_cuda and t.dim() == 4 and t.dtype in (f16, bf16) and t.stride(3) == 1):
                     raise ValueError(f"{name} must be a [pages, page_size, heads, dim] float16 or bfloat16 CUDA tensor "
                                      "with a contiguous last dimension")
+            if k.device != v.device:
+                raise ValueError("k and v are on different devices")
             if k.shape != v.shape or k.dtype != v.dtype or k.shape[1] != page_size or heads not in (None, k.shape[2]):
                 raise ValueError("k and v must agree in shape and type, and have page_size slots and `heads` heads")
             self.num_pages, _, self.heads, self.dim = k.shape
