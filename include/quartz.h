@@ -432,7 +432,8 @@ int32_t quartz_paged_append(const quartz_paged_cache_t *cache, const void *k, in
  *   window) <= t < len (window 0: all),  o = sum_t p_t v_t
  * for each of q_heads query heads; query head h reads key / value head
  * h / (q_heads / heads).  An empty sequence gives zeros.  q . k_t and s_t log2 e
- * have to be finite in binary32.  Products, softmax and sums in binary32; the
+ * have to be finite in binary32, and so has scale log2 e (QUARTZ_ERR_INVALID_ARG).
+ * Products, softmax and sums in binary32; the
  * weights p enter the value product as a sum of two 16-bit parts (bf16 and
  * encoded pages with binary32 results: three).
  *   q            [seqs, q_heads, dim], strides in elements (multiples of 8),

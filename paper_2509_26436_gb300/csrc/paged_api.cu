@@ -12,6 +12,7 @@ bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 int32_t map_cuda(cudaError_t e) { return e == cudaSuccess ? QUARTZ_OK : QUARTZ_ERR_CUDA; }
 
+constexpr float kLog2e = 1.4426950408889634f;
 constexpr int64_t kMaxLen = int64_t(1) << 30;
 constexpr int64_t kMaxRowStride = int64_t(1) << 40;  // of tables, weights, q, k, v, x, y: products stay below 2^63
 
@@ -140,7 +141,8 @@ int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_st
 {
     const int32_t rc = check_attention(cache, seqs, q_heads, max_len, window);
     if (rc) return rc;
-    if (!type_ok(o_type) || !std::isfinite(scale)) return QUARTZ_ERR_INVALID_ARG;
+    // the kernels multiply by scale log2 e
+    if (!type_ok(o_type) || !std::isfinite(scale * kLog2e)) return QUARTZ_ERR_INVALID_ARG;
     if (!stride_ok(q_stride_seq, 1) || !stride_ok(q_stride_head, 1) || !stride_ok(table_stride, 1) ||
         (weights && (!stride_ok(weights_stride_seq, 1) || !stride_ok(weights_stride_head, 1))))
         return QUARTZ_ERR_INVALID_ARG;
