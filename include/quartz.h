@@ -433,9 +433,13 @@ int32_t quartz_paged_append(const quartz_paged_cache_t *cache, const void *k, in
  * for each of q_heads query heads; query head h reads key / value head
  * h / (q_heads / heads).  An empty sequence gives zeros.  q . k_t and s_t log2 e
  * have to be finite in binary32, and so has scale log2 e (QUARTZ_ERR_INVALID_ARG).
- * Products, softmax and sums in binary32; the
- * weights p enter the value product as a sum of two 16-bit parts (bf16 and
- * encoded pages with binary32 results: three).
+ * A query head with others makes its own row of o NaN; an element of an attended
+ * value row that is infinite or NaN makes that element of o infinite or NaN
+ * (encoded pages: such a scale, its group of 64), whatever its weight.  What is
+ * not attended is not looked at.
+ * Products, softmax and sums in binary32; the weights p enter the value product
+ * as a sum of two 16-bit parts (bf16 and encoded pages with binary32 results:
+ * three).
  *   q            [seqs, q_heads, dim], strides in elements (multiples of 8),
  *                16-byte aligned, the pages' type (fp16 for encoded pages)
  *   block_table  int32 [seqs, >= ceil(max_len / page_size)], row stride
