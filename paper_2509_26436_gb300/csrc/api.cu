@@ -66,6 +66,18 @@ int32_t map_cuda(cudaError_t e) { return e == cudaSuccess ? QUARTZ_OK : QUARTZ_E
 
 }  // namespace
 
+int device_sms_or_zero()
+{
+    static std::atomic<int> cached[kMaxDevices];  // 0: not looked up yet
+    int dev = 0, n = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+    const bool slot = dev >= 0 && dev < kMaxDevices;
+    if (slot && (n = cached[dev].load(std::memory_order_relaxed)) > 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 0;
+    if (slot) cached[dev].store(n, std::memory_order_relaxed);
+    return n;
+}
+
 int *device_error_word()
 {
     int dev = 0;

@@ -200,7 +200,7 @@ cudaError_t launch_evict_select(const float *w, int64_t w_sb, int64_t w_sh, cons
     // More CTAs than SMs, of keys that leave room for several: CTAs of 256 threads,
     // up to six of which share an SM (64 x 32 heads of 4096 tokens: 40.8 us, 94.8
     // with 1024 threads; 32 x 8 of 8192: 16.3, 18.3; of 16384: 28.4, 26.2).
-    if (grid.x > 152 && max_len <= kSmallKeys) {
+    if (grid.x > static_cast<unsigned>(device_sms()) && max_len <= kSmallKeys) {
         const cudaError_t e = allow_shared<evict_select_kernel<true, 256>>(kSmallKeys * 4);
         if (e != cudaSuccess) return e;
         return launch_pdl(evict_select_kernel<true, 256>, grid, dim3(256), bytes, s, a);

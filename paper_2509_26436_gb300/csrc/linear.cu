@@ -1499,20 +1499,6 @@ bool make_output_map(CUtensorMap *m, void *y, int64_t M, int64_t N)
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// SM count of the current device (0 if there is none), looked up once per device.
-int device_sms_or_zero()
-{
-    constexpr int kMaxDevices = 64;
-    static std::atomic<int> cached[kMaxDevices];  // 0: not looked up yet
-    int dev = 0, n = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return 0;
-    const bool slot = dev >= 0 && dev < kMaxDevices;
-    if (slot && (n = cached[dev].load(std::memory_order_relaxed)) > 0) return n;
-    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 0;
-    if (slot) cached[dev].store(n, std::memory_order_relaxed);
-    return n;
-}
-
 int num_sms()
 {
     const int n = device_sms_or_zero();

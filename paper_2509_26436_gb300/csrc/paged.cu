@@ -459,14 +459,15 @@ cudaError_t launch_paged_append(const quartz_paged_cache_t *c, const AppendArgs 
     // bf16: 16384 tokens of one head 11.6 / 9.1 us (39.7 / 28.3 as few), 4096 of 8
     // 7.7 / 6.2 (13.4 / 12.3; with two CTAs per SM 8.5 / 6.2), 4096 of one 6.8 / 4.8
     // (11.8 / 8.6, and the same from 4096 elements on), 256 of 8 3.1 / 2.9.
-    const int64_t per_sm = tokens * call.heads * c->dim / 152;
+    const int sms = device_sms();
+    const int64_t per_sm = tokens * call.heads * c->dim / sms;
     const bool some = per_sm >= 2048, many = per_sm >= 32768;
     const bool both = some && (!a.rope.positions || (!a.rope.interleaved && a.rope.rotary == c->dim)) && (!encoded || c->dim % 128 == 0);
     if (both) call.units /= 2;
     int groups = many ? (call.heads + 1) / 2 : call.heads;
     if (groups > kAppendThreads / call.units) groups = kAppendThreads / call.units;
     int n = 1;
-    while (some && 2 * n <= kAppendTokens && 2 * n * call.units * groups <= kAppendThreads && tokens >= 2 * n * 608) n *= 2;
+    while (some && 2 * n <= kAppendTokens && 2 * n * call.units * groups <= kAppendThreads && tokens >= 2 * n * 4 * sms) n *= 2;
     call.tokens_here = n;
     call.groups = groups;
     call.each = (call.heads + groups - 1) / groups;
@@ -492,7 +493,7 @@ cudaError_t launch_cache_compact(const quartz_paged_cache_t *c, const CompactCal
     m.num_pages = c->num_pages;
     m.in_place = a.new_table == nullptr;
     m.planes = 0;
-    const int64_t bh = a.seqs * c->heads;
+    const int64_t bh = a.seqs * c->heads, sms = device_sms();
     const quartz_pages_t *side[2] = {&c->k, &c->v};
     auto add = [&](void *base, int64_t row_bytes, int64_t sp, int64_t ss, int64_t sh) {
         Plane &p = m.plane[m.planes++];
@@ -504,7 +505,7 @@ cudaError_t launch_cache_compact(const quartz_paged_cache_t *c, const CompactCal
         // in place, slices of a row (of 64 bytes or more) are what there is to
         // spread over the SMs beside sequences and heads
         if (m.in_place)
-            while (bh * 2 * p.slices < 304 && p.pieces % 2 == 0 && p.pieces * p.piece > 64) p.pieces /= 2, p.slices *= 2;
+            while (bh * 2 * p.slices < 2 * sms && p.pieces % 2 == 0 && p.pieces * p.piece > 64) p.pieces /= 2, p.slices *= 2;
     };
     for (int i = 0; i < 2; ++i) {
         if (c->type == QUARTZ_PAGES_ENCODED) {
@@ -523,7 +524,7 @@ cudaError_t launch_cache_compact(const quartz_paged_cache_t *c, const CompactCal
     } else {
         const int64_t rows = a.budget < a.max_len ? a.budget : a.max_len;
         const int64_t tile = kMoveThreads * kMovePieces * 16 / (2 * c->dim), most = (rows + tile - 1) / tile;
-        int64_t want = (152 * 8 + bh * 2 - 1) / (bh * 2);
+        int64_t want = (8 * sms + bh * 2 - 1) / (bh * 2);
         if (want > most) want = most;
         m.parts = want < 1 ? 1 : static_cast<int>(want);
     }

@@ -394,11 +394,7 @@ PagedPlan paged_plan(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, i
     const int64_t ctas = (seqs > 0 ? seqs : 1) * c->heads * ((group + kPagedHeads - 1) / kPagedHeads);
     const int occ = c->type == QUARTZ_PAGES_ENCODED ? paged_kernel_occupancy_encoded(c->dim, c->k.enc.p.group_s)
                                                     : paged_kernel_occupancy_16bit(c->type, c->dim);
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-        sms <= 0)
-        sms = 152;
-    const int64_t slots = static_cast<int64_t>(sms) * occ;
+    const int64_t slots = static_cast<int64_t>(device_sms()) * occ;
     int64_t n = ctas < 2 * slots ? (4 * slots + ctas - 1) / ctas : 1;
     const int64_t most = (p.tokens + 255) / 256, by_length = (p.tokens + 1023) / 1024, full = 16 * slots / ctas;
     if (n < by_length && n < full) n = by_length < full ? by_length : full;

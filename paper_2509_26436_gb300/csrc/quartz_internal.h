@@ -31,6 +31,17 @@ constexpr uint64_t kWaitLimitNs = 2000000000ull;
 // Device error word of the current device (see api.cu).
 int *device_error_word();
 
+// SM count of the current device (0 if there is none), looked up once per device.
+int device_sms_or_zero();
+
+// The count that plans go by: without a device (sizes asked on a host) that of
+// the whole chip.
+inline int device_sms()
+{
+    const int n = device_sms_or_zero();
+    return n > 0 ? n : 152;
+}
+
 #ifdef __CUDACC__
 // Let launches of Kernel on the current device have up to `bytes` of dynamic
 // shared memory (always the same number): once per device, since the call costs

@@ -127,8 +127,9 @@ cudaError_t launch_v(const RopeArgs &a, int64_t tokens, cudaStream_t s)
     const uint64_t inverse = pieces > 1 ? ~uint64_t(0) / pieces + 1 : 0;
     // More groups of heads per CTA while there are fewer than 2048 threads per SM
     // (8192 x 32 x 128: 23.7 us; up to 1024 25.6, up to 4096 24.5)
+    const int64_t threads = int64_t(device_sms()) * 2048;
     int groups = 1;
-    while (groups < 32 && groups < a.heads && places * groups < 152 * 2048) groups *= 2;
+    while (groups < 32 && groups < a.heads && places * groups < threads) groups *= 2;
     const int here = kThreads / groups, each = (a.heads + groups - 1) / groups;
     return launch_pdl(rope_kernel<T, V>, dim3(static_cast<unsigned>((places + here - 1) / here)), dim3(kThreads), 0, s, a, places,
                       inverse, here, each);
