@@ -133,7 +133,7 @@ __device__ __forceinline__ float2 load_scales2(const __half *scales, Row row)
 // `biased_bytes` into byte 0, 0x4B above it: 0x4B0000xx = 2^23 + xx).
 __device__ __forceinline__ float magic_float(uint32_t biased_bytes, uint32_t sel)
 {
-    return __int_as_float(prmt_b32(biased_bytes, 0x4B000000u, sel));
+    return __int_as_float(prmt(biased_bytes, 0x4B000000u, sel));
 }
 
 __device__ __forceinline__ uint4 lds_u4(uint32_t addr)
@@ -169,34 +169,10 @@ __device__ __forceinline__ void fma_codes2(float &acc0, float &acc1, float p, fl
         : "f"(f0), "f"(f1), "f"(p), "f"(-8388616.0f), "f"(-8388736.0f));
 }
 
-// Asynchronous 16-byte global -> shared copies (cp.async, completion tracked
-// per thread in commit groups; the wait is the hardware's own).
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-
 // Shared-memory offset of 16-byte chunk c (0..3) of token row r in a code
 // tile: rows of 64 bytes, chunks XOR-swizzled by (r / 2) % 4 so that eight
 // consecutive rows reading the same chunk hit eight different bank groups.
 __device__ __forceinline__ uint32_t tile_off(int r, int c) { return r * 64 + ((c ^ ((r >> 1) & 3)) << 4); }
-
-// Cluster barrier (all threads of all CTAs; the hardware's own wait) and
-// reads of another CTA's shared memory.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ uint32_t mapa(uint32_t addr, int rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
 
 __device__ __forceinline__ void store_out(void *out, int type, int64_t i, float v)
 {

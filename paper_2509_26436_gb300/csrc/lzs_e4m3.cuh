@@ -4,26 +4,19 @@
 #pragma once
 #include <cstdint>
 
-namespace quartz {
+#include "ptx.cuh"
 
-// Byte permute (PTX prmt, default mode: a selector nibble b < 8 copies byte b
-// of {hi:lo}, b + 8 replicates that byte's sign bit).
-__device__ __forceinline__ uint32_t prmt_b32(uint32_t lo, uint32_t hi, uint32_t sel)
-{
-    uint32_t d;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(lo), "r"(hi), "r"(sel));
-    return d;
-}
+namespace quartz {
 
 // Four table lookups at once: byte k of x (0..15) selects byte x_k of the
 // 16-byte table {t0, t1, t2, t3}.
 __device__ __forceinline__ uint32_t lut16(uint32_t x, uint32_t t0, uint32_t t1, uint32_t t2, uint32_t t3)
 {
     const uint32_t y = x & 0x07070707u;
-    const uint32_t sel = prmt_b32(y | (y >> 4), 0u, 0x0020u);  // nibble k = low 3 bits of byte k
-    const uint32_t lo = prmt_b32(t0, t1, sel);
-    const uint32_t hi = prmt_b32(t2, t3, sel);
-    const uint32_t use_hi = prmt_b32(x << 4, 0u, 0xBA98u);      // 0xFF where bit 3 of byte k is set
+    const uint32_t sel = prmt(y | (y >> 4), 0u, 0x0020u);  // nibble k = low 3 bits of byte k
+    const uint32_t lo = prmt(t0, t1, sel);
+    const uint32_t hi = prmt(t2, t3, sel);
+    const uint32_t use_hi = prmt(x << 4, 0u, 0xBA98u);      // 0xFF where bit 3 of byte k is set
     return (hi & use_hi) | (lo & ~use_hi);
 }
 
@@ -43,8 +36,8 @@ __device__ __forceinline__ void e4m3_from_codes8(uint32_t word, int flag, uint32
     const uint32_t t3 = 0xB8C0C4C8u + add;                  // -4, -3, -2, -1
     const uint32_t ev = lut16(word & 0x0F0F0F0Fu, t0, t1, t2, t3);         // codes 0, 2, 4, 6
     const uint32_t od = lut16((word >> 4) & 0x0F0F0F0Fu, t0, t1, t2, t3);  // codes 1, 3, 5, 7
-    lo = prmt_b32(ev, od, 0x5140u);
-    hi = prmt_b32(ev, od, 0x7362u);
+    lo = prmt(ev, od, 0x5140u);
+    hi = prmt(ev, od, 0x7362u);
 }
 
 // The same for codes with FLAGs up to 12 (16-bit stage-1 codes, Section 5
@@ -63,8 +56,8 @@ __device__ __forceinline__ void e5m2_from_codes8(uint32_t word, int flag, uint32
     const uint32_t t3 = 0xBCC0C2C4u + add;                  // -4, -3, -2, -1
     const uint32_t ev = lut16(word & 0x0F0F0F0Fu, t0, t1, t2, t3);
     const uint32_t od = lut16((word >> 4) & 0x0F0F0F0Fu, t0, t1, t2, t3);
-    lo = prmt_b32(ev, od, 0x5140u);
-    hi = prmt_b32(ev, od, 0x7362u);
+    lo = prmt(ev, od, 0x5140u);
+    hi = prmt(ev, od, 0x7362u);
 }
 
 // FLAG of subgroup k (global index over the flattened [rows, K/G_s] array):

@@ -6,6 +6,8 @@
 #include <cstdint>
 #include <cuda_fp16.h>
 
+#include "ptx.cuh"
+
 namespace quartz {
 
 __device__ __forceinline__ uint4 ldg_stream(const uint4 *p)
@@ -34,13 +36,6 @@ __device__ __forceinline__ float2 mul2_rn(float2 a, float2 b)
         "mov.b64 {%0, %1}, d;\n\t}"
         : "=f"(d.x), "=f"(d.y)
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
-    return d;
-}
-
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
-{
-    uint32_t d;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
     return d;
 }
 

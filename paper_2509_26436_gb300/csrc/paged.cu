@@ -250,13 +250,6 @@ cudaError_t launch_append(bool both, dim3 grid, dim3 block, cudaStream_t s, cons
                 : launch_pdl(paged_append_kernel<T, GS, false>, grid, block, 0, s, c, tokens);
 }
 
-int log2_of(int v)
-{
-    int n = 0;
-    while ((1 << n) < v) ++n;
-    return n;
-}
-
 // ---------------------------------------------------------------------------
 // Closing up
 // ---------------------------------------------------------------------------

@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
     const int end = range.base + min(begin + chunk, range.count());  // first token behind the split
     const int base0 = range.base + begin + warp * 16;
     const int tiles = base0 < end ? (end - base0 + kPagedWarps * 16 - 1) / (kPagedWarps * 16) : 0;
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + warp * kWarpBytes;
+    const uint32_t ring = smem_u32(s_ring) + warp * kWarpBytes;
 
     // --- copies of a tile: a lane takes chunks lane + 32 k.  Tokens that are not
     // seen repeat the nearest that is: nothing of theirs, which may be infinite
@@ -81,15 +81,15 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
             const int i = lane + 32 * k, t = i / Tile::kChunks, c = i % Tile::kChunks;
             const uint64_t page = __shfl_sync(0xffffffffu, pages, t);
             const uint64_t slot = static_cast<uint32_t>(seen(base + t)) & page_mask;
-            paged_copy16(to + Tile::at(t, c), kbase + (page * a.k.stride_page + slot * a.k.stride_slot) + c * 8);
-            paged_copy16(to + Tile::kSide + Tile::at(t, c), vbase + (page * a.v.stride_page + slot * a.v.stride_slot) + c * 8);
+            cp_async16(to + Tile::at(t, c), kbase + (page * a.k.stride_page + slot * a.k.stride_slot) + c * 8);
+            cp_async16(to + Tile::kSide + Tile::at(t, c), vbase + (page * a.v.stride_page + slot * a.v.stride_slot) + c * 8);
         }
     };
     uint32_t next_pages = 0;  // of the next tile to fetch
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) {
         if (s < tiles) fetch(base0 + s * kPagedWarps * 16, pages_of(base0 + s * kPagedWarps * 16), s);
-        paged_commit();
+        cp_async_commit();
     }
     if (kStages - 1 < tiles) next_pages = pages_of(base0 + (kStages - 1) * kPagedWarps * 16);
 
@@ -122,7 +122,7 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
     int stage = 0;
     for (int it = 0; it < tiles; ++it) {
         const int base = base0 + it * kPagedWarps * 16;
-        paged_wait<kStages - 2>();
+        cp_async_wait<kStages - 2>();
         __syncwarp();
         {
             const int ahead = it + kStages - 1;
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
                 fetch(base0 + ahead * kPagedWarps * 16, next_pages, stage == 0 ? kStages - 1 : stage - 1);
                 if (ahead + 1 < tiles) next_pages = pages_of(base0 + (ahead + 1) * kPagedWarps * 16);
             }
-            paged_commit();
+            cp_async_commit();
         }
         const uint32_t tile = ring + stage * Tile::kBytes;
         stage = stage == kStages - 1 ? 0 : stage + 1;
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kPagedThreads, Tile16<D>::kCtas) paged_attn_ke
             }
         }
     }
-    paged_wait<0>();
+    cp_async_wait<0>();
     __syncwarp();
     if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
     paged_finish<D, false, SHARE>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, kUp);
@@ -356,13 +356,6 @@ __global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(PagedArgs a, f
         for (int i = 0; i < 4; ++i)
             if (t + i < range.count() && range.base + t + i >= range.first) w[t + i] += p[i];
     }
-}
-
-int log2_of(int v)
-{
-    int n = 0;
-    while ((1 << n) < v) ++n;
-    return n;
 }
 
 // Splits per sequence and tokens per split (a multiple of one tile of each of

@@ -29,6 +29,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "ptx.cuh"
 #include "quartz_internal.h"
 
 namespace quartz {
@@ -153,13 +154,6 @@ __device__ __forceinline__ float ex2(float x)
     return y;
 }
 
-__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel)
-{
-    uint32_t d;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(sel));
-    return d;
-}
-
 // d += A B, 16 x 8 x 16.
 template <bool BF>
 __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -202,15 +196,6 @@ __device__ __forceinline__ uint32_t bf16_pair(float p0, float p1)
     const __nv_bfloat162 h = __floats2bfloat162_rn(p0, p1);
     return *reinterpret_cast<const uint32_t *>(&h);
 }
-
-// Asynchronous 16-byte copies global -> shared, one group per tile.
-__device__ __forceinline__ void paged_copy16(uint32_t dst, const void *src)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void paged_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void paged_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // A warp's accumulators (rows: heads; 8 columns of the head dimension per
 // entry) and its running softmax.  A lane holds the scores of two tokens and
@@ -306,31 +291,6 @@ __device__ __forceinline__ void paged_store4(void *o, int type, int64_t at, floa
     else paged_store4<float>(o, at, v);
 }
 
-// Cluster barrier (all threads of all CTAs) and reads of another CTA's shared
-// memory.
-__device__ __forceinline__ void paged_cluster_sync()
-{
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t paged_remote(uint32_t addr, int rank)
-{
-    uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
-    return r;
-}
-__device__ __forceinline__ float paged_remote_f32(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ float4 paged_remote_f4(uint32_t addr)
-{
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
-    return v;
-}
-
 // Join the warps of a CTA in a fixed order and write the split's result: the
 // output itself where there is one split; o (relative to the split's maximum)
 // with maximum and sum for the join kernel; or, where the splits of a head are
@@ -411,21 +371,22 @@ __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int wa
     }
     if (!a.cluster) return;
     __syncwarp();
-    paged_cluster_sync();
-    const uint32_t s_m = static_cast<uint32_t>(__cvta_generic_to_shared(s.all_m));
-    const uint32_t s_l = static_cast<uint32_t>(__cvta_generic_to_shared(s.all_l));
+    cluster_arrive();
+    cluster_wait();
+    const uint32_t s_m = smem_u32(s.all_m);
+    const uint32_t s_l = smem_u32(s.all_l);
     for (int e = split * kPagedThreads + threadIdx.x; e < kPagedHeads * (D / 4); e += a.n_split * kPagedThreads) {
         const int h = e / (D / 4), d = (e - h * (D / 4)) * 4;
         if (head0 + h >= a.group) break;
-        const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(so(0, h, d)));
+        const uint32_t mine = smem_u32(so(0, h, d));
         float ms[kPagedCluster], ls[kPagedCluster];  // all loads before their first use
         float4 us[kPagedCluster];
 #pragma unroll
         for (int c = 0; c < kPagedCluster; ++c) {
             const int from = min(c, a.n_split - 1);
-            ms[c] = paged_remote_f32(paged_remote(s_m + 4 * h, from));
-            ls[c] = paged_remote_f32(paged_remote(s_l + 4 * h, from));
-            us[c] = paged_remote_f4(paged_remote(mine, from));
+            ms[c] = ld_cluster_f32(mapa(s_m + 4 * h, from));
+            ls[c] = ld_cluster_f32(mapa(s_l + 4 * h, from));
+            us[c] = ld_cluster_f4(mapa(mine, from));
         }
         float m = ms[0], sum = 0.f;
 #pragma unroll
@@ -441,7 +402,8 @@ __device__ __forceinline__ void paged_finish(PagedJoin &s, uint8_t *smem, int wa
         paged_store4(a.o, a.o_type, (row0 + h) * D + d, make_float4(v.x * r, v.y * r, v.z * r, v.w * r));
     }
     __syncwarp();
-    paged_cluster_sync();  // no CTA leaves while another reads its shared memory
+    cluster_arrive();
+    cluster_wait();  // no CTA leaves while another reads its shared memory
 }
 
 // CTAs resident per SM of the kernel that serves this cache.

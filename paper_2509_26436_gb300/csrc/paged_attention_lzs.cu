@@ -101,7 +101,7 @@ __device__ __forceinline__ void key_codes(uint32_t w, const KeyFlag &f, uint32_t
 __device__ __forceinline__ void value_codes(uint32_t w0, uint32_t w1, uint32_t flags, uint32_t (&v)[8])
 {
     const uint32_t m = flags * 128u + 0x3F803F80u, a = mul_bf16x2(m, 0xC308C308u);  // 2^F, -136 2^F
-    const uint32_t lo = permute(w0, w1, 0x5410), hi = permute(w0, w1, 0x7632);
+    const uint32_t lo = prmt(w0, w1, 0x5410), hi = prmt(w0, w1, 0x7632);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         v[j] = fma_bf16x2(and_xor(lo >> (4 * j), 0x000F000Fu, 0x43084308u), m, a);
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     const int all_tiles = max(0, end - range.base - begin + 15) >> 4, warp_tiles = (all_tiles + kPagedWarps - 1) / kPagedWarps;
     const int tiles = max(0, min(warp_tiles, all_tiles - warp * warp_tiles));
     const int base0 = range.base + begin + warp * warp_tiles * 16;
-    const uint32_t ring = static_cast<uint32_t>(__cvta_generic_to_shared(s_ring)) + warp * kWarpBytes;
+    const uint32_t ring = smem_u32(s_ring) + warp * kWarpBytes;
 
     // --- copies of a tile -------------------------------------------------
     const int32_t *table = a.table + b * a.table_stride;
@@ -285,12 +285,12 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
             const uint8_t *kc = a.k.codes + row * (D / 2) + lane * 16, *vc = a.v.codes + row * (D / 2) + lane * 16;
 #pragma unroll
             for (int k = 0; k < Tile::kCodesPerLane; ++k) {
-                paged_copy16(to + key_dst[k], kc + k * 512);
-                paged_copy16(to + value_dst[k], vc + k * 512);
+                cp_async16(to + key_dst[k], kc + k * 512);
+                cp_async16(to + value_dst[k], vc + k * 512);
             }
 #pragma unroll
             for (int k = 0; k < Tile::kSmallPerLane; ++k)
-                if (small_row[k] >= 0) paged_copy16(to + small_dst[k], small_src[k] + row * small_row[k]);
+                if (small_row[k] >= 0) cp_async16(to + small_dst[k], small_src[k] + row * small_row[k]);
             at += 16;
             at_row += 16;
             if ((at & page_mask) == 0 && at < end) enter(page_behind);
@@ -301,8 +301,8 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
             for (int k = 0; k < Tile::kCodesPerLane; ++k) {
                 const int i = lane + 32 * k, t = i / Tile::kChunks, c = i % Tile::kChunks;
                 const uint64_t row = __shfl_sync(0xffffffffu, my_row, t);
-                paged_copy16(to + key_dst[k], a.k.codes + row * (D / 2) + c * 16);
-                paged_copy16(to + value_dst[k], a.v.codes + row * (D / 2) + c * 16);
+                cp_async16(to + key_dst[k], a.k.codes + row * (D / 2) + c * 16);
+                cp_async16(to + value_dst[k], a.v.codes + row * (D / 2) + c * 16);
             }
             const PagedSide &ps = lane < 16 ? a.k : a.v;  // a lane per row and side
             uint8_t *dst = s_ring + warp * kWarpBytes + stage * Tile::kBytes + (lane < 16 ? 0 : Tile::kSide) + Tile::kCodes;
@@ -319,7 +319,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
 #pragma unroll
     for (int s = 0; s < kStages - 1; ++s) {
         if (s < tiles) fetch(s);
-        paged_commit();
+        cp_async_commit();
     }
 
     // --- the query, in the order the keys' codes unpack to: pairs (k, k + 4) of
@@ -329,8 +329,8 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
         uint4 v = make_uint4(0, 0, 0, 0);
         if (head0 + h < a.group)
             v = *reinterpret_cast<const uint4 *>(a.q + b * a.q_sb + (static_cast<int64_t>(kv_head) * a.group + head0 + h) * a.q_sh + d);
-        *reinterpret_cast<uint4 *>(&s_q[h][d]) = make_uint4(permute(v.x, v.z, 0x5410), permute(v.x, v.z, 0x7632),
-                                                            permute(v.y, v.w, 0x5410), permute(v.y, v.w, 0x7632));
+        *reinterpret_cast<uint4 *>(&s_q[h][d]) = make_uint4(prmt(v.x, v.z, 0x5410), prmt(v.x, v.z, 0x7632),
+                                                            prmt(v.y, v.w, 0x5410), prmt(v.y, v.w, 0x7632));
     }
     __syncthreads();
     // lane q of a token holds codes 16 q .. 16 q + 15 of each group
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     // overlap the other's unpacking.
     float sc[2][2], p[2][2];
     if (tiles > 0) {
-        paged_wait<kStages - 2>();
+        cp_async_wait<kStages - 2>();
         __syncwarp();
         score(fixed(ring), base0, sc);
         st.weigh(sc, p, 0.f, 8.f);
@@ -464,10 +464,10 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
     int stage = 0;
     for (int it = 0; it < tiles; ++it) {
         const int base = base0 + it * 16;
-        paged_wait<kStages - 3>();
+        cp_async_wait<kStages - 3>();
         __syncwarp();
         if (it + kStages - 1 < tiles) fetch(stage == 0 ? kStages - 1 : stage - 1);
-        paged_commit();
+        cp_async_commit();
         const uint32_t tile = fixed(ring + stage * Tile::kBytes);
         stage = stage == kStages - 1 ? 0 : stage + 1;
         if (it + 1 < tiles) {
@@ -479,7 +479,7 @@ __global__ void __launch_bounds__(kPagedThreads, MINB) paged_attn_lzs_kernel(Pag
             add_values(tile, base, p);
         }
     }
-    paged_wait<0>();
+    cp_async_wait<0>();
     __syncwarp();
     if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
     paged_finish<D, true, SHARE>(s_join, s_ring, kWarpBytes, st, a, b, kv_head, head0, split, 0.f);

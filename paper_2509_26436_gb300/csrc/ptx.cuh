@@ -1,5 +1,6 @@
 // Inline-PTX helpers for sm_103a: mbarrier, TMA (cp.async.bulk), tcgen05
-// (TMEM allocation, MMA, loads) and a bounded wait used by every pipeline.
+// (TMEM allocation, MMA, loads), a bounded wait used by every pipeline, byte
+// permutes, cp.async copies and reads across a cluster.
 #pragma once
 
 #include <cstdint>
@@ -179,7 +180,47 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_
 // async proxy (TMA, tcgen05).
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// 8-byte asynchronous copy global -> shared by this thread, in commit groups.
+// Byte permute (PTX prmt, default mode: a selector nibble b < 8 copies byte b
+// of {hi:lo}, b + 8 replicates that byte's sign bit).
+__device__ __forceinline__ uint32_t prmt(uint32_t lo, uint32_t hi, uint32_t sel)
+{
+    uint32_t d;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(d) : "r"(lo), "r"(hi), "r"(sel));
+    return d;
+}
+
+// Cluster barrier (all threads of all CTAs; the hardware's own wait) and
+// reads of another CTA's shared memory.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t mapa(uint32_t addr, int rank)
+{
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t addr)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t addr)
+{
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(addr)
+                 : "memory");
+    return v;
+}
+
+// 16- and 8-byte asynchronous copies global -> shared by this thread, in commit
+// groups (the wait is the hardware's own).
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async8(uint32_t dst, const void *src)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");

@@ -42,6 +42,14 @@ inline int device_sms()
     return n > 0 ? n : 152;
 }
 
+// The shift for a power of two (page sizes).
+inline int log2_of(int v)
+{
+    int n = 0;
+    while ((1 << n) < v) ++n;
+    return n;
+}
+
 #ifdef __CUDACC__
 // Let launches of Kernel on the current device have up to `bytes` of dynamic
 // shared memory (always the same number): once per device, since the call costs
