@@ -370,7 +370,8 @@ typedef enum { QUARTZ_PAGES_F16 = 0, QUARTZ_PAGES_BF16 = 1, QUARTZ_PAGES_ENCODED
 /* One side (keys or values) of a paged cache.
  *   16-bit pages:  element (page, slot, head, d) at data[page * stride_page +
  *                  slot * stride_slot + head * stride_head + d]; data 16-byte
- *                  aligned, strides in elements, multiples of 8 in [0, 2^31)
+ *                  aligned, strides in elements, multiples of 8 in [0, 2^31);
+ *                  0 (of two or more) only where pages are read
  *   encoded pages: `enc`, num_pages * heads * page_size rows of dim columns,
  *                  token (page, head, slot) in row (page * heads + head) *
  *                  page_size + slot; group_q 64, SYMMETRIC, 8-bit codes, one
@@ -410,7 +411,8 @@ typedef struct {
 /* Rotate x [tokens, heads, dim] of `type` (quartz_out_t) into y of the same
  * type, in binary32, rounded once; elements from `rotary` on are copied.
  * Strides in elements: x[t * x_stride_token + h * x_stride_head + d], y alike.
- * y == x with equal strides works in place; other overlaps are undefined.
+ * y == x with equal strides works in place; other overlaps are undefined, and
+ * y strides of 0 (of two or more) are refused.
  * dim 2 .. 1024, tokens <= 2^30; any alignment of the type itself. */
 int32_t quartz_rope(const void *x, int64_t x_stride_token, int64_t x_stride_head, void *y, int64_t y_stride_token,
                     int64_t y_stride_head, int32_t type, int64_t tokens, int32_t heads, int32_t dim,

@@ -18,6 +18,9 @@ constexpr int64_t kMaxRowStride = int64_t(1) << 40;  // of tables, weights, q, k
 
 bool stride_ok(int64_t s, int64_t multiple) { return s >= 0 && s <= kMaxRowStride && s % multiple == 0; }
 
+// A stride that puts several written elements in one place.
+bool repeats(int64_t stride, int64_t n) { return stride == 0 && n > 1; }
+
 bool type_ok(int32_t t) { return t == QUARTZ_OUT_F16 || t == QUARTZ_OUT_BF16 || t == QUARTZ_OUT_F32; }
 
 int32_t check_side(const quartz_paged_cache_t *c, const quartz_pages_t *p)
@@ -61,6 +64,16 @@ int32_t check_cache(const quartz_paged_cache_t *c)
     return rc;
 }
 
+// Pages that are written hold each row once (attention may read repeated ones).
+int32_t check_written(const quartz_paged_cache_t *c)
+{
+    if (c->type == QUARTZ_PAGES_ENCODED) return QUARTZ_OK;
+    for (const quartz_pages_t *p : {&c->k, &c->v})
+        if (repeats(p->stride_page, c->num_pages) || repeats(p->stride_slot, c->page_size) || repeats(p->stride_head, c->heads))
+            return QUARTZ_ERR_INVALID_ARG;
+    return QUARTZ_OK;
+}
+
 int32_t check_rope(const quartz_rope_t *r, int32_t dim)
 {
     if (!r->positions || !r->freqs) return QUARTZ_ERR_INVALID_ARG;
@@ -99,6 +112,7 @@ int32_t quartz_rope(const void *x, int64_t x_stride_token, int64_t x_stride_head
     if (!x || !y) return QUARTZ_ERR_INVALID_ARG;
     const uintptr_t m = type == QUARTZ_OUT_F32 ? 3 : 1;
     if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(y)) & m) return QUARTZ_ERR_ALIGNMENT;
+    if (repeats(y_stride_token, tokens) || repeats(y_stride_head, heads)) return QUARTZ_ERR_INVALID_ARG;
     RopeArgs a{x, y, x_stride_token, x_stride_head, y_stride_token, y_stride_head, type, heads, dim, *rope};
     return map_cuda(launch_rope(a, tokens, static_cast<cudaStream_t>(stream)));
 }
@@ -120,6 +134,7 @@ int32_t quartz_paged_append(const quartz_paged_cache_t *cache, const void *k, in
     if (rope && rope->backward) return QUARTZ_ERR_INVALID_ARG;
     if (!k || !v || !slots) return QUARTZ_ERR_INVALID_ARG;
     if (!aligned16(k) || !aligned16(v) || (reinterpret_cast<uintptr_t>(slots) & 7)) return QUARTZ_ERR_ALIGNMENT;
+    if ((rc = check_written(cache)) != QUARTZ_OK) return rc;
     AppendArgs a{k, v, k_stride_token, k_stride_head, v_stride_token, v_stride_head, slots, {}, device_error_word()};
     if (!a.dev_err) return QUARTZ_ERR_CUDA;
     if (rope) a.rope = *rope;
@@ -152,6 +167,7 @@ int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_st
     if (!aligned16(q) || !aligned16(o) || (reinterpret_cast<uintptr_t>(block_table) & 3) ||
         (reinterpret_cast<uintptr_t>(seq_lens) & 3) || (reinterpret_cast<uintptr_t>(weights) & 3))
         return QUARTZ_ERR_ALIGNMENT;
+    if (weights && (repeats(weights_stride_seq, seqs) || repeats(weights_stride_head, cache->heads))) return QUARTZ_ERR_INVALID_ARG;
     if (!workspace || workspace_bytes < paged_attention_workspace_bytes(cache, seqs, q_heads, max_len, window, weights != nullptr))
         return QUARTZ_ERR_WORKSPACE;
     if (!aligned16(workspace)) return QUARTZ_ERR_ALIGNMENT;
@@ -199,6 +215,8 @@ int32_t quartz_cache_compact(const quartz_paged_cache_t *cache, int64_t seqs, co
     if ((reinterpret_cast<uintptr_t>(block_table) | reinterpret_cast<uintptr_t>(new_table) |
          reinterpret_cast<uintptr_t>(seq_lens) | reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(weights)) & 3)
         return QUARTZ_ERR_ALIGNMENT;
+    if (weights && (repeats(weights_stride_seq, seqs) || repeats(weights_stride_head, cache->heads))) return QUARTZ_ERR_INVALID_ARG;
+    if (const int32_t written = check_written(cache); written != QUARTZ_OK) return written;
     CompactCall a{seqs, block_table, new_table, table_stride, new_table_stride, seq_lens, kept, max_len, budget, weights,
                   weights_stride_seq, weights_stride_head, device_error_word()};
     if (!a.dev_err) return QUARTZ_ERR_CUDA;
