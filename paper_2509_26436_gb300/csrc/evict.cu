@@ -47,9 +47,6 @@ __global__ void __launch_bounds__(kThreads, kThreads == 1024 ? 1 : 6) evict_sele
     constexpr int kWarps = kThreads / 32;
     extern __shared__ uint32_t s_keys[];
     __shared__ uint32_t s_hist[kBuckets];
-    // The range and the counts in places of their own: between the range's reads and
-    // the last counts' stores there is no barrier where all keys are equal.
-    __shared__ uint32_t s_top[kWarps], s_bottom[kWarps];
     __shared__ uint32_t s_above[kWarps], s_equal[kWarps];
     __shared__ uint32_t s_bucket, s_left;
     const int64_t bh = blockIdx.x;
@@ -89,10 +86,14 @@ __global__ void __launch_bounds__(kThreads, kThreads == 1024 ? 1 : 6) evict_sele
     }
     top = __reduce_max_sync(0xffffffffu, top);
     bottom = __reduce_min_sync(0xffffffffu, bottom);
-    if (lane == 0) s_top[warp] = top, s_bottom[warp] = bottom;
+    if (lane == 0) s_above[warp] = top, s_equal[warp] = bottom;
     __syncthreads();
-    top = __reduce_max_sync(0xffffffffu, s_top[lane % kWarps]);
-    bottom = __reduce_min_sync(0xffffffffu, s_bottom[lane % kWarps]);
+    top = __reduce_max_sync(0xffffffffu, s_above[lane % kWarps]);
+    bottom = __reduce_min_sync(0xffffffffu, s_equal[lane % kWarps]);
+    // The warps' counts go to the same places, and where all keys are equal no barrier
+    // of the loop lies between.  (Places of their own instead: 64 x 32 heads of up to
+    // 4096 tokens 44.8 us, 37.1 with the barrier.)
+    __syncthreads();
     auto key_at = [&](int t) { return HELD ? s_keys[t - lo] : order_key(w[t]); };
 
     // the want-th largest key is in [bottom, bottom + span]
