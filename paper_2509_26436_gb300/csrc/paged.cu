@@ -157,7 +157,9 @@ __device__ __forceinline__ void rotate_unit(const T *row, int d0, const quartz_r
 // with units of 16, whose 32 bytes per lane split every line between two
 // loads; 24.2 with 5 CTAs per SM, 26.5 with 4; not rotated 20.0, 25.6 without
 // BOTH); encoded 26.4 us (38.8 without BOTH; 10% more with 3 CTAs per SM, 7%
-// with 5), bound by the encoder's instructions (12.9 us of bytes).
+// with 5; 12.9 us of bytes), where warps wait in the encoder's chains: issue slots
+// 72% busy, the logic pipe 57%.  64 registers leave 12 to 36 bytes of addresses
+// spilled in the encoded instances, 40 up to 28 in the 16-bit ones without BOTH.
 template <typename T, int GS, bool BOTH>
 __global__ void __launch_bounds__(kAppendThreads, GS == 0 ? 6 : 4) paged_append_kernel(AppendCall c, int tokens)
 {
@@ -304,8 +306,8 @@ __device__ __forceinline__ void store_piece(uint8_t *p, const uint4 v, int bytes
 // per row follows its kept index and the tables to the two addresses, then all
 // threads move pieces, eight loads in flight each; so the dependent reads are
 // paid once per tile and row, not per piece, and for the next tile while this
-// one's loads are under way (16 x 8 heads, 4096 rows of 2 x 256 bytes: 75 us, 93%
-// of the copy rate; followed per piece 97).  Into new pages, a part is a
+// one's loads are under way (16 x 8 heads, up to 4096 rows of 2 x 256 bytes:
+// 77 us, 91% of the copy rate; followed per piece 97).  Into new pages, a part is a
 // range of rows; in place it is a slice of every row, and the CTA goes through
 // the rows in order: row j is written after all rows up to its tile's last are
 // read (a barrier per tile), and rows after them come from places behind the

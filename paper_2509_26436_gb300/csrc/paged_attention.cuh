@@ -18,7 +18,7 @@
 // The scores arrive transposed to what the second product takes: one register
 // transpose (movmatrix) per 8 x 8 block of 16-bit weights, nothing through
 // shared memory.  Legacy tensor instructions are enough here: the step is
-// bound by HBM (or, encoded, by the decoding), and the tensor pipe has to keep
+// bound by HBM (or, encoded, waits in the decoding), and the tensor pipe has to keep
 // up with one pair of products per loaded row only (13% busy on 16-bit pages).
 // Measured (32 sequences of up to 8192 tokens, 32 / 8 heads of 128, bf16): 98.6
 // us, 88% of the copy rate; with tiles in registers instead of a ring 162 us,

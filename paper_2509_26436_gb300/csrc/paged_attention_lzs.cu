@@ -19,10 +19,12 @@
 // The contraction over the head dimension may take it in any order, so a
 // lane's 8 consecutive bytes of codes go into the operand's registers as they
 // unpack, and the query is permuted to match, once.
-// What bounds it: instructions, not HBM.  A tile of 16 tokens of 128 dimensions
-// takes 466 instructions of a warp, 172 of them logic and 152 of the half-rate
-// multiply-add pipe, which take two cycles of the scheduler each: 818 cycles, of
-// which unpacking is two fifths.  8 sequences of up to 65536 tokens, 64 / 8
+// What bounds it: latency, not HBM.  A tile of 16 tokens of 128 dimensions takes
+// 466 instructions of a warp, 172 of them logic and 152 of the half-rate
+// multiply-add pipe, whose pipes they hold for two cycles each: 466, 344 and 304
+// cycles side by side, of the 818 that it takes.  Meanwhile 2.8 warps per
+// scheduler (168 registers) wait for their own dependent instructions: issue slots
+// 62% busy, the logic pipe 47%, multiply-add 41%, tensor 25%.  8 sequences of up to 65536 tokens, 64 / 8
 // heads, G_s = 16: 96.0 us, 51% of the copy rate (245 us with tiles in
 // registers, 125 with the query as the first operand of the keys' product, whose
 // duplicated rows had to be copied for every tile).

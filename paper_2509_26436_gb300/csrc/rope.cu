@@ -38,7 +38,7 @@ __device__ __forceinline__ void store_rounded(T *to, const float (&f)[V])
 }
 
 // n / pieces by a product with 2^64 / pieces, rounded up (0: pieces is 1): exact
-// for n pieces < 2^64, and places are below 2^39.  (A 64-bit division is some
+// for n pieces < 2^64, and places are below 2^40.  (A 64-bit division is some
 // hundred instructions.)
 __device__ __forceinline__ int64_t token_of(int64_t n, uint64_t inverse)
 {
