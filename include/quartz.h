@@ -418,6 +418,68 @@ int32_t quartz_rope(const void *x, int64_t x_stride_token, int64_t x_stride_head
                     int64_t y_stride_head, int32_t type, int64_t tokens, int32_t heads, int32_t dim,
                     const quartz_rope_t *rope, void *stream);
 
+/* Rotary positions of one or several axes (time, row and column of an image's
+ * or a video's patches): as quartz_rope_t, with pair i turned by
+ * positions[pair_axis[i] * axis_stride + t] * freqs[i] radians. */
+typedef struct {
+    const int64_t *positions;  /* device, [axes] rows of one per token, axis_stride elements apart */
+    int64_t axis_stride;
+    const double *freqs;       /* device, [rotary / 2], radians per position, finite */
+    const int32_t *pair_axis;  /* device, [rotary / 2], each in [0, axes); NULL: all 0 */
+    int32_t axes;              /* 1 .. 16 */
+    int32_t rotary;            /* even, 2 .. dim */
+    int32_t interleaved;       /* 0 or 1 */
+    int32_t backward;          /* 0 or 1 */
+    float scale;               /* on cosine and sine */
+} quartz_rope_axes_t;
+
+/* Rotate x [tokens, heads, dim] into y as quartz_rope does, by positions of
+ * several axes.  dim 2 .. 256; otherwise the same limits, strides and overlaps.
+ * A pair_axis out of range counts as 0 and QUARTZ_ERR_INDEX is recorded
+ * (quartz_device_status). */
+int32_t quartz_rope_axes(const void *x, int64_t x_stride_token, int64_t x_stride_head, void *y, int64_t y_stride_token,
+                         int64_t y_stride_head, int32_t type, int64_t tokens, int32_t heads, int32_t dim,
+                         const quartz_rope_axes_t *rope, void *stream);
+
+/* Queries or keys of quartz_qk_norm_rope: [tokens, heads, dim], strides in
+ * elements as in quartz_rope.  Forward: y from x and w.  Backward: y is the
+ * gradient of x, from x, w and dy, the gradient of the forward pass's y; dw
+ * (NULL: not wanted) the gradient of w. */
+typedef struct {
+    const void *x;
+    int64_t x_stride_token, x_stride_head;
+    const void *dy;
+    int64_t dy_stride_token, dy_stride_head;
+    void *y;
+    int64_t y_stride_token, y_stride_head;
+    const void *w;  /* [dim] of w_type; NULL: ones */
+    void *dw;       /* [dim] of w_type */
+    int32_t heads;  /* 0: no such heads, nothing else is read, and a dw becomes 0 */
+} quartz_norm_side_t;
+
+/* The norm of each head's queries and keys, then the rotation, in one pass:
+ *   y = R (w x r),  r = (mean(x^2) + eps)^-1/2
+ * with the mean over the head's dim elements and R the rotation of `rope`
+ * (NULL: none; its `backward` is 0).  In binary32, rounded once; x^2 and its
+ * sum have to be finite there.  `type` of x and y, `w_type` of the weights of
+ * both sides (quartz_out_t).  y == x with equal strides works in place; other
+ * overlaps are undefined, of the two sides' too.  dim 2 .. 256, eps >= 0,
+ * tokens <= 2^30, heads <= 65535. */
+int32_t quartz_qk_norm_rope(const quartz_norm_side_t *q, const quartz_norm_side_t *k, int32_t type, int32_t w_type,
+                            int64_t tokens, int32_t dim, float eps, const quartz_rope_axes_t *rope, void *stream);
+
+/* Its gradient: with g = R' dy (R' the transpose of R) and n = x r,
+ *   dx = r (g w - n mean(g w n)),  dw = sum over tokens and heads of g n.
+ * dw is summed in binary32 in an order that depends on sizes and the device
+ * alone, and rounded once; without tokens it is 0.  y may be x or dy (the same
+ * strides).  workspace: quartz_qk_norm_rope_workspace_size bytes, 16-byte
+ * aligned, scratch (needed where a dw is wanted). */
+size_t quartz_qk_norm_rope_workspace_size(int32_t dim);
+int32_t quartz_qk_norm_rope_backward(const quartz_norm_side_t *q, const quartz_norm_side_t *k, int32_t type,
+                                     int32_t w_type, int64_t tokens, int32_t dim, float eps,
+                                     const quartz_rope_axes_t *rope, void *workspace, size_t workspace_bytes,
+                                     void *stream);
+
 /* Write the keys and values of `tokens` new tokens into their slots
  * (slots[t] = page * page_size + slot; negative: the token is skipped).  k and
  * v are [tokens, heads, dim] in the pages' type (fp16 for encoded pages),

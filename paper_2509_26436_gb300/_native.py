@@ -72,6 +72,18 @@ class QuartzRope(C.Structure):
                 ("backward", C.c_int32), ("scale", C.c_float)]
 
 
+class QuartzRopeAxes(C.Structure):
+    _fields_ = [("positions", _P), ("axis_stride", C.c_int64), ("freqs", _P), ("pair_axis", _P), ("axes", C.c_int32),
+                ("rotary", C.c_int32), ("interleaved", C.c_int32), ("backward", C.c_int32), ("scale", C.c_float)]
+
+
+class QuartzNormSide(C.Structure):
+    _fields_ = [("x", _P), ("x_stride_token", C.c_int64), ("x_stride_head", C.c_int64),
+                ("dy", _P), ("dy_stride_token", C.c_int64), ("dy_stride_head", C.c_int64),
+                ("y", _P), ("y_stride_token", C.c_int64), ("y_stride_head", C.c_int64),
+                ("w", _P), ("dw", _P), ("heads", C.c_int32)]
+
+
 SIGNATURES = {
     "quartz_status_string": (C.c_char_p, [_I32]),
     "quartz_version": (_I32, []),
@@ -100,6 +112,12 @@ SIGNATURES = {
                                        C.POINTER(QuartzEncoded), _I64, _I64, C.c_float, _P, _I32, _P, _SZ,
                                        _P]),
     "quartz_rope": (_I32, [_P, _I64, _I64, _P, _I64, _I64, _I32, _I64, _I32, _I32, C.POINTER(QuartzRope), _P]),
+    "quartz_rope_axes": (_I32, [_P, _I64, _I64, _P, _I64, _I64, _I32, _I64, _I32, _I32, C.POINTER(QuartzRopeAxes), _P]),
+    "quartz_qk_norm_rope": (_I32, [C.POINTER(QuartzNormSide), C.POINTER(QuartzNormSide), _I32, _I32, _I64, _I32,
+                                   C.c_float, C.POINTER(QuartzRopeAxes), _P]),
+    "quartz_qk_norm_rope_workspace_size": (_SZ, [_I32]),
+    "quartz_qk_norm_rope_backward": (_I32, [C.POINTER(QuartzNormSide), C.POINTER(QuartzNormSide), _I32, _I32, _I64,
+                                            _I32, C.c_float, C.POINTER(QuartzRopeAxes), _P, _SZ, _P]),
     "quartz_paged_append": (_I32, [C.POINTER(QuartzPagedCache), _P, _I64, _I64, _P, _I64, _I64, _I64, _P,
                                    C.POINTER(QuartzRope), _P]),
     "quartz_paged_attention_workspace_size": (_SZ, [C.POINTER(QuartzPagedCache), _I64, _I32, _I64, _I64, _I32]),

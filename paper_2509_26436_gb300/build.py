@@ -20,7 +20,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libquartz.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["api.cu", "quantize.cu", "linear.cu", "noalloc.cu", "attention.cu", "probe.cu", "rope.cu", "paged.cu",
-           "paged_attention.cu", "paged_attention_lzs.cu", "evict.cu", "paged_api.cu"]
+           "paged_attention.cu", "paged_attention_lzs.cu", "evict.cu", "paged_api.cu", "head_norm.cu", "tokens_api.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

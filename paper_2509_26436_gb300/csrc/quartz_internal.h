@@ -209,6 +209,32 @@ struct RopeArgs {
     quartz_rope_t rope;
 };
 cudaError_t launch_rope(const RopeArgs &a, int64_t tokens, cudaStream_t s);
+// Norm of each head with the rotation, rotation by several axes (head_norm.cu);
+// queries, then keys.  Arguments are pre-validated (tokens_api.cu).
+struct HeadNormSide {
+    const void *x, *dy;
+    void *y;
+    int64_t x_st, x_sh, dy_st, dy_sh, y_st, y_sh;  // strides in elements
+    const void *w;  // NULL: ones
+    void *dw;
+    int heads;      // 0: the side is not there
+};
+struct HeadNormArgs {
+    HeadNormSide side[2];
+    int64_t tokens, axis_stride;
+    const int64_t *positions;
+    const double *freqs;
+    const int32_t *pair_axis;  // NULL: one axis
+    int axes, type, w_type, dim, rotary, interleaved, backward;
+    float scale, eps, inv_dim;
+    float *part;  // backward: NULL, or the CTAs' sums for dw
+    int ctas[2];  // of each side
+    int *dev_err;
+};
+size_t head_norm_workspace_bytes(int dim);
+cudaError_t launch_rope_axes(HeadNormArgs a, cudaStream_t s);
+cudaError_t launch_head_norm(HeadNormArgs a, cudaStream_t s);
+cudaError_t launch_head_norm_backward(HeadNormArgs a, cudaStream_t s);
 struct AppendArgs {
     const void *k, *v;
     int64_t k_st, k_sh, v_st, v_sh;

@@ -1,0 +1,214 @@
+"""Several new tokens per sequence: the norm of each head's queries and keys with
+the rotary positions in the same pass (and its gradient), and rotary positions
+of several axes.
+
+As paged.py, whose cache and frequencies these go with, this only marshals torch
+CUDA tensors into the C ABI; every call is asynchronous on the current stream
+(or `stream`), and nothing is recorded for autograd: a tensor whose gradient
+would be lost is refused.
+
+    freqs, scale = rope_frequencies(128, base=500000.0)
+    q, k = qk_norm_rope(q, k, wq, wk, positions, freqs, scale=scale)
+    dq, dk, dwq, dwk = qk_norm_rope_backward(gq, gk, q, k, wq, wk, positions, freqs, scale=scale)
+"""
+from __future__ import annotations
+
+import ctypes as C
+
+import paper_2509_26436_gb300 as _Q
+
+from . import _native as N
+from . import paged as P
+
+_byref = C.byref
+
+
+def _no_gradient(name, instead, *tensors):
+    if P.torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{name} records no gradient: use torch.no_grad(), or {instead}")
+
+
+_FUNCTION = "an autograd function whose backward calls "
+
+
+def _axes_struct(positions, freqs, pair_axis, tokens, scale, interleaved, backward, device) -> N.QuartzRopeAxes:
+    """positions [tokens] (one axis), or [axes, tokens] with pair_axis."""
+    pairs = freqs.shape[0]
+    f = P._vector("freqs", freqs, P.f64, device)
+    if pair_axis is None:
+        at, stride, axes, pa = P._vector("positions", positions, P.i64, device), 0, 1, None
+    else:
+        stride = P._rows("positions", positions, 2, P.i64, device)[0]
+        at, axes, pa = positions.data_ptr(), positions.shape[0], P._vector("pair_axis", pair_axis, P.i32, device)
+        if pair_axis.shape[0] != pairs:
+            raise ValueError("pair_axis must have one entry per frequency")
+    if positions.shape[-1] != tokens:
+        raise ValueError("positions must have one entry per token")
+    return N.QuartzRopeAxes(at, stride, f, pa, axes, 2 * pairs, interleaved, backward, scale)
+
+
+def rope_axes(x, positions, freqs, pair_axis, interleaved: bool = False, scale: float = 1.0, backward: bool = False,
+              out=None, stream=None):
+    """rope() by positions of several axes (time, row and column of an image's
+    or a video's patches): x [tokens, heads, dim <= 256], positions int64 [axes,
+    tokens], and pair i turned by positions[pair_axis[i], t] * freqs[i], with
+    pair_axis int32 [len(freqs)] on the device.  Types, strides, `out` and
+    gradients as in rope()."""
+    if P.torch is None:
+        P._bind()
+    _no_gradient("rope_axes", _FUNCTION + "rope_axes(..., backward=True)", x, out)
+    dtype = x.dtype
+    kind = P._KIND.get(dtype)
+    if kind is None or not x.is_cuda:
+        raise ValueError("x must be a 3-D float16, bfloat16 or float32 CUDA tensor")
+    device = P._device()
+    xs = P._rows("x", x, 3, dtype, device)
+    T, H, D = x.shape
+    if pair_axis is None:
+        raise ValueError("pair_axis must name the axis of each frequency (one axis: rope())")
+    r = _axes_struct(positions, freqs, pair_axis, T, scale, interleaved, backward, device)
+    if out is None:
+        out = P._empty((T, H, D), dtype, x.device, stream)
+        s0, s1 = H * D, D
+    else:
+        s0, s1, _ = P._rows("out", out, 3, dtype, device)
+        if out.shape != x.shape:
+            raise ValueError("out must have the shape of x")
+    rc = P.lib.quartz_rope_axes(x.data_ptr(), xs[0], xs[1], out.data_ptr(), s0, s1, kind, T, H, D, _byref(r),
+                                _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_rope_axes")
+    return out
+
+
+def _norm_side(name, x, w, T, D, dtype, w_dtype, device):
+    """(strides of x, address of w) after the checks of one side."""
+    st = P._rows(name, x, 3, dtype, device)
+    if x.shape[0] != T or x.shape[2] != D:
+        raise ValueError("q and k must have the same tokens and dim")
+    if w is None:
+        return st, None
+    at = P._vector("w" + name, w, w_dtype, device)
+    if w.shape[0] != D:
+        raise ValueError(f"w{name} must have one entry per element of a head")
+    return st, at
+
+
+def _norm_types(q, wq, wk):
+    dtype = q.dtype
+    kind = P._KIND.get(dtype)
+    if kind is None or not q.is_cuda or q.dim() != 3:
+        raise ValueError("q must be a 3-D float16, bfloat16 or float32 CUDA tensor")
+    w_dtype = wq.dtype if wq is not None else wk.dtype if wk is not None else dtype
+    w_kind = P._KIND.get(w_dtype)
+    if w_kind is None or (wk is not None and wk.dtype is not w_dtype):
+        raise ValueError("wq and wk must be float16, bfloat16 or float32, of one type")
+    return dtype, kind, w_dtype, w_kind
+
+
+def _rope_of(positions, freqs, pair_axis, T, scale, interleaved, device):
+    if positions is None and freqs is None:
+        return None
+    if positions is None or freqs is None:
+        raise ValueError("positions and freqs go together")
+    return _byref(_axes_struct(positions, freqs, pair_axis, T, scale, interleaved, False, device))
+
+
+def qk_norm_rope(q, k, wq, wk, positions=None, freqs=None, eps: float = 1e-6, pair_axis=None, interleaved: bool = False,
+                 scale: float = 1.0, out=None, stream=None):
+    """(yq, yk): the norm of each head of q [tokens, q_heads, dim] and k [tokens,
+    k_heads, dim] (or None), x (mean x^2 + eps)^-1/2 w, then rope()'s rotation
+    of its first 2 len(freqs) elements by positions int64 [tokens], or with
+    pair_axis rope_axes()'s by positions [axes, tokens]; no positions and freqs:
+    no rotation.  float16, bfloat16 or float32, any strides with a contiguous
+    last dimension (views of a fused projection), dim <= 256; wq and wk [dim] in
+    one of these types, or None: ones.  In binary32, rounded once.  `out` (yq,
+    yk) may be (q, k).  Nothing is recorded for autograd (rope())."""
+    if P.torch is None:
+        P._bind()
+    _no_gradient("qk_norm_rope", _FUNCTION + "qk_norm_rope_backward", q, k, wq, wk, *(out or ()))
+    dtype, kind, w_dtype, w_kind = _norm_types(q, wq, wk)
+    device = P._device()
+    T, Hq, D = q.shape
+    qs, wq_ptr = _norm_side("q", q, wq, T, D, dtype, w_dtype, device)
+    yq, yk = (None, None) if out is None else out
+    if yq is None:
+        yq = P._empty((T, Hq, D), dtype, q.device, stream)
+        y0, y1 = Hq * D, D
+    else:
+        y0, y1, _ = P._rows("out", yq, 3, dtype, device)
+        if yq.shape != q.shape:
+            raise ValueError("out must have the shapes of q and k")
+    side_q = N.QuartzNormSide(q.data_ptr(), qs[0], qs[1], None, 0, 0, yq.data_ptr(), y0, y1, wq_ptr, None, Hq)
+    if k is None:
+        side_k, yk = N.QuartzNormSide(), None
+    else:
+        ks, wk_ptr = _norm_side("k", k, wk, T, D, dtype, w_dtype, device)
+        Hk = k.shape[1]
+        if yk is None:
+            yk = P._empty((T, Hk, D), dtype, q.device, stream)
+            y0, y1 = Hk * D, D
+        else:
+            y0, y1, _ = P._rows("out", yk, 3, dtype, device)
+            if yk.shape != k.shape:
+                raise ValueError("out must have the shapes of q and k")
+        side_k = N.QuartzNormSide(k.data_ptr(), ks[0], ks[1], None, 0, 0, yk.data_ptr(), y0, y1, wk_ptr, None, Hk)
+    r = _rope_of(positions, freqs, pair_axis, T, scale, interleaved, device)
+    rc = P.lib.quartz_qk_norm_rope(_byref(side_q), _byref(side_k), kind, w_kind, T, D, eps, r, _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_qk_norm_rope")
+    return yq, yk
+
+
+def qk_norm_rope_backward(dyq, dyk, q, k, wq, wk, positions=None, freqs=None, eps: float = 1e-6, pair_axis=None,
+                          interleaved: bool = False, scale: float = 1.0, workspace=None, stream=None):
+    """(dq, dk, dwq, dwk): the gradients of qk_norm_rope's q, k, wq and wk (None
+    for what is None) from those of its results (of their types and shapes, any
+    strides) and the same arguments.  The weights' gradients are summed in
+    binary32 in the same order on every call.  A workspace of the caller's
+    (qk_norm_rope_workspace_size bytes) is only good for one call at a time, and
+    for one captured graph."""
+    if P.torch is None:
+        P._bind()
+    _no_gradient("qk_norm_rope_backward", "detach what it gets", dyq, dyk)
+    dtype, kind, w_dtype, w_kind = _norm_types(q, wq, wk)
+    device = P._device()
+    T, _, D = q.shape
+    sides, grads = [], []
+    for name, x, dy, w in (("q", q, dyq, wq), ("k", k, dyk, wk)):
+        if x is None:
+            if dy is not None or w is not None:
+                raise ValueError(f"{name} is None, and has neither a gradient nor weights")
+            sides.append(N.QuartzNormSide())
+            grads += [None, None]
+            continue
+        st, w_ptr = _norm_side(name, x, w, T, D, dtype, w_dtype, device)
+        if dy is None or dy.shape != x.shape:
+            raise ValueError(f"dy{name} must have the shape of {name}")
+        ds = P._rows("dy" + name, dy, 3, dtype, device)
+        H = x.shape[1]
+        dx = P._empty((T, H, D), dtype, x.device, stream)
+        dw = None if w is None else P._empty((D,), w_dtype, x.device, stream)
+        sides.append(N.QuartzNormSide(x.data_ptr(), st[0], st[1], dy.data_ptr(), ds[0], ds[1], dx.data_ptr(), H * D, D,
+                                      w_ptr, None if w is None else dw.data_ptr(), H))
+        grads += [dx, dw]
+    ptr, size = None, 0
+    if wq is not None or wk is not None:
+        if workspace is None:
+            size = P.lib.quartz_qk_norm_rope_workspace_size(D)
+            workspace = P._empty(size, P.torch.uint8, q.device, stream)
+        else:
+            if workspace.get_device() != device or not workspace.is_contiguous():
+                raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
+            size = workspace.numel() * workspace.element_size()
+        ptr = workspace.data_ptr()
+    r = _rope_of(positions, freqs, pair_axis, T, scale, interleaved, device)
+    rc = P.lib.quartz_qk_norm_rope_backward(_byref(sides[0]), _byref(sides[1]), kind, w_kind, T, D, eps, r, ptr, size,
+                                            _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_qk_norm_rope_backward")
+    return grads[0], grads[2], grads[1], grads[3]
+
+
+def qk_norm_rope_workspace_size(dim: int) -> int:
+    return N.load().quartz_qk_norm_rope_workspace_size(dim)
