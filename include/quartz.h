@@ -526,6 +526,65 @@ int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_st
                                float scale, void *o, int32_t o_type, float *weights, int64_t weights_stride_seq,
                                int64_t weights_stride_head, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Attention of several new tokens per sequence: prompts, chunks of prompts
+ * behind what is cached already, trees of drafted tokens.  The new tokens are
+ * the last of their sequence, and in the cache (quartz_paged_append): new token
+ * j of sequence b is row starts[b] + j of q and o, and token base + j of the
+ * cache, base = seq_lens[b] - (starts[b + 1] - starts[b]).  Its position is
+ * base + j; in a tree base + its depth, the drafted tokens it sees but itself,
+ * and a drafted token's place is its position (of any other token: its index).
+ *   s_t = scale * q . k_t
+ *   s_t = cap tanh(s_t / cap)                     with cap > 0
+ *   s_t = s_t - slopes[h] |position - place_t|    with slopes
+ *   o = sum_t softmax(s)_t v_t over the tokens seen: t <= position (tree: t <
+ *       base, and the drafted tokens whose bits are set), of these with window
+ *       > 0 places > position - window, and always t < prefix_lens[b]
+ * A token that sees nothing gives zeros.  Query head h reads key / value head
+ * h / (q_heads / heads).  Encoded keys and values count as what
+ * quartz_dequantize gives (fp16).  Products, softmax and sums in binary32; the
+ * softmax weights, relative to the largest so far, enter the value product
+ * rounded to the pages' type.  q . k_t, s_t log2 e and the sums have to be
+ * finite in binary32; a query with others makes its own row of o NaN.  Tokens
+ * that none of a sequence's new tokens sees are not looked at, infinite and NaN
+ * ones either; an infinite or NaN element of a value that one of them sees may
+ * make that element of o NaN for the others too, whatever they see.
+ *   tree         NULL, or for every row of q the drafted tokens it sees, bit i
+ *                for token base + i (its own too, if it is to see itself);
+ *                max_new <= 64, bits behind the sequence's last are not looked at
+ *   prefix_lens  NULL, or int32 [seqs]; cut to 0 .. seq_lens[b]
+ *   slopes       NULL, or fp32 [q_heads], finite
+ *   window       0: none
+ *   cap          0: none; cap and scale / cap finite */
+typedef struct {
+    const uint64_t *tree;
+    const int32_t *prefix_lens;
+    const float *slopes;
+    int64_t window;
+    float cap;
+} quartz_tokens_mask_t;
+
+/*   q            [tokens, q_heads, dim], strides in elements (multiples of 8),
+ *                16-byte aligned, the pages' type (fp16 for encoded pages)
+ *   block_table, seq_lens, max_len  as in quartz_paged_attention
+ *   starts       int32 [seqs + 1], ascending, 0 .. tokens; each sequence at most
+ *                max_new apart.  Rows before the first and behind the last stay
+ *                as they are in o
+ *   mask         NULL: causal
+ *   o            [tokens, q_heads, dim] contiguous, o_type, 16-byte aligned
+ *   workspace    >= quartz_paged_attention_tokens_workspace_size bytes, 16-byte
+ *                aligned, scratch
+ * A length or start out of range: that sequence's rows are undefined and
+ * QUARTZ_ERR_INDEX is recorded.  seqs <= 65535, tokens <= 2^30, max_len <= 2^30,
+ * max_new q_heads / heads <= 2^30. */
+size_t quartz_paged_attention_tokens_workspace_size(const quartz_paged_cache_t *cache, int64_t tokens, int64_t seqs,
+                                                    int32_t q_heads, int64_t max_len, int64_t max_new);
+int32_t quartz_paged_attention_tokens(const void *q, int64_t q_stride_token, int64_t q_stride_head, int64_t tokens,
+                                      int32_t q_heads, const quartz_paged_cache_t *cache, const int32_t *block_table,
+                                      int64_t table_stride, const int32_t *seq_lens, const int32_t *starts,
+                                      int64_t seqs, int64_t max_len, int64_t max_new,
+                                      const quartz_tokens_mask_t *mask, float scale, void *o, int32_t o_type,
+                                      void *workspace, size_t workspace_bytes, void *stream);
+
 /* Choose the tokens that stay in each key / value head's cache: all of them
  * while len <= budget; else the first `sinks`, the last `recent`, and of those
  * between the budget - sinks - recent with the largest weights (equal weights:

@@ -28,6 +28,7 @@ __all__ = ["Params", "Encoded", "quantize", "encode_weights", "dequantize", "lin
            "rope_frequencies", "rope", "PagedCache", "empty_paged_cache", "paged_append",
            "attention_paged", "attention_paged_workspace_size", "evict_select", "cache_compact",
            "rope_axes", "qk_norm_rope", "qk_norm_rope_backward", "qk_norm_rope_workspace_size",
+           "attention_paged_tokens", "attention_paged_tokens_workspace_size",
            "SYMMETRIC", "ASYMMETRIC", "QuartzError"]
 
 
@@ -372,4 +373,5 @@ def attention_decode(q: Encoded, k_cache: Encoded, v_cache: Encoded, L_max: int,
 
 from .paged import (PagedCache, attention_paged, attention_paged_workspace_size, cache_compact,  # noqa: E402
                     empty_paged_cache, evict_select, paged_append, rope, rope_frequencies)
-from .tokens import qk_norm_rope, qk_norm_rope_backward, qk_norm_rope_workspace_size, rope_axes  # noqa: E402
+from .tokens import (attention_paged_tokens, attention_paged_tokens_workspace_size, qk_norm_rope,  # noqa: E402
+                     qk_norm_rope_backward, qk_norm_rope_workspace_size, rope_axes)

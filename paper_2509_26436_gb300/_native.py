@@ -84,6 +84,10 @@ class QuartzNormSide(C.Structure):
                 ("w", _P), ("dw", _P), ("heads", C.c_int32)]
 
 
+class QuartzTokensMask(C.Structure):
+    _fields_ = [("tree", _P), ("prefix_lens", _P), ("slopes", _P), ("window", C.c_int64), ("cap", C.c_float)]
+
+
 SIGNATURES = {
     "quartz_status_string": (C.c_char_p, [_I32]),
     "quartz_version": (_I32, []),
@@ -123,6 +127,10 @@ SIGNATURES = {
     "quartz_paged_attention_workspace_size": (_SZ, [C.POINTER(QuartzPagedCache), _I64, _I32, _I64, _I64, _I32]),
     "quartz_paged_attention": (_I32, [_P, _I64, _I64, _I64, _I32, C.POINTER(QuartzPagedCache), _P, _I64, _P, _I64,
                                       _I64, C.c_float, _P, _I32, _P, _I64, _I64, _P, _SZ, _P]),
+    "quartz_paged_attention_tokens_workspace_size": (_SZ, [C.POINTER(QuartzPagedCache), _I64, _I64, _I32, _I64, _I64]),
+    "quartz_paged_attention_tokens": (_I32, [_P, _I64, _I64, _I64, _I32, C.POINTER(QuartzPagedCache), _P, _I64, _P, _P,
+                                             _I64, _I64, _I64, C.POINTER(QuartzTokensMask), C.c_float, _P, _I32, _P, _SZ,
+                                             _P]),
     "quartz_evict_select": (_I32, [_P, _I64, _I64, _P, _I64, _I32, _I64, _I64, _I64, _I64, _P, _P, _P]),
     "quartz_cache_compact": (_I32, [C.POINTER(QuartzPagedCache), _I64, _P, _I64, _P, _I64, _P, _I64, _P, _I64, _P,
                                     _I64, _I64, _P]),

@@ -94,6 +94,8 @@ int32_t check_attention(const quartz_paged_cache_t *c, int64_t seqs, int32_t q_h
 
 }  // namespace
 
+int32_t quartz::check_paged_cache(const quartz_paged_cache_t *c) { return check_cache(c); }
+
 extern "C" {
 
 int32_t quartz_rope(const void *x, int64_t x_stride_token, int64_t x_stride_head, void *y, int64_t y_stride_token,

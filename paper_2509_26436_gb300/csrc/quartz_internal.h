@@ -262,6 +262,27 @@ struct PagedAttnCall {
 size_t paged_attention_workspace_bytes(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, int64_t max_len,
                                        int64_t window, bool with_weights);
 cudaError_t launch_paged_attention(const quartz_paged_cache_t *c, const PagedAttnCall &a, cudaStream_t s);
+// Several new tokens per sequence (tokens_attention.cu; checks: tokens_api.cu).
+struct PagedTokensCall {
+    const void *q;
+    int64_t q_st, q_sh, tokens;
+    int q_heads;
+    const int32_t *table;
+    int64_t table_stride;
+    const int32_t *lens, *starts;
+    int64_t seqs, max_len, max_new;
+    quartz_tokens_mask_t mask;
+    float scale;
+    void *o;
+    int o_type;
+    void *workspace;
+    int *dev_err;
+};
+size_t paged_tokens_workspace_bytes(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len,
+                                    int64_t max_new);
+cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokensCall &call, cudaStream_t s);
+// The checks of a cache's description (paged_api.cu).
+int32_t check_paged_cache(const quartz_paged_cache_t *c);
 cudaError_t launch_evict_select(const float *w, int64_t w_sb, int64_t w_sh, const int32_t *lens, int64_t seqs, int heads,
                                 int64_t max_len, int64_t budget, int64_t recent, int64_t sinks, int32_t *kept,
                                 int32_t *new_lens, int *dev_err, cudaStream_t s);

@@ -98,6 +98,18 @@ int32_t norm_args(const quartz_norm_side_t *q, const quartz_norm_side_t *k, int3
     return QUARTZ_OK;
 }
 
+int32_t check_tokens(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int32_t q_heads, int64_t max_len,
+                     int64_t max_new)
+{
+    const int32_t rc = check_paged_cache(c);
+    if (rc != QUARTZ_OK) return rc;
+    if (seqs < 0 || seqs > 65535 || q_heads < 1 || q_heads > 65536 || q_heads % c->heads) return QUARTZ_ERR_INVALID_ARG;
+    if (tokens < 0 || tokens > kMaxTokens || max_len < 0 || max_len > kMaxTokens || max_new < 0 ||
+        max_new > kMaxTokens / (q_heads / c->heads))
+        return QUARTZ_ERR_INVALID_ARG;
+    return QUARTZ_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -158,6 +170,43 @@ int32_t quartz_qk_norm_rope_backward(const quartz_norm_side_t *q, const quartz_n
     a.dev_err = device_error_word();
     if (!a.dev_err) return QUARTZ_ERR_CUDA;
     return map_cuda(launch_head_norm_backward(a, static_cast<cudaStream_t>(stream)));
+}
+
+size_t quartz_paged_attention_tokens_workspace_size(const quartz_paged_cache_t *cache, int64_t tokens, int64_t seqs,
+                                                    int32_t q_heads, int64_t max_len, int64_t max_new)
+{
+    if (check_tokens(cache, tokens, seqs, q_heads, max_len, max_new) != QUARTZ_OK) return 0;
+    return paged_tokens_workspace_bytes(cache, tokens, seqs, q_heads, max_len, max_new);
+}
+
+int32_t quartz_paged_attention_tokens(const void *q, int64_t q_stride_token, int64_t q_stride_head, int64_t tokens,
+                                      int32_t q_heads, const quartz_paged_cache_t *cache, const int32_t *block_table,
+                                      int64_t table_stride, const int32_t *seq_lens, const int32_t *starts,
+                                      int64_t seqs, int64_t max_len, int64_t max_new,
+                                      const quartz_tokens_mask_t *mask, float scale, void *o, int32_t o_type,
+                                      void *workspace, size_t workspace_bytes, void *stream)
+{
+    const int32_t rc = check_tokens(cache, tokens, seqs, q_heads, max_len, max_new);
+    if (rc != QUARTZ_OK) return rc;
+    const quartz_tokens_mask_t m = mask ? *mask : quartz_tokens_mask_t{};
+    constexpr float kLog2e = 1.4426950408889634f;  // the kernels work in the log2 domain
+    if (!type_ok(o_type) || !std::isfinite(scale * kLog2e) || m.window < 0 || !std::isfinite(m.cap * kLog2e) || m.cap < 0.f ||
+        (m.cap > 0.f && !std::isfinite(scale / m.cap)) || (m.tree && max_new > 64))
+        return QUARTZ_ERR_INVALID_ARG;
+    if (!stride_ok(q_stride_token) || !stride_ok(q_stride_head) || !stride_ok(table_stride)) return QUARTZ_ERR_INVALID_ARG;
+    if (q_stride_token % 8 || q_stride_head % 8) return QUARTZ_ERR_ALIGNMENT;
+    if (!aligned(m.tree, 8) || !aligned(m.prefix_lens, 4) || !aligned(m.slopes, 4)) return QUARTZ_ERR_ALIGNMENT;
+    if (seqs == 0 || tokens == 0 || max_new == 0) return QUARTZ_OK;
+    if (!q || !o || !seq_lens || !starts || (max_len > 0 && !block_table)) return QUARTZ_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(o, 16) || !aligned(block_table, 4) || !aligned(seq_lens, 4) || !aligned(starts, 4))
+        return QUARTZ_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < paged_tokens_workspace_bytes(cache, tokens, seqs, q_heads, max_len, max_new))
+        return QUARTZ_ERR_WORKSPACE;
+    if (!aligned(workspace, 16)) return QUARTZ_ERR_ALIGNMENT;
+    PagedTokensCall a{q, q_stride_token, q_stride_head, tokens, q_heads, block_table, table_stride, seq_lens, starts, seqs,
+                      max_len, max_new, m, scale, o, o_type, workspace, device_error_word()};
+    if (!a.dev_err) return QUARTZ_ERR_CUDA;
+    return map_cuda(launch_paged_tokens(cache, a, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -1,0 +1,136 @@
+// Attention of several new tokens over a paged cache: the plan, and the join of
+// tiles that were cut (tokens_attention.cuh has the scheme).
+#include "tokens_attention.cuh"
+
+namespace quartz {
+namespace {
+
+constexpr int kJoinThreads = 256, kJoinRows = 32;
+
+// CTA (x, y): rows 32 y .. of the block that CTA x of the attention began and the
+// next ones went on with, a thread per 4 elements, the parts in the keys' order.
+template <int D>
+__global__ void __launch_bounds__(kJoinThreads) tokens_join_kernel(TokensArgs a, int R)
+{
+    griddep_wait();
+    constexpr int kLanes = D / 4, kGroups = kJoinThreads / kLanes;
+    const TokensJoin j = a.joins[blockIdx.x];
+    if (j.parts < 2) return;
+    const int group = threadIdx.x / kLanes, d = (threadIdx.x - group * kLanes) * 4;
+    if (group >= kGroups) return;
+    const int end = min(j.rows, (static_cast<int>(blockIdx.y) + 1) * kJoinRows);
+    for (int r = blockIdx.y * kJoinRows + group; r < end; r += kGroups) {
+        auto at = [&](int p) {
+            const int64_t cta = blockIdx.x + p;
+            return (2 * cta + (p == 0)) * R + r;
+        };
+        float m = kPagedLow;
+#pragma unroll 4
+        for (int p = 0; p < j.parts; ++p) m = fmaxf(m, a.part_ml[at(p)].x);
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int p = 0; p < j.parts; ++p) {
+            const float2 ml = a.part_ml[at(p)];
+            const float4 u = *reinterpret_cast<const float4 *>(a.part_o + at(p) * D + d);
+            const float f = ex2(ml.x - m);
+            sum += f * ml.y;
+            v.x += f * u.x, v.y += f * u.y, v.z += f * u.z, v.w += f * u.w;
+        }
+        const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;  // NaN stays
+        const int row = j.row0 + r, token = row / a.group;
+        const int64_t out = (static_cast<int64_t>(j.token0 + token) * a.kv_heads * a.group + j.head0 + row - token * a.group) * D + d;
+        paged_store4(a.o, a.o_type, out, make_float4(v.x * inv, v.y * inv, v.z * inv, v.w * inv));
+    }
+}
+
+struct TokensPlan {
+    int tiles, ctas;
+};
+
+// Two tiles side by side where a sequence may have more rows than one holds and
+// TMEM has room for them; a CTA per SM, as long as there may be so many tiles of
+// keys.
+TokensPlan tokens_plan(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len, int64_t max_new)
+{
+    const int64_t group = q_heads / c->heads;
+    TokensPlan p;
+    p.tiles = c->dim <= 128 && max_new * group > 128 ? 2 : 1;
+    const int64_t most = (tokens * group / (128 * p.tiles) + seqs) * c->heads * (max_len / kTokKeys + 2);
+    p.ctas = static_cast<int>(most < device_sms() ? (most > 0 ? most : 1) : device_sms());
+    return p;
+}
+
+size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
+
+}  // namespace
+
+size_t paged_tokens_workspace_bytes(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len,
+                                    int64_t max_new)
+{
+    const TokensPlan p = tokens_plan(c, tokens, seqs, q_heads, max_len, max_new);
+    const size_t rows = static_cast<size_t>(p.ctas) * 2 * 128 * p.tiles;
+    return up256(rows * c->dim * 4) + up256(rows * 8) + up256(p.ctas * sizeof(TokensJoin));
+}
+
+cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokensCall &call, cudaStream_t s)
+{
+    const TokensPlan p = tokens_plan(c, call.tokens, call.seqs, call.q_heads, call.max_len, call.max_new);
+    TokensArgs a{};
+    a.q = static_cast<const uint16_t *>(call.q);
+    a.q_st = call.q_st, a.q_sh = call.q_sh;
+    a.table = call.table, a.table_stride = call.table_stride;
+    a.lens = call.lens, a.starts = call.starts;
+    a.tree = call.mask.tree, a.prefix = call.mask.prefix_lens, a.slopes = call.mask.slopes;
+    const quartz_pages_t *pages[2] = {&c->k, &c->v};
+    PagedSide *side[2] = {&a.k, &a.v};
+    for (int i = 0; i < 2; ++i) {
+        side[i]->data = static_cast<const uint8_t *>(pages[i]->data);
+        side[i]->stride_page = static_cast<uint32_t>(pages[i]->stride_page);
+        side[i]->stride_slot = static_cast<uint32_t>(pages[i]->stride_slot);
+        side[i]->stride_head = pages[i]->stride_head;
+        side[i]->codes = pages[i]->enc.codes;
+        side[i]->flags = pages[i]->enc.flags;
+        side[i]->scales = reinterpret_cast<const __half *>(pages[i]->enc.scales);
+    }
+    a.num_pages = static_cast<uint32_t>(c->num_pages);
+    a.page_shift = log2_of(c->page_size);
+    a.kv_heads = c->heads;
+    a.group = call.q_heads / c->heads;
+    a.seqs = static_cast<int>(call.seqs), a.tokens = static_cast<int>(call.tokens);
+    a.max_len = static_cast<int>(call.max_len), a.max_new = static_cast<int>(call.max_new);
+    a.window = static_cast<int>(call.mask.window < call.max_len ? call.mask.window : 0);
+    a.gs_shift = c->type == QUARTZ_PAGES_ENCODED ? log2_of(c->k.enc.p.group_s) : 0;
+    a.single = call.max_new * a.group <= 128 * p.tiles;
+    a.shaped = call.mask.cap > 0.f || call.mask.slopes || !(call.scale > 0.f);
+    a.scale_log2 = call.scale * kPagedLog2e;
+    if (call.mask.cap > 0.f) a.cap_log2 = call.mask.cap * kPagedLog2e, a.to_cap = call.scale / call.mask.cap;
+    a.o = call.o, a.o_type = call.o_type;
+    a.dev_err = call.dev_err;
+    uint8_t *ws = static_cast<uint8_t *>(call.workspace);
+    const size_t rows = static_cast<size_t>(p.ctas) * 2 * 128 * p.tiles;
+    a.part_o = reinterpret_cast<float *>(ws);
+    ws += up256(rows * c->dim * 4);
+    a.part_ml = reinterpret_cast<float2 *>(ws);
+    ws += up256(rows * 8);
+    a.joins = reinterpret_cast<TokensJoin *>(ws);
+    const dim3 grid(static_cast<unsigned>(p.ctas), static_cast<unsigned>(4 * p.tiles)), block(kJoinThreads);
+    const int R = 128 * p.tiles;
+    cudaError_t e;
+    switch (c->dim) {
+        case 64:
+            e = launch_tokens_attn_64(a, c->type, p.tiles, p.ctas, s);
+            return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<64>, grid, block, 0, s, a, R);
+        case 128:
+            e = launch_tokens_attn_128(a, c->type, p.tiles, p.ctas, s);
+            return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<128>, grid, block, 0, s, a, R);
+        case 192:
+            e = launch_tokens_attn_192(a, c->type, p.tiles, p.ctas, s);
+            return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<192>, grid, block, 0, s, a, R);
+        default:
+            e = launch_tokens_attn_256(a, c->type, p.tiles, p.ctas, s);
+            return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<256>, grid, block, 0, s, a, R);
+    }
+}
+
+}  // namespace quartz

@@ -1,0 +1,977 @@
+// Attention of several new tokens per sequence (prompts, chunks of prompts,
+// trees of drafted tokens) over a paged cache, on the 5th-generation tensor
+// cores:
+//   s = scale q . k, capped, less slope x distance;  p = softmax over the tokens
+//   seen;  o = sum p v
+// in one pass over the keys with the running maximum m and sum l.
+//
+// Rows are (new token, query head) pairs of one key / value head, 128 to a tile:
+// the query heads that share a key head share its loads and fill the tile when
+// tokens are few.  A CTA takes one tile, or two side by side, and goes over the
+// sequence's keys 128 at a time:
+//   S = Q K'    tcgen05.mma from shared memory, 128 x 128 binary32 in TMEM
+//   P           by the softmax warps, 16 bits, over S in TMEM
+//   O += P V    tcgen05.mma, P from TMEM, V as it lies (MN-major)
+// While the softmax warps work on one S the tensor cores make the other: of the
+// other tile (two tiles), or of the next keys (one tile; its columns are halved
+// between the two warpgroups).  O stays in TMEM; it is rescaled only when a
+// maximum rises by more than `slack`, so hardly ever.
+//
+// Warps: 8 softmax; 4 that fill a ring of [128 tokens x 64 or 128 dimensions]
+// units, keys and values in turn, from the pages (asynchronous 16-byte copies
+// into the 128-byte swizzle; encoded pages: decoded to fp16 on the way); one
+// that issues the products; one that loads queries.
+//
+// The keys of all rows' tiles, one behind the other, are cut into one run of
+// equal length per CTA (one CTA per SM), so that lengths, windows and the causal
+// edge leave no SM idle; tiles that a cut goes through are joined by a second
+// kernel, in the order of the keys.
+#pragma once
+
+#include "lzs_f16.cuh"
+#include "paged_attention.cuh"
+
+namespace quartz {
+
+constexpr int kTokSoftmaxWarps = 8, kTokFillWarps = 4;
+constexpr int kTokWarps = kTokSoftmaxWarps + kTokFillWarps + 2, kTokThreads = kTokWarps * 32;
+constexpr int kTokKeys = 128;  // keys of a tile
+constexpr int kTokTreeMost = 64;
+
+struct TokensArgs {
+    const uint16_t *q;
+    int64_t q_st, q_sh;
+    const int32_t *table;
+    int64_t table_stride;
+    const int32_t *lens, *starts;
+    const uint64_t *tree;    // NULL: causal
+    const int32_t *prefix;   // NULL: none
+    const float *slopes;     // NULL: none
+    PagedSide k, v;
+    uint32_t num_pages;
+    int page_shift, kv_heads, group, seqs, tokens, max_len, max_new, window, gs_shift;
+    int single;              // no sequence has more rows than one CTA takes
+    int shaped;              // scores need more than a positive factor
+    float scale_log2;
+    float cap_log2, to_cap;  // cap > 0: cap log2 e and scale / cap; else 0
+    void *o;
+    int o_type;
+    float *part_o;           // [CTA][2][rows][dim]: first (0) or last (1) tile of a CTA, cut
+    float2 *part_ml;         // [CTA][2][rows]: maximum (log2 domain) and sum
+    struct TokensJoin *joins;  // [CTA]
+    int *dev_err;
+};
+
+// A CTA whose last tile goes on in the next CTAs: what the join needs.
+struct TokensJoin {
+    int parts;  // 0: nothing to join
+    int token0, row0, rows, head0;  // rows row0 .. + rows of tokens from token0 on
+};
+
+struct TokensSeq {
+    int n, m, start, base, pre;  // cached, new (0: nothing to do), first row of q, n - m, prefix
+};
+
+__device__ __forceinline__ TokensSeq tokens_seq(const TokensArgs &a, int b)
+{
+    TokensSeq s;
+    const int s1 = a.starts[b + 1];
+    s.start = a.starts[b];
+    s.n = a.lens[b];
+    s.m = s1 - s.start;
+    if (s.start < 0 || s1 < s.start || s1 > a.tokens || s.m > a.max_new || s.n > a.max_len || s.n < s.m) {
+        atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
+        s.n = s.m = s.start = 0;
+    }
+    s.base = s.n - s.m;
+    s.pre = a.prefix ? max(0, min(a.prefix[b], s.n)) : 0;
+    return s;
+}
+
+// What the rows of a block see: [0, pre) and [lo, hi], as `lead` tiles from 0
+// and the rest from tile `first`.
+struct TokensTiles {
+    int lo, hi, lead, first, count;
+    __device__ __forceinline__ int at(int i) const { return i < lead ? i : first + i - lead; }
+};
+
+template <int R>
+__device__ __forceinline__ TokensTiles tokens_tiles(const TokensArgs &a, const TokensSeq &s, int block)
+{
+    TokensTiles t;
+    const int j0 = block * R / a.group, j1 = min(s.m - 1, (block * R + (R - 1)) / a.group);
+    t.lo = a.window > 0 ? max(0, s.base + (a.tree ? 0 : j0) - a.window + 1) : 0;
+    t.hi = s.base + (a.tree ? s.m - 1 : j1);
+    t.lead = (s.pre + kTokKeys - 1) / kTokKeys;
+    t.first = max(t.lead, t.lo / kTokKeys);
+    t.count = t.lead + max(0, t.hi / kTokKeys - t.first + 1);
+    return t;
+}
+
+template <int R>
+__device__ __forceinline__ int tokens_blocks(const TokensArgs &a, const TokensSeq &s) { return (s.m * a.group + R - 1) / R; }
+
+// Tiles of one key head of 32 sequences from b0 on (to b1), each in its lane.
+template <int R>
+__device__ __forceinline__ int tokens_seq_tiles(const TokensArgs &a, int b0, int b1)
+{
+    const int lane = threadIdx.x & 31;
+    TokensSeq s{};
+    if (b0 + lane < b1) s = tokens_seq(a, b0 + lane);
+    if (a.single) return s.m > 0 ? tokens_tiles<R>(a, s, 0).count : 0;
+    int mine = 0;
+    for (int i = 0; i < min(32, b1 - b0); ++i) {
+        TokensSeq t;
+        t.n = __shfl_sync(0xffffffffu, s.n, i), t.m = __shfl_sync(0xffffffffu, s.m, i);
+        t.pre = __shfl_sync(0xffffffffu, s.pre, i), t.base = t.n - t.m, t.start = 0;
+        int sum = 0;
+        for (int r = lane; r < tokens_blocks<R>(a, t); r += 32) sum += tokens_tiles<R>(a, t, r).count;
+        sum = __reduce_add_sync(0xffffffffu, sum);
+        if (lane == i) mine = sum;
+    }
+    return mine;
+}
+
+struct TokensPlace {
+    int b, head, block, off;
+};
+
+struct TokensFind {
+    long long sums[kTokWarps];
+    TokensPlace at;
+};
+
+// Of all tiles of all sequences, heads and row blocks, in that order, this CTA
+// takes [pos, end), which begins at `at`.  (All threads of the CTA.)  False: none.
+template <int R>
+__device__ bool tokens_find(const TokensArgs &a, TokensFind &f, long long &pos, long long &end, long long &chunk)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int share = (a.seqs + kTokWarps - 1) / kTokWarps;
+    const int b0 = min(a.seqs, warp * share), b1 = min(a.seqs, b0 + share);
+    long long sum = 0;
+    for (int b = b0; b < b1; b += 32) {
+        long long t = tokens_seq_tiles<R>(a, b, b1);
+#pragma unroll
+        for (int d = 16; d; d /= 2) t += __shfl_xor_sync(0xffffffffu, t, d);
+        sum += t;
+    }
+    if (lane == 0) f.sums[warp] = sum * a.kv_heads;
+    __syncthreads();
+    long long all = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < kTokWarps; ++w) {
+        if (w < warp) before += f.sums[w];
+        all += f.sums[w];
+    }
+    chunk = (all + gridDim.x - 1) / gridDim.x;
+    pos = chunk * blockIdx.x;
+    end = min(pos + chunk, all);
+    if (pos < end && pos >= before && pos < before + sum * a.kv_heads) {
+        for (int b = b0; b < b1; b += 32) {
+            const int mine = tokens_seq_tiles<R>(a, b, b1);
+            long long incl = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d *= 2) {
+                const long long v = __shfl_up_sync(0xffffffffu, incl, d);
+                if (lane >= d) incl += v;
+            }
+            const unsigned behind = __ballot_sync(0xffffffffu, pos < before + incl * a.kv_heads);
+            if (!behind) {
+                before += __shfl_sync(0xffffffffu, incl, 31) * a.kv_heads;
+                continue;
+            }
+            const int i = __ffs(behind) - 1;
+            const int per_head = __shfl_sync(0xffffffffu, mine, i);
+            const long long in = pos - before - (__shfl_sync(0xffffffffu, incl, i) - per_head) * a.kv_heads;
+            TokensPlace p;
+            p.b = b + i;
+            p.head = static_cast<int>(in / per_head);
+            int rest = static_cast<int>(in - static_cast<long long>(p.head) * per_head);
+            const TokensSeq s = tokens_seq(a, p.b);
+            const int blocks = tokens_blocks<R>(a, s);
+            for (int r0 = 0; r0 < blocks; r0 += 32) {
+                const int n = r0 + lane < blocks ? tokens_tiles<R>(a, s, r0 + lane).count : 0;
+                int sums = n;
+#pragma unroll
+                for (int d = 1; d < 32; d *= 2) {
+                    const int v = __shfl_up_sync(0xffffffffu, sums, d);
+                    if (lane >= d) sums += v;
+                }
+                const unsigned here = __ballot_sync(0xffffffffu, rest < sums);
+                if (here) {
+                    const int j = __ffs(here) - 1;
+                    p.block = r0 + j;
+                    p.off = rest - __shfl_sync(0xffffffffu, sums - n, j);
+                    break;
+                }
+                rest -= __shfl_sync(0xffffffffu, sums, 31);
+            }
+            if (lane == 0) f.at = p;
+            break;
+        }
+    }
+    __syncthreads();
+    return pos < end;
+}
+
+// A CTA's way over its tiles: one row block and the tiles [off, off + count) of
+// it at a time.  Every warp goes it for itself.
+template <int R>
+struct TokensWalk {
+    const TokensArgs &a;
+    long long pos, end;
+    TokensPlace p;
+    TokensSeq s;
+    TokensTiles t;
+    int count;
+
+    __device__ __forceinline__ TokensWalk(const TokensArgs &args, const TokensPlace &at, long long first, long long last)
+        : a(args), pos(first), end(last), p(at)
+    {
+        s = tokens_seq(a, p.b);
+        enter();
+    }
+    __device__ __forceinline__ void enter()
+    {
+        t = tokens_tiles<R>(a, s, p.block);
+        const long long left = end - pos;
+        count = left < t.count - p.off ? static_cast<int>(left) : t.count - p.off;
+    }
+    __device__ __forceinline__ bool more() const { return pos < end; }
+    __device__ __forceinline__ bool begins() const { return p.off == 0; }
+    __device__ __forceinline__ bool ends() const { return p.off + count == t.count; }
+    __device__ __forceinline__ int tile(int i) const { return t.at(p.off + i); }
+    __device__ __forceinline__ int rows() const { return min(R, s.m * a.group - p.block * R); }
+    __device__ __forceinline__ void next()
+    {
+        pos += count;
+        if (pos >= end) return;
+        p.off = 0;  // only the last block may be left before its end
+        if (++p.block >= tokens_blocks<R>(a, s)) {
+            p.block = 0;
+            if (++p.head >= a.kv_heads) {
+                p.head = 0;
+                do s = tokens_seq(a, ++p.b);
+                while (s.m == 0);
+            }
+        }
+        enter();
+    }
+};
+
+template <int D, int TILES>
+struct TokensShape {
+    static constexpr int kRows = 128 * TILES;
+    static constexpr int kUnitDims = D % 128 == 0 ? 128 : 64, kUnits = D / kUnitDims;  // units of a tile's side
+    static constexpr int kPanel = kTokKeys * 128;  // 64 dimensions, 128 bytes a row
+    static constexpr int kUnitBytes = kTokKeys * kUnitDims * 2, kQTile = 128 * D * 2, kQBytes = TILES * kQTile;
+    static constexpr int kMisc = 3072;  // static shared memory, with its padding
+    static constexpr int kFit = (232448 - kMisc - kQBytes) / kUnitBytes;
+    static constexpr int kRing = kFit < 12 ? kFit : 12;
+    static constexpr int kSmem = kQBytes + kRing * kUnitBytes;
+    static_assert(kRing >= 2 * kUnits, "the values of a tile and the next keys are held together");
+    static_assert(256 + TILES * D <= 512, "TMEM: two S, and O");
+};
+
+struct TokensShared {
+    uint64_t full[12], empty[12];
+    uint64_t q_full, q_free, s_full[2], p_ready[2], pv_done[2], swap[4], drain;
+    uint32_t tmem;
+    int abort;
+    TokensFind find;
+    float half[2][2][128];  // one tile: the warpgroups' maxima and sums of a row
+};
+static_assert(sizeof(TokensShared) <= 3072, "");
+
+// tanh of u, good to some 25 half steps of binary32: the series below 1/4 (its
+// next term is 3.3e-7 of the first there), else 1 - 2 / (1 + e^2|u|).
+__device__ __forceinline__ float tokens_tanh(float u)
+{
+    const float q = u * u, size = fabsf(u);
+    const float small = u + u * q * (-0.33333333f + q * (0.13333333f + q * -0.053968254f));
+    const float big = 1.f - __fdividef(2.f, 1.f + ex2(size * 2.8853901f));
+    return size < 0.25f ? small : copysignf(big, u);
+}
+
+// Bits 0 .. 31: columns [a, b] of the 32.
+__device__ __forceinline__ uint32_t tokens_bits(int a, int b)
+{
+    if (a > 31 || b < 0 || a > b) return 0u;
+    const uint32_t up = a <= 0 ? ~0u : ~0u << a, down = b >= 31 ? ~0u : (2u << b) - 1u;
+    return up & down;
+}
+
+// What a row sees of the keys, and how it weighs them.
+struct TokensRow {
+    int lo, hi, pre, pos, base;
+    uint64_t own;  // tree: bits of the new tokens
+    float slope;   // log2 domain
+    const uint64_t *tree;
+    uint64_t some;  // the sequence's new tokens
+
+    // Columns [t0, t0 + 32).
+    __device__ __forceinline__ uint32_t seen(int t0) const
+    {
+        uint32_t v = tokens_bits(lo - t0, hi - t0) | tokens_bits(0, pre - 1 - t0);
+        const int d = t0 - base;
+        if (own && d > -32 && d < 64) v |= static_cast<uint32_t>(d >= 0 ? own >> d : own << -d);
+        return v;
+    }
+    __device__ __forceinline__ int depth(int i) const { return max(0, __popcll(tree[i] & some) - 1); }
+    __device__ __forceinline__ int place(int t) const
+    {
+        return tree && t >= base && t - base < 64 && (some >> (t - base) & 1) ? base + depth(t - base) : t;
+    }
+};
+
+// 32 scores of columns t0 .. to the log2 domain, with cap, distance and mask.
+__device__ __forceinline__ void tokens_shape(const TokensArgs &a, const TokensRow &row, int t0, uint32_t (&s)[32])
+{
+    if (a.cap_log2 > 0.f) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(a.cap_log2 * tokens_tanh(__uint_as_float(s[j]) * a.to_cap));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) * a.scale_log2);
+    }
+    if (a.slopes) {
+        if (row.tree && t0 + 31 >= row.base) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                s[j] = __float_as_uint(__uint_as_float(s[j]) - row.slope * fabsf(static_cast<float>(row.pos - row.place(t0 + j))));
+        } else {
+            const int d = row.pos - t0;
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                s[j] = __float_as_uint(__uint_as_float(s[j]) - row.slope * fabsf(static_cast<float>(d - j)));
+        }
+    }
+    const uint32_t seen = row.seen(t0);
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (!(seen >> j & 1)) s[j] = 0xFF800000u;  // -inf
+}
+
+template <int D, int KIND, int TILES>
+struct TokensKernel {
+    using Shape = TokensShape<D, TILES>;
+    static constexpr int R = Shape::kRows;
+    static constexpr bool kBf = KIND == QUARTZ_PAGES_BF16, kLzs = KIND == QUARTZ_PAGES_ENCODED;
+    // Weights are 2^(score - m + up) up to 2^(up + slack): fp16 keeps those down
+    // to 2^-22 of the largest in full.
+    static constexpr float kUp = kBf ? 0.f : 8.f, kSlack = kBf ? 8.f : 7.f;
+    using Walk = TokensWalk<R>;
+
+    const TokensArgs &a;
+    TokensShared &sh;
+    const TokensPlace at;
+    const long long pos, end, chunk;
+    const uint32_t q_smem, ring, tmem;
+    volatile int *abort;
+
+    __device__ __forceinline__ bool wait(const uint64_t &bar, int phase) const
+    {
+        return mbar_wait_warp(smem_u32(&bar), static_cast<uint32_t>(phase) & 1u, abort, a.dev_err, kWaitLimitNs);
+    }
+    __device__ __forceinline__ uint32_t unit_at(int u) const { return ring + (u % Shape::kRing) * Shape::kUnitBytes; }
+    __device__ __forceinline__ bool wait_full(int u) const { return wait(sh.full[u % Shape::kRing], u / Shape::kRing); }
+    // of the ring's place of unit u, freed by unit u - kRing
+    __device__ __forceinline__ bool wait_empty(int u) const
+    {
+        return u < Shape::kRing || wait(sh.empty[u % Shape::kRing], u / Shape::kRing - 1);
+    }
+
+    // --- queries --------------------------------------------------------------
+    __device__ __forceinline__ void load_queries()
+    {
+        constexpr int kChunks = D / 8, kStep = kChunks >= 32 || kChunks == 24 ? 1 : 32 / kChunks;  // rows at a time
+        const int lane = threadIdx.x & 31, c = kStep == 1 ? lane : lane % kChunks, r_lane = kStep == 1 ? 0 : lane / kChunks;
+        const int dt = kStep / a.group, dg = kStep - dt * a.group;
+        int seg = 0;
+        for (Walk w(a, at, pos, end); w.more(); w.next(), ++seg) {
+            if (seg > 0 && !wait(sh.q_free, seg - 1)) return;
+            const int rows = w.rows(), first = w.p.block * R + r_lane;
+            int token = first / a.group, g = first - token * a.group;
+            const uint16_t *q = a.q + w.s.start * a.q_st + static_cast<int64_t>(w.p.head) * a.group * a.q_sh + c * 8;
+            auto to = [&](int r) {
+                return q_smem + (r / 128) * Shape::kQTile + (c / 8) * Shape::kPanel + (r % 128) * 128 + (((c ^ r) & 7) << 4);
+            };
+            auto step = [&] {
+                token += dt, g += dg;
+                if (g >= a.group) g -= a.group, ++token;
+            };
+            if (c < kChunks) {
+                if constexpr (!kLzs) {
+#pragma unroll 4
+                    for (int r = r_lane; r < rows; r += kStep, step()) cp_async16(to(r), q + token * a.q_st + g * a.q_sh);
+                } else {
+                    // the eight elements of a chunk in the order of the decoded keys
+                    for (int r0 = r_lane; r0 < rows; r0 += 8 * kStep) {
+                        uint4 v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            if (r0 + i * kStep < rows) v[i] = *reinterpret_cast<const uint4 *>(q + token * a.q_st + g * a.q_sh);
+                            step();
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (r0 + i * kStep < rows)
+                                sts_b128(to(r0 + i * kStep),
+                                         make_uint4(prmt(v[i].x, v[i].z, 0x5410), prmt(v[i].x, v[i].z, 0x7632),
+                                                    prmt(v[i].y, v[i].w, 0x5410), prmt(v[i].y, v[i].w, 0x7632)));
+                    }
+                }
+            }
+            cp_async_commit();
+            cp_async_wait<0>();
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.q_full));
+        }
+    }
+
+    // --- keys and values ------------------------------------------------------
+    // Page of token t (-1: not seen by any row, zeros in its place; nothing of
+    // it, which may be infinite or NaN, meets a weight of 0).
+    __device__ __forceinline__ int page_of(const Walk &w, int t, bool &bad) const
+    {
+        if (t >= w.s.n || !(t < w.s.pre || (t >= w.t.lo && t <= w.t.hi))) return -1;
+        const uint32_t page = static_cast<uint32_t>(a.table[w.p.b * a.table_stride + (t >> a.page_shift)]);
+        bad |= page >= a.num_pages;
+        return page < a.num_pages ? static_cast<int>(page) : 0;
+    }
+
+    __device__ __forceinline__ void arrive_full(int u)
+    {
+        fence_proxy_async();
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&sh.full[u % Shape::kRing]));
+    }
+
+    __device__ __forceinline__ void fill_16bit(int warp)
+    {
+        constexpr int kLag = Shape::kRing / 2, kLanes = Shape::kUnitDims / 8, kRowsEach = 32 / kLanes;
+        const int lane = threadIdx.x & 31, c = lane % kLanes, r_lane = lane / kLanes;
+        const uint32_t mask = (1u << a.page_shift) - 1;
+        int u = 0, arrived = 0;
+        bool bad = false, ok = true;
+        auto flush = [&] {
+            cp_async_wait<0>();
+            while (arrived < u) arrive_full(arrived++);
+        };
+        for (Walk w(a, at, pos, end); ok && w.more(); w.next()) {
+            const int row = warp * 32 + lane;
+            int page = page_of(w, w.tile(0) * kTokKeys + row, bad);
+            for (int i = 0; ok && i < w.count; ++i) {
+                const int t = w.tile(i) * kTokKeys + row;
+                const int64_t slot = static_cast<uint32_t>(t) & mask;
+                // element offsets of this lane's token; page -1 marks it
+                const int64_t off[2] = {static_cast<int64_t>(page) * a.k.stride_page + slot * a.k.stride_slot,
+                                        static_cast<int64_t>(page) * a.v.stride_page + slot * a.v.stride_slot};
+                const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
+                if (i + 1 < w.count) page = page_of(w, w.tile(i + 1) * kTokKeys + row, bad);
+#pragma unroll
+                for (int side = 0; side < 2; ++side) {
+                    const PagedSide &p = side ? a.v : a.k;
+                    const uint16_t *base = reinterpret_cast<const uint16_t *>(p.data) + w.p.head * p.stride_head + c * 8;
+#pragma unroll 1
+                    for (int k = 0; k < Shape::kUnits; ++k) {
+                        if (u >= Shape::kRing &&
+                            !__all_sync(0xffffffffu, mbar_try_wait(smem_u32(&sh.empty[u % Shape::kRing]), (u / Shape::kRing - 1) & 1))) {
+                            flush();  // what it waits for may wait for these
+                            if (!(ok = wait_empty(u))) break;
+                        }
+                        const uint32_t to = unit_at(u) + (c / 8) * Shape::kPanel;
+                        const uint16_t *from = base + k * Shape::kUnitDims;
+#pragma unroll
+                        for (int j = 0; j < 32 / kRowsEach; ++j) {
+                            const int src = j * kRowsEach + r_lane, r = warp * 32 + src;
+                            const int64_t o = __shfl_sync(0xffffffffu, off[side], src);
+                            const bool is = there >> src & 1;
+                            cp_async16_or_zero(to + r * 128 + (((c ^ r) & 7) << 4), is ? from + o : from, is ? 16 : 0);
+                        }
+                        cp_async_commit();
+                        ++u;
+                        if (u - arrived > kLag) {
+                            cp_async_wait<kLag>();
+                            arrive_full(arrived++);
+                        }
+                    }
+                    if (!ok) break;
+                }
+            }
+        }
+        flush();
+        if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
+    }
+
+    // A lane's pieces of a unit of encoded rows: 32 elements each.
+    static constexpr int kPieceLanes = Shape::kUnitDims / 32, kPieceRows = 32 / kPieceLanes, kPieces = kPieceLanes;
+    struct Pieces {
+        uint4 codes[kPieces];
+        uint32_t flags[kPieces];  // a byte per 8 elements
+        uint32_t scale[kPieces];  // twice
+    };
+
+    // Rows [kPieceRows i ..) of this warp's 32 tokens; `row` is this lane's token's
+    // row (-1: zeros).
+    __device__ __forceinline__ void load_pieces(const PagedSide &p, int row, int dim0, Pieces &to) const
+    {
+        const int lane = threadIdx.x & 31, c = lane % kPieceLanes;
+        const int e = dim0 + c * 32;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int64_t r = __shfl_sync(0xffffffffu, row, i * kPieceRows + lane / kPieceLanes);
+            to.codes[i] = make_uint4(0u, 0u, 0u, 0u);
+            to.flags[i] = 0, to.scale[i] = 0;
+            if (r >= 0) {
+                to.codes[i] = __ldg(reinterpret_cast<const uint4 *>(p.codes + r * (D / 2) + e / 2));
+                const uint8_t *f = p.flags + r * (D >> a.gs_shift) + (e >> a.gs_shift);
+                if (a.gs_shift == 3) to.flags[i] = __ldg(reinterpret_cast<const uint32_t *>(f));
+                else if (a.gs_shift == 4) to.flags[i] = prmt(__ldg(reinterpret_cast<const uint16_t *>(f)), 0, 0x1100);
+                else to.flags[i] = prmt(__ldg(f), 0, 0x0000);
+                to.scale[i] = prmt(__ldg(reinterpret_cast<const uint16_t *>(p.scales) + r * (D / 64) + e / 64), 0, 0x1010);
+            }
+        }
+    }
+
+    // Decoded to fp16, elements (0, 4), (1, 5), (2, 6), (3, 7) of each eight side
+    // by side.  Codes times 2^FLAG are exact; the product with the scale is
+    // rounded once.
+    __device__ __forceinline__ void store_pieces(const Pieces &p, uint32_t unit, int warp) const
+    {
+        const int lane = threadIdx.x & 31, c = lane % kPieceLanes, flip = (c >> 1) * 2;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+            const int r = warp * 32 + i * kPieceRows + lane / kPieceLanes;
+            const uint32_t w[4] = {p.codes[i].x, p.codes[i].y, p.codes[i].z, p.codes[i].w};
+            const uint32_t to = unit + (c >> 1) * Shape::kPanel + r * 128;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                // lanes of the second panel take the words in another order: other banks
+                const uint32_t word = flip ? w[j ^ 2] : w[j];
+                const uint32_t f = flip ? p.flags[i] >> (8 * (j ^ 2)) & 255 : p.flags[i] >> (8 * j) & 255;
+                uint32_t k[4];
+                key_codes(word, KeyFlag(f), k);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) k[x] = mul_f16x2(k[x], p.scale[i]);
+                const int chunk = (c & 1) * 4 + (j ^ flip);
+                sts_b128(to + (((chunk ^ r) & 7) << 4), make_uint4(k[0], k[1], k[2], k[3]));
+            }
+        }
+    }
+
+    __device__ __forceinline__ void fill_encoded(int warp)
+    {
+        const int lane = threadIdx.x & 31;
+        const int mask = (1 << a.page_shift) - 1;
+        Walk w(a, at, pos, end);
+        bool bad = false;
+        int i = 0, page = page_of(w, w.tile(0) * kTokKeys + warp * 32 + lane, bad), u = 0;
+        Pieces now, next;
+        bool held = false, ok = true;
+        while (ok) {
+            const bool more = w.more();
+            int row = -1;
+            if (more) {
+                const int t = w.tile(i) * kTokKeys + warp * 32 + lane;
+                if (page >= 0) row = ((page * a.kv_heads + w.p.head) << a.page_shift) + (t & mask);
+                if (i + 1 < w.count) {
+                    page = page_of(w, w.tile(i + 1) * kTokKeys + warp * 32 + lane, bad);
+                    ++i;
+                } else {
+                    w.next(), i = 0;
+                    if (w.more()) page = page_of(w, w.tile(0) * kTokKeys + warp * 32 + lane, bad);
+                }
+            }
+#pragma unroll 1
+            for (int k = 0; k < (more ? 2 * Shape::kUnits : 1); ++k) {
+                if (more) load_pieces(k < Shape::kUnits ? a.k : a.v, row, k % Shape::kUnits * Shape::kUnitDims, next);
+                if (held) {
+                    if (!(ok = wait_empty(u))) break;
+                    store_pieces(now, unit_at(u), warp);
+                    arrive_full(u++);
+                }
+                now = next;
+                held = more;
+            }
+            if (!more) break;
+        }
+        if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
+    }
+
+    // --- products -------------------------------------------------------------
+    static constexpr uint32_t kIdescS = idesc_16_f32(kBf, false, 128, kTokKeys);
+    static constexpr uint32_t kIdescO = idesc_16_f32(kBf, true, 128, Shape::kUnitDims);
+
+    // S[buf] = Q[tile] K', the keys in units u ..
+    __device__ __forceinline__ void issue_s(int tile, int buf, int u) const
+    {
+#pragma unroll
+        for (int k = 0; k < Shape::kUnits; ++k)
+#pragma unroll
+            for (int i = 0; i < Shape::kUnitDims / 16; ++i) {
+                const uint32_t in = (i / 4) * Shape::kPanel + (i % 4) * 32;
+                mma_f16_ss(tmem + buf * 128,
+                           sdesc_k_major_sw128(q_smem + tile * Shape::kQTile + k * (Shape::kUnitDims / 64) * Shape::kPanel + in),
+                           sdesc_k_major_sw128(unit_at(u + k) + in), kIdescS, k + i > 0);
+            }
+    }
+    // O[tile] (+)= P[buf] V, the values in units u ..; one tile: P's halves lie
+    // each in its half of S.
+    __device__ __forceinline__ void issue_o(int tile, int buf, int u, bool add) const
+    {
+#pragma unroll
+        for (int k = 0; k < Shape::kUnits; ++k)
+#pragma unroll
+            for (int i = 0; i < kTokKeys / 16; ++i)
+                mma_f16_ts(tmem + 256 + tile * D + k * Shape::kUnitDims,
+                           tmem + buf * 128 + (TILES == 2 ? i * 8 : (i / 4) * 64 + (i % 4) * 8),
+                           sdesc_mn_major_sw128(unit_at(u + k) + i * 2048, Shape::kPanel), kIdescO, add || i > 0);
+    }
+    __device__ __forceinline__ void release(int u) const
+    {
+#pragma unroll
+        for (int k = 0; k < Shape::kUnits; ++k) mma_commit(smem_u32(&sh.empty[(u + k) % Shape::kRing]));
+    }
+    __device__ __forceinline__ bool wait_units(int u) const
+    {
+        for (int k = 0; k < Shape::kUnits; ++k)
+            if (!wait_full(u + k)) return false;
+        return true;
+    }
+
+    __device__ __forceinline__ void products()
+    {
+        const bool leader = elect_one();
+        int it = 0, seg = 0;  // tiles and blocks so far
+        bool ok = true;
+        for (Walk w(a, at, pos, end); ok && w.more(); w.next(), ++seg) {
+            if (!(ok = wait(sh.q_full, seg) && wait_units(2 * Shape::kUnits * it))) break;
+            tc_fence_after();
+            if (leader) {
+                const int u = 2 * Shape::kUnits * it;
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) {
+                    issue_s(t, TILES == 2 ? t : it & 1, u);
+                    mma_commit(smem_u32(&sh.s_full[TILES == 2 ? t : it & 1]));
+                }
+                release(u);
+                if (w.count == 1) mma_commit(smem_u32(&sh.q_free));
+            }
+            for (int i = 0; i < w.count; ++i, ++it) {
+                const int uk = 2 * Shape::kUnits * (it + 1), uv = uk - Shape::kUnits;  // next keys, these values
+                const bool again = i + 1 < w.count, last = i + 2 == w.count;
+                if constexpr (TILES == 2) {
+#pragma unroll
+                    for (int t = 0; t < 2; ++t) {
+                        if (t == 0 && !(ok = wait_units(uv))) break;
+                        if (!(ok = wait(sh.p_ready[t], it))) break;
+                        tc_fence_after();
+                        if (leader) {
+                            issue_o(t, t, uv, i > 0);
+                            mma_commit(smem_u32(&sh.pv_done[t]));
+                            if (t == 1) release(uv);
+                        }
+                        if (!again) continue;
+                        if (t == 0 && !(ok = wait_units(uk))) break;
+                        if (leader) {
+                            issue_s(t, t, uk);
+                            mma_commit(smem_u32(&sh.s_full[t]));
+                            if (t == 1) {
+                                release(uk);
+                                if (last) mma_commit(smem_u32(&sh.q_free));
+                            }
+                        }
+                    }
+                    if (!ok) break;
+                } else {
+                    if (again) {
+                        if (!(ok = wait_units(uk))) break;
+                        if (leader) {
+                            issue_s(0, (it + 1) & 1, uk);
+                            mma_commit(smem_u32(&sh.s_full[(it + 1) & 1]));
+                            release(uk);
+                            if (last) mma_commit(smem_u32(&sh.q_free));
+                        }
+                    }
+                    if (!(ok = wait_units(uv) && wait(sh.p_ready[it & 1], it >> 1))) break;
+                    tc_fence_after();
+                    if (leader) {
+                        issue_o(0, it & 1, uv, i > 0);
+                        mma_commit(smem_u32(&sh.pv_done[0]));
+                        release(uv);
+                    }
+                }
+            }
+        }
+        // every product is done before the CTA gives its memory up
+        if (leader) mma_commit(smem_u32(&sh.drain));
+        volatile int zero = 0;
+        mbar_wait_bounded(smem_u32(&sh.drain), 0, &zero, a.dev_err, kWaitLimitNs);
+    }
+
+    // --- softmax --------------------------------------------------------------
+    // One tile: the two warps of a row exchange a number each.
+    __device__ __forceinline__ bool exchange(int row, int half, float &mine, float &theirs, int &count) const
+    {
+        const int quad = (threadIdx.x >> 5) & 3;
+        sh.half[count & 1][half][row] = mine;
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&sh.swap[quad]));
+        if (!wait(sh.swap[quad], count)) return false;
+        theirs = *reinterpret_cast<volatile float *>(&sh.half[count & 1][half ^ 1][row]);
+        ++count;
+        return true;
+    }
+
+    __device__ __forceinline__ void softmax(int warp)
+    {
+        constexpr int kCols = TILES == 2 ? 128 : 64;     // of S, per thread
+        constexpr int kDims = TILES == 2 ? D : D / 2;    // of O, per thread
+        const int lane = threadIdx.x & 31, wg = warp >> 2, row = (warp & 3) * 32 + lane;
+        const int tile = TILES == 2 ? wg : 0, half = TILES == 2 ? 0 : wg;
+        const uint32_t mine = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
+        const uint32_t o_at = mine + 256 + tile * D + half * kDims;
+        int it = 0, swaps = 0;
+        TokensJoin join{};
+        for (Walk w(a, at, pos, end); w.more(); w.next()) {
+            const int r = w.p.block * R + tile * 128 + row;
+            const bool valid = r < w.s.m * a.group;
+            const int j = valid ? r / a.group : 0, g = valid ? r - j * a.group : 0;
+            TokensRow see;
+            see.base = w.s.base, see.pre = w.s.pre, see.tree = nullptr, see.own = see.some = 0;
+            see.hi = see.pos = w.s.base + j;
+            if (a.tree) {
+                see.tree = a.tree + w.s.start;
+                see.some = w.s.m >= 64 ? ~0ull : (1ull << w.s.m) - 1;
+                see.own = see.tree[j] & see.some;
+                see.pos = w.s.base + see.depth(j);
+                see.hi = w.s.base - 1;
+            }
+            see.lo = a.window > 0 ? max(0, see.pos - a.window + 1) : 0;
+            if (a.tree && a.window > 0 && a.window < kTokTreeMost)
+                for (int i = 0; i < w.s.m; ++i)
+                    if (see.base + see.depth(i) < see.lo) see.own &= ~(1ull << i);
+            see.slope = a.slopes ? a.slopes[w.p.head * a.group + g] * kPagedLog2e : 0.f;
+            float m = kPagedLow, l = 0.f;
+            for (int i = 0; i < w.count; ++i, ++it) {
+                const int buf = TILES == 2 ? tile : it & 1, t0 = w.tile(i) * kTokKeys + half * kCols;
+                const uint32_t s_at = mine + buf * 128 + half * kCols;
+                if (!wait(sh.s_full[buf], TILES == 2 ? it : it >> 1)) return;
+                tc_fence_after();
+                const bool all = !valid || (t0 >= see.lo && t0 + kCols - 1 <= see.hi) || t0 + kCols <= see.pre;
+                const bool shaped = a.shaped || !__all_sync(0xffffffffu, all);
+                float top = -INFINITY;
+                uint32_t s[32];
+                if (!shaped) {
+#pragma unroll
+                    for (int c = 0; c < kCols; c += 32) {
+                        tmem_ld_row(s_at + c, s);
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(s[x]));
+                    }
+                    top *= a.scale_log2;
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < kCols; c += 32) {
+                        tmem_ld_row(s_at + c, s);
+                        tokens_shape(a, see, t0 + c, s);
+                        tmem_st_row(s_at + c, s);
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(s[x]));
+                    }
+                    tmem_wait_st();
+                }
+                if (TILES == 1) {
+                    float other;
+                    if (!exchange(row, half, top, other, swaps)) return;
+                    top = fmaxf(top, other);
+                }
+                if (i == 0) {
+                    m = fmaxf(m, top);
+                } else if (__any_sync(0xffffffffu, top > m + kSlack)) {
+                    const float f = ex2(m - fmaxf(m, top));
+                    m = fmaxf(m, top);
+                    l *= f;
+                    if (!wait(sh.pv_done[tile], it - 1)) return;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < kDims; c += 32) {
+                        tmem_ld_row(o_at + c, s);
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) s[x] = __float_as_uint(__uint_as_float(s[x]) * f);
+                        tmem_st_row(o_at + c, s);
+                    }
+                }
+                const float factor = shaped ? 1.f : a.scale_log2, shift = kUp - m;
+#pragma unroll
+                for (int c = 0; c < kCols; c += 32) {
+                    tmem_ld_row(s_at + c, s);
+                    uint32_t p[16];
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) {
+                        const float p0 = ex2(fmaf(__uint_as_float(s[2 * x]), factor, shift));
+                        const float p1 = ex2(fmaf(__uint_as_float(s[2 * x + 1]), factor, shift));
+                        l += p0 + p1;
+                        if (kBf) {
+                            p[x] = bf16_pair(p0, p1);
+                        } else {
+                            const __half2 h = __floats2half2_rn(p0, p1);
+                            p[x] = *reinterpret_cast<const uint32_t *>(&h);
+                        }
+                    }
+                    tmem_st_row(s_at + c / 2, p);
+                }
+                tmem_wait_st();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[buf]));
+            }
+            // the block's result, or this CTA's part of it; one tile: the product before
+            // the last may be under way too, and a parity tells only one phase from the next
+            if (TILES == 1 && it >= 2 && !wait(sh.pv_done[tile], it - 2)) return;
+            if (!wait(sh.pv_done[tile], it - 1)) return;
+            tc_fence_after();
+            if (TILES == 1) {
+                float other;
+                if (!exchange(row, half, l, other, swaps)) return;
+                l = half ? other + l : l + other;
+            }
+            const bool whole = w.begins() && w.ends();
+            const int slot = 2 * blockIdx.x + w.begins();
+            const int64_t part = static_cast<int64_t>(slot) * R + tile * 128 + row;
+            if (!whole && w.begins()) {
+                join.parts = 1 + static_cast<int>((w.t.count - w.count + chunk - 1) / chunk);
+                join.token0 = w.s.start, join.row0 = w.p.block * R, join.rows = w.rows(), join.head0 = w.p.head * a.group;
+            }
+            if (!whole && valid && half == 0) a.part_ml[part] = make_float2(m, l);
+            const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // NaN stays
+            const int64_t out = (static_cast<int64_t>(w.s.start + j) * a.kv_heads * a.group + w.p.head * a.group + g) * D + half * kDims;
+#pragma unroll 1
+            for (int c = 0; c < kDims; c += 32) {
+                uint32_t s[32];
+                tmem_ld_row(o_at + c, s);
+                if (!valid) continue;
+                float v[32];
+#pragma unroll
+                for (int x = 0; x < 32; ++x) {
+                    // encoded: dimension x is where the decoding puts it
+                    const int from = kLzs ? (x & ~7) + (x & 3) * 2 + (x >> 2 & 1) : x;
+                    v[x] = __uint_as_float(s[from]);
+                }
+                if (!whole) {
+#pragma unroll
+                    for (int x = 0; x < 32; x += 4)
+                        *reinterpret_cast<float4 *>(a.part_o + part * D + half * kDims + c + x) = make_float4(v[x], v[x + 1], v[x + 2], v[x + 3]);
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) v[x] *= inv;
+                    if (a.o_type == QUARTZ_OUT_F32) {
+#pragma unroll
+                        for (int x = 0; x < 32; x += 4) paged_store4<float>(a.o, out + c + x, make_float4(v[x], v[x + 1], v[x + 2], v[x + 3]));
+                    } else {
+#pragma unroll
+                        for (int x = 0; x < 32; x += 8) {
+                            uint32_t h[4];
+#pragma unroll
+                            for (int y = 0; y < 4; ++y) {
+                                if (a.o_type == QUARTZ_OUT_BF16) {
+                                    h[y] = bf16_pair(v[x + 2 * y], v[x + 2 * y + 1]);
+                                } else {
+                                    const __half2 two = __floats2half2_rn(v[x + 2 * y], v[x + 2 * y + 1]);
+                                    h[y] = *reinterpret_cast<const uint32_t *>(&two);
+                                }
+                            }
+                            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.o) + out + c + x) = make_uint4(h[0], h[1], h[2], h[3]);
+                        }
+                    }
+                }
+            }
+            tc_fence_before();
+        }
+        if (threadIdx.x == 0) a.joins[blockIdx.x] = join;
+    }
+};
+
+template <int D, int KIND, int TILES>
+__global__ void __launch_bounds__(kTokThreads, 1) tokens_attn_kernel(TokensArgs a)
+{
+    griddep_wait();
+    using K = TokensKernel<D, KIND, TILES>;
+    using Shape = TokensShape<D, TILES>;
+    extern __shared__ __align__(1024) uint8_t s_tokens[];
+    __shared__ TokensShared sh;
+    const int warp = threadIdx.x >> 5;
+    long long pos, end, chunk;
+    if (!tokens_find<Shape::kRows>(a, sh.find, pos, end, chunk)) {
+        if (threadIdx.x == 0) a.joins[blockIdx.x] = TokensJoin{};
+        return;
+    }
+    if (threadIdx.x == 0) {
+        a.joins[blockIdx.x] = TokensJoin{};  // for a CTA that gives up
+        for (int i = 0; i < Shape::kRing; ++i) {
+            mbar_init(smem_u32(&sh.full[i]), kTokFillWarps);
+            mbar_init(smem_u32(&sh.empty[i]), 1);
+        }
+        mbar_init(smem_u32(&sh.q_full), 1);
+        mbar_init(smem_u32(&sh.q_free), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh.s_full[i]), 1);
+            mbar_init(smem_u32(&sh.p_ready[i]), TILES == 2 ? 4 : 8);
+            mbar_init(smem_u32(&sh.pv_done[i]), 1);
+        }
+        for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&sh.swap[i]), 2);
+        mbar_init(smem_u32(&sh.drain), 1);
+        sh.abort = 0;
+        fence_mbar_init();
+    }
+    if (warp == 0) {
+        tmem_alloc(smem_u32(&sh.tmem), 512);
+        tmem_relinquish();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t q_smem = smem_u32(s_tokens), tmem = *reinterpret_cast<volatile uint32_t *>(&sh.tmem);
+    K k{a, sh, sh.find.at, pos, end, chunk, q_smem, q_smem + Shape::kQBytes, tmem, &sh.abort};
+    if (warp < kTokSoftmaxWarps) {
+        k.softmax(warp);
+    } else if (warp < kTokSoftmaxWarps + kTokFillWarps) {
+        if constexpr (K::kLzs) k.fill_encoded(warp - kTokSoftmaxWarps);
+        else k.fill_16bit(warp - kTokSoftmaxWarps);
+    } else if (warp == kTokSoftmaxWarps + kTokFillWarps) {
+        k.products();
+    } else {
+        k.load_queries();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 0) tmem_dealloc(tmem, 512);
+}
+
+cudaError_t launch_tokens_attn_64(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_128(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_192(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_256(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s);
+
+template <int D, int KIND, int TILES>
+cudaError_t launch_tokens_attn(const TokensArgs &a, int ctas, cudaStream_t s)
+{
+    constexpr int kSmem = TokensShape<D, TILES>::kSmem;
+    const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES>>(kSmem);
+    if (e != cudaSuccess) return e;
+    return launch_pdl(tokens_attn_kernel<D, KIND, TILES>, dim3(static_cast<unsigned>(ctas)), dim3(kTokThreads), kSmem, s, a);
+}
+
+template <int D, int TILES>
+cudaError_t launch_tokens_attn(const TokensArgs &a, int kind, int ctas, cudaStream_t s)
+{
+    if (kind == QUARTZ_PAGES_F16) return launch_tokens_attn<D, QUARTZ_PAGES_F16, TILES>(a, ctas, s);
+    if (kind == QUARTZ_PAGES_BF16) return launch_tokens_attn<D, QUARTZ_PAGES_BF16, TILES>(a, ctas, s);
+    return launch_tokens_attn<D, QUARTZ_PAGES_ENCODED, TILES>(a, ctas, s);
+}
+
+}  // namespace quartz

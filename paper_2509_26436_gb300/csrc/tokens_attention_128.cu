@@ -1,0 +1,12 @@
+// Attention of several new tokens over a paged cache: heads of 128
+// (tokens_attention.cuh).
+#include "tokens_attention.cuh"
+
+namespace quartz {
+
+cudaError_t launch_tokens_attn_128(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s)
+{
+    return tiles == 2 ? launch_tokens_attn<128, 2>(a, kind, ctas, s) : launch_tokens_attn<128, 1>(a, kind, ctas, s);
+}
+
+}  // namespace quartz

@@ -1,0 +1,12 @@
+// Attention of several new tokens over a paged cache: heads of 192
+// (tokens_attention.cuh).
+#include "tokens_attention.cuh"
+
+namespace quartz {
+
+cudaError_t launch_tokens_attn_192(const TokensArgs &a, int kind, int, int ctas, cudaStream_t s)
+{
+    return launch_tokens_attn<192, 1>(a, kind, ctas, s);
+}
+
+}  // namespace quartz

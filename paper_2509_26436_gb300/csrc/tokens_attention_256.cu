@@ -1,0 +1,12 @@
+// Attention of several new tokens over a paged cache: heads of 256
+// (tokens_attention.cuh).
+#include "tokens_attention.cuh"
+
+namespace quartz {
+
+cudaError_t launch_tokens_attn_256(const TokensArgs &a, int kind, int, int ctas, cudaStream_t s)
+{
+    return launch_tokens_attn<256, 1>(a, kind, ctas, s);
+}
+
+}  // namespace quartz

@@ -229,6 +229,16 @@ class PagedCache:
             self._workspace_sizes[key] = n
         return n
 
+    def _tokens_workspace_size(self, tokens, seqs, q_heads, max_len, max_new) -> int:
+        key = (tokens, seqs, q_heads, max_len, max_new, "tokens")
+        n = self._workspace_sizes.get(key)
+        if n is None:
+            if len(self._workspace_sizes) >= 1024:
+                self._workspace_sizes.clear()
+            n = N.load().quartz_paged_attention_tokens_workspace_size(self._ref, tokens, seqs, q_heads, max_len, max_new)
+            self._workspace_sizes[key] = n
+        return n
+
     def _check_device(self) -> int:
         device = _device()
         if self._index != device:

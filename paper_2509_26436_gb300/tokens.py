@@ -1,6 +1,7 @@
 """Several new tokens per sequence: the norm of each head's queries and keys with
-the rotary positions in the same pass (and its gradient), and rotary positions
-of several axes.
+the rotary positions in the same pass (and its gradient), rotary positions of
+several axes, and attention of prompts and of trees of drafted tokens over a
+paged cache.
 
 As paged.py, whose cache and frequencies these go with, this only marshals torch
 CUDA tensors into the C ABI; every call is asynchronous on the current stream
@@ -9,6 +10,8 @@ would be lost is refused.
 
     freqs, scale = rope_frequencies(128, base=500000.0)
     q, k = qk_norm_rope(q, k, wq, wk, positions, freqs, scale=scale)
+    paged_append(cache, k, v, slots)
+    o = attention_paged_tokens(q, cache, block_table, seq_lens, starts, 128 ** -0.5)
     dq, dk, dwq, dwk = qk_norm_rope_backward(gq, gk, q, k, wq, wk, positions, freqs, scale=scale)
 """
 from __future__ import annotations
@@ -21,6 +24,7 @@ from . import _native as N
 from . import paged as P
 
 _byref = C.byref
+_TREE_MOST = 64  # drafted tokens of a sequence: bits of a mask
 
 
 def _no_gradient(name, instead, *tensors):
@@ -212,3 +216,98 @@ def qk_norm_rope_backward(dyq, dyk, q, k, wq, wk, positions=None, freqs=None, ep
 
 def qk_norm_rope_workspace_size(dim: int) -> int:
     return N.load().quartz_qk_norm_rope_workspace_size(dim)
+
+
+# --- attention ----------------------------------------------------------------
+
+def attention_paged_tokens(q, cache: P.PagedCache, block_table, seq_lens, starts, scale: float, tree=None,
+                           prefix_lens=None, window: int = 0, cap: float = 0.0, slopes=None, max_len: int | None = None,
+                           max_new: int | None = None, out_dtype=None, out=None, workspace=None, stream=None):
+    """o [tokens, q_heads, dim]: attention of the new tokens of several sequences,
+    side by side in q [tokens, q_heads, dim] (the cache's type; float16 for
+    encoded pages), over the paged cache, in which they are the last of their
+    sequence already (paged_append).  Rows starts[b] to starts[b + 1] are
+    sequence b's (starts int32 [seqs + 1]; a sequence may have none); rows
+    before the first and behind the last are left as they are in `out`.
+    seq_lens int32 [seqs]: cached tokens, the new ones among them.
+
+    Each sees the tokens up to its own position; with `window` > 0 only those
+    less than `window` before it; and the first prefix_lens[b] tokens whatever
+    their position (int32 [seqs]).  `tree` int64 [tokens]: bit i of a row says
+    that it sees its sequence's drafted token i (itself too, by its own bit),
+    besides the tokens before them all; the position is then that of the last
+    of those plus the number of drafted tokens seen, itself included.  Scores:
+    scale q . k; cap > 0: cap tanh(score / cap); slopes float32 [q_heads]: less
+    slopes[h] times the distance of the positions.  A token that sees nothing
+    gives zeros.
+
+    max_len: at most this many cached tokens (default: what the table holds),
+    max_new: at most this many new ones per sequence (default: all of q; 64 in
+    a tree, which holds no more); known bounds plan better.  Softmax weights
+    are rounded to the cache's type before they multiply the values, whatever
+    out_dtype.  A workspace of the caller's is only good for one call at a time,
+    and for one captured graph."""
+    device = cache._check_device()
+    qs = P._rows("q", q, 3, cache.dtype, device)
+    ts = P._rows("block_table", block_table, 2, P.i32, device)
+    lens, at = P._vector("seq_lens", seq_lens, P.i32, device), P._vector("starts", starts, P.i32, device)
+    T, Hq, D = q.shape
+    B, width = block_table.shape
+    if D != cache.dim or Hq % cache.heads or seq_lens.shape[0] != B or starts.shape[0] != B + 1:
+        raise ValueError("q must be [tokens, a multiple of the cache's heads, dim]; block_table and seq_lens one row per "
+                         "sequence, starts one more")
+    held = width * cache.page_size
+    if max_len is None:
+        max_len = held
+    elif not 0 <= max_len <= held:
+        raise ValueError("max_len must be within what block_table holds")
+    most = T if tree is None else min(T, _TREE_MOST)
+    if max_new is None or max_new > T:
+        max_new = most
+    elif max_new < 0 or max_new > most:
+        raise ValueError("max_new must not be negative, nor above 64 in a tree")
+    m = None
+    if tree is not None or prefix_lens is not None or slopes is not None or window or cap:
+        tp = pp = sp = None
+        if tree is not None:
+            tp = P._vector("tree", tree, P.i64, device)
+            if tree.shape[0] != T:
+                raise ValueError("tree must have one entry per token")
+        if prefix_lens is not None:
+            pp = P._vector("prefix_lens", prefix_lens, P.i32, device)
+            if prefix_lens.shape[0] != B:
+                raise ValueError("prefix_lens must have one entry per sequence")
+        if slopes is not None:
+            sp = P._vector("slopes", slopes, P.f32, device)
+            if slopes.shape[0] != Hq:
+                raise ValueError("slopes must have one entry per query head")
+        m = _byref(N.QuartzTokensMask(tp, pp, sp, window, cap))
+    if out is None:
+        out_dtype = out_dtype or q.dtype
+        o = P._empty((T, Hq, D), out_dtype, cache.device, stream)
+    else:
+        o, out_dtype = out, out.dtype
+        P._rows("out", o, 3, out_dtype, device)
+        if o.shape != q.shape or not o.is_contiguous():
+            raise ValueError("out must be contiguous, of the shape of q")
+    kind = P._KIND.get(out_dtype)
+    if kind is None:
+        raise ValueError("the result is float16, bfloat16 or float32")
+    if workspace is None:
+        size = cache._tokens_workspace_size(T, B, Hq, max_len, max_new)
+        workspace = P._empty(size, P.torch.uint8, cache.device, stream)
+    else:
+        if workspace.get_device() != device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
+        size = workspace.numel() * workspace.element_size()
+    rc = P.lib.quartz_paged_attention_tokens(q.data_ptr(), qs[0], qs[1], T, Hq, cache._ref, block_table.data_ptr(), ts[0],
+                                             lens, at, B, max_len, max_new, m, scale, o.data_ptr(), kind,
+                                             workspace.data_ptr(), size, _Q._stream(stream))
+    if rc:
+        N.check(rc, "quartz_paged_attention_tokens")
+    return o
+
+
+def attention_paged_tokens_workspace_size(cache: P.PagedCache, tokens: int, seqs: int, q_heads: int, max_len: int,
+                                          max_new: int) -> int:
+    return cache._tokens_workspace_size(tokens, seqs, q_heads, max_len, max_new)

@@ -109,3 +109,35 @@ def test_a_gradient_that_would_be_lost_is_refused(lib, name):
                     torch.zeros(32, dtype=torch.int32))
     with pytest.raises(ValueError, match="records no gradient"):
         Q.qk_norm_rope_backward(x, None, x.detach(), None, None, None)
+
+
+def _cache(kind=N.PAGES_F16, page=16, heads=2, dim=128, pages=4, data=P):
+    side = N.QuartzPages()
+    side.data = data
+    side.stride_page, side.stride_slot, side.stride_head = page * heads * dim, heads * dim, dim
+    return N.QuartzPagedCache(kind, page, heads, dim, pages, side, side)
+
+
+def test_attention_refusals(lib):
+    def call(q=P, qs=(256, 128), T=5, Hq=4, cache=None, table=P, lens=P, starts=P, B=2, max_len=64, max_new=5, scale=1.0,
+             o=P, t=0, ws=P, wsb=1 << 40, ts=4, **m):
+        mask = C.byref(N.QuartzTokensMask(**m)) if m else None
+        return lib.quartz_paged_attention_tokens(q, *qs, T, Hq, C.byref(cache or _cache()), table, ts, lens, starts, B,
+                                                 max_len, max_new, mask, scale, o, t, ws, wsb, None)
+
+    assert call(cache=_cache(dim=96)) == UNSUP and call(cache=_cache(data=None)) == BAD and call(cache=_cache(page=24)) == BAD
+    assert call(T=-1) == BAD and call(T=(1 << 30) + 1) == BAD and call(B=-1) == BAD and call(B=65536) == BAD
+    assert call(Hq=3) == BAD and call(Hq=0) == BAD and call(max_len=-1) == BAD and call(max_len=(1 << 30) + 1) == BAD
+    assert call(max_new=-1) == BAD and call(max_new=(1 << 29) + 1) == BAD
+    assert call(scale=math.nan) == BAD and call(scale=math.inf) == BAD and call(scale=3e38) == BAD and call(t=3) == BAD
+    assert call(window=-1) == BAD and call(cap=-1.0) == BAD and call(cap=math.nan) == BAD and call(cap=3e38) == BAD
+    assert call(scale=1e30, cap=1e-30) == BAD and call(tree=P, max_new=65) == BAD
+    assert call(tree=P + 4) == ALIGN and call(prefix_lens=P + 2) == ALIGN and call(slopes=P + 2) == ALIGN
+    assert call(q=None) == BAD and call(o=None) == BAD and call(lens=None) == BAD and call(starts=None) == BAD
+    assert call(table=None) == BAD and call(qs=(-8, 128)) == BAD and call(ts=-1) == BAD
+    assert call(q=P + 2) == ALIGN and call(o=P + 4) == ALIGN and call(qs=(252, 128)) == ALIGN and call(qs=(256, 4)) == ALIGN
+    assert call(lens=P + 2) == ALIGN and call(starts=P + 2) == ALIGN and call(table=P + 2) == ALIGN
+    assert call(ws=None) == WS and call(wsb=0) == WS and call(ws=P + 4) == ALIGN
+    assert call(B=0, q=None) == 0 and call(T=0, q=None) == 0 and call(max_new=0, q=None) == 0
+    assert lib.quartz_paged_attention_tokens_workspace_size(C.byref(_cache(dim=96)), 5, 2, 4, 64, 5) == 0
+    assert lib.quartz_paged_attention_tokens_workspace_size(C.byref(_cache()), 5, 2, 4, 64, 5) > 0

@@ -84,3 +84,86 @@ def norm_grad(x, w, dy, eps, positions, freqs, axis, interleaved, scale):
     rows = x.shape[0] * x.shape[1]
     e_dw = (n.abs() * e_g + (g * n).abs() * (e_r + (3 + rows) * U)).sum((0, 1))
     return dx, dw, e_dx, e_dw
+
+
+# --- attention ----------------------------------------------------------------
+def places(n, m, tree=None):
+    """(positions of the m new tokens, places of the n cached ones)."""
+    base = n - m
+    if tree is None:
+        pos = [base + j for j in range(m)]
+        return pos, list(range(n))
+    pos = [base + max(0, bin(t & ((1 << m) - 1)).count("1") - 1) for t in tree]
+    return pos, list(range(base)) + pos
+
+
+def seen(n, m, tree=None, window=0, prefix=0):
+    """bool [m, n], from the definition, token by token."""
+    base = n - m
+    pos, place = places(n, m, tree)
+    out = torch.zeros((m, n), dtype=torch.bool)
+    t = torch.arange(n)
+    at = torch.tensor(place, dtype=torch.int64)
+    for j in range(m):
+        s = t <= pos[j] if tree is None else (t < base)
+        if tree is not None and m:
+            s[base:] = torch.tensor([(tree[j] >> i) & 1 == 1 for i in range(m)])
+        if window:
+            s = s & (at > pos[j] - window)
+        out[j] = s | (t < prefix)
+    return out
+
+
+def attention(q, k, v, scale, mask, dtype, pos=None, place=None, cap=0.0, slopes=None):
+    """(o, bound) of one sequence: q [m, Hq, D], k and v [n, H, D], mask [m, n].
+
+    A score is off by its products' sum, D + 1 half steps of binary32 of the sum
+    of their sizes, doubled since the tensor cores cut where binary32 rounds;
+    8 half steps of itself for its factors (a cap: 25 of the capped score, and a
+    capped score moves by no more than the score), 4 of the distance's product
+    and the result.  A weight is off by that, by 2^-22 (ex2) and by half a step
+    of the pages' type (relative to the largest: fp16 holds weights from 2^-22
+    of the largest down to 2^-33 of it); sums of n weights, or of n products,
+    by n + 2 half steps, doubled for the tensor cores, and the rescaling and the
+    join by 16 more."""
+    m, Hq, D = q.shape
+    n, H, _ = k.shape
+    G = Hq // H
+    o, bound = torch.zeros((m, Hq, D), dtype=torch.float64), torch.zeros((m, Hq, D), dtype=torch.float64)
+    if n == 0:
+        return o, bound
+    info = torch.finfo(dtype)
+    for h in range(Hq):
+        kk, vv = k[:, h // G].double(), v[:, h // G].double()
+        qq = q[:, h].double()
+        # what is not seen may be anything
+        some = mask.any(0)
+        kk, vv = (torch.where(some[:, None], x, torch.zeros_like(x)) for x in (kk, vv))
+        s = qq @ kk.t() * scale
+        size = qq.abs() @ kk.abs().t() * abs(scale)
+        err = size * 2 * (D + 1) * U + s.abs() * 8 * U
+        if cap:
+            s = cap * torch.tanh(s / cap)
+            err = err + s.abs() * 25 * U
+        if slopes is not None:
+            far = (pos[:, None] - place[None]).abs().double() * float(slopes[h])
+            s = s - far
+            err = err + far.abs() * 4 * U + s.abs() * 4 * U
+        s = s.masked_fill(~mask, -torch.inf)
+        top = s.amax(-1, keepdim=True).clamp(min=-1e300)
+        e = torch.exp(s - top)
+        total = e.sum(-1, keepdim=True)
+        p = torch.where(total > 0, e / total.clamp(min=1e-300), torch.zeros_like(e))
+        err = torch.where(mask, err, torch.zeros_like(err))
+        # the running maximum that all are relative to is off as well: by the largest error
+        rel = err + err.amax(-1, keepdim=True) * 2 ** -20 + (s - top).abs().nan_to_num(0, 0, 0) * 4 * U + 2.0 ** -22
+        rel = rel * 1.01 + info.eps / 2
+        small = 2.0 ** -33 if dtype == torch.float16 else 0.0
+        a = p @ vv.abs()
+        sums = (2 * (n + 2) + 16) * U
+        o[:, h] = p @ vv
+        low = torch.where(mask, torch.full_like(p, small), torch.zeros_like(p)) @ vv.abs()
+        # numerator, and the denominator's part: the weights' own errors without the rounding, as l is not rounded
+        den = (p * (rel - info.eps / 2)).sum(-1, keepdim=True) + sums
+        bound[:, h] = (p * rel) @ vv.abs() + a * (sums + den) * 1.01 + low
+    return o, bound
