@@ -1909,6 +1909,20 @@ __global__ void selftest_timeout_kernel(uint64_t limit_ns, int *dev_err)
 }
 }  // namespace
 
+bool make_pool_map(void *map, bool bf16, const void *base, const uint64_t (&dims)[4], const uint64_t (&strides)[3],
+                   const uint32_t (&box)[4])
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    cuuint64_t d[4], st[3];
+    cuuint32_t b[4], ones[4] = {1, 1, 1, 1};
+    for (int i = 0; i < 4; ++i) d[i] = dims[i], b[i] = box[i];
+    for (int i = 0; i < 3; ++i) st[i] = strides[i];
+    return fn(static_cast<CUtensorMap *>(map), bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4,
+              const_cast<void *>(base), d, st, b, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 cudaError_t launch_selftest_timeout(int64_t limit_ns, int *dev_err, cudaStream_t s)
 {
     selftest_timeout_kernel<<<1, 32, 0, s>>>(static_cast<uint64_t>(limit_ns), dev_err);

@@ -166,6 +166,17 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void *tmap, int3
         : "memory");
 }
 
+// The same of a 4-D tensor.
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int32_t x, int32_t c1, int32_t c2, int32_t c3,
+                                            uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+        "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+        "l"(tmap), "r"(x), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+        : "memory");
+}
+
 // Untiled bulk copy global -> shared of `bytes` bytes (a multiple of 16; both
 // addresses 16-byte aligned), completion counted on `bar` in bytes.
 __device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar)
@@ -364,6 +375,15 @@ __device__ __forceinline__ uint64_t sdesc_sw128(uint32_t addr, uint32_t next)
 __device__ __forceinline__ uint64_t sdesc_k_major_sw128(uint32_t addr) { return sdesc_sw128(addr, 16); }
 __device__ __forceinline__ uint64_t sdesc_mn_major_sw128(uint32_t addr, uint32_t next) { return sdesc_sw128(addr, next); }
 
+// The same from the lower word of one, `more` bytes on.
+__device__ __forceinline__ uint32_t sdesc_low(uint64_t d) { return static_cast<uint32_t>(d); }
+__device__ __forceinline__ uint64_t sdesc_sw128_at(uint32_t low, uint32_t more)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "r"(low + (more >> 4)), "n"((1024u >> 4) | (1u << 14) | (2u << 29)));
+    return d;
+}
+
 // Instruction descriptor of kind::f16: fp16 or (bf) bf16 A and B, A K-major, B
 // K-major or (b_mn) MN-major, fp32 D.
 __host__ __device__ constexpr uint32_t idesc_16_f32(bool bf, bool b_mn, uint32_t M, uint32_t N)
@@ -483,5 +503,45 @@ __device__ __forceinline__ void tmem_st_row(uint32_t t0, const uint32_t (&r)[32]
         : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// The largest of three (NaN ones are not).
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// Two binary32 operations in one instruction, each rounded by itself.
+__device__ __forceinline__ uint64_t pack2(float a, float b)
+{
+    uint64_t d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(a), "f"(b));
+    return d;
+}
+__device__ __forceinline__ float2 unpack2(uint64_t v)
+{
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+    return f;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 
 }  // namespace quartz

@@ -262,6 +262,11 @@ struct PagedAttnCall {
 size_t paged_attention_workspace_bytes(const quartz_paged_cache_t *c, int64_t seqs, int q_heads, int64_t max_len,
                                        int64_t window, bool with_weights);
 cudaError_t launch_paged_attention(const quartz_paged_cache_t *c, const PagedAttnCall &a, cudaStream_t s);
+// A CUtensorMap of a 4-D tensor of 16-bit elements with the 128-byte swizzle
+// (strides of dimensions 1 to 3 in bytes); false: it cannot be described
+// (linear.cu).
+bool make_pool_map(void *map, bool bf16, const void *base, const uint64_t (&dims)[4], const uint64_t (&strides)[3],
+                   const uint32_t (&box)[4]);
 // Several new tokens per sequence (tokens_attention.cu; checks: tokens_api.cu).
 struct PagedTokensCall {
     const void *q;

@@ -1,5 +1,7 @@
 // Attention of several new tokens over a paged cache: the plan, and the join of
 // tiles that were cut (tokens_attention.cuh has the scheme).
+#include <utility>
+
 #include "tokens_attention.cuh"
 
 namespace quartz {
@@ -61,6 +63,34 @@ TokensPlan tokens_plan(const quartz_paged_cache_t *c, int64_t tokens, int64_t se
     return p;
 }
 
+// A side of 16-bit pages as boxes of `rows` slots x 64 dimensions: dimensions 1
+// to 3 are head, slot and page in the order of their strides; `order` says which
+// is which.  False: the map cannot describe it (a stride of 0, say).
+bool pool_map(CUtensorMap *map, const quartz_paged_cache_t *c, const quartz_pages_t &p, int rows, int &order)
+{
+    struct {
+        int64_t stride;
+        uint64_t n;
+        int what;
+    } dim[3] = {{p.stride_head, static_cast<uint64_t>(c->heads), 0},
+                {p.stride_slot, static_cast<uint64_t>(c->page_size), 1},
+                {p.stride_page, static_cast<uint64_t>(c->num_pages), 2}};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (dim[j].stride > dim[j + 1].stride) std::swap(dim[j], dim[j + 1]);
+    uint64_t dims[4] = {static_cast<uint64_t>(c->dim), 0, 0, 0}, strides[3];
+    uint32_t box[4] = {64, 1, 1, 1};
+    order = 0;
+    for (int i = 0; i < 3; ++i) {
+        if (dim[i].stride < c->dim) return false;
+        dims[i + 1] = dim[i].n;
+        strides[i] = static_cast<uint64_t>(dim[i].stride) * 2;
+        if (dim[i].what == 1) box[i + 1] = static_cast<uint32_t>(rows);
+        order |= (i + 1) << (2 * dim[i].what);
+    }
+    return make_pool_map(map, c->type == QUARTZ_PAGES_BF16, p.data, dims, strides, box);
+}
+
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 
 }  // namespace
@@ -114,21 +144,26 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
     a.part_ml = reinterpret_cast<float2 *>(ws);
     ws += up256(rows * 8);
     a.joins = reinterpret_cast<TokensJoin *>(ws);
+    TokensMaps m{};
+    if (c->type != QUARTZ_PAGES_ENCODED && c->page_size >= 8) {
+        const int rows = c->page_size < kTokKeys ? c->page_size : kTokKeys;
+        if (pool_map(&m.k, c, c->k, rows, a.k_order) && pool_map(&m.v, c, c->v, rows, a.v_order)) a.box_rows = rows;
+    }
     const dim3 grid(static_cast<unsigned>(p.ctas), static_cast<unsigned>(4 * p.tiles)), block(kJoinThreads);
     const int R = 128 * p.tiles;
     cudaError_t e;
     switch (c->dim) {
         case 64:
-            e = launch_tokens_attn_64(a, c->type, p.tiles, p.ctas, s);
+            e = launch_tokens_attn_64(a, m, c->type, p.tiles, p.ctas, s);
             return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<64>, grid, block, 0, s, a, R);
         case 128:
-            e = launch_tokens_attn_128(a, c->type, p.tiles, p.ctas, s);
+            e = launch_tokens_attn_128(a, m, c->type, p.tiles, p.ctas, s);
             return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<128>, grid, block, 0, s, a, R);
         case 192:
-            e = launch_tokens_attn_192(a, c->type, p.tiles, p.ctas, s);
+            e = launch_tokens_attn_192(a, m, c->type, p.tiles, p.ctas, s);
             return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<192>, grid, block, 0, s, a, R);
         default:
-            e = launch_tokens_attn_256(a, c->type, p.tiles, p.ctas, s);
+            e = launch_tokens_attn_256(a, m, c->type, p.tiles, p.ctas, s);
             return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<256>, grid, block, 0, s, a, R);
     }
 }

@@ -28,13 +28,16 @@
 // kernel, in the order of the keys.
 #pragma once
 
+#include <cuda.h>
+
 #include "lzs_f16.cuh"
 #include "paged_attention.cuh"
 
 namespace quartz {
 
 constexpr int kTokSoftmaxWarps = 8, kTokFillWarps = 4;
-constexpr int kTokWarps = kTokSoftmaxWarps + kTokFillWarps + 2, kTokThreads = kTokWarps * 32;
+// A last warpgroup: products, queries, two idle warps.
+constexpr int kTokWarps = 16, kTokThreads = kTokWarps * 32;
 constexpr int kTokKeys = 128;  // keys of a tile
 constexpr int kTokTreeMost = 64;
 
@@ -50,6 +53,10 @@ struct TokensArgs {
     PagedSide k, v;
     uint32_t num_pages;
     int page_shift, kv_heads, group, seqs, tokens, max_len, max_new, window, gs_shift;
+    // 16-bit pages of 8 tokens or more that a tensor map describes: rows of a box
+    // (0: none), and which of the map's dimensions 1 .. 3 head, slot and page are
+    int box_rows;
+    int k_order, v_order;
     int single;              // no sequence has more rows than one CTA takes
     int shaped;              // scores need more than a positive factor
     float scale_log2;
@@ -325,32 +332,48 @@ struct TokensRow {
     }
 };
 
-// 32 scores of columns t0 .. to the log2 domain, with cap, distance and mask.
+// Masks of 32 scores of columns t0 ..: -inf where the row does not see.
+__device__ __forceinline__ void tokens_mask(uint32_t seen, uint32_t (&s)[32])
+{
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (!(seen >> j & 1)) s[j] = 0xFF800000u;
+}
+
+// Their factor or cap, and distance: to the log2 domain.
 __device__ __forceinline__ void tokens_shape(const TokensArgs &a, const TokensRow &row, int t0, uint32_t (&s)[32])
 {
     if (a.cap_log2 > 0.f) {
 #pragma unroll
         for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(a.cap_log2 * tokens_tanh(__uint_as_float(s[j]) * a.to_cap));
     } else {
+        const uint64_t scale = pack2(a.scale_log2, a.scale_log2);
 #pragma unroll
-        for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(__uint_as_float(s[j]) * a.scale_log2);
-    }
-    if (a.slopes) {
-        if (row.tree && t0 + 31 >= row.base) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                s[j] = __float_as_uint(__uint_as_float(s[j]) - row.slope * fabsf(static_cast<float>(row.pos - row.place(t0 + j))));
-        } else {
-            const int d = row.pos - t0;
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                s[j] = __float_as_uint(__uint_as_float(s[j]) - row.slope * fabsf(static_cast<float>(d - j)));
+        for (int j = 0; j < 32; j += 2) {
+            const float2 v = unpack2(mul2(pack2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), scale));
+            s[j] = __float_as_uint(v.x), s[j + 1] = __float_as_uint(v.y);
         }
     }
-    const uint32_t seen = row.seen(t0);
+    if (!a.slopes) return;
+    const int d = row.pos - t0;
+    const bool drafted = row.tree && t0 + 31 >= row.base;
+    if (__all_sync(0xffffffffu, d >= 31 && !drafted)) {  // all of them behind the row: no sign to take off
+        const uint64_t far = pack2(static_cast<float>(d), static_cast<float>(d)), slope = pack2(-row.slope, -row.slope);
 #pragma unroll
-    for (int j = 0; j < 32; ++j)
-        if (!(seen >> j & 1)) s[j] = 0xFF800000u;  // -inf
+        for (int j = 0; j < 32; j += 2) {
+            const uint64_t dist = add2(far, pack2(-static_cast<float>(j), -static_cast<float>(j + 1)));
+            const float2 v = unpack2(fma2(dist, slope, pack2(__uint_as_float(s[j]), __uint_as_float(s[j + 1]))));
+            s[j] = __float_as_uint(v.x), s[j + 1] = __float_as_uint(v.y);
+        }
+    } else if (!drafted) {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            s[j] = __float_as_uint(fmaf(-row.slope, fabsf(static_cast<float>(d - j)), __uint_as_float(s[j])));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            s[j] = __float_as_uint(fmaf(-row.slope, fabsf(static_cast<float>(row.pos - row.place(t0 + j))), __uint_as_float(s[j])));
+    }
 }
 
 template <int D, int KIND, int TILES>
@@ -362,6 +385,9 @@ struct TokensKernel {
     // to 2^-22 of the largest in full.
     static constexpr float kUp = kBf ? 0.f : 8.f, kSlack = kBf ? 8.f : 7.f;
     using Walk = TokensWalk<R>;
+    // Registers a thread of the softmax, filling and last warpgroups, of 512 x 128.
+    static constexpr int kSoftmaxRegs = kLzs ? 184 : 192, kFillRegs = kLzs ? 80 : 64, kLastRegs = 64;
+    static_assert(2 * kSoftmaxRegs + kFillRegs + kLastRegs <= 4 * 128, "");
 
     const TokensArgs &a;
     TokensShared &sh;
@@ -369,6 +395,7 @@ struct TokensKernel {
     const long long pos, end, chunk;
     const uint32_t q_smem, ring, tmem;
     volatile int *abort;
+    const void *k_map, *v_map;
 
     __device__ __forceinline__ bool wait(const uint64_t &bar, int phase) const
     {
@@ -432,11 +459,40 @@ struct TokensKernel {
     }
 
     // --- keys and values ------------------------------------------------------
-    // Page of token t (-1: not seen by any row, zeros in its place; nothing of
-    // it, which may be infinite or NaN, meets a weight of 0).
-    __device__ __forceinline__ int page_of(const Walk &w, int t, bool &bad) const
+    // The cached tokens that some new token of the sequence sees: those before
+    // `pre`, and from `lo` on to base (causal: to n); of a tree's drafted ones those
+    // in `own`.
+    struct Loaded {
+        int pre, lo, hi, base;
+        uint64_t own;
+        __device__ __forceinline__ bool all(int t0) const { return t0 + kTokKeys <= pre || (t0 >= lo && t0 + kTokKeys <= hi); }
+        __device__ __forceinline__ bool has(int t) const
+        {
+            return t < pre || (t >= lo && t < hi) || (t >= base && t - base < kTokTreeMost && (own >> (t - base) & 1));
+        }
+    };
+    __device__ __forceinline__ Loaded loaded(const Walk &w) const
     {
-        if (t >= w.s.n || !(t < w.s.pre || (t >= w.t.lo && t <= w.t.hi))) return -1;
+        Loaded l;
+        l.pre = w.s.pre, l.base = w.s.base, l.hi = w.s.n, l.own = 0;
+        l.lo = a.window > 0 ? max(0, w.s.base - a.window + 1) : 0;
+        if (a.tree) {
+            const int lane = threadIdx.x & 31;
+            const uint64_t *tree = a.tree + w.s.start;
+            uint64_t bits = (lane < w.s.m ? tree[lane] : 0) | (lane + 32 < w.s.m ? tree[lane + 32] : 0);
+            if (w.s.m < kTokTreeMost) bits &= (1ull << w.s.m) - 1;
+            const uint32_t low = __reduce_or_sync(0xffffffffu, static_cast<uint32_t>(bits));
+            l.own = static_cast<uint64_t>(__reduce_or_sync(0xffffffffu, static_cast<uint32_t>(bits >> 32))) << 32 | low;
+            l.hi = l.base;
+        }
+        return l;
+    }
+
+    // Page of token t (-1: none sees it; zeros take its place, so that nothing of
+    // it, which may be infinite or NaN, meets a weight of 0).
+    __device__ __forceinline__ int page_of(const Walk &w, const Loaded &l, int t, bool &bad) const
+    {
+        if (!l.has(t)) return -1;
         const uint32_t page = static_cast<uint32_t>(a.table[w.p.b * a.table_stride + (t >> a.page_shift)]);
         bad |= page >= a.num_pages;
         return page < a.num_pages ? static_cast<int>(page) : 0;
@@ -449,11 +505,19 @@ struct TokensKernel {
         if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&sh.full[u % Shape::kRing]));
     }
 
+    // 16-bit pages.  Tiles that are seen whole come by TMA, a box per page and 64
+    // dimensions, dealt to the warps; the others (a sequence's end, a window's
+    // begin; pages that are no boxes) by 16-byte copies with zeros in the rest.
     __device__ __forceinline__ void fill_16bit(int warp)
     {
         constexpr int kLag = Shape::kRing / 2, kLanes = Shape::kUnitDims / 8, kRowsEach = 32 / kLanes;
+        constexpr int kPanels = Shape::kUnitDims / 64;
         const int lane = threadIdx.x & 31, c = lane % kLanes, r_lane = lane / kLanes;
         const uint32_t mask = (1u << a.page_shift) - 1;
+        const int boxes = a.box_rows ? kPanels * (kTokKeys / a.box_rows) : 0, box = warp + 4 * lane;
+        const int box_row = box / kPanels * a.box_rows, panel = box % kPanels;
+        const uint32_t box_to = panel * Shape::kPanel + box_row * 128;
+        const uint32_t box_bytes = static_cast<uint32_t>(max(0, (boxes - warp + 3) / 4) * a.box_rows * 128);
         int u = 0, arrived = 0;
         bool bad = false, ok = true;
         auto flush = [&] {
@@ -461,16 +525,45 @@ struct TokensKernel {
             while (arrived < u) arrive_full(arrived++);
         };
         for (Walk w(a, at, pos, end); ok && w.more(); w.next()) {
-            const int row = warp * 32 + lane;
-            int page = page_of(w, w.tile(0) * kTokKeys + row, bad);
+            const Loaded l = loaded(w);
+            auto lookup = [&](int i) {
+                const int t0 = w.tile(i) * kTokKeys;
+                const bool boxed = boxes && l.all(t0);
+                if (boxed && box >= boxes) return 0;
+                return page_of(w, l, t0 + (boxed ? box_row : warp * 32 + lane), bad);
+            };
+            int page = lookup(0);
             for (int i = 0; ok && i < w.count; ++i) {
-                const int t = w.tile(i) * kTokKeys + row;
-                const int64_t slot = static_cast<uint32_t>(t) & mask;
+                const int t0 = w.tile(i) * kTokKeys, here = page;
+                if (i + 1 < w.count) page = lookup(i + 1);
+                if (boxes && l.all(t0)) {
+                    if (arrived < u) flush();
+                    const int slot = static_cast<int>(static_cast<uint32_t>(t0 + box_row) & mask);
+#pragma unroll
+                    for (int side = 0; side < 2; ++side) {
+                        const int order = side ? a.v_order : a.k_order;  // 2 bits each: head, slot, page
+                        const int c1 = (order & 3) == 1 ? w.p.head : (order >> 2 & 3) == 1 ? slot : here;
+                        const int c2 = (order & 3) == 2 ? w.p.head : (order >> 2 & 3) == 2 ? slot : here;
+                        const int c3 = (order & 3) == 3 ? w.p.head : (order >> 2 & 3) == 3 ? slot : here;
+#pragma unroll 1
+                        for (int k = 0; k < Shape::kUnits; ++k, ++u) {
+                            if (!(ok = wait_empty(u))) break;
+                            const uint32_t bar = smem_u32(&sh.full[u % Shape::kRing]);
+                            if (lane == 0) mbar_arrive_expect_tx(bar, box_bytes);
+                            __syncwarp();
+                            if (box < boxes)
+                                tma_load_4d(unit_at(u) + box_to, side ? v_map : k_map, k * Shape::kUnitDims + panel * 64, c1, c2, c3, bar);
+                        }
+                        if (!ok) break;
+                    }
+                    arrived = u;
+                    continue;
+                }
+                const int64_t slot = static_cast<uint32_t>(t0 + warp * 32 + lane) & mask;
                 // element offsets of this lane's token; page -1 marks it
-                const int64_t off[2] = {static_cast<int64_t>(page) * a.k.stride_page + slot * a.k.stride_slot,
-                                        static_cast<int64_t>(page) * a.v.stride_page + slot * a.v.stride_slot};
-                const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
-                if (i + 1 < w.count) page = page_of(w, w.tile(i + 1) * kTokKeys + row, bad);
+                const int64_t off[2] = {static_cast<int64_t>(here) * a.k.stride_page + slot * a.k.stride_slot,
+                                        static_cast<int64_t>(here) * a.v.stride_page + slot * a.v.stride_slot};
+                const unsigned there = __ballot_sync(0xffffffffu, here >= 0);
 #pragma unroll
                 for (int side = 0; side < 2; ++side) {
                     const PagedSide &p = side ? a.v : a.k;
@@ -484,7 +577,7 @@ struct TokensKernel {
                         }
                         const uint32_t to = unit_at(u) + (c / 8) * Shape::kPanel;
                         const uint16_t *from = base + k * Shape::kUnitDims;
-#pragma unroll
+#pragma unroll 4
                         for (int j = 0; j < 32 / kRowsEach; ++j) {
                             const int src = j * kRowsEach + r_lane, r = warp * 32 + src;
                             const int64_t o = __shfl_sync(0xffffffffu, off[side], src);
@@ -503,14 +596,19 @@ struct TokensKernel {
             }
         }
         flush();
+        if (!ok) {  // a role gave up: no box is left under way when the CTA ends
+            volatile int zero = 0;
+            for (int v = max(0, u - Shape::kRing); v < u; ++v)
+                mbar_wait_bounded(smem_u32(&sh.full[v % Shape::kRing]), (v / Shape::kRing) & 1, &zero, a.dev_err, kWaitLimitNs);
+        }
         if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
     }
 
-    // A lane's pieces of a unit of encoded rows: 32 elements each.
-    static constexpr int kPieceLanes = Shape::kUnitDims / 32, kPieceRows = 32 / kPieceLanes, kPieces = kPieceLanes;
+    // A lane's pieces of a unit of encoded rows: 64 elements each, a scale's.
+    static constexpr int kPieces = Shape::kUnitDims / 64, kPieceRows = 32 / kPieces;
     struct Pieces {
-        uint4 codes[kPieces];
-        uint32_t flags[kPieces];  // a byte per 8 elements
+        uint4 codes[kPieces][2];
+        uint2 flags[kPieces];     // G_s = 8: a byte per 8 elements; 16, 32, 64: the first 4, 2, 1 bytes
         uint32_t scale[kPieces];  // twice
     };
 
@@ -518,19 +616,20 @@ struct TokensKernel {
     // row (-1: zeros).
     __device__ __forceinline__ void load_pieces(const PagedSide &p, int row, int dim0, Pieces &to) const
     {
-        const int lane = threadIdx.x & 31, c = lane % kPieceLanes;
-        const int e = dim0 + c * 32;
+        const int lane = threadIdx.x & 31, e = dim0 + (lane % kPieces) * 64;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int64_t r = __shfl_sync(0xffffffffu, row, i * kPieceRows + lane / kPieceLanes);
-            to.codes[i] = make_uint4(0u, 0u, 0u, 0u);
-            to.flags[i] = 0, to.scale[i] = 0;
+            const int64_t r = __shfl_sync(0xffffffffu, row, i * kPieceRows + lane / kPieces);
+            to.codes[i][0] = to.codes[i][1] = make_uint4(0u, 0u, 0u, 0u);
+            to.flags[i] = make_uint2(0u, 0u), to.scale[i] = 0;
             if (r >= 0) {
-                to.codes[i] = __ldg(reinterpret_cast<const uint4 *>(p.codes + r * (D / 2) + e / 2));
+                const uint4 *c = reinterpret_cast<const uint4 *>(p.codes + r * (D / 2) + e / 2);
+                to.codes[i][0] = __ldg(c), to.codes[i][1] = __ldg(c + 1);
                 const uint8_t *f = p.flags + r * (D >> a.gs_shift) + (e >> a.gs_shift);
-                if (a.gs_shift == 3) to.flags[i] = __ldg(reinterpret_cast<const uint32_t *>(f));
-                else if (a.gs_shift == 4) to.flags[i] = prmt(__ldg(reinterpret_cast<const uint16_t *>(f)), 0, 0x1100);
-                else to.flags[i] = prmt(__ldg(f), 0, 0x0000);
+                if (a.gs_shift == 3) to.flags[i] = __ldg(reinterpret_cast<const uint2 *>(f));
+                else if (a.gs_shift == 4) to.flags[i].x = __ldg(reinterpret_cast<const uint32_t *>(f));
+                else if (a.gs_shift == 5) to.flags[i].x = __ldg(reinterpret_cast<const uint16_t *>(f));
+                else to.flags[i].x = __ldg(f);
                 to.scale[i] = prmt(__ldg(reinterpret_cast<const uint16_t *>(p.scales) + r * (D / 64) + e / 64), 0, 0x1010);
             }
         }
@@ -541,23 +640,29 @@ struct TokensKernel {
     // rounded once.
     __device__ __forceinline__ void store_pieces(const Pieces &p, uint32_t unit, int warp) const
     {
-        const int lane = threadIdx.x & 31, c = lane % kPieceLanes, flip = (c >> 1) * 2;
+        const int lane = threadIdx.x & 31, c = lane % kPieces, flip = c * 4;
 #pragma unroll
         for (int i = 0; i < kPieces; ++i) {
-            const int r = warp * 32 + i * kPieceRows + lane / kPieceLanes;
-            const uint32_t w[4] = {p.codes[i].x, p.codes[i].y, p.codes[i].z, p.codes[i].w};
-            const uint32_t to = unit + (c >> 1) * Shape::kPanel + r * 128;
+            const int r = warp * 32 + i * kPieceRows + lane / kPieces;
+            const uint4 c0 = c ? p.codes[i][1] : p.codes[i][0], c1 = c ? p.codes[i][0] : p.codes[i][1];
+            const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
+            const uint32_t to = unit + c * Shape::kPanel + r * 128;
+            // a byte per 8 elements, in the order of w
+            uint32_t f0 = p.flags[i].x, f1 = p.flags[i].y;
+            if (a.gs_shift == 4) f1 = prmt(f0, 0, 0x3322), f0 = prmt(f0, 0, 0x1100);
+            else if (a.gs_shift == 5) f1 = prmt(f0, 0, 0x1111), f0 = prmt(f0, 0, 0x0000);
+            else if (a.gs_shift == 6) f0 = f1 = prmt(f0, 0, 0x0000);
+            const uint32_t f[2] = {c ? f1 : f0, c ? f0 : f1};
+            KeyFlag flag(0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                // lanes of the second panel take the words in another order: other banks
-                const uint32_t word = flip ? w[j ^ 2] : w[j];
-                const uint32_t f = flip ? p.flags[i] >> (8 * (j ^ 2)) & 255 : p.flags[i] >> (8 * j) & 255;
+            for (int j = 0; j < 8; ++j) {
+                // lanes of the second panel begin with the other half: other banks
+                if (j % 2 == 0 || a.gs_shift == 3) flag = KeyFlag(f[j / 4] >> (j % 4 * 8) & 255);
                 uint32_t k[4];
-                key_codes(word, KeyFlag(f), k);
+                key_codes(w[j], flag, k);
 #pragma unroll
                 for (int x = 0; x < 4; ++x) k[x] = mul_f16x2(k[x], p.scale[i]);
-                const int chunk = (c & 1) * 4 + (j ^ flip);
-                sts_b128(to + (((chunk ^ r) & 7) << 4), make_uint4(k[0], k[1], k[2], k[3]));
+                sts_b128(to + (((j ^ flip ^ r) & 7) << 4), make_uint4(k[0], k[1], k[2], k[3]));
             }
         }
     }
@@ -567,8 +672,9 @@ struct TokensKernel {
         const int lane = threadIdx.x & 31;
         const int mask = (1 << a.page_shift) - 1;
         Walk w(a, at, pos, end);
+        Loaded l = loaded(w);
         bool bad = false;
-        int i = 0, page = page_of(w, w.tile(0) * kTokKeys + warp * 32 + lane, bad), u = 0;
+        int i = 0, page = page_of(w, l, w.tile(0) * kTokKeys + warp * 32 + lane, bad), u = 0;
         Pieces now, next;
         bool held = false, ok = true;
         while (ok) {
@@ -578,11 +684,14 @@ struct TokensKernel {
                 const int t = w.tile(i) * kTokKeys + warp * 32 + lane;
                 if (page >= 0) row = ((page * a.kv_heads + w.p.head) << a.page_shift) + (t & mask);
                 if (i + 1 < w.count) {
-                    page = page_of(w, w.tile(i + 1) * kTokKeys + warp * 32 + lane, bad);
+                    page = page_of(w, l, w.tile(i + 1) * kTokKeys + warp * 32 + lane, bad);
                     ++i;
                 } else {
                     w.next(), i = 0;
-                    if (w.more()) page = page_of(w, w.tile(0) * kTokKeys + warp * 32 + lane, bad);
+                    if (w.more()) {
+                        l = loaded(w);
+                        page = page_of(w, l, w.tile(0) * kTokKeys + warp * 32 + lane, bad);
+                    }
                 }
             }
 #pragma unroll 1
@@ -608,27 +717,31 @@ struct TokensKernel {
     // S[buf] = Q[tile] K', the keys in units u ..
     __device__ __forceinline__ void issue_s(int tile, int buf, int u) const
     {
+        const uint32_t q_low = sdesc_low(sdesc_k_major_sw128(q_smem + tile * Shape::kQTile));
 #pragma unroll
-        for (int k = 0; k < Shape::kUnits; ++k)
+        for (int k = 0; k < Shape::kUnits; ++k) {
+            const uint32_t k_low = sdesc_low(sdesc_k_major_sw128(unit_at(u + k)));
 #pragma unroll
             for (int i = 0; i < Shape::kUnitDims / 16; ++i) {
                 const uint32_t in = (i / 4) * Shape::kPanel + (i % 4) * 32;
-                mma_f16_ss(tmem + buf * 128,
-                           sdesc_k_major_sw128(q_smem + tile * Shape::kQTile + k * (Shape::kUnitDims / 64) * Shape::kPanel + in),
-                           sdesc_k_major_sw128(unit_at(u + k) + in), kIdescS, k + i > 0);
+                mma_f16_ss(tmem + buf * 128, sdesc_sw128_at(q_low, k * (Shape::kUnitDims / 64) * Shape::kPanel + in),
+                           sdesc_sw128_at(k_low, in), kIdescS, k + i > 0);
             }
+        }
     }
     // O[tile] (+)= P[buf] V, the values in units u ..; one tile: P's halves lie
     // each in its half of S.
     __device__ __forceinline__ void issue_o(int tile, int buf, int u, bool add) const
     {
 #pragma unroll
-        for (int k = 0; k < Shape::kUnits; ++k)
+        for (int k = 0; k < Shape::kUnits; ++k) {
+            const uint32_t v_low = sdesc_low(sdesc_mn_major_sw128(unit_at(u + k), Shape::kPanel));
 #pragma unroll
             for (int i = 0; i < kTokKeys / 16; ++i)
                 mma_f16_ts(tmem + 256 + tile * D + k * Shape::kUnitDims,
-                           tmem + buf * 128 + (TILES == 2 ? i * 8 : (i / 4) * 64 + (i % 4) * 8),
-                           sdesc_mn_major_sw128(unit_at(u + k) + i * 2048, Shape::kPanel), kIdescO, add || i > 0);
+                           tmem + buf * 128 + (TILES == 2 ? i * 8 : (i / 4) * 64 + (i % 4) * 8), sdesc_sw128_at(v_low, i * 2048),
+                           kIdescO, add || i > 0);
+        }
     }
     __device__ __forceinline__ void release(int u) const
     {
@@ -761,29 +874,34 @@ struct TokensKernel {
                 const uint32_t s_at = mine + buf * 128 + half * kCols;
                 if (!wait(sh.s_full[buf], TILES == 2 ? it : it >> 1)) return;
                 tc_fence_after();
+                // Masks, and what else the scores need, in place, 32 columns at a time
                 const bool all = !valid || (t0 >= see.lo && t0 + kCols - 1 <= see.hi) || t0 + kCols <= see.pre;
-                const bool shaped = a.shaped || !__all_sync(0xffffffffu, all);
-                float top = -INFINITY;
-                uint32_t s[32];
-                if (!shaped) {
-#pragma unroll
-                    for (int c = 0; c < kCols; c += 32) {
-                        tmem_ld_row(s_at + c, s);
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(s[x]));
-                    }
-                    top *= a.scale_log2;
-                } else {
+                const bool masked = !__all_sync(0xffffffffu, all);
+                if (a.shaped || masked) {
 #pragma unroll 1
                     for (int c = 0; c < kCols; c += 32) {
+                        const uint32_t seen = valid ? see.seen(t0 + c) : ~0u;
+                        const bool mask = masked && __any_sync(0xffffffffu, seen != ~0u);
+                        if (!a.shaped && !mask) continue;
+                        uint32_t s[32];
                         tmem_ld_row(s_at + c, s);
-                        tokens_shape(a, see, t0 + c, s);
+                        if (a.shaped) tokens_shape(a, see, t0 + c, s);
+                        if (mask) tokens_mask(seen, s);
                         tmem_st_row(s_at + c, s);
-#pragma unroll
-                        for (int x = 0; x < 32; ++x) top = fmaxf(top, __uint_as_float(s[x]));
                     }
                     tmem_wait_st();
                 }
+                uint32_t s[kCols];
+                tmem_ld_row(s_at, *reinterpret_cast<uint32_t(*)[64]>(&s[0]));
+                if constexpr (kCols == 128) tmem_ld_row(s_at + 64, *reinterpret_cast<uint32_t(*)[64]>(&s[kCols - 64]));
+                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int x = 0; x < kCols; x += 8)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        tops[y] = max3(tops[y], __uint_as_float(s[x + 2 * y]), __uint_as_float(s[x + 2 * y + 1]));
+                float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                if (!a.shaped) top *= a.scale_log2;
                 if (TILES == 1) {
                     float other;
                     if (!exchange(row, half, top, other, swaps)) return;
@@ -799,31 +917,35 @@ struct TokensKernel {
                     tc_fence_after();
 #pragma unroll 1
                     for (int c = 0; c < kDims; c += 32) {
-                        tmem_ld_row(o_at + c, s);
+                        uint32_t o[32];
+                        tmem_ld_row(o_at + c, o);
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) s[x] = __float_as_uint(__uint_as_float(s[x]) * f);
-                        tmem_st_row(o_at + c, s);
+                        for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+                        tmem_st_row(o_at + c, o);
                     }
                 }
-                const float factor = shaped ? 1.f : a.scale_log2, shift = kUp - m;
+                const float scale = a.shaped ? 1.f : a.scale_log2;
+                const uint64_t factor = pack2(scale, scale), shift = pack2(kUp - m, kUp - m);
+                uint64_t sum[2] = {0, 0};
 #pragma unroll
                 for (int c = 0; c < kCols; c += 32) {
-                    tmem_ld_row(s_at + c, s);
                     uint32_t p[16];
 #pragma unroll
                     for (int x = 0; x < 16; ++x) {
-                        const float p0 = ex2(fmaf(__uint_as_float(s[2 * x]), factor, shift));
-                        const float p1 = ex2(fmaf(__uint_as_float(s[2 * x + 1]), factor, shift));
-                        l += p0 + p1;
+                        float2 e = unpack2(fma2(pack2(__uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1])), factor, shift));
+                        e.x = ex2(e.x), e.y = ex2(e.y);
+                        sum[x & 1] = add2(sum[x & 1], pack2(e.x, e.y));
                         if (kBf) {
-                            p[x] = bf16_pair(p0, p1);
+                            p[x] = bf16_pair(e.x, e.y);
                         } else {
-                            const __half2 h = __floats2half2_rn(p0, p1);
+                            const __half2 h = __floats2half2_rn(e.x, e.y);
                             p[x] = *reinterpret_cast<const uint32_t *>(&h);
                         }
                     }
                     tmem_st_row(s_at + c / 2, p);
                 }
+                const float2 sums = unpack2(add2(sum[0], sum[1]));
+                l += sums.x + sums.y;
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
@@ -896,7 +1018,8 @@ struct TokensKernel {
 };
 
 template <int D, int KIND, int TILES>
-__global__ void __launch_bounds__(kTokThreads, 1) tokens_attn_kernel(TokensArgs a)
+__global__ void __launch_bounds__(kTokThreads, 1)
+    tokens_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, TokensArgs a)
 {
     griddep_wait();
     using K = TokensKernel<D, KIND, TILES>;
@@ -935,16 +1058,18 @@ __global__ void __launch_bounds__(kTokThreads, 1) tokens_attn_kernel(TokensArgs 
     __syncthreads();
     tc_fence_after();
     const uint32_t q_smem = smem_u32(s_tokens), tmem = *reinterpret_cast<volatile uint32_t *>(&sh.tmem);
-    K k{a, sh, sh.find.at, pos, end, chunk, q_smem, q_smem + Shape::kQBytes, tmem, &sh.abort};
+    K k{a, sh, sh.find.at, pos, end, chunk, q_smem, q_smem + Shape::kQBytes, tmem, &sh.abort, &k_map, &v_map};
     if (warp < kTokSoftmaxWarps) {
+        regs_increase<K::kSoftmaxRegs>();
         k.softmax(warp);
     } else if (warp < kTokSoftmaxWarps + kTokFillWarps) {
+        regs_decrease<K::kFillRegs>();
         if constexpr (K::kLzs) k.fill_encoded(warp - kTokSoftmaxWarps);
         else k.fill_16bit(warp - kTokSoftmaxWarps);
-    } else if (warp == kTokSoftmaxWarps + kTokFillWarps) {
-        k.products();
     } else {
-        k.load_queries();
+        regs_decrease<K::kLastRegs>();
+        if (warp == kTokSoftmaxWarps + kTokFillWarps) k.products();
+        else if (warp == kTokSoftmaxWarps + kTokFillWarps + 1) k.load_queries();
     }
     tc_fence_before();
     __syncthreads();
@@ -952,26 +1077,31 @@ __global__ void __launch_bounds__(kTokThreads, 1) tokens_attn_kernel(TokensArgs 
     if (warp == 0) tmem_dealloc(tmem, 512);
 }
 
-cudaError_t launch_tokens_attn_64(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_128(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_192(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_256(const TokensArgs &a, int kind, int tiles, int ctas, cudaStream_t s);
+struct TokensMaps {
+    CUtensorMap k, v;
+};
+
+cudaError_t launch_tokens_attn_64(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_128(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_192(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_256(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
 
 template <int D, int KIND, int TILES>
-cudaError_t launch_tokens_attn(const TokensArgs &a, int ctas, cudaStream_t s)
+cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int ctas, cudaStream_t s)
 {
     constexpr int kSmem = TokensShape<D, TILES>::kSmem;
     const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES>>(kSmem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(tokens_attn_kernel<D, KIND, TILES>, dim3(static_cast<unsigned>(ctas)), dim3(kTokThreads), kSmem, s, a);
+    return launch_pdl(tokens_attn_kernel<D, KIND, TILES>, dim3(static_cast<unsigned>(ctas)), dim3(kTokThreads), kSmem, s, m.k,
+                      m.v, a);
 }
 
 template <int D, int TILES>
-cudaError_t launch_tokens_attn(const TokensArgs &a, int kind, int ctas, cudaStream_t s)
+cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int kind, int ctas, cudaStream_t s)
 {
-    if (kind == QUARTZ_PAGES_F16) return launch_tokens_attn<D, QUARTZ_PAGES_F16, TILES>(a, ctas, s);
-    if (kind == QUARTZ_PAGES_BF16) return launch_tokens_attn<D, QUARTZ_PAGES_BF16, TILES>(a, ctas, s);
-    return launch_tokens_attn<D, QUARTZ_PAGES_ENCODED, TILES>(a, ctas, s);
+    if (kind == QUARTZ_PAGES_F16) return launch_tokens_attn<D, QUARTZ_PAGES_F16, TILES>(a, m, ctas, s);
+    if (kind == QUARTZ_PAGES_BF16) return launch_tokens_attn<D, QUARTZ_PAGES_BF16, TILES>(a, m, ctas, s);
+    return launch_tokens_attn<D, QUARTZ_PAGES_ENCODED, TILES>(a, m, ctas, s);
 }
 
 }  // namespace quartz
