@@ -488,12 +488,13 @@ struct TokensKernel {
         return l;
     }
 
-    // Page of token t (-1: none sees it; zeros take its place, so that nothing of
-    // it, which may be infinite or NaN, meets a weight of 0).
-    __device__ __forceinline__ int page_of(const Walk &w, const Loaded &l, int t, bool &bad) const
+    // Place of token t's page in the table, asked for some time before it is used.
+    __device__ __forceinline__ uint32_t page_entry(const Walk &w, int t, bool there) const
     {
-        if (!l.has(t)) return -1;
-        const uint32_t page = static_cast<uint32_t>(a.table[w.p.b * a.table_stride + (t >> a.page_shift)]);
+        return there ? static_cast<uint32_t>(__ldg(a.table + (w.p.b * a.table_stride + (t >> a.page_shift)))) : 0u;
+    }
+    __device__ __forceinline__ int checked(uint32_t page, bool &bad) const
+    {
         bad |= page >= a.num_pages;
         return page < a.num_pages ? static_cast<int>(page) : 0;
     }
@@ -526,16 +527,21 @@ struct TokensKernel {
         };
         for (Walk w(a, at, pos, end); ok && w.more(); w.next()) {
             const Loaded l = loaded(w);
-            auto lookup = [&](int i) {
+            // of a box, or of this lane's token (not there: none sees it; zeros take its
+            // place, so that nothing of it, which may be infinite or NaN, meets a weight of 0)
+            auto lookup = [&](int i, bool &there) {
                 const int t0 = w.tile(i) * kTokKeys;
                 const bool boxed = boxes && l.all(t0);
-                if (boxed && box >= boxes) return 0;
-                return page_of(w, l, t0 + (boxed ? box_row : warp * 32 + lane), bad);
+                const int t = t0 + (boxed ? box_row : warp * 32 + lane);
+                there = boxed ? box < boxes : l.has(t);
+                return page_entry(w, t, there);
             };
-            int page = lookup(0);
+            bool there_next;
+            uint32_t page_next = lookup(0, there_next);
             for (int i = 0; ok && i < w.count; ++i) {
-                const int t0 = w.tile(i) * kTokKeys, here = page;
-                if (i + 1 < w.count) page = lookup(i + 1);
+                const int t0 = w.tile(i) * kTokKeys, here = checked(page_next, bad);
+                const unsigned there = __ballot_sync(0xffffffffu, there_next);
+                if (i + 1 < w.count) page_next = lookup(i + 1, there_next);
                 if (boxes && l.all(t0)) {
                     if (arrived < u) flush();
                     const int slot = static_cast<int>(static_cast<uint32_t>(t0 + box_row) & mask);
@@ -560,10 +566,9 @@ struct TokensKernel {
                     continue;
                 }
                 const int64_t slot = static_cast<uint32_t>(t0 + warp * 32 + lane) & mask;
-                // element offsets of this lane's token; page -1 marks it
+                // element offsets of this lane's token
                 const int64_t off[2] = {static_cast<int64_t>(here) * a.k.stride_page + slot * a.k.stride_slot,
                                         static_cast<int64_t>(here) * a.v.stride_page + slot * a.v.stride_slot};
-                const unsigned there = __ballot_sync(0xffffffffu, here >= 0);
 #pragma unroll
                 for (int side = 0; side < 2; ++side) {
                     const PagedSide &p = side ? a.v : a.k;
@@ -674,23 +679,29 @@ struct TokensKernel {
         Walk w(a, at, pos, end);
         Loaded l = loaded(w);
         bool bad = false;
-        int i = 0, page = page_of(w, l, w.tile(0) * kTokKeys + warp * 32 + lane, bad), u = 0;
+        int i = 0, u = 0;
+        bool there_next;
+        auto lookup = [&](int i) {
+            const int t = w.tile(i) * kTokKeys + warp * 32 + lane;
+            there_next = l.has(t);
+            return page_entry(w, t, there_next);
+        };
+        uint32_t page_next = lookup(0);
         Pieces now, next;
         bool held = false, ok = true;
         while (ok) {
             const bool more = w.more();
             int row = -1;
             if (more) {
-                const int t = w.tile(i) * kTokKeys + warp * 32 + lane;
-                if (page >= 0) row = ((page * a.kv_heads + w.p.head) << a.page_shift) + (t & mask);
+                const int t = w.tile(i) * kTokKeys + warp * 32 + lane, page = checked(page_next, bad);
+                if (there_next) row = ((page * a.kv_heads + w.p.head) << a.page_shift) + (t & mask);
                 if (i + 1 < w.count) {
-                    page = page_of(w, l, w.tile(i + 1) * kTokKeys + warp * 32 + lane, bad);
-                    ++i;
+                    page_next = lookup(++i);
                 } else {
                     w.next(), i = 0;
                     if (w.more()) {
                         l = loaded(w);
-                        page = page_of(w, l, w.tile(0) * kTokKeys + warp * 32 + lane, bad);
+                        page_next = lookup(0);
                     }
                 }
             }
