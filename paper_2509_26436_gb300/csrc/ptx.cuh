@@ -512,6 +512,13 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return d;
 }
 
+__device__ __forceinline__ float min3(float a, float b, float c)
+{
+    float d;
+    asm("min.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
 // Two binary32 operations in one instruction, each rounded by itself.
 __device__ __forceinline__ uint64_t pack2(float a, float b)
 {

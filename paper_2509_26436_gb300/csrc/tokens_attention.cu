@@ -1,5 +1,6 @@
 // Attention of several new tokens over a paged cache: the plan, and the join of
 // tiles that were cut (tokens_attention.cuh has the scheme).
+#include <cmath>
 #include <utility>
 
 #include "tokens_attention.cuh"
@@ -135,6 +136,7 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
     a.shaped = call.mask.cap > 0.f || call.mask.slopes || !(call.scale > 0.f);
     a.scale_log2 = call.scale * kPagedLog2e;
     if (call.mask.cap > 0.f) a.cap_log2 = call.mask.cap * kPagedLog2e, a.to_cap = call.scale / call.mask.cap;
+    a.cap_near = std::fabs(a.to_cap) > 1e-4f && std::fabs(a.to_cap) < 1e3f;
     a.o = call.o, a.o_type = call.o_type;
     a.dev_err = call.dev_err;
     uint8_t *ws = static_cast<uint8_t *>(call.workspace);
@@ -148,6 +150,12 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
     if (c->type != QUARTZ_PAGES_ENCODED && c->page_size >= 8) {
         const int rows = c->page_size < kTokKeys ? c->page_size : kTokKeys;
         if (pool_map(&m.k, c, c->k, rows, a.k_order) && pool_map(&m.v, c, c->v, rows, a.v_order)) a.box_rows = rows;
+    }
+    if (c->type != QUARTZ_PAGES_ENCODED && 128 % a.group == 0 && call.q_sh >= c->dim && call.q_st >= c->dim) {
+        const uint64_t dims[4] = {static_cast<uint64_t>(c->dim), static_cast<uint64_t>(call.q_heads), static_cast<uint64_t>(call.tokens), 1};
+        const uint64_t strides[3] = {static_cast<uint64_t>(call.q_sh) * 2, static_cast<uint64_t>(call.q_st) * 2, static_cast<uint64_t>(call.q_st) * 2};
+        const uint32_t box[4] = {64, static_cast<uint32_t>(a.group), static_cast<uint32_t>(128 / a.group), 1};
+        a.q_box = make_pool_map(&m.q, c->type == QUARTZ_PAGES_BF16, call.q, dims, strides, box);
     }
     const dim3 grid(static_cast<unsigned>(p.ctas), static_cast<unsigned>(4 * p.tiles)), block(kJoinThreads);
     const int R = 128 * p.tiles;

@@ -12,15 +12,16 @@
 //   S = Q K'    tcgen05.mma from shared memory, 128 x 128 binary32 in TMEM
 //   P           by the softmax warps, 16 bits, over S in TMEM
 //   O += P V    tcgen05.mma, P from TMEM, V as it lies (MN-major)
-// While the softmax warps work on one S the tensor cores make the other: of the
-// other tile (two tiles), or of the next keys (one tile; its columns are halved
-// between the two warpgroups).  O stays in TMEM; it is rescaled only when a
-// maximum rises by more than `slack`, so hardly ever.
+// While the softmax warps work on one S the tensor cores make the other.  There
+// are two softmax warpgroups, a thread per row: two tiles have one each; with one
+// tile they take its keys in turn and hand the maximum on as soon as it is known.
+// O stays in TMEM; it is rescaled only when a maximum rises by more than `slack`,
+// so hardly ever.
 //
 // Warps: 8 softmax; 4 that fill a ring of [128 tokens x 64 or 128 dimensions]
-// units, keys and values in turn, from the pages (asynchronous 16-byte copies
-// into the 128-byte swizzle; encoded pages: decoded to fp16 on the way); one
-// that issues the products; one that loads queries.
+// units, keys and values in turn, from the pages (TMA or 16-byte copies, into the
+// 128-byte swizzle; encoded pages: decoded to fp16 on the way); one that issues
+// the products; three that load queries.
 //
 // The keys of all rows' tiles, one behind the other, are cut into one run of
 // equal length per CTA (one CTA per SM), so that lengths, windows and the causal
@@ -36,8 +37,8 @@
 namespace quartz {
 
 constexpr int kTokSoftmaxWarps = 8, kTokFillWarps = 4;
-// A last warpgroup: products, queries, two idle warps.
-constexpr int kTokWarps = 16, kTokThreads = kTokWarps * 32;
+constexpr int kTokQueryWarps = 3;
+constexpr int kTokWarps = kTokSoftmaxWarps + kTokFillWarps + 1 + kTokQueryWarps, kTokThreads = kTokWarps * 32;
 constexpr int kTokKeys = 128;  // keys of a tile
 constexpr int kTokTreeMost = 64;
 
@@ -57,8 +58,10 @@ struct TokensArgs {
     // (0: none), and which of the map's dimensions 1 .. 3 head, slot and page are
     int box_rows;
     int k_order, v_order;
+    int q_box;  // a box of the queries' map is a tile's rows and 64 dimensions
     int single;              // no sequence has more rows than one CTA takes
     int shaped;              // scores need more than a positive factor
+    int cap_near;            // the powers of to_cap fit binary32: the cap's short polynomial may be used
     float scale_log2;
     float cap_log2, to_cap;  // cap > 0: cap log2 e and scale / cap; else 0
     void *o;
@@ -283,22 +286,30 @@ struct TokensShape {
 
 struct TokensShared {
     uint64_t full[12], empty[12];
-    uint64_t q_full, q_free, s_full[2], p_ready[2], pv_done[2], swap[4], drain;
+    uint64_t q_full, q_free, s_full[2], p_ready[2], pv_done[2], swap[4], hand[8], o_done, o_free, drain;
     uint32_t tmem;
     int abort;
     TokensFind find;
-    float half[2][2][128];  // one tile: the warpgroups' maxima and sums of a row
+    float m[2][128], l[2][128];  // one tile: a row's maximum and sum, by warpgroup
 };
 static_assert(sizeof(TokensShared) <= 3072, "");
 
-// tanh of u, good to some 25 half steps of binary32: the series below 1/4 (its
-// next term is 3.3e-7 of the first there), else 1 - 2 / (1 + e^2|u|).
+// tanh of u, |u| <= 1, good to 3 half steps of binary32: an odd polynomial fitted
+// to the least largest relative error (5e-8); above, 1 - 2 / (1 + e^2|u|).
+__device__ __forceinline__ constexpr float tokens_tanh_term(int i)
+{
+    constexpr float c[7] = {0.99999994f, -0.3333284f, 0.13325204f, -0.05345702f, 0.020289967f, -0.006203367f, 0.0010410185f};
+    return c[i];
+}
+
 __device__ __forceinline__ float tokens_tanh(float u)
 {
     const float q = u * u, size = fabsf(u);
-    const float small = u + u * q * (-0.33333333f + q * (0.13333333f + q * -0.053968254f));
+    float p = tokens_tanh_term(6);
+#pragma unroll
+    for (int i = 5; i >= 0; --i) p = fmaf(p, q, tokens_tanh_term(i));
     const float big = 1.f - __fdividef(2.f, 1.f + ex2(size * 2.8853901f));
-    return size < 0.25f ? small : copysignf(big, u);
+    return size <= 1.f ? p * u : copysignf(big, u);
 }
 
 // Bits 0 .. 31: columns [a, b] of the 32.
@@ -341,38 +352,58 @@ __device__ __forceinline__ void tokens_mask(uint32_t seen, uint32_t (&s)[32])
 }
 
 // Their factor or cap, and distance: to the log2 domain.
-__device__ __forceinline__ void tokens_shape(const TokensArgs &a, const TokensRow &row, int t0, uint32_t (&s)[32])
+__device__ __forceinline__ void tokens_shape(const TokensArgs &a, const TokensRow &row, bool valid, int t0, uint32_t (&s)[32])
 {
+    const float by = a.cap_log2 > 0.f ? a.to_cap : a.scale_log2;
+    const uint64_t factor = pack2(by, by);
+    uint64_t v[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) v[j] = mul2(pack2(__uint_as_float(s[2 * j]), __uint_as_float(s[2 * j + 1])), factor);
     if (a.cap_log2 > 0.f) {
+        float most = 0.f;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) s[j] = __float_as_uint(a.cap_log2 * tokens_tanh(__uint_as_float(s[j]) * a.to_cap));
-    } else {
-        const uint64_t scale = pack2(a.scale_log2, a.scale_log2);
+        for (int j = 0; j < 16; ++j) most = max3(most, fabsf(unpack2(v[j]).x), fabsf(unpack2(v[j]).y));
+        const uint64_t cap = pack2(a.cap_log2, a.cap_log2);
+        if (__all_sync(0xffffffffu, !valid || most <= 1.f)) {
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            const float2 v = unpack2(mul2(pack2(__uint_as_float(s[j]), __uint_as_float(s[j + 1])), scale));
-            s[j] = __float_as_uint(v.x), s[j + 1] = __float_as_uint(v.y);
+            for (int j = 0; j < 16; ++j) {
+                const uint64_t q = mul2(v[j], v[j]);
+                uint64_t p = pack2(tokens_tanh_term(6), tokens_tanh_term(6));
+#pragma unroll
+                for (int i = 5; i >= 0; --i) p = fma2(p, q, pack2(tokens_tanh_term(i), tokens_tanh_term(i)));
+                v[j] = mul2(mul2(p, v[j]), cap);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[j] = mul2(pack2(tokens_tanh(unpack2(v[j]).x), tokens_tanh(unpack2(v[j]).y)), cap);
         }
     }
-    if (!a.slopes) return;
-    const int d = row.pos - t0;
-    const bool drafted = row.tree && t0 + 31 >= row.base;
-    if (__all_sync(0xffffffffu, d >= 31 && !drafted)) {  // all of them behind the row: no sign to take off
-        const uint64_t far = pack2(static_cast<float>(d), static_cast<float>(d)), slope = pack2(-row.slope, -row.slope);
+    if (a.slopes) {
+        const bool drafted = row.tree && t0 + 31 >= row.base;
+        if (!drafted) {
+            const int d = row.pos - t0;
+            const float far = static_cast<float>(d);
+            const uint64_t from = pack2(far, far), slope = pack2(-row.slope, -row.slope);
+            const bool behind = __all_sync(0xffffffffu, d >= 31);  // no sign to take off
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-            const uint64_t dist = add2(far, pack2(-static_cast<float>(j), -static_cast<float>(j + 1)));
-            const float2 v = unpack2(fma2(dist, slope, pack2(__uint_as_float(s[j]), __uint_as_float(s[j + 1]))));
-            s[j] = __float_as_uint(v.x), s[j + 1] = __float_as_uint(v.y);
+            for (int j = 0; j < 16; ++j) {
+                uint64_t dist = add2(from, pack2(-2.f * j, -2.f * j - 1.f));
+                if (!behind) dist &= 0x7FFFFFFF7FFFFFFFull;
+                v[j] = fma2(dist, slope, v[j]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float2 dist = make_float2(fabsf(static_cast<float>(row.pos - row.place(t0 + 2 * j))),
+                                                fabsf(static_cast<float>(row.pos - row.place(t0 + 2 * j + 1))));
+                v[j] = fma2(pack2(dist.x, dist.y), pack2(-row.slope, -row.slope), v[j]);
+            }
         }
-    } else if (!drafted) {
+    }
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
-            s[j] = __float_as_uint(fmaf(-row.slope, fabsf(static_cast<float>(d - j)), __uint_as_float(s[j])));
-    } else {
-#pragma unroll
-        for (int j = 0; j < 32; ++j)
-            s[j] = __float_as_uint(fmaf(-row.slope, fabsf(static_cast<float>(row.pos - row.place(t0 + j))), __uint_as_float(s[j])));
+    for (int j = 0; j < 16; ++j) {
+        const float2 f = unpack2(v[j]);
+        s[2 * j] = __float_as_uint(f.x), s[2 * j + 1] = __float_as_uint(f.y);
     }
 }
 
@@ -386,7 +417,7 @@ struct TokensKernel {
     static constexpr float kUp = kBf ? 0.f : 8.f, kSlack = kBf ? 8.f : 7.f;
     using Walk = TokensWalk<R>;
     // Registers a thread of the softmax, filling and last warpgroups, of 512 x 128.
-    static constexpr int kSoftmaxRegs = kLzs ? 184 : 192, kFillRegs = kLzs ? 80 : 64, kLastRegs = 64;
+    static constexpr int kSoftmaxRegs = 152, kFillRegs = kLzs ? 128 : 104, kLastRegs = kLzs ? 80 : 104;
     static_assert(2 * kSoftmaxRegs + kFillRegs + kLastRegs <= 4 * 128, "");
 
     const TokensArgs &a;
@@ -395,7 +426,7 @@ struct TokensKernel {
     const long long pos, end, chunk;
     const uint32_t q_smem, ring, tmem;
     volatile int *abort;
-    const void *k_map, *v_map;
+    const void *k_map, *v_map, *q_map;
 
     __device__ __forceinline__ bool wait(const uint64_t &bar, int phase) const
     {
@@ -410,15 +441,34 @@ struct TokensKernel {
     }
 
     // --- queries --------------------------------------------------------------
-    __device__ __forceinline__ void load_queries()
+    // A box per tile and 64 dimensions where the heads of a token fill a tile in
+    // whole tokens (rows behind the sequence's are others' or zeros, and weigh on
+    // nothing); else 16 bytes a lane.
+    __device__ __forceinline__ void load_queries(int warp)
     {
-        constexpr int kChunks = D / 8, kStep = kChunks >= 32 || kChunks == 24 ? 1 : 32 / kChunks;  // rows at a time
-        const int lane = threadIdx.x & 31, c = kStep == 1 ? lane : lane % kChunks, r_lane = kStep == 1 ? 0 : lane / kChunks;
+        constexpr int kChunks = D / 8, kEach = kChunks >= 32 || kChunks == 24 ? 1 : 32 / kChunks;  // rows at a time
+        constexpr int kStep = kEach * kTokQueryWarps;
+        const int lane = threadIdx.x & 31, c = kEach == 1 ? lane : lane % kChunks;
+        const int r_first = warp * kEach + (kEach == 1 ? 0 : lane / kChunks);
         const int dt = kStep / a.group, dg = kStep - dt * a.group;
         int seg = 0;
         for (Walk w(a, at, pos, end); w.more(); w.next(), ++seg) {
-            if (seg > 0 && !wait(sh.q_free, seg - 1)) return;
-            const int rows = w.rows(), first = w.p.block * R + r_lane;
+            if (seg > 0 && !wait(sh.q_free, seg - 1)) break;
+            const int rows = w.rows();
+            if (!kLzs && a.q_box) {
+                const int boxes = (rows + 127) / 128 * (D / 64), tile = lane / (D / 64), panel = lane - tile * (D / 64);
+                const uint32_t bar = smem_u32(&sh.q_full);
+                if (lane == 0) {
+                    if (warp == 0) mbar_arrive_expect_tx(bar, boxes * Shape::kPanel);
+                    else mbar_arrive(bar);
+                }
+                __syncwarp();
+                if (warp == 0 && lane < boxes)
+                    tma_load_4d(q_smem + tile * Shape::kQTile + panel * Shape::kPanel, q_map, panel * 64, w.p.head * a.group,
+                                w.s.start + (w.p.block * R + tile * 128) / a.group, 0, bar);
+                continue;
+            }
+            const int first = w.p.block * R + r_first;
             int token = first / a.group, g = first - token * a.group;
             const uint16_t *q = a.q + w.s.start * a.q_st + static_cast<int64_t>(w.p.head) * a.group * a.q_sh + c * 8;
             auto to = [&](int r) {
@@ -431,10 +481,10 @@ struct TokensKernel {
             if (c < kChunks) {
                 if constexpr (!kLzs) {
 #pragma unroll 4
-                    for (int r = r_lane; r < rows; r += kStep, step()) cp_async16(to(r), q + token * a.q_st + g * a.q_sh);
+                    for (int r = r_first; r < rows; r += kStep, step()) cp_async16(to(r), q + token * a.q_st + g * a.q_sh);
                 } else {
                     // the eight elements of a chunk in the order of the decoded keys
-                    for (int r0 = r_lane; r0 < rows; r0 += 8 * kStep) {
+                    for (int r0 = r_first; r0 < rows; r0 += 8 * kStep) {
                         uint4 v[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
@@ -455,6 +505,10 @@ struct TokensKernel {
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.q_full));
+        }
+        if (!kLzs && a.q_box && warp == 0 && *abort) {  // as in fill_16bit
+            volatile int zero = 0;
+            if (seg > 0) mbar_wait_bounded(smem_u32(&sh.q_full), (seg - 1) & 1, &zero, a.dev_err, kWaitLimitNs);
         }
     }
 
@@ -613,8 +667,8 @@ struct TokensKernel {
     static constexpr int kPieces = Shape::kUnitDims / 64, kPieceRows = 32 / kPieces;
     struct Pieces {
         uint4 codes[kPieces][2];
-        uint2 flags[kPieces];     // G_s = 8: a byte per 8 elements; 16, 32, 64: the first 4, 2, 1 bytes
-        uint32_t scale[kPieces];  // twice
+        uint2 flags[kPieces];  // G_s = 8: a byte per 8 elements; 16, 32, 64: the first 4, 2, 1 bytes
+        uint16_t scale[kPieces];
     };
 
     // Rows [kPieceRows i ..) of this warp's 32 tokens; `row` is this lane's token's
@@ -635,7 +689,7 @@ struct TokensKernel {
                 else if (a.gs_shift == 4) to.flags[i].x = __ldg(reinterpret_cast<const uint32_t *>(f));
                 else if (a.gs_shift == 5) to.flags[i].x = __ldg(reinterpret_cast<const uint16_t *>(f));
                 else to.flags[i].x = __ldg(f);
-                to.scale[i] = prmt(__ldg(reinterpret_cast<const uint16_t *>(p.scales) + r * (D / 64) + e / 64), 0, 0x1010);
+                to.scale[i] = __ldg(reinterpret_cast<const uint16_t *>(p.scales) + r * (D / 64) + e / 64);
             }
         }
     }
@@ -658,6 +712,7 @@ struct TokensKernel {
             else if (a.gs_shift == 5) f1 = prmt(f0, 0, 0x1111), f0 = prmt(f0, 0, 0x0000);
             else if (a.gs_shift == 6) f0 = f1 = prmt(f0, 0, 0x0000);
             const uint32_t f[2] = {c ? f1 : f0, c ? f0 : f1};
+            const uint32_t scale = prmt(p.scale[i], 0, 0x1010);
             KeyFlag flag(0);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -666,7 +721,7 @@ struct TokensKernel {
                 uint32_t k[4];
                 key_codes(w[j], flag, k);
 #pragma unroll
-                for (int x = 0; x < 4; ++x) k[x] = mul_f16x2(k[x], p.scale[i]);
+                for (int x = 0; x < 4; ++x) k[x] = mul_f16x2(k[x], scale);
                 sts_b128(to + (((j ^ flip ^ r) & 7) << 4), make_uint4(k[0], k[1], k[2], k[3]));
             }
         }
@@ -740,8 +795,7 @@ struct TokensKernel {
             }
         }
     }
-    // O[tile] (+)= P[buf] V, the values in units u ..; one tile: P's halves lie
-    // each in its half of S.
+    // O[tile] (+)= P[buf] V, the values in units u ..
     __device__ __forceinline__ void issue_o(int tile, int buf, int u, bool add) const
     {
 #pragma unroll
@@ -750,7 +804,7 @@ struct TokensKernel {
 #pragma unroll
             for (int i = 0; i < kTokKeys / 16; ++i)
                 mma_f16_ts(tmem + 256 + tile * D + k * Shape::kUnitDims,
-                           tmem + buf * 128 + (TILES == 2 ? i * 8 : (i / 4) * 64 + (i % 4) * 8), sdesc_sw128_at(v_low, i * 2048),
+                           tmem + buf * 128 + i * 8, sdesc_sw128_at(v_low, i * 2048),
                            kIdescO, add || i > 0);
         }
     }
@@ -821,11 +875,13 @@ struct TokensKernel {
                         }
                     }
                     if (!(ok = wait_units(uv) && wait(sh.p_ready[it & 1], it >> 1))) break;
+                    if (i == 0 && seg > 0 && !(ok = wait(sh.o_free, seg - 1))) break;
                     tc_fence_after();
                     if (leader) {
                         issue_o(0, it & 1, uv, i > 0);
                         mma_commit(smem_u32(&sh.pv_done[0]));
                         release(uv);
+                        if (!again) mma_commit(smem_u32(&sh.o_done));
                     }
                 }
             }
@@ -837,30 +893,34 @@ struct TokensKernel {
     }
 
     // --- softmax --------------------------------------------------------------
-    // One tile: the two warps of a row exchange a number each.
-    __device__ __forceinline__ bool exchange(int row, int half, float &mine, float &theirs, int &count) const
+    // One tile: the two warps that have a row's sums add them up.  The barrier's
+    // phases are in turn: written, read.
+    __device__ __forceinline__ bool add_sums(int row, int wg, float &l, int &count) const
     {
-        const int quad = (threadIdx.x >> 5) & 3;
-        sh.half[count & 1][half][row] = mine;
+        const uint64_t &bar = sh.swap[(threadIdx.x >> 5) & 3];
+        if (count > 0 && !wait(bar, 2 * count - 1)) return false;
+        sh.l[wg][row] = l;
         __syncwarp();
-        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&sh.swap[quad]));
-        if (!wait(sh.swap[quad], count)) return false;
-        theirs = *reinterpret_cast<volatile float *>(&sh.half[count & 1][half ^ 1][row]);
+        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&bar));
+        if (!wait(bar, 2 * count)) return false;
+        const volatile float *both = &sh.l[0][row];
+        l = both[0] + both[128];
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) mbar_arrive(smem_u32(&bar));
         ++count;
         return true;
     }
 
     __device__ __forceinline__ void softmax(int warp)
     {
-        constexpr int kCols = TILES == 2 ? 128 : 64;     // of S, per thread
-        constexpr int kDims = TILES == 2 ? D : D / 2;    // of O, per thread
-        const int lane = threadIdx.x & 31, wg = warp >> 2, row = (warp & 3) * 32 + lane;
+        constexpr int kDims = TILES == 2 ? D : D / 2;  // of O, per thread, when a block is done
+        const int lane = threadIdx.x & 31, wg = warp >> 2, quad = warp & 3, row = quad * 32 + lane;
         const int tile = TILES == 2 ? wg : 0, half = TILES == 2 ? 0 : wg;
-        const uint32_t mine = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-        const uint32_t o_at = mine + 256 + tile * D + half * kDims;
-        int it = 0, swaps = 0;
+        const uint32_t mine = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        const uint32_t o_at = mine + 256 + tile * D, s_at = mine + wg * 128;
+        int it = 0, seg = 0, swaps = 0;
         TokensJoin join{};
-        for (Walk w(a, at, pos, end); w.more(); w.next()) {
+        for (Walk w(a, at, pos, end); w.more(); w.next(), ++seg) {
             const int r = w.p.block * R + tile * 128 + row;
             const bool valid = r < w.s.m * a.group;
             const int j = valid ? r / a.group : 0, g = valid ? r - j * a.group : 0;
@@ -881,53 +941,101 @@ struct TokensKernel {
             see.slope = a.slopes ? a.slopes[w.p.head * a.group + g] * kPagedLog2e : 0.f;
             float m = kPagedLow, l = 0.f;
             for (int i = 0; i < w.count; ++i, ++it) {
-                const int buf = TILES == 2 ? tile : it & 1, t0 = w.tile(i) * kTokKeys + half * kCols;
-                const uint32_t s_at = mine + buf * 128 + half * kCols;
-                if (!wait(sh.s_full[buf], TILES == 2 ? it : it >> 1)) return;
-                tc_fence_after();
-                // Masks, and what else the scores need, in place, 32 columns at a time
-                const bool all = !valid || (t0 >= see.lo && t0 + kCols - 1 <= see.hi) || t0 + kCols <= see.pre;
+                if (TILES == 1 && (it & 1) != wg) continue;
+                const int t0 = w.tile(i) * kTokKeys;
+                const bool all = !valid || (t0 >= see.lo && t0 + kTokKeys - 1 <= see.hi) || t0 + kTokKeys <= see.pre;
                 const bool masked = !__all_sync(0xffffffffu, all);
-                if (a.shaped || masked) {
+                if (!wait(sh.s_full[wg], TILES == 2 ? it : it >> 1)) return;
+                tc_fence_after();
+                // What the scores need beside their factor.  On the way, in registers: a factor
+                // and distances of tokens behind the row (whose sign is known); a cap that all
+                // are far below.  Masks, and the rest, 32 columns at a time in TMEM.
+                const bool ahead = __any_sync(0xffffffffu, valid && see.pre > see.pos + 1 && t0 < see.pre && t0 + kTokKeys > see.pos + 1);
+                const bool drafted = see.tree && t0 + kTokKeys > see.base;
+                bool far = a.slopes && a.cap_log2 == 0.f && a.scale_log2 > 0.f && !ahead && !drafted;
+                bool near = a.cap_near && !a.slopes && !masked;
+                auto prepare = [&](bool shape) {
 #pragma unroll 1
-                    for (int c = 0; c < kCols; c += 32) {
-                        const uint32_t seen = valid ? see.seen(t0 + c) : ~0u;
+                    for (int c = 0; c < kTokKeys; c += 32) {
+                        const uint32_t seen = valid && masked ? see.seen(t0 + c) : ~0u;
                         const bool mask = masked && __any_sync(0xffffffffu, seen != ~0u);
-                        if (!a.shaped && !mask) continue;
-                        uint32_t s[32];
-                        tmem_ld_row(s_at + c, s);
-                        if (a.shaped) tokens_shape(a, see, t0 + c, s);
-                        if (mask) tokens_mask(seen, s);
-                        tmem_st_row(s_at + c, s);
+                        if (!shape && !mask) continue;
+                        uint32_t x[32];
+                        tmem_ld_row(s_at + c, x);
+                        if (shape) tokens_shape(a, see, valid, t0 + c, x);
+                        if (mask) tokens_mask(seen, x);
+                        tmem_st_row(s_at + c, x);
                     }
                     tmem_wait_st();
+                };
+                bool done = a.shaped && !far && !near;  // the scores are in the log2 domain
+                if (done || masked) prepare(done);
+                // The maximum, of the upper 64 columns, then of the lower, which stay in
+                // registers.  (Loops over the halves, since code for all 128 runs out of the
+                // instruction cache, and all 128 out of registers.)
+                uint32_t s[64];
+                const uint64_t factor = pack2(a.scale_log2, a.scale_log2), slope = pack2(see.slope, see.slope);
+                // -slope (d - c) of column c, to which slope j is added: scale s - slope (d - c - j)
+                auto origin = [&](int c) { return -see.slope * static_cast<float>(see.pos - t0 - c); };
+                float top, least;
+                auto range = [&] {
+                    float t[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY}, l[4] = {INFINITY, INFINITY, INFINITY, INFINITY};
+#pragma unroll 1
+                    for (int c = 64; c >= 0; c -= 64) {
+                        tmem_ld_row(s_at + c, s);
+                        if (far) {
+                            const float from = origin(c);
+#pragma unroll
+                            for (int x = 0; x < 64; x += 2) {
+                                const uint64_t v = fma2(pack2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), factor, pack2(from, from));
+                                const float2 f = unpack2(fma2(slope, pack2(1.f * x, 1.f * x + 1.f), v));
+                                t[x / 2 & 3] = max3(t[x / 2 & 3], f.x, f.y);
+                            }
+                            continue;
+                        }
+#pragma unroll
+                        for (int x = 0; x < 64; x += 2) t[x / 2 & 3] = max3(t[x / 2 & 3], __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
+                        if (near)
+#pragma unroll
+                            for (int x = 0; x < 64; x += 2) l[x / 2 & 3] = min3(l[x / 2 & 3], __uint_as_float(s[x]), __uint_as_float(s[x + 1]));
+                    }
+                    top = fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3]));
+                    least = fminf(fminf(l[0], l[1]), fminf(l[2], l[3]));
+                };
+                range();
+                if (near) {
+                    near = __all_sync(0xffffffffu, !valid || fmaxf(fabsf(top * a.to_cap), fabsf(least * a.to_cap)) <= 0.5f);
+                    if (near) {
+                        top = a.cap_log2 * fmaxf(tokens_tanh(top * a.to_cap), tokens_tanh(least * a.to_cap));
+                    } else {
+                        done = true;
+                        prepare(true);
+                        range();
+                    }
+                } else if (!a.shaped) {
+                    top *= a.scale_log2;
                 }
-                uint32_t s[kCols];
-                tmem_ld_row(s_at, *reinterpret_cast<uint32_t(*)[64]>(&s[0]));
-                if constexpr (kCols == 128) tmem_ld_row(s_at + 64, *reinterpret_cast<uint32_t(*)[64]>(&s[kCols - 64]));
-                float tops[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-                for (int x = 0; x < kCols; x += 8)
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        tops[y] = max3(tops[y], __uint_as_float(s[x + 2 * y]), __uint_as_float(s[x + 2 * y + 1]));
-                float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                if (!a.shaped) top *= a.scale_log2;
+                if (TILES == 1 && i > 0) {  // the maximum as the tile before left it
+                    if (!wait(sh.hand[quad * 2 + (wg ^ 1)], (it - 1) >> 1)) return;
+                    const float now = *reinterpret_cast<volatile float *>(&sh.m[wg ^ 1][row]);
+                    l *= ex2(m - now);
+                    m = now;
+                }
+                const bool rises = i > 0 && __any_sync(0xffffffffu, valid && top > m + kSlack);
+                const float before = m;
+                if (i == 0 || rises) m = fmaxf(m, top);
                 if (TILES == 1) {
-                    float other;
-                    if (!exchange(row, half, top, other, swaps)) return;
-                    top = fmaxf(top, other);
+                    sh.m[wg][row] = m;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sh.hand[quad * 2 + wg]));
                 }
-                if (i == 0) {
-                    m = fmaxf(m, top);
-                } else if (__any_sync(0xffffffffu, top > m + kSlack)) {
-                    const float f = ex2(m - fmaxf(m, top));
-                    m = fmaxf(m, top);
+                if (rises) {
+                    const float f = ex2(before - m);
                     l *= f;
                     if (!wait(sh.pv_done[tile], it - 1)) return;
                     tc_fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < kDims; c += 32) {
+                    for (int c = 0; c < D; c += 32) {
                         uint32_t o[32];
                         tmem_ld_row(o_at + c, o);
 #pragma unroll
@@ -935,43 +1043,75 @@ struct TokensKernel {
                         tmem_st_row(o_at + c, o);
                     }
                 }
-                const float scale = a.shaped ? 1.f : a.scale_log2;
-                const uint64_t factor = pack2(scale, scale), shift = pack2(kUp - m, kUp - m);
                 uint64_t sum[2] = {0, 0};
+                // Weights; `exponent` gives those of a pair, column x of the 64 from c on
+                auto weigh = [&](auto exponent) {
+#pragma unroll 1
+                    for (int c = 0; c < kTokKeys; c += 64) {
+                        if (c) tmem_ld_row(s_at + c, s);
+                        const auto of = exponent(c);
 #pragma unroll
-                for (int c = 0; c < kCols; c += 32) {
-                    uint32_t p[16];
+                        for (int y = 0; y < 64; y += 32) {
+                            uint32_t p[16];
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) {
-                        float2 e = unpack2(fma2(pack2(__uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1])), factor, shift));
-                        e.x = ex2(e.x), e.y = ex2(e.y);
-                        sum[x & 1] = add2(sum[x & 1], pack2(e.x, e.y));
-                        if (kBf) {
-                            p[x] = bf16_pair(e.x, e.y);
-                        } else {
-                            const __half2 h = __floats2half2_rn(e.x, e.y);
-                            p[x] = *reinterpret_cast<const uint32_t *>(&h);
+                            for (int x = 0; x < 16; ++x) {
+                                float2 e = unpack2(of(pack2(__uint_as_float(s[y + 2 * x]), __uint_as_float(s[y + 2 * x + 1])), y + 2 * x));
+                                e.x = ex2(e.x), e.y = ex2(e.y);
+                                sum[x & 1] = add2(sum[x & 1], pack2(e.x, e.y));
+                                if (kBf) {
+                                    p[x] = bf16_pair(e.x, e.y);
+                                } else {
+                                    const __half2 h = __floats2half2_rn(e.x, e.y);
+                                    p[x] = *reinterpret_cast<const uint32_t *>(&h);
+                                }
+                            }
+                            tmem_st_row(s_at + (c + y) / 2, p);
                         }
                     }
-                    tmem_st_row(s_at + c / 2, p);
+                };
+                const uint64_t shift = pack2(kUp - m, kUp - m);
+                if (near) {
+                    // cap tanh(s / cap) by an odd polynomial, good to 9 half steps up to cap / 2
+                    const float by = a.cap_log2 * a.to_cap, q = a.to_cap * a.to_cap;
+                    const uint64_t c0 = pack2(0.99999946f * by, 0.99999946f * by), c1 = pack2(-0.3332632f * by * q, -0.3332632f * by * q),
+                                   c2 = pack2(0.13190296f * by * q * q, 0.13190296f * by * q * q),
+                                   c3 = pack2(-0.04440222f * by * q * q * q, -0.04440222f * by * q * q * q);
+                    weigh([&](int) {
+                        return [&](uint64_t v, int) {
+                            const uint64_t w = mul2(v, v);
+                            return fma2(fma2(fma2(fma2(c3, w, c2), w, c1), w, c0), v, shift);
+                        };
+                    });
+                } else if (far) {
+                    weigh([&](int c) {
+                        const float from = origin(c) + (kUp - m);
+                        return [=](uint64_t v, int x) { return fma2(slope, pack2(1.f * x, 1.f * x + 1.f), fma2(v, factor, pack2(from, from))); };
+                    });
+                } else {
+                    const float by = a.shaped ? 1.f : a.scale_log2;  // done, or plain
+                    const uint64_t f = pack2(by, by);
+                    weigh([&](int) { return [&](uint64_t v, int) { return fma2(v, f, shift); }; });
                 }
                 const float2 sums = unpack2(add2(sum[0], sum[1]));
                 l += sums.x + sums.y;
                 tmem_wait_st();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[buf]));
+                if (lane == 0) mbar_arrive(smem_u32(&sh.p_ready[wg]));
             }
-            // the block's result, or this CTA's part of it; one tile: the product before
-            // the last may be under way too, and a parity tells only one phase from the next
-            if (TILES == 1 && it >= 2 && !wait(sh.pv_done[tile], it - 2)) return;
-            if (!wait(sh.pv_done[tile], it - 1)) return;
-            tc_fence_after();
             if (TILES == 1) {
-                float other;
-                if (!exchange(row, half, l, other, swaps)) return;
-                l = half ? other + l : l + other;
+                const int last = (it - 1) & 1;
+                if (wg != last) {
+                    if (!wait(sh.hand[quad * 2 + last], (it - 1) >> 1)) return;
+                    const float now = *reinterpret_cast<volatile float *>(&sh.m[last][row]);
+                    l *= ex2(m - now);
+                    m = now;
+                }
+                if (!add_sums(row, wg, l, swaps)) return;
             }
+            // the block's result, or this CTA's part of it
+            if (!(TILES == 2 ? wait(sh.pv_done[tile], it - 1) : wait(sh.o_done, seg))) return;
+            tc_fence_after();
             const bool whole = w.begins() && w.ends();
             const int slot = 2 * blockIdx.x + w.begins();
             const int64_t part = static_cast<int64_t>(slot) * R + tile * 128 + row;
@@ -985,7 +1125,7 @@ struct TokensKernel {
 #pragma unroll 1
             for (int c = 0; c < kDims; c += 32) {
                 uint32_t s[32];
-                tmem_ld_row(o_at + c, s);
+                tmem_ld_row(o_at + half * kDims + c, s);
                 if (!valid) continue;
                 float v[32];
 #pragma unroll
@@ -1023,6 +1163,10 @@ struct TokensKernel {
                 }
             }
             tc_fence_before();
+            if (TILES == 1) {  // O may be written again when both warpgroups have read it
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.o_free));
+            }
         }
         if (threadIdx.x == 0) a.joins[blockIdx.x] = join;
     }
@@ -1030,7 +1174,8 @@ struct TokensKernel {
 
 template <int D, int KIND, int TILES>
 __global__ void __launch_bounds__(kTokThreads, 1)
-    tokens_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, TokensArgs a)
+    tokens_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
+                       const __grid_constant__ CUtensorMap q_map, TokensArgs a)
 {
     griddep_wait();
     using K = TokensKernel<D, KIND, TILES>;
@@ -1049,14 +1194,17 @@ __global__ void __launch_bounds__(kTokThreads, 1)
             mbar_init(smem_u32(&sh.full[i]), kTokFillWarps);
             mbar_init(smem_u32(&sh.empty[i]), 1);
         }
-        mbar_init(smem_u32(&sh.q_full), 1);
+        mbar_init(smem_u32(&sh.q_full), kTokQueryWarps);
         mbar_init(smem_u32(&sh.q_free), 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh.s_full[i]), 1);
-            mbar_init(smem_u32(&sh.p_ready[i]), TILES == 2 ? 4 : 8);
+            mbar_init(smem_u32(&sh.p_ready[i]), 4);
             mbar_init(smem_u32(&sh.pv_done[i]), 1);
         }
         for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&sh.swap[i]), 2);
+        for (int i = 0; i < 8; ++i) mbar_init(smem_u32(&sh.hand[i]), 1);
+        mbar_init(smem_u32(&sh.o_done), 1);
+        mbar_init(smem_u32(&sh.o_free), kTokSoftmaxWarps);
         mbar_init(smem_u32(&sh.drain), 1);
         sh.abort = 0;
         fence_mbar_init();
@@ -1069,7 +1217,7 @@ __global__ void __launch_bounds__(kTokThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t q_smem = smem_u32(s_tokens), tmem = *reinterpret_cast<volatile uint32_t *>(&sh.tmem);
-    K k{a, sh, sh.find.at, pos, end, chunk, q_smem, q_smem + Shape::kQBytes, tmem, &sh.abort, &k_map, &v_map};
+    K k{a, sh, sh.find.at, pos, end, chunk, q_smem, q_smem + Shape::kQBytes, tmem, &sh.abort, &k_map, &v_map, &q_map};
     if (warp < kTokSoftmaxWarps) {
         regs_increase<K::kSoftmaxRegs>();
         k.softmax(warp);
@@ -1080,7 +1228,7 @@ __global__ void __launch_bounds__(kTokThreads, 1)
     } else {
         regs_decrease<K::kLastRegs>();
         if (warp == kTokSoftmaxWarps + kTokFillWarps) k.products();
-        else if (warp == kTokSoftmaxWarps + kTokFillWarps + 1) k.load_queries();
+        else k.load_queries(warp - kTokSoftmaxWarps - kTokFillWarps - 1);
     }
     tc_fence_before();
     __syncthreads();
@@ -1089,7 +1237,7 @@ __global__ void __launch_bounds__(kTokThreads, 1)
 }
 
 struct TokensMaps {
-    CUtensorMap k, v;
+    CUtensorMap k, v, q;
 };
 
 cudaError_t launch_tokens_attn_64(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
@@ -1104,7 +1252,7 @@ cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int cta
     const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES>>(kSmem);
     if (e != cudaSuccess) return e;
     return launch_pdl(tokens_attn_kernel<D, KIND, TILES>, dim3(static_cast<unsigned>(ctas)), dim3(kTokThreads), kSmem, s, m.k,
-                      m.v, a);
+                      m.v, m.q, a);
 }
 
 template <int D, int TILES>

@@ -121,7 +121,7 @@ def attention(q, k, v, scale, mask, dtype, pos=None, place=None, cap=0.0, slopes
     of their sizes, doubled since the tensor cores cut where binary32 rounds;
     8 half steps of itself for its factors (a cap: 25 of the capped score, and a
     capped score moves by no more than the score), 4 of the distance's product
-    and the result.  A weight is off by that, by 2^-22 (ex2) and by half a step
+    (of up to 128 more) and the result.  A weight is off by that, by 2^-22 (ex2) and by half a step
     of the pages' type (relative to the largest: fp16 holds weights from 2^-22
     of the largest down to 2^-33 of it); sums of n weights, or of n products,
     by n + 2 half steps, doubled for the tensor cores, and the rescaling and the
@@ -148,7 +148,8 @@ def attention(q, k, v, scale, mask, dtype, pos=None, place=None, cap=0.0, slopes
         if slopes is not None:
             far = (pos[:, None] - place[None]).abs().double() * float(slopes[h])
             s = s - far
-            err = err + far.abs() * 4 * U + s.abs() * 4 * U
+            # the distance from a tile of 128 keys' first one is rounded by itself
+            err = err + (far.abs() + 128 * abs(float(slopes[h]))) * 4 * U + s.abs() * 4 * U
         s = s.masked_fill(~mask, -torch.inf)
         top = s.amax(-1, keepdim=True).clamp(min=-1e300)
         e = torch.exp(s - top)
