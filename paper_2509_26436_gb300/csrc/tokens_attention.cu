@@ -133,7 +133,6 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
     a.window = static_cast<int>(call.mask.window < call.max_len ? call.mask.window : 0);
     a.gs_shift = c->type == QUARTZ_PAGES_ENCODED ? log2_of(c->k.enc.p.group_s) : 0;
     a.single = call.max_new * a.group <= 128 * p.tiles;
-    a.shaped = call.mask.cap > 0.f || call.mask.slopes || !(call.scale > 0.f);
     a.scale_log2 = call.scale * kPagedLog2e;
     if (call.mask.cap > 0.f) a.cap_log2 = call.mask.cap * kPagedLog2e, a.to_cap = call.scale / call.mask.cap;
     a.cap_near = std::fabs(a.to_cap) > 1e-4f && std::fabs(a.to_cap) < 1e3f;
@@ -159,19 +158,20 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
     }
     const dim3 grid(static_cast<unsigned>(p.ctas), static_cast<unsigned>(4 * p.tiles)), block(kJoinThreads);
     const int R = 128 * p.tiles;
+    const bool shaped = call.mask.cap > 0.f || call.mask.slopes || !(call.scale > 0.f);
     cudaError_t e;
     switch (c->dim) {
         case 64:
-            e = launch_tokens_attn_64(a, m, c->type, p.tiles, p.ctas, s);
+            e = (shaped ? launch_tokens_attn_64_shaped : launch_tokens_attn_64)(a, m, c->type, p.tiles, p.ctas, s);
             return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<64>, grid, block, 0, s, a, R);
         case 128:
-            e = launch_tokens_attn_128(a, m, c->type, p.tiles, p.ctas, s);
+            e = (shaped ? launch_tokens_attn_128_shaped : launch_tokens_attn_128)(a, m, c->type, p.tiles, p.ctas, s);
             return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<128>, grid, block, 0, s, a, R);
         case 192:
-            e = launch_tokens_attn_192(a, m, c->type, p.tiles, p.ctas, s);
+            e = (shaped ? launch_tokens_attn_192_shaped : launch_tokens_attn_192)(a, m, c->type, p.tiles, p.ctas, s);
             return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<192>, grid, block, 0, s, a, R);
         default:
-            e = launch_tokens_attn_256(a, m, c->type, p.tiles, p.ctas, s);
+            e = (shaped ? launch_tokens_attn_256_shaped : launch_tokens_attn_256)(a, m, c->type, p.tiles, p.ctas, s);
             return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<256>, grid, block, 0, s, a, R);
     }
 }

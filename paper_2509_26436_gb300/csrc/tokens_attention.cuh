@@ -60,7 +60,6 @@ struct TokensArgs {
     int k_order, v_order;
     int q_box;  // a box of the queries' map is a tile's rows and 64 dimensions
     int single;              // no sequence has more rows than one CTA takes
-    int shaped;              // scores need more than a positive factor
     int cap_near;            // the powers of to_cap fit binary32: the cap's short polynomial may be used
     float scale_log2;
     float cap_log2, to_cap;  // cap > 0: cap log2 e and scale / cap; else 0
@@ -407,7 +406,9 @@ __device__ __forceinline__ void tokens_shape(const TokensArgs &a, const TokensRo
     }
 }
 
-template <int D, int KIND, int TILES>
+// SHAPED: scores need more than a positive factor.  (An instance of its own: the
+// code for it in the others' loop cost them 14%, waiting for instructions.)
+template <int D, int KIND, int TILES, bool SHAPED>
 struct TokensKernel {
     using Shape = TokensShape<D, TILES>;
     static constexpr int R = Shape::kRows;
@@ -938,7 +939,7 @@ struct TokensKernel {
             if (a.tree && a.window > 0 && a.window < kTokTreeMost)
                 for (int i = 0; i < w.s.m; ++i)
                     if (see.base + see.depth(i) < see.lo) see.own &= ~(1ull << i);
-            see.slope = a.slopes ? a.slopes[w.p.head * a.group + g] * kPagedLog2e : 0.f;
+            see.slope = SHAPED && a.slopes ? a.slopes[w.p.head * a.group + g] * kPagedLog2e : 0.f;
             float m = kPagedLow, l = 0.f;
             for (int i = 0; i < w.count; ++i, ++it) {
                 if (TILES == 1 && (it & 1) != wg) continue;
@@ -950,10 +951,10 @@ struct TokensKernel {
                 // What the scores need beside their factor.  On the way, in registers: a factor
                 // and distances of tokens behind the row (whose sign is known); a cap that all
                 // are far below.  Masks, and the rest, 32 columns at a time in TMEM.
-                const bool ahead = __any_sync(0xffffffffu, valid && see.pre > see.pos + 1 && t0 < see.pre && t0 + kTokKeys > see.pos + 1);
+                const bool ahead = SHAPED && __any_sync(0xffffffffu, valid && see.pre > see.pos + 1 && t0 < see.pre && t0 + kTokKeys > see.pos + 1);
                 const bool drafted = see.tree && t0 + kTokKeys > see.base;
-                bool far = a.slopes && a.cap_log2 == 0.f && a.scale_log2 > 0.f && !ahead && !drafted;
-                bool near = a.cap_near && !a.slopes && !masked;
+                bool far = SHAPED && a.slopes && a.cap_log2 == 0.f && a.scale_log2 > 0.f && !ahead && !drafted;
+                bool near = SHAPED && a.cap_near && !a.slopes && !masked;
                 auto prepare = [&](bool shape) {
 #pragma unroll 1
                     for (int c = 0; c < kTokKeys; c += 32) {
@@ -962,13 +963,13 @@ struct TokensKernel {
                         if (!shape && !mask) continue;
                         uint32_t x[32];
                         tmem_ld_row(s_at + c, x);
-                        if (shape) tokens_shape(a, see, valid, t0 + c, x);
+                        if (SHAPED && shape) tokens_shape(a, see, valid, t0 + c, x);
                         if (mask) tokens_mask(seen, x);
                         tmem_st_row(s_at + c, x);
                     }
                     tmem_wait_st();
                 };
-                bool done = a.shaped && !far && !near;  // the scores are in the log2 domain
+                bool done = SHAPED && !far && !near;  // the scores are in the log2 domain
                 if (done || masked) prepare(done);
                 // The maximum, of the upper 64 columns, then of the lower, which stay in
                 // registers.  (Loops over the halves, since code for all 128 runs out of the
@@ -1012,7 +1013,7 @@ struct TokensKernel {
                         prepare(true);
                         range();
                     }
-                } else if (!a.shaped) {
+                } else if (!SHAPED) {
                     top *= a.scale_log2;
                 }
                 if (TILES == 1 && i > 0) {  // the maximum as the tile before left it
@@ -1088,7 +1089,7 @@ struct TokensKernel {
                         return [=](uint64_t v, int x) { return fma2(slope, pack2(1.f * x, 1.f * x + 1.f), fma2(v, factor, pack2(from, from))); };
                     });
                 } else {
-                    const float by = a.shaped ? 1.f : a.scale_log2;  // done, or plain
+                    const float by = SHAPED ? 1.f : a.scale_log2;  // done, or plain
                     const uint64_t f = pack2(by, by);
                     weigh([&](int) { return [&](uint64_t v, int) { return fma2(v, f, shift); }; });
                 }
@@ -1172,13 +1173,13 @@ struct TokensKernel {
     }
 };
 
-template <int D, int KIND, int TILES>
+template <int D, int KIND, int TILES, bool SHAPED>
 __global__ void __launch_bounds__(kTokThreads, 1)
     tokens_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                        const __grid_constant__ CUtensorMap q_map, TokensArgs a)
 {
     griddep_wait();
-    using K = TokensKernel<D, KIND, TILES>;
+    using K = TokensKernel<D, KIND, TILES, SHAPED>;
     using Shape = TokensShape<D, TILES>;
     extern __shared__ __align__(1024) uint8_t s_tokens[];
     __shared__ TokensShared sh;
@@ -1240,27 +1241,32 @@ struct TokensMaps {
     CUtensorMap k, v, q;
 };
 
+// `shaped`: scores need more than a positive factor.
 cudaError_t launch_tokens_attn_64(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_64_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
 cudaError_t launch_tokens_attn_128(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_128_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
 cudaError_t launch_tokens_attn_192(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_192_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
 cudaError_t launch_tokens_attn_256(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_256_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
 
-template <int D, int KIND, int TILES>
+template <int D, int KIND, int TILES, bool SHAPED>
 cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int ctas, cudaStream_t s)
 {
     constexpr int kSmem = TokensShape<D, TILES>::kSmem;
-    const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES>>(kSmem);
+    const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES, SHAPED>>(kSmem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(tokens_attn_kernel<D, KIND, TILES>, dim3(static_cast<unsigned>(ctas)), dim3(kTokThreads), kSmem, s, m.k,
-                      m.v, m.q, a);
+    return launch_pdl(tokens_attn_kernel<D, KIND, TILES, SHAPED>, dim3(static_cast<unsigned>(ctas)), dim3(kTokThreads), kSmem, s,
+                      m.k, m.v, m.q, a);
 }
 
-template <int D, int TILES>
+template <int D, int TILES, bool SHAPED>
 cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int kind, int ctas, cudaStream_t s)
 {
-    if (kind == QUARTZ_PAGES_F16) return launch_tokens_attn<D, QUARTZ_PAGES_F16, TILES>(a, m, ctas, s);
-    if (kind == QUARTZ_PAGES_BF16) return launch_tokens_attn<D, QUARTZ_PAGES_BF16, TILES>(a, m, ctas, s);
-    return launch_tokens_attn<D, QUARTZ_PAGES_ENCODED, TILES>(a, m, ctas, s);
+    if (kind == QUARTZ_PAGES_F16) return launch_tokens_attn<D, QUARTZ_PAGES_F16, TILES, SHAPED>(a, m, ctas, s);
+    if (kind == QUARTZ_PAGES_BF16) return launch_tokens_attn<D, QUARTZ_PAGES_BF16, TILES, SHAPED>(a, m, ctas, s);
+    return launch_tokens_attn<D, QUARTZ_PAGES_ENCODED, TILES, SHAPED>(a, m, ctas, s);
 }
 
 }  // namespace quartz

@@ -6,7 +6,7 @@ namespace quartz {
 
 cudaError_t launch_tokens_attn_256(const TokensArgs &a, const TokensMaps &m, int kind, int, int ctas, cudaStream_t s)
 {
-    return launch_tokens_attn<256, 1>(a, m, kind, ctas, s);
+    return launch_tokens_attn<256, 1, false>(a, m, kind, ctas, s);
 }
 
 }  // namespace quartz

@@ -1,0 +1,12 @@
+// Attention of several new tokens over a paged cache: heads of 256 with a cap, distances, or a factor that is not positive
+// (tokens_attention.cuh).
+#include "tokens_attention.cuh"
+
+namespace quartz {
+
+cudaError_t launch_tokens_attn_256_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int, int ctas, cudaStream_t s)
+{
+    return launch_tokens_attn<256, 1, true>(a, m, kind, ctas, s);
+}
+
+}  // namespace quartz

@@ -6,7 +6,8 @@ namespace quartz {
 
 cudaError_t launch_tokens_attn_64(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s)
 {
-    return tiles == 2 ? launch_tokens_attn<64, 2>(a, m, kind, ctas, s) : launch_tokens_attn<64, 1>(a, m, kind, ctas, s);
+    return tiles == 2 ? launch_tokens_attn<64, 2, false>(a, m, kind, ctas, s)
+                      : launch_tokens_attn<64, 1, false>(a, m, kind, ctas, s);
 }
 
 }  // namespace quartz
