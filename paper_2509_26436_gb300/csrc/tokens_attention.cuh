@@ -24,9 +24,10 @@
 // the products; three that load queries.
 //
 // The keys of all rows' tiles, one behind the other, are cut into one run of
-// equal length per CTA (one CTA per SM), so that lengths, windows and the causal
-// edge leave no SM idle; tiles that a cut goes through are joined by a second
-// kernel, in the order of the keys.
+// equal work per CTA (one CTA per SM), so that lengths, windows and the causal
+// edge leave no SM idle; a block of rows counts some tiles more than it has, for
+// its queries, masks and results.  Blocks that a cut goes through are joined by
+// a second kernel, in the order of the keys.
 #pragma once
 
 #include <cuda.h>
@@ -120,15 +121,16 @@ __device__ __forceinline__ TokensTiles tokens_tiles(const TokensArgs &a, const T
 template <int R>
 __device__ __forceinline__ int tokens_blocks(const TokensArgs &a, const TokensSeq &s) { return (s.m * a.group + R - 1) / R; }
 
-// Tiles of one key head of 32 sequences from b0 on (to b1), each in its lane.
+// Tiles and row blocks of one key head of 32 sequences from b0 on (to b1), each
+// in its lane.
 template <int R>
-__device__ __forceinline__ int tokens_seq_tiles(const TokensArgs &a, int b0, int b1)
+__device__ __forceinline__ int2 tokens_seq_tiles(const TokensArgs &a, int b0, int b1)
 {
     const int lane = threadIdx.x & 31;
     TokensSeq s{};
     if (b0 + lane < b1) s = tokens_seq(a, b0 + lane);
-    if (a.single) return s.m > 0 ? tokens_tiles<R>(a, s, 0).count : 0;
-    int mine = 0;
+    if (a.single) return s.m > 0 ? make_int2(tokens_tiles<R>(a, s, 0).count, 1) : make_int2(0, 0);
+    int2 mine = make_int2(0, tokens_blocks<R>(a, s));
     for (int i = 0; i < min(32, b1 - b0); ++i) {
         TokensSeq t;
         t.n = __shfl_sync(0xffffffffu, s.n, i), t.m = __shfl_sync(0xffffffffu, s.m, i);
@@ -136,7 +138,7 @@ __device__ __forceinline__ int tokens_seq_tiles(const TokensArgs &a, int b0, int
         int sum = 0;
         for (int r = lane; r < tokens_blocks<R>(a, t); r += 32) sum += tokens_tiles<R>(a, t, r).count;
         sum = __reduce_add_sync(0xffffffffu, sum);
-        if (lane == i) mine = sum;
+        if (lane == i) mine.x = sum;
     }
     return mine;
 }
@@ -146,39 +148,51 @@ struct TokensPlace {
 };
 
 struct TokensFind {
-    long long sums[kTokWarps];
+    long long tiles[kTokWarps], blocks[kTokWarps];
     TokensPlace at;
 };
 
-// Of all tiles of all sequences, heads and row blocks, in that order, this CTA
-// takes [pos, end), which begins at `at`.  (All threads of the CTA.)  False: none.
+// What a CTA takes: [pos, end) of all work, in tiles.
+struct TokensRun {
+    long long pos, end, chunk;
+    int edge;  // tiles that a block of rows counts for besides its own
+};
+
+// Most of a block's edge: it costs as much as 3 tiles.  Less where a CTA has few
+// tiles (a sixteenth), so that none has edges alone.
+constexpr int kTokEdge = 3;
+
+// Of all tiles of all sequences, heads and row blocks, in that order, this CTA's
+// run, which begins at `at`.  (All threads of the CTA.)  False: none.
 template <int R>
-__device__ bool tokens_find(const TokensArgs &a, TokensFind &f, long long &pos, long long &end, long long &chunk)
+__device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int share = (a.seqs + kTokWarps - 1) / kTokWarps;
     const int b0 = min(a.seqs, warp * share), b1 = min(a.seqs, b0 + share);
-    long long sum = 0;
+    long long tiles = 0, blocks = 0;
     for (int b = b0; b < b1; b += 32) {
-        long long t = tokens_seq_tiles<R>(a, b, b1);
+        const int2 n = tokens_seq_tiles<R>(a, b, b1);
+        long long t = n.x, k = n.y;
 #pragma unroll
-        for (int d = 16; d; d /= 2) t += __shfl_xor_sync(0xffffffffu, t, d);
-        sum += t;
+        for (int d = 16; d; d /= 2) t += __shfl_xor_sync(0xffffffffu, t, d), k += __shfl_xor_sync(0xffffffffu, k, d);
+        tiles += t, blocks += k;
     }
-    if (lane == 0) f.sums[warp] = sum * a.kv_heads;
+    if (lane == 0) f.tiles[warp] = tiles * a.kv_heads, f.blocks[warp] = blocks * a.kv_heads;
     __syncthreads();
-    long long all = 0, before = 0;
+    long long all_tiles = 0, all_blocks = 0, before = 0;
 #pragma unroll
-    for (int w = 0; w < kTokWarps; ++w) {
-        if (w < warp) before += f.sums[w];
-        all += f.sums[w];
-    }
-    chunk = (all + gridDim.x - 1) / gridDim.x;
-    pos = chunk * blockIdx.x;
-    end = min(pos + chunk, all);
-    if (pos < end && pos >= before && pos < before + sum * a.kv_heads) {
+    for (int w = 0; w < kTokWarps; ++w) all_tiles += f.tiles[w], all_blocks += f.blocks[w];
+    run.edge = static_cast<int>(min(static_cast<long long>(kTokEdge), all_tiles / (16 * gridDim.x)));
+    for (int w = 0; w < warp; ++w) before += f.tiles[w] + run.edge * f.blocks[w];
+    const long long all = all_tiles + run.edge * all_blocks, mine_all = (tiles + run.edge * blocks) * a.kv_heads;
+    run.chunk = (all + gridDim.x - 1) / gridDim.x;
+    const long long pos = run.pos = run.chunk * blockIdx.x;
+    run.end = min(pos + run.chunk, all);
+    if (pos < run.end && pos >= before && pos < before + mine_all) {
         for (int b = b0; b < b1; b += 32) {
-            const int mine = tokens_seq_tiles<R>(a, b, b1);
+            const int2 n2 = tokens_seq_tiles<R>(a, b, b1);
+            const int mine = n2.x + run.edge * n2.y;
             long long incl = mine;
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
@@ -198,9 +212,9 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, long long &pos, 
             p.head = static_cast<int>(in / per_head);
             int rest = static_cast<int>(in - static_cast<long long>(p.head) * per_head);
             const TokensSeq s = tokens_seq(a, p.b);
-            const int blocks = tokens_blocks<R>(a, s);
+            const int blocks = tokens_blocks<R>(a, s);  // of this sequence
             for (int r0 = 0; r0 < blocks; r0 += 32) {
-                const int n = r0 + lane < blocks ? tokens_tiles<R>(a, s, r0 + lane).count : 0;
+                const int n = r0 + lane < blocks ? tokens_tiles<R>(a, s, r0 + lane).count + run.edge : 0;
                 int sums = n;
 #pragma unroll
                 for (int d = 1; d < 32; d *= 2) {
@@ -221,41 +235,52 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, long long &pos, 
         }
     }
     __syncthreads();
-    return pos < end;
+    return pos < run.end;
 }
 
-// A CTA's way over its tiles: one row block and the tiles [off, off + count) of
-// it at a time.  Every warp goes it for itself.
+// A CTA's way over its run: one row block and tiles [first, first + count) of it
+// at a time.  Every warp goes it for itself.
 template <int R>
 struct TokensWalk {
     const TokensArgs &a;
-    long long pos, end;
+    const TokensRun &run;
+    long long pos;
     TokensPlace p;
     TokensSeq s;
     TokensTiles t;
-    int count;
+    int span, first, count;
 
-    __device__ __forceinline__ TokensWalk(const TokensArgs &args, const TokensPlace &at, long long first, long long last)
-        : a(args), pos(first), end(last), p(at)
+    __device__ __forceinline__ TokensWalk(const TokensArgs &args, const TokensPlace &at, const TokensRun &r)
+        : a(args), run(r), pos(r.pos), p(at)
     {
         s = tokens_seq(a, p.b);
         enter();
     }
+    // The block's edge comes before its tiles.
     __device__ __forceinline__ void enter()
     {
         t = tokens_tiles<R>(a, s, p.block);
-        const long long left = end - pos;
-        count = left < t.count - p.off ? static_cast<int>(left) : t.count - p.off;
+        const long long left = run.end - pos;
+        const int most = t.count + run.edge - p.off;
+        span = left < most ? static_cast<int>(left) : most;
+        first = max(0, p.off - run.edge);
+        count = max(0, p.off + span - run.edge) - first;
+        if (count == 0) pos = run.end;  // the run ends within the edge: the next CTA's
     }
-    __device__ __forceinline__ bool more() const { return pos < end; }
-    __device__ __forceinline__ bool begins() const { return p.off == 0; }
-    __device__ __forceinline__ bool ends() const { return p.off + count == t.count; }
-    __device__ __forceinline__ int tile(int i) const { return t.at(p.off + i); }
+    __device__ __forceinline__ bool more() const { return pos < run.end; }
+    __device__ __forceinline__ bool begins() const { return first == 0; }
+    __device__ __forceinline__ bool ends() const { return first + count == t.count; }
+    // CTAs that the block goes on in
+    __device__ __forceinline__ int behind() const
+    {
+        return static_cast<int>((t.count + run.edge - p.off - span + run.chunk - 1) / run.chunk);
+    }
+    __device__ __forceinline__ int tile(int i) const { return t.at(first + i); }
     __device__ __forceinline__ int rows() const { return min(R, s.m * a.group - p.block * R); }
     __device__ __forceinline__ void next()
     {
-        pos += count;
-        if (pos >= end) return;
+        pos += span;
+        if (pos >= run.end) return;
         p.off = 0;  // only the last block may be left before its end
         if (++p.block >= tokens_blocks<R>(a, s)) {
             p.block = 0;
@@ -276,9 +301,10 @@ struct TokensShape {
     static constexpr int kPanel = kTokKeys * 128;  // 64 dimensions, 128 bytes a row
     static constexpr int kUnitBytes = kTokKeys * kUnitDims * 2, kQTile = 128 * D * 2, kQBytes = TILES * kQTile;
     static constexpr int kMisc = 3072;  // static shared memory, with its padding
-    static constexpr int kFit = (232448 - kMisc - kQBytes) / kUnitBytes;
+    static constexpr int kOutWarp = 4096, kOut = kTokSoftmaxWarps * kOutWarp;  // results on their way out: 32 rows x 32 columns
+    static constexpr int kFit = (232448 - kMisc - kQBytes - kOut) / kUnitBytes;
     static constexpr int kRing = kFit < 12 ? kFit : 12;
-    static constexpr int kSmem = kQBytes + kRing * kUnitBytes;
+    static constexpr int kSmem = kQBytes + kRing * kUnitBytes + kOut;
     static_assert(kRing >= 2 * kUnits, "the values of a tile and the next keys are held together");
     static_assert(256 + TILES * D <= 512, "TMEM: two S, and O");
 };
@@ -424,7 +450,7 @@ struct TokensKernel {
     const TokensArgs &a;
     TokensShared &sh;
     const TokensPlace at;
-    const long long pos, end, chunk;
+    const TokensRun &run;
     const uint32_t q_smem, ring, tmem;
     volatile int *abort;
     const void *k_map, *v_map, *q_map;
@@ -453,7 +479,7 @@ struct TokensKernel {
         const int r_first = warp * kEach + (kEach == 1 ? 0 : lane / kChunks);
         const int dt = kStep / a.group, dg = kStep - dt * a.group;
         int seg = 0;
-        for (Walk w(a, at, pos, end); w.more(); w.next(), ++seg) {
+        for (Walk w(a, at, run); w.more(); w.next(), ++seg) {
             if (seg > 0 && !wait(sh.q_free, seg - 1)) break;
             const int rows = w.rows();
             if (!kLzs && a.q_box) {
@@ -580,7 +606,7 @@ struct TokensKernel {
             cp_async_wait<0>();
             while (arrived < u) arrive_full(arrived++);
         };
-        for (Walk w(a, at, pos, end); ok && w.more(); w.next()) {
+        for (Walk w(a, at, run); ok && w.more(); w.next()) {
             const Loaded l = loaded(w);
             // of a box, or of this lane's token (not there: none sees it; zeros take its
             // place, so that nothing of it, which may be infinite or NaN, meets a weight of 0)
@@ -732,7 +758,7 @@ struct TokensKernel {
     {
         const int lane = threadIdx.x & 31;
         const int mask = (1 << a.page_shift) - 1;
-        Walk w(a, at, pos, end);
+        Walk w(a, at, run);
         Loaded l = loaded(w);
         bool bad = false;
         int i = 0, u = 0;
@@ -826,7 +852,7 @@ struct TokensKernel {
         const bool leader = elect_one();
         int it = 0, seg = 0;  // tiles and blocks so far
         bool ok = true;
-        for (Walk w(a, at, pos, end); ok && w.more(); w.next(), ++seg) {
+        for (Walk w(a, at, run); ok && w.more(); w.next(), ++seg) {
             if (!(ok = wait(sh.q_full, seg) && wait_units(2 * Shape::kUnits * it))) break;
             tc_fence_after();
             if (leader) {
@@ -921,7 +947,7 @@ struct TokensKernel {
         const uint32_t o_at = mine + 256 + tile * D, s_at = mine + wg * 128;
         int it = 0, seg = 0, swaps = 0;
         TokensJoin join{};
-        for (Walk w(a, at, pos, end); w.more(); w.next(), ++seg) {
+        for (Walk w(a, at, run); w.more(); w.next(), ++seg) {
             const int r = w.p.block * R + tile * 128 + row;
             const bool valid = r < w.s.m * a.group;
             const int j = valid ? r / a.group : 0, g = valid ? r - j * a.group : 0;
@@ -1117,51 +1143,69 @@ struct TokensKernel {
             const int slot = 2 * blockIdx.x + w.begins();
             const int64_t part = static_cast<int64_t>(slot) * R + tile * 128 + row;
             if (!whole && w.begins()) {
-                join.parts = 1 + static_cast<int>((w.t.count - w.count + chunk - 1) / chunk);
+                join.parts = 1 + w.behind();
                 join.token0 = w.s.start, join.row0 = w.p.block * R, join.rows = w.rows(), join.head0 = w.p.head * a.group;
             }
             if (!whole && valid && half == 0) a.part_ml[part] = make_float2(m, l);
-            const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;  // NaN stays
+            const float inv = whole ? (l > 0.f ? 1.f / l : l == 0.f ? 0.f : l) : 1.f;  // NaN stays
             const int64_t out = (static_cast<int64_t>(w.s.start + j) * a.kv_heads * a.group + w.p.head * a.group + g) * D + half * kDims;
+            const unsigned rows = __ballot_sync(0xffffffffu, valid);
+            const int64_t part0 = (part - lane) * D + half * kDims;  // of the warp's first row
+            const uint32_t stage = q_smem + Shape::kQBytes + Shape::kRing * Shape::kUnitBytes + warp * Shape::kOutWarp;
+            // 32 columns at a time through shared memory, so that the lanes of a row write
+            // side by side: a row's store for itself takes as many steps as there are rows.
 #pragma unroll 1
-            for (int c = 0; c < kDims; c += 32) {
+            for (int c = 0; rows && c < kDims; c += 32) {
                 uint32_t s[32];
                 tmem_ld_row(o_at + half * kDims + c, s);
-                if (!valid) continue;
                 float v[32];
 #pragma unroll
                 for (int x = 0; x < 32; ++x) {
                     // encoded: dimension x is where the decoding puts it
                     const int from = kLzs ? (x & ~7) + (x & 3) * 2 + (x >> 2 & 1) : x;
-                    v[x] = __uint_as_float(s[from]);
+                    v[x] = __uint_as_float(s[from]) * inv;
                 }
-                if (!whole) {
+                if (!whole || a.o_type == QUARTZ_OUT_F32) {
 #pragma unroll
-                    for (int x = 0; x < 32; x += 4)
-                        *reinterpret_cast<float4 *>(a.part_o + part * D + half * kDims + c + x) = make_float4(v[x], v[x + 1], v[x + 2], v[x + 3]);
-                } else {
+                    for (int x = 0; x < 8; ++x)
+                        sts_b128(stage + lane * 128 + (((x ^ lane) & 7) << 4),
+                                 make_uint4(__float_as_uint(v[4 * x]), __float_as_uint(v[4 * x + 1]), __float_as_uint(v[4 * x + 2]), __float_as_uint(v[4 * x + 3])));
+                    __syncwarp();
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) v[x] *= inv;
-                    if (a.o_type == QUARTZ_OUT_F32) {
-#pragma unroll
-                        for (int x = 0; x < 32; x += 4) paged_store4<float>(a.o, out + c + x, make_float4(v[x], v[x + 1], v[x + 2], v[x + 3]));
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < 32; x += 8) {
-                            uint32_t h[4];
-#pragma unroll
-                            for (int y = 0; y < 4; ++y) {
-                                if (a.o_type == QUARTZ_OUT_BF16) {
-                                    h[y] = bf16_pair(v[x + 2 * y], v[x + 2 * y + 1]);
-                                } else {
-                                    const __half2 two = __floats2half2_rn(v[x + 2 * y], v[x + 2 * y + 1]);
-                                    h[y] = *reinterpret_cast<const uint32_t *>(&two);
-                                }
-                            }
-                            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.o) + out + c + x) = make_uint4(h[0], h[1], h[2], h[3]);
+                    for (int i = 0; i < 8; ++i) {
+                        const int to = i * 4 + lane / 8, x = lane % 8;
+                        const float4 f = lds_f4(stage + to * 128 + (((x ^ to) & 7) << 4));
+                        const int64_t at_row = __shfl_sync(0xffffffffu, out, to);
+                        if (rows >> to & 1) {
+                            if (whole) *reinterpret_cast<float4 *>(static_cast<float *>(a.o) + at_row + c + x * 4) = f;
+                            else *reinterpret_cast<float4 *>(a.part_o + part0 + to * D + c + x * 4) = f;
                         }
                     }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        uint32_t h[4];
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            if (a.o_type == QUARTZ_OUT_BF16) {
+                                h[y] = bf16_pair(v[8 * x + 2 * y], v[8 * x + 2 * y + 1]);
+                            } else {
+                                const __half2 two = __floats2half2_rn(v[8 * x + 2 * y], v[8 * x + 2 * y + 1]);
+                                h[y] = *reinterpret_cast<const uint32_t *>(&two);
+                            }
+                        }
+                        sts_b128(stage + lane * 64 + (((x ^ lane >> 1) & 3) << 4), make_uint4(h[0], h[1], h[2], h[3]));
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int to = i * 8 + lane / 4, x = lane % 4;
+                        const float4 f = lds_f4(stage + to * 64 + (((x ^ to >> 1) & 3) << 4));
+                        const int64_t at_row = __shfl_sync(0xffffffffu, out, to);
+                        if (rows >> to & 1) *reinterpret_cast<float4 *>(static_cast<uint16_t *>(a.o) + at_row + c + x * 8) = f;
+                    }
                 }
+                __syncwarp();
             }
             tc_fence_before();
             if (TILES == 1) {  // O may be written again when both warpgroups have read it
@@ -1184,8 +1228,8 @@ __global__ void __launch_bounds__(kTokThreads, 1)
     extern __shared__ __align__(1024) uint8_t s_tokens[];
     __shared__ TokensShared sh;
     const int warp = threadIdx.x >> 5;
-    long long pos, end, chunk;
-    if (!tokens_find<Shape::kRows>(a, sh.find, pos, end, chunk)) {
+    TokensRun run;
+    if (!tokens_find<Shape::kRows>(a, sh.find, run)) {
         if (threadIdx.x == 0) a.joins[blockIdx.x] = TokensJoin{};
         return;
     }
@@ -1218,7 +1262,7 @@ __global__ void __launch_bounds__(kTokThreads, 1)
     __syncthreads();
     tc_fence_after();
     const uint32_t q_smem = smem_u32(s_tokens), tmem = *reinterpret_cast<volatile uint32_t *>(&sh.tmem);
-    K k{a, sh, sh.find.at, pos, end, chunk, q_smem, q_smem + Shape::kQBytes, tmem, &sh.abort, &k_map, &v_map, &q_map};
+    K k{a, sh, sh.find.at, run, q_smem, q_smem + Shape::kQBytes, tmem, &sh.abort, &k_map, &v_map, &q_map};
     if (warp < kTokSoftmaxWarps) {
         regs_increase<K::kSoftmaxRegs>();
         k.softmax(warp);
