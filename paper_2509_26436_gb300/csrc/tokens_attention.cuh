@@ -159,7 +159,7 @@ struct TokensRun {
 };
 
 // Most of a block's edge: it costs as much as 3 tiles.  Less where a CTA has few
-// tiles (a sixteenth), so that none has edges alone.
+// tiles (a quarter of them), so that none has edges alone.
 constexpr int kTokEdge = 3;
 
 // Of all tiles of all sequences, heads and row blocks, in that order, this CTA's
@@ -183,7 +183,7 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
     long long all_tiles = 0, all_blocks = 0, before = 0;
 #pragma unroll
     for (int w = 0; w < kTokWarps; ++w) all_tiles += f.tiles[w], all_blocks += f.blocks[w];
-    run.edge = static_cast<int>(min(static_cast<long long>(kTokEdge), all_tiles / (16 * gridDim.x)));
+    run.edge = static_cast<int>(min(static_cast<long long>(kTokEdge), all_tiles / (4 * gridDim.x)));
     for (int w = 0; w < warp; ++w) before += f.tiles[w] + run.edge * f.blocks[w];
     const long long all = all_tiles + run.edge * all_blocks, mine_all = (tiles + run.edge * blocks) * a.kv_heads;
     run.chunk = (all + gridDim.x - 1) / gridDim.x;
@@ -297,13 +297,15 @@ struct TokensWalk {
 template <int D, int TILES>
 struct TokensShape {
     static constexpr int kRows = 128 * TILES;
-    static constexpr int kUnitDims = D % 128 == 0 ? 128 : 64, kUnits = D / kUnitDims;  // units of a tile's side
+    static constexpr int kUnitDims = D == 128 ? 128 : 64, kUnits = D / kUnitDims;  // units of a tile's side
+    // Units that one product of the weights takes: next to each other in the ring
+    static constexpr int kTogether = D == 256 ? 2 : kUnits;
     static constexpr int kPanel = kTokKeys * 128;  // 64 dimensions, 128 bytes a row
     static constexpr int kUnitBytes = kTokKeys * kUnitDims * 2, kQTile = 128 * D * 2, kQBytes = TILES * kQTile;
     static constexpr int kMisc = 3072;  // static shared memory, with its padding
-    static constexpr int kOutWarp = 4096, kOut = kTokSoftmaxWarps * kOutWarp;  // results on their way out: 32 rows x 32 columns
+    static constexpr int kOutWarp = 2048, kOut = kTokSoftmaxWarps * kOutWarp;  // results on their way out: 32 rows x 64 bytes
     static constexpr int kFit = (232448 - kMisc - kQBytes - kOut) / kUnitBytes;
-    static constexpr int kRing = kFit < 12 ? kFit : 12;
+    static constexpr int kRing = (kFit < 12 ? kFit : 12) / kTogether * kTogether;
     static constexpr int kSmem = kQBytes + kRing * kUnitBytes + kOut;
     static_assert(kRing >= 2 * kUnits, "the values of a tile and the next keys are held together");
     static_assert(256 + TILES * D <= 512, "TMEM: two S, and O");
@@ -805,14 +807,17 @@ struct TokensKernel {
 
     // --- products -------------------------------------------------------------
     static constexpr uint32_t kIdescS = idesc_16_f32(kBf, false, 128, kTokKeys);
-    static constexpr uint32_t kIdescO = idesc_16_f32(kBf, true, 128, Shape::kUnitDims);
+    static constexpr uint32_t kIdescO = idesc_16_f32(kBf, true, 128, Shape::kTogether * Shape::kUnitDims);
 
-    // S[buf] = Q[tile] K', the keys in units u ..
-    __device__ __forceinline__ void issue_s(int tile, int buf, int u) const
+    // S[buf] = Q[tile] K', the keys in units u .., each when it is there.  `last`:
+    // its place is free again.  (All lanes; false: gave up.)
+    __device__ __forceinline__ bool issue_s(int tile, int buf, int u, bool leader, bool last) const
     {
         const uint32_t q_low = sdesc_low(sdesc_k_major_sw128(q_smem + tile * Shape::kQTile));
 #pragma unroll
         for (int k = 0; k < Shape::kUnits; ++k) {
+            if (!wait_full(u + k)) return false;
+            if (!leader) continue;
             const uint32_t k_low = sdesc_low(sdesc_k_major_sw128(unit_at(u + k)));
 #pragma unroll
             for (int i = 0; i < Shape::kUnitDims / 16; ++i) {
@@ -820,30 +825,28 @@ struct TokensKernel {
                 mma_f16_ss(tmem + buf * 128, sdesc_sw128_at(q_low, k * (Shape::kUnitDims / 64) * Shape::kPanel + in),
                            sdesc_sw128_at(k_low, in), kIdescS, k + i > 0);
             }
+            if (last) mma_commit(smem_u32(&sh.empty[(u + k) % Shape::kRing]));
         }
+        if (leader) mma_commit(smem_u32(&sh.s_full[buf]));
+        return true;
     }
     // O[tile] (+)= P[buf] V, the values in units u ..
-    __device__ __forceinline__ void issue_o(int tile, int buf, int u, bool add) const
+    __device__ __forceinline__ bool issue_o(int tile, int buf, int u, bool add, bool leader, bool last) const
     {
 #pragma unroll
-        for (int k = 0; k < Shape::kUnits; ++k) {
+        for (int k = 0; k < Shape::kUnits; k += Shape::kTogether) {
+            for (int x = 0; x < Shape::kTogether; ++x)
+                if (!wait_full(u + k + x)) return false;
+            if (!leader) continue;
             const uint32_t v_low = sdesc_low(sdesc_mn_major_sw128(unit_at(u + k), Shape::kPanel));
 #pragma unroll
             for (int i = 0; i < kTokKeys / 16; ++i)
-                mma_f16_ts(tmem + 256 + tile * D + k * Shape::kUnitDims,
-                           tmem + buf * 128 + i * 8, sdesc_sw128_at(v_low, i * 2048),
+                mma_f16_ts(tmem + 256 + tile * D + k * Shape::kUnitDims, tmem + buf * 128 + i * 8, sdesc_sw128_at(v_low, i * 2048),
                            kIdescO, add || i > 0);
+            if (last)
+                for (int x = 0; x < Shape::kTogether; ++x) mma_commit(smem_u32(&sh.empty[(u + k + x) % Shape::kRing]));
         }
-    }
-    __device__ __forceinline__ void release(int u) const
-    {
-#pragma unroll
-        for (int k = 0; k < Shape::kUnits; ++k) mma_commit(smem_u32(&sh.empty[(u + k) % Shape::kRing]));
-    }
-    __device__ __forceinline__ bool wait_units(int u) const
-    {
-        for (int k = 0; k < Shape::kUnits; ++k)
-            if (!wait_full(u + k)) return false;
+        if (leader) mma_commit(smem_u32(&sh.pv_done[tile]));
         return true;
     }
 
@@ -853,63 +856,35 @@ struct TokensKernel {
         int it = 0, seg = 0;  // tiles and blocks so far
         bool ok = true;
         for (Walk w(a, at, run); ok && w.more(); w.next(), ++seg) {
-            if (!(ok = wait(sh.q_full, seg) && wait_units(2 * Shape::kUnits * it))) break;
+            if (!(ok = wait(sh.q_full, seg))) break;
             tc_fence_after();
-            if (leader) {
-                const int u = 2 * Shape::kUnits * it;
 #pragma unroll
-                for (int t = 0; t < TILES; ++t) {
-                    issue_s(t, TILES == 2 ? t : it & 1, u);
-                    mma_commit(smem_u32(&sh.s_full[TILES == 2 ? t : it & 1]));
-                }
-                release(u);
-                if (w.count == 1) mma_commit(smem_u32(&sh.q_free));
-            }
+            for (int t = 0; ok && t < TILES; ++t) ok = issue_s(t, TILES == 2 ? t : it & 1, 2 * Shape::kUnits * it, leader, t + 1 == TILES);
+            if (!ok) break;
+            if (leader && w.count == 1) mma_commit(smem_u32(&sh.q_free));
             for (int i = 0; i < w.count; ++i, ++it) {
                 const int uk = 2 * Shape::kUnits * (it + 1), uv = uk - Shape::kUnits;  // next keys, these values
                 const bool again = i + 1 < w.count, last = i + 2 == w.count;
                 if constexpr (TILES == 2) {
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
-                        if (t == 0 && !(ok = wait_units(uv))) break;
                         if (!(ok = wait(sh.p_ready[t], it))) break;
                         tc_fence_after();
-                        if (leader) {
-                            issue_o(t, t, uv, i > 0);
-                            mma_commit(smem_u32(&sh.pv_done[t]));
-                            if (t == 1) release(uv);
-                        }
-                        if (!again) continue;
-                        if (t == 0 && !(ok = wait_units(uk))) break;
-                        if (leader) {
-                            issue_s(t, t, uk);
-                            mma_commit(smem_u32(&sh.s_full[t]));
-                            if (t == 1) {
-                                release(uk);
-                                if (last) mma_commit(smem_u32(&sh.q_free));
-                            }
-                        }
+                        if (!(ok = issue_o(t, t, uv, i > 0, leader, t == 1))) break;
+                        if (again && !(ok = issue_s(t, t, uk, leader, t == 1))) break;
                     }
                     if (!ok) break;
+                    if (leader && last) mma_commit(smem_u32(&sh.q_free));
                 } else {
                     if (again) {
-                        if (!(ok = wait_units(uk))) break;
-                        if (leader) {
-                            issue_s(0, (it + 1) & 1, uk);
-                            mma_commit(smem_u32(&sh.s_full[(it + 1) & 1]));
-                            release(uk);
-                            if (last) mma_commit(smem_u32(&sh.q_free));
-                        }
+                        if (!(ok = issue_s(0, (it + 1) & 1, uk, leader, true))) break;
+                        if (leader && last) mma_commit(smem_u32(&sh.q_free));
                     }
-                    if (!(ok = wait_units(uv) && wait(sh.p_ready[it & 1], it >> 1))) break;
+                    if (!(ok = wait(sh.p_ready[it & 1], it >> 1))) break;
                     if (i == 0 && seg > 0 && !(ok = wait(sh.o_free, seg - 1))) break;
                     tc_fence_after();
-                    if (leader) {
-                        issue_o(0, it & 1, uv, i > 0);
-                        mma_commit(smem_u32(&sh.pv_done[0]));
-                        release(uv);
-                        if (!again) mma_commit(smem_u32(&sh.o_done));
-                    }
+                    if (!(ok = issue_o(0, it & 1, uv, i > 0, leader, true))) break;
+                    if (leader && !again) mma_commit(smem_u32(&sh.o_done));
                 }
             }
         }
@@ -1167,19 +1142,24 @@ struct TokensKernel {
                 }
                 if (!whole || a.o_type == QUARTZ_OUT_F32) {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        sts_b128(stage + lane * 128 + (((x ^ lane) & 7) << 4),
-                                 make_uint4(__float_as_uint(v[4 * x]), __float_as_uint(v[4 * x + 1]), __float_as_uint(v[4 * x + 2]), __float_as_uint(v[4 * x + 3])));
-                    __syncwarp();
+                    for (int y = 0; y < 32; y += 16) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int to = i * 4 + lane / 8, x = lane % 8;
-                        const float4 f = lds_f4(stage + to * 128 + (((x ^ to) & 7) << 4));
-                        const int64_t at_row = __shfl_sync(0xffffffffu, out, to);
-                        if (rows >> to & 1) {
-                            if (whole) *reinterpret_cast<float4 *>(static_cast<float *>(a.o) + at_row + c + x * 4) = f;
-                            else *reinterpret_cast<float4 *>(a.part_o + part0 + to * D + c + x * 4) = f;
+                        for (int x = 0; x < 4; ++x)
+                            sts_b128(stage + lane * 64 + (((x ^ lane >> 1) & 3) << 4),
+                                     make_uint4(__float_as_uint(v[y + 4 * x]), __float_as_uint(v[y + 4 * x + 1]),
+                                                __float_as_uint(v[y + 4 * x + 2]), __float_as_uint(v[y + 4 * x + 3])));
+                        __syncwarp();
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int to = i * 8 + lane / 4, x = lane % 4;
+                            const float4 f = lds_f4(stage + to * 64 + (((x ^ to >> 1) & 3) << 4));
+                            const int64_t at_row = __shfl_sync(0xffffffffu, out, to);
+                            if (rows >> to & 1) {
+                                if (whole) *reinterpret_cast<float4 *>(static_cast<float *>(a.o) + at_row + c + y + x * 4) = f;
+                                else *reinterpret_cast<float4 *>(a.part_o + part0 + to * D + c + y + x * 4) = f;
+                            }
                         }
+                        __syncwarp();
                     }
                 } else {
 #pragma unroll
