@@ -20,7 +20,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libquartz.so")
 BUILD_DIR = os.path.join(ROOT, "_build")
 SOURCES = ["api.cu", "quantize.cu", "linear.cu", "noalloc.cu", "attention.cu", "probe.cu", "rope.cu", "paged.cu",
-           "paged_attention.cu", "paged_attention_lzs.cu", "evict.cu", "paged_api.cu", "head_norm.cu", "tokens_api.cu",
+           "paged_attention.cu", "paged_attention_lzs.cu", "evict.cu", "paged_api.cu", "head_norm.cu",
+           "head_norm_rotate.cu", "head_norm_backward.cu", "tokens_api.cu",
            "tokens_attention.cu"] + [f"tokens_attention_{d}{x}.cu" for d in (64, 128, 192, 256) for x in ("", "_shaped")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 

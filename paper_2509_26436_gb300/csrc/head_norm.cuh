@@ -1,0 +1,386 @@
+// The norm of each head and rotary positions of one or several axes in one pass,
+// for sm_103a, and their gradient:
+//   n = x r,  r = (mean x^2 + eps)^-1/2,  y = R (n w)
+//   g = R' dy,  dx = r (g w - n mean(g w n)),  dw = sum over tokens and heads of g n
+// (R turns pair i by position[axis of i] times frequency i; R' is its transpose),
+// and R or R' alone.
+//
+// HBM-bound: x (and dy) read and y (dx) written once, some 5 to 15 operations per
+// element.  A row (a head of a token) belongs to a group of 4 to 32 lanes, each
+// with V pairs (two vectors) or V elements that are not turned; the sums over the
+// head, in binary32, go across the lanes, and the next row's loads are under way
+// meanwhile.  A CTA takes blocks of tokens of one side (queries or keys), whose
+// angles it computes once for all their heads: an angle costs about as much as
+// six heads' pairs.  dw: each lane sums its elements over its rows, a CTA joins
+// its groups, a second kernel the CTAs; all in a fixed order.
+#pragma once
+
+#include "quartz_internal.h"
+#include "rope.cuh"
+
+namespace quartz {
+
+constexpr int kNormThreads = 256;
+constexpr int kMostHere = 16;  // tokens of a block
+
+enum NormMode { kRotate, kForward, kBackward };
+
+// CTAs per SM: as many as the registers of a lane's vectors, angles, weights and
+// sums allow.
+template <typename T, int MODE, int E>  // E: pairs a lane
+constexpr int kPerSm = MODE == kRotate ? 4 : MODE == kForward ? (sizeof(T) == 4 ? 2 : 3) : (sizeof(T) * E <= 16 ? 2 : 1);
+constexpr int kMostBackward = 2;
+
+template <typename T, int V>
+struct alignas(sizeof(T) * V) Vec {
+    T e[V];
+};
+
+// The elements of a vector in binary32.
+template <typename T, int V>
+__device__ __forceinline__ void to_floats(const Vec<T, V> &v, float (&f)[V])
+{
+#pragma unroll
+    for (int j = 0; j < V; ++j) f[j] = to_f32<T>(v.e[j]);
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_rounded(T *to, const float (&f)[V])
+{
+    Vec<T, V> v;
+    if constexpr (sizeof(T) == 2 && V > 1) {
+        uint32_t *w = reinterpret_cast<uint32_t *>(&v);
+#pragma unroll
+        for (int j = 0; j < V / 2; ++j) w[j] = pack_pair<T>(f[2 * j], f[2 * j + 1]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) v.e[j] = from_f32<T>(f[j]);
+    }
+    *reinterpret_cast<Vec<T, V> *>(to) = v;
+}
+
+__device__ __forceinline__ float weight_at(const void *w, int type, int i)
+{
+    if (!w) return 1.f;
+    if (type == QUARTZ_OUT_F32) return static_cast<const float *>(w)[i];
+    if (type == QUARTZ_OUT_F16) return __half2float(static_cast<const __half *>(w)[i]);
+    return __bfloat162float(static_cast<const __nv_bfloat16 *>(w)[i]);
+}
+
+// Elements a lane's piece p holds: pairs p V .. as two vectors (first, first +
+// gap), or V elements behind the turned ones (a second vector of nothing).
+struct NormPiece {
+    int first;
+    bool in, turn;
+};
+
+// L lanes a row, NP pieces a lane (L NP >= pieces).  A group of L lanes takes one
+// token of the block and every (groups / here)-th of its heads, so that a lane's
+// angles, as its weights, are in registers.  INTER: pairs lie side by side.
+template <typename T, int V, int NP, int MODE, bool INTER>
+__global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_norm_kernel(HeadNormArgs a, int lanes_log2, int here)
+{
+    griddep_wait();
+    extern __shared__ __align__(16) float s_dyn[];
+    constexpr bool kBack = MODE == kBackward;
+    const int pairs = a.rotary / 2, turns = pairs / V, pieces = turns + (a.dim - a.rotary) / V;
+    const int L = 1 << lanes_log2, groups = kNormThreads >> lanes_log2;
+    const int width = L * NP * V;  // places of a head, at [j][piece] for each j < V
+    // pairs' units and axes; the block's angles [token][j][piece]
+    uint64_t *s_unit = reinterpret_cast<uint64_t *>(s_dyn);
+    int *s_axis = reinterpret_cast<int *>(s_unit + pairs);
+    float2 *s_cs = reinterpret_cast<float2 *>(s_axis + ((pairs + 1) & ~1));
+
+    const int side = static_cast<int>(blockIdx.x) >= a.ctas[0];
+    const int cta = static_cast<int>(blockIdx.x) - (side ? a.ctas[0] : 0), ctas = a.ctas[side];
+    const HeadNormSide &sd = a.side[side];
+    const int heads = sd.heads;
+    const int group = threadIdx.x >> lanes_log2, lane = threadIdx.x & (L - 1);
+    const int tk = group & (here - 1), sub = group / here, step = groups / here;  // `here` is a power of two
+
+    // pairs side by side in memory, or (V = 1 either way) `gap` apart
+    const bool beside = INTER || (V == 1 && a.interleaved);
+    NormPiece pc[NP];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int p = lane + i * L;
+        pc[i].in = p < pieces;
+        pc[i].turn = p < turns;
+        pc[i].first = !pc[i].in ? 0 : pc[i].turn ? (beside ? 2 * p * V : p * V) : a.rotary + (p - turns) * V;
+    }
+    const int gap = beside ? V : pairs;
+    // element of the first (x) and second (y) of a pair, place j of piece p
+    auto element = [&](int p, int j, int second) {
+        if (p < turns) return beside ? 2 * (p * V + j) + second : p * V + j + second * pairs;
+        return a.rotary + (p - turns) * V + j;
+    };
+    for (int i = threadIdx.x; i < pairs; i += kNormThreads) {
+        s_unit[i] = rope_unit(a.freqs[i]);
+        int axis = a.pair_axis ? a.pair_axis[i] : 0;
+        if (axis < 0 || axis >= a.axes) {
+            atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
+            axis = 0;
+        }
+        s_axis[i] = axis;
+    }
+    constexpr int NW = MODE == kRotate ? 1 : NP, VW = MODE == kRotate ? 1 : V, ND = kBack ? NP : 1, VD = kBack ? V : 1;
+    float w1[NW][VW], w2[NW][VW], dw1[ND][VD], dw2[ND][VD];
+    if (MODE != kRotate)
+#pragma unroll
+        for (int i = 0; i < NW; ++i)
+#pragma unroll
+            for (int j = 0; j < VW; ++j) {
+                w1[i][j] = pc[i].in ? weight_at(sd.w, a.w_type, element(lane + i * L, j, 0)) : 0.f;
+                w2[i][j] = pc[i].turn ? weight_at(sd.w, a.w_type, element(lane + i * L, j, 1)) : 0.f;
+            }
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int j = 0; j < VD; ++j) dw1[i][j] = dw2[i][j] = 0.f;
+
+    // The pairs of two vectors; a piece that is not turned has zeros for its seconds,
+    // one that is not there (or a row) zeros.
+    auto pairs_of = [&](const Vec<T, V> &u, const Vec<T, V> &v, bool in, bool turn, float (&x1)[V], float (&x2)[V]) {
+        float f[2][V];
+        to_floats<T, V>(u, f[0]);
+        to_floats<T, V>(v, f[1]);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (INTER && turn) x1[j] = f[2 * j / V][2 * j % V], x2[j] = f[(2 * j + 1) / V][(2 * j + 1) % V];
+            else x1[j] = f[0][j], x2[j] = f[1][j];
+        }
+        if (!turn)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                x2[j] = 0.f;
+                if (!in) x1[j] = 0.f;
+            }
+    };
+    const int rounds = (heads + step - 1) / step;  // as often for every lane of a warp
+    for (int64_t t0 = static_cast<int64_t>(cta) * here; t0 < a.tokens; t0 += static_cast<int64_t>(ctas) * here) {
+        const int its = static_cast<int>(min(static_cast<int64_t>(here), a.tokens - t0));
+        const int64_t t = t0 + tk;
+        const int end = tk < its ? heads : 0;
+        const T *x = static_cast<const T *>(sd.x) + t * sd.x_st;
+        const T *dy = kBack ? static_cast<const T *>(sd.dy) + t * sd.dy_st : nullptr;
+        T *y = static_cast<T *>(sd.y) + t * sd.y_st;
+        // the row's vectors; the loads of a row that is not there are left out
+        Vec<T, V> u[NP], v[NP], du[ND], dv[ND];
+        auto load = [&](int h) {
+            if (h >= end) return;
+            const T *from = x + h * sd.x_sh;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                if (pc[i].in) u[i] = *reinterpret_cast<const Vec<T, V> *>(from + pc[i].first);
+                if (pc[i].turn) v[i] = *reinterpret_cast<const Vec<T, V> *>(from + pc[i].first + gap);
+            }
+            if constexpr (kBack) {
+                const T *d = dy + h * sd.dy_sh;
+#pragma unroll
+                for (int i = 0; i < NP; ++i) {
+                    if (pc[i].in) du[i] = *reinterpret_cast<const Vec<T, V> *>(d + pc[i].first);
+                    if (pc[i].turn) dv[i] = *reinterpret_cast<const Vec<T, V> *>(d + pc[i].first + gap);
+                }
+            }
+        };
+        load(sub);        // under way while the angles are computed
+        __syncthreads();  // the units; the block before is done with its angles
+        for (int i = threadIdx.x; i < its * pairs; i += kNormThreads) {
+            const int k = i / pairs, j = i - k * pairs;
+            float2 cs = rope_cos_sin(a.positions[s_axis[j] * a.axis_stride + t0 + k], s_unit[j], a.scale);
+            if (kBack || (MODE == kRotate && a.backward)) cs.y = -cs.y;
+            s_cs[k * width + (j % V) * (L * NP) + j / V] = cs;
+        }
+        __syncthreads();
+        float2 cs[NP][V];
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                cs[i][j] = s_cs[tk * width + lane + j * (L * NP) + i * L];
+                if (!pc[i].turn) cs[i][j] = make_float2(1.f, 0.f);
+            }
+        for (int n = 0, h = sub; n < rounds; ++n, h += step) {
+            const bool in = h < end;
+            float x1[NP][V], x2[NP][V], g1[ND][VD], g2[ND][VD];
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                pairs_of(u[i], v[i], in && pc[i].in, pc[i].turn, x1[i], x2[i]);
+                if constexpr (kBack) {
+                    pairs_of(du[i], dv[i], in && pc[i].in, pc[i].turn, g1[i], g2[i]);
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const float2 g = rope_turn(g1[i][j], g2[i][j], cs[i][j]);
+                        g1[i][j] = g.x, g2[i][j] = g.y;
+                    }
+                }
+            }
+            load(h + step);
+            float r = 1.f, ra = 0.f;
+            if (MODE != kRotate) {
+                float ss = 0.f, dot = 0.f;
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        ss += x1[i][j] * x1[i][j];
+                        ss += x2[i][j] * x2[i][j];
+                        if constexpr (kBack) {
+                            dot += g1[i][j] * w1[i][j] * x1[i][j];
+                            dot += g2[i][j] * w2[i][j] * x2[i][j];
+                        }
+                    }
+                for (int d = 1; d < L; d *= 2) {
+                    ss += __shfl_xor_sync(0xffffffffu, ss, d);
+                    if (kBack) dot += __shfl_xor_sync(0xffffffffu, dot, d);
+                }
+                r = rsqrtf(ss * a.inv_dim + a.eps);
+                ra = r * r * r * dot * a.inv_dim;
+            }
+            if (!in) continue;
+            T *to = y + h * sd.y_sh;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                if (!pc[i].in) continue;
+                float f[2][V];  // the two vectors' elements
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    float2 z;
+                    if constexpr (kBack) {
+                        z.x = r * g1[i][j] * w1[i][j] - x1[i][j] * ra;
+                        z.y = r * g2[i][j] * w2[i][j] - x2[i][j] * ra;
+                        dw1[i][j] += g1[i][j] * (x1[i][j] * r);
+                        dw2[i][j] += g2[i][j] * (x2[i][j] * r);
+                    } else if constexpr (MODE == kForward) {
+                        z = rope_turn(x1[i][j] * (r * w1[i][j]), x2[i][j] * (r * w2[i][j]), cs[i][j]);
+                    } else {
+                        z = rope_turn(x1[i][j], x2[i][j], cs[i][j]);
+                    }
+                    if (INTER && pc[i].turn) f[2 * j / V][2 * j % V] = z.x, f[(2 * j + 1) / V][(2 * j + 1) % V] = z.y;
+                    else f[0][j] = z.x, f[1][j] = z.y;
+                }
+                store_rounded<T, V>(to + pc[i].first, f[0]);
+                if (pc[i].turn) store_rounded<T, V>(to + pc[i].first + gap, f[1]);
+            }
+        }
+    }
+    if constexpr (kBack) {
+        if (!a.part) return;
+        // the groups' sums, [group][element], over the angles' memory
+        float *s_dw = reinterpret_cast<float *>(s_cs);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int p = lane + i * L;
+                if (pc[i].in) s_dw[group * a.dim + element(p, j, 0)] = dw1[i][j];
+                if (pc[i].turn) s_dw[group * a.dim + element(p, j, 1)] = dw2[i][j];
+            }
+        __syncthreads();
+        for (int d = threadIdx.x; d < a.dim; d += kNormThreads) {
+            float s = 0.f;
+            for (int g = 0; g < groups; ++g) s += s_dw[g * a.dim + d];
+            a.part[static_cast<int64_t>(blockIdx.x) * a.dim + d] = s;
+        }
+    }
+}
+
+// Lanes of a row, tokens of a block and CTAs of each side.
+struct HeadNormPlan {
+    int lanes_log2, here, groups;
+    int ctas[2];
+};
+
+inline HeadNormPlan head_norm_plan(const int (&heads)[2], int64_t tokens, int pieces, int per_sm)
+{
+    HeadNormPlan p;
+    p.lanes_log2 = 2;
+    while (p.lanes_log2 < 5 && (1 << p.lanes_log2) < pieces) ++p.lanes_log2;
+    p.groups = kNormThreads >> p.lanes_log2;
+    const int64_t all = static_cast<int64_t>(heads[0]) + heads[1], wave = static_cast<int64_t>(device_sms()) * per_sm;
+    // Blocks of up to 16 tokens, at most one for each group, while they fill the
+    // SMs twice and leave a group some heads: a token's angles are read once then.
+    int here = 1;
+    while (here < kMostHere && here < p.groups && (tokens + 2 * here - 1) / (2 * here) >= 2 * wave &&
+           static_cast<int64_t>(heads[0]) * here >= p.groups / 2)
+        here *= 2;
+    p.here = here;
+    const int64_t blocks = (tokens + here - 1) / here;
+    for (int i = 0; i < 2; ++i) {
+        int64_t n = heads[i] ? (wave * heads[i] + all - 1) / all : 0;
+        p.ctas[i] = static_cast<int>(n < blocks ? n : blocks);
+    }
+    return p;
+}
+
+template <typename T>
+bool norm_fits(const HeadNormArgs &a, int mode, int v)
+{
+    const uintptr_t m = v * sizeof(T) - 1;
+    if ((a.rotary / 2) % v || (a.dim - a.rotary) % v) return false;
+    for (const HeadNormSide &s : a.side) {
+        if (!s.heads) continue;
+        int64_t strides = s.x_st | s.x_sh | s.y_st | s.y_sh;
+        uintptr_t places = reinterpret_cast<uintptr_t>(s.x) | reinterpret_cast<uintptr_t>(s.y);
+        if (mode == kBackward) strides |= s.dy_st | s.dy_sh, places |= reinterpret_cast<uintptr_t>(s.dy);
+        if (strides % v || (places & m)) return false;
+    }
+    return true;
+}
+
+template <typename T, int V, int NP, int MODE, bool INTER>
+cudaError_t launch_norm_v(HeadNormArgs &a, cudaStream_t s)
+{
+    const int pairs = a.rotary / 2, pieces = pairs / V + (a.dim - a.rotary) / V;
+    const int heads[2] = {a.side[0].heads, a.side[1].heads};
+    const HeadNormPlan p = head_norm_plan(heads, a.tokens, pieces, kPerSm<T, MODE, V * NP>);
+    a.ctas[0] = p.ctas[0], a.ctas[1] = p.ctas[1];
+    const int width = (1 << p.lanes_log2) * NP * V;
+    int bytes = pairs * 8 + ((pairs + 1) & ~1) * 4;
+    int rest = p.here * width * 8;
+    if (MODE == kBackward && rest < p.groups * a.dim * 4) rest = p.groups * a.dim * 4;
+    bytes += rest;
+    static_assert(NP * V * 32 <= 256, "shared memory stays below 48 KB");
+    return launch_pdl(head_norm_kernel<T, V, NP, MODE, INTER>, dim3(static_cast<unsigned>(p.ctas[0] + p.ctas[1])), dim3(kNormThreads),
+                      bytes, s, a, p.lanes_log2, p.here);
+}
+
+// Pieces a lane: one where 32 lanes' are enough (heads of up to 256 elements).
+template <typename T, int V, int MODE, bool INTER>
+cudaError_t launch_norm_np(HeadNormArgs &a, cudaStream_t s)
+{
+    if constexpr (V * 32 < 256)
+        if (a.rotary / 2 / V + (a.dim - a.rotary) / V > 32) return launch_norm_v<T, V, 256 / V / 32, MODE, INTER>(a, s);
+    return launch_norm_v<T, V, 1, MODE, INTER>(a, s);
+}
+
+// The widest vectors (16 bytes, or 8) that sizes, strides and addresses allow;
+// else one element at a time.
+template <typename T, int MODE>
+cudaError_t launch_norm_t(HeadNormArgs &a, cudaStream_t s)
+{
+    constexpr int wide = 16 / sizeof(T);
+    for (int v = wide; v > 1; v /= 2) {
+        if (!norm_fits<T>(a, MODE, v)) continue;
+        if (v == wide) return a.interleaved ? launch_norm_np<T, wide, MODE, true>(a, s) : launch_norm_np<T, wide, MODE, false>(a, s);
+        if (v == wide / 2) return a.interleaved ? launch_norm_np<T, wide / 2, MODE, true>(a, s) : launch_norm_np<T, wide / 2, MODE, false>(a, s);
+        break;
+    }
+    return launch_norm_v<T, 1, 8, MODE, false>(a, s);
+}
+
+template <int MODE>
+cudaError_t launch_norm_mode(HeadNormArgs &a, cudaStream_t s)
+{
+    if (a.type == QUARTZ_OUT_F16) return launch_norm_t<__half, MODE>(a, s);
+    if (a.type == QUARTZ_OUT_BF16) return launch_norm_t<__nv_bfloat16, MODE>(a, s);
+    return launch_norm_t<float, MODE>(a, s);
+}
+
+// A unit each (head_norm_rotate.cu, head_norm.cu, head_norm_backward.cu); the
+// last sets a.ctas.
+cudaError_t launch_norm_rotate(HeadNormArgs &a, cudaStream_t s);
+cudaError_t launch_norm_forward(HeadNormArgs &a, cudaStream_t s);
+cudaError_t launch_norm_backward(HeadNormArgs &a, cudaStream_t s);
+
+}  // namespace quartz

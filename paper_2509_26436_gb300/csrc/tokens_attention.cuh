@@ -446,7 +446,7 @@ struct TokensKernel {
     static constexpr float kUp = kBf ? 0.f : 8.f, kSlack = kBf ? 8.f : 7.f;
     using Walk = TokensWalk<R>;
     // Registers a thread of the softmax, filling and last warpgroups, of 512 x 128.
-    static constexpr int kSoftmaxRegs = 152, kFillRegs = kLzs ? 128 : 104, kLastRegs = kLzs ? 80 : 104;
+    static constexpr int kSoftmaxRegs = 160, kFillRegs = kLzs ? 112 : 96, kLastRegs = kLzs ? 80 : 96;
     static_assert(2 * kSoftmaxRegs + kFillRegs + kLastRegs <= 4 * 128, "");
 
     const TokensArgs &a;
