@@ -15,7 +15,7 @@
 // its groups, a second kernel the CTAs; all in a fixed order.
 #pragma once
 
-#include "quartz_internal.h"
+#include "ptx.cuh"
 #include "rope.cuh"
 
 namespace quartz {
@@ -30,6 +30,11 @@ enum NormMode { kRotate, kForward, kBackward };
 template <typename T, int MODE, int E>  // E: pairs a lane
 constexpr int kPerSm = MODE == kRotate ? 4 : MODE == kForward ? (sizeof(T) == 4 ? 2 : 3) : (sizeof(T) * E <= 16 ? 2 : 1);
 constexpr int kMostBackward = 2;
+
+// Rows that a lane's copies are ahead, each in memory of its own, so that some
+// 128 KB per SM are on their way; elements one at a time are loaded as needed.
+template <typename T, int MODE, int V>
+constexpr int kAhead = sizeof(T) * V < 8 ? 0 : MODE == kBackward ? 4 : MODE == kForward ? 6 : 5;
 
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Vec {
@@ -77,7 +82,7 @@ struct NormPiece {
 // token of the block and every (groups / here)-th of its heads, so that a lane's
 // angles, as its weights, are in registers.  INTER: pairs lie side by side.
 template <typename T, int V, int NP, int MODE, bool INTER>
-__global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_norm_kernel(HeadNormArgs a, int lanes_log2, int here)
+__global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_norm_kernel(HeadNormArgs a, int lanes_log2, int q_here, int k_here)
 {
     griddep_wait();
     extern __shared__ __align__(16) float s_dyn[];
@@ -93,7 +98,7 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
     const int side = static_cast<int>(blockIdx.x) >= a.ctas[0];
     const int cta = static_cast<int>(blockIdx.x) - (side ? a.ctas[0] : 0), ctas = a.ctas[side];
     const HeadNormSide &sd = a.side[side];
-    const int heads = sd.heads;
+    const int heads = sd.heads, here = side ? k_here : q_here;
     const int group = threadIdx.x >> lanes_log2, lane = threadIdx.x & (L - 1);
     const int tk = group & (here - 1), sub = group / here, step = groups / here;  // `here` is a power of two
 
@@ -155,34 +160,49 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
                 if (!in) x1[j] = 0.f;
             }
     };
+    // The rows' vectors on their way: [stage][vector][thread], read by the lane that
+    // copies them alone.  `ahead` is the row that is asked for next.
+    constexpr int S = kAhead<T, MODE, V>, kVecs = (kBack ? 4 : 2) * NP;
+    Vec<T, V> *s_ring = reinterpret_cast<Vec<T, V> *>(reinterpret_cast<uint8_t *>(s_dyn) + a.ring_at) + threadIdx.x;
     const int rounds = (heads + step - 1) / step;  // as often for every lane of a warp
-    for (int64_t t0 = static_cast<int64_t>(cta) * here; t0 < a.tokens; t0 += static_cast<int64_t>(ctas) * here) {
+    const int64_t stride = static_cast<int64_t>(ctas) * here;
+    int64_t t_ahead = static_cast<int64_t>(cta) * here;  // of a block
+    int n_ahead = 0, stage_ahead = 0, stage = 0;
+    auto vectors = [&](int64_t t, int h, auto take) {
+        const T *from = static_cast<const T *>(sd.x) + t * sd.x_st + h * sd.x_sh;
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            if (pc[i].in) take(2 * i, from + pc[i].first);
+            if (pc[i].turn) take(2 * i + 1, from + pc[i].first + gap);
+        }
+        if constexpr (kBack) {
+            const T *d = static_cast<const T *>(sd.dy) + t * sd.dy_st + h * sd.dy_sh;
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                if (pc[i].in) take(2 * NP + 2 * i, d + pc[i].first);
+                if (pc[i].turn) take(2 * NP + 2 * i + 1, d + pc[i].first + gap);
+            }
+        }
+    };
+    auto ask = [&] {
+        if constexpr (S > 0) {
+            if (t_ahead + tk < a.tokens && sub + n_ahead * step < heads)
+                vectors(t_ahead + tk, sub + n_ahead * step, [&](int k, const T *from) {
+                    const uint32_t to = smem_u32(s_ring + (stage_ahead * kVecs + k) * kNormThreads);
+                    if constexpr (sizeof(T) * V == 16) cp_async16(to, from);
+                    else cp_async8(to, from);
+                });
+            cp_async_commit();
+            stage_ahead = stage_ahead + 1 == S ? 0 : stage_ahead + 1;
+            if (++n_ahead == rounds) n_ahead = 0, t_ahead += stride;
+        }
+    };
+    for (int i = 0; i < S - 1; ++i) ask();
+    for (int64_t t0 = static_cast<int64_t>(cta) * here; t0 < a.tokens; t0 += stride) {
         const int its = static_cast<int>(min(static_cast<int64_t>(here), a.tokens - t0));
         const int64_t t = t0 + tk;
         const int end = tk < its ? heads : 0;
-        const T *x = static_cast<const T *>(sd.x) + t * sd.x_st;
-        const T *dy = kBack ? static_cast<const T *>(sd.dy) + t * sd.dy_st : nullptr;
         T *y = static_cast<T *>(sd.y) + t * sd.y_st;
-        // the row's vectors; the loads of a row that is not there are left out
-        Vec<T, V> u[NP], v[NP], du[ND], dv[ND];
-        auto load = [&](int h) {
-            if (h >= end) return;
-            const T *from = x + h * sd.x_sh;
-#pragma unroll
-            for (int i = 0; i < NP; ++i) {
-                if (pc[i].in) u[i] = *reinterpret_cast<const Vec<T, V> *>(from + pc[i].first);
-                if (pc[i].turn) v[i] = *reinterpret_cast<const Vec<T, V> *>(from + pc[i].first + gap);
-            }
-            if constexpr (kBack) {
-                const T *d = dy + h * sd.dy_sh;
-#pragma unroll
-                for (int i = 0; i < NP; ++i) {
-                    if (pc[i].in) du[i] = *reinterpret_cast<const Vec<T, V> *>(d + pc[i].first);
-                    if (pc[i].turn) dv[i] = *reinterpret_cast<const Vec<T, V> *>(d + pc[i].first + gap);
-                }
-            }
-        };
-        load(sub);        // under way while the angles are computed
         __syncthreads();  // the units; the block before is done with its angles
         for (int i = threadIdx.x; i < its * pairs; i += kNormThreads) {
             const int k = i / pairs, j = i - k * pairs;
@@ -201,12 +221,23 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
             }
         for (int n = 0, h = sub; n < rounds; ++n, h += step) {
             const bool in = h < end;
+            Vec<T, V> raw[kVecs];
+            ask();
+            if constexpr (S > 0) {
+                cp_async_wait<S - 1>();
+                if (in)
+#pragma unroll
+                    for (int k = 0; k < kVecs; ++k) raw[k] = s_ring[(stage * kVecs + k) * kNormThreads];
+                stage = stage + 1 == S ? 0 : stage + 1;
+            } else if (in) {
+                vectors(t, h, [&](int k, const T *from) { raw[k] = *reinterpret_cast<const Vec<T, V> *>(from); });
+            }
             float x1[NP][V], x2[NP][V], g1[ND][VD], g2[ND][VD];
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                pairs_of(u[i], v[i], in && pc[i].in, pc[i].turn, x1[i], x2[i]);
+                pairs_of(raw[2 * i], raw[2 * i + 1], in && pc[i].in, in && pc[i].turn, x1[i], x2[i]);
                 if constexpr (kBack) {
-                    pairs_of(du[i], dv[i], in && pc[i].in, pc[i].turn, g1[i], g2[i]);
+                    pairs_of(raw[2 * NP + 2 * i], raw[2 * NP + 2 * i + 1], in && pc[i].in, in && pc[i].turn, g1[i], g2[i]);
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const float2 g = rope_turn(g1[i][j], g2[i][j], cs[i][j]);
@@ -214,7 +245,6 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
                     }
                 }
             }
-            load(h + step);
             float r = 1.f, ra = 0.f;
             if (MODE != kRotate) {
                 float ss = 0.f, dot = 0.f;
@@ -264,6 +294,7 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
         }
     }
     if constexpr (kBack) {
+        cp_async_wait<0>();
         if (!a.part) return;
         // the groups' sums, [group][element], over the angles' memory
         float *s_dw = reinterpret_cast<float *>(s_cs);
@@ -285,30 +316,38 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
     }
 }
 
-// Lanes of a row, tokens of a block and CTAs of each side.
+// Lanes of a row; tokens of a block and CTAs of each side.
 struct HeadNormPlan {
-    int lanes_log2, here, groups;
-    int ctas[2];
+    int lanes_log2, groups;
+    int here[2], ctas[2];
 };
 
-inline HeadNormPlan head_norm_plan(const int (&heads)[2], int64_t tokens, int pieces, int per_sm)
+inline HeadNormPlan head_norm_plan(const int (&heads)[2], int64_t tokens, int pieces, int pairs, int per_sm)
 {
     HeadNormPlan p;
     p.lanes_log2 = 2;
     while (p.lanes_log2 < 5 && (1 << p.lanes_log2) < pieces) ++p.lanes_log2;
     p.groups = kNormThreads >> p.lanes_log2;
-    const int64_t all = static_cast<int64_t>(heads[0]) + heads[1], wave = static_cast<int64_t>(device_sms()) * per_sm;
-    // Blocks of up to 16 tokens, at most one for each group, while they fill the
-    // SMs twice and leave a group some heads: a token's angles are read once then.
-    int here = 1;
-    while (here < kMostHere && here < p.groups && (tokens + 2 * here - 1) / (2 * here) >= 2 * wave &&
-           static_cast<int64_t>(heads[0]) * here >= p.groups / 2)
-        here *= 2;
-    p.here = here;
-    const int64_t blocks = (tokens + here - 1) / here;
+    const int64_t wave = static_cast<int64_t>(device_sms()) * per_sm;
+    // A side's work: its heads, and the angles, which cost about as much as 3.
+    const int64_t work[2] = {heads[0] ? heads[0] + 3 : 0, heads[1] ? heads[1] + 3 : 0}, sum = work[0] + work[1];
     for (int i = 0; i < 2; ++i) {
-        int64_t n = heads[i] ? (wave * heads[i] + all - 1) / all : 0;
-        p.ctas[i] = static_cast<int>(n < blocks ? n : blocks);
+        p.here[i] = 1, p.ctas[i] = 0;
+        if (!heads[i]) continue;
+        const int64_t most = (wave * work[i] + sum - 1) / sum;
+        // Of blocks of 1, 2, .. 16 tokens (one for each group at most) those whose last
+        // CTA is done first: in rows a group, a block costs its rows, one for the waits
+        // and a third for each angle a thread has.
+        int64_t least = 0;
+        for (int here = 1; here <= kMostHere && here <= p.groups; here *= 2) {
+            const int64_t blocks = (tokens + here - 1) / here, step = p.groups / here;
+            const int64_t turns = blocks < most ? 1 : (blocks + most - 1) / most;
+            const int64_t cost = turns * (3 * ((heads[i] + step - 1) / step) + 3 + (here * pairs + kNormThreads - 1) / kNormThreads);
+            if (here > 1 && cost >= least) continue;
+            least = cost;
+            p.here[i] = here;
+            p.ctas[i] = static_cast<int>(blocks < most ? blocks : most);
+        }
     }
     return p;
 }
@@ -333,16 +372,21 @@ cudaError_t launch_norm_v(HeadNormArgs &a, cudaStream_t s)
 {
     const int pairs = a.rotary / 2, pieces = pairs / V + (a.dim - a.rotary) / V;
     const int heads[2] = {a.side[0].heads, a.side[1].heads};
-    const HeadNormPlan p = head_norm_plan(heads, a.tokens, pieces, kPerSm<T, MODE, V * NP>);
+    const HeadNormPlan p = head_norm_plan(heads, a.tokens, pieces, pairs, kPerSm<T, MODE, V * NP>);
     a.ctas[0] = p.ctas[0], a.ctas[1] = p.ctas[1];
     const int width = (1 << p.lanes_log2) * NP * V;
     int bytes = pairs * 8 + ((pairs + 1) & ~1) * 4;
-    int rest = p.here * width * 8;
+    int rest = (p.here[0] > p.here[1] ? p.here[0] : p.here[1]) * width * 8;
     if (MODE == kBackward && rest < p.groups * a.dim * 4) rest = p.groups * a.dim * 4;
-    bytes += rest;
-    static_assert(NP * V * 32 <= 256, "shared memory stays below 48 KB");
+    bytes = (bytes + rest + 15) & ~15;
+    static_assert(NP * V * 32 <= 256, "units, angles and sums stay below 37 KB");
+    constexpr int kRing = kAhead<T, MODE, V> * (MODE == kBackward ? 4 : 2) * NP * static_cast<int>(sizeof(T)) * V * kNormThreads;
+    a.ring_at = bytes;
+    bytes += kRing;
+    const cudaError_t e = allow_shared<head_norm_kernel<T, V, NP, MODE, INTER>>(kRing + 37 * 1024);
+    if (e != cudaSuccess) return e;
     return launch_pdl(head_norm_kernel<T, V, NP, MODE, INTER>, dim3(static_cast<unsigned>(p.ctas[0] + p.ctas[1])), dim3(kNormThreads),
-                      bytes, s, a, p.lanes_log2, p.here);
+                      bytes, s, a, p.lanes_log2, p.here[0], p.here[1]);
 }
 
 // Pieces a lane: one where 32 lanes' are enough (heads of up to 256 elements).

@@ -229,6 +229,7 @@ struct HeadNormArgs {
     float scale, eps, inv_dim;
     float *part;  // backward: NULL, or the CTAs' sums for dw
     int ctas[2];  // of each side
+    int ring_at;  // where the rows on their way begin in shared memory
     int *dev_err;
 };
 size_t head_norm_workspace_bytes(int dim);
