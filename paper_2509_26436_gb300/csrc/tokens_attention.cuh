@@ -303,7 +303,10 @@ struct TokensShape {
     static constexpr int kPanel = kTokKeys * 128;  // 64 dimensions, 128 bytes a row
     static constexpr int kUnitBytes = kTokKeys * kUnitDims * 2, kQTile = 128 * D * 2, kQBytes = TILES * kQTile;
     static constexpr int kMisc = 3072;  // static shared memory, with its padding
-    static constexpr int kOutWarp = 2048, kOut = kTokSoftmaxWarps * kOutWarp;  // results on their way out: 32 rows x 64 bytes
+    // Results on their way out, 32 rows x 64 bytes a warp.  Heads of 256 have none: the
+    // ring holds two units more than a tile's keys and values instead, which are under
+    // way while those are used.
+    static constexpr int kOutWarp = D == 256 ? 0 : 2048, kOut = kTokSoftmaxWarps * kOutWarp;
     static constexpr int kFit = (232448 - kMisc - kQBytes - kOut) / kUnitBytes;
     static constexpr int kRing = (kFit < 12 ? kFit : 12) / kTogether * kTogether;
     static constexpr int kSmem = kQBytes + kRing * kUnitBytes + kOut;
@@ -1140,7 +1143,23 @@ struct TokensKernel {
                     const int from = kLzs ? (x & ~7) + (x & 3) * 2 + (x >> 2 & 1) : x;
                     v[x] = __uint_as_float(s[from]) * inv;
                 }
-                if (!whole || a.o_type == QUARTZ_OUT_F32) {
+                auto halves = [&](int x) {  // elements x and x + 1 in the result's type
+                    if (a.o_type == QUARTZ_OUT_BF16) return bf16_pair(v[x], v[x + 1]);
+                    const __half2 h = __floats2half2_rn(v[x], v[x + 1]);
+                    return *reinterpret_cast<const uint32_t *>(&h);
+                };
+                if constexpr (Shape::kOut == 0) {
+                    if (valid && (!whole || a.o_type == QUARTZ_OUT_F32)) {
+                        float *to = whole ? static_cast<float *>(a.o) + out + c : a.part_o + part0 + lane * D + c;
+#pragma unroll
+                        for (int x = 0; x < 32; x += 4) *reinterpret_cast<float4 *>(to + x) = make_float4(v[x], v[x + 1], v[x + 2], v[x + 3]);
+                    } else if (valid) {
+#pragma unroll
+                        for (int x = 0; x < 32; x += 8)
+                            *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(a.o) + out + c + x) =
+                                make_uint4(halves(x), halves(x + 2), halves(x + 4), halves(x + 6));
+                    }
+                } else if (!whole || a.o_type == QUARTZ_OUT_F32) {
 #pragma unroll
                     for (int y = 0; y < 32; y += 16) {
 #pragma unroll
@@ -1164,17 +1183,8 @@ struct TokensKernel {
                 } else {
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        uint32_t h[4];
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) {
-                            if (a.o_type == QUARTZ_OUT_BF16) {
-                                h[y] = bf16_pair(v[8 * x + 2 * y], v[8 * x + 2 * y + 1]);
-                            } else {
-                                const __half2 two = __floats2half2_rn(v[8 * x + 2 * y], v[8 * x + 2 * y + 1]);
-                                h[y] = *reinterpret_cast<const uint32_t *>(&two);
-                            }
-                        }
-                        sts_b128(stage + lane * 64 + (((x ^ lane >> 1) & 3) << 4), make_uint4(h[0], h[1], h[2], h[3]));
+                        sts_b128(stage + lane * 64 + (((x ^ lane >> 1) & 3) << 4),
+                                 make_uint4(halves(8 * x), halves(8 * x + 2), halves(8 * x + 4), halves(8 * x + 6)));
                     }
                     __syncwarp();
 #pragma unroll
