@@ -8,9 +8,9 @@
 namespace quartz {
 namespace {
 
-constexpr int kJoinThreads = 256, kJoinRows = 32;
+constexpr int kJoinThreads = 256, kJoinRows = 8;
 
-// CTA (x, y): rows 32 y .. of the block that CTA x of the attention began and the
+// CTA (x, y): rows 8 y .. of the block that CTA x of the attention began and the
 // next ones went on with, a thread per 4 elements, the parts in the keys' order.
 template <int D>
 __global__ void __launch_bounds__(kJoinThreads) tokens_join_kernel(TokensArgs a, int R)
@@ -156,7 +156,7 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
         const uint32_t box[4] = {64, static_cast<uint32_t>(a.group), static_cast<uint32_t>(128 / a.group), 1};
         a.q_box = make_pool_map(&m.q, c->type == QUARTZ_PAGES_BF16, call.q, dims, strides, box);
     }
-    const dim3 grid(static_cast<unsigned>(p.ctas), static_cast<unsigned>(4 * p.tiles)), block(kJoinThreads);
+    const dim3 grid(static_cast<unsigned>(p.ctas), static_cast<unsigned>(128 / kJoinRows * p.tiles)), block(kJoinThreads);
     const int R = 128 * p.tiles;
     const bool shaped = call.mask.cap > 0.f || call.mask.slopes || !(call.scale > 0.f);
     cudaError_t e;
