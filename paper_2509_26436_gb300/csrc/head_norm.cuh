@@ -80,8 +80,9 @@ struct NormPiece {
 
 // L lanes a row, NP pieces a lane (L NP >= pieces).  A group of L lanes takes one
 // token of the block and every (groups / here)-th of its heads, so that a lane's
-// angles, as its weights, are in registers.  INTER: pairs lie side by side.
-template <typename T, int V, int NP, int MODE, bool INTER>
+// angles, as its weights, are in registers.  INTER: pairs lie side by side.  FULL:
+// every lane has pairs alone (else a third more instructions, for what is not).
+template <typename T, int V, int NP, int MODE, bool INTER, bool FULL>
 __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_norm_kernel(HeadNormArgs a, int lanes_log2, int q_here, int k_here)
 {
     griddep_wait();
@@ -108,14 +109,14 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int p = lane + i * L;
-        pc[i].in = p < pieces;
-        pc[i].turn = p < turns;
+        pc[i].in = FULL || p < pieces;
+        pc[i].turn = FULL || p < turns;
         pc[i].first = !pc[i].in ? 0 : pc[i].turn ? (beside ? 2 * p * V : p * V) : a.rotary + (p - turns) * V;
     }
     const int gap = beside ? V : pairs;
     // element of the first (x) and second (y) of a pair, place j of piece p
     auto element = [&](int p, int j, int second) {
-        if (p < turns) return beside ? 2 * (p * V + j) + second : p * V + j + second * pairs;
+        if (FULL || p < turns) return beside ? 2 * (p * V + j) + second : p * V + j + second * pairs;
         return a.rotary + (p - turns) * V + j;
     };
     for (int i = threadIdx.x; i < pairs; i += kNormThreads) {
@@ -143,7 +144,7 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
         for (int j = 0; j < VD; ++j) dw1[i][j] = dw2[i][j] = 0.f;
 
     // The pairs of two vectors; a piece that is not turned has zeros for its seconds,
-    // one that is not there (or a row) zeros.
+    // one that is not there zeros.  (Of a row that is not there they may be anything.)
     auto pairs_of = [&](const Vec<T, V> &u, const Vec<T, V> &v, bool in, bool turn, float (&x1)[V], float (&x2)[V]) {
         float f[2][V];
         to_floats<T, V>(u, f[0]);
@@ -225,7 +226,6 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
             ask();
             if constexpr (S > 0) {
                 cp_async_wait<S - 1>();
-                if (in)
 #pragma unroll
                     for (int k = 0; k < kVecs; ++k) raw[k] = s_ring[(stage * kVecs + k) * kNormThreads];
                 stage = stage + 1 == S ? 0 : stage + 1;
@@ -235,9 +235,9 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
             float x1[NP][V], x2[NP][V], g1[ND][VD], g2[ND][VD];
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
-                pairs_of(raw[2 * i], raw[2 * i + 1], in && pc[i].in, in && pc[i].turn, x1[i], x2[i]);
+                pairs_of(raw[2 * i], raw[2 * i + 1], pc[i].in, pc[i].turn, x1[i], x2[i]);
                 if constexpr (kBack) {
-                    pairs_of(raw[2 * NP + 2 * i], raw[2 * NP + 2 * i + 1], in && pc[i].in, in && pc[i].turn, g1[i], g2[i]);
+                    pairs_of(raw[2 * NP + 2 * i], raw[2 * NP + 2 * i + 1], pc[i].in, pc[i].turn, g1[i], g2[i]);
 #pragma unroll
                     for (int j = 0; j < V; ++j) {
                         const float2 g = rope_turn(g1[i][j], g2[i][j], cs[i][j]);
@@ -367,7 +367,7 @@ bool norm_fits(const HeadNormArgs &a, int mode, int v)
     return true;
 }
 
-template <typename T, int V, int NP, int MODE, bool INTER>
+template <typename T, int V, int NP, int MODE, bool INTER, bool FULL>
 cudaError_t launch_norm_v(HeadNormArgs &a, cudaStream_t s)
 {
     const int pairs = a.rotary / 2, pieces = pairs / V + (a.dim - a.rotary) / V;
@@ -383,9 +383,9 @@ cudaError_t launch_norm_v(HeadNormArgs &a, cudaStream_t s)
     constexpr int kRing = kAhead<T, MODE, V> * (MODE == kBackward ? 4 : 2) * NP * static_cast<int>(sizeof(T)) * V * kNormThreads;
     a.ring_at = bytes;
     bytes += kRing;
-    const cudaError_t e = allow_shared<head_norm_kernel<T, V, NP, MODE, INTER>>(kRing + 37 * 1024);
+    const cudaError_t e = allow_shared<head_norm_kernel<T, V, NP, MODE, INTER, FULL>>(kRing + 37 * 1024);
     if (e != cudaSuccess) return e;
-    return launch_pdl(head_norm_kernel<T, V, NP, MODE, INTER>, dim3(static_cast<unsigned>(p.ctas[0] + p.ctas[1])), dim3(kNormThreads),
+    return launch_pdl(head_norm_kernel<T, V, NP, MODE, INTER, FULL>, dim3(static_cast<unsigned>(p.ctas[0] + p.ctas[1])), dim3(kNormThreads),
                       bytes, s, a, p.lanes_log2, p.here[0], p.here[1]);
 }
 
@@ -393,9 +393,12 @@ cudaError_t launch_norm_v(HeadNormArgs &a, cudaStream_t s)
 template <typename T, int V, int MODE, bool INTER>
 cudaError_t launch_norm_np(HeadNormArgs &a, cudaStream_t s)
 {
+    const int turns = a.rotary / 2 / V, pieces = turns + (a.dim - a.rotary) / V;
     if constexpr (V * 32 < 256)
-        if (a.rotary / 2 / V + (a.dim - a.rotary) / V > 32) return launch_norm_v<T, V, 256 / V / 32, MODE, INTER>(a, s);
-    return launch_norm_v<T, V, 1, MODE, INTER>(a, s);
+        if (pieces > 32) return launch_norm_v<T, V, 256 / V / 32, MODE, INTER, false>(a, s);
+    if constexpr (V * sizeof(T) == 16)
+        if (pieces == turns && (pieces == 4 || pieces == 8 || pieces == 16 || pieces == 32)) return launch_norm_v<T, V, 1, MODE, INTER, true>(a, s);
+    return launch_norm_v<T, V, 1, MODE, INTER, false>(a, s);
 }
 
 // The widest vectors (16 bytes, or 8) that sizes, strides and addresses allow;
@@ -410,7 +413,7 @@ cudaError_t launch_norm_t(HeadNormArgs &a, cudaStream_t s)
         if (v == wide / 2) return a.interleaved ? launch_norm_np<T, wide / 2, MODE, true>(a, s) : launch_norm_np<T, wide / 2, MODE, false>(a, s);
         break;
     }
-    return launch_norm_v<T, 1, 8, MODE, false>(a, s);
+    return launch_norm_v<T, 1, 8, MODE, false, false>(a, s);
 }
 
 template <int MODE>

@@ -18,7 +18,7 @@
 // O stays in TMEM; it is rescaled only when a maximum rises by more than `slack`,
 // so hardly ever.
 //
-// Warps: 8 softmax; 4 that fill a ring of [128 tokens x 64 or 128 dimensions]
+// Warps: 8 softmax; 4 or 8 that fill a ring of [128 tokens x 64 or 128 dimensions]
 // units, keys and values in turn, from the pages (TMA or 16-byte copies, into the
 // 128-byte swizzle; encoded pages: decoded to fp16 on the way); one that issues
 // the products; three that load queries.
@@ -37,9 +37,9 @@
 
 namespace quartz {
 
-constexpr int kTokSoftmaxWarps = 8, kTokFillWarps = 4;
+constexpr int kTokSoftmaxWarps = 8;
 constexpr int kTokQueryWarps = 3;
-constexpr int kTokWarps = kTokSoftmaxWarps + kTokFillWarps + 1 + kTokQueryWarps, kTokThreads = kTokWarps * 32;
+constexpr int kTokMostWarps = 20;
 constexpr int kTokKeys = 128;  // keys of a tile
 constexpr int kTokTreeMost = 64;
 
@@ -148,7 +148,7 @@ struct TokensPlace {
 };
 
 struct TokensFind {
-    long long tiles[kTokWarps], blocks[kTokWarps];
+    long long tiles[kTokMostWarps], blocks[kTokMostWarps];
     TokensPlace at;
 };
 
@@ -167,8 +167,8 @@ constexpr int kTokEdge = 3;
 template <int R>
 __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
 {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int share = (a.seqs + kTokWarps - 1) / kTokWarps;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+    const int share = (a.seqs + warps - 1) / warps;
     const int b0 = min(a.seqs, warp * share), b1 = min(a.seqs, b0 + share);
     long long tiles = 0, blocks = 0;
     for (int b = b0; b < b1; b += 32) {
@@ -181,8 +181,7 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
     if (lane == 0) f.tiles[warp] = tiles * a.kv_heads, f.blocks[warp] = blocks * a.kv_heads;
     __syncthreads();
     long long all_tiles = 0, all_blocks = 0, before = 0;
-#pragma unroll
-    for (int w = 0; w < kTokWarps; ++w) all_tiles += f.tiles[w], all_blocks += f.blocks[w];
+    for (int w = 0; w < warps; ++w) all_tiles += f.tiles[w], all_blocks += f.blocks[w];
     run.edge = static_cast<int>(min(static_cast<long long>(kTokEdge), all_tiles / (4 * gridDim.x)));
     for (int w = 0; w < warp; ++w) before += f.tiles[w] + run.edge * f.blocks[w];
     const long long all = all_tiles + run.edge * all_blocks, mine_all = (tiles + run.edge * blocks) * a.kv_heads;
@@ -448,9 +447,13 @@ struct TokensKernel {
     // to 2^-22 of the largest in full.
     static constexpr float kUp = kBf ? 0.f : 8.f, kSlack = kBf ? 8.f : 7.f;
     using Walk = TokensWalk<R>;
-    // Registers a thread of the softmax, filling and last warpgroups, of 512 x 128.
-    static constexpr int kSoftmaxRegs = 160, kFillRegs = kLzs ? 112 : 96, kLastRegs = kLzs ? 80 : 96;
-    static_assert(2 * kSoftmaxRegs + kFillRegs + kLastRegs <= 4 * 128, "");
+    // Filling warps: decoding takes twice as many.  Then registers a thread of the
+    // softmax, the filling and the last warps, together what the CTA is launched with.
+    static constexpr int kFillWarps = kLzs ? 8 : 4, kWarps = kTokSoftmaxWarps + kFillWarps + 1 + kTokQueryWarps, kThreads = kWarps * 32;
+    static constexpr int kLaunchRegs = kLzs ? 96 : 128;
+    static constexpr int kSoftmaxRegs = kLzs ? 144 : 160, kFillRegs = kLzs ? 72 : 96, kLastRegs = kLzs ? 48 : 96;
+    static_assert(kTokSoftmaxWarps * kSoftmaxRegs + kFillWarps * kFillRegs + 4 * kLastRegs <= kWarps * kLaunchRegs, "");
+    static_assert(kWarps <= kTokMostWarps, "");
 
     const TokensArgs &a;
     TokensShared &sh;
@@ -516,15 +519,15 @@ struct TokensKernel {
                     for (int r = r_first; r < rows; r += kStep, step()) cp_async16(to(r), q + token * a.q_st + g * a.q_sh);
                 } else {
                     // the eight elements of a chunk in the order of the decoded keys
-                    for (int r0 = r_first; r0 < rows; r0 += 8 * kStep) {
-                        uint4 v[8];
+                    for (int r0 = r_first; r0 < rows; r0 += 4 * kStep) {
+                        uint4 v[4];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
+                        for (int i = 0; i < 4; ++i) {
                             if (r0 + i * kStep < rows) v[i] = *reinterpret_cast<const uint4 *>(q + token * a.q_st + g * a.q_sh);
                             step();
                         }
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
+                        for (int i = 0; i < 4; ++i)
                             if (r0 + i * kStep < rows)
                                 sts_b128(to(r0 + i * kStep),
                                          make_uint4(prmt(v[i].x, v[i].z, 0x5410), prmt(v[i].x, v[i].z, 0x7632),
@@ -695,67 +698,89 @@ struct TokensKernel {
         if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
     }
 
-    // A lane's pieces of a unit of encoded rows: 64 elements each, a scale's.
-    static constexpr int kPieces = Shape::kUnitDims / 64, kPieceRows = 32 / kPieces;
-    struct Pieces {
-        uint4 codes[kPieces][2];
-        uint2 flags[kPieces];  // G_s = 8: a byte per 8 elements; 16, 32, 64: the first 4, 2, 1 bytes
-        uint16_t scale[kPieces];
+    // A lane's piece of a unit of encoded rows: half a row's elements of it.  A warp
+    // has 16 rows.
+    static constexpr int kWarpRows = kTokKeys / kFillWarps, kPiece = Shape::kUnitDims / 2;
+    struct Piece {
+        uint4 codes[kPiece / 32];
+        uint32_t flags[kPiece / 32];  // bytes; G_s = 8: 4 or 8 of them, 16: 2 or 4, 32: 1 or 2, 64: 1
+        uint16_t scale;
     };
 
-    // Rows [kPieceRows i ..) of this warp's 32 tokens; `row` is this lane's token's
-    // row (-1: zeros).
-    __device__ __forceinline__ void load_pieces(const PagedSide &p, int row, int dim0, Pieces &to) const
+    // Lane / 2 of this warp's rows; `row` is that of lane's token (-1: zeros).
+    __device__ __forceinline__ void load_piece(const PagedSide &p, int row, int dim0, Piece &to) const
     {
-        const int lane = threadIdx.x & 31, e = dim0 + (lane % kPieces) * 64;
+        const int lane = threadIdx.x & 31, e = dim0 + (lane & 1) * kPiece;
+        const int64_t r = __shfl_sync(0xffffffffu, row, lane >> 1);
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int64_t r = __shfl_sync(0xffffffffu, row, i * kPieceRows + lane / kPieces);
-            to.codes[i][0] = to.codes[i][1] = make_uint4(0u, 0u, 0u, 0u);
-            to.flags[i] = make_uint2(0u, 0u), to.scale[i] = 0;
-            if (r >= 0) {
-                const uint4 *c = reinterpret_cast<const uint4 *>(p.codes + r * (D / 2) + e / 2);
-                to.codes[i][0] = __ldg(c), to.codes[i][1] = __ldg(c + 1);
-                const uint8_t *f = p.flags + r * (D >> a.gs_shift) + (e >> a.gs_shift);
-                if (a.gs_shift == 3) to.flags[i] = __ldg(reinterpret_cast<const uint2 *>(f));
-                else if (a.gs_shift == 4) to.flags[i].x = __ldg(reinterpret_cast<const uint32_t *>(f));
-                else if (a.gs_shift == 5) to.flags[i].x = __ldg(reinterpret_cast<const uint16_t *>(f));
-                else to.flags[i].x = __ldg(f);
-                to.scale[i] = __ldg(reinterpret_cast<const uint16_t *>(p.scales) + r * (D / 64) + e / 64);
+        for (int i = 0; i < kPiece / 32; ++i) to.codes[i] = make_uint4(0u, 0u, 0u, 0u), to.flags[i] = 0;
+        to.scale = 0;
+        if (r < 0) return;
+        const uint4 *c = reinterpret_cast<const uint4 *>(p.codes + r * (D / 2) + e / 2);
+#pragma unroll
+        for (int i = 0; i < kPiece / 32; ++i) to.codes[i] = __ldg(c + i);
+        const uint8_t *f = p.flags + r * (D >> a.gs_shift) + (e >> a.gs_shift);
+        if constexpr (kPiece == 64) {
+            if (a.gs_shift == 3) {
+                const uint2 two = __ldg(reinterpret_cast<const uint2 *>(f));
+                to.flags[0] = two.x, to.flags[1] = two.y;
+            } else if (a.gs_shift == 4) {
+                to.flags[0] = __ldg(reinterpret_cast<const uint32_t *>(f));
+            } else if (a.gs_shift == 5) {
+                to.flags[0] = __ldg(reinterpret_cast<const uint16_t *>(f));
+            } else {
+                to.flags[0] = __ldg(f);
             }
+        } else {
+            if (a.gs_shift == 3) to.flags[0] = __ldg(reinterpret_cast<const uint32_t *>(f));
+            else if (a.gs_shift == 4) to.flags[0] = __ldg(reinterpret_cast<const uint16_t *>(f));
+            else to.flags[0] = __ldg(f);
         }
+        to.scale = __ldg(reinterpret_cast<const uint16_t *>(p.scales) + r * (D / 64) + e / 64);
     }
 
     // Decoded to fp16, elements (0, 4), (1, 5), (2, 6), (3, 7) of each eight side
     // by side.  Codes times 2^FLAG are exact; the product with the scale is
     // rounded once.
-    __device__ __forceinline__ void store_pieces(const Pieces &p, uint32_t unit, int warp) const
+    __device__ __forceinline__ void store_piece(const Piece &p, uint32_t unit, int warp) const
     {
-        const int lane = threadIdx.x & 31, c = lane % kPieces, flip = c * 4;
+        constexpr int kWords = kPiece / 8;
+        const int lane = threadIdx.x & 31, c = lane & 1, r = warp * kWarpRows + (lane >> 1);
+        const uint32_t scale = prmt(p.scale, 0, 0x1010);
+        // a byte per 8 elements
+        uint32_t f[kPiece / 32];
+        if (a.gs_shift == 3) {
+            for (int i = 0; i < kPiece / 32; ++i) f[i] = p.flags[i];
+        } else {
+            f[0] = prmt(p.flags[0], 0, a.gs_shift == 4 ? 0x1100 : 0x0000);
+            if (kPiece == 64) f[kPiece / 32 - 1] = prmt(p.flags[0], 0, a.gs_shift == 4 ? 0x3322 : a.gs_shift == 5 ? 0x1111 : 0x0000);
+        }
+        uint32_t w[kWords];
 #pragma unroll
-        for (int i = 0; i < kPieces; ++i) {
-            const int r = warp * 32 + i * kPieceRows + lane / kPieces;
-            const uint4 c0 = c ? p.codes[i][1] : p.codes[i][0], c1 = c ? p.codes[i][0] : p.codes[i][1];
-            const uint32_t w[8] = {c0.x, c0.y, c0.z, c0.w, c1.x, c1.y, c1.z, c1.w};
-            const uint32_t to = unit + c * Shape::kPanel + r * 128;
-            // a byte per 8 elements, in the order of w
-            uint32_t f0 = p.flags[i].x, f1 = p.flags[i].y;
-            if (a.gs_shift == 4) f1 = prmt(f0, 0, 0x3322), f0 = prmt(f0, 0, 0x1100);
-            else if (a.gs_shift == 5) f1 = prmt(f0, 0, 0x1111), f0 = prmt(f0, 0, 0x0000);
-            else if (a.gs_shift == 6) f0 = f1 = prmt(f0, 0, 0x0000);
-            const uint32_t f[2] = {c ? f1 : f0, c ? f0 : f1};
-            const uint32_t scale = prmt(p.scale[i], 0, 0x1010);
-            KeyFlag flag(0);
+        for (int i = 0; i < kPiece / 32; ++i) w[4 * i] = p.codes[i].x, w[4 * i + 1] = p.codes[i].y, w[4 * i + 2] = p.codes[i].z, w[4 * i + 3] = p.codes[i].w;
+        // The lanes of a row write to other banks at a time: 128 dimensions, two panels,
+        // the second begins with its other half; 64, one panel, a half each.
+        const bool flip = kPiece == 64 && c;
+        if (flip) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                // lanes of the second panel begin with the other half: other banks
-                if (j % 2 == 0 || a.gs_shift == 3) flag = KeyFlag(f[j / 4] >> (j % 4 * 8) & 255);
-                uint32_t k[4];
-                key_codes(w[j], flag, k);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) k[x] = mul_f16x2(k[x], scale);
-                sts_b128(to + (((j ^ flip ^ r) & 7) << 4), make_uint4(k[0], k[1], k[2], k[3]));
+            for (int i = 0; i < kWords / 2; ++i) {
+                const uint32_t t = w[i];
+                w[i] = w[i + kWords / 2], w[i + kWords / 2] = t;
             }
+            const uint32_t t = f[0];
+            f[0] = f[kPiece / 32 - 1], f[kPiece / 32 - 1] = t;
+        }
+        const uint32_t to = unit + (kPiece == 64 ? c * Shape::kPanel : 0) + r * 128;
+        const int first = kPiece == 64 ? (flip ? 4 : 0) : c * 4;  // chunk of the first word
+        KeyFlag flag(0);
+#pragma unroll
+        for (int j = 0; j < kWords; ++j) {
+            if (j % 2 == 0 || a.gs_shift == 3) flag = KeyFlag(f[j / 4] >> (j % 4 * 8) & 255);
+            uint32_t k[4];
+            key_codes(w[j], flag, k);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) k[x] = mul_f16x2(k[x], scale);
+            sts_b128(to + ((((j ^ first) ^ r) & 7) << 4), make_uint4(k[0], k[1], k[2], k[3]));
         }
     }
 
@@ -769,18 +794,18 @@ struct TokensKernel {
         int i = 0, u = 0;
         bool there_next;
         auto lookup = [&](int i) {
-            const int t = w.tile(i) * kTokKeys + warp * 32 + lane;
+            const int t = w.tile(i) * kTokKeys + warp * kWarpRows + lane % kWarpRows;
             there_next = l.has(t);
             return page_entry(w, t, there_next);
         };
         uint32_t page_next = lookup(0);
-        Pieces now, next;
+        Piece now, next;
         bool held = false, ok = true;
         while (ok) {
             const bool more = w.more();
             int row = -1;
             if (more) {
-                const int t = w.tile(i) * kTokKeys + warp * 32 + lane, page = checked(page_next, bad);
+                const int t = w.tile(i) * kTokKeys + warp * kWarpRows + lane % kWarpRows, page = checked(page_next, bad);
                 if (there_next) row = ((page * a.kv_heads + w.p.head) << a.page_shift) + (t & mask);
                 if (i + 1 < w.count) {
                     page_next = lookup(++i);
@@ -794,10 +819,10 @@ struct TokensKernel {
             }
 #pragma unroll 1
             for (int k = 0; k < (more ? 2 * Shape::kUnits : 1); ++k) {
-                if (more) load_pieces(k < Shape::kUnits ? a.k : a.v, row, k % Shape::kUnits * Shape::kUnitDims, next);
+                if (more) load_piece(k < Shape::kUnits ? a.k : a.v, row, k % Shape::kUnits * Shape::kUnitDims, next);
                 if (held) {
                     if (!(ok = wait_empty(u))) break;
-                    store_pieces(now, unit_at(u), warp);
+                    store_piece(now, unit_at(u), warp);
                     arrive_full(u++);
                 }
                 now = next;
@@ -1208,7 +1233,7 @@ struct TokensKernel {
 };
 
 template <int D, int KIND, int TILES, bool SHAPED>
-__global__ void __launch_bounds__(kTokThreads, 1)
+__global__ void __launch_bounds__(TokensKernel<D, KIND, TILES, SHAPED>::kThreads, 1)
     tokens_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                        const __grid_constant__ CUtensorMap q_map, TokensArgs a)
 {
@@ -1226,7 +1251,7 @@ __global__ void __launch_bounds__(kTokThreads, 1)
     if (threadIdx.x == 0) {
         a.joins[blockIdx.x] = TokensJoin{};  // for a CTA that gives up
         for (int i = 0; i < Shape::kRing; ++i) {
-            mbar_init(smem_u32(&sh.full[i]), kTokFillWarps);
+            mbar_init(smem_u32(&sh.full[i]), K::kFillWarps);
             mbar_init(smem_u32(&sh.empty[i]), 1);
         }
         mbar_init(smem_u32(&sh.q_full), kTokQueryWarps);
@@ -1256,14 +1281,14 @@ __global__ void __launch_bounds__(kTokThreads, 1)
     if (warp < kTokSoftmaxWarps) {
         regs_increase<K::kSoftmaxRegs>();
         k.softmax(warp);
-    } else if (warp < kTokSoftmaxWarps + kTokFillWarps) {
+    } else if (warp < kTokSoftmaxWarps + K::kFillWarps) {
         regs_decrease<K::kFillRegs>();
         if constexpr (K::kLzs) k.fill_encoded(warp - kTokSoftmaxWarps);
         else k.fill_16bit(warp - kTokSoftmaxWarps);
     } else {
         regs_decrease<K::kLastRegs>();
-        if (warp == kTokSoftmaxWarps + kTokFillWarps) k.products();
-        else k.load_queries(warp - kTokSoftmaxWarps - kTokFillWarps - 1);
+        if (warp == kTokSoftmaxWarps + K::kFillWarps) k.products();
+        else k.load_queries(warp - kTokSoftmaxWarps - K::kFillWarps - 1);
     }
     tc_fence_before();
     __syncthreads();
@@ -1291,7 +1316,7 @@ cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int cta
     constexpr int kSmem = TokensShape<D, TILES>::kSmem;
     const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES, SHAPED>>(kSmem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(tokens_attn_kernel<D, KIND, TILES, SHAPED>, dim3(static_cast<unsigned>(ctas)), dim3(kTokThreads), kSmem, s,
+    return launch_pdl(tokens_attn_kernel<D, KIND, TILES, SHAPED>, dim3(static_cast<unsigned>(ctas)), dim3(TokensKernel<D, KIND, TILES, SHAPED>::kThreads), kSmem, s,
                       m.k, m.v, m.q, a);
 }
 
