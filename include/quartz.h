@@ -570,7 +570,8 @@ typedef struct {
  *                max_new apart.  Rows before the first and behind the last stay
  *                as they are in o
  *   mask         NULL: causal
- *   o            [tokens, q_heads, dim] contiguous, o_type, 16-byte aligned
+ *   o            [tokens, q_heads, dim] contiguous, o_type, 16-byte aligned; not
+ *                the memory of q
  *   workspace    >= quartz_paged_attention_tokens_workspace_size bytes, 16-byte
  *                aligned, scratch
  * A length or start out of range: that sequence's rows are undefined and
