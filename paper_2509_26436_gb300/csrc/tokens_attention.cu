@@ -49,17 +49,26 @@ __global__ void __launch_bounds__(kJoinThreads) tokens_join_kernel(TokensArgs a,
 
 struct TokensPlan {
     int tiles, ctas;
+    bool uncut;
 };
 
 // Two tiles side by side where a sequence may have more rows than one holds and
 // TMEM has room for them; a CTA per SM, as long as there may be so many tiles of
-// keys.
+// keys.  Blocks that all have an SM, of 8 tiles of keys at most, stay whole: the
+// join, and its workspace, cost more than they take from a CTA (8 drafted tokens,
+// 40 heads, 777 cached: 12.0 us a call, cut 17.8).
 TokensPlan tokens_plan(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len, int64_t max_new)
 {
     const int64_t group = q_heads / c->heads;
     TokensPlan p;
     p.tiles = c->dim <= 128 && max_new * group > 128 ? 2 : 1;
     const int64_t most = (tokens * group / (128 * p.tiles) + seqs) * c->heads * (max_len / kTokKeys + 2);
+    const int64_t blocks = (tokens * group / (128 * p.tiles) + seqs) * c->heads;
+    p.uncut = blocks <= device_sms() && max_len <= 8 * kTokKeys;
+    if (p.uncut) {
+        p.ctas = static_cast<int>(blocks > 0 ? blocks : 1);
+        return p;
+    }
     p.ctas = static_cast<int>(most < device_sms() ? (most > 0 ? most : 1) : device_sms());
     return p;
 }
@@ -100,6 +109,7 @@ size_t paged_tokens_workspace_bytes(const quartz_paged_cache_t *c, int64_t token
                                     int64_t max_new)
 {
     const TokensPlan p = tokens_plan(c, tokens, seqs, q_heads, max_len, max_new);
+    if (p.uncut) return 256;  // nothing is written to it
     const size_t rows = static_cast<size_t>(p.ctas) * 2 * 128 * p.tiles;
     return up256(rows * c->dim * 4) + up256(rows * 8) + up256(p.ctas * sizeof(TokensJoin));
 }
@@ -132,6 +142,7 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
     a.max_len = static_cast<int>(call.max_len), a.max_new = static_cast<int>(call.max_new);
     a.window = static_cast<int>(call.mask.window < call.max_len ? call.mask.window : 0);
     a.gs_shift = c->type == QUARTZ_PAGES_ENCODED ? log2_of(c->k.enc.p.group_s) : 0;
+    a.uncut = p.uncut;
     a.single = call.max_new * a.group <= 128 * p.tiles;
     a.scale_log2 = call.scale * kPagedLog2e;
     if (call.mask.cap > 0.f) a.cap_log2 = call.mask.cap * kPagedLog2e, a.to_cap = call.scale / call.mask.cap;
@@ -150,7 +161,8 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
         const int rows = c->page_size < kTokKeys ? c->page_size : kTokKeys;
         if (pool_map(&m.k, c, c->k, rows, a.k_order) && pool_map(&m.v, c, c->v, rows, a.v_order)) a.box_rows = rows;
     }
-    if (c->type != QUARTZ_PAGES_ENCODED && 128 % a.group == 0 && call.q_sh >= c->dim && call.q_st >= c->dim) {
+    // (a map costs the host 1 us, which few queries do not save)
+    if (c->type != QUARTZ_PAGES_ENCODED && 128 % a.group == 0 && call.max_new * a.group > 32 && call.q_sh >= c->dim && call.q_st >= c->dim) {
         const uint64_t dims[4] = {static_cast<uint64_t>(c->dim), static_cast<uint64_t>(call.q_heads), static_cast<uint64_t>(call.tokens), 1};
         const uint64_t strides[3] = {static_cast<uint64_t>(call.q_sh) * 2, static_cast<uint64_t>(call.q_st) * 2, static_cast<uint64_t>(call.q_st) * 2};
         const uint32_t box[4] = {64, static_cast<uint32_t>(a.group), static_cast<uint32_t>(128 / a.group), 1};
@@ -163,16 +175,16 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
     switch (c->dim) {
         case 64:
             e = (shaped ? launch_tokens_attn_64_shaped : launch_tokens_attn_64)(a, m, c->type, p.tiles, p.ctas, s);
-            return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<64>, grid, block, 0, s, a, R);
+            return e != cudaSuccess || p.uncut ? e : launch_pdl(tokens_join_kernel<64>, grid, block, 0, s, a, R);
         case 128:
             e = (shaped ? launch_tokens_attn_128_shaped : launch_tokens_attn_128)(a, m, c->type, p.tiles, p.ctas, s);
-            return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<128>, grid, block, 0, s, a, R);
+            return e != cudaSuccess || p.uncut ? e : launch_pdl(tokens_join_kernel<128>, grid, block, 0, s, a, R);
         case 192:
             e = (shaped ? launch_tokens_attn_192_shaped : launch_tokens_attn_192)(a, m, c->type, p.tiles, p.ctas, s);
-            return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<192>, grid, block, 0, s, a, R);
+            return e != cudaSuccess || p.uncut ? e : launch_pdl(tokens_join_kernel<192>, grid, block, 0, s, a, R);
         default:
             e = (shaped ? launch_tokens_attn_256_shaped : launch_tokens_attn_256)(a, m, c->type, p.tiles, p.ctas, s);
-            return e != cudaSuccess || p.ctas == 1 ? e : launch_pdl(tokens_join_kernel<256>, grid, block, 0, s, a, R);
+            return e != cudaSuccess || p.uncut ? e : launch_pdl(tokens_join_kernel<256>, grid, block, 0, s, a, R);
     }
 }
 

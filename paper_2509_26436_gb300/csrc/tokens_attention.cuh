@@ -61,6 +61,7 @@ struct TokensArgs {
     int k_order, v_order;
     int q_box;  // a box of the queries' map is a tile's rows and 64 dimensions
     int single;              // no sequence has more rows than one CTA takes
+    int uncut;               // a CTA per block of rows: no block is cut, and nothing joined
     int cap_near;            // the powers of to_cap fit binary32: the cap's short polynomial may be used
     float scale_log2;
     float cap_log2, to_cap;  // cap > 0: cap log2 e and scale / cap; else 0
@@ -183,15 +184,17 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
     long long all_tiles = 0, all_blocks = 0, before = 0;
     for (int w = 0; w < warps; ++w) all_tiles += f.tiles[w], all_blocks += f.blocks[w];
     run.edge = static_cast<int>(min(static_cast<long long>(kTokEdge), all_tiles / (4 * gridDim.x)));
-    for (int w = 0; w < warp; ++w) before += f.tiles[w] + run.edge * f.blocks[w];
-    const long long all = all_tiles + run.edge * all_blocks, mine_all = (tiles + run.edge * blocks) * a.kv_heads;
+    const int each = a.uncut ? 0 : 1;  // what a tile counts; uncut: blocks are counted instead
+    if (a.uncut) run.edge = 1;
+    for (int w = 0; w < warp; ++w) before += each * f.tiles[w] + run.edge * f.blocks[w];
+    const long long all = each * all_tiles + run.edge * all_blocks, mine_all = (each * tiles + run.edge * blocks) * a.kv_heads;
     run.chunk = (all + gridDim.x - 1) / gridDim.x;
     const long long pos = run.pos = run.chunk * blockIdx.x;
     run.end = min(pos + run.chunk, all);
     if (pos < run.end && pos >= before && pos < before + mine_all) {
         for (int b = b0; b < b1; b += 32) {
             const int2 n2 = tokens_seq_tiles<R>(a, b, b1);
-            const int mine = n2.x + run.edge * n2.y;
+            const int mine = each * n2.x + run.edge * n2.y;
             long long incl = mine;
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
@@ -213,7 +216,7 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
             const TokensSeq s = tokens_seq(a, p.b);
             const int blocks = tokens_blocks<R>(a, s);  // of this sequence
             for (int r0 = 0; r0 < blocks; r0 += 32) {
-                const int n = r0 + lane < blocks ? tokens_tiles<R>(a, s, r0 + lane).count + run.edge : 0;
+                const int n = r0 + lane < blocks ? each * tokens_tiles<R>(a, s, r0 + lane).count + run.edge : 0;
                 int sums = n;
 #pragma unroll
                 for (int d = 1; d < 32; d *= 2) {
@@ -259,6 +262,10 @@ struct TokensWalk {
     __device__ __forceinline__ void enter()
     {
         t = tokens_tiles<R>(a, s, p.block);
+        if (a.uncut) {
+            span = 1, first = 0, count = t.count;
+            return;
+        }
         const long long left = run.end - pos;
         const int most = t.count + run.edge - p.off;
         span = left < most ? static_cast<int>(left) : most;
@@ -1228,7 +1235,7 @@ struct TokensKernel {
                 if (lane == 0) mbar_arrive(smem_u32(&sh.o_free));
             }
         }
-        if (threadIdx.x == 0) a.joins[blockIdx.x] = join;
+        if (threadIdx.x == 0 && !a.uncut) a.joins[blockIdx.x] = join;
     }
 };
 
@@ -1245,11 +1252,11 @@ __global__ void __launch_bounds__(TokensKernel<D, KIND, TILES, SHAPED>::kThreads
     const int warp = threadIdx.x >> 5;
     TokensRun run;
     if (!tokens_find<Shape::kRows>(a, sh.find, run)) {
-        if (threadIdx.x == 0) a.joins[blockIdx.x] = TokensJoin{};
+        if (threadIdx.x == 0 && !a.uncut) a.joins[blockIdx.x] = TokensJoin{};
         return;
     }
     if (threadIdx.x == 0) {
-        a.joins[blockIdx.x] = TokensJoin{};  // for a CTA that gives up
+        if (!a.uncut) a.joins[blockIdx.x] = TokensJoin{};  // for a CTA that gives up
         for (int i = 0; i < Shape::kRing; ++i) {
             mbar_init(smem_u32(&sh.full[i]), K::kFillWarps);
             mbar_init(smem_u32(&sh.empty[i]), 1);

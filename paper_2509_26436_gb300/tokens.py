@@ -200,7 +200,7 @@ def qk_norm_rope_backward(dyq, dyk, q, k, wq, wk, positions=None, freqs=None, ep
     if wq is not None or wk is not None:
         if workspace is None:
             size = P.lib.quartz_qk_norm_rope_workspace_size(D)
-            workspace = P._empty(size, P.torch.uint8, q.device, stream)
+            workspace = P._empty((size,), P.torch.uint8, q.device, stream)
         else:
             if workspace.get_device() != device or not workspace.is_contiguous():
                 raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
@@ -295,7 +295,7 @@ def attention_paged_tokens(q, cache: P.PagedCache, block_table, seq_lens, starts
         raise ValueError("the result is float16, bfloat16 or float32")
     if workspace is None:
         size = cache._tokens_workspace_size(T, B, Hq, max_len, max_new)
-        workspace = P._empty(size, P.torch.uint8, cache.device, stream)
+        workspace = cache._no_workspace if size <= P._NO_WORKSPACE else P._empty((size,), P.torch.uint8, cache.device, stream)
     else:
         if workspace.get_device() != device or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous CUDA tensor on the current device")
