@@ -85,29 +85,34 @@ def rope_axes(x, positions, freqs, pair_axis, interleaved: bool = False, scale: 
     return out
 
 
-def _norm_side(name, x, w, T, D, dtype, w_dtype, device):
-    """(strides of x, address of w) after the checks of one side."""
-    st = P._rows(name, x, 3, dtype, device)
-    if x.shape[0] != T or x.shape[2] != D:
-        raise ValueError("q and k must have the same tokens and dim")
-    if w is None:
-        return st, None
-    at = P._vector("w" + name, w, w_dtype, device)
-    if w.shape[0] != D:
-        raise ValueError(f"w{name} must have one entry per element of a head")
-    return st, at
-
-
 def _norm_types(q, wq, wk):
+    """(type of q and k, of the weights, and both as the ABI's)."""
     dtype = q.dtype
-    kind = P._KIND.get(dtype)
+    w_dtype = wq.dtype if wq is not None else wk.dtype if wk is not None else dtype
+    kind, w_kind = P._KIND.get(dtype), P._KIND.get(w_dtype)
     if kind is None or not q.is_cuda or q.dim() != 3:
         raise ValueError("q must be a 3-D float16, bfloat16 or float32 CUDA tensor")
-    w_dtype = wq.dtype if wq is not None else wk.dtype if wk is not None else dtype
-    w_kind = P._KIND.get(w_dtype)
     if w_kind is None or (wk is not None and wk.dtype is not w_dtype):
         raise ValueError("wq and wk must be float16, bfloat16 or float32, of one type")
-    return dtype, kind, w_dtype, w_kind
+    return dtype, w_dtype, kind, w_kind
+
+
+def _norm_side(name, x, w, T, D, dtype, w_dtype, device):
+    """(strides, heads and address of x, address of w) after the checks of one
+    side.  (P._rows and P._vector in line: a call's host time is mostly these.)"""
+    st = x.stride()
+    if x.dtype is not dtype or len(st) != 3 or x.get_device() != device or (st[2] != 1 and x.shape[-1] > 1):
+        P._refuse(name, x, 3, dtype)
+    tokens, heads, dim = x.shape
+    if tokens != T or dim != D:
+        raise ValueError("q and k must have the same tokens and dim")
+    if w is None:
+        return st[0], st[1], heads, x.data_ptr(), None
+    if w.dtype is not w_dtype or w.dim() != 1 or w.get_device() != device or not w.is_contiguous():
+        P._refuse("w" + name, w, 1, w_dtype)
+    if w.shape[0] != D:
+        raise ValueError(f"w{name} must have one entry per element of a head")
+    return st[0], st[1], heads, x.data_ptr(), w.data_ptr()
 
 
 def _rope_of(positions, freqs, pair_axis, T, scale, interleaved, device):
@@ -116,6 +121,16 @@ def _rope_of(positions, freqs, pair_axis, T, scale, interleaved, device):
     if positions is None or freqs is None:
         raise ValueError("positions and freqs go together")
     return _byref(_axes_struct(positions, freqs, pair_axis, T, scale, interleaved, False, device))
+
+
+def _norm_out(x, y, T, H, D, dtype, device, stream):
+    """The result (given, or new) with its strides."""
+    if y is None:
+        return P._empty((T, H, D), dtype, x.device, stream), H * D, D
+    y0, y1, _ = P._rows("out", y, 3, dtype, device)
+    if y.shape != x.shape:
+        raise ValueError("out must have the shapes of q and k")
+    return y, y0, y1
 
 
 def qk_norm_rope(q, k, wq, wk, positions=None, freqs=None, eps: float = 1e-6, pair_axis=None, interleaved: bool = False,
@@ -130,33 +145,21 @@ def qk_norm_rope(q, k, wq, wk, positions=None, freqs=None, eps: float = 1e-6, pa
     yk) may be (q, k).  Nothing is recorded for autograd (rope())."""
     if P.torch is None:
         P._bind()
-    _no_gradient("qk_norm_rope", _FUNCTION + "qk_norm_rope_backward", q, k, wq, wk, *(out or ()))
-    dtype, kind, w_dtype, w_kind = _norm_types(q, wq, wk)
+    if P.torch.is_grad_enabled():
+        _no_gradient("qk_norm_rope", _FUNCTION + "qk_norm_rope_backward", q, k, wq, wk, *(out or ()))
+    dtype, w_dtype, kind, w_kind = _norm_types(q, wq, wk)
     device = P._device()
     T, Hq, D = q.shape
-    qs, wq_ptr = _norm_side("q", q, wq, T, D, dtype, w_dtype, device)
+    x0, x1, _, x_ptr, w_ptr = _norm_side("q", q, wq, T, D, dtype, w_dtype, device)
     yq, yk = (None, None) if out is None else out
-    if yq is None:
-        yq = P._empty((T, Hq, D), dtype, q.device, stream)
-        y0, y1 = Hq * D, D
-    else:
-        y0, y1, _ = P._rows("out", yq, 3, dtype, device)
-        if yq.shape != q.shape:
-            raise ValueError("out must have the shapes of q and k")
-    side_q = N.QuartzNormSide(q.data_ptr(), qs[0], qs[1], None, 0, 0, yq.data_ptr(), y0, y1, wq_ptr, None, Hq)
+    yq, y0, y1 = _norm_out(q, yq, T, Hq, D, dtype, device, stream)
+    side_q = N.QuartzNormSide(x_ptr, x0, x1, None, 0, 0, yq.data_ptr(), y0, y1, w_ptr, None, Hq)
     if k is None:
         side_k, yk = N.QuartzNormSide(), None
     else:
-        ks, wk_ptr = _norm_side("k", k, wk, T, D, dtype, w_dtype, device)
-        Hk = k.shape[1]
-        if yk is None:
-            yk = P._empty((T, Hk, D), dtype, q.device, stream)
-            y0, y1 = Hk * D, D
-        else:
-            y0, y1, _ = P._rows("out", yk, 3, dtype, device)
-            if yk.shape != k.shape:
-                raise ValueError("out must have the shapes of q and k")
-        side_k = N.QuartzNormSide(k.data_ptr(), ks[0], ks[1], None, 0, 0, yk.data_ptr(), y0, y1, wk_ptr, None, Hk)
+        x0, x1, Hk, x_ptr, w_ptr = _norm_side("k", k, wk, T, D, dtype, w_dtype, device)
+        yk, y0, y1 = _norm_out(k, yk, T, Hk, D, dtype, device, stream)
+        side_k = N.QuartzNormSide(x_ptr, x0, x1, None, 0, 0, yk.data_ptr(), y0, y1, w_ptr, None, Hk)
     r = _rope_of(positions, freqs, pair_axis, T, scale, interleaved, device)
     rc = P.lib.quartz_qk_norm_rope(_byref(side_q), _byref(side_k), kind, w_kind, T, D, eps, r, _Q._stream(stream))
     if rc:
@@ -174,8 +177,9 @@ def qk_norm_rope_backward(dyq, dyk, q, k, wq, wk, positions=None, freqs=None, ep
     for one captured graph."""
     if P.torch is None:
         P._bind()
-    _no_gradient("qk_norm_rope_backward", "detach what it gets", dyq, dyk)
-    dtype, kind, w_dtype, w_kind = _norm_types(q, wq, wk)
+    if P.torch.is_grad_enabled():
+        _no_gradient("qk_norm_rope_backward", "detach what it gets", dyq, dyk)
+    dtype, w_dtype, kind, w_kind = _norm_types(q, wq, wk)
     device = P._device()
     T, _, D = q.shape
     sides, grads = [], []
@@ -184,18 +188,17 @@ def qk_norm_rope_backward(dyq, dyk, q, k, wq, wk, positions=None, freqs=None, ep
             if dy is not None or w is not None:
                 raise ValueError(f"{name} is None, and has neither a gradient nor weights")
             sides.append(N.QuartzNormSide())
-            grads += [None, None]
+            grads += (None, None)
             continue
-        st, w_ptr = _norm_side(name, x, w, T, D, dtype, w_dtype, device)
+        x0, x1, H, x_ptr, w_ptr = _norm_side(name, x, w, T, D, dtype, w_dtype, device)
         if dy is None or dy.shape != x.shape:
             raise ValueError(f"dy{name} must have the shape of {name}")
         ds = P._rows("dy" + name, dy, 3, dtype, device)
-        H = x.shape[1]
-        dx = P._empty((T, H, D), dtype, x.device, stream)
+        dx, y0, y1 = _norm_out(x, None, T, H, D, dtype, device, stream)
         dw = None if w is None else P._empty((D,), w_dtype, x.device, stream)
-        sides.append(N.QuartzNormSide(x.data_ptr(), st[0], st[1], dy.data_ptr(), ds[0], ds[1], dx.data_ptr(), H * D, D,
-                                      w_ptr, None if w is None else dw.data_ptr(), H))
-        grads += [dx, dw]
+        sides.append(N.QuartzNormSide(x_ptr, x0, x1, dy.data_ptr(), ds[0], ds[1], dx.data_ptr(), y0, y1, w_ptr,
+                                      None if w is None else dw.data_ptr(), H))
+        grads += (dx, dw)
     ptr, size = None, 0
     if wq is not None or wk is not None:
         if workspace is None:
