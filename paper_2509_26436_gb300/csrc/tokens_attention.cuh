@@ -605,6 +605,10 @@ struct TokensKernel {
     // 16-bit pages.  Tiles that are seen whole come by TMA, a box per page and 64
     // dimensions, dealt to the warps; the others (a sequence's end, a window's
     // begin; pages that are no boxes) by 16-byte copies with zeros in the rest.
+    // Units in the order of the products: keys, values, keys, .. with two tiles; with
+    // one the next keys before these values.
+    static constexpr int kSkew = TILES == 1;
+
     __device__ __forceinline__ void fill_16bit(int warp)
     {
         constexpr int kLag = Shape::kRing / 2, kLanes = Shape::kUnitDims / 8, kRowsEach = 32 / kLanes;
@@ -632,17 +636,20 @@ struct TokensKernel {
                 there = boxed ? box < boxes : l.has(t);
                 return page_entry(w, t, there);
             };
-            bool there_next;
-            uint32_t page_next = lookup(0, there_next);
-            for (int i = 0; ok && i < w.count; ++i) {
-                const int t0 = w.tile(i) * kTokKeys, here = checked(page_next, bad);
-                const unsigned there = __ballot_sync(0xffffffffu, there_next);
-                if (i + 1 < w.count) page_next = lookup(i + 1, there_next);
-                if (boxes && l.all(t0)) {
-                    if (arrived < u) flush();
-                    const int slot = static_cast<int>(static_cast<uint32_t>(t0 + box_row) & mask);
-#pragma unroll
-                    for (int side = 0; side < 2; ++side) {
+            bool there_k, there_v = false, there_next = false;
+            uint32_t page_k = lookup(0, there_k), page_v = 0, page_next = 0;
+            for (int i = -kSkew; ok && i < w.count; ++i) {
+                if (i + kSkew + 1 < w.count) page_next = lookup(i + kSkew + 1, there_next);
+                if (kSkew == 0) page_v = page_k, there_v = there_k;
+#pragma unroll 1
+                for (int side = 0; ok && side < 2; ++side) {
+                    const int tile = side ? i : i + kSkew;
+                    if (tile < 0 || tile >= w.count) continue;
+                    const int t0 = w.tile(tile) * kTokKeys, here = checked(side ? page_v : page_k, bad);
+                    const PagedSide &p = side ? a.v : a.k;
+                    if (boxes && l.all(t0)) {
+                        if (arrived < u) flush();
+                        const int slot = static_cast<int>(static_cast<uint32_t>(t0 + box_row) & mask);
                         const int order = side ? a.v_order : a.k_order;  // 2 bits each: head, slot, page
                         const int c1 = (order & 3) == 1 ? w.p.head : (order >> 2 & 3) == 1 ? slot : here;
                         const int c2 = (order & 3) == 2 ? w.p.head : (order >> 2 & 3) == 2 ? slot : here;
@@ -656,18 +663,13 @@ struct TokensKernel {
                             if (box < boxes)
                                 tma_load_4d(unit_at(u) + box_to, side ? v_map : k_map, k * Shape::kUnitDims + panel * 64, c1, c2, c3, bar);
                         }
-                        if (!ok) break;
+                        arrived = u;
+                        continue;
                     }
-                    arrived = u;
-                    continue;
-                }
-                const int64_t slot = static_cast<uint32_t>(t0 + warp * 32 + lane) & mask;
-                // element offsets of this lane's token
-                const int64_t off[2] = {static_cast<int64_t>(here) * a.k.stride_page + slot * a.k.stride_slot,
-                                        static_cast<int64_t>(here) * a.v.stride_page + slot * a.v.stride_slot};
-#pragma unroll
-                for (int side = 0; side < 2; ++side) {
-                    const PagedSide &p = side ? a.v : a.k;
+                    const unsigned there = __ballot_sync(0xffffffffu, side ? there_v : there_k);
+                    const int64_t slot = static_cast<uint32_t>(t0 + warp * 32 + lane) & mask;
+                    // element offset of this lane's token
+                    const int64_t off = static_cast<int64_t>(here) * p.stride_page + slot * p.stride_slot;
                     const uint16_t *base = reinterpret_cast<const uint16_t *>(p.data) + w.p.head * p.stride_head + c * 8;
 #pragma unroll 1
                     for (int k = 0; k < Shape::kUnits; ++k) {
@@ -681,7 +683,7 @@ struct TokensKernel {
 #pragma unroll 4
                         for (int j = 0; j < 32 / kRowsEach; ++j) {
                             const int src = j * kRowsEach + r_lane, r = warp * 32 + src;
-                            const int64_t o = __shfl_sync(0xffffffffu, off[side], src);
+                            const int64_t o = __shfl_sync(0xffffffffu, off, src);
                             const bool is = there >> src & 1;
                             cp_async16_or_zero(to + r * 128 + (((c ^ r) & 7) << 4), is ? from + o : from, is ? 16 : 0);
                         }
@@ -692,8 +694,9 @@ struct TokensKernel {
                             arrive_full(arrived++);
                         }
                     }
-                    if (!ok) break;
                 }
+                page_v = page_k, there_v = there_k;
+                page_k = page_next, there_k = there_next;
             }
         }
         flush();
@@ -795,48 +798,49 @@ struct TokensKernel {
     {
         const int lane = threadIdx.x & 31;
         const int mask = (1 << a.page_shift) - 1;
-        Walk w(a, at, run);
-        Loaded l = loaded(w);
-        bool bad = false;
-        int i = 0, u = 0;
-        bool there_next;
-        auto lookup = [&](int i) {
-            const int t = w.tile(i) * kTokKeys + warp * kWarpRows + lane % kWarpRows;
-            there_next = l.has(t);
-            return page_entry(w, t, there_next);
+        Piece now, next;  // the next unit's is on its way while one is decoded
+        bool held = false, ok = true, bad = false;
+        int u = 0;
+        auto decode = [&] {
+            if (!held) return true;
+            if (!wait_empty(u)) return false;
+            store_piece(now, unit_at(u), warp);
+            arrive_full(u++);
+            return true;
         };
-        uint32_t page_next = lookup(0);
-        Piece now, next;
-        bool held = false, ok = true;
-        while (ok) {
-            const bool more = w.more();
-            int row = -1;
-            if (more) {
-                const int t = w.tile(i) * kTokKeys + warp * kWarpRows + lane % kWarpRows, page = checked(page_next, bad);
-                if (there_next) row = ((page * a.kv_heads + w.p.head) << a.page_shift) + (t & mask);
-                if (i + 1 < w.count) {
-                    page_next = lookup(++i);
-                } else {
-                    w.next(), i = 0;
-                    if (w.more()) {
-                        l = loaded(w);
-                        page_next = lookup(0);
-                    }
+        for (Walk w(a, at, run); ok && w.more(); w.next()) {
+            const Loaded l = loaded(w);
+            auto lookup = [&](int i, bool &there) {
+                const int t = w.tile(i) * kTokKeys + warp * kWarpRows + lane % kWarpRows;
+                there = l.has(t);
+                return page_entry(w, t, there);
+            };
+            bool there_k, there_next = false;
+            uint32_t page_k = lookup(0, there_k), page_next = 0;
+            int row_v = -1;
+            for (int i = -kSkew; ok && i < w.count; ++i) {
+                int row_k = -1;
+                if (i + kSkew < w.count) {
+                    const int t = w.tile(i + kSkew) * kTokKeys + warp * kWarpRows + lane % kWarpRows, page = checked(page_k, bad);
+                    if (there_k) row_k = ((page * a.kv_heads + w.p.head) << a.page_shift) + (t & mask);
                 }
-            }
+                if (i + kSkew + 1 < w.count) page_next = lookup(i + kSkew + 1, there_next);
+                if (kSkew == 0) row_v = row_k;
 #pragma unroll 1
-            for (int k = 0; k < (more ? 2 * Shape::kUnits : 1); ++k) {
-                if (more) load_piece(k < Shape::kUnits ? a.k : a.v, row, k % Shape::kUnits * Shape::kUnitDims, next);
-                if (held) {
-                    if (!(ok = wait_empty(u))) break;
-                    store_piece(now, unit_at(u), warp);
-                    arrive_full(u++);
+                for (int k = 0; k < 2 * Shape::kUnits; ++k) {
+                    const bool side = k >= Shape::kUnits;
+                    const int tile = side ? i : i + kSkew;
+                    if (tile < 0 || tile >= w.count) continue;
+                    load_piece(side ? a.v : a.k, side ? row_v : row_k, k % Shape::kUnits * Shape::kUnitDims, next);
+                    if (!(ok = decode())) break;
+                    now = next;
+                    held = true;
                 }
-                now = next;
-                held = more;
+                row_v = row_k;
+                page_k = page_next, there_k = there_next;
             }
-            if (!more) break;
         }
+        if (ok) decode();
         if (bad) atomicOr(a.dev_err, QUARTZ_DEV_INDEX);
     }
 
@@ -888,37 +892,40 @@ struct TokensKernel {
     __device__ __forceinline__ void products()
     {
         const bool leader = elect_one();
-        int it = 0, seg = 0;  // tiles and blocks so far
+        int it = 0, seg = 0, u = 0;  // tiles, blocks and units so far
         bool ok = true;
         for (Walk w(a, at, run); ok && w.more(); w.next(), ++seg) {
             if (!(ok = wait(sh.q_full, seg))) break;
             tc_fence_after();
 #pragma unroll
-            for (int t = 0; ok && t < TILES; ++t) ok = issue_s(t, TILES == 2 ? t : it & 1, 2 * Shape::kUnits * it, leader, t + 1 == TILES);
+            for (int t = 0; ok && t < TILES; ++t) ok = issue_s(t, TILES == 2 ? t : it & 1, u, leader, t + 1 == TILES);
             if (!ok) break;
+            u += Shape::kUnits;
             if (leader && w.count == 1) mma_commit(smem_u32(&sh.q_free));
             for (int i = 0; i < w.count; ++i, ++it) {
-                const int uk = 2 * Shape::kUnits * (it + 1), uv = uk - Shape::kUnits;  // next keys, these values
                 const bool again = i + 1 < w.count, last = i + 2 == w.count;
                 if constexpr (TILES == 2) {
 #pragma unroll
                     for (int t = 0; t < 2; ++t) {
                         if (!(ok = wait(sh.p_ready[t], it))) break;
                         tc_fence_after();
-                        if (!(ok = issue_o(t, t, uv, i > 0, leader, t == 1))) break;
-                        if (again && !(ok = issue_s(t, t, uk, leader, t == 1))) break;
+                        if (!(ok = issue_o(t, t, u, i > 0, leader, t == 1))) break;
+                        if (again && !(ok = issue_s(t, t, u + Shape::kUnits, leader, t == 1))) break;
                     }
                     if (!ok) break;
+                    u += again ? 2 * Shape::kUnits : Shape::kUnits;
                     if (leader && last) mma_commit(smem_u32(&sh.q_free));
                 } else {
                     if (again) {
-                        if (!(ok = issue_s(0, (it + 1) & 1, uk, leader, true))) break;
+                        if (!(ok = issue_s(0, (it + 1) & 1, u, leader, true))) break;
+                        u += Shape::kUnits;
                         if (leader && last) mma_commit(smem_u32(&sh.q_free));
                     }
                     if (!(ok = wait(sh.p_ready[it & 1], it >> 1))) break;
                     if (i == 0 && seg > 0 && !(ok = wait(sh.o_free, seg - 1))) break;
                     tc_fence_after();
-                    if (!(ok = issue_o(0, it & 1, uv, i > 0, leader, true))) break;
+                    if (!(ok = issue_o(0, it & 1, u, i > 0, leader, true))) break;
+                    u += Shape::kUnits;
                     if (leader && !again) mma_commit(smem_u32(&sh.o_done));
                 }
             }
