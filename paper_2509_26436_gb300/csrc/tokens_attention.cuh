@@ -300,12 +300,13 @@ struct TokensWalk {
     }
 };
 
-template <int D, int TILES>
+// LZS: encoded pages, whose decoding pays for every unit, not for its size alone.
+template <int D, int TILES, bool LZS>
 struct TokensShape {
     static constexpr int kRows = 128 * TILES;
-    static constexpr int kUnitDims = D == 128 ? 128 : 64, kUnits = D / kUnitDims;  // units of a tile's side
+    static constexpr int kUnitDims = D == 128 || (LZS && D == 256) ? 128 : 64, kUnits = D / kUnitDims;  // units of a tile's side
     // Units that one product of the weights takes: next to each other in the ring
-    static constexpr int kTogether = D == 256 ? 2 : kUnits;
+    static constexpr int kTogether = kUnitDims == 128 ? 1 : D == 256 ? 2 : kUnits;
     static constexpr int kPanel = kTokKeys * 128;  // 64 dimensions, 128 bytes a row
     static constexpr int kUnitBytes = kTokKeys * kUnitDims * 2, kQTile = 128 * D * 2, kQBytes = TILES * kQTile;
     static constexpr int kMisc = 3072;  // static shared memory, with its padding
@@ -447,7 +448,7 @@ __device__ __forceinline__ void tokens_shape(const TokensArgs &a, const TokensRo
 // code for it in the others' loop cost them 14%, waiting for instructions.)
 template <int D, int KIND, int TILES, bool SHAPED>
 struct TokensKernel {
-    using Shape = TokensShape<D, TILES>;
+    using Shape = TokensShape<D, TILES, KIND == QUARTZ_PAGES_ENCODED>;
     static constexpr int R = Shape::kRows;
     static constexpr bool kBf = KIND == QUARTZ_PAGES_BF16, kLzs = KIND == QUARTZ_PAGES_ENCODED;
     // Weights are 2^(score - m + up) up to 2^(up + slack): fp16 keeps those down
@@ -1253,7 +1254,7 @@ __global__ void __launch_bounds__(TokensKernel<D, KIND, TILES, SHAPED>::kThreads
 {
     griddep_wait();
     using K = TokensKernel<D, KIND, TILES, SHAPED>;
-    using Shape = TokensShape<D, TILES>;
+    using Shape = typename K::Shape;
     extern __shared__ __align__(1024) uint8_t s_tokens[];
     __shared__ TokensShared sh;
     const int warp = threadIdx.x >> 5;
@@ -1327,7 +1328,7 @@ cudaError_t launch_tokens_attn_256_shaped(const TokensArgs &a, const TokensMaps 
 template <int D, int KIND, int TILES, bool SHAPED>
 cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int ctas, cudaStream_t s)
 {
-    constexpr int kSmem = TokensShape<D, TILES>::kSmem;
+    constexpr int kSmem = TokensKernel<D, KIND, TILES, SHAPED>::Shape::kSmem;
     const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES, SHAPED>>(kSmem);
     if (e != cudaSuccess) return e;
     return launch_pdl(tokens_attn_kernel<D, KIND, TILES, SHAPED>, dim3(static_cast<unsigned>(ctas)), dim3(TokensKernel<D, KIND, TILES, SHAPED>::kThreads), kSmem, s,
