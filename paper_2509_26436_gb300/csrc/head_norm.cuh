@@ -232,7 +232,7 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
             } else if (in) {
                 vectors(t, h, [&](int k, const T *from) { raw[k] = *reinterpret_cast<const Vec<T, V> *>(from); });
             }
-            float x1[NP][V], x2[NP][V], g1[ND][VD], g2[ND][VD];
+            float x1[NP][V], x2[NP][V], g1[ND][VD], g2[ND][VD], gx1[ND][VD], gx2[ND][VD];
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 pairs_of(raw[2 * i], raw[2 * i + 1], pc[i].in, pc[i].turn, x1[i], x2[i]);
@@ -255,8 +255,9 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
                         ss += x1[i][j] * x1[i][j];
                         ss += x2[i][j] * x2[i][j];
                         if constexpr (kBack) {
-                            dot += g1[i][j] * w1[i][j] * x1[i][j];
-                            dot += g2[i][j] * w2[i][j] * x2[i][j];
+                            gx1[i][j] = g1[i][j] * x1[i][j], gx2[i][j] = g2[i][j] * x2[i][j];
+                            dot += gx1[i][j] * w1[i][j];
+                            dot += gx2[i][j] * w2[i][j];
                         }
                     }
                 for (int d = 1; d < L; d *= 2) {
@@ -276,10 +277,10 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
                 for (int j = 0; j < V; ++j) {
                     float2 z;
                     if constexpr (kBack) {
-                        z.x = r * g1[i][j] * w1[i][j] - x1[i][j] * ra;
-                        z.y = r * g2[i][j] * w2[i][j] - x2[i][j] * ra;
-                        dw1[i][j] += g1[i][j] * (x1[i][j] * r);
-                        dw2[i][j] += g2[i][j] * (x2[i][j] * r);
+                        z.x = g1[i][j] * (r * w1[i][j]) - x1[i][j] * ra;
+                        z.y = g2[i][j] * (r * w2[i][j]) - x2[i][j] * ra;
+                        dw1[i][j] += gx1[i][j] * r;
+                        dw2[i][j] += gx2[i][j] * r;
                     } else if constexpr (MODE == kForward) {
                         z = rope_turn(x1[i][j] * (r * w1[i][j]), x2[i][j] * (r * w2[i][j]), cs[i][j]);
                     } else {
