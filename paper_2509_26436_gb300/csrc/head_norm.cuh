@@ -8,11 +8,16 @@
 // HBM-bound: x (and dy) read and y (dx) written once, some 5 to 15 operations per
 // element.  A row (a head of a token) belongs to a group of 4 to 32 lanes, each
 // with V pairs (two vectors) or V elements that are not turned; the sums over the
-// head, in binary32, go across the lanes, and the next row's loads are under way
-// meanwhile.  A CTA takes blocks of tokens of one side (queries or keys), whose
-// angles it computes once for all their heads: an angle costs about as much as
-// six heads' pairs.  dw: each lane sums its elements over its rows, a CTA joins
-// its groups, a second kernel the CTAs; all in a fixed order.
+// head, in binary32, go across the lanes, and the next rows are on their way into
+// shared memory meanwhile.  A CTA takes blocks of tokens of one side (queries or
+// keys), whose angles it computes once for all their heads: an angle costs about as
+// much as three heads' pairs.  dw: each lane sums its elements over its rows, a CTA
+// joins its groups, a second kernel the CTAs; all in a fixed order.
+// Measured (bf16; us, of the copy rate): gradient of 8192 x 40 heads of 128 73, 50%
+// (230 with angles and weights from shared memory for each row, 170 in registers,
+// 93 with rows on their way, 73 with instances for lanes full of pairs; then issue
+// slots are 64% busy, the rest waits for chains at 4 warps a scheduler); rotation of
+// 17550 x 16 heads by three axes 24.1, 88%; fp16, 4608 x 48 heads, forward 30.5, 55%.
 #pragma once
 
 #include "ptx.cuh"
