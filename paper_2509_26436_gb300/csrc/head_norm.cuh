@@ -17,7 +17,8 @@
 // (230 with angles and weights from shared memory for each row, 170 in registers,
 // 93 with rows on their way, 73 with instances for lanes full of pairs; then issue
 // slots are 64% busy, the rest waits for chains at 4 warps a scheduler); rotation of
-// 17550 x 16 heads by three axes 24.1, 88%; fp16, 4608 x 48 heads, forward 30.5, 55%.
+// 17550 x 16 heads by three axes 24.1, 88%; fp16, 4608 x 48 heads, forward 28.5, 59%
+// (30.5 with three CTAs per SM and rows six ahead).
 #pragma once
 
 #include "ptx.cuh"
@@ -33,13 +34,13 @@ enum NormMode { kRotate, kForward, kBackward };
 // CTAs per SM: as many as the registers of a lane's vectors, angles, weights and
 // sums allow.
 template <typename T, int MODE, int E>  // E: pairs a lane
-constexpr int kPerSm = MODE == kRotate ? 4 : MODE == kForward ? (sizeof(T) == 4 ? 2 : 3) : (sizeof(T) * E <= 16 ? 2 : 1);
+constexpr int kPerSm = MODE == kRotate ? 4 : MODE == kForward ? (sizeof(T) == 4 ? 2 : 4) : (sizeof(T) * E <= 16 ? 2 : 1);
 constexpr int kMostBackward = 2;
 
 // Rows that a lane's copies are ahead, each in memory of its own, so that some
 // 128 KB per SM are on their way; elements one at a time are loaded as needed.
 template <typename T, int MODE, int V>
-constexpr int kAhead = sizeof(T) * V < 8 ? 0 : MODE == kBackward ? 4 : MODE == kForward ? 6 : 5;
+constexpr int kAhead = sizeof(T) * V < 8 ? 0 : MODE == kBackward ? 4 : MODE == kForward ? (sizeof(T) == 4 ? 6 : 4) : 5;
 
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Vec {

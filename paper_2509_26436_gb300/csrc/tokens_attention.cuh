@@ -324,7 +324,7 @@ struct TokensShape {
     static constexpr int kTogether = kUnitDims == 128 ? 1 : D == 256 ? 2 : kUnits;
     static constexpr int kPanel = kTokKeys * 128;  // 64 dimensions, 128 bytes a row
     static constexpr int kUnitBytes = kTokKeys * kUnitDims * 2, kQTile = 128 * D * 2, kQBytes = TILES * kQTile;
-    static constexpr int kMisc = 3072;  // static shared memory, with its padding
+    static constexpr int kMisc = 3 * 1024;  // static shared memory, with its padding
     // Results on their way out, 32 rows x 64 bytes a warp.  Heads of 256 have none: the
     // ring holds two units more than a tile's keys and values instead, which are under
     // way while those are used.
@@ -344,7 +344,7 @@ struct TokensShared {
     TokensFind find;
     float m[2][128], l[2][128];  // one tile: a row's maximum and sum, by warpgroup
 };
-static_assert(sizeof(TokensShared) <= 3072, "");
+static_assert(sizeof(TokensShared) <= 3 * 1024, "");
 
 // tanh of u, |u| <= 1, good to 3 half steps of binary32: an odd polynomial fitted
 // to the least largest relative error (5e-8); above, 1 - 2 / (1 + e^2|u|).
