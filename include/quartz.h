@@ -542,9 +542,11 @@ int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_st
  * A token that sees nothing gives zeros.  Query head h reads key / value head
  * h / (q_heads / heads).  Encoded keys and values count as what
  * quartz_dequantize gives (fp16).  Products, softmax and sums in binary32; the
- * softmax weights, relative to the largest so far, enter the value product
- * rounded to the pages' type.  q . k_t, s_t log2 e and the sums have to be
- * finite in binary32; a query with others makes its own row of o NaN.  Tokens
+ * softmax weights, relative to the largest so far, enter the value product as
+ * two numbers of the pages' type (the rounded weight, and what that left,
+ * rounded) with max_new q_heads / heads <= 128 or an o of fp32; else rounded to
+ * the pages' type.  q . k_t, s_t log2 e and the sums have to be finite in
+ * binary32; a query with others makes its own row of o NaN.  Tokens
  * that none of a sequence's new tokens sees are not looked at, infinite and NaN
  * ones either; an infinite or NaN element of a value that one of them sees may
  * make that element of o NaN for the others too, whatever they see.

@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kJoinThreads) tokens_join_kernel(TokensArgs a,
 }
 
 struct TokensPlan {
-    int tiles, ctas;
+    int tiles, ctas, parts;
     bool uncut;
 };
 
@@ -57,11 +57,21 @@ struct TokensPlan {
 // keys.  Blocks that all have an SM, of 8 tiles of keys at most, stay whole: the
 // join, and its workspace, cost more than they take from a CTA (8 drafted tokens,
 // 40 heads, 777 cached: 11.2 us a call, cut 17.8).
-TokensPlan tokens_plan(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len, int64_t max_new)
+//
+// Weights enter the value product in two parts, so that only the result's rounding
+// is left of the error (relative to 64 bits, bf16 pages and results: 0.0016; in one
+// part 0.0021).  Few rows are bound by the pages, not by products (16 trees of 16
+// over up to 8192: 65.4 us, in one part 63.1).  Sequences with more rows than a tile
+// are bound by products and the softmax (8192 causal tokens: 513 us, in one part
+// 400; trees of 61 over up to 65536 encoded tokens 280, 211; heads of 256 in a
+// window 164, 144): one part, unless the result is binary32.
+TokensPlan tokens_plan(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len, int64_t max_new,
+                       int o_type)
 {
     const int64_t group = q_heads / c->heads;
     TokensPlan p;
     p.tiles = c->dim <= 128 && max_new * group > 128 ? 2 : 1;
+    p.parts = max_new * group <= 128 || o_type == QUARTZ_OUT_F32 ? 2 : 1;
     const int64_t most = (tokens * group / (128 * p.tiles) + seqs) * c->heads * (max_len / kTokKeys + 2);
     const int64_t blocks = (tokens * group / (128 * p.tiles) + seqs) * c->heads;
     p.uncut = blocks <= device_sms() && max_len <= 8 * kTokKeys;
@@ -108,7 +118,7 @@ size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 size_t paged_tokens_workspace_bytes(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len,
                                     int64_t max_new)
 {
-    const TokensPlan p = tokens_plan(c, tokens, seqs, q_heads, max_len, max_new);
+    const TokensPlan p = tokens_plan(c, tokens, seqs, q_heads, max_len, max_new, QUARTZ_OUT_F16);  // the same for every result
     if (p.uncut) return 256;  // nothing is written to it
     const size_t rows = static_cast<size_t>(p.ctas) * 2 * 128 * p.tiles;
     return up256(rows * c->dim * 4) + up256(rows * 8) + up256(p.ctas * sizeof(TokensJoin));
@@ -116,7 +126,7 @@ size_t paged_tokens_workspace_bytes(const quartz_paged_cache_t *c, int64_t token
 
 cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokensCall &call, cudaStream_t s)
 {
-    const TokensPlan p = tokens_plan(c, call.tokens, call.seqs, call.q_heads, call.max_len, call.max_new);
+    const TokensPlan p = tokens_plan(c, call.tokens, call.seqs, call.q_heads, call.max_len, call.max_new, call.o_type);
     TokensArgs a{};
     a.q = static_cast<const uint16_t *>(call.q);
     a.q_st = call.q_st, a.q_sh = call.q_sh;
@@ -174,16 +184,16 @@ cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokens
     cudaError_t e;
     switch (c->dim) {
         case 64:
-            e = (shaped ? launch_tokens_attn_64_shaped : launch_tokens_attn_64)(a, m, c->type, p.tiles, p.ctas, s);
+            e = (shaped ? launch_tokens_attn_64_shaped : launch_tokens_attn_64)(a, m, c->type, p.tiles, p.parts, p.ctas, s);
             return e != cudaSuccess || p.uncut ? e : launch_pdl(tokens_join_kernel<64>, grid, block, 0, s, a, R);
         case 128:
-            e = (shaped ? launch_tokens_attn_128_shaped : launch_tokens_attn_128)(a, m, c->type, p.tiles, p.ctas, s);
+            e = (shaped ? launch_tokens_attn_128_shaped : launch_tokens_attn_128)(a, m, c->type, p.tiles, p.parts, p.ctas, s);
             return e != cudaSuccess || p.uncut ? e : launch_pdl(tokens_join_kernel<128>, grid, block, 0, s, a, R);
         case 192:
-            e = (shaped ? launch_tokens_attn_192_shaped : launch_tokens_attn_192)(a, m, c->type, p.tiles, p.ctas, s);
+            e = (shaped ? launch_tokens_attn_192_shaped : launch_tokens_attn_192)(a, m, c->type, p.tiles, p.parts, p.ctas, s);
             return e != cudaSuccess || p.uncut ? e : launch_pdl(tokens_join_kernel<192>, grid, block, 0, s, a, R);
         default:
-            e = (shaped ? launch_tokens_attn_256_shaped : launch_tokens_attn_256)(a, m, c->type, p.tiles, p.ctas, s);
+            e = (shaped ? launch_tokens_attn_256_shaped : launch_tokens_attn_256)(a, m, c->type, p.tiles, p.parts, p.ctas, s);
             return e != cudaSuccess || p.uncut ? e : launch_pdl(tokens_join_kernel<256>, grid, block, 0, s, a, R);
     }
 }

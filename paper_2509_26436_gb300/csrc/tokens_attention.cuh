@@ -10,7 +10,7 @@
 // tokens are few.  A CTA takes one tile, or two side by side, and goes over the
 // sequence's keys 128 at a time:
 //   S = Q K'    tcgen05.mma from shared memory, 128 x 128 binary32 in TMEM
-//   P           by the softmax warps, 16 bits, over S in TMEM
+//   P           by the softmax warps, in one or two parts of 16 bits, over S in TMEM
 //   O += P V    tcgen05.mma, P from TMEM, V as it lies (MN-major)
 // While the softmax warps work on one S the tensor cores make the other.  There
 // are two softmax warpgroups, a thread per row: two tiles have one each; with one
@@ -459,9 +459,27 @@ __device__ __forceinline__ void tokens_shape(const TokensArgs &a, const TokensRo
     }
 }
 
+// Two values rounded to the pages' type, and what that left of them.
+template <bool BF>
+__device__ __forceinline__ uint32_t pair_of(float2 v)
+{
+    if (BF) return bf16_pair(v.x, v.y);
+    const __half2 h = __floats2half2_rn(v.x, v.y);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+template <bool BF>
+__device__ __forceinline__ float2 left_of(float2 v, uint32_t pair)
+{
+    const float2 f = BF ? make_float2(__uint_as_float(pair << 16), __uint_as_float(pair & 0xFFFF0000u))
+                        : __half22float2(*reinterpret_cast<const __half2 *>(&pair));
+    return make_float2(v.x - f.x, v.y - f.y);
+}
+
+// PARTS: of a weight, one (rounded to the pages' type), or two (that, and what it
+// left, rounded); tokens_plan chooses.
 // SHAPED: scores need more than a positive factor.  (An instance of its own: the
 // code for it in the others' loop cost them 14%, waiting for instructions.)
-template <int D, int KIND, int TILES, bool SHAPED>
+template <int D, int KIND, int TILES, bool SHAPED, int PARTS>
 struct TokensKernel {
     using Shape = TokensShape<D, TILES, KIND == QUARTZ_PAGES_ENCODED>;
     static constexpr int R = Shape::kRows;
@@ -886,6 +904,11 @@ struct TokensKernel {
         if (leader) mma_commit(smem_u32(&sh.s_full[buf]));
         return true;
     }
+    // Column of S that the weight of key t is written over (two weights to a column):
+    // one after the other; two parts: those of 64 keys, then the second parts of these,
+    // over the scores that both are from.
+    __device__ __forceinline__ static constexpr int weights_at(int t) { return PARTS == 1 ? t / 2 : t / 64 * 64 + t % 64 / 2; }
+
     // O[tile] (+)= P[buf] V, the values in units u ..
     __device__ __forceinline__ bool issue_o(int tile, int buf, int u, bool add, bool leader, bool last) const
     {
@@ -897,8 +920,10 @@ struct TokensKernel {
             const uint32_t v_low = sdesc_low(sdesc_mn_major_sw128(unit_at(u + k), Shape::kPanel));
 #pragma unroll
             for (int i = 0; i < kTokKeys / 16; ++i)
-                mma_f16_ts(tmem + 256 + tile * D + k * Shape::kUnitDims, tmem + buf * 128 + i * 8, sdesc_sw128_at(v_low, i * 2048),
-                           kIdescO, add || i > 0);
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part)
+                    mma_f16_ts(tmem + 256 + tile * D + k * Shape::kUnitDims, tmem + buf * 128 + weights_at(16 * i) + 32 * part,
+                               sdesc_sw128_at(v_low, i * 2048), kIdescO, add || i + part > 0);
             if (last)
                 for (int x = 0; x < Shape::kTogether; ++x) mma_commit(smem_u32(&sh.empty[(u + k + x) % Shape::kRing]));
         }
@@ -1113,20 +1138,17 @@ struct TokensKernel {
                         const auto of = exponent(c);
 #pragma unroll
                         for (int y = 0; y < 64; y += 32) {
-                            uint32_t p[16];
+                            uint32_t p[16], second[PARTS == 1 ? 1 : 16];
 #pragma unroll
                             for (int x = 0; x < 16; ++x) {
                                 float2 e = unpack2(of(pack2(__uint_as_float(s[y + 2 * x]), __uint_as_float(s[y + 2 * x + 1])), y + 2 * x));
                                 e.x = ex2(e.x), e.y = ex2(e.y);
                                 sum[x & 1] = add2(sum[x & 1], pack2(e.x, e.y));
-                                if (kBf) {
-                                    p[x] = bf16_pair(e.x, e.y);
-                                } else {
-                                    const __half2 h = __floats2half2_rn(e.x, e.y);
-                                    p[x] = *reinterpret_cast<const uint32_t *>(&h);
-                                }
+                                p[x] = pair_of<kBf>(e);
+                                if constexpr (PARTS == 2) second[x] = pair_of<kBf>(left_of<kBf>(e, p[x]));
                             }
-                            tmem_st_row(s_at + (c + y) / 2, p);
+                            tmem_st_row(s_at + weights_at(c + y), p);
+                            if constexpr (PARTS == 2) tmem_st_row(s_at + weights_at(c + y) + 32, second);
                         }
                     }
                 };
@@ -1263,13 +1285,13 @@ struct TokensKernel {
     }
 };
 
-template <int D, int KIND, int TILES, bool SHAPED>
-__global__ void __launch_bounds__(TokensKernel<D, KIND, TILES, SHAPED>::kThreads, 1)
+template <int D, int KIND, int TILES, bool SHAPED, int PARTS>
+__global__ void __launch_bounds__(TokensKernel<D, KIND, TILES, SHAPED, PARTS>::kThreads, 1)
     tokens_attn_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                        const __grid_constant__ CUtensorMap q_map, TokensArgs a)
 {
     griddep_wait();
-    using K = TokensKernel<D, KIND, TILES, SHAPED>;
+    using K = TokensKernel<D, KIND, TILES, SHAPED, PARTS>;
     using Shape = typename K::Shape;
     extern __shared__ __align__(1024) uint8_t s_tokens[];
     __shared__ TokensShared sh;
@@ -1332,31 +1354,31 @@ struct TokensMaps {
 };
 
 // `shaped`: scores need more than a positive factor.
-cudaError_t launch_tokens_attn_64(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_64_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_128(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_128_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_192(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_192_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_256(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
-cudaError_t launch_tokens_attn_256_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_64(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_64_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_128(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_128_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_192(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_192_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_256(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s);
+cudaError_t launch_tokens_attn_256_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s);
 
-template <int D, int KIND, int TILES, bool SHAPED>
+template <int D, int KIND, int TILES, bool SHAPED, int PARTS>
 cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int ctas, cudaStream_t s)
 {
-    constexpr int kSmem = TokensKernel<D, KIND, TILES, SHAPED>::Shape::kSmem;
-    const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES, SHAPED>>(kSmem);
+    constexpr int kSmem = TokensKernel<D, KIND, TILES, SHAPED, PARTS>::Shape::kSmem;
+    const cudaError_t e = allow_shared<tokens_attn_kernel<D, KIND, TILES, SHAPED, PARTS>>(kSmem);
     if (e != cudaSuccess) return e;
-    return launch_pdl(tokens_attn_kernel<D, KIND, TILES, SHAPED>, dim3(static_cast<unsigned>(ctas)), dim3(TokensKernel<D, KIND, TILES, SHAPED>::kThreads), kSmem, s,
+    return launch_pdl(tokens_attn_kernel<D, KIND, TILES, SHAPED, PARTS>, dim3(static_cast<unsigned>(ctas)), dim3(TokensKernel<D, KIND, TILES, SHAPED, PARTS>::kThreads), kSmem, s,
                       m.k, m.v, m.q, a);
 }
 
-template <int D, int TILES, bool SHAPED>
+template <int D, int TILES, bool SHAPED, int PARTS>
 cudaError_t launch_tokens_attn(const TokensArgs &a, const TokensMaps &m, int kind, int ctas, cudaStream_t s)
 {
-    if (kind == QUARTZ_PAGES_F16) return launch_tokens_attn<D, QUARTZ_PAGES_F16, TILES, SHAPED>(a, m, ctas, s);
-    if (kind == QUARTZ_PAGES_BF16) return launch_tokens_attn<D, QUARTZ_PAGES_BF16, TILES, SHAPED>(a, m, ctas, s);
-    return launch_tokens_attn<D, QUARTZ_PAGES_ENCODED, TILES, SHAPED>(a, m, ctas, s);
+    if (kind == QUARTZ_PAGES_F16) return launch_tokens_attn<D, QUARTZ_PAGES_F16, TILES, SHAPED, PARTS>(a, m, ctas, s);
+    if (kind == QUARTZ_PAGES_BF16) return launch_tokens_attn<D, QUARTZ_PAGES_BF16, TILES, SHAPED, PARTS>(a, m, ctas, s);
+    return launch_tokens_attn<D, QUARTZ_PAGES_ENCODED, TILES, SHAPED, PARTS>(a, m, ctas, s);
 }
 
 }  // namespace quartz

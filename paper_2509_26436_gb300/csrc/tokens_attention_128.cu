@@ -4,10 +4,10 @@
 
 namespace quartz {
 
-cudaError_t launch_tokens_attn_128(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int ctas, cudaStream_t s)
+cudaError_t launch_tokens_attn_128(const TokensArgs &a, const TokensMaps &m, int kind, int tiles, int parts, int ctas, cudaStream_t s)
 {
-    return tiles == 2 ? launch_tokens_attn<128, 2, false>(a, m, kind, ctas, s)
-                      : launch_tokens_attn<128, 1, false>(a, m, kind, ctas, s);
+    if (tiles == 1) return launch_tokens_attn<128, 1, false, 2>(a, m, kind, ctas, s);
+    return parts == 2 ? launch_tokens_attn<128, 2, false, 2>(a, m, kind, ctas, s) : launch_tokens_attn<128, 2, false, 1>(a, m, kind, ctas, s);
 }
 
 }  // namespace quartz

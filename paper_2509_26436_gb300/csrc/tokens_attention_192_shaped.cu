@@ -4,9 +4,9 @@
 
 namespace quartz {
 
-cudaError_t launch_tokens_attn_192_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int, int ctas, cudaStream_t s)
+cudaError_t launch_tokens_attn_192_shaped(const TokensArgs &a, const TokensMaps &m, int kind, int, int parts, int ctas, cudaStream_t s)
 {
-    return launch_tokens_attn<192, 1, true>(a, m, kind, ctas, s);
+    return parts == 2 ? launch_tokens_attn<192, 1, true, 2>(a, m, kind, ctas, s) : launch_tokens_attn<192, 1, true, 1>(a, m, kind, ctas, s);
 }
 
 }  // namespace quartz

@@ -247,9 +247,10 @@ def attention_paged_tokens(q, cache: P.PagedCache, block_table, seq_lens, starts
     max_len: at most this many cached tokens (default: what the table holds),
     max_new: at most this many new ones per sequence (default: all of q; 64 in
     a tree, which holds no more); known bounds plan better.  Softmax weights
-    are rounded to the cache's type before they multiply the values, whatever
-    out_dtype.  A workspace of the caller's is only good for one call at a time,
-    and for one captured graph."""
+    multiply the values as two parts of the cache's type where a key head has at
+    most 128 rows (max_new times its query heads) or the result is float32;
+    else rounded to that type.  A workspace of the caller's is only good for one
+    call at a time, and for one captured graph."""
     device = cache._check_device()
     qs = P._rows("q", q, 3, cache.dtype, device)
     ts = P._rows("block_table", block_table, 2, P.i32, device)
