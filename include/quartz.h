@@ -461,7 +461,7 @@ typedef struct {
  *   y = R (w x r),  r = (mean(x^2) + eps)^-1/2
  * with the mean over the head's dim elements and R the rotation of `rope`
  * (NULL: none; its `backward` is 0).  In binary32, rounded once; x^2 and its
- * sum have to be finite there.  `type` of x and y, `w_type` of the weights of
+ * sum have to be finite there, and with eps = 0 the mean 2^-126 or more.  `type` of x and y, `w_type` of the weights of
  * both sides (quartz_out_t).  y == x with equal strides works in place; other
  * overlaps are undefined, of the two sides' too.  dim 2 .. 256, eps >= 0,
  * tokens <= 2^30, heads <= 65535. */
@@ -470,8 +470,9 @@ int32_t quartz_qk_norm_rope(const quartz_norm_side_t *q, const quartz_norm_side_
 
 /* Its gradient: with g = R' dy (R' the transpose of R) and n = x r,
  *   dx = r (g w - n mean(g w n)),  dw = sum over tokens and heads of g n.
- * dw is summed in binary32 in an order that depends on sizes and the device
- * alone, and rounded once; without tokens it is 0.  y may be x or dy (the same
+ * g w x and its sum over the head have to be finite in binary32 as well, and
+ * what is below 2^-126 there is lost.  dw is summed in binary32 in an order that
+ * depends on sizes and the device alone, and rounded once; without tokens it is 0.  y may be x or dy (the same
  * strides).  workspace: quartz_qk_norm_rope_workspace_size bytes, 16-byte
  * aligned, scratch (needed where a dw is wanted). */
 size_t quartz_qk_norm_rope_workspace_size(int32_t dim);

@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
             } else if (in) {
                 vectors(t, h, [&](int k, const T *from) { raw[k] = *reinterpret_cast<const Vec<T, V> *>(from); });
             }
-            float x1[NP][V], x2[NP][V], g1[ND][VD], g2[ND][VD], gx1[ND][VD], gx2[ND][VD];
+            float x1[NP][V], x2[NP][V], g1[ND][VD], g2[ND][VD], gw1[ND][VD], gw2[ND][VD];
 #pragma unroll
             for (int i = 0; i < NP; ++i) {
                 pairs_of(raw[2 * i], raw[2 * i + 1], pc[i].in, pc[i].turn, x1[i], x2[i]);
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
                     }
                 }
             }
-            float r = 1.f, ra = 0.f;
+            float r = 1.f, along = 0.f;  // mean(g w n)
             if (MODE != kRotate) {
                 float ss = 0.f, dot = 0.f;
 #pragma unroll
@@ -261,9 +261,9 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
                         ss += x1[i][j] * x1[i][j];
                         ss += x2[i][j] * x2[i][j];
                         if constexpr (kBack) {
-                            gx1[i][j] = g1[i][j] * x1[i][j], gx2[i][j] = g2[i][j] * x2[i][j];
-                            dot += gx1[i][j] * w1[i][j];
-                            dot += gx2[i][j] * w2[i][j];
+                            gw1[i][j] = g1[i][j] * w1[i][j], gw2[i][j] = g2[i][j] * w2[i][j];
+                            dot += gw1[i][j] * x1[i][j];
+                            dot += gw2[i][j] * x2[i][j];
                         }
                     }
                 for (int d = 1; d < L; d *= 2) {
@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
                     if (kBack) dot += __shfl_xor_sync(0xffffffffu, dot, d);
                 }
                 r = rsqrtf(ss * a.inv_dim + a.eps);
-                ra = r * r * r * dot * a.inv_dim;
+                along = r * dot * a.inv_dim;
             }
             if (!in) continue;
             T *to = y + h * sd.y_sh;
@@ -283,10 +283,12 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
                 for (int j = 0; j < V; ++j) {
                     float2 z;
                     if constexpr (kBack) {
-                        z.x = g1[i][j] * (r * w1[i][j]) - x1[i][j] * ra;
-                        z.y = g2[i][j] * (r * w2[i][j]) - x2[i][j] * ra;
-                        dw1[i][j] += gx1[i][j] * r;
-                        dw2[i][j] += gx2[i][j] * r;
+                        // by n = x r, not by powers of r, which leave binary32 before x^2 does
+                        const float n1 = x1[i][j] * r, n2 = x2[i][j] * r;
+                        z.x = r * (gw1[i][j] - n1 * along);
+                        z.y = r * (gw2[i][j] - n2 * along);
+                        dw1[i][j] += g1[i][j] * n1;
+                        dw2[i][j] += g2[i][j] * n2;
                     } else if constexpr (MODE == kForward) {
                         z = rope_turn(x1[i][j] * (r * w1[i][j]), x2[i][j] * (r * w2[i][j]), cs[i][j]);
                     } else {
