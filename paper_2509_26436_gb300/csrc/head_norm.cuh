@@ -32,15 +32,18 @@ constexpr int kMostHere = 16;  // tokens of a block
 enum NormMode { kRotate, kForward, kBackward };
 
 // CTAs per SM: as many as the registers of a lane's vectors, angles, weights and
-// sums allow.
-template <typename T, int MODE, int E>  // E: pairs a lane
-constexpr int kPerSm = MODE == kRotate ? 4 : MODE == kForward ? (sizeof(T) == 4 ? 2 : 4) : (sizeof(T) * E <= 16 ? 2 : 1);
+// sums allow.  16-bit types forward: four where every lane has pairs alone (4608 x
+// 48 heads of 128: 28.5 us, three 30.5), else three, whose code needs the registers
+// (8192 x 40 heads of 80: 37 us, four 40.5; 4608 x 48 of 128, element by element:
+// 136, 150).
+template <typename T, int MODE, int E, bool FULL>  // E: pairs a lane
+constexpr int kPerSm = MODE == kRotate ? 4 : MODE == kForward ? (sizeof(T) == 4 ? 2 : FULL ? 4 : 3) : (sizeof(T) * E <= 16 ? 2 : 1);
 constexpr int kMostBackward = 2;
 
 // Rows that a lane's copies are ahead, each in memory of its own, so that some
 // 128 KB per SM are on their way; elements one at a time are loaded as needed.
-template <typename T, int MODE, int V>
-constexpr int kAhead = sizeof(T) * V < 8 ? 0 : MODE == kBackward ? 4 : MODE == kForward ? (sizeof(T) == 4 ? 6 : 4) : 5;
+template <typename T, int MODE, int V, bool FULL>
+constexpr int kAhead = sizeof(T) * V < 8 ? 0 : MODE == kBackward ? 4 : MODE == kForward ? (sizeof(T) == 2 && FULL ? 4 : 6) : 5;
 
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Vec {
@@ -89,7 +92,7 @@ struct NormPiece {
 // angles, as its weights, are in registers.  INTER: pairs lie side by side.  FULL:
 // every lane has pairs alone (else a third more instructions, for what is not).
 template <typename T, int V, int NP, int MODE, bool INTER, bool FULL>
-__global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_norm_kernel(HeadNormArgs a, int lanes_log2, int q_here, int k_here)
+__global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP, FULL>) head_norm_kernel(HeadNormArgs a, int lanes_log2, int q_here, int k_here)
 {
     griddep_wait();
     extern __shared__ __align__(16) float s_dyn[];
@@ -169,7 +172,7 @@ __global__ void __launch_bounds__(kNormThreads, kPerSm<T, MODE, V * NP>) head_no
     };
     // The rows' vectors on their way: [stage][vector][thread], read by the lane that
     // copies them alone.  `ahead` is the row that is asked for next.
-    constexpr int S = kAhead<T, MODE, V>, kVecs = (kBack ? 4 : 2) * NP;
+    constexpr int S = kAhead<T, MODE, V, FULL>, kVecs = (kBack ? 4 : 2) * NP;
     Vec<T, V> *s_ring = reinterpret_cast<Vec<T, V> *>(reinterpret_cast<uint8_t *>(s_dyn) + a.ring_at) + threadIdx.x;
     const int rounds = (heads + step - 1) / step;  // as often for every lane of a warp
     const int64_t stride = static_cast<int64_t>(ctas) * here;
@@ -381,7 +384,7 @@ cudaError_t launch_norm_v(HeadNormArgs &a, cudaStream_t s)
 {
     const int pairs = a.rotary / 2, pieces = pairs / V + (a.dim - a.rotary) / V;
     const int heads[2] = {a.side[0].heads, a.side[1].heads};
-    const HeadNormPlan p = head_norm_plan(heads, a.tokens, pieces, pairs, kPerSm<T, MODE, V * NP>);
+    const HeadNormPlan p = head_norm_plan(heads, a.tokens, pieces, pairs, kPerSm<T, MODE, V * NP, FULL>);
     a.ctas[0] = p.ctas[0], a.ctas[1] = p.ctas[1];
     const int width = (1 << p.lanes_log2) * NP * V;
     int bytes = pairs * 8 + ((pairs + 1) & ~1) * 4;
@@ -389,7 +392,7 @@ cudaError_t launch_norm_v(HeadNormArgs &a, cudaStream_t s)
     if (MODE == kBackward && rest < p.groups * a.dim * 4) rest = p.groups * a.dim * 4;
     bytes = (bytes + rest + 15) & ~15;
     static_assert(NP * V * 32 <= 256, "units, angles and sums stay below 37 KB");
-    constexpr int kRing = kAhead<T, MODE, V> * (MODE == kBackward ? 4 : 2) * NP * static_cast<int>(sizeof(T)) * V * kNormThreads;
+    constexpr int kRing = kAhead<T, MODE, V, FULL> * (MODE == kBackward ? 4 : 2) * NP * static_cast<int>(sizeof(T)) * V * kNormThreads;
     a.ring_at = bytes;
     bytes += kRing;
     const cudaError_t e = allow_shared<head_norm_kernel<T, V, NP, MODE, INTER, FULL>>(kRing + 37 * 1024);
