@@ -579,7 +579,8 @@ typedef struct {
  *                aligned, scratch
  * A length or start out of range: that sequence's rows are undefined and
  * QUARTZ_ERR_INDEX is recorded.  seqs <= 65535, tokens <= 2^30, max_len <= 2^30,
- * max_new q_heads / heads <= 2^30. */
+ * max_new q_heads / heads <= 2^30; bounds that allow an SM more than 2^28 tiles of
+ * 128 tokens (minutes of one kernel) are unsupported. */
 size_t quartz_paged_attention_tokens_workspace_size(const quartz_paged_cache_t *cache, int64_t tokens, int64_t seqs,
                                                     int32_t q_heads, int64_t max_len, int64_t max_new);
 int32_t quartz_paged_attention_tokens(const void *q, int64_t q_stride_token, int64_t q_stride_head, int64_t tokens,

@@ -284,6 +284,8 @@ struct PagedTokensCall {
     void *workspace;
     int *dev_err;
 };
+bool paged_tokens_countable(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len,
+                            int64_t max_new);
 size_t paged_tokens_workspace_bytes(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len,
                                     int64_t max_new);
 cudaError_t launch_paged_tokens(const quartz_paged_cache_t *c, const PagedTokensCall &call, cudaStream_t s);

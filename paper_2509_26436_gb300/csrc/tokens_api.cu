@@ -107,7 +107,7 @@ int32_t check_tokens(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs
     if (tokens < 0 || tokens > kMaxTokens || max_len < 0 || max_len > kMaxTokens || max_new < 0 ||
         max_new > kMaxTokens / (q_heads / c->heads))
         return QUARTZ_ERR_INVALID_ARG;
-    return QUARTZ_OK;
+    return paged_tokens_countable(c, tokens, seqs, q_heads, max_len, max_new) ? QUARTZ_OK : QUARTZ_ERR_UNSUPPORTED;
 }
 
 }  // namespace

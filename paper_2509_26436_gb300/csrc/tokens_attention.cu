@@ -50,6 +50,7 @@ __global__ void __launch_bounds__(kJoinThreads) tokens_join_kernel(TokensArgs a,
 struct TokensPlan {
     int tiles, ctas, parts;
     bool uncut;
+    int64_t each;  // tiles of keys a CTA, at most
 };
 
 // Two tiles side by side where a sequence may have more rows than one holds and
@@ -72,14 +73,15 @@ TokensPlan tokens_plan(const quartz_paged_cache_t *c, int64_t tokens, int64_t se
     TokensPlan p;
     p.tiles = c->dim <= 128 && max_new * group > 128 ? 2 : 1;
     p.parts = max_new * group <= 128 || o_type == QUARTZ_OUT_F32 ? 2 : 1;
-    const int64_t most = (tokens * group / (128 * p.tiles) + seqs) * c->heads * (max_len / kTokKeys + 2);
-    const int64_t blocks = (tokens * group / (128 * p.tiles) + seqs) * c->heads;
+    const int64_t blocks = (tokens * group / (128 * p.tiles) + seqs) * c->heads, most = blocks * (max_len / kTokKeys + 2);
     p.uncut = blocks <= device_sms() && max_len <= 8 * kTokKeys;
     if (p.uncut) {
         p.ctas = static_cast<int>(blocks > 0 ? blocks : 1);
+        p.each = max_len / kTokKeys + 2;
         return p;
     }
     p.ctas = static_cast<int>(most < device_sms() ? (most > 0 ? most : 1) : device_sms());
+    p.each = (most + p.ctas - 1) / p.ctas;
     return p;
 }
 
@@ -114,6 +116,12 @@ bool pool_map(CUtensorMap *map, const quartz_paged_cache_t *c, const quartz_page
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 
 }  // namespace
+
+// A CTA counts its tiles, and the up to 8 units of each, in 32 bits.
+bool paged_tokens_countable(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len, int64_t max_new)
+{
+    return tokens_plan(c, tokens, seqs, q_heads, max_len, max_new, QUARTZ_OUT_F16).each <= (int64_t(1) << 28) - 64;
+}
 
 size_t paged_tokens_workspace_bytes(const quartz_paged_cache_t *c, int64_t tokens, int64_t seqs, int q_heads, int64_t max_len,
                                     int64_t max_new)

@@ -138,23 +138,30 @@ template <int R>
 __device__ __forceinline__ int tokens_blocks(const TokensArgs &a, const TokensSeq &s) { return (s.m * a.group + R - 1) / R; }
 
 // Tiles and row blocks of one key head of 32 sequences from b0 on (to b1), each
-// in its lane.
+// in its lane.  Tiles of a sequence pass 32 bits: m tokens of `group` heads have some
+// m^2 group / 2^16 (2^15 where a CTA takes one tile).
+struct TokensCount {
+    long long tiles;
+    int blocks;
+};
+
 template <int R>
-__device__ __forceinline__ int2 tokens_seq_tiles(const TokensArgs &a, int b0, int b1)
+__device__ __forceinline__ TokensCount tokens_seq_tiles(const TokensArgs &a, int b0, int b1)
 {
     const int lane = threadIdx.x & 31;
     TokensSeq s{};
     if (b0 + lane < b1) s = tokens_seq(a, b0 + lane);
-    if (a.single) return s.m > 0 ? make_int2(tokens_tiles<R>(a, s, 0).count, 1) : make_int2(0, 0);
-    int2 mine = make_int2(0, tokens_blocks<R>(a, s));
+    if (a.single) return s.m > 0 ? TokensCount{tokens_tiles<R>(a, s, 0).count, 1} : TokensCount{0, 0};
+    TokensCount mine{0, tokens_blocks<R>(a, s)};
     for (int i = 0; i < min(32, b1 - b0); ++i) {
         TokensSeq t;
         t.n = __shfl_sync(0xffffffffu, s.n, i), t.m = __shfl_sync(0xffffffffu, s.m, i);
         t.pre = __shfl_sync(0xffffffffu, s.pre, i), t.base = t.n - t.m, t.start = 0;
-        int sum = 0;
+        long long sum = 0;
         for (int r = lane; r < tokens_blocks<R>(a, t); r += 32) sum += tokens_tiles<R>(a, t, r).count;
-        sum = __reduce_add_sync(0xffffffffu, sum);
-        if (lane == i) mine.x = sum;
+#pragma unroll
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == i) mine.tiles = sum;
     }
     return mine;
 }
@@ -188,8 +195,8 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
     const int b0 = min(a.seqs, warp * share), b1 = min(a.seqs, b0 + share);
     long long tiles = 0, blocks = 0;
     for (int b = b0; b < b1; b += 32) {
-        const int2 n = tokens_seq_tiles<R>(a, b, b1);
-        long long t = n.x, k = n.y;
+        const TokensCount n = tokens_seq_tiles<R>(a, b, b1);
+        long long t = n.tiles, k = n.blocks;
 #pragma unroll
         for (int d = 16; d; d /= 2) t += __shfl_xor_sync(0xffffffffu, t, d), k += __shfl_xor_sync(0xffffffffu, k, d);
         tiles += t, blocks += k;
@@ -208,8 +215,8 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
     run.end = min(pos + run.chunk, all);
     if (pos < run.end && pos >= before && pos < before + mine_all) {
         for (int b = b0; b < b1; b += 32) {
-            const int2 n2 = tokens_seq_tiles<R>(a, b, b1);
-            const int mine = each * n2.x + run.edge * n2.y;
+            const TokensCount n = tokens_seq_tiles<R>(a, b, b1);
+            const long long mine = each * n.tiles + static_cast<long long>(run.edge) * n.blocks;
             long long incl = mine;
 #pragma unroll
             for (int d = 1; d < 32; d *= 2) {
@@ -222,12 +229,12 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
                 continue;
             }
             const int i = __ffs(behind) - 1;
-            const int per_head = __shfl_sync(0xffffffffu, mine, i);
+            const long long per_head = __shfl_sync(0xffffffffu, mine, i);
             const long long in = pos - before - (__shfl_sync(0xffffffffu, incl, i) - per_head) * a.kv_heads;
             TokensPlace p;
             p.b = b + i;
             p.head = static_cast<int>(in / per_head);
-            int rest = static_cast<int>(in - static_cast<long long>(p.head) * per_head);
+            long long rest = in - p.head * per_head;
             const TokensSeq s = tokens_seq(a, p.b);
             const int blocks = tokens_blocks<R>(a, s);  // of this sequence
             for (int r0 = 0; r0 < blocks; r0 += 32) {
@@ -242,7 +249,7 @@ __device__ bool tokens_find(const TokensArgs &a, TokensFind &f, TokensRun &run)
                 if (here) {
                     const int j = __ffs(here) - 1;
                     p.block = r0 + j;
-                    p.off = rest - __shfl_sync(0xffffffffu, sums - n, j);
+                    p.off = static_cast<int>(rest) - __shfl_sync(0xffffffffu, sums - n, j);
                     break;
                 }
                 rest -= __shfl_sync(0xffffffffu, sums, 31);
