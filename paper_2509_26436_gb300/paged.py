@@ -207,7 +207,7 @@ class PagedCache:
             self.heads, self.dim, self.num_pages = heads, k.K, k.rows // (heads * page_size)
             self.dtype, self.device = f16, k.codes.device
             sides = [N.QuartzPages(None, 0, 0, 0, e.c()) for e in (k, v)]
-            kind = N.PAGES_ENCODED
+            kind, self._pools = N.PAGES_ENCODED, ()
         else:
             for name, t in (("k", k), ("v", v)):
                 if not (t.is_cuda and t.dim() == 4 and t.dtype in (f16, bf16) and t.stride(3) == 1):
@@ -220,7 +220,7 @@ class PagedCache:
             self.num_pages, _, self.heads, self.dim = k.shape
             self.dtype, self.device = k.dtype, k.device
             sides = [N.QuartzPages(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2), N.QuartzEncoded()) for t in (k, v)]
-            kind = N.PAGES_F16 if k.dtype is f16 else N.PAGES_BF16
+            kind, self._pools = N.PAGES_F16 if k.dtype is f16 else N.PAGES_BF16, (k, v)
         self.c = N.QuartzPagedCache(kind, page_size, self.heads, self.dim, self.num_pages, *sides)
         self._ref = _byref(self.c)
         self._index = self.device.index

@@ -28,8 +28,9 @@ _TREE_MOST = 64  # drafted tokens of a sequence: bits of a mask
 
 
 def _no_gradient(name, instead, *tensors):
-    if P.torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise ValueError(f"{name} records no gradient: use torch.no_grad(), or {instead}")
+    for t in tensors:
+        if t is not None and t.requires_grad:
+            raise ValueError(f"{name} records no gradient: use torch.no_grad(), or {instead}")
 
 
 _FUNCTION = "an autograd function whose backward calls "
@@ -60,7 +61,8 @@ def rope_axes(x, positions, freqs, pair_axis, interleaved: bool = False, scale: 
     gradients as in rope()."""
     if P.torch is None:
         P._bind()
-    _no_gradient("rope_axes", _FUNCTION + "rope_axes(..., backward=True)", x, out)
+    if P.torch.is_grad_enabled():
+        _no_gradient("rope_axes", _FUNCTION + "rope_axes(..., backward=True)", x, out, freqs)
     dtype = x.dtype
     kind = P._KIND.get(dtype)
     if kind is None or not x.is_cuda:
@@ -146,7 +148,7 @@ def qk_norm_rope(q, k, wq, wk, positions=None, freqs=None, eps: float = 1e-6, pa
     if P.torch is None:
         P._bind()
     if P.torch.is_grad_enabled():
-        _no_gradient("qk_norm_rope", _FUNCTION + "qk_norm_rope_backward", q, k, wq, wk, *(out or ()))
+        _no_gradient("qk_norm_rope", _FUNCTION + "qk_norm_rope_backward", q, k, wq, wk, freqs, *(out or ()))
     dtype, w_dtype, kind, w_kind = _norm_types(q, wq, wk)
     device = P._device()
     T, Hq, D = q.shape
@@ -172,13 +174,14 @@ def qk_norm_rope_backward(dyq, dyk, q, k, wq, wk, positions=None, freqs=None, ep
     """(dq, dk, dwq, dwk): the gradients of qk_norm_rope's q, k, wq and wk (None
     for what is None) from those of its results (of their types and shapes, any
     strides) and the same arguments.  The weights' gradients are summed in
-    binary32 in the same order on every call.  A workspace of the caller's
+    binary32 in the same order on every call.  Nothing is recorded for autograd,
+    for a second derivative neither (rope()).  A workspace of the caller's
     (qk_norm_rope_workspace_size bytes) is only good for one call at a time, and
     for one captured graph."""
     if P.torch is None:
         P._bind()
     if P.torch.is_grad_enabled():
-        _no_gradient("qk_norm_rope_backward", "detach what it gets", dyq, dyk)
+        _no_gradient("qk_norm_rope_backward", "detach what it gets", dyq, dyk, q, k, wq, wk, freqs)
     dtype, w_dtype, kind, w_kind = _norm_types(q, wq, wk)
     device = P._device()
     T, _, D = q.shape
@@ -250,7 +253,10 @@ def attention_paged_tokens(q, cache: P.PagedCache, block_table, seq_lens, starts
     multiply the values as two parts of the cache's type where a key head has at
     most 128 rows (max_new times its query heads) or the result is float32;
     else rounded to that type.  A workspace of the caller's is only good for one
-    call at a time, and for one captured graph."""
+    call at a time, and for one captured graph.  Nothing is recorded for autograd
+    (rope())."""
+    if P.torch.is_grad_enabled():
+        _no_gradient("attention_paged_tokens", "detach what it gets", q, slopes, out, *cache._pools)
     device = cache._check_device()
     qs = P._rows("q", q, 3, cache.dtype, device)
     ts = P._rows("block_table", block_table, 2, P.i32, device)
