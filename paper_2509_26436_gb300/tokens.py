@@ -173,7 +173,7 @@ def qk_norm_rope_backward(dyq, dyk, q, k, wq, wk, positions=None, freqs=None, ep
                           interleaved: bool = False, scale: float = 1.0, workspace=None, stream=None):
     """(dq, dk, dwq, dwk): the gradients of qk_norm_rope's q, k, wq and wk (None
     for what is None) from those of its results (of their types and shapes, any
-    strides) and the same arguments.  The weights' gradients are summed in
+    strides with a contiguous last dimension) and the same arguments.  The weights' gradients are summed in
     binary32 in the same order on every call.  Nothing is recorded for autograd,
     for a second derivative neither (rope()).  A workspace of the caller's
     (qk_norm_rope_workspace_size bytes) is only good for one call at a time, and

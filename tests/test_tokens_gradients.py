@@ -66,7 +66,8 @@ def test_on_the_device(Q):
 
         @staticmethod
         def backward(ctx, g):
-            dq, _, dw, _ = Q.qk_norm_rope_backward(g, None, ctx.saved_tensors[0], None, ctx.saved_tensors[1], None)
+            # (a sum's gradient is broadcast, which is refused as any last dimension that is not contiguous)
+            dq, _, dw, _ = Q.qk_norm_rope_backward(g.contiguous(), None, ctx.saved_tensors[0], None, ctx.saved_tensors[1], None)
             return dq, dw
 
     q, w = torch.randn(5, 2, 64, device="cuda", requires_grad=True), torch.ones(64, device="cuda", requires_grad=True)
