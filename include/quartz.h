@@ -532,8 +532,8 @@ int32_t quartz_paged_attention(const void *q, int64_t q_stride_seq, int64_t q_st
  * the last of their sequence, and in the cache (quartz_paged_append): new token
  * j of sequence b is row starts[b] + j of q and o, and token base + j of the
  * cache, base = seq_lens[b] - (starts[b + 1] - starts[b]).  Its position is
- * base + j; in a tree base + its depth, the drafted tokens it sees but itself,
- * and a drafted token's place is its position (of any other token: its index).
+ * base + j; in a tree base + its depth, the number of other drafted tokens that
+ * it sees (its own bit counts for nothing here), and a drafted token's place is its position (of any other token: its index).
  *   s_t = scale * q . k_t
  *   s_t = cap tanh(s_t / cap)                     with cap > 0
  *   s_t = s_t - slopes[h] |position - place_t|    with slopes

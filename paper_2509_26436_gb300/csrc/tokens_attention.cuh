@@ -395,7 +395,8 @@ struct TokensRow {
         if (own && d > -32 && d < 64) v |= static_cast<uint32_t>(d >= 0 ? own >> d : own << -d);
         return v;
     }
-    __device__ __forceinline__ int depth(int i) const { return max(0, __popcll(tree[i] & some) - 1); }
+    // The others that drafted token i sees, whether it sees itself or not.
+    __device__ __forceinline__ int depth(int i) const { return __popcll(tree[i] & some & ~(1ull << i)); }
     __device__ __forceinline__ int place(int t) const
     {
         return tree && t >= base && t - base < 64 && (some >> (t - base) & 1) ? base + depth(t - base) : t;

@@ -241,8 +241,8 @@ def attention_paged_tokens(q, cache: P.PagedCache, block_table, seq_lens, starts
     less than `window` before it; and the first prefix_lens[b] tokens whatever
     their position (int32 [seqs]).  `tree` int64 [tokens]: bit i of a row says
     that it sees its sequence's drafted token i (itself too, by its own bit),
-    besides the tokens before them all; the position is then that of the last
-    of those plus the number of drafted tokens seen, itself included.  Scores:
+    besides the tokens before them all; the position is then that of the first
+    drafted token plus the number of other drafted tokens that it sees.  Scores:
     scale q . k; cap > 0: cap tanh(score / cap); slopes float32 [q_heads]: less
     slopes[h] times the distance of the positions.  A token that sees nothing
     gives zeros.
