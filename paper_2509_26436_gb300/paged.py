@@ -39,10 +39,23 @@ def _bind():
     f16, bf16, f32, f64, i32, i64 = t.float16, t.bfloat16, t.float32, t.float64, t.int32, t.int64
     _KIND.update({f16: N.OUT_F16, bf16: N.OUT_BF16, f32: N.OUT_F32})
     _device = getattr(t._C, "_cuda_getDevice", None) or t.cuda.current_device
-    # memory of the current device; half of what torch.empty costs the host (1.6 us for 3.4)
-    _empty_strided = getattr(getattr(getattr(t._C, "_dynamo", None), "guards", None), "_empty_strided_cuda", None)
+    _empty_strided = _quick_empty(t)
     lib = N.load()
     torch = t
+
+
+def _quick_empty(t):
+    """torch's own short way to memory of the current device, for half of what
+    torch.empty costs the host (1.6 us for 3.4); None where it is not there or
+    is not what it was."""
+    try:
+        f = t._C._dynamo.guards._empty_strided_cuda
+        x = f((2, 3, 4), (12, 4, 1), t.float16)
+        if x.shape == (2, 3, 4) and x.stride() == (12, 4, 1) and x.dtype is t.float16 and x.get_device() == _device():
+            return f
+    except Exception:  # whatever another version makes of it: torch.empty serves
+        pass
+    return None
 
 
 def _refuse(name, x, dim, kind, last=True):
@@ -74,7 +87,8 @@ def _empty(shape, dtype, device, stream):
     that the call runs on: memory of another one could still be in use there, or
     be given away too early."""
     if stream is None:
-        if _empty_strided is not None:
+        # (memory that torch is to fill, so that results repeat, it fills in torch.empty)
+        if _empty_strided is not None and not torch.are_deterministic_algorithms_enabled():
             if len(shape) == 3:
                 return _empty_strided(shape, (shape[1] * shape[2], shape[2], 1), dtype)
             if len(shape) == 1:
