@@ -56,8 +56,12 @@ struct TokensPlan {
 // Two tiles side by side where a sequence may have more rows than one holds and
 // TMEM has room for them; a CTA per SM, as long as there may be so many tiles of
 // keys.  Blocks that all have an SM, of 8 tiles of keys at most, stay whole: the
-// join, and its workspace, cost more than they take from a CTA (8 drafted tokens,
-// 40 heads, 777 cached: 11.2 us a call, cut 17.8).
+// join, and its workspace, cost the host some 5 us and the GPU about what they take
+// from a CTA.  Tiles of encoded pages and of wider heads take twice as long: 4 of
+// them, unless blocks fill half the SMs.  Whole and cut, us a call (8 new tokens,
+// 1 to 40 heads of 128, bf16): 256 keys 13 and 18, 777 18.6 and 17.6 to 21, 1024 19.2
+// and 18.6 to 20; heads of 256: 512 18.5 and 18.3, 1024 29 and 20 to 25; encoded: 512
+// 18.3 and 16.7, 1024 28 and 17.4 to 24; 128 blocks 29 and 34.
 //
 // Weights enter the value product in two parts, so that only the result's rounding
 // is left of the error (relative to 64 bits, bf16 pages and results: 0.0016; in one
@@ -74,7 +78,8 @@ TokensPlan tokens_plan(const quartz_paged_cache_t *c, int64_t tokens, int64_t se
     p.tiles = c->dim <= 128 && max_new * group > 128 ? 2 : 1;
     p.parts = max_new * group <= 128 || o_type == QUARTZ_OUT_F32 ? 2 : 1;
     const int64_t blocks = (tokens * group / (128 * p.tiles) + seqs) * c->heads, most = blocks * (max_len / kTokKeys + 2);
-    p.uncut = blocks <= device_sms() && max_len <= 8 * kTokKeys;
+    const bool dear = (c->type == QUARTZ_PAGES_ENCODED || c->dim > 128) && blocks <= device_sms() / 2;
+    p.uncut = blocks <= device_sms() && max_len <= (dear ? 4 : 8) * kTokKeys;
     if (p.uncut) {
         p.ctas = static_cast<int>(blocks > 0 ? blocks : 1);
         p.each = max_len / kTokKeys + 2;
