@@ -484,6 +484,13 @@ __device__ __forceinline__ void tmem_ld_row(uint32_t t0, uint32_t (&r)[64])
         : "r"(t0)
         : "memory");
 }
+__device__ __forceinline__ void tmem_st_row(uint32_t t0, const uint32_t (&r)[8])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(t0),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+        : "memory");
+}
 __device__ __forceinline__ void tmem_st_row(uint32_t t0, const uint32_t (&r)[16])
 {
     asm volatile(

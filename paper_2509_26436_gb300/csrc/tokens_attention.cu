@@ -66,7 +66,9 @@ struct TokensPlan {
 // Weights enter the value product in two parts, so that only the result's rounding
 // is left of the error (relative to 64 bits, bf16 pages and results: 0.0016; in one
 // part 0.0021).  Few rows are bound by the pages, not by products (16 trees of 16
-// over up to 8192: 65.4 us, in one part 63.1).  Sequences with more rows than a tile
+// over up to 8192: 65.4 us, in one part 63.1), with a cap or distances by the softmax
+// as well (16 x 16 tokens over 8192, fp16: 104 us, 101; a cap 136, 117; distances 160,
+// 121), where one rule for all few rows was kept.  Sequences with more rows than a tile
 // are bound by products and the softmax (8192 causal tokens: 513 us, in one part
 // 400; trees of 61 over up to 65536 encoded tokens 280, 211; heads of 256 in a
 // window 164, 144): one part, unless the result is binary32.

@@ -34,15 +34,19 @@
 // instruction, 1024 of each scheduler; in long runs an iteration takes some 2700
 // (1024 tokens over 65536, 32 / 8 heads, bf16: 735-753 us, 1450-1480 TFLOP/s of
 // 1950), the rest waits between product, softmax and product.  Causal prompts of
-// 8192: 380-400 us, their ends of blocks on top.  Steps on the latter (us): 637 with
+// 8192: 380-400 us, their ends of blocks among it, and the join 15 (a call 400-425,
+// 1320 TFLOP/s).  Steps on the kernel (us): 637 with
 // 16-byte copies and scores read twice; 556 by TMA; 474 with queries by TMA and
 // instances without what plain scores do not need (code for it in the same loop:
 // 556, a quarter of the active time waiting for instructions); 457 with results
 // through shared memory; 379 with blocks' ends counted in the cut.  Heads of 256
 // (128 KB of keys and values for 128 rows): 749 us for 1024 tokens over 32768 with
 // whole units in the order keys, values; 516 in the order of the products.
-// Encoded pages are bound by decoding: 100 instructions for 32 elements of a row,
-// in four warps 255 us where eight take 217 (trees of 61 over up to 65536).
+// Encoded pages wait for what is decoded: 100 instructions for 32 elements of a row
+// (in four warps 255 us where eight take 217, trees of 61 over up to 65536), but issue
+// slots are half busy only; codes on their way, a unit ahead, are waited for most.
+// Every instance spills, 260 to 510 bytes of stores a thread: some 0.6% of the
+// instructions that run.
 #pragma once
 
 #include <cuda.h>
@@ -354,7 +358,8 @@ struct TokensShared {
 static_assert(sizeof(TokensShared) <= 3 * 1024, "");
 
 // tanh of u, |u| <= 1, good to 3 half steps of binary32: an odd polynomial fitted
-// to the least largest relative error (5e-8); above, 1 - 2 / (1 + e^2|u|).
+// to the least largest relative error (6.7e-8 with these coefficients, before it is
+// evaluated); above, 1 - 2 / (1 + e^2|u|).
 __device__ __forceinline__ constexpr float tokens_tanh_term(int i)
 {
     constexpr float c[7] = {0.99999994f, -0.3333284f, 0.13325204f, -0.05345702f, 0.020289967f, -0.006203367f, 0.0010410185f};
@@ -1137,6 +1142,10 @@ struct TokensKernel {
                         tmem_st_row(o_at + c, o);
                     }
                 }
+                // Pairs at a time: shaped scores in two parts run out of registers with 16 (900
+                // bytes of spills; 512 new tokens over 4096 encoded ones, a cap: 189 us, 8: 149).
+                // Plain ones do not (110, 8: 117).
+                constexpr int kPairs = PARTS == 2 && SHAPED ? 8 : 16;
                 uint64_t sum[2] = {0, 0};
                 // Weights; `exponent` gives those of a pair, column x of the 64 from c on
                 auto weigh = [&](auto exponent) {
@@ -1145,10 +1154,10 @@ struct TokensKernel {
                         if (c) tmem_ld_row(s_at + c, s);
                         const auto of = exponent(c);
 #pragma unroll
-                        for (int y = 0; y < 64; y += 32) {
-                            uint32_t p[16], second[PARTS == 1 ? 1 : 16];
+                        for (int y = 0; y < 64; y += 2 * kPairs) {
+                            uint32_t p[kPairs], second[PARTS == 1 ? 1 : kPairs];
 #pragma unroll
-                            for (int x = 0; x < 16; ++x) {
+                            for (int x = 0; x < kPairs; ++x) {
                                 float2 e = unpack2(of(pack2(__uint_as_float(s[y + 2 * x]), __uint_as_float(s[y + 2 * x + 1])), y + 2 * x));
                                 e.x = ex2(e.x), e.y = ex2(e.y);
                                 sum[x & 1] = add2(sum[x & 1], pack2(e.x, e.y));
@@ -1162,7 +1171,8 @@ struct TokensKernel {
                 };
                 const uint64_t shift = pack2(kUp - m, kUp - m);
                 if (near) {
-                    // cap tanh(s / cap) by an odd polynomial, good to 9 half steps up to cap / 2
+                    // cap tanh(s / cap) by an odd polynomial, good to 11 half steps up to cap / 2
+                    // (9.3 before it is evaluated)
                     const float by = a.cap_log2 * a.to_cap, q = a.to_cap * a.to_cap;
                     const uint64_t c0 = pack2(0.99999946f * by, 0.99999946f * by), c1 = pack2(-0.3332632f * by * q, -0.3332632f * by * q),
                                    c2 = pack2(0.13190296f * by * q * q, 0.13190296f * by * q * q),
